@@ -479,6 +479,127 @@ int patch_soft_mask_backward(const void* W_dev, int64_t ldw, const float* P_tile
                              uint64_t seed, int flags, const void* Gw_dev, int64_t ldg, double c1, double c2,
                              float* gP_tile_dev, float* gP24_dev, void* stream);
 
+/* =========================================================================================
+ * Between the linear layers: what a decoder does with the q/k/v projection before the o projection.
+ * Queries, keys and values are rows of heads: head h of token m starts at element m * ld + h * D, so the
+ * column ranges of one stacked q/k/v projection are passed as they are (pointer to the range, ld = the stack's pitch).
+ * Everything is bf16; arithmetic is fp32 with one rounding at the end.  The launches are ordinary ones as far as
+ * the GEMMs' overlap window goes: they start when everything before them on the stream has completed, and they have
+ * completed when the next kernel starts.
+ * ========================================================================================= */
+
+/*
+ * Rotation of a head's first rotary_dim elements by its token's position p.  With the table's row p holding
+ * c_0 .. c_{R/2-1}, s_0 .. s_{R/2-1} (cosines, then sines, fp32; R = rotary_dim), the pair
+ *     (a, b) = (x_i, x_{i+R/2})  (interleaved = 0)   or   (x_{2i}, x_{2i+1})  (interleaved = 1)
+ * becomes (a c_i - b s_i, b c_i + a s_i); elements from rotary_dim on are left as they are.
+ *   rotary_dim  0 (no rotation; cos_sin_dev and positions may be NULL), or a multiple of 16 (interleaved: of 8), at most D
+ */
+typedef struct patch_rope_t {
+    const float* cos_sin_dev;   /* [max_positions x rotary_dim], 16-byte aligned */
+    int64_t max_positions;
+    int32_t rotary_dim;
+    int32_t interleaved;
+} patch_rope_t;
+
+/*
+ * A paged cache of keys and values: slot s of head h in page p is D elements from
+ *     k_dev + p * page_stride + (h * page_size + s) * D          (v_dev alike),
+ * so a page holds, head by head, page_size rows of D.  Keys and values may share one buffer (page_stride counts the
+ * elements from one page of keys to the next).
+ *   page_size  a power of two, 16 .. 256;  page_stride >= Hkv * page_size * D, a multiple of 8;  D a multiple of 8, <= 256
+ * "Slot number" below means p * page_size + s.
+ */
+typedef struct patch_kv_cache_t {
+    void* k_dev;
+    void* v_dev;
+    int64_t num_pages;
+    int64_t page_stride;
+    int32_t page_size;
+    int32_t Hkv;
+    int32_t D;
+    int32_t reserved;           /* 0 */
+} patch_kv_cache_t;
+
+/*
+ * Norms of queries and keys for each head and the rotation, in one pass over them:
+ *     y = R(p) n(x),   n(x) = x / sqrt(mean(x^2) + eps) * w  (the mean over the head's D elements),  n(x) = x where w is NULL.
+ *   Q_dev  [M x Hq heads], pitch ldq;  K_dev [M x Hkv heads], pitch ldk;  either may be NULL with its head count 0
+ *   wq_dev / wk_dev  bf16 [D], 16-byte aligned, or NULL (rotation only), each by itself
+ *   rope   NULL = no rotation;  positions_dev  int32 [M]
+ *   Qo_dev / Ko_dev  results, pitches ldqo / ldko; may be Q_dev / K_dev themselves with the same pitch (in place)
+ *   status_dev  optional device int (zero before the call): PATCH_ERR_SIZE if a position lies outside the table (it
+ *               is then taken as 0)
+ * D is a multiple of 8, 8 <= D <= 256; M == 0 returns PATCH_OK without launching.  One kernel.
+ */
+int patch_qk_norm_rope(const void* Q_dev, int64_t ldq, int Hq, const void* K_dev, int64_t ldk, int Hkv, int64_t M, int D,
+                       const void* wq_dev, const void* wk_dev, float eps, const patch_rope_t* rope,
+                       const int32_t* positions_dev, void* Qo_dev, int64_t ldqo, void* Ko_dev, int64_t ldko,
+                       int* status_dev, void* stream);
+
+/*
+ * Gradient of patch_qk_norm_rope.  With g = R(p)^T gy, r = 1 / sqrt(mean(x^2) + eps), xh = x r:
+ *     gx = r (g w - xh mean(g w xh)),   gw = sum over tokens and heads of g xh        (gx = g where w is NULL)
+ *   gQo_dev / gKo_dev  gradients of the results;  Q_dev / K_dev  the inputs of the forward call (NULL where the weight is)
+ *   gQ_dev / gK_dev    gradients of the inputs; may be gQo_dev / gKo_dev themselves with the same pitch
+ *   gwq_dev / gwk_dev  fp32 [D], written (not accumulated into); required where the weight is given
+ *   workspace_dev      at least patch_qk_norm_rope_backward_workspace_size bytes, 256-byte aligned, no initialisation
+ *                      needed (0 bytes where no weight is given)
+ * Sums of gw are taken in an order that depends on the arguments only: equal calls give equal bits.  One kernel for the
+ * gradients of the inputs and one that adds up the weight's partial sums.
+ */
+int patch_qk_norm_rope_backward_workspace_size(int64_t M, int Hq, int Hkv, int D, size_t* bytes_out);
+int patch_qk_norm_rope_backward(const void* gQo_dev, int64_t ldgqo, const void* gKo_dev, int64_t ldgko,
+                                const void* Q_dev, int64_t ldq, int Hq, const void* K_dev, int64_t ldk, int Hkv,
+                                int64_t M, int D, const void* wq_dev, const void* wk_dev, float eps,
+                                const patch_rope_t* rope, const int32_t* positions_dev, void* gQ_dev, int64_t ldgq,
+                                void* gK_dev, int64_t ldgk, float* gwq_dev, float* gwk_dev, void* workspace_dev,
+                                size_t workspace_bytes, int* status_dev, void* stream);
+
+/*
+ * Keys and values of M tokens into their slots of a paged cache, the keys normed and rotated on the way as by
+ * patch_qk_norm_rope; with Q_dev also the tokens' queries (into Qo_dev), so that one launch lies between a step's q/k/v
+ * projection and its attention.  Serves a decode step (one token of each sequence) and a prompt alike.
+ *   K_dev, V_dev  [M x Hkv heads of D] (the cache's), pitches ldk, ldv
+ *   slots_dev     int64 [M], the slot number of each token; negative: the token's key and value are not stored (padding).
+ *                 Two tokens with one slot leave either's row there.
+ *   Q_dev         NULL (Hq = 0), or [M x Hq heads of D];  Qo_dev as in patch_qk_norm_rope
+ *   status_dev    PATCH_ERR_SIZE for a position outside the table (taken as 0) or a slot outside the cache (not stored)
+ * One kernel.
+ */
+int patch_kv_append(const patch_kv_cache_t* cache, const void* K_dev, int64_t ldk, const void* V_dev, int64_t ldv,
+                    const int64_t* slots_dev, int64_t M, const void* wk_dev, float eps, const patch_rope_t* rope,
+                    const int32_t* positions_dev, const void* Q_dev, int64_t ldq, int Hq, const void* wq_dev,
+                    void* Qo_dev, int64_t ldqo, int* status_dev, void* stream);
+
+/*
+ * Attention of a batch whose sequences share a prefix, over a paged cache.  Sequence b has T query tokens (1: decoding;
+ * more: drafted tokens scored at once), rows b T .. b T + T - 1 of Q; its keys are the prefix_len keys of the shared prefix
+ * followed by suffix_lens[b] keys of its own, the last T of which belong to the query tokens themselves:
+ *     query token t sees the whole prefix and the first max(0, suffix_lens[b] - (T - 1 - t)) of the own keys;
+ *     O = softmax(scale q k^T) v over what it sees,  lse = ln sum exp(scale q k^T);  nothing seen: O = 0, lse = -inf.
+ * Query head h reads key head h / (Hq / Hkv).  The prefix is read once for all sequences (the batch's rows of one key
+ * head are one operand), and no key or value past a length is used, whatever the cache holds there; keys and values that some query token of a
+ * sequence sees are assumed finite.
+ *   cache             D = 64 or 128
+ *   Q_dev, O_dev      [B T x Hq heads of D], pitches ldq, ldo;  Hq a multiple of the cache's Hkv
+ *   prefix_pages_dev  int32 [ceil(prefix_len / page_size)] pages of the prefix, in order (NULL if prefix_len is 0)
+ *   page_table_dev    int32 [B x ld_table]: row b lists the pages of sequence b's own keys, which start at slot 0 of the first
+ *                     (entries past its length are not used)
+ *   suffix_lens_dev   int32 [B], 0 <= length <= ld_table * page_size, in device memory: a captured launch follows the lengths
+ *   lse_dev           NULL or fp32 [B T x Hq]
+ *   workspace_dev     at least patch_prefix_attention_workspace_size bytes (it depends on neither lengths nor prefix), 256-byte
+ *                     aligned, no initialisation needed
+ *   status_dev        PATCH_ERR_SIZE: a length outside its range (clamped); PATCH_ERR_FORMAT: a page outside the cache (page 0
+ *                     is read in its place); PATCH_ERR_TIMEOUT: a bounded wait expired.  O is undefined in the last two.
+ * B <= 2048, B T Hq D < 2^31, scale > 0.  Fixed lengths give fixed bits.  At most three launches, no host synchronisation.
+ */
+int patch_prefix_attention_workspace_size(const patch_kv_cache_t* cache, int64_t B, int T, int Hq, size_t* bytes_out);
+int patch_prefix_attention(const patch_kv_cache_t* cache, const void* Q_dev, int64_t ldq, int64_t B, int T, int Hq,
+                           const int32_t* prefix_pages_dev, int64_t prefix_len, const int32_t* page_table_dev,
+                           int64_t ld_table, const int32_t* suffix_lens_dev, float scale, void* O_dev, int64_t ldo,
+                           float* lse_dev, void* workspace_dev, size_t workspace_bytes, int* status_dev, void* stream);
+
 /* Human-readable text for a status code (static storage). */
 const char* patch_strerror(int status);
 

@@ -29,6 +29,8 @@ EXPORTS = ["patch_packed_size", "patch_pack", "patch_unpack", "patch_gemm_worksp
            "patch_gemm_noalloc",
            "patch_hard_mask", "patch_pack_patterns", "patch_pack_dev", "patch_read_layout", "patch_soft_mask_workspace_size", "patch_soft_mask",
            "patch_mask_regularizers", "patch_mask_regularizer_coefficients", "patch_soft_mask_backward",
+           "patch_qk_norm_rope", "patch_qk_norm_rope_backward_workspace_size", "patch_qk_norm_rope_backward",
+           "patch_kv_append", "patch_prefix_attention_workspace_size", "patch_prefix_attention",
            "patch_strerror", "patch_version"]
 MASK_NO_NOISE = 1
 
@@ -42,6 +44,19 @@ class Layout(ctypes.Structure):
                 ("table_off", ctypes.c_uint64), ("payload_off", ctypes.c_uint64),
                 ("payload_bytes", ctypes.c_uint64), ("total_bytes", ctypes.c_uint64),
                 ("n_dense_q4", ctypes.c_int64), ("n_sparse_q4", ctypes.c_int64)]
+
+
+class Rope(ctypes.Structure):
+    """Mirror of ``patch_rope_t``; keeps its table alive."""
+    _fields_ = [("cos_sin_dev", ctypes.c_void_p), ("max_positions", ctypes.c_int64), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
+class KVCache(ctypes.Structure):
+    """Mirror of ``patch_kv_cache_t``; keeps its page buffers alive."""
+    _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p), ("num_pages", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("page_size", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class PatchError(RuntimeError):
@@ -90,6 +105,14 @@ def load(path: str) -> ctypes.CDLL:
                                                ctypes.c_double, vp, vp, vp]
         L.patch_pack_dev.argtypes = [vp, i64, vp, vp, i64, i64, ctypes.c_int, ctypes.c_int, vp, sz, vp, vp]
         L.patch_read_layout.argtypes = [vp, ctypes.POINTER(Layout), vp]
+        i32, f32, rp, cp = ctypes.c_int, ctypes.c_float, ctypes.POINTER(Rope), ctypes.POINTER(KVCache)
+        L.patch_qk_norm_rope.argtypes = [vp, i64, i32, vp, i64, i32, i64, i32, vp, vp, f32, rp, vp, vp, i64, vp, i64, vp, vp]
+        L.patch_qk_norm_rope_backward_workspace_size.argtypes = [i64, i32, i32, i32, ctypes.POINTER(sz)]
+        L.patch_qk_norm_rope_backward.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, i64, i32, i64, i32, vp, vp, f32, rp, vp,
+                                                  vp, i64, vp, i64, vp, vp, vp, sz, vp, vp]
+        L.patch_kv_append.argtypes = [cp, vp, i64, vp, i64, vp, i64, vp, f32, rp, vp, vp, i64, i32, vp, vp, i64, vp, vp]
+        L.patch_prefix_attention_workspace_size.argtypes = [cp, i64, i32, i32, ctypes.POINTER(sz)]
+        L.patch_prefix_attention.argtypes = [cp, vp, i64, i64, i32, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, vp, sz, vp, vp]
         L.patch_strerror.argtypes = [ctypes.c_int]
         L.patch_strerror.restype = ctypes.c_char_p
         for name in EXPORTS:
@@ -404,3 +427,163 @@ def patch_read_layout(packed, stream=None) -> Layout:
     L = Layout()
     _check(lib().patch_read_layout(_ptr(packed), ctypes.byref(L), _stream(stream)), "patch_read_layout")
     return L
+
+
+# ---------------------------------------------------------------------------------------------
+# Between the linear layers: norms and rotation of queries and keys, the paged cache, attention behind a shared prefix.
+
+
+def _heads(x, D: int | None = None):
+    """Rows of heads [M x H x D], bf16, heads side by side, any row pitch: (pointer, pitch, H)."""
+    import torch
+    if x is None:
+        return None, 0, 0
+    assert x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 3, "heads are bf16 CUDA tensors [M, H, D]"
+    M, H, d = x.shape
+    sm, sh, sd = x.stride()
+    assert (sd == 1 or d == 1) and (sh == d or H == 1) and (D is None or d == D), "a row holds its heads side by side"
+    return x.data_ptr(), sm if M > 1 else H * d, H
+
+
+def _vec(x, dtype, n: int):
+    if x is None:
+        return None
+    assert x.is_cuda and x.dtype == dtype and x.is_contiguous() and x.numel() == n, f"expected {n} contiguous {dtype} values on the GPU"
+    return x.data_ptr()
+
+
+def patch_rope(cos_sin, interleaved: bool = False) -> Rope:
+    """Rotation by a table float32 [max_positions, rotary_dim]: a position's cosines, then its sines."""
+    import torch
+    assert cos_sin.is_cuda and cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.is_contiguous()
+    r = Rope(cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], 1 if interleaved else 0)
+    r.table = cos_sin
+    return r
+
+
+def patch_kv_cache(k, v) -> KVCache:
+    """Paged cache over bf16 page buffers [num_pages, Hkv, page_size, D]; the two may be views of one buffer."""
+    import torch
+    assert k.is_cuda and v.is_cuda and k.dtype == v.dtype == torch.bfloat16 and k.dim() == 4
+    assert k.shape == v.shape and k.stride() == v.stride(), "keys and values have the same shape and strides"
+    pages, H, page, D = k.shape
+    assert k.stride()[1:] == (page * D, D, 1), "a page holds [Hkv, page_size, D] without gaps"
+    c = KVCache(k.data_ptr(), v.data_ptr(), pages, max(k.stride(0), H * page * D) if pages == 1 else k.stride(0), page, H, D, 0)
+    c.buffers = (k, v)
+    return c
+
+
+def patch_qk_norm_rope(Q, K, rope: Rope | None, positions, wq=None, wk=None, eps: float = 1e-6, Q_out=None, K_out=None,
+                       status=None, stream=None):
+    """Norms of queries [M, Hq, D] and keys [M, Hkv, D] (either may be None) and the rotation: returns (Q_out, K_out)."""
+    import torch
+    M, _, D = (Q if Q is not None else K).shape
+    if Q_out is None and Q is not None:
+        Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if K_out is None and K is not None:
+        K_out = torch.empty(K.shape, dtype=K.dtype, device=K.device)
+    q, ldq, Hq = _heads(Q, D)
+    k, ldk, Hkv = _heads(K, D)
+    qo, ldqo, Hqo = _heads(Q_out if Q is not None else None, D)
+    ko, ldko, Hko = _heads(K_out if K is not None else None, D)
+    assert Hqo == Hq and Hko == Hkv and all(x is None or x.shape[0] == M for x in (Q, K, Q_out, K_out))
+    _check(lib().patch_qk_norm_rope(q, ldq, Hq, k, ldk, Hkv, M, D, _vec(wq, torch.bfloat16, D), _vec(wk, torch.bfloat16, D), eps,
+                                    rope, _vec(positions, torch.int32, M), qo, ldqo, ko, ldko, _ptr(status), _stream(stream)),
+           "patch_qk_norm_rope")
+    return Q_out, K_out
+
+
+def patch_qk_norm_rope_backward_workspace_size(M: int, Hq: int, Hkv: int, D: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().patch_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D, ctypes.byref(n)),
+           "patch_qk_norm_rope_backward_workspace_size")
+    return int(n.value)
+
+
+def patch_qk_norm_rope_backward(gQ_out, gK_out, rope: Rope | None, positions, Q=None, K=None, wq=None, wk=None, eps: float = 1e-6,
+                                gQ=None, gK=None, gwq=None, gwk=None, workspace=None, status=None, stream=None):
+    """Gradient of ``patch_qk_norm_rope``: returns (gQ, gK, gwq, gwk); the inputs Q, K are needed where a weight is given."""
+    import torch
+    some = gQ_out if gQ_out is not None else gK_out
+    M, _, D = some.shape
+    if gQ is None and gQ_out is not None:
+        gQ = torch.empty(gQ_out.shape, dtype=gQ_out.dtype, device=some.device)
+    if gK is None and gK_out is not None:
+        gK = torch.empty(gK_out.shape, dtype=gK_out.dtype, device=some.device)
+    if gwq is None and wq is not None:
+        gwq = torch.empty(D, dtype=torch.float32, device=some.device)
+    if gwk is None and wk is not None:
+        gwk = torch.empty(D, dtype=torch.float32, device=some.device)
+    gqo, ldgqo, Hq = _heads(gQ_out, D)
+    gko, ldgko, Hkv = _heads(gK_out, D)
+    if workspace is None and (wq is not None or wk is not None):
+        workspace = torch.empty(patch_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D), dtype=torch.uint8, device=some.device)
+    q, ldq, hq = _heads(Q if wq is not None else None, D)
+    k, ldk, hk = _heads(K if wk is not None else None, D)
+    gq, ldgq, h1 = _heads(gQ if gQ_out is not None else None, D)
+    gk, ldgk, h2 = _heads(gK if gK_out is not None else None, D)
+    assert hq in (0, Hq) and hk in (0, Hkv) and h1 == Hq and h2 == Hkv
+    assert all(x is None or x.shape[0] == M for x in (gQ_out, gK_out, Q, K, gQ, gK))
+    _check(lib().patch_qk_norm_rope_backward(gqo, ldgqo, gko, ldgko, q, ldq, Hq, k, ldk, Hkv, M, D, _vec(wq, torch.bfloat16, D),
+                                             _vec(wk, torch.bfloat16, D), eps, rope, _vec(positions, torch.int32, M), gq, ldgq, gk,
+                                             ldgk, _vec(gwq, torch.float32, D), _vec(gwk, torch.float32, D), _ptr(workspace),
+                                             workspace.numel() if workspace is not None else 0, _ptr(status), _stream(stream)),
+           "patch_qk_norm_rope_backward")
+    return gQ, gK, gwq, gwk
+
+
+def patch_kv_append(cache: KVCache, K, V, slots, rope: Rope | None = None, positions=None, wk=None, eps: float = 1e-6, Q=None,
+                    wq=None, Q_out=None, status=None, stream=None):
+    """Keys (normed and rotated) and values [M, Hkv, D] into the cache's slots (int64 [M]; negative: not stored); with Q
+    [M, Hq, D] also the queries, normed and rotated: returns Q_out (None without Q)."""
+    import torch
+    M, D = K.shape[0], cache.D
+    if Q_out is None and Q is not None:
+        Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    k, ldk, Hk = _heads(K, D)
+    v, ldv, Hv = _heads(V, D)
+    q, ldq, Hq = _heads(Q, D)
+    qo, ldqo, Hqo = _heads(Q_out if Q is not None else None, D)
+    assert Hk == Hv == cache.Hkv and Hqo == Hq and all(x is None or x.shape[0] == M for x in (V, Q, Q_out))
+    _check(lib().patch_kv_append(cache, k, ldk, v, ldv, _vec(slots, torch.int64, M), M, _vec(wk, torch.bfloat16, D), eps, rope,
+                                 _vec(positions, torch.int32, M), q, ldq, Hq, _vec(wq, torch.bfloat16, D), qo, ldqo, _ptr(status),
+                                 _stream(stream)), "patch_kv_append")
+    return Q_out
+
+
+def patch_prefix_attention_workspace_size(cache: KVCache, B: int, T: int, Hq: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().patch_prefix_attention_workspace_size(cache, B, T, Hq, ctypes.byref(n)), "patch_prefix_attention_workspace_size")
+    return int(n.value)
+
+
+def patch_prefix_attention(cache: KVCache, Q, prefix_pages, prefix_len: int, page_table, suffix_lens, scale: float | None = None,
+                           O=None, lse=None, workspace=None, status=None, stream=None):
+    """Attention of Q [B T, Hq, D] over the shared prefix (int32 ``prefix_pages``, ``prefix_len`` keys) and each sequence's own
+    keys (int32 ``page_table`` [B, n], int32 ``suffix_lens`` [B]): returns O; ``lse`` float32 [B T, Hq] is written if given.
+    ``scale`` defaults to 1 / sqrt(D)."""
+    import torch
+    B = suffix_lens.numel()
+    rows, Hq, D = Q.shape
+    T = rows // B if B else 1
+    assert D == cache.D and rows == B * T and (B == 0 or T > 0)
+    assert prefix_pages is None or (prefix_pages.is_cuda and prefix_pages.dtype == torch.int32 and prefix_pages.is_contiguous())
+    need = -(-prefix_len // cache.page_size)
+    assert need == 0 or (prefix_pages is not None and prefix_pages.numel() >= need), "prefix_pages does not cover prefix_len"
+    assert page_table.is_cuda and page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == B
+    assert page_table.shape[1] <= 1 or page_table.stride(1) == 1
+    ld = page_table.stride(0) if B > 1 else page_table.shape[1]
+    assert ld == page_table.shape[1], "page_table is contiguous"
+    if O is None:
+        O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if workspace is None:
+        workspace = torch.empty(patch_prefix_attention_workspace_size(cache, B, T, Hq), dtype=torch.uint8, device=Q.device)
+    q, ldq, _ = _heads(Q, D)
+    o, ldo, Ho = _heads(O, D)
+    assert Ho == Hq and O.shape[0] == rows
+    _check(lib().patch_prefix_attention(cache, q, ldq, B, T, Hq, prefix_pages.data_ptr() if need else None, prefix_len,
+                                        page_table.data_ptr(), ld, _vec(suffix_lens, torch.int32, B),
+                                        D ** -0.5 if scale is None else scale, o, ldo, _vec(lse, torch.float32, rows * Hq),
+                                        workspace.data_ptr(), workspace.numel(), _ptr(status), _stream(stream)),
+           "patch_prefix_attention")
+    return O

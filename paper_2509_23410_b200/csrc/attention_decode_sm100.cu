@@ -1,0 +1,513 @@
+// Attention over the paged cache for items of few query rows (public header: patch_prefix_attention), the kernel that joins the
+// partial results, and the entry points.
+//
+// Mathematics.  For every row the running maximum m of the scaled scores (in powers of two), the sum l of 2^(s - m) and the
+// unnormalised output o = sum 2^(s - m) v; parts of the keys are joined with weights 2^(m_i - m).  All three are fp32; the
+// probabilities are rounded to bf16 for the product with V (they are at most 1; the sum takes them unrounded).
+//
+// Kernel.  One CTA per SM walks over its share of the work list (attention.cuh).  Warp 4 requests tiles of 64 keys
+// and values with TMA, one copy per page and operand, into a ring of stages; warps 0..3 each take 16 of the 64 keys: S = Q K^T
+// (16 rows x 16 keys), probabilities in registers, O += P V, with a maximum of their own, so that within an item no warp waits
+// for another.  At the end of a share the four warps' results are joined in shared memory.
+// What bounds it: HBM.  A 64-key tile is 32 KB (D = 128), about 1 430 cycles of an SM's share of the bandwidth; its
+// 32 + 32 products of 16 x 8 x 16 per warp and the softmax of 16 x 16 scores take a third of that.
+#include "attention.cuh"
+
+namespace patch {
+namespace attn {
+
+constexpr int kRows = 16;                     // query rows of an item
+constexpr int kKeys = 64;                     // keys of a tile
+constexpr int kStages = 5;
+constexpr int kWarps = 4;                     // consuming warps
+constexpr int kThreads = 32 * (kWarps + 1);
+
+template <int D> struct Cfg {
+    static constexpr uint32_t kOperandBytes = kKeys * D * 2;
+    static constexpr uint32_t kStageBytes = 2 * kOperandBytes;
+    static constexpr int kJoinPitch = D + 8;  // floats; the eight rows of a fragment fall into different banks
+    static constexpr uint32_t kJoinOffset = kStages * kStageBytes;
+    static constexpr uint32_t kJoinBytes = kWarps * kRows * kJoinPitch * 4;
+    static constexpr uint32_t kMlOffset = kJoinOffset + kJoinBytes;          // (m, l) of every warp and row
+    static constexpr uint32_t kBarOffset = kMlOffset + kWarps * kRows * 8;
+    static constexpr uint32_t kCumOffset = kBarOffset + 128;
+    static constexpr uint32_t kFixedBytes = kCumOffset + 1024;               // + alignment of the ring
+    static uint32_t smem_bytes(int B) { return kFixedBytes + uint32_t(B + 1) * 8 + uint32_t(B) * 4; }
+};
+
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr) : "memory");
+}
+// c[16 x 8] += a[16 x 16] b[16 x 8]
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int row, int head, int page, uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
+        ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(0), "r"(head), "r"(page), "r"(bar), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void consumer_barrier() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+
+struct Units { int64_t prefix, total; int per; };   // units of prefix items, of all; suffix items per sequence
+__device__ __forceinline__ Segment locate(const Problem& p, const Line& w, const Units& n, const int64_t* cum, const int* len,
+                                          int64_t u, int64_t end) {
+    Segment s;
+    int tiles;
+    if (u < n.prefix) {
+        s.item = u / w.tiles_p;
+        s.t0 = int(u - s.item * w.tiles_p);
+        s.b = -1;
+        s.kvh = int(s.item) / w.blocks_p;
+        s.block = int(s.item) - s.kvh * w.blocks_p;
+        s.len = p.prefix_len;
+        tiles = w.tiles_p;
+    } else {
+        const int64_t v = u - n.prefix, q = v / n.per;
+        int lo = 0, hi = p.B;                        // the sequence with cum[lo] <= q < cum[lo + 1]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (cum[mid] <= q) lo = mid; else hi = mid;
+        }
+        tiles = int(cum[lo + 1] - cum[lo]);
+        const int64_t r = v - cum[lo] * n.per;
+        const int sub = int(r / tiles);
+        s.t0 = int(r - int64_t(sub) * tiles);
+        s.b = lo;
+        s.kvh = sub / w.blocks_s;
+        s.block = sub - s.kvh * w.blocks_s;
+        s.item = int64_t(p.Hkv) * w.blocks_p + int64_t(lo) * n.per + sub;
+        s.len = len[lo];
+    }
+    const int64_t left = end - u;
+    s.t1 = left < tiles - s.t0 ? s.t0 + int(left) : tiles;
+    return s;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const Line w,
+                   float* __restrict__ part_o, float2* __restrict__ part_ml, int64_t* __restrict__ cum_out) {
+    using C = Cfg<D>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t bar_full = base + C::kBarOffset, bar_empty = bar_full + 8 * kStages;
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kBarOffset + 16 * kStages);
+    int64_t* cum = reinterpret_cast<int64_t*>(smem + C::kCumOffset);
+    int* lens = reinterpret_cast<int*>(cum + p.B + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    grid_launch_dependents();                        // the joining kernel waits for this one's end by itself
+    if (threadIdx.x == 32) {
+        for (int i = 0; i < kStages; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, kWarps); }
+        *abort_flag = 0;
+        mbar_init_fence();
+        tma_prefetch_map(&map_k);
+        tma_prefetch_map(&map_v);
+    }
+    if (warp == 0) {                                 // running number of tiles before each sequence
+        int64_t before = 0;
+        if (w.blocks_s)
+            for (int b0 = 0; b0 < p.B; b0 += 32) {
+                const int b = b0 + lane, n = b < p.B ? suffix_len(p, b) : 0;
+                int64_t t = (n + kKeys - 1) / kKeys;
+                if (b < p.B) lens[b] = n;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int64_t o = __shfl_up_sync(0xFFFFFFFFu, t, d);
+                    if (lane >= d) t += o;
+                }
+                if (b < p.B) cum[b + 1] = before + t;
+                before += __shfl_sync(0xFFFFFFFFu, t, 31);
+            }
+        else
+            for (int b = lane; b < p.B; b += 32) cum[b + 1] = 0;
+        if (lane == 0) cum[0] = 0;
+    }
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b <= p.B; b += kThreads) cum_out[b] = cum[b];
+
+    Units n;
+    n.prefix = int64_t(p.Hkv) * w.blocks_p * w.tiles_p;
+    n.per = p.Hkv * w.blocks_s;
+    n.total = n.prefix + cum[p.B] * n.per;
+    const int ctas = n.total < gridDim.x ? int(n.total) : int(gridDim.x);
+    if (int(blockIdx.x) >= ctas) return;
+    const int64_t u0 = n.total * blockIdx.x / ctas, u1 = n.total * (blockIdx.x + 1) / ctas;
+    // a copy brings the rows of one page that fall into a tile
+    const int rows_log2 = p.shift < 6 ? p.shift : 6;
+    const uint32_t copy_bytes = uint32_t(D * 2) << rows_log2;
+
+    if (warp == kWarps) {
+        // ---------------- producer ----------------
+        const uint64_t policy = l2_policy_evict_first();
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        int issued = 0;
+        for (int64_t u = u0; u < u1 && ok;) {
+            const Segment s = locate(p, w, n, cum, lens, u, u1);
+            const int32_t* pages = s.b < 0 ? p.prefix_pages : p.table + s.b * p.ld_table;
+            const int n_pages = int((int64_t(s.len) + (1 << p.shift) - 1) >> p.shift);
+            int page0 = -32, mine = 0;               // this lane holds the page number of page0 + lane
+            for (int t = s.t0; t < s.t1 && ok; ++t) {
+                const int64_t key0 = int64_t(t) * kKeys;
+                const int first = int(key0 >> p.shift);
+                if (first >= page0 + 32 || page0 < 0) {
+                    page0 = first;                   // a tile's pages divide 32, so a tile never straddles a reload
+                    mine = page0 + lane < n_pages ? pages[page0 + lane] : 0;
+                    if (mine < 0 || mine >= p.num_pages) {
+                        if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_FORMAT);
+                        mine = 0;
+                    }
+                }
+                const int keys = s.len - key0 < kKeys ? int(s.len - key0) : kKeys;
+                const int copies = (keys + (1 << rows_log2) - 1) >> rows_log2;
+                const int page = __shfl_sync(0xFFFFFFFFu, mine, (first - page0) + (p.shift < 6 ? (lane >> 1) & ((kKeys >> rows_log2) - 1) : 0));
+                bool free_slot = true;
+                if (lane == 0 && issued >= kStages) free_slot = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status);
+                ok = __shfl_sync(0xFFFFFFFFu, free_slot ? 1 : 0, 0) != 0;
+                if (!ok) break;
+                const uint32_t full = bar_full + 8 * stage;
+                if (lane == 0) mbar_expect_tx(full, uint32_t(copies) * 2u * copy_bytes);
+                __syncwarp();
+                if (lane < 2 * copies) {
+                    const uint32_t dst = base + stage * C::kStageBytes + (lane & 1) * C::kOperandBytes + (lane >> 1) * copy_bytes;
+                    tma_load_5d(dst, lane & 1 ? &map_v : &map_k, p.shift < 6 ? 0 : int(key0 & ((1 << p.shift) - 1)), s.kvh, page, full, policy);
+                }
+                ++issued;
+                if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            }
+            u += s.t1 - s.t0;
+        }
+        if (*abort_flag) {                           // wait (bounded) for the copies in flight before the CTA may leave
+            const uint64_t t0 = global_timer_ns();
+            for (int j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
+                while (!mbar_try_wait(bar_full + 8 * (j % kStages), uint32_t(j / kStages) & 1u) && global_timer_ns() - t0 < kDrainLimitNs) {}
+        }
+        return;
+    }
+
+    // ---------------- consumers ----------------
+    const int g = lane >> 2, t4 = lane & 3;
+    float* join_o = reinterpret_cast<float*>(smem + C::kJoinOffset);
+    float2* join_ml = reinterpret_cast<float2*>(smem + C::kMlOffset);
+    int stage = 0;
+    uint32_t phase = 0;
+    // address of this lane's row of a 16 x 16 block of keys (K: lanes 0..7 keys 0..7 at element 0, 8..15 keys 0..7 at element 8,
+    // 16..31 keys 8..15; V: lanes 0..15 keys 0..15 at element 0, 16..31 at element 8)
+    const int krow = warp * 16 + (lane & 7) + ((lane >> 4) << 3), vrow = warp * 16 + (lane & 15);
+    const int in_copy = (1 << rows_log2) - 1;
+    const uint32_t half_bytes = 128u << rows_log2;
+    const uint32_t k_at = uint32_t(krow >> rows_log2) * copy_bytes + uint32_t(krow & in_copy) * 128u, k_sw = krow & 7, k_c = (lane >> 3) & 1;
+    const uint32_t v_at = C::kOperandBytes + uint32_t(vrow >> rows_log2) * copy_bytes + uint32_t(vrow & in_copy) * 128u, v_sw = vrow & 7, v_c = lane >> 4;
+
+    for (int64_t u = u0; u < u1;) {
+        const Segment s = locate(p, w, n, cum, lens, u, u1);
+        u += s.t1 - s.t0;
+        const int rows = s.b < 0 ? p.B * p.T * p.G : p.T * p.G;
+        const int r0 = s.block * kRows + g, r1 = r0 + 8;
+        const int64_t tok0 = s.b < 0 ? 0 : int64_t(s.b) * p.T;
+        uint32_t qa[D / 16][4];
+        {
+            const __nv_bfloat16* q0 = p.Q + (tok0 + r0 / p.G) * p.ldq + int64_t(s.kvh * p.G + r0 % p.G) * D + 2 * t4;
+            const __nv_bfloat16* q1 = p.Q + (tok0 + r1 / p.G) * p.ldq + int64_t(s.kvh * p.G + r1 % p.G) * D + 2 * t4;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                qa[i][0] = r0 < rows ? *reinterpret_cast<const uint32_t*>(q0 + 16 * i) : 0u;
+                qa[i][1] = r1 < rows ? *reinterpret_cast<const uint32_t*>(q1 + 16 * i) : 0u;
+                qa[i][2] = r0 < rows ? *reinterpret_cast<const uint32_t*>(q0 + 16 * i + 8) : 0u;
+                qa[i][3] = r1 < rows ? *reinterpret_cast<const uint32_t*>(q1 + 16 * i + 8) : 0u;
+            }
+        }
+        // keys a row sees; rows past the item's are computed on zeros and never stored
+        const int see0 = s.b < 0 ? s.len : s.len - (p.T - 1 - r0 / p.G), see1 = s.b < 0 ? s.len : s.len - (p.T - 1 - r1 / p.G);
+        float o[D / 8][4], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+
+        bool failed = false;
+        for (int t = s.t0; t < s.t1; ++t) {
+            failed = !mbar_wait(bar_full + 8 * stage, phase, abort_flag, p.status);
+            if (failed) break;
+            const int key0 = t * kKeys + warp * 16, left = s.len - key0;         // this warp's keys
+            if (left > 0) {
+                const uint32_t sb = base + stage * C::kStageBytes;
+                float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    uint32_t b0, b1, b2, b3;
+                    ldmatrix4(sb + k_at + (i >> 2) * half_bytes + (((uint32_t((i & 3) * 2) + k_c) ^ k_sw) << 4), b0, b1, b2, b3);
+                    mma16816(sc[0], qa[i], b0, b1);
+                    mma16816(sc[1], qa[i], b2, b3);
+                }
+                const int last = see0 < see1 ? see0 : see1;
+                if (key0 + 16 > last) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int key = key0 + 8 * j + 2 * t4 + e;
+                            if (key >= see0) sc[j][e] = -INFINITY;
+                            if (key >= see1) sc[j][2 + e] = -INFINITY;
+                        }
+                }
+                float x0 = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]));
+                float x1 = fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]));
+                x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1));
+                x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
+                x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2)) * p.scale_log2;
+                x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2)) * p.scale_log2;
+                if (__any_sync(0xFFFFFFFFu, x0 > m0 || x1 > m1)) {
+                    const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
+                    const float a0 = n0 == -INFINITY ? 1.0f : ex2(m0 - n0), a1 = n1 == -INFINITY ? 1.0f : ex2(m1 - n1);
+                    m0 = n0;
+                    m1 = n1;
+                    l0 *= a0;
+                    l1 *= a1;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) { o[i][0] *= a0; o[i][1] *= a0; o[i][2] *= a1; o[i][3] *= a1; }
+                }
+                const float c0 = m0 == -INFINITY ? 0.0f : m0, c1 = m1 == -INFINITY ? 0.0f : m1;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    sc[j][0] = ex2(fmaf(sc[j][0], p.scale_log2, -c0));
+                    sc[j][1] = ex2(fmaf(sc[j][1], p.scale_log2, -c0));
+                    sc[j][2] = ex2(fmaf(sc[j][2], p.scale_log2, -c1));
+                    sc[j][3] = ex2(fmaf(sc[j][3], p.scale_log2, -c1));
+                    l0 += sc[j][0] + sc[j][1];
+                    l1 += sc[j][2] + sc[j][3];
+                }
+                const uint32_t pa[4] = {pack2(sc[0][0], sc[0][1]), pack2(sc[0][2], sc[0][3]), pack2(sc[1][0], sc[1][1]), pack2(sc[1][2], sc[1][3])};
+                // values past the length may be anything, and 0 times that is not always 0: they are taken as 0
+                uint32_t keep0 = 0xFFFFFFFFu, keep1 = 0xFFFFFFFFu;
+                if (left < 16) {
+                    const int k0 = 2 * t4;
+                    keep0 = (k0 < left ? 0x0000FFFFu : 0u) | (k0 + 1 < left ? 0xFFFF0000u : 0u);
+                    keep1 = (k0 + 8 < left ? 0x0000FFFFu : 0u) | (k0 + 9 < left ? 0xFFFF0000u : 0u);
+                }
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    uint32_t b0, b1, b2, b3;
+                    ldmatrix4_trans(sb + v_at + (i >> 2) * half_bytes + (((uint32_t((i & 3) * 2) + v_c) ^ v_sw) << 4), b0, b1, b2, b3);
+                    mma16816(o[2 * i], pa, b0 & keep0, b1 & keep1);
+                    mma16816(o[2 * i + 1], pa, b2 & keep0, b3 & keep1);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_empty + 8 * stage);
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+
+        // the four warps' parts of this share -> one partial result
+        l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 1);
+        l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 1);
+        l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 2);
+        l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 2);
+        const int valid = rows - s.block * kRows < kRows ? rows - s.block * kRows : kRows;
+        float* jo = join_o + (warp * kRows + g) * C::kJoinPitch + 2 * t4;
+        if (g < valid) {
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2*>(jo + 8 * i) = make_float2(o[i][0], o[i][1]);
+            if (t4 == 0) join_ml[warp * kRows + g] = make_float2(m0, l0);
+        }
+        if (g + 8 < valid) {
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2*>(jo + 8 * C::kJoinPitch + 8 * i) = make_float2(o[i][2], o[i][3]);
+            if (t4 == 0) join_ml[warp * kRows + g + 8] = make_float2(m1, l1);
+        }
+        if (barrier_any(failed, 1, 32 * kWarps)) return;         // one warp gave up: all leave
+        const int64_t slot = s.item + blockIdx.x;
+        for (int i = threadIdx.x; i < valid * (D / 4); i += 32 * kWarps) {
+            const int r = i / (D / 4), c = i - r * (D / 4);
+            float mx = -INFINITY, ls = 0.0f;
+#pragma unroll
+            for (int q = 0; q < kWarps; ++q) mx = fmaxf(mx, join_ml[q * kRows + r].x);
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < kWarps; ++q) {
+                const float2 ml = join_ml[q * kRows + r];
+                const float a = ml.x == -INFINITY ? 0.0f : ex2(ml.x - mx);
+                const float4 v = *reinterpret_cast<const float4*>(join_o + (q * kRows + r) * C::kJoinPitch + 4 * c);
+                ls = fmaf(ml.y, a, ls);
+                sum.x = fmaf(v.x, a, sum.x); sum.y = fmaf(v.y, a, sum.y); sum.z = fmaf(v.z, a, sum.z); sum.w = fmaf(v.w, a, sum.w);
+            }
+            *reinterpret_cast<float4*>(part_o + (slot * kRows + r) * D + 4 * c) = sum;
+            if (c == 0) part_ml[slot * kRows + r] = make_float2(mx, ls);
+        }
+        consumer_barrier();                          // the join buffer is free again
+    }
+}
+
+// Joins the partial results: one warp per query row and head.
+struct Parts { const float* o; const float2* ml; const int64_t* cum; Line w; int ctas, rows; };
+
+template <int D>
+__global__ void __launch_bounds__(256)
+attn_join_kernel(const Problem p, const Parts parts, __nv_bfloat16* __restrict__ O, int64_t ldo, float* __restrict__ lse) {
+    constexpr int V = D / 32;                        // elements per lane
+    grid_dependency_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t row = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    const int Hq = p.Hkv * p.G;
+    if (row >= int64_t(p.B) * p.T * Hq) return;
+    const int tok = int(row / Hq), hq = int(row - int64_t(tok) * Hq), kvh = hq / p.G, gq = hq - kvh * p.G, b = tok / p.T;
+    const Line& w = parts.w;
+    const int per = p.Hkv * w.blocks_s;
+    const int64_t prefix = int64_t(p.Hkv) * w.blocks_p * w.tiles_p, total = prefix + parts.cum[p.B] * per;
+    const int n = total < parts.ctas ? int(total) : parts.ctas;
+
+    float m = -INFINITY, l = 0.0f, acc[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+    auto add = [&](int64_t first, int64_t count, int64_t item, int r) {
+        if (count <= 0) return;
+        const int c0 = owner(first, total, n), c1 = owner(first + count - 1, total, n);
+        for (int c = c0; c <= c1; ++c) {
+            const int64_t at = (item + c) * parts.rows + r;
+            const float2 ml = parts.ml[at];
+            const float mx = fmaxf(m, ml.x);
+            const float a = m == -INFINITY ? 0.0f : ex2(m - mx), f = ml.x == -INFINITY ? 0.0f : ex2(ml.x - mx);
+            const float* src = parts.o + at * D + lane * V;
+            float v[V];
+            if constexpr (V == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
+            else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] = acc[i] * a + v[i] * f;
+            l = l * a + ml.y * f;
+            m = mx;
+        }
+    };
+    if (w.blocks_p) {
+        const int r = tok * p.G + gq, blk = r / parts.rows, item = kvh * w.blocks_p + blk;
+        add(int64_t(item) * w.tiles_p, w.tiles_p, item, r - blk * parts.rows);
+    }
+    if (w.blocks_s) {
+        const int r = (tok - b * p.T) * p.G + gq, blk = r / parts.rows, sub = kvh * w.blocks_s + blk;
+        const int64_t tiles = parts.cum[b + 1] - parts.cum[b];
+        add(prefix + parts.cum[b] * per + sub * tiles, tiles, int64_t(p.Hkv) * w.blocks_p + int64_t(b) * per + sub, r - blk * parts.rows);
+    }
+    const float inv = l > 0.0f ? 1.0f / l : (l == l ? 0.0f : l);       // nothing seen: 0; NaN stays NaN
+    __nv_bfloat16* dst = O + int64_t(tok) * ldo + int64_t(hq) * D + lane * V;
+    if constexpr (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(acc[0] * inv, acc[1] * inv), pack2(acc[2] * inv, acc[3] * inv));
+    else *reinterpret_cast<uint32_t*>(dst) = pack2(acc[0] * inv, acc[1] * inv);
+    if (lse && lane == 0) lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+
+static int blocks_of(int64_t rows) { return int((rows + kRows - 1) / kRows); }
+
+struct Workspace { size_t ml, o, bytes; };           // [cum | (m, l) | outputs]
+static Workspace workspace_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G) {
+    const size_t items = size_t(c->Hkv) * (size_t(blocks_of(B * T * G)) + size_t(B) * blocks_of(T * G));
+    const size_t slots = items + kMaxCtas;
+    Workspace w;
+    w.ml = (size_t(B + 1) * 8 + 255) / 256 * 256;
+    w.o = w.ml + (slots * kRows * 8 + 255) / 256 * 256;
+    w.bytes = w.o + slots * kRows * size_t(c->D) * 4;
+    return w;
+}
+
+static int check_batch(const patch_kv_cache_t* c, int64_t B, int T, int Hq) {
+    int rc = validate_kv_cache(c);
+    if (rc) return rc;
+    if (c->D != 64 && c->D != 128) return PATCH_ERR_SHAPE;
+    if (B < 0 || B > kMaxBatch || T < 1 || Hq < 1 || Hq > (1 << 16) || Hq % c->Hkv) return PATCH_ERR_SHAPE;
+    if (B * T > 0x7FFFFFFF / c->D / Hq) return PATCH_ERR_SHAPE;
+    return PATCH_OK;
+}
+
+template <int D>
+static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, uint8_t* ws, const Workspace& at, __nv_bfloat16* O,
+                  int64_t ldo, float* lse, cudaStream_t stream) {
+    CUtensorMap mk, mv;
+    const int rows = c->page_size < kKeys ? c->page_size : kKeys;
+    int rc = make_kv_tensor_map(&mk, c, c->k_dev, rows, D / 64);
+    if (!rc) rc = make_kv_tensor_map(&mv, c, c->v_dev, rows, D / 64);
+    if (rc) return rc;
+    auto kern = attn_decode_kernel<D>;
+    static std::atomic<uint64_t> configured{0};
+    if ((rc = allow_dynamic_smem(kern, Cfg<D>::smem_bytes(kMaxBatch), configured))) return rc;
+    const int sms = sm_count();
+    if (sms <= 0) return PATCH_ERR_CUDA;
+    const int ctas = sms < kMaxCtas ? sms : kMaxCtas;
+    int64_t* cum = reinterpret_cast<int64_t*>(ws);
+    float2* ml = reinterpret_cast<float2*>(ws + at.ml);
+    float* po = reinterpret_cast<float*>(ws + at.o);
+    kern<<<ctas, kThreads, Cfg<D>::smem_bytes(p.B), stream>>>(mk, mv, p, w, po, ml, cum);
+    if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
+    const Parts parts = {po, ml, cum, w, ctas, kRows};
+    const int64_t out_rows = int64_t(p.B) * p.T * p.Hkv * p.G;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    cfg.gridDim = dim3(unsigned((out_rows + 7) / 8), 1, 1);
+    cfg.blockDim = dim3(256, 1, 1);
+    cfg.stream = stream;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attn_join_kernel<D>, p, parts, O, ldo, lse) == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+}
+
+}  // namespace attn
+}  // namespace patch
+
+using namespace patch;
+
+extern "C" int patch_prefix_attention_workspace_size(const patch_kv_cache_t* cache, int64_t B, int T, int Hq, size_t* bytes_out) {
+    if (!bytes_out) return PATCH_ERR_NULL;
+    int rc = attn::check_batch(cache, B, T, Hq);
+    if (rc) return rc;
+    *bytes_out = attn::workspace_of(cache, B, T, Hq / cache->Hkv).bytes;
+    return PATCH_OK;
+}
+
+extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void* Q, int64_t ldq, int64_t B, int T, int Hq,
+                                      const int32_t* prefix_pages, int64_t prefix_len, const int32_t* page_table, int64_t ld_table,
+                                      const int32_t* suffix_lens, float scale, void* O, int64_t ldo, float* lse, void* workspace,
+                                      size_t workspace_bytes, int* status_dev, void* stream) {
+    int rc = attn::check_batch(cache, B, T, Hq);
+    if (rc) return rc;
+    if (prefix_len < 0 || prefix_len > 0x7FFFFF00 || ld_table < 0 || !(scale > 0.0f) || scale > 3.0e38f) return PATCH_ERR_SHAPE;
+    if (B == 0) return PATCH_OK;
+    if (!Q || !O || !suffix_lens || (prefix_len && !prefix_pages) || (ld_table && !page_table)) return PATCH_ERR_NULL;
+    const int D = cache->D;
+    if (ldq < int64_t(Hq) * D || ldo < int64_t(Hq) * D || ldq % 8 || ldo % 8) return PATCH_ERR_SHAPE;
+    if (!aligned16(Q) || !aligned16(O)) return PATCH_ERR_ALIGN;
+    const int G = Hq / cache->Hkv;
+    const attn::Workspace at = attn::workspace_of(cache, B, T, G);
+    if (!workspace) return PATCH_ERR_NULL;
+    if (workspace_bytes < at.bytes) return PATCH_ERR_SIZE;
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PATCH_ERR_ALIGN;
+    if ((rc = check_device())) return rc;
+    attn::Problem p = {static_cast<const __nv_bfloat16*>(Q), ldq, int(B), T, cache->Hkv, G, prefix_pages, int(prefix_len), page_table,
+                       ld_table, suffix_lens, 0, int(cache->num_pages), scale * 1.4426950408889634f, status_dev};
+    while ((1 << p.shift) < cache->page_size) ++p.shift;
+    attn::Line w;
+    w.tiles_p = int((prefix_len + attn::kKeys - 1) / attn::kKeys);
+    w.blocks_p = prefix_len ? attn::blocks_of(B * T * G) : 0;
+    w.blocks_s = attn::blocks_of(int64_t(T) * G);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(O);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    return D == 128 ? attn::launch<128>(cache, p, w, ws, at, o, ldo, lse, s) : attn::launch<64>(cache, p, w, ws, at, o, ldo, lse, s);
+}
