@@ -493,7 +493,7 @@ int patch_soft_mask_backward(const void* W_dev, int64_t ldw, const float* P_tile
  * c_0 .. c_{R/2-1}, s_0 .. s_{R/2-1} (cosines, then sines, fp32; R = rotary_dim), the pair
  *     (a, b) = (x_i, x_{i+R/2})  (interleaved = 0)   or   (x_{2i}, x_{2i+1})  (interleaved = 1)
  * becomes (a c_i - b s_i, b c_i + a s_i); elements from rotary_dim on are left as they are.
- *   rotary_dim  0 (no rotation; cos_sin_dev and positions may be NULL), or a multiple of 16 (interleaved: of 8), at most D
+ *   rotary_dim  0 (no rotation; cos_sin_dev and positions may be NULL), or a multiple of 8, at most D
  */
 typedef struct patch_rope_t {
     const float* cos_sin_dev;   /* [max_positions x rotary_dim], 16-byte aligned */

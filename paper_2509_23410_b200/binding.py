@@ -431,31 +431,48 @@ def patch_read_layout(packed, stream=None) -> Layout:
 
 # ---------------------------------------------------------------------------------------------
 # Between the linear layers: norms and rotation of queries and keys, the paged cache, attention behind a shared prefix.
+#
+# These calls take a few microseconds on the GPU for a decode step's handful of tokens, so what the host does for each of them
+# counts: tensors are taken apart with one unpacking of shape and strides each.
+
+_torch = _bf16 = _f32 = _i32 = _i64 = _raw_stream = None
 
 
-def _heads(x, D: int | None = None):
-    """Rows of heads [M x H x D], bf16, heads side by side, any row pitch: (pointer, pitch, H)."""
+def _use_torch():
+    global _torch, _bf16, _f32, _i32, _i64, _raw_stream
     import torch
-    if x is None:
-        return None, 0, 0
-    assert x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 3, "heads are bf16 CUDA tensors [M, H, D]"
-    M, H, d = x.shape
+    _torch, _bf16, _f32, _i32, _i64 = torch, torch.bfloat16, torch.float32, torch.int32, torch.int64
+    # the current stream's handle without a Stream object around it (five times quicker); device index -> handle
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _stream_of(x, stream):
+    return _raw_stream(x.get_device()) if stream is None else stream.cuda_stream
+
+
+def _rows(x, M, D):
+    """Rows of heads [M, H, D]: bf16, heads side by side, any row pitch -> (pointer, pitch, H)."""
+    m, H, d = x.shape
     sm, sh, sd = x.stride()
-    assert (sd == 1 or d == 1) and (sh == d or H == 1) and (D is None or d == D), "a row holds its heads side by side"
-    return x.data_ptr(), sm if M > 1 else H * d, H
+    assert x.dtype is _bf16 and x.is_cuda and m == M and d == D and sd == 1 and (sh == D or H == 1), \
+        "heads are bf16 CUDA tensors [tokens, heads, D] whose rows hold the heads side by side"
+    return x.data_ptr(), sm if M > 1 else H * D, H
 
 
-def _vec(x, dtype, n: int):
+def _vec(x, dtype, n):
     if x is None:
         return None
-    assert x.is_cuda and x.dtype == dtype and x.is_contiguous() and x.numel() == n, f"expected {n} contiguous {dtype} values on the GPU"
+    assert x.dtype is dtype and x.is_cuda and x.is_contiguous() and x.numel() == n, f"expected {n} contiguous {dtype} values on the GPU"
     return x.data_ptr()
+
+
+_NONE = (None, 0, 0)
 
 
 def patch_rope(cos_sin, interleaved: bool = False) -> Rope:
     """Rotation by a table float32 [max_positions, rotary_dim]: a position's cosines, then its sines."""
-    import torch
-    assert cos_sin.is_cuda and cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.is_contiguous()
+    _use_torch()
+    assert cos_sin.is_cuda and cos_sin.dtype is _f32 and cos_sin.dim() == 2 and cos_sin.is_contiguous()
     r = Rope(cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], 1 if interleaved else 0)
     r.table = cos_sin
     return r
@@ -463,33 +480,38 @@ def patch_rope(cos_sin, interleaved: bool = False) -> Rope:
 
 def patch_kv_cache(k, v) -> KVCache:
     """Paged cache over bf16 page buffers [num_pages, Hkv, page_size, D]; the two may be views of one buffer."""
-    import torch
-    assert k.is_cuda and v.is_cuda and k.dtype == v.dtype == torch.bfloat16 and k.dim() == 4
+    _use_torch()
+    assert k.is_cuda and v.is_cuda and k.dtype is _bf16 and v.dtype is _bf16 and k.dim() == 4
     assert k.shape == v.shape and k.stride() == v.stride(), "keys and values have the same shape and strides"
     pages, H, page, D = k.shape
     assert k.stride()[1:] == (page * D, D, 1), "a page holds [Hkv, page_size, D] without gaps"
-    c = KVCache(k.data_ptr(), v.data_ptr(), pages, max(k.stride(0), H * page * D) if pages == 1 else k.stride(0), page, H, D, 0)
-    c.buffers = (k, v)
+    c = KVCache(k.data_ptr(), v.data_ptr(), pages, k.stride(0) if pages > 1 else H * page * D, page, H, D, 0)
+    c.buffers, c.shape = (k, v), (H, page, D)
     return c
 
 
 def patch_qk_norm_rope(Q, K, rope: Rope | None, positions, wq=None, wk=None, eps: float = 1e-6, Q_out=None, K_out=None,
                        status=None, stream=None):
     """Norms of queries [M, Hq, D] and keys [M, Hkv, D] (either may be None) and the rotation: returns (Q_out, K_out)."""
-    import torch
-    M, _, D = (Q if Q is not None else K).shape
-    if Q_out is None and Q is not None:
-        Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-    if K_out is None and K is not None:
-        K_out = torch.empty(K.shape, dtype=K.dtype, device=K.device)
-    q, ldq, Hq = _heads(Q, D)
-    k, ldk, Hkv = _heads(K, D)
-    qo, ldqo, Hqo = _heads(Q_out if Q is not None else None, D)
-    ko, ldko, Hko = _heads(K_out if K is not None else None, D)
-    assert Hqo == Hq and Hko == Hkv and all(x is None or x.shape[0] == M for x in (Q, K, Q_out, K_out))
-    _check(lib().patch_qk_norm_rope(q, ldq, Hq, k, ldk, Hkv, M, D, _vec(wq, torch.bfloat16, D), _vec(wk, torch.bfloat16, D), eps,
-                                    rope, _vec(positions, torch.int32, M), qo, ldqo, ko, ldko, _ptr(status), _stream(stream)),
-           "patch_qk_norm_rope")
+    if _torch is None:
+        _use_torch()
+    some = Q if Q is not None else K
+    M, _, D = some.shape
+    q = k = qo = ko = _NONE
+    if Q is not None:
+        if Q_out is None:
+            Q_out = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
+        q, qo = _rows(Q, M, D), _rows(Q_out, M, D)
+    if K is not None:
+        if K_out is None:
+            K_out = _torch.empty(K.shape, dtype=_bf16, device=K.device)
+        k, ko = _rows(K, M, D), _rows(K_out, M, D)
+    assert qo[2] == q[2] and ko[2] == k[2]
+    rc = lib().patch_qk_norm_rope(q[0], q[1], q[2], k[0], k[1], k[2], M, D, _vec(wq, _bf16, D), _vec(wk, _bf16, D), eps,
+                                  rope, _vec(positions, _i32, M), qo[0], qo[1], ko[0], ko[1],
+                                  status.data_ptr() if status is not None else None, _stream_of(some, stream))
+    if rc:
+        _check(rc, "patch_qk_norm_rope")
     return Q_out, K_out
 
 
@@ -503,32 +525,38 @@ def patch_qk_norm_rope_backward_workspace_size(M: int, Hq: int, Hkv: int, D: int
 def patch_qk_norm_rope_backward(gQ_out, gK_out, rope: Rope | None, positions, Q=None, K=None, wq=None, wk=None, eps: float = 1e-6,
                                 gQ=None, gK=None, gwq=None, gwk=None, workspace=None, status=None, stream=None):
     """Gradient of ``patch_qk_norm_rope``: returns (gQ, gK, gwq, gwk); the inputs Q, K are needed where a weight is given."""
-    import torch
+    if _torch is None:
+        _use_torch()
     some = gQ_out if gQ_out is not None else gK_out
     M, _, D = some.shape
-    if gQ is None and gQ_out is not None:
-        gQ = torch.empty(gQ_out.shape, dtype=gQ_out.dtype, device=some.device)
-    if gK is None and gK_out is not None:
-        gK = torch.empty(gK_out.shape, dtype=gK_out.dtype, device=some.device)
-    if gwq is None and wq is not None:
-        gwq = torch.empty(D, dtype=torch.float32, device=some.device)
-    if gwk is None and wk is not None:
-        gwk = torch.empty(D, dtype=torch.float32, device=some.device)
-    gqo, ldgqo, Hq = _heads(gQ_out, D)
-    gko, ldgko, Hkv = _heads(gK_out, D)
+    dev = some.device
+    q = k = gqo = gko = gq = gk = _NONE
+    if gQ_out is not None:
+        if gQ is None:
+            gQ = _torch.empty(gQ_out.shape, dtype=_bf16, device=dev)
+        gqo, gq = _rows(gQ_out, M, D), _rows(gQ, M, D)
+        if wq is not None:
+            q = _rows(Q, M, D)
+            gwq = gwq if gwq is not None else _torch.empty(D, dtype=_f32, device=dev)
+    if gK_out is not None:
+        if gK is None:
+            gK = _torch.empty(gK_out.shape, dtype=_bf16, device=dev)
+        gko, gk = _rows(gK_out, M, D), _rows(gK, M, D)
+        if wk is not None:
+            k = _rows(K, M, D)
+            gwk = gwk if gwk is not None else _torch.empty(D, dtype=_f32, device=dev)
+    Hq, Hkv = gqo[2], gko[2]
+    assert gq[2] == Hq and gk[2] == Hkv and q[2] in (0, Hq) and k[2] in (0, Hkv)
     if workspace is None and (wq is not None or wk is not None):
-        workspace = torch.empty(patch_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D), dtype=torch.uint8, device=some.device)
-    q, ldq, hq = _heads(Q if wq is not None else None, D)
-    k, ldk, hk = _heads(K if wk is not None else None, D)
-    gq, ldgq, h1 = _heads(gQ if gQ_out is not None else None, D)
-    gk, ldgk, h2 = _heads(gK if gK_out is not None else None, D)
-    assert hq in (0, Hq) and hk in (0, Hkv) and h1 == Hq and h2 == Hkv
-    assert all(x is None or x.shape[0] == M for x in (gQ_out, gK_out, Q, K, gQ, gK))
-    _check(lib().patch_qk_norm_rope_backward(gqo, ldgqo, gko, ldgko, q, ldq, Hq, k, ldk, Hkv, M, D, _vec(wq, torch.bfloat16, D),
-                                             _vec(wk, torch.bfloat16, D), eps, rope, _vec(positions, torch.int32, M), gq, ldgq, gk,
-                                             ldgk, _vec(gwq, torch.float32, D), _vec(gwk, torch.float32, D), _ptr(workspace),
-                                             workspace.numel() if workspace is not None else 0, _ptr(status), _stream(stream)),
-           "patch_qk_norm_rope_backward")
+        workspace = _torch.empty(patch_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D), dtype=_torch.uint8, device=dev)
+    rc = lib().patch_qk_norm_rope_backward(gqo[0], gqo[1], gko[0], gko[1], q[0], q[1], Hq, k[0], k[1], Hkv, M, D, _vec(wq, _bf16, D),
+                                           _vec(wk, _bf16, D), eps, rope, _vec(positions, _i32, M),
+                                           gq[0], gq[1], gk[0], gk[1], _vec(gwq, _f32, D), _vec(gwk, _f32, D),
+                                           workspace.data_ptr() if workspace is not None else None,
+                                           workspace.numel() if workspace is not None else 0,
+                                           status.data_ptr() if status is not None else None, _stream_of(some, stream))
+    if rc:
+        _check(rc, "patch_qk_norm_rope_backward")
     return gQ, gK, gwq, gwk
 
 
@@ -536,24 +564,28 @@ def patch_kv_append(cache: KVCache, K, V, slots, rope: Rope | None = None, posit
                     wq=None, Q_out=None, status=None, stream=None):
     """Keys (normed and rotated) and values [M, Hkv, D] into the cache's slots (int64 [M]; negative: not stored); with Q
     [M, Hq, D] also the queries, normed and rotated: returns Q_out (None without Q)."""
-    import torch
-    M, D = K.shape[0], cache.D
-    if Q_out is None and Q is not None:
-        Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-    k, ldk, Hk = _heads(K, D)
-    v, ldv, Hv = _heads(V, D)
-    q, ldq, Hq = _heads(Q, D)
-    qo, ldqo, Hqo = _heads(Q_out if Q is not None else None, D)
-    assert Hk == Hv == cache.Hkv and Hqo == Hq and all(x is None or x.shape[0] == M for x in (V, Q, Q_out))
-    _check(lib().patch_kv_append(cache, k, ldk, v, ldv, _vec(slots, torch.int64, M), M, _vec(wk, torch.bfloat16, D), eps, rope,
-                                 _vec(positions, torch.int32, M), q, ldq, Hq, _vec(wq, torch.bfloat16, D), qo, ldqo, _ptr(status),
-                                 _stream(stream)), "patch_kv_append")
+    Hkv, _, D = cache.shape
+    M = K.shape[0]
+    k, v = _rows(K, M, D), _rows(V, M, D)
+    q = qo = _NONE
+    if Q is not None:
+        if Q_out is None:
+            Q_out = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
+        q, qo = _rows(Q, M, D), _rows(Q_out, M, D)
+    assert k[2] == v[2] == Hkv and qo[2] == q[2]
+    rc = lib().patch_kv_append(cache, k[0], k[1], v[0], v[1], _vec(slots, _i64, M), M, _vec(wk, _bf16, D), eps,
+                               rope, _vec(positions, _i32, M), q[0], q[1], q[2],
+                               _vec(wq, _bf16, D), qo[0], qo[1], status.data_ptr() if status is not None else None,
+                               _stream_of(K, stream))
+    if rc:
+        _check(rc, "patch_kv_append")
     return Q_out
 
 
 def patch_prefix_attention_workspace_size(cache: KVCache, B: int, T: int, Hq: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(lib().patch_prefix_attention_workspace_size(cache, B, T, Hq, ctypes.byref(n)), "patch_prefix_attention_workspace_size")
+    _check(lib().patch_prefix_attention_workspace_size(cache, B, T, Hq, ctypes.byref(n)),
+           "patch_prefix_attention_workspace_size")
     return int(n.value)
 
 
@@ -562,28 +594,24 @@ def patch_prefix_attention(cache: KVCache, Q, prefix_pages, prefix_len: int, pag
     """Attention of Q [B T, Hq, D] over the shared prefix (int32 ``prefix_pages``, ``prefix_len`` keys) and each sequence's own
     keys (int32 ``page_table`` [B, n], int32 ``suffix_lens`` [B]): returns O; ``lse`` float32 [B T, Hq] is written if given.
     ``scale`` defaults to 1 / sqrt(D)."""
-    import torch
-    B = suffix_lens.numel()
-    rows, Hq, D = Q.shape
-    T = rows // B if B else 1
-    assert D == cache.D and rows == B * T and (B == 0 or T > 0)
-    assert prefix_pages is None or (prefix_pages.is_cuda and prefix_pages.dtype == torch.int32 and prefix_pages.is_contiguous())
-    need = -(-prefix_len // cache.page_size)
-    assert need == 0 or (prefix_pages is not None and prefix_pages.numel() >= need), "prefix_pages does not cover prefix_len"
-    assert page_table.is_cuda and page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == B
-    assert page_table.shape[1] <= 1 or page_table.stride(1) == 1
-    ld = page_table.stride(0) if B > 1 else page_table.shape[1]
-    assert ld == page_table.shape[1], "page_table is contiguous"
+    _, page, D = cache.shape
+    B, ld = page_table.shape
+    M, Hq, _ = Q.shape
+    T = M // B if B else 1
+    need = -(-prefix_len // page)
+    assert M == B * T and (T > 0 or B == 0) and page_table.dtype is _i32 and page_table.is_cuda and page_table.is_contiguous()
+    assert need == 0 or (prefix_pages.dtype is _i32 and prefix_pages.is_cuda and prefix_pages.is_contiguous()
+                         and prefix_pages.numel() >= need), "prefix_pages does not cover prefix_len"
     if O is None:
-        O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        O = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
     if workspace is None:
-        workspace = torch.empty(patch_prefix_attention_workspace_size(cache, B, T, Hq), dtype=torch.uint8, device=Q.device)
-    q, ldq, _ = _heads(Q, D)
-    o, ldo, Ho = _heads(O, D)
-    assert Ho == Hq and O.shape[0] == rows
-    _check(lib().patch_prefix_attention(cache, q, ldq, B, T, Hq, prefix_pages.data_ptr() if need else None, prefix_len,
-                                        page_table.data_ptr(), ld, _vec(suffix_lens, torch.int32, B),
-                                        D ** -0.5 if scale is None else scale, o, ldo, _vec(lse, torch.float32, rows * Hq),
-                                        workspace.data_ptr(), workspace.numel(), _ptr(status), _stream(stream)),
-           "patch_prefix_attention")
+        workspace = _torch.empty(patch_prefix_attention_workspace_size(cache, B, T, Hq), dtype=_torch.uint8, device=Q.device)
+    q, o = _rows(Q, M, D), _rows(O, M, D)
+    assert o[2] == Hq
+    rc = lib().patch_prefix_attention(cache, q[0], q[1], B, T, Hq, prefix_pages.data_ptr() if need else None, prefix_len,
+                                      page_table.data_ptr(), ld, _vec(suffix_lens, _i32, B), D ** -0.5 if scale is None else scale,
+                                      o[0], o[1], _vec(lse, _f32, M * Hq), workspace.data_ptr(), workspace.numel(),
+                                      status.data_ptr() if status is not None else None, _stream_of(Q, stream))
+    if rc:
+        _check(rc, "patch_prefix_attention")
     return O

@@ -8,10 +8,13 @@
 // the same form with the sine's sign changed) and needs two sums over the head, of x^2 and of g w x, taken together:
 //     gx = r g w - x r^3 mean(g w x),   gw_j = sum g_j x_j r.
 //
-// Layout.  A group of LANES lanes owns a head, 16 bytes (8 elements) per lane: 8 lanes for D <= 64, 16 for D <= 128, 32
-// for D <= 256, so a warp works on 4, 2 or 1 heads and every load and store is 16 bytes per lane, 128 consecutive bytes or more
-// per head.  Pairs (i, i + R/2) sit R/16 lanes apart (one 4-register exchange of the raw bf16 values), pairs (2i, 2i + 1) in one
-// lane.  A group keeps its token's coefficients in registers and walks over several heads of the token.
+// Layout.  A group of LANES lanes owns a head, 8 elements per lane: 8 lanes for D <= 64, 16 for D <= 128, 32 for D <= 256, so a
+// warp works on 4, 2 or 1 heads.  A lane of the rotated part takes four elements of the first half and their four partners
+// of the second (pairs (i, i + R/2); two 8-byte loads, each 64 consecutive bytes or more per group), or eight consecutive elements
+// (pairs (2i, 2i + 1), and the unrotated rest): either way a pair meets in one lane, needs no exchange between lanes, and shares one
+// cosine and sine.  (Sixteen consecutive bytes per lane with an exchange of the raw values: 162 warp instructions per head
+// against about 60; that version issued 0.71 instructions per cycle and stayed at 4.1 TB/s.)  Arithmetic is in pairs of fp32
+// (one instruction each).  A group keeps its token's coefficients in registers and walks over several heads of the token.
 //
 // What bounds it: HBM.  Four bytes move per element (six in the gradient), plus 4 R bytes of table per token.
 #include "patch_internal.cuh"
@@ -22,6 +25,7 @@ namespace rope {
 
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;                 // heads whose loads are in flight together
+constexpr int kGradAhead = 2;             // the same in the gradient, which loads two operands per head
 
 struct Heads {                            // one kind of head (queries or keys) of the forward kernels
     const __nv_bfloat16* x;
@@ -50,79 +54,80 @@ struct Turn {
     int R;
 };
 
-__device__ __forceinline__ uint4 ld16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
-__device__ __forceinline__ void st16(void* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
-__device__ __forceinline__ void unpack(uint4 v, float (&f)[8]) {
-    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(u[i] << 16);
-        f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-    }
-}
-__device__ __forceinline__ uint4 pack(const float (&f)[8]) {
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-        u[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    return make_uint4(u[0], u[1], u[2], u[3]);
+// ---- pairs of fp32 in a 64-bit register ----
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 mk2(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void un2(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f2 swap2(f2 v) { float a, b; un2(v, a, b); return mk2(b, a); }
+__device__ __forceinline__ float sum2(f2 v) { float a, b; un2(v, a, b); return a + b; }
+// two bf16 -> two fp32 and back
+__device__ __forceinline__ f2 widen(uint32_t u) { return mk2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u)); }
+__device__ __forceinline__ uint32_t narrow(f2 v) {
+    float a, b;
+    un2(v, a, b);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// One group of lanes: its lane's place in the head, who holds the other halves of its pairs, and the mask its exchanges use
-// (groups of a warp may walk over different numbers of heads).
-template <int LANES, bool INTER>
+struct Raw { uint2 a, b; };               // a lane's eight bf16 of a head
+__device__ __forceinline__ void widen(const Raw& r, f2 (&v)[4]) {
+    v[0] = widen(r.a.x); v[1] = widen(r.a.y); v[2] = widen(r.b.x); v[3] = widen(r.b.y);
+}
+
+// One group of lanes.  DT: head size known at compile time (then every lane is inside the head), 0: given at run time.
+// INTER: pairs (2i, 2i + 1).  FULL: the whole head is rotated.
+template <int LANES, int DT, bool INTER, bool FULL>
 struct Group {
-    int c;                  // chunk of the head this lane holds: elements 8c .. 8c + 7
-    int partner;            // lane (in the warp) with the other elements of the pairs
-    uint32_t mask;
+    int c;                  // lane's number in the group
+    int o0, o1;             // its elements of a head: o0 .. o0 + 3 and o1 .. o1 + 3
+    uint32_t mask;          // lanes of the group (groups of a warp may walk over different numbers of heads)
     bool on, turned;        // inside the head; inside the rotated part
-    float side;             // sign of the sine: -1 where this lane holds the pairs' first elements
     __device__ __forceinline__ Group(int D, int R) {
         const int lane = threadIdx.x & 31;
         c = lane & (LANES - 1);
         mask = LANES == 32 ? 0xFFFFFFFFu : ((1u << (LANES & 31)) - 1u) << (lane & ~(LANES - 1));
-        on = c * 8 < D;
-        turned = c * 8 < R;
-        const bool first = c * 16 < R;
-        side = first ? -1.0f : 1.0f;
-        partner = INTER || !turned ? lane : first ? lane + R / 16 : lane - R / 16;
+        on = DT == LANES * 8 || c * 8 < D;
+        turned = FULL || c * 8 < R;
+        o0 = !INTER && turned ? 4 * c : 8 * c;
+        o1 = !INTER && turned ? 4 * c + R / 2 : 8 * c + 4;
     }
-    // the pairs' other elements; zeros where nothing is rotated
-    __device__ __forceinline__ uint4 other(uint4 v) const {
-        if constexpr (INTER) {
-            v.x = __byte_perm(v.x, 0, 0x1032); v.y = __byte_perm(v.y, 0, 0x1032);
-            v.z = __byte_perm(v.z, 0, 0x1032); v.w = __byte_perm(v.w, 0, 0x1032);
-        } else {
-            v.x = __shfl_sync(mask, v.x, partner); v.y = __shfl_sync(mask, v.y, partner);
-            v.z = __shfl_sync(mask, v.z, partner); v.w = __shfl_sync(mask, v.w, partner);
+    __device__ __forceinline__ Raw load(const __nv_bfloat16* head, bool in = true) const {
+        Raw r = {make_uint2(0u, 0u), make_uint2(0u, 0u)};
+        if (on && in) {
+            r.a = *reinterpret_cast<const uint2*>(head + o0);
+            r.b = *reinterpret_cast<const uint2*>(head + o1);
         }
-        return turned ? v : make_uint4(0u, 0u, 0u, 0u);
+        return r;
     }
-    // c and (signed) s of this lane's eight elements at position p: y_j = x_j c_j + x_{j'} s_j
-    __device__ __forceinline__ void angles(const Turn& t, int64_t p, float (&co)[8], float (&si)[8]) const {
+    __device__ __forceinline__ void store(__nv_bfloat16* head, const f2 (&v)[4]) const {
+        if (!on) return;
+        *reinterpret_cast<uint2*>(head + o0) = make_uint2(narrow(v[0]), narrow(v[1]));
+        *reinterpret_cast<uint2*>(head + o1) = make_uint2(narrow(v[2]), narrow(v[3]));
+    }
+    // the pairs' other elements; zeros where nothing is rotated (an infinity there must not meet a zero sine)
+    __device__ __forceinline__ void other(const f2 (&v)[4], f2 (&o)[4]) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { co[i] = 1.0f; si[i] = 0.0f; }
-        if (!turned) return;
-        const float* row = t.cos_sin + p * t.R;
+        for (int i = 0; i < 4; ++i) {
+            o[i] = INTER ? swap2(v[i]) : v[i ^ 2];
+            if (!FULL) o[i] = turned ? o[i] : 0ull;
+        }
+    }
+    // cosines and signed sines of this lane's elements at position p: y = x co + other(x) si
+    __device__ __forceinline__ void angles(const Turn& t, int64_t p, f2 (&co)[4], f2 (&si)[4]) const {
+        float4 cs = make_float4(1.f, 1.f, 1.f, 1.f), sn = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (turned && on) {
+            const float* row = t.cos_sin + p * t.R + 4 * c;
+            cs = *reinterpret_cast<const float4*>(row);
+            sn = *reinterpret_cast<const float4*>(row + t.R / 2);
+        }
         if constexpr (INTER) {
-            const float4 a = *reinterpret_cast<const float4*>(row + 4 * c), b = *reinterpret_cast<const float4*>(row + t.R / 2 + 4 * c);
-            const float ca[4] = {a.x, a.y, a.z, a.w}, sa[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                co[2 * i] = co[2 * i + 1] = ca[i];
-                si[2 * i] = -sa[i];
-                si[2 * i + 1] = sa[i];
-            }
+            co[0] = mk2(cs.x, cs.x); co[1] = mk2(cs.y, cs.y); co[2] = mk2(cs.z, cs.z); co[3] = mk2(cs.w, cs.w);
+            si[0] = mk2(-sn.x, sn.x); si[1] = mk2(-sn.y, sn.y); si[2] = mk2(-sn.z, sn.z); si[3] = mk2(-sn.w, sn.w);
         } else {
-            const float* r = row + 8 * c - (side > 0.0f ? t.R / 2 : 0);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float4 a = *reinterpret_cast<const float4*>(r + 4 * h), b = *reinterpret_cast<const float4*>(r + t.R / 2 + 4 * h);
-                co[4 * h] = a.x; co[4 * h + 1] = a.y; co[4 * h + 2] = a.z; co[4 * h + 3] = a.w;
-                si[4 * h] = side * b.x; si[4 * h + 1] = side * b.y; si[4 * h + 2] = side * b.z; si[4 * h + 3] = side * b.w;
-            }
+            co[0] = co[2] = mk2(cs.x, cs.y); co[1] = co[3] = mk2(cs.z, cs.w);
+            si[0] = mk2(-sn.x, -sn.y); si[1] = mk2(-sn.z, -sn.w); si[2] = mk2(sn.x, sn.y); si[3] = mk2(sn.z, sn.w);
         }
     }
     __device__ __forceinline__ float sum(float v) const {
@@ -141,9 +146,10 @@ __device__ __forceinline__ int64_t position(const Turn& t, int64_t m, int* statu
 }
 
 // Forward.  Groups are numbered token by token, the token's query groups first.
-template <int LANES, bool INTER, bool APPEND>
-__global__ void __launch_bounds__(kThreads)
-rope_kernel(const Heads q, const Heads k, const Cache cache, const Turn turn, int64_t M, int D, float eps, int* status_dev) {
+template <int LANES, int DT, bool INTER, bool FULL, bool APPEND>
+__global__ void __launch_bounds__(kThreads, 4)
+rope_kernel(const Heads q, const Heads k, const Cache cache, const Turn turn, int64_t M, int d, float eps, int* status_dev) {
+    const int D = DT ? DT : d;
     const int per_token = q.groups + k.groups;
     const int64_t idx = (int64_t(blockIdx.x) * kThreads + threadIdx.x) / LANES;
     const int64_t m = idx / per_token;
@@ -152,67 +158,79 @@ rope_kernel(const Heads q, const Heads k, const Cache cache, const Turn turn, in
     const bool is_q = gi < q.groups;
     const Heads& hd = is_q ? q : k;
     const int h0 = (is_q ? gi : gi - q.groups) * hd.per, h1 = min(hd.H, h0 + hd.per);
-    const Group<LANES, INTER> g(D, turn.R);
-    const int e = g.c * 8;
-    const bool norm = hd.w != nullptr;
+    const Group<LANES, DT, INTER, FULL> g(D, FULL ? D : turn.R);
+    const bool norm = hd.w != nullptr, store_kv = APPEND && !is_q;
 
+    const __nv_bfloat16* x = hd.x + m * hd.ldx + int64_t(h0) * D;
+    Raw raw[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) raw[i] = g.load(x + i * D, h0 + i < h1);
     int64_t slot = -1;
-    if (APPEND && !is_q) {
+    if (store_kv) {
         slot = cache.slots[m];
         if (slot >= cache.n_slots) {
             if (status_dev) atomicCAS(status_dev, PATCH_OK, PATCH_ERR_SIZE);
             slot = -1;
         }
     }
-    const __nv_bfloat16* x = hd.x + m * hd.ldx + e;
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    uint4 raw[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) raw[i] = g.on && h0 + i < h1 ? ld16(x + int64_t(h0 + i) * D) : zero;
-
-    float A[8], B[8];
+    f2 A[4], B[4];
     g.angles(turn, position(turn, m, status_dev), A, B);
     if (norm) {
-        const uint4 wr = g.on ? ld16(hd.w + e) : zero;
-        float w[8], wo[8];
-        unpack(wr, w);
-        unpack(g.other(wr), wo);
+        f2 w[4], wo[4];
+        widen(g.load(hd.w), w);
+        g.other(w, wo);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { A[i] *= w[i]; B[i] *= wo[i]; }
+        for (int i = 0; i < 4; ++i) { A[i] = mul2(A[i], w[i]); B[i] = mul2(B[i], wo[i]); }
     }
+    // results: rows of heads, or the token's slot of the cache
+    __nv_bfloat16* y = store_kv ? cache.k + cache.at(slot < 0 ? 0 : slot, h0) : hd.y + m * hd.ldy + int64_t(h0) * D;
+    const int64_t step = store_kv ? int64_t(D) << cache.shift : D;
+    const bool keep = !store_kv || slot >= 0;
     const float inv_d = 1.0f / float(D);
     for (int h = h0; h < h1; h += kAhead) {
-        uint4 next[kAhead];
+        if (h > h0) {
+            x += kAhead * D;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) next[i] = g.on && h + kAhead + i < h1 ? ld16(x + int64_t(h + kAhead + i) * D) : zero;
+            for (int i = 0; i < kAhead; ++i) raw[i] = g.load(x + i * D, h + i < h1);
+        }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (h + i >= h1) break;
-            float v[8], o[8];
-            unpack(raw[i], v);
-            unpack(g.other(raw[i]), o);
-            float r = 1.0f;
+            f2 v[4], o[4];
+            widen(raw[i], v);
+            g.other(v, o);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = mul2(o[j], B[j]);
             if (norm) {
-                float ss = 0.0f;
+                f2 ss = mul2(v[0], v[0]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) ss = fmaf(v[j], v[j], ss);
-                r = rsqrtf(fmaf(g.sum(ss), inv_d, eps));
-            }
+                for (int j = 1; j < 4; ++j) ss = fma2(v[j], v[j], ss);
+                const float r = rsqrtf(fmaf(g.sum(sum2(ss)), inv_d, eps));
+                const f2 rr = mk2(r, r);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = r * fmaf(v[j], A[j], o[j] * B[j]);
-            if (!g.on) continue;
-            if (APPEND && !is_q) {
-                if (slot >= 0) {
-                    const int64_t at = cache.at(slot, h + i) + e;
-                    st16(cache.k + at, pack(v));
-                    st16(cache.v + at, ld16(cache.src_v + m * cache.ldv + int64_t(h + i) * D + e));
-                }
+                for (int j = 0; j < 4; ++j) v[j] = mul2(rr, fma2(v[j], A[j], o[j]));
             } else {
-                st16(hd.y + m * hd.ldy + int64_t(h + i) * D + e, pack(v));
-            }
-        }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) raw[i] = next[i];
+                for (int j = 0; j < 4; ++j) v[j] = fma2(v[j], A[j], o[j]);
+            }
+            if (keep) g.store(y, v);
+            y += step;
+        }
+    }
+    if (store_kv && keep && g.on) {                  // the same heads of V, copied
+        const __nv_bfloat16* src = cache.src_v + m * cache.ldv + int64_t(h0) * D + 8 * g.c;
+        __nv_bfloat16* dst = cache.v + cache.at(slot, h0) + 8 * g.c;
+        for (int h = h0; h < h1; h += kAhead) {
+            uint4 t[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (h + i < h1) t[i] = *reinterpret_cast<const uint4*>(src + i * D);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (h + i < h1) *reinterpret_cast<uint4*>(dst + i * step) = t[i];
+            src += kAhead * D;
+            dst += kAhead * step;
+        }
     }
 }
 
@@ -227,13 +245,14 @@ struct GradHeads {                        // one kind of head of the gradient ke
 
 // Gradient.  A group keeps its place in the token (which kind, which heads) and walks over tokens, so that the weight's
 // gradient stays in registers; a block then adds its groups' sums in group order and writes one row of partial sums per kind.
-template <int LANES, bool INTER>
-__global__ void __launch_bounds__(kThreads)
-rope_backward_kernel(const GradHeads q, const GradHeads k, const Turn turn, int64_t M, int D, float eps, int64_t token_stride,
+template <int LANES, int DT, bool INTER, bool FULL>
+__global__ void __launch_bounds__(kThreads, 3)
+rope_backward_kernel(const GradHeads q, const GradHeads k, const Turn turn, int64_t M, int d, float eps, int64_t token_stride,
                      float* __restrict__ partial, int* status_dev) {
     constexpr int kGroups = kThreads / LANES;
     __shared__ float sums[kGroups][LANES * 8];
     __shared__ int kinds[kGroups];
+    const int D = DT ? DT : d;
     const int per_token = q.groups + k.groups;
     const int group = threadIdx.x / LANES;
     const int64_t idx = int64_t(blockIdx.x) * kGroups + group;
@@ -242,64 +261,68 @@ rope_backward_kernel(const GradHeads q, const GradHeads k, const Turn turn, int6
     const bool is_q = gi < q.groups;
     const GradHeads& hd = is_q ? q : k;
     const int h0 = (is_q ? gi : gi - q.groups) * hd.per, h1 = min(hd.H, h0 + hd.per);
-    const Group<LANES, INTER> g(D, turn.R);
-    const int e = g.c * 8;
+    const Group<LANES, DT, INTER, FULL> g(D, FULL ? D : turn.R);
     const bool norm = hd.w != nullptr;
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
     const float inv_d = 1.0f / float(D);
-    float w[8], gw[8];
-    unpack(norm && g.on ? ld16(hd.w + e) : zero, w);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) gw[j] = 0.0f;
+    const f2 minus = mk2(-1.0f, -1.0f);
+    f2 w[4] = {0ull, 0ull, 0ull, 0ull}, gw[4] = {0ull, 0ull, 0ull, 0ull};
+    if (norm) widen(g.load(hd.w), w);
     if (first < token_stride) {           // the last groups of the grid may be over
         for (int64_t m = first; m < M; m += token_stride) {
-            float co[8], si[8];
+            const __nv_bfloat16* gy = hd.gy + m * hd.ldgy + int64_t(h0) * D;
+            const __nv_bfloat16* x = hd.x + m * hd.ldx + int64_t(h0) * D;
+            __nv_bfloat16* gx = hd.gx + m * hd.ldgx + int64_t(h0) * D;
+            f2 co[4], si[4];
             g.angles(turn, position(turn, m, status_dev), co, si);
-            const __nv_bfloat16* gy = hd.gy + m * hd.ldgy + e;
-            const __nv_bfloat16* x = hd.x + m * hd.ldx + e;
-            __nv_bfloat16* gx = hd.gx + m * hd.ldgx + e;
-            for (int h = h0; h < h1; h += kAhead) {
-                uint4 ry[kAhead], rx[kAhead];
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    const bool in = g.on && h + i < h1;
-                    ry[i] = in ? ld16(gy + int64_t(h + i) * D) : zero;
-                    rx[i] = in && norm ? ld16(x + int64_t(h + i) * D) : zero;
+            for (int j = 0; j < 4; ++j) si[j] = mul2(si[j], minus);          // R^T
+            for (int h = h0; h < h1; h += kGradAhead) {
+                Raw ry[kGradAhead], rx[kGradAhead];
+#pragma unroll
+                for (int i = 0; i < kGradAhead; ++i) {
+                    ry[i] = g.load(gy + i * D, h + i < h1);
+                    rx[i] = g.load(x + i * D, norm && h + i < h1);
                 }
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
+                for (int i = 0; i < kGradAhead; ++i) {
                     if (h + i >= h1) break;
-                    float v[8], t[8];
-                    unpack(ry[i], v);
-                    unpack(g.other(ry[i]), t);
+                    f2 v[4], t[4];
+                    widen(ry[i], v);
+                    g.other(v, t);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = fmaf(v[j], co[j], -t[j] * si[j]);     // R^T gy
+                    for (int j = 0; j < 4; ++j) v[j] = fma2(v[j], co[j], mul2(t[j], si[j]));
                     if (norm) {
-                        unpack(rx[i], t);
-                        float ss = 0.0f, gx_sum = 0.0f;
+                        widen(rx[i], t);
+                        f2 wg[4], ss = 0ull, gs = 0ull;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            ss = fmaf(t[j], t[j], ss);
-                            gx_sum = fmaf(v[j] * w[j], t[j], gx_sum);
+                        for (int j = 0; j < 4; ++j) {
+                            wg[j] = mul2(v[j], w[j]);
+                            ss = fma2(t[j], t[j], ss);
+                            gs = fma2(wg[j], t[j], gs);
                         }
-                        ss = g.sum(ss);
-                        gx_sum = g.sum(gx_sum);
-                        const float r = rsqrtf(fmaf(ss, inv_d, eps));
-                        const float back = r * r * (gx_sum * inv_d);
+                        const float sx = g.sum(sum2(ss)), sg = g.sum(sum2(gs));
+                        const float r = rsqrtf(fmaf(sx, inv_d, eps)), back = -r * r * (sg * inv_d);
+                        const f2 rr = mk2(r, r), bb = mk2(back, back);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            gw[j] = fmaf(v[j], t[j] * r, gw[j]);
-                            v[j] = r * fmaf(v[j], w[j], -t[j] * back);
+                        for (int j = 0; j < 4; ++j) {
+                            t[j] = mul2(t[j], rr);
+                            gw[j] = fma2(v[j], t[j], gw[j]);
+                            v[j] = fma2(wg[j], rr, mul2(t[j], bb));
                         }
                     }
-                    if (g.on) st16(gx + int64_t(h + i) * D, pack(v));
+                    g.store(gx + i * D, v);
                 }
+                gy += kGradAhead * D;
+                x += kGradAhead * D;
+                gx += kGradAhead * D;
             }
         }
     }
     if (!partial) return;
+    if (g.on) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[group][e + j] = gw[j];
+        for (int j = 0; j < 4; ++j) un2(gw[j], sums[group][(j < 2 ? g.o0 : g.o1 - 4) + 2 * j], sums[group][(j < 2 ? g.o0 : g.o1 - 4) + 2 * j + 1]);
+    }
     if (g.c == 0) kinds[group] = is_q ? 0 : 1;
     __syncthreads();
     for (int j = threadIdx.x; j < 2 * D; j += kThreads) {
@@ -337,7 +360,7 @@ static int check_rope(const patch_rope_t* rope, int D, const int32_t* positions,
     *t = Turn{nullptr, nullptr, 0, 0};
     if (!rope || rope->rotary_dim == 0) return PATCH_OK;
     const int R = rope->rotary_dim;
-    if (R < 0 || R > D || R % (rope->interleaved ? 8 : 16) || rope->max_positions < 1) return PATCH_ERR_SHAPE;
+    if (R < 0 || R > D || R % 8 || rope->max_positions < 1) return PATCH_ERR_SHAPE;
     if (!rope->cos_sin_dev || !positions) return PATCH_ERR_NULL;
     if (!aligned16(rope->cos_sin_dev)) return PATCH_ERR_ALIGN;
     *t = Turn{rope->cos_sin_dev, positions, rope->max_positions, R};
@@ -358,52 +381,83 @@ static int check_heads(int64_t M, int Hq, int Hkv, int D) {
 // of them, but while the launch has fewer groups than the GPU's SMs can hold (128 warps' worth of 16-lane groups
 // each), splitting the token further fills more of the GPU.
 static int heads_per_group(int64_t M, int heads, int lanes) {
-    const int64_t room = int64_t(sm_count()) * (2048 / lanes);
+    const int64_t room = int64_t(sm_count()) * (1024 / lanes);
     int per = 1;
-    while (per < 8 && M * heads / (2 * per) >= room) per *= 2;
+    while (per < 8 && M * heads / per > room) per *= 2;
     return per;
 }
 static unsigned blocks_for(int64_t groups, int lanes) { return unsigned((groups * lanes + kThreads - 1) / kThreads); }
 
-template <int LANES, bool INTER>
-static int launch_forward(const Heads& q, const Heads& k, const Cache* cache, const Turn& t, int64_t M, int D, float eps,
-                          int* status_dev, cudaStream_t s) {
-    const int64_t groups = M * (q.groups + k.groups);
-    if ((groups * LANES + kThreads - 1) / kThreads > 0x7FFFFFFF) return PATCH_ERR_SHAPE;
-    if (cache) rope_kernel<LANES, INTER, true><<<blocks_for(groups, LANES), kThreads, 0, s>>>(q, k, *cache, t, M, D, eps, status_dev);
-    else rope_kernel<LANES, INTER, false><<<blocks_for(groups, LANES), kThreads, 0, s>>>(q, k, Cache{}, t, M, D, eps, status_dev);
-    return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+// Runs `f` with the kernel variant for heads of D elements of which R are rotated as its template arguments: heads of 64 and
+// 128 have kernels of their own with D known at compile time (offsets become immediates, no lane is outside the head), and
+// so has the head that is rotated as a whole; any other D or R takes the general ones.
+template <class F>
+static int dispatch(int D, int R, bool inter, F&& f) {
+#define PATCH_ROPE_CASE(LANES, DT) \
+    return R == D ? (inter ? f.template operator()<LANES, DT, true, true>() : f.template operator()<LANES, DT, false, true>()) \
+                  : (inter ? f.template operator()<LANES, DT, true, false>() : f.template operator()<LANES, DT, false, false>())
+    if (D == 64) PATCH_ROPE_CASE(8, 64);
+    if (D == 128) PATCH_ROPE_CASE(16, 128);
+#undef PATCH_ROPE_CASE
+    if (D <= 64) return inter ? f.template operator()<8, 0, true, false>() : f.template operator()<8, 0, false, false>();
+    if (D <= 128) return inter ? f.template operator()<16, 0, true, false>() : f.template operator()<16, 0, false, false>();
+    return inter ? f.template operator()<32, 0, true, false>() : f.template operator()<32, 0, false, false>();
 }
+
+struct Forward {
+    const Heads &q, &k;
+    const Cache* cache;
+    const Turn& t;
+    int64_t M;
+    int D;
+    float eps;
+    int* status_dev;
+    cudaStream_t s;
+    template <int LANES, int DT, bool INTER, bool FULL> int operator()() const {
+        const int64_t groups = M * (q.groups + k.groups);
+        if ((groups * LANES + kThreads - 1) / kThreads > 0x7FFFFFFF) return PATCH_ERR_SHAPE;
+        const unsigned blocks = blocks_for(groups, LANES);
+        if (cache) rope_kernel<LANES, DT, INTER, FULL, true><<<blocks, kThreads, 0, s>>>(q, k, *cache, t, M, D, eps, status_dev);
+        else rope_kernel<LANES, DT, INTER, FULL, false><<<blocks, kThreads, 0, s>>>(q, k, Cache{}, t, M, D, eps, status_dev);
+        return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+    }
+};
 static int forward(Heads q, Heads k, const Cache* cache, const Turn& t, bool inter, int64_t M, int D, float eps, int* status_dev,
                    cudaStream_t s) {
     const int lanes = lanes_of(D), per = heads_per_group(M, q.H + k.H, lanes);
     q.per = k.per = per;
     q.groups = (q.H + per - 1) / per;
     k.groups = (k.H + per - 1) / per;
-    if (lanes == 8) return inter ? launch_forward<8, true>(q, k, cache, t, M, D, eps, status_dev, s) : launch_forward<8, false>(q, k, cache, t, M, D, eps, status_dev, s);
-    if (lanes == 16) return inter ? launch_forward<16, true>(q, k, cache, t, M, D, eps, status_dev, s) : launch_forward<16, false>(q, k, cache, t, M, D, eps, status_dev, s);
-    return inter ? launch_forward<32, true>(q, k, cache, t, M, D, eps, status_dev, s) : launch_forward<32, false>(q, k, cache, t, M, D, eps, status_dev, s);
+    return dispatch(D, t.R, inter, Forward{q, k, cache, t, M, D, eps, status_dev, s});
 }
 
 // Blocks of the gradient kernel: enough to fill the GPU, at most one group of lanes per (token, group of heads).
-constexpr int kMaxBackwardBlocks = 160 * 6;
+constexpr int kMaxBackwardBlocks = 160 * 3;
 static int backward_blocks(int64_t M, int per_token, int lanes) {
-    const int64_t want = blocks_for(M * per_token, lanes) ? (M * per_token * lanes + kThreads - 1) / kThreads : 1;
-    const int64_t cap = int64_t(sm_count()) * 6 < kMaxBackwardBlocks ? int64_t(sm_count()) * 6 : kMaxBackwardBlocks;
+    const int64_t want = (M * per_token * lanes + kThreads - 1) / kThreads;
+    const int64_t cap = int64_t(sm_count()) * 3 < kMaxBackwardBlocks ? int64_t(sm_count()) * 3 : kMaxBackwardBlocks;
     return int(want < cap ? want : cap);
 }
-template <int LANES, bool INTER>
-static int launch_backward(const GradHeads& q, const GradHeads& k, const Turn& t, int64_t M, int D, float eps, float* partial,
-                           float* gwq, float* gwk, int* status_dev, cudaStream_t s) {
-    const int per_token = q.groups + k.groups;
-    int blocks = backward_blocks(M, per_token, LANES);
-    const int64_t least = (per_token * LANES + kThreads - 1) / kThreads;       // every group of a token has to be somewhere
-    if (blocks < least) blocks = int(least);
-    const int64_t stride = int64_t(blocks) * (kThreads / LANES) / per_token;
-    rope_backward_kernel<LANES, INTER><<<blocks, kThreads, 0, s>>>(q, k, t, M, D, eps, stride, partial, status_dev);
-    if (partial) rope_weight_sum_kernel<<<(2 * D + 31) / 32, 1024, 0, s>>>(partial, blocks, D, gwq, gwk);
-    return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
-}
+struct Backward {
+    const GradHeads &q, &k;
+    const Turn& t;
+    int64_t M;
+    int D;
+    float eps;
+    float *partial, *gwq, *gwk;
+    int* status_dev;
+    cudaStream_t s;
+    template <int LANES, int DT, bool INTER, bool FULL> int operator()() const {
+        const int per_token = q.groups + k.groups;
+        int blocks = backward_blocks(M, per_token, LANES);
+        const int least = (per_token * LANES + kThreads - 1) / kThreads;       // every group of a token has to be somewhere
+        if (blocks < least) blocks = least;
+        const int64_t stride = int64_t(blocks) * (kThreads / LANES) / per_token;
+        rope_backward_kernel<LANES, DT, INTER, FULL><<<blocks, kThreads, 0, s>>>(q, k, t, M, D, eps, stride, partial, status_dev);
+        if (partial) rope_weight_sum_kernel<<<(2 * D + 31) / 32, 1024, 0, s>>>(partial, blocks, D, gwq, gwk);
+        return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+    }
+};
 
 }  // namespace rope
 
@@ -523,11 +577,5 @@ extern "C" int patch_qk_norm_rope_backward(const void* gQo, int64_t ldgqo, const
     float* partial = wq || wk ? static_cast<float*>(workspace) : nullptr;
     gwq = wq ? gwq : nullptr;
     gwk = wk ? gwk : nullptr;
-    const bool inter = rope && rope->interleaved;
-    if (lanes == 8) return inter ? rope::launch_backward<8, true>(q, k, t, M, D, eps, partial, gwq, gwk, status_dev, s)
-                                 : rope::launch_backward<8, false>(q, k, t, M, D, eps, partial, gwq, gwk, status_dev, s);
-    if (lanes == 16) return inter ? rope::launch_backward<16, true>(q, k, t, M, D, eps, partial, gwq, gwk, status_dev, s)
-                                  : rope::launch_backward<16, false>(q, k, t, M, D, eps, partial, gwq, gwk, status_dev, s);
-    return inter ? rope::launch_backward<32, true>(q, k, t, M, D, eps, partial, gwq, gwk, status_dev, s)
-                 : rope::launch_backward<32, false>(q, k, t, M, D, eps, partial, gwq, gwk, status_dev, s);
+    return rope::dispatch(D, t.R, rope && rope->interleaved, rope::Backward{q, k, t, M, D, eps, partial, gwq, gwk, status_dev, s});
 }

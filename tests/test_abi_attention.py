@@ -50,7 +50,7 @@ def rope(B, **kw):
 
 
 BAD_ROPES = [(dict(cos_sin_dev=None), "ERR_NULL"), (dict(cos_sin_dev=FAKE + 4), "ERR_ALIGN"), (dict(max_positions=0), "ERR_SHAPE"),
-             (dict(rotary_dim=144), "ERR_SHAPE"), (dict(rotary_dim=-16), "ERR_SHAPE"), (dict(rotary_dim=24), "ERR_SHAPE"),
+             (dict(rotary_dim=144), "ERR_SHAPE"), (dict(rotary_dim=-16), "ERR_SHAPE"), (dict(rotary_dim=20), "ERR_SHAPE"),
              (dict(rotary_dim=12, interleaved=1), "ERR_SHAPE")]
 
 
