@@ -50,10 +50,63 @@ __device__ __forceinline__ int suffix_len(const Problem& p, int b) {
 // First unit after which ... the CTA that owns unit u of U spread over n <= U CTAs.
 __device__ __forceinline__ int owner(int64_t u, int64_t U, int n) { return int(((u + 1) * n - 1) / U); }
 
-struct Segment {                              // one CTA's share of one item
-    int64_t item;
-    int b, kvh, block;                        // b < 0: the prefix
-    int t0, t1, len;                          // tiles [t0, t1) of len keys
+// The walk of one CTA along the line: the item that holds a unit, and the items after it.  `cum` is the number of key tiles before each
+// sequence (one key head, one row block), `len` the clamped lengths, both in shared memory.
+struct Walk {
+    const Problem& p;
+    const Line& w;
+    const int* cum;
+    const int* len;
+    int b, kvh, block, tiles, keys;           // b < 0: the prefix
+    int item;
+
+    __device__ __forceinline__ Walk(const Problem& p_, const Line& w_, const int* cum_, const int* len_) : p(p_), w(w_), cum(cum_), len(len_) {}
+    __device__ __forceinline__ int64_t prefix_units() const { return int64_t(p.Hkv) * w.blocks_p * w.tiles_p; }
+    __device__ __forceinline__ int per() const { return p.Hkv * w.blocks_s; }          // items of a sequence
+    __device__ __forceinline__ int64_t total() const { return prefix_units() + int64_t(cum[p.B]) * per(); }
+    __device__ __forceinline__ void at_sequence(int b_) {
+        b = b_;
+        tiles = cum[b + 1] - cum[b];
+        keys = len[b];
+    }
+    // to the item of unit u; returns the tile
+    __device__ __forceinline__ int seek(int64_t u) {
+        const int64_t before = prefix_units();
+        if (u < before) {
+            item = int(u / w.tiles_p);
+            b = -1;
+            kvh = item / w.blocks_p;
+            block = item - kvh * w.blocks_p;
+            tiles = w.tiles_p;
+            keys = p.prefix_len;
+            return int(u - int64_t(item) * w.tiles_p);
+        }
+        const int64_t v = u - before, q = v / per();
+        int lo = 0, hi = p.B;                 // the sequence with cum[lo] <= q < cum[lo + 1]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (cum[mid] <= q) lo = mid; else hi = mid;
+        }
+        at_sequence(lo);
+        const int64_t r = v - int64_t(cum[lo]) * per();
+        const int sub = int(r / tiles);
+        kvh = sub / w.blocks_s;
+        block = sub - kvh * w.blocks_s;
+        item = p.Hkv * w.blocks_p + lo * per() + sub;
+        return int(r - int64_t(sub) * tiles);
+    }
+    // to the next item that has tiles (there is one)
+    __device__ __forceinline__ void next() {
+        ++item;
+        if (++block < (b < 0 ? w.blocks_p : w.blocks_s)) return;
+        block = 0;
+        if (++kvh < p.Hkv) return;
+        kvh = 0;
+        int n = b + 1;
+        while (n + 1 < p.B && cum[n + 1] == cum[n]) ++n;
+        item = p.Hkv * w.blocks_p + n * per();
+        at_sequence(n);
+    }
 };
 
 }  // namespace attn

@@ -5,12 +5,15 @@
 // unnormalised output o = sum 2^(s - m) v; parts of the keys are joined with weights 2^(m_i - m).  All three are fp32; the
 // probabilities are rounded to bf16 for the product with V (they are at most 1; the sum takes them unrounded).
 //
-// Kernel.  One CTA per SM walks over its share of the work list (attention.cuh).  Warp 4 requests tiles of 64 keys
-// and values with TMA, one copy per page and operand, into a ring of stages; warps 0..3 each take 16 of the 64 keys: S = Q K^T
+// Kernel.  One CTA per SM walks over its share of the work list (attention.cuh).  Warp 4 alone knows the list: it requests tiles
+// of 64 keys and values with TMA, one copy per page and operand, into a ring of stages, and with an item's first tile the
+// item's query rows; a note in the stage says what the tile is.  Warps 0..3 each take 16 of the 64 keys: S = Q K^T
 // (16 rows x 16 keys), probabilities in registers, O += P V, with a maximum of their own, so that within an item no warp waits
 // for another.  At the end of a share the four warps' results are joined in shared memory.
 // What bounds it: HBM.  A 64-key tile is 32 KB (D = 128), about 1 430 cycles of an SM's share of the bandwidth; its
-// 32 + 32 products of 16 x 8 x 16 per warp and the softmax of 16 x 16 scores take a third of that.
+// 32 + 32 products of 16 x 8 x 16 per warp and the softmax of 16 x 16 scores take half of that.  Batches with many short
+// items live off the hand-over between items: with every warp looking its items up and fetching their queries itself, an
+// item cost about 1.5 us on top of its tiles (16 sequences of up to 1024 keys, 32 heads: 59 us against a floor of 27).
 #include "attention.cuh"
 
 namespace patch {
@@ -18,22 +21,30 @@ namespace attn {
 
 constexpr int kRows = 16;                     // query rows of an item
 constexpr int kKeys = 64;                     // keys of a tile
-constexpr int kStages = 5;
+constexpr int kStages = 4;
 constexpr int kWarps = 4;                     // consuming warps
 constexpr int kThreads = 32 * (kWarps + 1);
 
 template <int D> struct Cfg {
     static constexpr uint32_t kOperandBytes = kKeys * D * 2;
     static constexpr uint32_t kStageBytes = 2 * kOperandBytes;
-    static constexpr int kJoinPitch = D + 8;  // floats; the eight rows of a fragment fall into different banks
-    static constexpr uint32_t kJoinOffset = kStages * kStageBytes;
+    static constexpr uint32_t kQPitch = D * 2 + 16;                          // bytes; eight rows of a fragment fall into different banks
+    static constexpr uint32_t kQBytes = kRows * kQPitch;
+    static constexpr int kJoinPitch = D + 8;                                 // floats, likewise
+    static constexpr uint32_t kQOffset = kStages * kStageBytes;
+    static constexpr uint32_t kJoinOffset = kQOffset + kStages * kQBytes;
     static constexpr uint32_t kJoinBytes = kWarps * kRows * kJoinPitch * 4;
     static constexpr uint32_t kMlOffset = kJoinOffset + kJoinBytes;          // (m, l) of every warp and row
-    static constexpr uint32_t kBarOffset = kMlOffset + kWarps * kRows * 8;
+    static constexpr uint32_t kNoteOffset = kMlOffset + kWarps * kRows * 8;
+    static constexpr uint32_t kBarOffset = kNoteOffset + kStages * 32;
     static constexpr uint32_t kCumOffset = kBarOffset + 128;
     static constexpr uint32_t kFixedBytes = kCumOffset + 1024;               // + alignment of the ring
-    static uint32_t smem_bytes(int B) { return kFixedBytes + uint32_t(B + 1) * 8 + uint32_t(B) * 4; }
+    static uint32_t smem_bytes(int B) { return kFixedBytes + uint32_t(2 * B + 1) * 4; }
 };
+// What a stage holds.
+struct Note { int slot, key0, keys, rows, block, flags, pad0, pad1; };
+constexpr int kFirst = 1, kLast = 2, kOwn = 4;        // first / last tile of the CTA's share of an item; the sequence's own keys
+static_assert(sizeof(Note) == 32, "note");
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr) : "memory");
@@ -61,55 +72,19 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map
         " [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
         ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(0), "r"(head), "r"(page), "r"(bar), "l"(policy) : "memory");
 }
-__device__ __forceinline__ void consumer_barrier() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
-
-struct Units { int64_t prefix, total; int per; };   // units of prefix items, of all; suffix items per sequence
-__device__ __forceinline__ Segment locate(const Problem& p, const Line& w, const Units& n, const int64_t* cum, const int* len,
-                                          int64_t u, int64_t end) {
-    Segment s;
-    int tiles;
-    if (u < n.prefix) {
-        s.item = u / w.tiles_p;
-        s.t0 = int(u - s.item * w.tiles_p);
-        s.b = -1;
-        s.kvh = int(s.item) / w.blocks_p;
-        s.block = int(s.item) - s.kvh * w.blocks_p;
-        s.len = p.prefix_len;
-        tiles = w.tiles_p;
-    } else {
-        const int64_t v = u - n.prefix, q = v / n.per;
-        int lo = 0, hi = p.B;                        // the sequence with cum[lo] <= q < cum[lo + 1]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (cum[mid] <= q) lo = mid; else hi = mid;
-        }
-        tiles = int(cum[lo + 1] - cum[lo]);
-        const int64_t r = v - cum[lo] * n.per;
-        const int sub = int(r / tiles);
-        s.t0 = int(r - int64_t(sub) * tiles);
-        s.b = lo;
-        s.kvh = sub / w.blocks_s;
-        s.block = sub - s.kvh * w.blocks_s;
-        s.item = int64_t(p.Hkv) * w.blocks_p + int64_t(lo) * n.per + sub;
-        s.len = len[lo];
-    }
-    const int64_t left = end - u;
-    s.t1 = left < tiles - s.t0 ? s.t0 + int(left) : tiles;
-    return s;
-}
-
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const Line w,
-                   float* __restrict__ part_o, float2* __restrict__ part_ml, int64_t* __restrict__ cum_out) {
+                   float* __restrict__ part_o, float2* __restrict__ part_ml, int* __restrict__ cum_out) {
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t bar_full = base + C::kBarOffset, bar_empty = bar_full + 8 * kStages;
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kBarOffset + 16 * kStages);
-    int64_t* cum = reinterpret_cast<int64_t*>(smem + C::kCumOffset);
-    int* lens = reinterpret_cast<int*>(cum + p.B + 1);
+    Note* notes = reinterpret_cast<Note*>(smem + C::kNoteOffset);
+    int* cum = reinterpret_cast<int*>(smem + C::kCumOffset);
+    int* lens = cum + p.B + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     grid_launch_dependents();                        // the joining kernel waits for this one's end by itself
@@ -121,35 +96,30 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         tma_prefetch_map(&map_v);
     }
     if (warp == 0) {                                 // running number of tiles before each sequence
-        int64_t before = 0;
-        if (w.blocks_s)
-            for (int b0 = 0; b0 < p.B; b0 += 32) {
-                const int b = b0 + lane, n = b < p.B ? suffix_len(p, b) : 0;
-                int64_t t = (n + kKeys - 1) / kKeys;
-                if (b < p.B) lens[b] = n;
+        int before = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            const int b = b0 + lane, n = w.blocks_s && b < p.B ? suffix_len(p, b) : 0;
+            int t = n / kKeys + (n % kKeys != 0);
+            if (b < p.B) lens[b] = n;
 #pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const int64_t o = __shfl_up_sync(0xFFFFFFFFu, t, d);
-                    if (lane >= d) t += o;
-                }
-                if (b < p.B) cum[b + 1] = before + t;
-                before += __shfl_sync(0xFFFFFFFFu, t, 31);
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xFFFFFFFFu, t, d);
+                if (lane >= d) t += o;
             }
-        else
-            for (int b = lane; b < p.B; b += 32) cum[b + 1] = 0;
+            if (b < p.B) cum[b + 1] = before + t;
+            before += __shfl_sync(0xFFFFFFFFu, t, 31);
+        }
         if (lane == 0) cum[0] = 0;
     }
     __syncthreads();
     if (blockIdx.x == 0)
         for (int b = threadIdx.x; b <= p.B; b += kThreads) cum_out[b] = cum[b];
 
-    Units n;
-    n.prefix = int64_t(p.Hkv) * w.blocks_p * w.tiles_p;
-    n.per = p.Hkv * w.blocks_s;
-    n.total = n.prefix + cum[p.B] * n.per;
-    const int ctas = n.total < gridDim.x ? int(n.total) : int(gridDim.x);
+    Walk walk(p, w, cum, lens);
+    const int64_t total = walk.total();
+    const int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
     if (int(blockIdx.x) >= ctas) return;
-    const int64_t u0 = n.total * blockIdx.x / ctas, u1 = n.total * (blockIdx.x + 1) / ctas;
+    const int64_t u0 = total * blockIdx.x / ctas, u1 = total * (blockIdx.x + 1) / ctas;
     // a copy brings the rows of one page that fall into a tile
     const int rows_log2 = p.shift < 6 ? p.shift : 6;
     const uint32_t copy_bytes = uint32_t(D * 2) << rows_log2;
@@ -157,44 +127,75 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (warp == kWarps) {
         // ---------------- producer ----------------
         const uint64_t policy = l2_policy_evict_first();
-        int stage = 0;
+        int stage = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
-        int issued = 0;
+        // this lane's page number of an item: entry page0 + lane of its list
+        auto fetch = [&](const Walk& at, int page0) {
+            const int32_t* list = at.b < 0 ? p.prefix_pages : p.table + at.b * p.ld_table;
+            const int n = int((int64_t(at.keys) + (1 << p.shift) - 1) >> p.shift);
+            return page0 + lane < n ? list[page0 + lane] : 0;
+        };
+        int t = walk.seek(u0), page0 = int((int64_t(t) * kKeys) >> p.shift);
+        int mine = fetch(walk, page0);
         for (int64_t u = u0; u < u1 && ok;) {
-            const Segment s = locate(p, w, n, cum, lens, u, u1);
-            const int32_t* pages = s.b < 0 ? p.prefix_pages : p.table + s.b * p.ld_table;
-            const int n_pages = int((int64_t(s.len) + (1 << p.shift) - 1) >> p.shift);
-            int page0 = -32, mine = 0;               // this lane holds the page number of page0 + lane
-            for (int t = s.t0; t < s.t1 && ok; ++t) {
-                const int64_t key0 = int64_t(t) * kKeys;
+            const int t1 = u1 - u < walk.tiles - t ? t + int(u1 - u) : walk.tiles;
+            // the next item's pages are on their way while this one's tiles are requested
+            Walk ahead(walk.p, walk.w, walk.cum, walk.len);
+            ahead.b = walk.b; ahead.kvh = walk.kvh; ahead.block = walk.block; ahead.tiles = walk.tiles; ahead.keys = walk.keys; ahead.item = walk.item;
+            int mine_ahead = 0;
+            const bool more = u + (t1 - t) < u1;
+            if (more) {
+                ahead.next();
+                mine_ahead = fetch(ahead, 0);
+            }
+            const int rows_all = walk.b < 0 ? p.B * p.T * p.G : p.T * p.G;
+            const int rows = rows_all - walk.block * kRows < kRows ? rows_all - walk.block * kRows : kRows;
+            for (int i = t; i < t1 && ok; ++i) {
+                const int64_t key0 = int64_t(i) * kKeys;
                 const int first = int(key0 >> p.shift);
-                if (first >= page0 + 32 || page0 < 0) {
+                if (first >= page0 + 32) {
                     page0 = first;                   // a tile's pages divide 32, so a tile never straddles a reload
-                    mine = page0 + lane < n_pages ? pages[page0 + lane] : 0;
-                    if (mine < 0 || mine >= p.num_pages) {
-                        if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_FORMAT);
-                        mine = 0;
-                    }
+                    mine = fetch(walk, page0);
                 }
-                const int keys = s.len - key0 < kKeys ? int(s.len - key0) : kKeys;
+                int page = __shfl_sync(0xFFFFFFFFu, mine, (first - page0) + (p.shift < 6 ? (lane >> 1) & ((kKeys >> rows_log2) - 1) : 0));
+                const int keys = walk.keys - key0 < kKeys ? int(walk.keys - key0) : kKeys;
                 const int copies = (keys + (1 << rows_log2) - 1) >> rows_log2;
-                const int page = __shfl_sync(0xFFFFFFFFu, mine, (first - page0) + (p.shift < 6 ? (lane >> 1) & ((kKeys >> rows_log2) - 1) : 0));
+                if (lane < 2 * copies && (page < 0 || page >= p.num_pages)) {
+                    if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_FORMAT);
+                    page = 0;
+                }
                 bool free_slot = true;
                 if (lane == 0 && issued >= kStages) free_slot = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status);
                 ok = __shfl_sync(0xFFFFFFFFu, free_slot ? 1 : 0, 0) != 0;
                 if (!ok) break;
                 const uint32_t full = bar_full + 8 * stage;
-                if (lane == 0) mbar_expect_tx(full, uint32_t(copies) * 2u * copy_bytes);
+                const bool opens = i == t;
+                if (lane == 0) {
+                    notes[stage] = Note{walk.item + int(blockIdx.x), int(key0), walk.keys, rows, walk.block,
+                                        (opens ? kFirst : 0) | (i + 1 == t1 ? kLast : 0) | (walk.b < 0 ? 0 : kOwn), 0, 0};
+                    mbar_expect_tx(full, uint32_t(copies) * 2u * copy_bytes + (opens ? uint32_t(rows) * D * 2u : 0u));
+                }
                 __syncwarp();
                 if (lane < 2 * copies) {
                     const uint32_t dst = base + stage * C::kStageBytes + (lane & 1) * C::kOperandBytes + (lane >> 1) * copy_bytes;
-                    tma_load_5d(dst, lane & 1 ? &map_v : &map_k, p.shift < 6 ? 0 : int(key0 & ((1 << p.shift) - 1)), s.kvh, page, full, policy);
+                    tma_load_5d(dst, lane & 1 ? &map_v : &map_k, p.shift < 6 ? 0 : int(key0 & ((1 << p.shift) - 1)), walk.kvh, page, full, policy);
+                }
+                if (opens && lane >= 16 && lane - 16 < rows) {
+                    const int r = walk.block * kRows + lane - 16;
+                    const int64_t tok = (walk.b < 0 ? 0 : int64_t(walk.b) * p.T) + r / p.G;
+                    tma_bulk_load(base + C::kQOffset + stage * C::kQBytes + (lane - 16) * C::kQPitch,
+                                  p.Q + tok * p.ldq + int64_t(walk.kvh * p.G + r % p.G) * D, D * 2, full, policy);
                 }
                 ++issued;
                 if (++stage == kStages) { stage = 0; phase ^= 1u; }
             }
-            u += s.t1 - s.t0;
+            u += t1 - t;
+            if (more) {
+                walk.b = ahead.b; walk.kvh = ahead.kvh; walk.block = ahead.block; walk.tiles = ahead.tiles; walk.keys = ahead.keys; walk.item = ahead.item;
+                t = page0 = 0;
+                mine = mine_ahead;
+            }
         }
         if (*abort_flag) {                           // wait (bounded) for the copies in flight before the CTA may leave
             const uint64_t t0 = global_timer_ns();
@@ -217,124 +218,116 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const uint32_t half_bytes = 128u << rows_log2;
     const uint32_t k_at = uint32_t(krow >> rows_log2) * copy_bytes + uint32_t(krow & in_copy) * 128u, k_sw = krow & 7, k_c = (lane >> 3) & 1;
     const uint32_t v_at = C::kOperandBytes + uint32_t(vrow >> rows_log2) * copy_bytes + uint32_t(vrow & in_copy) * 128u, v_sw = vrow & 7, v_c = lane >> 4;
+    const uint32_t q_at = base + C::kQOffset + (lane & 15) * C::kQPitch + (lane >> 4) * 16u;
 
-    for (int64_t u = u0; u < u1;) {
-        const Segment s = locate(p, w, n, cum, lens, u, u1);
-        u += s.t1 - s.t0;
-        const int rows = s.b < 0 ? p.B * p.T * p.G : p.T * p.G;
-        const int r0 = s.block * kRows + g, r1 = r0 + 8;
-        const int64_t tok0 = s.b < 0 ? 0 : int64_t(s.b) * p.T;
-        uint32_t qa[D / 16][4];
-        {
-            const __nv_bfloat16* q0 = p.Q + (tok0 + r0 / p.G) * p.ldq + int64_t(s.kvh * p.G + r0 % p.G) * D + 2 * t4;
-            const __nv_bfloat16* q1 = p.Q + (tok0 + r1 / p.G) * p.ldq + int64_t(s.kvh * p.G + r1 % p.G) * D + 2 * t4;
+    uint32_t qa[D / 16][4];
+    float o[D / 8][4], m0, m1, l0, l1;
+    int see0 = 0, see1 = 0;                          // keys that the lane's rows see
+    bool failed = false;
+    for (int64_t u = u0; u < u1; ++u) {
+        failed = !mbar_wait(bar_full + 8 * stage, phase, abort_flag, p.status);
+        if (failed) break;
+        const Note n = notes[stage];
+        if (n.flags & kFirst) {
+            // rows past the item's are whatever lies there: their results are never stored
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) ldmatrix4(q_at + stage * C::kQBytes + i * 32, qa[i][0], qa[i][1], qa[i][2], qa[i][3]);
+            const int r0 = n.block * kRows + g;
+            see0 = n.flags & kOwn ? n.keys - (p.T - 1 - r0 / p.G) : n.keys;
+            see1 = n.flags & kOwn ? n.keys - (p.T - 1 - (r0 + 8) / p.G) : n.keys;
+            m0 = m1 = -INFINITY;
+            l0 = l1 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+        }
+        const int key0 = n.key0 + warp * 16, left = n.keys - key0;           // this warp's keys
+        if (left > 0) {
+            const uint32_t sb = base + stage * C::kStageBytes;
+            float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
-                qa[i][0] = r0 < rows ? *reinterpret_cast<const uint32_t*>(q0 + 16 * i) : 0u;
-                qa[i][1] = r1 < rows ? *reinterpret_cast<const uint32_t*>(q1 + 16 * i) : 0u;
-                qa[i][2] = r0 < rows ? *reinterpret_cast<const uint32_t*>(q0 + 16 * i + 8) : 0u;
-                qa[i][3] = r1 < rows ? *reinterpret_cast<const uint32_t*>(q1 + 16 * i + 8) : 0u;
+                uint32_t b0, b1, b2, b3;
+                ldmatrix4(sb + k_at + (i >> 2) * half_bytes + (((uint32_t((i & 3) * 2) + k_c) ^ k_sw) << 4), b0, b1, b2, b3);
+                mma16816(sc[0], qa[i], b0, b1);
+                mma16816(sc[1], qa[i], b2, b3);
+            }
+            const int last = see0 < see1 ? see0 : see1;
+            if (key0 + 16 > last) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int key = key0 + 8 * j + 2 * t4 + e;
+                        if (key >= see0) sc[j][e] = -INFINITY;
+                        if (key >= see1) sc[j][2 + e] = -INFINITY;
+                    }
+            }
+            float x0 = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]));
+            float x1 = fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]));
+            x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1));
+            x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
+            x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2)) * p.scale_log2;
+            x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2)) * p.scale_log2;
+            if (__any_sync(0xFFFFFFFFu, x0 > m0 || x1 > m1)) {
+                const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
+                const float a0 = n0 == -INFINITY ? 1.0f : ex2(m0 - n0), a1 = n1 == -INFINITY ? 1.0f : ex2(m1 - n1);
+                m0 = n0;
+                m1 = n1;
+                l0 *= a0;
+                l1 *= a1;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) { o[i][0] *= a0; o[i][1] *= a0; o[i][2] *= a1; o[i][3] *= a1; }
+            }
+            const float c0 = m0 == -INFINITY ? 0.0f : m0, c1 = m1 == -INFINITY ? 0.0f : m1;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                sc[j][0] = ex2(fmaf(sc[j][0], p.scale_log2, -c0));
+                sc[j][1] = ex2(fmaf(sc[j][1], p.scale_log2, -c0));
+                sc[j][2] = ex2(fmaf(sc[j][2], p.scale_log2, -c1));
+                sc[j][3] = ex2(fmaf(sc[j][3], p.scale_log2, -c1));
+                l0 += sc[j][0] + sc[j][1];
+                l1 += sc[j][2] + sc[j][3];
+            }
+            const uint32_t pa[4] = {pack2(sc[0][0], sc[0][1]), pack2(sc[0][2], sc[0][3]), pack2(sc[1][0], sc[1][1]), pack2(sc[1][2], sc[1][3])};
+            // values past the length may be anything, and 0 times that is not always 0: they are taken as 0
+            uint32_t keep0 = 0xFFFFFFFFu, keep1 = 0xFFFFFFFFu;
+            if (left < 16) {
+                const int k0 = 2 * t4;
+                keep0 = (k0 < left ? 0x0000FFFFu : 0u) | (k0 + 1 < left ? 0xFFFF0000u : 0u);
+                keep1 = (k0 + 8 < left ? 0x0000FFFFu : 0u) | (k0 + 9 < left ? 0xFFFF0000u : 0u);
+            }
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                uint32_t b0, b1, b2, b3;
+                ldmatrix4_trans(sb + v_at + (i >> 2) * half_bytes + (((uint32_t((i & 3) * 2) + v_c) ^ v_sw) << 4), b0, b1, b2, b3);
+                mma16816(o[2 * i], pa, b0 & keep0, b1 & keep1);
+                mma16816(o[2 * i + 1], pa, b2 & keep0, b3 & keep1);
             }
         }
-        // keys a row sees; rows past the item's are computed on zeros and never stored
-        const int see0 = s.b < 0 ? s.len : s.len - (p.T - 1 - r0 / p.G), see1 = s.b < 0 ? s.len : s.len - (p.T - 1 - r1 / p.G);
-        float o[D / 8][4], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-
-        bool failed = false;
-        for (int t = s.t0; t < s.t1; ++t) {
-            failed = !mbar_wait(bar_full + 8 * stage, phase, abort_flag, p.status);
-            if (failed) break;
-            const int key0 = t * kKeys + warp * 16, left = s.len - key0;         // this warp's keys
-            if (left > 0) {
-                const uint32_t sb = base + stage * C::kStageBytes;
-                float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    uint32_t b0, b1, b2, b3;
-                    ldmatrix4(sb + k_at + (i >> 2) * half_bytes + (((uint32_t((i & 3) * 2) + k_c) ^ k_sw) << 4), b0, b1, b2, b3);
-                    mma16816(sc[0], qa[i], b0, b1);
-                    mma16816(sc[1], qa[i], b2, b3);
-                }
-                const int last = see0 < see1 ? see0 : see1;
-                if (key0 + 16 > last) {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int key = key0 + 8 * j + 2 * t4 + e;
-                            if (key >= see0) sc[j][e] = -INFINITY;
-                            if (key >= see1) sc[j][2 + e] = -INFINITY;
-                        }
-                }
-                float x0 = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]));
-                float x1 = fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]));
-                x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1));
-                x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
-                x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2)) * p.scale_log2;
-                x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2)) * p.scale_log2;
-                if (__any_sync(0xFFFFFFFFu, x0 > m0 || x1 > m1)) {
-                    const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
-                    const float a0 = n0 == -INFINITY ? 1.0f : ex2(m0 - n0), a1 = n1 == -INFINITY ? 1.0f : ex2(m1 - n1);
-                    m0 = n0;
-                    m1 = n1;
-                    l0 *= a0;
-                    l1 *= a1;
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) { o[i][0] *= a0; o[i][1] *= a0; o[i][2] *= a1; o[i][3] *= a1; }
-                }
-                const float c0 = m0 == -INFINITY ? 0.0f : m0, c1 = m1 == -INFINITY ? 0.0f : m1;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    sc[j][0] = ex2(fmaf(sc[j][0], p.scale_log2, -c0));
-                    sc[j][1] = ex2(fmaf(sc[j][1], p.scale_log2, -c0));
-                    sc[j][2] = ex2(fmaf(sc[j][2], p.scale_log2, -c1));
-                    sc[j][3] = ex2(fmaf(sc[j][3], p.scale_log2, -c1));
-                    l0 += sc[j][0] + sc[j][1];
-                    l1 += sc[j][2] + sc[j][3];
-                }
-                const uint32_t pa[4] = {pack2(sc[0][0], sc[0][1]), pack2(sc[0][2], sc[0][3]), pack2(sc[1][0], sc[1][1]), pack2(sc[1][2], sc[1][3])};
-                // values past the length may be anything, and 0 times that is not always 0: they are taken as 0
-                uint32_t keep0 = 0xFFFFFFFFu, keep1 = 0xFFFFFFFFu;
-                if (left < 16) {
-                    const int k0 = 2 * t4;
-                    keep0 = (k0 < left ? 0x0000FFFFu : 0u) | (k0 + 1 < left ? 0xFFFF0000u : 0u);
-                    keep1 = (k0 + 8 < left ? 0x0000FFFFu : 0u) | (k0 + 9 < left ? 0xFFFF0000u : 0u);
-                }
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    uint32_t b0, b1, b2, b3;
-                    ldmatrix4_trans(sb + v_at + (i >> 2) * half_bytes + (((uint32_t((i & 3) * 2) + v_c) ^ v_sw) << 4), b0, b1, b2, b3);
-                    mma16816(o[2 * i], pa, b0 & keep0, b1 & keep1);
-                    mma16816(o[2 * i + 1], pa, b2 & keep0, b3 & keep1);
-                }
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_empty + 8 * stage);
-            if (++stage == kStages) { stage = 0; phase ^= 1u; }
-        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_empty + 8 * stage);
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        if (!(n.flags & kLast)) continue;
 
         // the four warps' parts of this share -> one partial result
         l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 1);
         l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 1);
         l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 2);
         l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 2);
-        const int valid = rows - s.block * kRows < kRows ? rows - s.block * kRows : kRows;
+        if (barrier_any(false, 1, 32 * kWarps)) return;          // the join buffer is free; true: a warp gave up, all leave
         float* jo = join_o + (warp * kRows + g) * C::kJoinPitch + 2 * t4;
-        if (g < valid) {
+        if (g < n.rows) {
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2*>(jo + 8 * i) = make_float2(o[i][0], o[i][1]);
             if (t4 == 0) join_ml[warp * kRows + g] = make_float2(m0, l0);
         }
-        if (g + 8 < valid) {
+        if (g + 8 < n.rows) {
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2*>(jo + 8 * C::kJoinPitch + 8 * i) = make_float2(o[i][2], o[i][3]);
             if (t4 == 0) join_ml[warp * kRows + g + 8] = make_float2(m1, l1);
         }
-        if (barrier_any(failed, 1, 32 * kWarps)) return;         // one warp gave up: all leave
-        const int64_t slot = s.item + blockIdx.x;
-        for (int i = threadIdx.x; i < valid * (D / 4); i += 32 * kWarps) {
+        if (barrier_any(false, 1, 32 * kWarps)) return;
+        for (int i = threadIdx.x; i < n.rows * (D / 4); i += 32 * kWarps) {
             const int r = i / (D / 4), c = i - r * (D / 4);
             float mx = -INFINITY, ls = 0.0f;
 #pragma unroll
@@ -348,15 +341,15 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 ls = fmaf(ml.y, a, ls);
                 sum.x = fmaf(v.x, a, sum.x); sum.y = fmaf(v.y, a, sum.y); sum.z = fmaf(v.z, a, sum.z); sum.w = fmaf(v.w, a, sum.w);
             }
-            *reinterpret_cast<float4*>(part_o + (slot * kRows + r) * D + 4 * c) = sum;
-            if (c == 0) part_ml[slot * kRows + r] = make_float2(mx, ls);
+            *reinterpret_cast<float4*>(part_o + (int64_t(n.slot) * kRows + r) * D + 4 * c) = sum;
+            if (c == 0) part_ml[int64_t(n.slot) * kRows + r] = make_float2(mx, ls);
         }
-        consumer_barrier();                          // the join buffer is free again
     }
+    if (failed) barrier_any(true, 1, 32 * kWarps);
 }
 
 // Joins the partial results: one warp per query row and head.
-struct Parts { const float* o; const float2* ml; const int64_t* cum; Line w; int ctas, rows; };
+struct Parts { const float* o; const float2* ml; const int* cum; Line w; int ctas, rows; };
 
 template <int D>
 __global__ void __launch_bounds__(256)
@@ -370,7 +363,7 @@ attn_join_kernel(const Problem p, const Parts parts, __nv_bfloat16* __restrict__
     const int tok = int(row / Hq), hq = int(row - int64_t(tok) * Hq), kvh = hq / p.G, gq = hq - kvh * p.G, b = tok / p.T;
     const Line& w = parts.w;
     const int per = p.Hkv * w.blocks_s;
-    const int64_t prefix = int64_t(p.Hkv) * w.blocks_p * w.tiles_p, total = prefix + parts.cum[p.B] * per;
+    const int64_t prefix = int64_t(p.Hkv) * w.blocks_p * w.tiles_p, total = prefix + int64_t(parts.cum[p.B]) * per;
     const int n = total < parts.ctas ? int(total) : parts.ctas;
 
     float m = -INFINITY, l = 0.0f, acc[V];
@@ -401,7 +394,7 @@ attn_join_kernel(const Problem p, const Parts parts, __nv_bfloat16* __restrict__
     if (w.blocks_s) {
         const int r = (tok - b * p.T) * p.G + gq, blk = r / parts.rows, sub = kvh * w.blocks_s + blk;
         const int64_t tiles = parts.cum[b + 1] - parts.cum[b];
-        add(prefix + parts.cum[b] * per + sub * tiles, tiles, int64_t(p.Hkv) * w.blocks_p + int64_t(b) * per + sub, r - blk * parts.rows);
+        add(prefix + int64_t(parts.cum[b]) * per + sub * tiles, tiles, int64_t(p.Hkv) * w.blocks_p + int64_t(b) * per + sub, r - blk * parts.rows);
     }
     const float inv = l > 0.0f ? 1.0f / l : (l == l ? 0.0f : l);       // nothing seen: 0; NaN stays NaN
     __nv_bfloat16* dst = O + int64_t(tok) * ldo + int64_t(hq) * D + lane * V;
@@ -420,7 +413,7 @@ static Workspace workspace_of(const patch_kv_cache_t* c, int64_t B, int64_t T, i
     const size_t items = size_t(c->Hkv) * (size_t(blocks_of(B * T * G)) + size_t(B) * blocks_of(T * G));
     const size_t slots = items + kMaxCtas;
     Workspace w;
-    w.ml = (size_t(B + 1) * 8 + 255) / 256 * 256;
+    w.ml = (size_t(B + 1) * 4 + 255) / 256 * 256;
     w.o = w.ml + (slots * kRows * 8 + 255) / 256 * 256;
     w.bytes = w.o + slots * kRows * size_t(c->D) * 4;
     return w;
@@ -449,7 +442,7 @@ static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, ui
     const int sms = sm_count();
     if (sms <= 0) return PATCH_ERR_CUDA;
     const int ctas = sms < kMaxCtas ? sms : kMaxCtas;
-    int64_t* cum = reinterpret_cast<int64_t*>(ws);
+    int* cum = reinterpret_cast<int*>(ws);
     float2* ml = reinterpret_cast<float2*>(ws + at.ml);
     float* po = reinterpret_cast<float*>(ws + at.o);
     kern<<<ctas, kThreads, Cfg<D>::smem_bytes(p.B), stream>>>(mk, mv, p, w, po, ml, cum);
@@ -489,6 +482,7 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     if (rc) return rc;
     if (prefix_len < 0 || prefix_len > 0x7FFFFF00 || ld_table < 0 || !(scale > 0.0f) || scale > 3.0e38f) return PATCH_ERR_SHAPE;
     if (B == 0) return PATCH_OK;
+    if (ld_table > 0x7FFFFFFF || B * ((ld_table * cache->page_size + attn::kKeys - 1) / attn::kKeys) > 0x7FFFFFFF) return PATCH_ERR_SHAPE;
     if (!Q || !O || !suffix_lens || (prefix_len && !prefix_pages) || (ld_table && !page_table)) return PATCH_ERR_NULL;
     const int D = cache->D;
     if (ldq < int64_t(Hq) * D || ldo < int64_t(Hq) * D || ldq % 8 || ldo % 8) return PATCH_ERR_SHAPE;
