@@ -1,13 +1,13 @@
 // Shared by the attention kernels: the problem as the kernels see it, the work list (which CTA owns which tiles of which
 // item) and the partial results that the joining kernel adds up.
 //
-// Work list.  An item is a set of query rows of one key head that read the same keys: the batch's rows against the shared
+// Work list.  An item is a set of query rows of one key head that read the same keys: rows of the batch against the shared
 // prefix, or one sequence's rows against its own keys.  An item's keys are cut into tiles; all tiles of all items,
-// item after item, form one line of U units, and CTA c of n owns units [c U / n, (c + 1) U / n): every CTA gets the same number of
-// tiles whatever the lengths are, at the price of items that several CTAs share.  Each CTA writes one partial result
-// (running maximum, sum and unnormalised output, fp32) per item it has a share of.  Along the line the pair (item,
-// CTA) changes one step at a time, so item + c numbers the partial results without gaps worth caring about, and the joining
-// kernel finds an item's partial results from its first and last unit.
+// item after item, form one line of U units, and CTA c of n owns units [c U / n, (c + 1) U / n): every CTA gets the same amount of
+// work whatever the lengths are, at the price of items that several CTAs share.  An item also has a few units without a tile, which
+// stand for what it costs by itself.  Each CTA writes one partial result (running maximum, sum and unnormalised output, fp32)
+// per item it has a share of.  Along the line the pair (item, CTA) changes one step at a time, so item + c numbers the partial
+// results, and the joining kernel finds an item's from the item's first and last tile.
 #pragma once
 #include "sm100_ptx.cuh"
 
@@ -15,7 +15,7 @@ namespace patch {
 namespace attn {
 
 constexpr int kMaxBatch = 2048;
-constexpr int kMaxCtas = 160;                 // CTAs of an attention launch: one per SM, at most these (sizes the workspace)
+constexpr int kMaxSms = 160;                  // sizes the workspace
 
 struct Problem {
     const __nv_bfloat16* Q;
@@ -31,10 +31,17 @@ struct Problem {
     int* status;
 };
 
-// Line of units of one kernel.  rows_p / rows_s: query rows of a prefix / suffix item; blocks of kRows rows are items of their own.
+// The line of units of one kernel.  Blocks of query rows are items of their own.
 struct Line {
-    int blocks_p, blocks_s;                   // row blocks per key head: prefix items (0: none in this kernel), suffix items (0: none)
+    int blocks_p, blocks_s;                   // row blocks per key head: prefix items, suffix items (0: none in this kernel)
     int tiles_p;                              // key tiles of a prefix item
+    int cost;                                 // units of an item beside its tiles
+};
+// Where a kernel's partial results go: of prefix items, of suffix items; `rows` is the row count of a slot.
+struct Parts {
+    float *o_p, *o_s;
+    float2 *ml_p, *ml_s;                      // maximum (in powers of two), sum
+    int rows_p, rows_s;
 };
 
 // len -> clamped length of sequence b's own keys
@@ -47,67 +54,141 @@ __device__ __forceinline__ int suffix_len(const Problem& p, int b) {
     return int(n);
 }
 
-// First unit after which ... the CTA that owns unit u of U spread over n <= U CTAs.
+// Executed by one warp: units before each sequence (one key head, one row block) and the clamped lengths.
+__device__ __forceinline__ void lay_out(const Problem& p, const Line& w, int tile_keys, int* cum, int* lens) {
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+        const int b = b0 + lane, n = w.blocks_s && b < p.B ? suffix_len(p, b) : 0;
+        int t = n / tile_keys + (n % tile_keys != 0);
+        if (t) t += w.cost;
+        if (b < p.B) lens[b] = n;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xFFFFFFFFu, t, d);
+            if (lane >= d) t += o;
+        }
+        if (b < p.B) cum[b + 1] = before + t;
+        before += __shfl_sync(0xFFFFFFFFu, t, 31);
+    }
+    if (lane == 0) cum[0] = 0;
+}
+
+__host__ __device__ __forceinline__ int64_t prefix_units(const Line& w, int Hkv) { return int64_t(Hkv) * w.blocks_p * (w.tiles_p + w.cost); }
+__device__ __forceinline__ int64_t total_units(const Line& w, int Hkv, int cum_all) {
+    return prefix_units(w, Hkv) + int64_t(cum_all) * Hkv * w.blocks_s;
+}
+// The CTA that owns unit u of U spread over n <= U CTAs.
 __device__ __forceinline__ int owner(int64_t u, int64_t U, int n) { return int(((u + 1) * n - 1) / U); }
 
-// The walk of one CTA along the line: the item that holds a unit, and the items after it.  `cum` is the number of key tiles before each
-// sequence (one key head, one row block), `len` the clamped lengths, both in shared memory.
-struct Walk {
+// One CTA's share of the line, item by item.
+struct Share {
     const Problem& p;
     const Line& w;
     const int* cum;
     const int* len;
-    int b, kvh, block, tiles, keys;           // b < 0: the prefix
-    int item;
+    int b, kvh, block, item;                  // b < 0: the prefix; item: number among the prefix's or the suffixes' items
+    int tiles, keys;
+    int t0, t1;                               // the share's tiles of the item
+    int64_t u, u1;                            // the item's first unit, the share's end
 
-    __device__ __forceinline__ Walk(const Problem& p_, const Line& w_, const int* cum_, const int* len_) : p(p_), w(w_), cum(cum_), len(len_) {}
-    __device__ __forceinline__ int64_t prefix_units() const { return int64_t(p.Hkv) * w.blocks_p * w.tiles_p; }
-    __device__ __forceinline__ int per() const { return p.Hkv * w.blocks_s; }          // items of a sequence
-    __device__ __forceinline__ int64_t total() const { return prefix_units() + int64_t(cum[p.B]) * per(); }
+    __device__ __forceinline__ Share(const Problem& p_, const Line& w_, const int* cum_, const int* len_)
+        : p(p_), w(w_), cum(cum_), len(len_), b(-1), kvh(0), block(0), item(0), tiles(0), keys(0), t0(0), t1(0), u(0), u1(0) {}
+    __device__ __forceinline__ void operator=(const Share& o) {
+        b = o.b; kvh = o.kvh; block = o.block; item = o.item; tiles = o.tiles; keys = o.keys; t0 = o.t0; t1 = o.t1; u = o.u; u1 = o.u1;
+    }
     __device__ __forceinline__ void at_sequence(int b_) {
         b = b_;
-        tiles = cum[b + 1] - cum[b];
+        tiles = cum[b + 1] - cum[b] - w.cost;
         keys = len[b];
     }
-    // to the item of unit u; returns the tile
-    __device__ __forceinline__ int seek(int64_t u) {
-        const int64_t before = prefix_units();
-        if (u < before) {
-            item = int(u / w.tiles_p);
+    __device__ __forceinline__ void clip() { const int64_t end = u1 - u - w.cost; t1 = end < tiles ? int(end) : tiles; }
+    // to the first item of units [u0, end) that has a tile among them; false: none
+    __device__ __forceinline__ bool start(int64_t u0, int64_t end) {
+        if (u0 >= end) return false;
+        const int64_t before = prefix_units(w, p.Hkv);
+        int place;                            // of u0 among its item's units
+        if (u0 < before) {
+            const int each = w.tiles_p + w.cost;
+            item = int(u0 / each);
             b = -1;
             kvh = item / w.blocks_p;
             block = item - kvh * w.blocks_p;
             tiles = w.tiles_p;
             keys = p.prefix_len;
-            return int(u - int64_t(item) * w.tiles_p);
+            place = int(u0 - int64_t(item) * each);
+        } else {
+            const int per = p.Hkv * w.blocks_s;
+            const int64_t v = u0 - before, q = v / per;
+            int lo = 0, hi = p.B;             // the sequence with cum[lo] <= q < cum[lo + 1]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (cum[mid] <= q) lo = mid; else hi = mid;
+            }
+            at_sequence(lo);
+            const int64_t r = v - int64_t(cum[lo]) * per;
+            const int each = tiles + w.cost, sub = int(r / each);
+            kvh = sub / w.blocks_s;
+            block = sub - kvh * w.blocks_s;
+            item = lo * per + sub;
+            place = int(r - int64_t(sub) * each);
         }
-        const int64_t v = u - before, q = v / per();
-        int lo = 0, hi = p.B;                 // the sequence with cum[lo] <= q < cum[lo + 1]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (cum[mid] <= q) lo = mid; else hi = mid;
-        }
-        at_sequence(lo);
-        const int64_t r = v - int64_t(cum[lo]) * per();
-        const int sub = int(r / tiles);
-        kvh = sub / w.blocks_s;
-        block = sub - kvh * w.blocks_s;
-        item = p.Hkv * w.blocks_p + lo * per() + sub;
-        return int(r - int64_t(sub) * tiles);
+        u = u0 - place;
+        u1 = end;
+        t0 = place < w.cost ? 0 : place - w.cost;
+        clip();
+        return t0 < t1 || next();
     }
-    // to the next item that has tiles (there is one)
-    __device__ __forceinline__ void next() {
+    // to the next item with a tile in the share; false: none
+    __device__ __forceinline__ bool next() {
+        u += tiles + w.cost;
+        if (u + w.cost >= u1) return false;
         ++item;
-        if (++block < (b < 0 ? w.blocks_p : w.blocks_s)) return;
-        block = 0;
-        if (++kvh < p.Hkv) return;
-        kvh = 0;
-        int n = b + 1;
-        while (n + 1 < p.B && cum[n + 1] == cum[n]) ++n;
-        item = p.Hkv * w.blocks_p + n * per();
-        at_sequence(n);
+        if (++block == (b < 0 ? w.blocks_p : w.blocks_s)) {
+            block = 0;
+            if (++kvh == p.Hkv) {
+                kvh = 0;
+                int n = b + 1;                // u < u1: there is a sequence with tiles
+                while (n + 1 < p.B && cum[n + 1] == cum[n]) ++n;
+                item = n * p.Hkv * w.blocks_s;
+                at_sequence(n);
+            }
+        }
+        t0 = 0;
+        clip();
+        return true;
     }
+    __device__ __forceinline__ int rows() const { return b < 0 ? p.B * p.T * p.G : p.T * p.G; }
+    __device__ __forceinline__ const int32_t* list() const { return b < 0 ? p.prefix_pages : p.table + b * p.ld_table; }
+    __device__ __forceinline__ int pages() const { return int((int64_t(keys) + (1 << p.shift) - 1) >> p.shift); }
 };
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// rows of one page (and of one half or all halves, by the map's box) of one head -> shared memory
+__device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* map, int row, int half, int head, int page, uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
+        ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(bar), "l"(policy) : "memory");
+}
+
+// Items of at most kFewRows query rows per key head go to the decode kernel (attention_decode_sm100.cu), others to the block
+// kernel (attention_block_sm100.cu).
+constexpr int kFewRows = 16;
+constexpr int kBlockRows = 256;
+constexpr int kDecodeKeys = 64, kBlockKeys = 128;     // keys of a tile
+constexpr int kDecodeCost = 1, kBlockCost = 1;        // Line::cost
+int decode_ctas(int sms);
+int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, bool after_block, cudaStream_t s);
+int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, cudaStream_t s);
 
 }  // namespace attn
 

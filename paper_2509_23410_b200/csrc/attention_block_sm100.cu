@@ -1,0 +1,457 @@
+// Attention over the paged cache for items of more than 16 query rows: the batch's rows of one key head against the shared prefix,
+// or the drafted tokens of one sequence against its own keys (public header: patch_prefix_attention; the work list and the partial
+// results are described in attention.cuh).
+//
+// Mathematics.  As in the decode kernel: running maximum m, sum l and unnormalised output o of every row, fp32, scores in powers of
+// two.  m is only raised when the scores of a tile exceed it by more than 8 (a factor of 256, harmless in fp32 and
+// for the bf16 probabilities, whose relative rounding does not depend on their size), so the accumulator is rarely rescaled.
+//
+// Kernel.  One CTA per SM, 128 query rows and 128 keys per tcgen05.mma, two streams x = 0, 1 of
+//     S_x = Q_x K^T (shared x shared -> TMEM),  P_x = 2^(S_x - m) (TMEM -> registers -> TMEM, over S_x),  O_x += P_x V (TMEM x shared)
+// so that one stream multiplies while the other is in its softmax.  An item of more than 128 rows gives each stream 128 rows, both
+// read the same keys; an item of fewer gives both streams the same rows and every second tile of keys, and the
+// two results are joined in TMEM at the end.
+//   warp 0       producer: tiles of keys and values, one TMA box per page and 64-element half, into a ring of four 32 KB stages (D = 128)
+//   warp 1       issues the MMAs; zeroes the rows of V past the item's last key (a probability of 0 times whatever the
+//                cache holds there is not always 0)
+//   warps 4..7   softmax of stream 0, one thread per row; warps 8..11 stream 1.  They also bring an item's query rows into the
+//                swizzled layout (any head count per key head, any row pitch) and write its partial result.
+// What bounds it: HBM up to about 256 rows per key head -- 64 KB of keys and values per tile and SM take 2 850 cycles, its
+// four products (two streams) 2 048, the exponentials 2 048.
+#include "attention.cuh"
+
+namespace patch {
+namespace attn {
+namespace blk {
+
+constexpr int kKeys = kBlockKeys;
+constexpr int kRing = 4;
+constexpr int kThreads = 384;
+constexpr uint32_t kTmemCols = 512;                   // S_0, S_1 at 0, 128; O_0, O_1 at 256, 384
+constexpr float kSlack = 8.0f;                        // powers of two the running maximum may lag behind
+
+template <int D> struct Cfg {
+    static constexpr uint32_t kAtom = 128 * 128;      // 128 rows x 64 elements
+    static constexpr uint32_t kTile = kKeys * D * 2;  // one operand of a key tile = one ring stage
+    static constexpr uint32_t kQTile = 128 * D * 2;
+    static constexpr uint32_t kQOffset = kRing * kTile;
+    static constexpr uint32_t kMlOffset = kQOffset + 2 * kQTile;             // (m, l) of both streams' rows, to join them
+    static constexpr uint32_t kBarOffset = kMlOffset + 2 * 128 * 8;
+    static constexpr uint32_t kCumOffset = kBarOffset + 256;
+    static constexpr uint32_t kFixedBytes = kCumOffset + 1024;
+    static uint32_t smem_bytes(int B) { return kFixedBytes + uint32_t(2 * B + 1) * 4; }
+};
+
+// MN-major operand in 128-byte-swizzled atoms of 64 elements x 8 rows (the rows are the product's K): start address, stride between
+// the 64-element atoms, stride between groups of eight rows.
+__device__ __forceinline__ uint64_t desc_mnmajor_sw128(uint32_t saddr, uint32_t atom_stride) {
+    return uint64_t((saddr & 0x3FFFFu) >> 4) | (uint64_t(atom_stride >> 4) << 16) | (uint64_t(1024 >> 4) << 32) |
+           (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+// D[tmem] (+)= A[tmem] * B[smem]: lane = row of A, a 32-bit column holds two consecutive K elements
+__device__ __forceinline__ void mma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+#define PATCH_R32(v) "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), \
+    "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), \
+    "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+#define PATCH_S32(v) "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), \
+    "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), \
+    "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+// 32 lanes x 32 consecutive 32-bit columns <-> 32 registers per thread (thread = lane)
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+        "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];" : PATCH_R32(v) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+        "%24,%25,%26,%27,%28,%29,%30,%31};" ::PATCH_S32(v), "r"(taddr) : "memory");
+}
+#undef PATCH_R32
+#undef PATCH_S32
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void st_global32(float* p, const float (&v)[8]) {
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]),
+                 "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}
+
+// Number of a stream's tiles among n: all of them where each stream has rows of its own, else every second.
+__device__ __forceinline__ int stream_tiles(int n, bool dual, int x) { return dual ? n : (n + 1 - x) >> 1; }
+
+}  // namespace blk
+
+template <int D>
+__global__ void __launch_bounds__(blk::kThreads, 1)
+attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const Line w,
+                  const Parts parts, int* __restrict__ cum_out) {
+    using namespace blk;
+    using C = Cfg<D>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t bar_full = base + C::kBarOffset, bar_empty = bar_full + 8 * kRing, bar_q = bar_empty + 8 * kRing, bar_s = bar_q + 8,
+                   bar_p = bar_s + 16, bar_o = bar_p + 16;
+    uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::kBarOffset + 192);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
+    int* cum = reinterpret_cast<int*>(smem + C::kCumOffset);
+    int* lens = cum + p.B + 1;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    grid_launch_dependents();
+    if (threadIdx.x == 32) {
+        for (int i = 0; i < kRing; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+        mbar_init(bar_q, 8);                                   // one arrival per softmax warp
+        for (int x = 0; x < 2; ++x) { mbar_init(bar_s + 8 * x, 1); mbar_init(bar_p + 8 * x, 4); }
+        mbar_init(bar_o, 1);
+        *abort_flag = 0;
+        mbar_init_fence();
+        tma_prefetch_map(&map_k);
+        tma_prefetch_map(&map_v);
+    }
+    if (warp == 0) lay_out(p, w, kKeys, cum, lens);
+    if (warp == 2) tmem_alloc(smem_u32(misc), kTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *misc;
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b <= p.B; b += kThreads) cum_out[b] = cum[b];
+
+    const int64_t total = total_units(w, p.Hkv, cum[p.B]);
+    const int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
+    const bool busy = int(blockIdx.x) < ctas;
+    const int64_t u0 = busy ? total * blockIdx.x / ctas : 0, u1 = busy ? total * (blockIdx.x + 1) / ctas : 0;
+    Share s(p, w, cum, lens);
+
+    if (warp == 0) {
+        // ---------------- producer: K0 K1 V0 K2 V1 ... (one stream's rows twice) or K0 V0 K1 V1 ... ----------------
+        const uint64_t policy = l2_policy_evict_first();
+        const int rows_log2 = p.shift < 7 ? p.shift : 7;       // rows of a box: what one page gives to a tile
+        const uint32_t box_bytes = 128u << rows_log2;
+        int stage = 0, issued = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (bool have = s.start(u0, u1); have && ok; have = s.next()) {
+            const int n_pages = s.pages();
+            const bool dual = s.rows() - s.block * kBlockRows > 128;
+            const int n = s.t1 - s.t0;
+            // page numbers of the item's K tiles and V tiles, one per lane; the two run one or two tiles apart
+            int at[2] = {-64, -64}, mine[2] = {0, 0};
+            auto load = [&](int i, int v) {                    // tile i of the share, v = 0: keys, 1: values
+                const int64_t key0 = int64_t(s.t0 + i) * kKeys;
+                const int first = int(key0 >> p.shift);
+                if (first >= at[v] + 32 || at[v] < 0) {
+                    at[v] = first;
+                    mine[v] = first + lane < n_pages ? s.list()[first + lane] : 0;
+                }
+                const int box = lane >> 1;                     // lane: box of the tile, half
+                int page = __shfl_sync(0xFFFFFFFFu, mine[v], (first - at[v]) + (p.shift < 7 ? box & ((kKeys >> rows_log2) - 1) : 0));
+                const int keys = s.keys - key0 < kKeys ? int(s.keys - key0) : kKeys;
+                const int boxes = (keys + (1 << rows_log2) - 1) >> rows_log2;
+                const bool on = box < boxes && (lane & 1) < D / 64;
+                if (on && (page < 0 || page >= p.num_pages)) {
+                    if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_FORMAT);
+                    page = 0;
+                }
+                bool free_slot = true;
+                if (lane == 0 && issued >= kRing) free_slot = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status);
+                ok = __shfl_sync(0xFFFFFFFFu, free_slot ? 1 : 0, 0) != 0;
+                if (!ok) return;
+                const uint32_t full = bar_full + 8 * stage;
+                if (lane == 0) mbar_expect_tx(full, uint32_t(boxes) * uint32_t(D / 64) * box_bytes);
+                __syncwarp();
+                if (on)
+                    tma_load_page(base + stage * C::kTile + (lane & 1) * C::kAtom + box * box_bytes, v ? &map_v : &map_k,
+                                  p.shift < 7 ? 0 : int(key0 & ((1 << p.shift) - 1)), lane & 1, s.kvh, page, full, policy);
+                ++issued;
+                if (++stage == kRing) { stage = 0; phase ^= 1u; }
+            };
+            const int lead = dual ? 1 : 2;
+            for (int i = 0; i < lead && i < n && ok; ++i) load(i, 0);
+            for (int i = 0; i < n && ok; ++i) {
+                load(i, 1);
+                if (i + lead < n && ok) load(i + lead, 0);
+            }
+        }
+        if (*abort_flag) {
+            const uint64_t t0 = global_timer_ns();
+            for (int j = issued > kRing ? issued - kRing : 0; j < issued; ++j)
+                while (!mbar_try_wait(bar_full + 8 * (j % kRing), uint32_t(j / kRing) & 1u) && global_timer_ns() - t0 < kDrainLimitNs) {}
+        }
+    } else if (warp == 1) {
+        // ---------------- MMAs ----------------
+        constexpr uint32_t idesc_s = instr_desc(kKeys, false), idesc_o = instr_desc(D, false) | (1u << 16);      // V is MN-major
+        int stage = 0;
+        uint32_t phase = 0, phase_q = 0, phase_p[2] = {0, 0};
+        bool ok = true;
+        auto wait = [&](uint32_t bar, uint32_t parity) {       // the whole warp goes on together
+            bool good = true;
+            if (lane == 0) good = mbar_wait(bar, parity, abort_flag, p.status);
+            ok = ok && __shfl_sync(0xFFFFFFFFu, good ? 1 : 0, 0) != 0;
+            tc_fence_after();
+        };
+        auto advance = [&] { if (++stage == kRing) { stage = 0; phase ^= 1u; } };
+        auto scores = [&](int x, uint32_t q_tile, uint32_t k_tile) {
+            const uint64_t dq = desc_kmajor_sw128(q_tile), dk = desc_kmajor_sw128(k_tile);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const uint64_t off = uint64_t(((ks >> 2) * C::kAtom + (ks & 3) * 32) >> 4);
+                mma_dense(tmem + 128u * x, dq + off, dk + off, idesc_s, ks != 0);
+            }
+            mma_commit(bar_s + 8 * x);
+        };
+        auto outputs = [&](int x, uint32_t v_tile, bool first) {
+            const uint64_t dv = desc_mnmajor_sw128(v_tile, C::kAtom);
+#pragma unroll
+            for (int ks = 0; ks < kKeys / 16; ++ks)
+                mma_ta(tmem + 256u + 128u * x, tmem + 128u * x + 8u * ks, dv + uint64_t((ks * 2048) >> 4), idesc_o, !(first && ks == 0));
+        };
+        for (bool have = s.start(u0, u1); have && ok; have = s.next()) {
+            const bool dual = s.rows() - s.block * kBlockRows > 128;
+            const int n = s.t1 - s.t0, lead = dual ? 1 : 2;
+            const uint32_t q0 = base + C::kQOffset, q1 = dual ? q0 + C::kQTile : q0;
+            wait(bar_q, phase_q);
+            phase_q ^= 1u;
+            for (int i = 0; i < lead && i < n && ok; ++i) {
+                wait(bar_full + 8 * stage, phase);
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t k_tile = base + stage * C::kTile;
+                    if (dual || i == 0) scores(0, q0, k_tile);
+                    if (dual || i == 1) scores(1, q1, k_tile);
+                    mma_commit(bar_empty + 8 * stage);
+                }
+                __syncwarp();
+                advance();
+            }
+            for (int i = 0; i < n && ok; ++i) {
+                wait(bar_full + 8 * stage, phase);
+                if (!ok) break;
+                const uint32_t v_tile = base + stage * C::kTile, v_empty = bar_empty + 8 * stage;
+                advance();
+                const int valid = s.keys - (s.t0 + i) * kKeys;
+                if (valid < kKeys) {                           // rows past the last key: zeros
+                    for (int j = valid * (D / 8) + lane; j < kKeys * (D / 8); j += 32) {
+                        const int r = j / (D / 8), c = j - r * (D / 8);
+                        *reinterpret_cast<uint4*>(smem + (v_tile - base) + (c >> 3) * C::kAtom + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    fence_async_shared();
+                    __syncwarp();
+                }
+                const bool more = i + lead < n;
+                const uint32_t k_stage = stage;
+                for (int y = 0; y < (dual ? 2 : 1) && ok; ++y) {
+                    const int x = dual ? y : i & 1;
+                    wait(bar_p + 8 * x, phase_p[x]);
+                    phase_p[x] ^= 1u;
+                    if (!ok) break;
+                    if (more && y == 0) {
+                        // the products go out first where the keys are still on their way
+                        if (lane == 0) outputs(x, v_tile, dual ? i == 0 : i < 2);
+                        __syncwarp();
+                        if (!dual && lane == 0) mma_commit(v_empty);
+                        wait(bar_full + 8 * k_stage, phase);
+                        if (!ok) break;
+                        advance();
+                        if (lane == 0) {
+                            scores(x, x ? q1 : q0, base + k_stage * C::kTile);
+                            if (!dual) mma_commit(bar_empty + 8 * k_stage);
+                        }
+                    } else if (lane == 0) {
+                        outputs(x, v_tile, dual ? i == 0 : i < 2);
+                        if (!dual || y == 1) mma_commit(v_empty);
+                        if (more) {
+                            scores(x, x ? q1 : q0, base + k_stage * C::kTile);
+                            mma_commit(bar_empty + 8 * k_stage);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            if (ok && lane == 0) mma_commit(bar_o);
+            __syncwarp();
+        }
+    } else if (warp >= 4) {
+        // ---------------- softmax: thread = row of the stream ----------------
+        const int x = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t lanes = uint32_t(quad * 32) << 16;
+        const uint32_t t_s = tmem + lanes + 128u * x, t_o = tmem + lanes + 256u + 128u * x;
+        float2* ml = reinterpret_cast<float2*>(smem + C::kMlOffset);
+        uint32_t phase_s = 0, phase_o = 0;
+        bool failed = false;
+        for (bool have = s.start(u0, u1); have && !failed; have = s.next()) {
+            const int rows = s.rows() - s.block * kBlockRows;  // of this block and the ones after it
+            const bool dual = rows > 128;
+            const int n = s.t1 - s.t0, mine = stream_tiles(n, dual, x);
+            const int r = s.block * kBlockRows + (dual ? 128 * x : 0) + row;     // row of the item
+            const bool valid = r < s.rows();
+            // the query rows, 16 bytes at a time, into the swizzled layout; rows past the item's are zeros
+            if (dual || x == 0) {
+                const int64_t tok = (s.b < 0 ? 0 : int64_t(s.b) * p.T) + r / p.G;
+                const __nv_bfloat16* src = p.Q + tok * p.ldq + int64_t(s.kvh * p.G + r % p.G) * D;
+                uint8_t* dst = smem + C::kQOffset + x * C::kQTile;
+                uint4 v[D / 8];
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) v[c] = valid ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(dst + (c >> 3) * C::kAtom + atom_chunk_offset(row, c & 7)) = v[c];
+                fence_async_shared();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_q);
+            const int see = s.b < 0 ? s.keys : s.keys - (p.T - 1 - r / p.G);      // keys the row sees
+            float m = -INFINITY, l = 0.0f;
+            for (int j = 0; j < mine; ++j) {
+                failed = !mbar_wait(bar_s + 8 * x, phase_s, abort_flag, p.status);
+                failed = __any_sync(0xFFFFFFFFu, failed);
+                if (failed) break;
+                phase_s ^= 1u;
+                tc_fence_after();
+                uint32_t v[4][32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_ld32(t_s + 32u * q, v[q]);
+                tmem_ld_wait();
+                const int key0 = (s.t0 + (dual ? j : 2 * j + x)) * kKeys;
+                if (key0 + kKeys > see) {
+                    const int left = see - key0;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (32 * q + c >= left) v[q][c] = 0xFF800000u;        // -inf
+                }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(v[q][c]));
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+                if (__any_sync(0xFFFFFFFFu, top > m + kSlack)) {
+                    const float up = fmaxf(m, top), a = up == -INFINITY ? 1.0f : ex2(m - up);
+                    m = up;
+                    l *= a;
+                    if (j > 0) {                               // the scores were issued behind the last product, which is done
+#pragma unroll
+                        for (int q = 0; q < D / 32; ++q) {
+                            uint32_t o[32];
+                            tmem_ld32(t_o + 32u * q, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * a);
+                            tmem_st32(t_o + 32u * q, o);
+                        }
+                    }
+                }
+                const float off = m == -INFINITY ? 0.0f : -m;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                // the probabilities take the place of scores that have been read: two in a register
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        const float e0 = ex2(fmaf(__uint_as_float(v[q][c]), p.scale_log2, off));
+                        const float e1 = ex2(fmaf(__uint_as_float(v[q][c + 1]), p.scale_log2, off));
+                        sum[c & 2] += e0;
+                        sum[(c & 2) + 1] += e1;
+                        v[q >> 1][(q & 1) * 16 + (c >> 1)] = pack2(e0, e1);
+                    }
+                tmem_st32(t_s, v[0]);
+                tmem_st32(t_s + 32u, v[1]);
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_p + 8 * x);
+            }
+            if (!failed) failed = !mbar_wait(bar_o, phase_o, abort_flag, p.status);
+            phase_o ^= 1u;
+            tc_fence_after();
+            ml[128 * x + row] = make_float2(m, l);
+            if (barrier_any(failed, 1, 256)) { failed = true; break; }
+            // ---- the partial result ----
+            const bool own = s.b >= 0;
+            const int64_t slot = s.item + int64_t(blockIdx.x);
+            const int rows_slot = own ? parts.rows_s : parts.rows_p;
+            const int64_t at = slot * rows_slot + (dual ? 128 * x : 0) + row;
+            float* dst = (own ? parts.o_s : parts.o_p) + at * D;
+            if (dual) {
+#pragma unroll
+                for (int q = 0; q < D / 32; ++q) {
+                    uint32_t o[32];
+                    tmem_ld32(t_o + 32u * q, o);
+                    tmem_ld_wait();
+                    if (valid) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 8) {
+                            float f[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[c + i]);
+                            st_global32(dst + 32 * q + c, f);
+                        }
+                    }
+                }
+                if (valid) (own ? parts.ml_s : parts.ml_p)[at] = make_float2(m, l);
+            } else {
+                // both streams hold a part of the same rows: each takes half of the columns of both
+                const float2 a = ml[row], b = ml[128 + row];
+                const float mx = fmaxf(a.x, b.x);
+                const float fa = a.x == -INFINITY ? 0.0f : ex2(a.x - mx), fb = b.x == -INFINITY ? 0.0f : ex2(b.x - mx);
+#pragma unroll
+                for (int q = 0; q < D / 64; ++q) {
+                    const uint32_t col = uint32_t(x) * (D / 2) + 32u * q;
+                    uint32_t o0[32], o1[32];
+                    tmem_ld32(tmem + lanes + 256u + col, o0);
+                    if (n > 1) tmem_ld32(tmem + lanes + 384u + col, o1);
+                    tmem_ld_wait();
+                    if (valid) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 8) {
+                            float f[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                f[i] = __uint_as_float(o0[c + i]) * fa + (n > 1 ? __uint_as_float(o1[c + i]) * fb : 0.0f);
+                            st_global32(dst + col + c, f);
+                        }
+                    }
+                }
+                if (valid && x == 0) (own ? parts.ml_s : parts.ml_p)[at] = make_float2(mx, a.y * fa + b.y * fb);
+            }
+            tc_fence_before();
+            if (barrier_any(false, 1, 256)) { failed = true; break; }             // nobody's accumulators are read any more
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 2) tmem_dealloc(tmem, blk::kTmemCols);
+}
+
+template <int D>
+static int launch_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, cudaStream_t stream) {
+    using C = blk::Cfg<D>;
+    CUtensorMap mk, mv;
+    const int rows = c->page_size < blk::kKeys ? c->page_size : blk::kKeys;
+    int rc = make_kv_tensor_map(&mk, c, c->k_dev, rows, 1);
+    if (!rc) rc = make_kv_tensor_map(&mv, c, c->v_dev, rows, 1);
+    if (rc) return rc;
+    auto kern = attn_block_kernel<D>;
+    static std::atomic<uint64_t> configured{0};
+    if ((rc = allow_dynamic_smem(kern, C::smem_bytes(kMaxBatch), configured))) return rc;
+    const int sms = sm_count();
+    if (sms <= 0) return PATCH_ERR_CUDA;
+    kern<<<sms < kMaxSms ? sms : kMaxSms, blk::kThreads, C::smem_bytes(p.B), stream>>>(mk, mv, p, w, parts, cum_out);
+    return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+}
+
+int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, cudaStream_t s) {
+    return c->D == 128 ? launch_block<128>(c, p, w, parts, cum_out, s) : launch_block<64>(c, p, w, parts, cum_out, s);
+}
+
+}  // namespace attn
+}  // namespace patch

@@ -1,5 +1,5 @@
-// Attention over the paged cache for items of few query rows (public header: patch_prefix_attention), the kernel that joins the
-// partial results, and the entry points.
+// Attention over the paged cache for items of at most 16 query rows (public header: patch_prefix_attention; the work list and the
+// partial results are described in attention.cuh).
 //
 // Mathematics.  For every row the running maximum m of the scaled scores (in powers of two), the sum l of 2^(s - m) and the
 // unnormalised output o = sum 2^(s - m) v; parts of the keys are joined with weights 2^(m_i - m).  All three are fp32; the
@@ -9,7 +9,8 @@
 // of 64 keys and values with TMA, one copy per page and operand, into a ring of stages, and with an item's first tile the
 // item's query rows; a note in the stage says what the tile is.  Warps 0..3 each take 16 of the 64 keys: S = Q K^T
 // (16 rows x 16 keys), probabilities in registers, O += P V, with a maximum of their own, so that within an item no warp waits
-// for another.  At the end of a share the four warps' results are joined in shared memory.
+// for another.  At the end of a share the four warps' results are joined in shared memory.  Two CTAs share an SM, so that one
+// streams while the other hands an item over.
 // What bounds it: HBM.  A 64-key tile is 32 KB (D = 128), about 1 430 cycles of an SM's share of the bandwidth; its
 // 32 + 32 products of 16 x 8 x 16 per warp and the softmax of 16 x 16 scores take half of that.  Batches with many short
 // items live off the hand-over between items: with every warp looking its items up and fetching their queries itself, an
@@ -19,9 +20,9 @@
 namespace patch {
 namespace attn {
 
-constexpr int kRows = 16;                     // query rows of an item
-constexpr int kKeys = 64;                     // keys of a tile
-constexpr int kStages = 4;
+constexpr int kRows = kFewRows;               // query rows of an item
+constexpr int kKeys = kDecodeKeys;
+constexpr int kStages = 2;
 constexpr int kWarps = 4;                     // consuming warps
 constexpr int kThreads = 32 * (kWarps + 1);
 
@@ -42,8 +43,8 @@ template <int D> struct Cfg {
     static uint32_t smem_bytes(int B) { return kFixedBytes + uint32_t(2 * B + 1) * 4; }
 };
 // What a stage holds.
-struct Note { int slot, key0, keys, rows, block, flags, pad0, pad1; };
-constexpr int kFirst = 1, kLast = 2, kOwn = 4;        // first / last tile of the CTA's share of an item; the sequence's own keys
+struct Note { int slot, key0, keys, rows, flags, pad[3]; };
+constexpr int kFirst = 1, kLast = 2, kOwn = 4, kEnd = 8;   // first / last tile of the CTA's share of an item; the sequence's own keys; no tile: the end
 static_assert(sizeof(Note) == 32, "note");
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
@@ -57,25 +58,11 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int row, int head, int page, uint32_t bar, uint64_t policy) {
-    asm volatile(
-        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-        " [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
-        ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(0), "r"(head), "r"(page), "r"(bar), "l"(policy) : "memory");
-}
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+// AFTER: launched behind the block kernel, which need not have ended when this one starts; it ends after it.
+template <int D, bool AFTER>
+__global__ void __launch_bounds__(kThreads, 2)
 attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const Line w,
-                   float* __restrict__ part_o, float2* __restrict__ part_ml, int* __restrict__ cum_out) {
+                   const Parts parts, int* __restrict__ cum_out) {
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -95,71 +82,49 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         tma_prefetch_map(&map_k);
         tma_prefetch_map(&map_v);
     }
-    if (warp == 0) {                                 // running number of tiles before each sequence
-        int before = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 32) {
-            const int b = b0 + lane, n = w.blocks_s && b < p.B ? suffix_len(p, b) : 0;
-            int t = n / kKeys + (n % kKeys != 0);
-            if (b < p.B) lens[b] = n;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up_sync(0xFFFFFFFFu, t, d);
-                if (lane >= d) t += o;
-            }
-            if (b < p.B) cum[b + 1] = before + t;
-            before += __shfl_sync(0xFFFFFFFFu, t, 31);
-        }
-        if (lane == 0) cum[0] = 0;
-    }
+    if (warp == 0) lay_out(p, w, kKeys, cum, lens);
     __syncthreads();
     if (blockIdx.x == 0)
         for (int b = threadIdx.x; b <= p.B; b += kThreads) cum_out[b] = cum[b];
 
-    Walk walk(p, w, cum, lens);
-    const int64_t total = walk.total();
+    const int64_t total = total_units(w, p.Hkv, cum[p.B]);
     const int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
-    if (int(blockIdx.x) >= ctas) return;
-    const int64_t u0 = total * blockIdx.x / ctas, u1 = total * (blockIdx.x + 1) / ctas;
+    const bool busy = int(blockIdx.x) < ctas;
     // a copy brings the rows of one page that fall into a tile
     const int rows_log2 = p.shift < 6 ? p.shift : 6;
     const uint32_t copy_bytes = uint32_t(D * 2) << rows_log2;
 
     if (warp == kWarps) {
         // ---------------- producer ----------------
+        if (!busy) {
+            if (AFTER && blockIdx.x == 0) grid_dependency_wait();
+            return;
+        }
         const uint64_t policy = l2_policy_evict_first();
         int stage = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
         // this lane's page number of an item: entry page0 + lane of its list
-        auto fetch = [&](const Walk& at, int page0) {
-            const int32_t* list = at.b < 0 ? p.prefix_pages : p.table + at.b * p.ld_table;
-            const int n = int((int64_t(at.keys) + (1 << p.shift) - 1) >> p.shift);
-            return page0 + lane < n ? list[page0 + lane] : 0;
-        };
-        int t = walk.seek(u0), page0 = int((int64_t(t) * kKeys) >> p.shift);
-        int mine = fetch(walk, page0);
-        for (int64_t u = u0; u < u1 && ok;) {
-            const int t1 = u1 - u < walk.tiles - t ? t + int(u1 - u) : walk.tiles;
+        auto fetch = [&](const Share& s, int page0) { return page0 + lane < s.pages() ? s.list()[page0 + lane] : 0; };
+        Share s(p, w, cum, lens), ahead(s);
+        bool have = s.start(total * blockIdx.x / ctas, total * (blockIdx.x + 1) / ctas);
+        int page0 = have ? int((int64_t(s.t0) * kKeys) >> p.shift) : 0;
+        int mine = have ? fetch(s, page0) : 0;
+        while (have && ok) {
             // the next item's pages are on their way while this one's tiles are requested
-            Walk ahead(walk.p, walk.w, walk.cum, walk.len);
-            ahead.b = walk.b; ahead.kvh = walk.kvh; ahead.block = walk.block; ahead.tiles = walk.tiles; ahead.keys = walk.keys; ahead.item = walk.item;
+            ahead = s;
+            const bool more = ahead.next();
             int mine_ahead = 0;
-            const bool more = u + (t1 - t) < u1;
-            if (more) {
-                ahead.next();
-                mine_ahead = fetch(ahead, 0);
-            }
-            const int rows_all = walk.b < 0 ? p.B * p.T * p.G : p.T * p.G;
-            const int rows = rows_all - walk.block * kRows < kRows ? rows_all - walk.block * kRows : kRows;
-            for (int i = t; i < t1 && ok; ++i) {
+            if (more) mine_ahead = ahead.b == s.b && page0 == 0 ? mine : fetch(ahead, 0);      // another head: the same list
+            for (int i = s.t0; i < s.t1 && ok; ++i) {
                 const int64_t key0 = int64_t(i) * kKeys;
                 const int first = int(key0 >> p.shift);
                 if (first >= page0 + 32) {
                     page0 = first;                   // a tile's pages divide 32, so a tile never straddles a reload
-                    mine = fetch(walk, page0);
+                    mine = fetch(s, page0);
                 }
                 int page = __shfl_sync(0xFFFFFFFFu, mine, (first - page0) + (p.shift < 6 ? (lane >> 1) & ((kKeys >> rows_log2) - 1) : 0));
-                const int keys = walk.keys - key0 < kKeys ? int(walk.keys - key0) : kKeys;
+                const int keys = s.keys - key0 < kKeys ? int(s.keys - key0) : kKeys;
                 const int copies = (keys + (1 << rows_log2) - 1) >> rows_log2;
                 if (lane < 2 * copies && (page < 0 || page >= p.num_pages)) {
                     if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_FORMAT);
@@ -170,33 +135,37 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 ok = __shfl_sync(0xFFFFFFFFu, free_slot ? 1 : 0, 0) != 0;
                 if (!ok) break;
                 const uint32_t full = bar_full + 8 * stage;
-                const bool opens = i == t;
+                const bool opens = i == s.t0;
+                const int rows = s.rows();
                 if (lane == 0) {
-                    notes[stage] = Note{walk.item + int(blockIdx.x), int(key0), walk.keys, rows, walk.block,
-                                        (opens ? kFirst : 0) | (i + 1 == t1 ? kLast : 0) | (walk.b < 0 ? 0 : kOwn), 0, 0};
+                    notes[stage] = Note{s.item + int(blockIdx.x), int(key0), s.keys, rows,
+                                        (opens ? kFirst : 0) | (i + 1 == s.t1 ? kLast : 0) | (s.b < 0 ? 0 : kOwn), {0, 0, 0}};
                     mbar_expect_tx(full, uint32_t(copies) * 2u * copy_bytes + (opens ? uint32_t(rows) * D * 2u : 0u));
                 }
                 __syncwarp();
                 if (lane < 2 * copies) {
                     const uint32_t dst = base + stage * C::kStageBytes + (lane & 1) * C::kOperandBytes + (lane >> 1) * copy_bytes;
-                    tma_load_5d(dst, lane & 1 ? &map_v : &map_k, p.shift < 6 ? 0 : int(key0 & ((1 << p.shift) - 1)), walk.kvh, page, full, policy);
+                    tma_load_page(dst, lane & 1 ? &map_v : &map_k, p.shift < 6 ? 0 : int(key0 & ((1 << p.shift) - 1)), 0, s.kvh, page, full, policy);
                 }
                 if (opens && lane >= 16 && lane - 16 < rows) {
-                    const int r = walk.block * kRows + lane - 16;
-                    const int64_t tok = (walk.b < 0 ? 0 : int64_t(walk.b) * p.T) + r / p.G;
-                    tma_bulk_load(base + C::kQOffset + stage * C::kQBytes + (lane - 16) * C::kQPitch,
-                                  p.Q + tok * p.ldq + int64_t(walk.kvh * p.G + r % p.G) * D, D * 2, full, policy);
+                    const int r = lane - 16;
+                    const int64_t tok = (s.b < 0 ? 0 : int64_t(s.b) * p.T) + r / p.G;
+                    tma_bulk_load(base + C::kQOffset + stage * C::kQBytes + r * C::kQPitch,
+                                  p.Q + tok * p.ldq + int64_t(s.kvh * p.G + r % p.G) * D, D * 2, full, policy);
                 }
                 ++issued;
                 if (++stage == kStages) { stage = 0; phase ^= 1u; }
             }
-            u += t1 - t;
-            if (more) {
-                walk.b = ahead.b; walk.kvh = ahead.kvh; walk.block = ahead.block; walk.tiles = ahead.tiles; walk.keys = ahead.keys; walk.item = ahead.item;
-                t = page0 = 0;
-                mine = mine_ahead;
-            }
+            s = ahead;
+            have = more;
+            page0 = 0;
+            mine = mine_ahead;
         }
+        if (lane == 0 && ok && (issued < kStages || mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status))) {
+            notes[stage].flags = kEnd;
+            mbar_arrive(bar_full + 8 * stage);
+        }
+        if (AFTER && blockIdx.x == 0) grid_dependency_wait();
         if (*abort_flag) {                           // wait (bounded) for the copies in flight before the CTA may leave
             const uint64_t t0 = global_timer_ns();
             for (int j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
@@ -206,6 +175,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
 
     // ---------------- consumers ----------------
+    if (!busy) return;
     const int g = lane >> 2, t4 = lane & 3;
     float* join_o = reinterpret_cast<float*>(smem + C::kJoinOffset);
     float2* join_ml = reinterpret_cast<float2*>(smem + C::kMlOffset);
@@ -224,17 +194,17 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     float o[D / 8][4], m0, m1, l0, l1;
     int see0 = 0, see1 = 0;                          // keys that the lane's rows see
     bool failed = false;
-    for (int64_t u = u0; u < u1; ++u) {
+    for (;;) {
         failed = !mbar_wait(bar_full + 8 * stage, phase, abort_flag, p.status);
         if (failed) break;
         const Note n = notes[stage];
+        if (n.flags & kEnd) break;
         if (n.flags & kFirst) {
             // rows past the item's are whatever lies there: their results are never stored
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) ldmatrix4(q_at + stage * C::kQBytes + i * 32, qa[i][0], qa[i][1], qa[i][2], qa[i][3]);
-            const int r0 = n.block * kRows + g;
-            see0 = n.flags & kOwn ? n.keys - (p.T - 1 - r0 / p.G) : n.keys;
-            see1 = n.flags & kOwn ? n.keys - (p.T - 1 - (r0 + 8) / p.G) : n.keys;
+            see0 = n.flags & kOwn ? n.keys - (p.T - 1 - g / p.G) : n.keys;
+            see1 = n.flags & kOwn ? n.keys - (p.T - 1 - (g + 8) / p.G) : n.keys;
             m0 = m1 = -INFINITY;
             l0 = l1 = 0.0f;
 #pragma unroll
@@ -327,6 +297,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             if (t4 == 0) join_ml[warp * kRows + g + 8] = make_float2(m1, l1);
         }
         if (barrier_any(false, 1, 32 * kWarps)) return;
+        const bool own = n.flags & kOwn;
+        const int64_t row0 = int64_t(n.slot) * (own ? parts.rows_s : parts.rows_p);
+        float* part_o = (own ? parts.o_s : parts.o_p) + row0 * D;
+        float2* part_ml = (own ? parts.ml_s : parts.ml_p) + row0;
         for (int i = threadIdx.x; i < n.rows * (D / 4); i += 32 * kWarps) {
             const int r = i / (D / 4), c = i - r * (D / 4);
             float mx = -INFINITY, ls = 0.0f;
@@ -341,167 +315,44 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 ls = fmaf(ml.y, a, ls);
                 sum.x = fmaf(v.x, a, sum.x); sum.y = fmaf(v.y, a, sum.y); sum.z = fmaf(v.z, a, sum.z); sum.w = fmaf(v.w, a, sum.w);
             }
-            *reinterpret_cast<float4*>(part_o + (int64_t(n.slot) * kRows + r) * D + 4 * c) = sum;
-            if (c == 0) part_ml[int64_t(n.slot) * kRows + r] = make_float2(mx, ls);
+            *reinterpret_cast<float4*>(part_o + r * D + 4 * c) = sum;
+            if (c == 0) part_ml[r] = make_float2(mx, ls);
         }
     }
     if (failed) barrier_any(true, 1, 32 * kWarps);
 }
 
-// Joins the partial results: one warp per query row and head.
-struct Parts { const float* o; const float2* ml; const int* cum; Line w; int ctas, rows; };
+int decode_ctas(int sms) { return 2 * (sms < kMaxSms ? sms : kMaxSms); }
 
-template <int D>
-__global__ void __launch_bounds__(256)
-attn_join_kernel(const Problem p, const Parts parts, __nv_bfloat16* __restrict__ O, int64_t ldo, float* __restrict__ lse) {
-    constexpr int V = D / 32;                        // elements per lane
-    grid_dependency_wait();
-    const int lane = threadIdx.x & 31;
-    const int64_t row = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    const int Hq = p.Hkv * p.G;
-    if (row >= int64_t(p.B) * p.T * Hq) return;
-    const int tok = int(row / Hq), hq = int(row - int64_t(tok) * Hq), kvh = hq / p.G, gq = hq - kvh * p.G, b = tok / p.T;
-    const Line& w = parts.w;
-    const int per = p.Hkv * w.blocks_s;
-    const int64_t prefix = int64_t(p.Hkv) * w.blocks_p * w.tiles_p, total = prefix + int64_t(parts.cum[p.B]) * per;
-    const int n = total < parts.ctas ? int(total) : parts.ctas;
-
-    float m = -INFINITY, l = 0.0f, acc[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
-    auto add = [&](int64_t first, int64_t count, int64_t item, int r) {
-        if (count <= 0) return;
-        const int c0 = owner(first, total, n), c1 = owner(first + count - 1, total, n);
-        for (int c = c0; c <= c1; ++c) {
-            const int64_t at = (item + c) * parts.rows + r;
-            const float2 ml = parts.ml[at];
-            const float mx = fmaxf(m, ml.x);
-            const float a = m == -INFINITY ? 0.0f : ex2(m - mx), f = ml.x == -INFINITY ? 0.0f : ex2(ml.x - mx);
-            const float* src = parts.o + at * D + lane * V;
-            float v[V];
-            if constexpr (V == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
-            else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
-#pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] = acc[i] * a + v[i] * f;
-            l = l * a + ml.y * f;
-            m = mx;
-        }
-    };
-    if (w.blocks_p) {
-        const int r = tok * p.G + gq, blk = r / parts.rows, item = kvh * w.blocks_p + blk;
-        add(int64_t(item) * w.tiles_p, w.tiles_p, item, r - blk * parts.rows);
-    }
-    if (w.blocks_s) {
-        const int r = (tok - b * p.T) * p.G + gq, blk = r / parts.rows, sub = kvh * w.blocks_s + blk;
-        const int64_t tiles = parts.cum[b + 1] - parts.cum[b];
-        add(prefix + int64_t(parts.cum[b]) * per + sub * tiles, tiles, int64_t(p.Hkv) * w.blocks_p + int64_t(b) * per + sub, r - blk * parts.rows);
-    }
-    const float inv = l > 0.0f ? 1.0f / l : (l == l ? 0.0f : l);       // nothing seen: 0; NaN stays NaN
-    __nv_bfloat16* dst = O + int64_t(tok) * ldo + int64_t(hq) * D + lane * V;
-    if constexpr (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(acc[0] * inv, acc[1] * inv), pack2(acc[2] * inv, acc[3] * inv));
-    else *reinterpret_cast<uint32_t*>(dst) = pack2(acc[0] * inv, acc[1] * inv);
-    if (lse && lane == 0) lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-}
-
-// ---------------------------------------------------------------------------------------------
-// host side
-
-static int blocks_of(int64_t rows) { return int((rows + kRows - 1) / kRows); }
-
-struct Workspace { size_t ml, o, bytes; };           // [cum | (m, l) | outputs]
-static Workspace workspace_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G) {
-    const size_t items = size_t(c->Hkv) * (size_t(blocks_of(B * T * G)) + size_t(B) * blocks_of(T * G));
-    const size_t slots = items + kMaxCtas;
-    Workspace w;
-    w.ml = (size_t(B + 1) * 4 + 255) / 256 * 256;
-    w.o = w.ml + (slots * kRows * 8 + 255) / 256 * 256;
-    w.bytes = w.o + slots * kRows * size_t(c->D) * 4;
-    return w;
-}
-
-static int check_batch(const patch_kv_cache_t* c, int64_t B, int T, int Hq) {
-    int rc = validate_kv_cache(c);
-    if (rc) return rc;
-    if (c->D != 64 && c->D != 128) return PATCH_ERR_SHAPE;
-    if (B < 0 || B > kMaxBatch || T < 1 || Hq < 1 || Hq > (1 << 16) || Hq % c->Hkv) return PATCH_ERR_SHAPE;
-    if (B * T > 0x7FFFFFFF / c->D / Hq) return PATCH_ERR_SHAPE;
-    return PATCH_OK;
-}
-
-template <int D>
-static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, uint8_t* ws, const Workspace& at, __nv_bfloat16* O,
-                  int64_t ldo, float* lse, cudaStream_t stream) {
+template <int D, bool AFTER>
+static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, cudaStream_t stream) {
     CUtensorMap mk, mv;
     const int rows = c->page_size < kKeys ? c->page_size : kKeys;
     int rc = make_kv_tensor_map(&mk, c, c->k_dev, rows, D / 64);
     if (!rc) rc = make_kv_tensor_map(&mv, c, c->v_dev, rows, D / 64);
     if (rc) return rc;
-    auto kern = attn_decode_kernel<D>;
+    auto kern = attn_decode_kernel<D, AFTER>;
     static std::atomic<uint64_t> configured{0};
     if ((rc = allow_dynamic_smem(kern, Cfg<D>::smem_bytes(kMaxBatch), configured))) return rc;
     const int sms = sm_count();
     if (sms <= 0) return PATCH_ERR_CUDA;
-    const int ctas = sms < kMaxCtas ? sms : kMaxCtas;
-    int* cum = reinterpret_cast<int*>(ws);
-    float2* ml = reinterpret_cast<float2*>(ws + at.ml);
-    float* po = reinterpret_cast<float*>(ws + at.o);
-    kern<<<ctas, kThreads, Cfg<D>::smem_bytes(p.B), stream>>>(mk, mv, p, w, po, ml, cum);
-    if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
-    const Parts parts = {po, ml, cum, w, ctas, kRows};
-    const int64_t out_rows = int64_t(p.B) * p.T * p.Hkv * p.G;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
-    cfg.gridDim = dim3(unsigned((out_rows + 7) / 8), 1, 1);
-    cfg.blockDim = dim3(256, 1, 1);
+    cfg.gridDim = dim3(unsigned(decode_ctas(sms)), 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = Cfg<D>::smem_bytes(p.B);
     cfg.stream = stream;
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attn_join_kernel<D>, p, parts, O, ldo, lse) == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+    cfg.numAttrs = AFTER ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, mk, mv, p, w, parts, cum_out) == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+}
+
+int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, bool after_block, cudaStream_t s) {
+    if (c->D == 128) return after_block ? launch<128, true>(c, p, w, parts, cum_out, s) : launch<128, false>(c, p, w, parts, cum_out, s);
+    return after_block ? launch<64, true>(c, p, w, parts, cum_out, s) : launch<64, false>(c, p, w, parts, cum_out, s);
 }
 
 }  // namespace attn
 }  // namespace patch
-
-using namespace patch;
-
-extern "C" int patch_prefix_attention_workspace_size(const patch_kv_cache_t* cache, int64_t B, int T, int Hq, size_t* bytes_out) {
-    if (!bytes_out) return PATCH_ERR_NULL;
-    int rc = attn::check_batch(cache, B, T, Hq);
-    if (rc) return rc;
-    *bytes_out = attn::workspace_of(cache, B, T, Hq / cache->Hkv).bytes;
-    return PATCH_OK;
-}
-
-extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void* Q, int64_t ldq, int64_t B, int T, int Hq,
-                                      const int32_t* prefix_pages, int64_t prefix_len, const int32_t* page_table, int64_t ld_table,
-                                      const int32_t* suffix_lens, float scale, void* O, int64_t ldo, float* lse, void* workspace,
-                                      size_t workspace_bytes, int* status_dev, void* stream) {
-    int rc = attn::check_batch(cache, B, T, Hq);
-    if (rc) return rc;
-    if (prefix_len < 0 || prefix_len > 0x7FFFFF00 || ld_table < 0 || !(scale > 0.0f) || scale > 3.0e38f) return PATCH_ERR_SHAPE;
-    if (B == 0) return PATCH_OK;
-    if (ld_table > 0x7FFFFFFF || B * ((ld_table * cache->page_size + attn::kKeys - 1) / attn::kKeys) > 0x7FFFFFFF) return PATCH_ERR_SHAPE;
-    if (!Q || !O || !suffix_lens || (prefix_len && !prefix_pages) || (ld_table && !page_table)) return PATCH_ERR_NULL;
-    const int D = cache->D;
-    if (ldq < int64_t(Hq) * D || ldo < int64_t(Hq) * D || ldq % 8 || ldo % 8) return PATCH_ERR_SHAPE;
-    if (!aligned16(Q) || !aligned16(O)) return PATCH_ERR_ALIGN;
-    const int G = Hq / cache->Hkv;
-    const attn::Workspace at = attn::workspace_of(cache, B, T, G);
-    if (!workspace) return PATCH_ERR_NULL;
-    if (workspace_bytes < at.bytes) return PATCH_ERR_SIZE;
-    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PATCH_ERR_ALIGN;
-    if ((rc = check_device())) return rc;
-    attn::Problem p = {static_cast<const __nv_bfloat16*>(Q), ldq, int(B), T, cache->Hkv, G, prefix_pages, int(prefix_len), page_table,
-                       ld_table, suffix_lens, 0, int(cache->num_pages), scale * 1.4426950408889634f, status_dev};
-    while ((1 << p.shift) < cache->page_size) ++p.shift;
-    attn::Line w;
-    w.tiles_p = int((prefix_len + attn::kKeys - 1) / attn::kKeys);
-    w.blocks_p = prefix_len ? attn::blocks_of(B * T * G) : 0;
-    w.blocks_s = attn::blocks_of(int64_t(T) * G);
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(O);
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
-    return D == 128 ? attn::launch<128>(cache, p, w, ws, at, o, ldo, lse, s) : attn::launch<64>(cache, p, w, ws, at, o, ldo, lse, s);
-}
