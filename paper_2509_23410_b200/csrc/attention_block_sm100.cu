@@ -81,6 +81,12 @@ __device__ __forceinline__ void st_global32(float* p, const float (&v)[8]) {
                  "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
 
+// true in one lane of the (converged) warp, always the same one
+__device__ __forceinline__ bool elect_one() {
+    uint32_t pred;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
+    return pred != 0;
+}
 // Number of a stream's tiles among n: all of them where each stream has rows of its own, else every second.
 __device__ __forceinline__ int stream_tiles(int n, bool dual, int x) { return dual ? n : (n + 1 - x) >> 1; }
 
@@ -129,6 +135,9 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int64_t u0 = busy ? total * blockIdx.x / ctas : 0, u1 = busy ? total * (blockIdx.x + 1) / ctas : 0;
     Share s(p, w, cum, lens);
 
+    // registers: 384 threads x 168 at launch = 128 x 72 + 256 x 216
+    if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
         // ---------------- producer: K0 K1 V0 K2 V1 ... (one stream's rows twice) or K0 V0 K1 V1 ... ----------------
         const uint64_t policy = l2_policy_evict_first();
@@ -191,9 +200,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         uint32_t phase = 0, phase_q = 0, phase_p[2] = {0, 0};
         bool ok = true;
         auto wait = [&](uint32_t bar, uint32_t parity) {       // the whole warp goes on together
-            bool good = true;
-            if (lane == 0) good = mbar_wait(bar, parity, abort_flag, p.status);
-            ok = ok && __shfl_sync(0xFFFFFFFFu, good ? 1 : 0, 0) != 0;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, p.status)) && ok;
             tc_fence_after();
         };
         auto advance = [&] { if (++stage == kRing) { stage = 0; phase ^= 1u; } };
@@ -221,7 +228,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             for (int i = 0; i < lead && i < n && ok; ++i) {
                 wait(bar_full + 8 * stage, phase);
                 if (!ok) break;
-                if (lane == 0) {
+                if (elect_one()) {
                     const uint32_t k_tile = base + stage * C::kTile;
                     if (dual || i == 0) scores(0, q0, k_tile);
                     if (dual || i == 1) scores(1, q1, k_tile);
@@ -245,39 +252,34 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     __syncwarp();
                 }
                 const bool more = i + lead < n;
-                const uint32_t k_stage = stage;
                 for (int y = 0; y < (dual ? 2 : 1) && ok; ++y) {
                     const int x = dual ? y : i & 1;
                     wait(bar_p + 8 * x, phase_p[x]);
                     phase_p[x] ^= 1u;
                     if (!ok) break;
-                    if (more && y == 0) {
-                        // the products go out first where the keys are still on their way
-                        if (lane == 0) outputs(x, v_tile, dual ? i == 0 : i < 2);
-                        __syncwarp();
-                        if (!dual && lane == 0) mma_commit(v_empty);
-                        wait(bar_full + 8 * k_stage, phase);
-                        if (!ok) break;
-                        advance();
-                        if (lane == 0) {
-                            scores(x, x ? q1 : q0, base + k_stage * C::kTile);
-                            if (!dual) mma_commit(bar_empty + 8 * k_stage);
-                        }
-                    } else if (lane == 0) {
-                        outputs(x, v_tile, dual ? i == 0 : i < 2);
-                        if (!dual || y == 1) mma_commit(v_empty);
-                        if (more) {
-                            scores(x, x ? q1 : q0, base + k_stage * C::kTile);
-                            mma_commit(bar_empty + 8 * k_stage);
-                        }
+                    const bool first = dual ? i == 0 : i < 2, v_done = !dual || y == 1;
+                    if (elect_one()) {
+                        outputs(x, v_tile, first);
+                        if (v_done) mma_commit(v_empty);
+                    }
+                    __syncwarp();
+                    if (!more) continue;
+                    if (y == 0) wait(bar_full + 8 * stage, phase);       // the stream's next keys
+                    if (!ok) break;
+                    if (elect_one()) {
+                        scores(x, x ? q1 : q0, base + stage * C::kTile);
+                        if (v_done) mma_commit(bar_empty + 8 * stage);
                     }
                     __syncwarp();
                 }
+                if (more) advance();
             }
-            if (ok && lane == 0) mma_commit(bar_o);
+            if (ok && elect_one()) mma_commit(bar_o);
             __syncwarp();
         }
-    } else if (warp >= 4) {
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ---------------- softmax: thread = row of the stream ----------------
         const int x = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = uint32_t(quad * 32) << 16;
