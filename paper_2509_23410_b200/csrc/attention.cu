@@ -9,69 +9,71 @@
 namespace patch {
 namespace attn {
 
-// One line of units and the CTAs that shared it.
-struct Source { Line w; const int* cum; int ctas; };
-
-// Joins the partial results: one warp per query row and head.  Bound by the latency of a few dependent reads from L2; the
-// (m, l) pairs of up to 32 parts are read at once, one per lane, and their outputs four at a time.
+// Joins the partial results: one warp per query row and head.  Bound by the latency of three dependent reads (which CTAs, their
+// (m, l), their outputs); the (m, l) of up to 32 parts are read at once, one per lane, their outputs eight at a time.
 template <int D>
 __global__ void __launch_bounds__(256)
-attn_join_kernel(const Problem p, const Source sp, const Source ss, const Parts parts, __nv_bfloat16* __restrict__ O, int64_t ldo,
+attn_join_kernel(const Problem p, const Results from, const int blocks_p, const int blocks_s, __nv_bfloat16* __restrict__ O, int64_t ldo,
                  float* __restrict__ lse) {
     constexpr int V = D / 32;                        // elements per lane
-    grid_dependency_wait();
     const int lane = threadIdx.x & 31;
-    const int64_t row = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    const int Hq = p.Hkv * p.G;
-    if (row >= int64_t(p.B) * p.T * Hq) return;
-    const int tok = int(row / Hq), hq = int(row - int64_t(tok) * Hq), kvh = hq / p.G, gq = hq - kvh * p.G, b = tok / p.T;
+    const int row = blockIdx.x * 8 + (threadIdx.x >> 5), Hq = p.Hkv * p.G;
+    const bool on = row < p.B * p.T * Hq;
+    const int tok = row / Hq, hq = row - tok * Hq, kvh = hq / p.G, gq = hq - kvh * p.G, b = tok / p.T;
+    const bool own = on && suffix_len(p, b) > 0;
+    grid_dependency_wait();
+    if (!on) return;
 
+    // slot of the item's first part, and the row's place in a slot
+    int count[2] = {0, 0};
+    int64_t at[2] = {0, 0};
+    if (blocks_p) {
+        const int r = tok * p.G + gq, blk = r / from.p.rows, item = kvh * blocks_p + blk;
+        const int2 span = from.p.span[item];
+        count[0] = span.y - span.x + 1;
+        at[0] = (int64_t(item) + span.x) * from.p.rows + (r - blk * from.p.rows);
+    }
+    if (own) {
+        const int r = (tok - b * p.T) * p.G + gq, blk = r / from.s.rows, item = (b * p.Hkv + kvh) * blocks_s + blk;
+        const int2 span = from.s.span[item];
+        count[1] = span.y - span.x + 1;
+        at[1] = (int64_t(item) + span.x) * from.s.rows + (r - blk * from.s.rows);
+    }
     float m = -INFINITY, l = 0.0f, acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.0f;
-    // the parts of one item: tiles are `count` units from `first` on; (m, l) and outputs of the slots item + CTA
-    auto add = [&](const Source& src, int64_t first, int64_t count, int64_t item, int r, const float* o, const float2* ml, int rows) {
-        if (count <= 0) return;
-        const int64_t total = total_units(src.w, p.Hkv, src.cum[p.B]);
-        const int n = total < src.ctas ? int(total) : src.ctas;
-        const int c0 = owner(first, total, n), parts_n = owner(first + count - 1, total, n) - c0 + 1;
-        const int64_t at = (item + c0) * rows + r;
-        for (int k0 = 0; k0 < parts_n; k0 += 32) {
-            const int here = parts_n - k0 < 32 ? parts_n - k0 : 32;
-            const float2 mine = lane < here ? ml[at + int64_t(k0 + lane) * rows] : make_float2(-INFINITY, 0.0f);
-            float mx = fmaxf(m, mine.x);
+    const int all = count[0] + count[1];
+    for (int k0 = 0; k0 < all; k0 += 32) {
+        const int here = all - k0 < 32 ? all - k0 : 32;
+        // this lane's part: its row in the outputs, and (m, l)
+        const int k = k0 + lane;
+        const bool of_p = k < count[0];
+        const Parts& part = of_p ? from.p : from.s;
+        const int64_t mine_at = of_p ? at[0] + int64_t(k) * part.rows : at[1] + int64_t(k - count[0]) * part.rows;
+        const float2 mine = lane < here ? part.ml[mine_at] : make_float2(-INFINITY, 0.0f);
+        const float* src = part.o + mine_at * D;
+        float mx = fmaxf(m, mine.x);
 #pragma unroll
-            for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
-            if (mx == -INFINITY) continue;
-            const float f = ex2(mine.x - mx), a = ex2(m - mx);
-            float add_l = mine.y * f;
+        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
+        if (mx == -INFINITY) continue;
+        const float f = ex2(mine.x - mx), a = ex2(m - mx);
+        float add = mine.y * f;
 #pragma unroll
-            for (int d = 16; d > 0; d >>= 1) add_l += __shfl_xor_sync(0xFFFFFFFFu, add_l, d);
-            l = l * a + add_l;
-            m = mx;
+        for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, d);
+        l = l * a + add;
+        m = mx;
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] *= a;
-#pragma unroll 4
-            for (int k = 0; k < here; ++k) {
-                const float* src_o = o + (at + int64_t(k0 + k) * rows) * D + lane * V;
-                const float fk = __shfl_sync(0xFFFFFFFFu, f, k);
-                float v[V];
-                if constexpr (V == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src_o);
-                else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src_o);
+        for (int i = 0; i < V; ++i) acc[i] *= a;
+#pragma unroll 8
+        for (int q = 0; q < here; ++q) {
+            const float fq = __shfl_sync(0xFFFFFFFFu, f, q);
+            const float* from_o = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(src), q)) + lane * V;
+            float v[V];
+            if constexpr (V == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(from_o);
+            else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(from_o);
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] = fmaf(v[i], fk, acc[i]);
-            }
+            for (int i = 0; i < V; ++i) acc[i] = fmaf(v[i], fq, acc[i]);
         }
-    };
-    if (sp.w.blocks_p) {
-        const int r = tok * p.G + gq, blk = r / parts.rows_p, item = kvh * sp.w.blocks_p + blk;
-        add(sp, int64_t(item) * (sp.w.tiles_p + sp.w.cost) + sp.w.cost, sp.w.tiles_p, item, r - blk * parts.rows_p, parts.o_p, parts.ml_p, parts.rows_p);
-    }
-    {
-        const int r = (tok - b * p.T) * p.G + gq, blk = r / parts.rows_s, sub = kvh * ss.w.blocks_s + blk, per = p.Hkv * ss.w.blocks_s;
-        const int each = ss.cum[b + 1] - ss.cum[b];
-        add(ss, prefix_units(ss.w, p.Hkv) + int64_t(ss.cum[b]) * per + int64_t(sub) * each + ss.w.cost, each - ss.w.cost, int64_t(b) * per + sub,
-            r - blk * parts.rows_s, parts.o_s, parts.ml_s, parts.rows_s);
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // nothing seen: 0
     __nv_bfloat16* dst = O + int64_t(tok) * ldo + int64_t(hq) * D + lane * V;
@@ -88,7 +90,7 @@ attn_join_kernel(const Problem p, const Source sp, const Source ss, const Parts 
 struct Plan {
     bool block_p, block_s;                           // prefix / suffixes on the block kernel
     int blocks_p, blocks_s, rows_p, rows_s;          // row blocks per key head, rows of a slot
-    size_t cum_block, ml_p, ml_s, o_p, o_s, bytes;   // workspace: [units of the decode kernel | of the block kernel | (m, l) | outputs]
+    size_t span_s, ml_p, ml_s, o_p, o_s, bytes;      // workspace: [spans of prefix items | of suffix items | (m, l) | outputs]
 };
 static Plan plan_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G) {
     Plan q;
@@ -100,10 +102,11 @@ static Plan plan_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G) 
     };
     q.rows_p = rows(B * T * G, q.block_p, q.blocks_p);
     q.rows_s = rows(T * G, q.block_s, q.blocks_s);
-    // a slot for every item and every CTA that may share one (the decode kernel has two CTAs per SM)
-    const size_t slots_p = size_t(c->Hkv) * q.blocks_p + 2 * kMaxSms, slots_s = size_t(c->Hkv) * B * q.blocks_s + 2 * kMaxSms;
-    q.cum_block = up(size_t(B + 1) * 4);
-    q.ml_p = 2 * q.cum_block;
+    // a slot for every item and every CTA that may share one
+    const size_t items_p = size_t(c->Hkv) * q.blocks_p, items_s = size_t(c->Hkv) * B * q.blocks_s;
+    const size_t slots_p = items_p + kMaxShares, slots_s = items_s + kMaxShares;
+    q.span_s = up(items_p * 8);
+    q.ml_p = q.span_s + up(items_s * 8);
     q.ml_s = q.ml_p + up(slots_p * q.rows_p * 8);
     q.o_p = q.ml_s + up(slots_s * q.rows_s * 8);
     q.o_s = q.o_p + up(slots_p * q.rows_p * size_t(c->D) * 4);
@@ -154,23 +157,19 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     if (workspace_bytes < q.bytes) return PATCH_ERR_SIZE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PATCH_ERR_ALIGN;
     if ((rc = check_device())) return rc;
-    const int sms = sm_count() < kMaxSms ? sm_count() : kMaxSms;
-    if (sms <= 0) return PATCH_ERR_CUDA;
     Problem p = {static_cast<const __nv_bfloat16*>(Q), ldq, int(B), T, cache->Hkv, G, prefix_pages, int(prefix_len), page_table,
                  ld_table, suffix_lens, 0, int(cache->num_pages), scale * 1.4426950408889634f, status_dev};
     while ((1 << p.shift) < cache->page_size) ++p.shift;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const Parts parts = {reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_p),
-                         reinterpret_cast<float2*>(ws + q.ml_s), q.rows_p, q.rows_s};
+    const Results to = {{reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float2*>(ws + q.ml_p), reinterpret_cast<int2*>(ws), q.rows_p},
+                        {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s}};
     const bool prefix = prefix_len > 0;
-    Source dec = {{prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : 1, 0, kDecodeCost}, reinterpret_cast<const int*>(ws), decode_ctas(sms)};
-    Source blk = {{prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, 0, kBlockCost}, reinterpret_cast<const int*>(ws + q.cum_block), sms};
-    dec.w.tiles_p = int((prefix_len + kDecodeKeys - 1) / kDecodeKeys);
-    blk.w.tiles_p = int((prefix_len + kBlockKeys - 1) / kBlockKeys);
-    const bool use_block = blk.w.blocks_p || blk.w.blocks_s, use_decode = dec.w.blocks_p || dec.w.blocks_s;
-    if (use_block && (rc = launch_attn_block(cache, p, blk.w, parts, const_cast<int*>(blk.cum), s))) return rc;
-    if (use_decode && (rc = launch_attn_decode(cache, p, dec.w, parts, const_cast<int*>(dec.cum), use_block, s))) return rc;
+    const Line dec = {prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : 1, int((prefix_len + kDecodeKeys - 1) / kDecodeKeys), kDecodeCost};
+    const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, int((prefix_len + kBlockKeys - 1) / kBlockKeys), kBlockCost};
+    const bool use_block = blk.blocks_p || blk.blocks_s, use_decode = dec.blocks_p || dec.blocks_s;
+    if (use_block && (rc = launch_attn_block(cache, p, blk, to, use_decode, s))) return rc;
+    if (use_decode && (rc = launch_attn_decode(cache, p, dec, to, use_block, s))) return rc;
     const int64_t out_rows = B * T * Hq;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
@@ -182,7 +181,8 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     __nv_bfloat16* o = static_cast<__nv_bfloat16*>(O);
-    const cudaError_t e = D == 128 ? cudaLaunchKernelEx(&cfg, attn_join_kernel<128>, p, q.block_p ? blk : dec, q.block_s ? blk : dec, parts, o, ldo, lse)
-                                   : cudaLaunchKernelEx(&cfg, attn_join_kernel<64>, p, q.block_p ? blk : dec, q.block_s ? blk : dec, parts, o, ldo, lse);
+    const int blocks_p = prefix ? q.blocks_p : 0;
+    const cudaError_t e = D == 128 ? cudaLaunchKernelEx(&cfg, attn_join_kernel<128>, p, to, blocks_p, q.blocks_s, o, ldo, lse)
+                                   : cudaLaunchKernelEx(&cfg, attn_join_kernel<64>, p, to, blocks_p, q.blocks_s, o, ldo, lse);
     return e == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
 }

@@ -7,7 +7,7 @@
 // work whatever the lengths are, at the price of items that several CTAs share.  An item also has a few units without a tile, which
 // stand for what it costs by itself.  Each CTA writes one partial result (running maximum, sum and unnormalised output, fp32)
 // per item it has a share of.  Along the line the pair (item, CTA) changes one step at a time, so item + c numbers the partial
-// results, and the joining kernel finds an item's from the item's first and last tile.
+// results; the CTAs with an item's first and last tile note their numbers for the joining kernel.
 #pragma once
 #include "sm100_ptx.cuh"
 
@@ -37,12 +37,14 @@ struct Line {
     int tiles_p;                              // key tiles of a prefix item
     int cost;                                 // units of an item beside its tiles
 };
-// Where a kernel's partial results go: of prefix items, of suffix items; `rows` is the row count of a slot.
+// Where partial results go, of prefix items and of suffix items.
 struct Parts {
-    float *o_p, *o_s;
-    float2 *ml_p, *ml_s;                      // maximum (in powers of two), sum
-    int rows_p, rows_s;
+    float* o;                                 // [slot][rows][D]
+    float2* ml;                               // [slot][rows]: maximum (in powers of two), sum
+    int2* span;                               // [item]: first and last CTA with a share of it
+    int rows;                                 // rows of a slot
 };
+struct Results { Parts p, s; };
 
 // len -> clamped length of sequence b's own keys
 __device__ __forceinline__ int suffix_len(const Problem& p, int b) {
@@ -59,8 +61,8 @@ __device__ __forceinline__ void lay_out(const Problem& p, const Line& w, int til
     const int lane = threadIdx.x & 31;
     int before = 0;
     for (int b0 = 0; b0 < p.B; b0 += 32) {
-        const int b = b0 + lane, n = w.blocks_s && b < p.B ? suffix_len(p, b) : 0;
-        int t = n / tile_keys + (n % tile_keys != 0);
+        const int b = b0 + lane, n = b < p.B ? suffix_len(p, b) : 0;
+        int t = w.blocks_s ? n / tile_keys + (n % tile_keys != 0) : 0;
         if (t) t += w.cost;
         if (b < p.B) lens[b] = n;
 #pragma unroll
@@ -78,9 +80,6 @@ __host__ __device__ __forceinline__ int64_t prefix_units(const Line& w, int Hkv)
 __device__ __forceinline__ int64_t total_units(const Line& w, int Hkv, int cum_all) {
     return prefix_units(w, Hkv) + int64_t(cum_all) * Hkv * w.blocks_s;
 }
-// The CTA that owns unit u of U spread over n <= U CTAs.
-__device__ __forceinline__ int owner(int64_t u, int64_t U, int n) { return int(((u + 1) * n - 1) / U); }
-
 // One CTA's share of the line, item by item.
 struct Share {
     const Problem& p;
@@ -158,6 +157,11 @@ struct Share {
         clip();
         return true;
     }
+    __device__ __forceinline__ void note(const Results& to, int cta) const {
+        int2* span = (b < 0 ? to.p.span : to.s.span) + item;
+        if (t0 == 0) span->x = cta;
+        if (t1 == tiles) span->y = cta;
+    }
     __device__ __forceinline__ int rows() const { return b < 0 ? p.B * p.T * p.G : p.T * p.G; }
     __device__ __forceinline__ const int32_t* list() const { return b < 0 ? p.prefix_pages : p.table + b * p.ld_table; }
     __device__ __forceinline__ int pages() const { return int((int64_t(keys) + (1 << p.shift) - 1) >> p.shift); }
@@ -186,9 +190,9 @@ constexpr int kFewRows = 16;
 constexpr int kBlockRows = 256;
 constexpr int kDecodeKeys = 64, kBlockKeys = 128;     // keys of a tile
 constexpr int kDecodeCost = 1, kBlockCost = 1;        // Line::cost
-int decode_ctas(int sms);
-int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, bool after_block, cudaStream_t s);
-int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, cudaStream_t s);
+constexpr int kMaxShares = 4 * kMaxSms;               // CTAs of one launch, at most
+int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool after_block, cudaStream_t s);
+int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool decode_follows, cudaStream_t s);
 
 }  // namespace attn
 

@@ -87,15 +87,96 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
     return pred != 0;
 }
+// ---- pairs of fp32 in a 64-bit register ----
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 mk2(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void un2(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// scores past the row's last column: -inf
+__device__ __forceinline__ void hide(uint32_t (&v)[32], int left) {
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+        if (c >= left) v[c] = 0xFF800000u;
+}
+__device__ __forceinline__ float top_of(const uint32_t (&v)[32], float top) {
+    float t[4] = {top, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int c = 0; c < 32; ++c) t[c & 3] = fmaxf(t[c & 3], __uint_as_float(v[c]));
+    return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+}
+// Maximum of the row's 128 scores.
+__device__ __forceinline__ float row_top(uint32_t t_s, int left, bool partly) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint32_t v[32];
+        tmem_ld32(t_s + 32u * q, v);
+        tmem_ld_wait();
+        if (partly) hide(v, left - 32 * q);
+        top = top_of(v, top);
+    }
+    return top;
+}
+// 2^(s scale + off) of the row's 128 scores as bf16, their sum (of the unrounded values) and the scores' maximum.  A quarter is
+// on its way from TMEM while the one before it is worked on.
+__device__ __forceinline__ void probabilities(uint32_t t_s, int left, bool partly, float scale, float off, uint32_t (&pr)[2][32],
+                                              float& top, float& sum) {
+    const f2 scale2 = mk2(scale, scale), off2 = mk2(off, off);
+    f2 total[2] = {0ull, 0ull};
+    top = -INFINITY;
+    uint32_t v[2][32];
+    tmem_ld32(t_s, v[0]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint32_t (&s)[32] = v[q & 1];
+        tmem_ld_wait();
+        if (q < 3) tmem_ld32(t_s + 32u * (q + 1), v[(q + 1) & 1]);
+        if (partly) hide(s, left - 32 * q);
+        top = top_of(s, top);
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+            float e0, e1;
+            un2(fma2(mk2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, off2), e0, e1);
+            e0 = ex2(e0);
+            e1 = ex2(e1);
+            total[(c >> 1) & 1] = add2(total[(c >> 1) & 1], mk2(e0, e1));
+            pr[q >> 1][(q & 1) * 16 + (c >> 1)] = pack2(e0, e1);
+        }
+    }
+    float a, b;
+    un2(add2(total[0], total[1]), a, b);
+    sum = a + b;
+}
+
 // Number of a stream's tiles among n: all of them where each stream has rows of its own, else every second.
 __device__ __forceinline__ int stream_tiles(int n, bool dual, int x) { return dual ? n : (n + 1 - x) >> 1; }
 
+// How many SMs the block kernel takes where the decode kernel has the suffixes.  Together they are done no sooner than HBM has
+// delivered the keys and values and the SMs have done their cycles; with as many SMs as its own cycles need in that time, the block
+// kernel ends with the decode kernel, which streams from the other SMs meanwhile -- one is short of arithmetic, the other of
+// bandwidth.  Cycles measured: 4 000 for a key tile and 256 rows, 2 000 for one and 128 rows, 700 for a tile of the decode kernel (two
+// CTAs share its latencies); bandwidth in bytes per cycle of 6.5 TB/s at 1.9 GHz.
+template <int D>
+__device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w, const int* lens, int sms) {
+    float keys = 0.0f;
+    for (int b = threadIdx.x & 31; b < p.B; b += 32) keys += float(lens[b]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) keys += __shfl_xor_sync(0xFFFFFFFFu, keys, d);
+    const float rows = float(p.B) * p.T * p.G, heads = float(p.Hkv);
+    const float mine = heads * w.tiles_p * 2000.0f * ceilf(rows / 128.0f);
+    const float theirs = heads * keys / kDecodeKeys * 700.0f;
+    const float bytes = heads * (keys + float(p.prefix_len)) * D * 4.0f;
+    const float time = fmaxf(bytes / 3420.0f, (mine + theirs) / sms);
+    return max(1, min(sms, int(ceilf(mine / time))));
+}
 }  // namespace blk
 
 template <int D>
 __global__ void __launch_bounds__(blk::kThreads, 1)
 attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const Line w,
-                  const Parts parts, int* __restrict__ cum_out) {
+                  const Results to, const int share_gpu) {
     using namespace blk;
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -126,11 +207,10 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *misc;
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= p.B; b += kThreads) cum_out[b] = cum[b];
 
     const int64_t total = total_units(w, p.Hkv, cum[p.B]);
-    const int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
+    int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
+    if (share_gpu) ctas = min(ctas, sms_beside_decode<D>(p, w, lens, gridDim.x));
     const bool busy = int(blockIdx.x) < ctas;
     const int64_t u0 = busy ? total * blockIdx.x / ctas : 0, u1 = busy ? total * (blockIdx.x + 1) / ctas : 0;
     Share s(p, w, cum, lens);
@@ -147,6 +227,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         uint32_t phase = 0;
         bool ok = true;
         for (bool have = s.start(u0, u1); have && ok; have = s.next()) {
+            if (lane == 0) s.note(to, blockIdx.x);
             const int n_pages = s.pages();
             const bool dual = s.rows() - s.block * kBlockRows > 128;
             const int n = s.t1 - s.t0;
@@ -315,26 +396,22 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 if (failed) break;
                 phase_s ^= 1u;
                 tc_fence_after();
-                uint32_t v[4][32];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_ld32(t_s + 32u * q, v[q]);
-                tmem_ld_wait();
-                const int key0 = (s.t0 + (dual ? j : 2 * j + x)) * kKeys;
-                if (key0 + kKeys > see) {
-                    const int left = see - key0;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-#pragma unroll
-                        for (int c = 0; c < 32; ++c)
-                            if (32 * q + c >= left) v[q][c] = 0xFF800000u;        // -inf
+                const int left = see - (s.t0 + (dual ? j : 2 * j + x)) * kKeys;      // columns the row sees
+                const bool partly = __any_sync(0xFFFFFFFFu, left < kKeys);
+                if (j == 0) {
+                    m = fmaxf(m, row_top(t_s, left, partly) * p.scale_log2);
                 }
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(v[q][c]));
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
-                if (__any_sync(0xFFFFFFFFu, top > m + kSlack)) {
+                // Probabilities with the maximum as it stands, and the scores' maximum beside them: a pass that turns out to need
+                // a higher one is taken again (S is overwritten only by the stores below), which is rare after the first tile.
+                uint32_t pr[2][32];
+                for (;;) {
+                    float top, sum;
+                    probabilities(t_s, left, partly, p.scale_log2, m == -INFINITY ? 0.0f : -m, pr, top, sum);
+                    top *= p.scale_log2;
+                    if (!__any_sync(0xFFFFFFFFu, top > m + kSlack)) {
+                        l += sum;
+                        break;
+                    }
                     const float up = fmaxf(m, top), a = up == -INFINITY ? 1.0f : ex2(m - up);
                     m = up;
                     l *= a;
@@ -350,22 +427,8 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         }
                     }
                 }
-                const float off = m == -INFINITY ? 0.0f : -m;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                // the probabilities take the place of scores that have been read: two in a register
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) {
-                        const float e0 = ex2(fmaf(__uint_as_float(v[q][c]), p.scale_log2, off));
-                        const float e1 = ex2(fmaf(__uint_as_float(v[q][c + 1]), p.scale_log2, off));
-                        sum[c & 2] += e0;
-                        sum[(c & 2) + 1] += e1;
-                        v[q >> 1][(q & 1) * 16 + (c >> 1)] = pack2(e0, e1);
-                    }
-                tmem_st32(t_s, v[0]);
-                tmem_st32(t_s + 32u, v[1]);
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tmem_st32(t_s, pr[0]);
+                tmem_st32(t_s + 32u, pr[1]);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -377,11 +440,9 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             ml[128 * x + row] = make_float2(m, l);
             if (barrier_any(failed, 1, 256)) { failed = true; break; }
             // ---- the partial result ----
-            const bool own = s.b >= 0;
-            const int64_t slot = s.item + int64_t(blockIdx.x);
-            const int rows_slot = own ? parts.rows_s : parts.rows_p;
-            const int64_t at = slot * rows_slot + (dual ? 128 * x : 0) + row;
-            float* dst = (own ? parts.o_s : parts.o_p) + at * D;
+            const Parts& part = s.b < 0 ? to.p : to.s;
+            const int64_t at = (s.item + int64_t(blockIdx.x)) * part.rows + (dual ? 128 * x : 0) + row;
+            float* dst = part.o + at * D;
             if (dual) {
 #pragma unroll
                 for (int q = 0; q < D / 32; ++q) {
@@ -398,7 +459,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         }
                     }
                 }
-                if (valid) (own ? parts.ml_s : parts.ml_p)[at] = make_float2(m, l);
+                if (valid) part.ml[at] = make_float2(m, l);
             } else {
                 // both streams hold a part of the same rows: each takes half of the columns of both
                 const float2 a = ml[row], b = ml[128 + row];
@@ -422,7 +483,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         }
                     }
                 }
-                if (valid && x == 0) (own ? parts.ml_s : parts.ml_p)[at] = make_float2(mx, a.y * fa + b.y * fb);
+                if (valid && x == 0) part.ml[at] = make_float2(mx, a.y * fa + b.y * fb);
             }
             tc_fence_before();
             if (barrier_any(false, 1, 256)) { failed = true; break; }             // nobody's accumulators are read any more
@@ -435,7 +496,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 }
 
 template <int D>
-static int launch_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, cudaStream_t stream) {
+static int launch_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool share_gpu, cudaStream_t stream) {
     using C = blk::Cfg<D>;
     CUtensorMap mk, mv;
     const int rows = c->page_size < blk::kKeys ? c->page_size : blk::kKeys;
@@ -447,12 +508,12 @@ static int launch_block(const patch_kv_cache_t* c, const Problem& p, const Line&
     if ((rc = allow_dynamic_smem(kern, C::smem_bytes(kMaxBatch), configured))) return rc;
     const int sms = sm_count();
     if (sms <= 0) return PATCH_ERR_CUDA;
-    kern<<<sms < kMaxSms ? sms : kMaxSms, blk::kThreads, C::smem_bytes(p.B), stream>>>(mk, mv, p, w, parts, cum_out);
+    kern<<<sms < kMaxSms ? sms : kMaxSms, blk::kThreads, C::smem_bytes(p.B), stream>>>(mk, mv, p, w, to, share_gpu);
     return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
 }
 
-int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, cudaStream_t s) {
-    return c->D == 128 ? launch_block<128>(c, p, w, parts, cum_out, s) : launch_block<64>(c, p, w, parts, cum_out, s);
+int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool decode_follows, cudaStream_t s) {
+    return c->D == 128 ? launch_block<128>(c, p, w, to, decode_follows, s) : launch_block<64>(c, p, w, to, decode_follows, s);
 }
 
 }  // namespace attn

@@ -62,7 +62,7 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
 template <int D, bool AFTER>
 __global__ void __launch_bounds__(kThreads, 2)
 attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const Line w,
-                   const Parts parts, int* __restrict__ cum_out) {
+                   const Results to) {
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -84,9 +84,6 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
     if (warp == 0) lay_out(p, w, kKeys, cum, lens);
     __syncthreads();
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= p.B; b += kThreads) cum_out[b] = cum[b];
-
     const int64_t total = total_units(w, p.Hkv, cum[p.B]);
     const int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
     const bool busy = int(blockIdx.x) < ctas;
@@ -111,6 +108,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         int page0 = have ? int((int64_t(s.t0) * kKeys) >> p.shift) : 0;
         int mine = have ? fetch(s, page0) : 0;
         while (have && ok) {
+            if (lane == 0) s.note(to, blockIdx.x);
             // the next item's pages are on their way while this one's tiles are requested
             ahead = s;
             const bool more = ahead.next();
@@ -297,10 +295,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             if (t4 == 0) join_ml[warp * kRows + g + 8] = make_float2(m1, l1);
         }
         if (barrier_any(false, 1, 32 * kWarps)) return;
-        const bool own = n.flags & kOwn;
-        const int64_t row0 = int64_t(n.slot) * (own ? parts.rows_s : parts.rows_p);
-        float* part_o = (own ? parts.o_s : parts.o_p) + row0 * D;
-        float2* part_ml = (own ? parts.ml_s : parts.ml_p) + row0;
+        const Parts& part = n.flags & kOwn ? to.s : to.p;
+        const int64_t row0 = int64_t(n.slot) * part.rows;
+        float* part_o = part.o + row0 * D;
+        float2* part_ml = part.ml + row0;
         for (int i = threadIdx.x; i < n.rows * (D / 4); i += 32 * kWarps) {
             const int r = i / (D / 4), c = i - r * (D / 4);
             float mx = -INFINITY, ls = 0.0f;
@@ -322,10 +320,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (failed) barrier_any(true, 1, 32 * kWarps);
 }
 
-int decode_ctas(int sms) { return 2 * (sms < kMaxSms ? sms : kMaxSms); }
-
 template <int D, bool AFTER>
-static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, cudaStream_t stream) {
+static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, cudaStream_t stream) {
     CUtensorMap mk, mv;
     const int rows = c->page_size < kKeys ? c->page_size : kKeys;
     int rc = make_kv_tensor_map(&mk, c, c->k_dev, rows, D / 64);
@@ -334,11 +330,14 @@ static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, co
     auto kern = attn_decode_kernel<D, AFTER>;
     static std::atomic<uint64_t> configured{0};
     if ((rc = allow_dynamic_smem(kern, Cfg<D>::smem_bytes(kMaxBatch), configured))) return rc;
-    const int sms = sm_count();
+    const int sms = sm_count() < kMaxSms ? sm_count() : kMaxSms;
     if (sms <= 0) return PATCH_ERR_CUDA;
+    // alone, one wave; beside the block kernel, which leaves an unknown part of the SMs free, shares half the size, so that
+    // the last ones do not run by themselves for long
+    const int ctas = (AFTER ? 4 : 2) * sms;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
-    cfg.gridDim = dim3(unsigned(decode_ctas(sms)), 1, 1);
+    cfg.gridDim = dim3(unsigned(ctas), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = Cfg<D>::smem_bytes(p.B);
     cfg.stream = stream;
@@ -346,12 +345,12 @@ static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, co
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = AFTER ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, mk, mv, p, w, parts, cum_out) == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kern, mk, mv, p, w, to) == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
 }
 
-int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Parts& parts, int* cum_out, bool after_block, cudaStream_t s) {
-    if (c->D == 128) return after_block ? launch<128, true>(c, p, w, parts, cum_out, s) : launch<128, false>(c, p, w, parts, cum_out, s);
-    return after_block ? launch<64, true>(c, p, w, parts, cum_out, s) : launch<64, false>(c, p, w, parts, cum_out, s);
+int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool after_block, cudaStream_t s) {
+    if (c->D == 128) return after_block ? launch<128, true>(c, p, w, to, s) : launch<128, false>(c, p, w, to, s);
+    return after_block ? launch<64, true>(c, p, w, to, s) : launch<64, false>(c, p, w, to, s);
 }
 
 }  // namespace attn
