@@ -146,7 +146,7 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     if (prefix_len < 0 || prefix_len > 0x7FFFFF00 || ld_table < 0 || !(scale > 0.0f) || scale > 3.0e38f) return PATCH_ERR_SHAPE;
     if (B == 0) return PATCH_OK;
     // units of a sequence, summed over the batch, are counted in 32 bits (tiles of 64 keys or more, and each item's own cost)
-    if (ld_table > 0x7FFFFFFF || B * ((ld_table * cache->page_size + 63) / 64 + 8) > 0x7FFFFFFF) return PATCH_ERR_SHAPE;
+    if (ld_table > 0x7FFFFFFF || B * ((ld_table * cache->page_size + kDecodeKeys - 1) / kDecodeKeys + 8) > 0x7FFFFFFF) return PATCH_ERR_SHAPE;
     if (!Q || !O || !suffix_lens || (prefix_len && !prefix_pages) || (ld_table && !page_table)) return PATCH_ERR_NULL;
     const int D = cache->D;
     if (ldq < int64_t(Hq) * D || ldo < int64_t(Hq) * D || ldq % 8 || ldo % 8) return PATCH_ERR_SHAPE;
@@ -165,8 +165,9 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     const Results to = {{reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float2*>(ws + q.ml_p), reinterpret_cast<int2*>(ws), q.rows_p},
                         {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s}};
     const bool prefix = prefix_len > 0;
-    const Line dec = {prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : 1, int((prefix_len + kDecodeKeys - 1) / kDecodeKeys), kDecodeCost};
-    const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, int((prefix_len + kBlockKeys - 1) / kBlockKeys), kBlockCost};
+    auto tiles = [&](int keys) { return int((prefix_len + keys - 1) / keys); };
+    const Line dec = {prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : 1, tiles(kDecodeKeys), kDecodeCost};
+    const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, tiles(kBlockKeys), kBlockCost};
     const bool use_block = blk.blocks_p || blk.blocks_s, use_decode = dec.blocks_p || dec.blocks_s;
     if (use_block && (rc = launch_attn_block(cache, p, blk, to, use_decode, s))) return rc;
     if (use_decode && (rc = launch_attn_decode(cache, p, dec, to, use_block, s))) return rc;

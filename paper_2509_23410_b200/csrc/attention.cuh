@@ -56,13 +56,17 @@ __device__ __forceinline__ int suffix_len(const Problem& p, int b) {
     return int(n);
 }
 
-// Executed by one warp: units before each sequence (one key head, one row block) and the clamped lengths.
-__device__ __forceinline__ void lay_out(const Problem& p, const Line& w, int tile_keys, int* cum, int* lens) {
+// Executed by one warp: where the kernel has suffix items, units before each sequence (one key head, one row block) and the clamped
+// lengths.  Returns the batch's own keys.
+__device__ __forceinline__ int64_t lay_out(const Problem& p, const Line& w, int tile_keys, int* cum, int* lens) {
     const int lane = threadIdx.x & 31;
     int before = 0;
+    int64_t keys = 0;
     for (int b0 = 0; b0 < p.B; b0 += 32) {
         const int b = b0 + lane, n = b < p.B ? suffix_len(p, b) : 0;
-        int t = w.blocks_s ? n / tile_keys + (n % tile_keys != 0) : 0;
+        keys += n;
+        if (!w.blocks_s) continue;
+        int t = n / tile_keys + (n % tile_keys != 0);
         if (t) t += w.cost;
         if (b < p.B) lens[b] = n;
 #pragma unroll
@@ -73,12 +77,15 @@ __device__ __forceinline__ void lay_out(const Problem& p, const Line& w, int til
         if (b < p.B) cum[b + 1] = before + t;
         before += __shfl_sync(0xFFFFFFFFu, t, 31);
     }
-    if (lane == 0) cum[0] = 0;
+    if (lane == 0 && w.blocks_s) cum[0] = 0;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) keys += __shfl_xor_sync(0xFFFFFFFFu, keys, d);
+    return keys;
 }
 
 __host__ __device__ __forceinline__ int64_t prefix_units(const Line& w, int Hkv) { return int64_t(Hkv) * w.blocks_p * (w.tiles_p + w.cost); }
-__device__ __forceinline__ int64_t total_units(const Line& w, int Hkv, int cum_all) {
-    return prefix_units(w, Hkv) + int64_t(cum_all) * Hkv * w.blocks_s;
+__device__ __forceinline__ int64_t total_units(const Line& w, const Problem& p, const int* cum) {
+    return prefix_units(w, p.Hkv) + (w.blocks_s ? int64_t(cum[p.B]) * p.Hkv * w.blocks_s : 0);
 }
 // One CTA's share of the line, item by item.
 struct Share {

@@ -3,44 +3,63 @@
 // results are described in attention.cuh).
 //
 // Mathematics.  As in the decode kernel: running maximum m, sum l and unnormalised output o of every row, fp32, scores in powers of
-// two.  m is only raised when the scores of a tile exceed it by more than 8 (a factor of 256, harmless in fp32 and
-// for the bf16 probabilities, whose relative rounding does not depend on their size), so the accumulator is rarely rescaled.
+// two.  Any m serves as long as nothing overflows, so it is the maximum of the row's first tile and is raised only when a tile's
+// sum of 2^(s - m) passes 256: the sum is needed anyway, no maximum is taken of the other tiles, and the accumulator is rarely
+// rescaled.  (The relative rounding of the bf16 probabilities does not depend on their size.)
 //
-// Kernel.  One CTA per SM, 128 query rows and 128 keys per tcgen05.mma, two streams x = 0, 1 of
+// Kernel.  One CTA per SM, 128 query rows and 128 keys per tile, two streams x = 0, 1 of
 //     S_x = Q_x K^T (shared x shared -> TMEM),  P_x = 2^(S_x - m) (TMEM -> registers -> TMEM, over S_x),  O_x += P_x V (TMEM x shared)
 // so that one stream multiplies while the other is in its softmax.  An item of more than 128 rows gives each stream 128 rows, both
-// read the same keys; an item of fewer gives both streams the same rows and every second tile of keys, and the
-// two results are joined in TMEM at the end.
-//   warp 0       producer: tiles of keys and values, one TMA box per page and 64-element half, into a ring of four 32 KB stages (D = 128)
+// read the same keys; an item of fewer gives both streams the same rows and every second tile, and the two results are joined in
+// TMEM at the end.
+//   warp 0       producer: tiles of keys and values, one TMA box per page and 64-element half, into a ring of 32 KB stages (D = 128),
+//                as many as fit beside the query tiles
 //   warp 1       issues the MMAs; zeroes the rows of V past the item's last key (a probability of 0 times whatever the
 //                cache holds there is not always 0)
 //   warps 4..7   softmax of stream 0, one thread per row; warps 8..11 stream 1.  They also bring an item's query rows into the
 //                swizzled layout (any head count per key head, any row pitch) and write its partial result.
 // What bounds it: HBM up to about 256 rows per key head -- 64 KB of keys and values per tile and SM take 2 850 cycles, its
 // four products (two streams) 2 048, the exponentials 2 048.
+// Tried: tiles of 64 keys with two score buffers per stream, so that no stream waits for its own products: 5 600 cycles per 128
+// keys and two streams -- twice the MMAs of the scores and twice the waits, and the warp that issues them became the bottleneck.
 #include "attention.cuh"
 
 namespace patch {
 namespace attn {
 namespace blk {
+#ifndef V_TC
+#define V_TC 2000.0f
+#endif
 
 constexpr int kKeys = kBlockKeys;
-constexpr int kRing = 4;
+constexpr int kMaxRing = 8;
 constexpr int kThreads = 384;
-constexpr uint32_t kTmemCols = 512;                   // S_0, S_1 at 0, 128; O_0, O_1 at 256, 384
-constexpr float kSlack = 8.0f;                        // powers of two the running maximum may lag behind
+constexpr uint32_t kTmemCols = 512;                   // S_x at 128 x, O_x at 256 + 128 x
+constexpr float kMostSum = 256.0f;                    // of a tile's probabilities, before the maximum is raised
 
 template <int D> struct Cfg {
-    static constexpr uint32_t kAtom = 128 * 128;      // 128 rows x 64 elements
+    static constexpr uint32_t kAtom = kKeys * 128;    // 64 elements of every key
+    static constexpr uint32_t kQAtom = 128 * 128;     // 64 elements of every query row
     static constexpr uint32_t kTile = kKeys * D * 2;  // one operand of a key tile = one ring stage
     static constexpr uint32_t kQTile = 128 * D * 2;
-    static constexpr uint32_t kQOffset = kRing * kTile;
-    static constexpr uint32_t kMlOffset = kQOffset + 2 * kQTile;             // (m, l) of both streams' rows, to join them
-    static constexpr uint32_t kBarOffset = kMlOffset + 2 * 128 * 8;
-    static constexpr uint32_t kCumOffset = kBarOffset + 256;
-    static constexpr uint32_t kFixedBytes = kCumOffset + 1024;
-    static uint32_t smem_bytes(int B) { return kFixedBytes + uint32_t(2 * B + 1) * 4; }
+    static constexpr uint32_t kBarBytes = 256;
 };
+// Shared memory: [ring | query tiles | barriers | units and lengths of the sequences, where the kernel has suffix items].
+struct Room { int ring, q_tiles; uint32_t q, bars, cum, bytes; };
+template <int D>
+static Room room_of(const Line& w, int B, int rows) {
+    using C = Cfg<D>;
+    Room r;
+    r.q_tiles = rows > 128 ? 2 : 1;
+    const uint32_t cum = w.blocks_s ? uint32_t(2 * B + 1) * 4 : 0, rest = r.q_tiles * C::kQTile + C::kBarBytes + cum + 1024;
+    r.ring = int((227u * 1024 - rest) / C::kTile);
+    if (r.ring > kMaxRing) r.ring = kMaxRing;
+    r.q = r.ring * C::kTile;
+    r.bars = r.q + r.q_tiles * C::kQTile;
+    r.cum = r.bars + C::kBarBytes;
+    r.bytes = rest + r.ring * C::kTile;
+    return r;
+}
 
 // MN-major operand in 128-byte-swizzled atoms of 64 elements x 8 rows (the rows are the product's K): start address, stride between
 // the 64-element atoms, stride between groups of eight rows.
@@ -106,48 +125,45 @@ __device__ __forceinline__ float top_of(const uint32_t (&v)[32], float top) {
     for (int c = 0; c < 32; ++c) t[c & 3] = fmaxf(t[c & 3], __uint_as_float(v[c]));
     return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
-// Maximum of the row's 128 scores.
-__device__ __forceinline__ float row_top(uint32_t t_s, int left, bool partly) {
+// Maximum of the row's scores.
+__device__ __forceinline__ float row_top(uint32_t t_s, int left) {
     float top = -INFINITY;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
+#pragma unroll 1
+    for (int q = 0; q < kKeys / 32; ++q) {
         uint32_t v[32];
         tmem_ld32(t_s + 32u * q, v);
         tmem_ld_wait();
-        if (partly) hide(v, left - 32 * q);
+        hide(v, left - 32 * q);
         top = top_of(v, top);
     }
     return top;
 }
-// 2^(s scale + off) of the row's 128 scores as bf16, their sum (of the unrounded values) and the scores' maximum.  A quarter is
-// on its way from TMEM while the one before it is worked on.
-__device__ __forceinline__ void probabilities(uint32_t t_s, int left, bool partly, float scale, float off, uint32_t (&pr)[2][32],
-                                              float& top, float& sum) {
+// 2^(s scale + off) of the row's scores as bf16 and the sum of the unrounded values.  A quarter is on its way from TMEM while the
+// one before it is worked on.
+__device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool partly, float scale, float off, uint32_t (&pr)[2][32]) {
     const f2 scale2 = mk2(scale, scale), off2 = mk2(off, off);
-    f2 total[2] = {0ull, 0ull};
-    top = -INFINITY;
+    f2 sum[2] = {0ull, 0ull};
     uint32_t v[2][32];
     tmem_ld32(t_s, v[0]);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < kKeys / 32; ++q) {
         uint32_t (&s)[32] = v[q & 1];
         tmem_ld_wait();
-        if (q < 3) tmem_ld32(t_s + 32u * (q + 1), v[(q + 1) & 1]);
+        if (q + 1 < kKeys / 32) tmem_ld32(t_s + 32u * (q + 1), v[(q + 1) & 1]);
         if (partly) hide(s, left - 32 * q);
-        top = top_of(s, top);
 #pragma unroll
         for (int c = 0; c < 32; c += 2) {
             float e0, e1;
             un2(fma2(mk2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, off2), e0, e1);
             e0 = ex2(e0);
             e1 = ex2(e1);
-            total[(c >> 1) & 1] = add2(total[(c >> 1) & 1], mk2(e0, e1));
+            sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], mk2(e0, e1));
             pr[q >> 1][(q & 1) * 16 + (c >> 1)] = pack2(e0, e1);
         }
     }
     float a, b;
-    un2(add2(total[0], total[1]), a, b);
-    sum = a + b;
+    un2(add2(sum[0], sum[1]), a, b);
+    return a + b;
 }
 
 // Number of a stream's tiles among n: all of them where each stream has rows of its own, else every second.
@@ -159,13 +175,9 @@ __device__ __forceinline__ int stream_tiles(int n, bool dual, int x) { return du
 // bandwidth.  Cycles measured: 4 000 for a key tile and 256 rows, 2 000 for one and 128 rows, 700 for a tile of the decode kernel (two
 // CTAs share its latencies); bandwidth in bytes per cycle of 6.5 TB/s at 1.9 GHz.
 template <int D>
-__device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w, const int* lens, int sms) {
-    float keys = 0.0f;
-    for (int b = threadIdx.x & 31; b < p.B; b += 32) keys += float(lens[b]);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) keys += __shfl_xor_sync(0xFFFFFFFFu, keys, d);
+__device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w, float keys, int sms) {
     const float rows = float(p.B) * p.T * p.G, heads = float(p.Hkv);
-    const float mine = heads * w.tiles_p * 2000.0f * ceilf(rows / 128.0f);
+    const float mine = heads * w.tiles_p * V_TC * ceilf(rows / 128.0f);
     const float theirs = heads * keys / kDecodeKeys * 700.0f;
     const float bytes = heads * (keys + float(p.prefix_len)) * D * 4.0f;
     const float time = fmaxf(bytes / 3420.0f, (mine + theirs) / sms);
@@ -176,23 +188,25 @@ __device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w
 template <int D>
 __global__ void __launch_bounds__(blk::kThreads, 1)
 attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const Line w,
-                  const Results to, const int share_gpu) {
+                  const Results to, const blk::Room room, const bool share_gpu) {
     using namespace blk;
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t bar_full = base + C::kBarOffset, bar_empty = bar_full + 8 * kRing, bar_q = bar_empty + 8 * kRing, bar_s = bar_q + 8,
+    const int ring = room.ring;
+    const uint32_t bar_full = base + room.bars, bar_empty = bar_full + 8 * kMaxRing, bar_q = bar_empty + 8 * kMaxRing, bar_s = bar_q + 8,
                    bar_p = bar_s + 16, bar_o = bar_p + 16;
-    uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::kBarOffset + 192);
+    uint32_t* misc = reinterpret_cast<uint32_t*>(smem + room.bars + 208);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
-    int* cum = reinterpret_cast<int*>(smem + C::kCumOffset);
+    float* own_keys = reinterpret_cast<float*>(misc + 2);
+    int* cum = reinterpret_cast<int*>(smem + room.cum);
     int* lens = cum + p.B + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     grid_launch_dependents();
     if (threadIdx.x == 32) {
-        for (int i = 0; i < kRing; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+        for (int i = 0; i < ring; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
         mbar_init(bar_q, 8);                                   // one arrival per softmax warp
         for (int x = 0; x < 2; ++x) { mbar_init(bar_s + 8 * x, 1); mbar_init(bar_p + 8 * x, 4); }
         mbar_init(bar_o, 1);
@@ -201,25 +215,25 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         tma_prefetch_map(&map_k);
         tma_prefetch_map(&map_v);
     }
-    if (warp == 0) lay_out(p, w, kKeys, cum, lens);
+    if (warp == 0) {
+        const float keys = float(lay_out(p, w, kKeys, cum, lens));
+        if (lane == 0) *own_keys = keys;
+    }
     if (warp == 2) tmem_alloc(smem_u32(misc), kTmemCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *misc;
 
-    const int64_t total = total_units(w, p.Hkv, cum[p.B]);
+    const int64_t total = total_units(w, p, cum);
     int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
-    if (share_gpu) ctas = min(ctas, sms_beside_decode<D>(p, w, lens, gridDim.x));
+    if (share_gpu) ctas = min(ctas, sms_beside_decode<D>(p, w, *own_keys, gridDim.x));
     const bool busy = int(blockIdx.x) < ctas;
     const int64_t u0 = busy ? total * blockIdx.x / ctas : 0, u1 = busy ? total * (blockIdx.x + 1) / ctas : 0;
     Share s(p, w, cum, lens);
 
-    // registers: 384 threads x 168 at launch = 128 x 72 + 256 x 216
-    if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
-        // ---------------- producer: K0 K1 V0 K2 V1 ... (one stream's rows twice) or K0 V0 K1 V1 ... ----------------
+        // ---------------- producer: the first keys, then V0 K(lead) V1 K(lead + 1) ... as they are consumed ----------------
         const uint64_t policy = l2_policy_evict_first();
         const int rows_log2 = p.shift < 7 ? p.shift : 7;       // rows of a box: what one page gives to a tile
         const uint32_t box_bytes = 128u << rows_log2;
@@ -250,7 +264,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     page = 0;
                 }
                 bool free_slot = true;
-                if (lane == 0 && issued >= kRing) free_slot = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status);
+                if (lane == 0 && issued >= ring) free_slot = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status);
                 ok = __shfl_sync(0xFFFFFFFFu, free_slot ? 1 : 0, 0) != 0;
                 if (!ok) return;
                 const uint32_t full = bar_full + 8 * stage;
@@ -260,7 +274,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     tma_load_page(base + stage * C::kTile + (lane & 1) * C::kAtom + box * box_bytes, v ? &map_v : &map_k,
                                   p.shift < 7 ? 0 : int(key0 & ((1 << p.shift) - 1)), lane & 1, s.kvh, page, full, policy);
                 ++issued;
-                if (++stage == kRing) { stage = 0; phase ^= 1u; }
+                if (++stage == ring) { stage = 0; phase ^= 1u; }
             };
             const int lead = dual ? 1 : 2;
             for (int i = 0; i < lead && i < n && ok; ++i) load(i, 0);
@@ -271,27 +285,26 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
         if (*abort_flag) {
             const uint64_t t0 = global_timer_ns();
-            for (int j = issued > kRing ? issued - kRing : 0; j < issued; ++j)
-                while (!mbar_try_wait(bar_full + 8 * (j % kRing), uint32_t(j / kRing) & 1u) && global_timer_ns() - t0 < kDrainLimitNs) {}
+            for (int j = issued > ring ? issued - ring : 0; j < issued; ++j)
+                while (!mbar_try_wait(bar_full + 8 * (j % ring), uint32_t(j / ring) & 1u) && global_timer_ns() - t0 < kDrainLimitNs) {}
         }
     } else if (warp == 1) {
         // ---------------- MMAs ----------------
         constexpr uint32_t idesc_s = instr_desc(kKeys, false), idesc_o = instr_desc(D, false) | (1u << 16);      // V is MN-major
         int stage = 0;
-        uint32_t phase = 0, phase_q = 0, phase_p[2] = {0, 0};
+        uint32_t phase = 0, phase_q = 0, phase_p = 0;          // phase_p: bit x
         bool ok = true;
-        auto wait = [&](uint32_t bar, uint32_t parity) {       // the whole warp goes on together
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, p.status)) && ok;
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            ok = mbar_wait(bar, parity, abort_flag, p.status) && ok;
             tc_fence_after();
         };
-        auto advance = [&] { if (++stage == kRing) { stage = 0; phase ^= 1u; } };
+        auto advance = [&] { if (++stage == ring) { stage = 0; phase ^= 1u; } };
         auto scores = [&](int x, uint32_t q_tile, uint32_t k_tile) {
             const uint64_t dq = desc_kmajor_sw128(q_tile), dk = desc_kmajor_sw128(k_tile);
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                const uint64_t off = uint64_t(((ks >> 2) * C::kAtom + (ks & 3) * 32) >> 4);
-                mma_dense(tmem + 128u * x, dq + off, dk + off, idesc_s, ks != 0);
-            }
+            for (int ks = 0; ks < D / 16; ++ks)
+                mma_dense(tmem + 128u * x, dq + uint64_t(((ks >> 2) * C::kQAtom + (ks & 3) * 32) >> 4),
+                          dk + uint64_t(((ks >> 2) * C::kAtom + (ks & 3) * 32) >> 4), idesc_s, ks != 0);
             mma_commit(bar_s + 8 * x);
         };
         auto outputs = [&](int x, uint32_t v_tile, bool first) {
@@ -300,72 +313,78 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             for (int ks = 0; ks < kKeys / 16; ++ks)
                 mma_ta(tmem + 256u + 128u * x, tmem + 128u * x + 8u * ks, dv + uint64_t((ks * 2048) >> 4), idesc_o, !(first && ks == 0));
         };
+        // One thread runs an item from its first tile to its last (a vote of the warp at every wait cost 200 to 400 cycles each);
+        // only a tile with rows past the last key, an item's last, brings the warp together.
         for (bool have = s.start(u0, u1); have && ok; have = s.next()) {
             const bool dual = s.rows() - s.block * kBlockRows > 128;
             const int n = s.t1 - s.t0, lead = dual ? 1 : 2;
-            const uint32_t q0 = base + C::kQOffset, q1 = dual ? q0 + C::kQTile : q0;
-            wait(bar_q, phase_q);
-            phase_q ^= 1u;
-            for (int i = 0; i < lead && i < n && ok; ++i) {
-                wait(bar_full + 8 * stage, phase);
-                if (!ok) break;
-                if (elect_one()) {
+            const int valid = s.keys - (s.t1 - 1) * kKeys;     // rows of the last tile
+            const uint32_t q0 = base + room.q, q1 = dual ? q0 + C::kQTile : q0;
+            const bool leader = elect_one();
+            // products of tile i, and the scores of the tile that takes their place
+            auto tile = [&](int i, uint32_t v_stage) {
+                const bool more = i + lead < n;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    if (y == 1 && !dual) break;
+                    const int x = dual ? y : i & 1;
+                    const bool last = !dual || y == 1;
+                    wait(bar_p + 8 * x, (phase_p >> x) & 1u);
+                    phase_p ^= 1u << x;
+                    if (!ok) return;
+                    outputs(x, base + v_stage * C::kTile, dual ? i == 0 : i < 2);
+                    if (last) mma_commit(bar_empty + 8 * v_stage);
+                    if (!more) continue;
+                    if (y == 0) wait(bar_full + 8 * stage, phase);
+                    if (!ok) return;
+                    scores(x, x ? q1 : q0, base + stage * C::kTile);
+                    if (last) mma_commit(bar_empty + 8 * stage);
+                }
+                if (more) advance();
+            };
+            uint32_t v_last = 0;
+            if (leader) {
+                wait(bar_q, phase_q);
+                for (int i = 0; i < lead && i < n && ok; ++i) {
+                    wait(bar_full + 8 * stage, phase);
+                    if (!ok) break;
                     const uint32_t k_tile = base + stage * C::kTile;
                     if (dual || i == 0) scores(0, q0, k_tile);
                     if (dual || i == 1) scores(1, q1, k_tile);
                     mma_commit(bar_empty + 8 * stage);
+                    advance();
                 }
-                __syncwarp();
-                advance();
+                for (int i = 0; i < n && ok; ++i) {
+                    wait(bar_full + 8 * stage, phase);
+                    if (!ok) break;
+                    const uint32_t v_stage = stage;
+                    advance();
+                    if (i == n - 1 && valid < kKeys) v_last = v_stage;
+                    else tile(i, v_stage);
+                }
             }
-            for (int i = 0; i < n && ok; ++i) {
-                wait(bar_full + 8 * stage, phase);
+            phase_q ^= 1u;
+            if (valid < kKeys) {                               // rows past the last key: zeros
+                ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
-                const uint32_t v_tile = base + stage * C::kTile, v_empty = bar_empty + 8 * stage;
-                advance();
-                const int valid = s.keys - (s.t0 + i) * kKeys;
-                if (valid < kKeys) {                           // rows past the last key: zeros
-                    for (int j = valid * (D / 8) + lane; j < kKeys * (D / 8); j += 32) {
-                        const int r = j / (D / 8), c = j - r * (D / 8);
-                        *reinterpret_cast<uint4*>(smem + (v_tile - base) + (c >> 3) * C::kAtom + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    fence_async_shared();
-                    __syncwarp();
+                v_last = __reduce_max_sync(0xFFFFFFFFu, v_last);
+                for (int j = valid * (D / 8) + lane; j < kKeys * (D / 8); j += 32) {
+                    const int r = j / (D / 8), c = j - r * (D / 8);
+                    *reinterpret_cast<uint4*>(smem + v_last * C::kTile + (c >> 3) * C::kAtom + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
-                const bool more = i + lead < n;
-                for (int y = 0; y < (dual ? 2 : 1) && ok; ++y) {
-                    const int x = dual ? y : i & 1;
-                    wait(bar_p + 8 * x, phase_p[x]);
-                    phase_p[x] ^= 1u;
-                    if (!ok) break;
-                    const bool first = dual ? i == 0 : i < 2, v_done = !dual || y == 1;
-                    if (elect_one()) {
-                        outputs(x, v_tile, first);
-                        if (v_done) mma_commit(v_empty);
-                    }
-                    __syncwarp();
-                    if (!more) continue;
-                    if (y == 0) wait(bar_full + 8 * stage, phase);       // the stream's next keys
-                    if (!ok) break;
-                    if (elect_one()) {
-                        scores(x, x ? q1 : q0, base + stage * C::kTile);
-                        if (v_done) mma_commit(bar_empty + 8 * stage);
-                    }
-                    __syncwarp();
-                }
-                if (more) advance();
+                fence_async_shared();
+                __syncwarp();
+                if (leader) tile(n - 1, v_last);
             }
-            if (ok && elect_one()) mma_commit(bar_o);
-            __syncwarp();
+            if (leader && ok) mma_commit(bar_o);
+            ok = __all_sync(0xFFFFFFFFu, ok);
         }
-    }
-    } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    } else if (warp >= 4) {
         // ---------------- softmax: thread = row of the stream ----------------
         const int x = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = uint32_t(quad * 32) << 16;
         const uint32_t t_s = tmem + lanes + 128u * x, t_o = tmem + lanes + 256u + 128u * x;
-        float2* ml = reinterpret_cast<float2*>(smem + C::kMlOffset);
+        float2* ml = reinterpret_cast<float2*>(smem + room.q);       // (m, l) of both streams' rows, where the queries were
         uint32_t phase_s = 0, phase_o = 0;
         bool failed = false;
         for (bool have = s.start(u0, u1); have && !failed; have = s.next()) {
@@ -378,12 +397,15 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             if (dual || x == 0) {
                 const int64_t tok = (s.b < 0 ? 0 : int64_t(s.b) * p.T) + r / p.G;
                 const __nv_bfloat16* src = p.Q + tok * p.ldq + int64_t(s.kvh * p.G + r % p.G) * D;
-                uint8_t* dst = smem + C::kQOffset + x * C::kQTile;
-                uint4 v[D / 8];
+                uint8_t* dst = smem + room.q + x * C::kQTile;
+#pragma unroll 1
+                for (int h = 0; h < D / 64; ++h) {
+                    uint4 v[8];
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) v[c] = valid ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int c = 0; c < 8; ++c) v[c] = valid ? *reinterpret_cast<const uint4*>(src + 64 * h + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(dst + (c >> 3) * C::kAtom + atom_chunk_offset(row, c & 7)) = v[c];
+                    for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(dst + h * C::kQAtom + atom_chunk_offset(row, c)) = v[c];
+                }
                 fence_async_shared();
             }
             __syncwarp();
@@ -391,41 +413,36 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const int see = s.b < 0 ? s.keys : s.keys - (p.T - 1 - r / p.G);      // keys the row sees
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < mine; ++j) {
-                failed = !mbar_wait(bar_s + 8 * x, phase_s, abort_flag, p.status);
-                failed = __any_sync(0xFFFFFFFFu, failed);
+                failed = __any_sync(0xFFFFFFFFu, !mbar_wait(bar_s + 8 * x, phase_s, abort_flag, p.status));
                 if (failed) break;
                 phase_s ^= 1u;
                 tc_fence_after();
                 const int left = see - (s.t0 + (dual ? j : 2 * j + x)) * kKeys;      // columns the row sees
                 const bool partly = __any_sync(0xFFFFFFFFu, left < kKeys);
-                if (j == 0) {
-                    m = fmaxf(m, row_top(t_s, left, partly) * p.scale_log2);
-                }
-                // Probabilities with the maximum as it stands, and the scores' maximum beside them: a pass that turns out to need
-                // a higher one is taken again (S is overwritten only by the stores below), which is rare after the first tile.
+                if (j == 0) m = row_top(t_s, left) * p.scale_log2;
                 uint32_t pr[2][32];
                 for (;;) {
-                    float top, sum;
-                    probabilities(t_s, left, partly, p.scale_log2, m == -INFINITY ? 0.0f : -m, pr, top, sum);
-                    top *= p.scale_log2;
-                    if (!__any_sync(0xFFFFFFFFu, top > m + kSlack)) {
+                    const float sum = probabilities(t_s, left, partly, p.scale_log2, m == -INFINITY ? 0.0f : -m, pr);
+                    if (!__any_sync(0xFFFFFFFFu, sum > kMostSum && m != INFINITY)) {
                         l += sum;
                         break;
                     }
-                    const float up = fmaxf(m, top), a = up == -INFINITY ? 1.0f : ex2(m - up);
+                    // a higher maximum, and the scores (still in TMEM) once more: afterwards the sum is at most the tile's keys
+                    const float up = fmaxf(m, row_top(t_s, left) * p.scale_log2), a = up == -INFINITY ? 1.0f : ex2(m - up);
                     m = up;
                     l *= a;
-                    if (j > 0) {                               // the scores were issued behind the last product, which is done
+                    if (j == 0) continue;
+                    // the scores were issued behind the stream's last product, which is therefore done
+#pragma unroll 1
+                    for (int q = 0; q < D / 32; ++q) {
+                        uint32_t o[32];
+                        tmem_ld32(t_o + 32u * q, o);
+                        tmem_ld_wait();
 #pragma unroll
-                        for (int q = 0; q < D / 32; ++q) {
-                            uint32_t o[32];
-                            tmem_ld32(t_o + 32u * q, o);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * a);
-                            tmem_st32(t_o + 32u * q, o);
-                        }
+                        for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * a);
+                        tmem_st32(t_o + 32u * q, o);
                     }
+                    tmem_st_wait();
                 }
                 tmem_st32(t_s, pr[0]);
                 tmem_st32(t_s + 32u, pr[1]);
@@ -444,7 +461,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const int64_t at = (s.item + int64_t(blockIdx.x)) * part.rows + (dual ? 128 * x : 0) + row;
             float* dst = part.o + at * D;
             if (dual) {
-#pragma unroll
+#pragma unroll 1
                 for (int q = 0; q < D / 32; ++q) {
                     uint32_t o[32];
                     tmem_ld32(t_o + 32u * q, o);
@@ -465,7 +482,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 const float2 a = ml[row], b = ml[128 + row];
                 const float mx = fmaxf(a.x, b.x);
                 const float fa = a.x == -INFINITY ? 0.0f : ex2(a.x - mx), fb = b.x == -INFINITY ? 0.0f : ex2(b.x - mx);
-#pragma unroll
+#pragma unroll 1
                 for (int q = 0; q < D / 64; ++q) {
                     const uint32_t col = uint32_t(x) * (D / 2) + 32u * q;
                     uint32_t o0[32], o1[32];
@@ -497,7 +514,6 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
 template <int D>
 static int launch_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool share_gpu, cudaStream_t stream) {
-    using C = blk::Cfg<D>;
     CUtensorMap mk, mv;
     const int rows = c->page_size < blk::kKeys ? c->page_size : blk::kKeys;
     int rc = make_kv_tensor_map(&mk, c, c->k_dev, rows, 1);
@@ -505,10 +521,11 @@ static int launch_block(const patch_kv_cache_t* c, const Problem& p, const Line&
     if (rc) return rc;
     auto kern = attn_block_kernel<D>;
     static std::atomic<uint64_t> configured{0};
-    if ((rc = allow_dynamic_smem(kern, C::smem_bytes(kMaxBatch), configured))) return rc;
+    if ((rc = allow_dynamic_smem(kern, 227 * 1024, configured))) return rc;
+    const blk::Room room = blk::room_of<D>(w, p.B, w.blocks_p ? to.p.rows : to.s.rows);
     const int sms = sm_count();
     if (sms <= 0) return PATCH_ERR_CUDA;
-    kern<<<sms < kMaxSms ? sms : kMaxSms, blk::kThreads, C::smem_bytes(p.B), stream>>>(mk, mv, p, w, to, share_gpu);
+    kern<<<sms < kMaxSms ? sms : kMaxSms, blk::kThreads, room.bytes, stream>>>(mk, mv, p, w, to, room, share_gpu);
     return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
 }
 

@@ -84,7 +84,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
     if (warp == 0) lay_out(p, w, kKeys, cum, lens);
     __syncthreads();
-    const int64_t total = total_units(w, p.Hkv, cum[p.B]);
+    const int64_t total = total_units(w, p, cum);
     const int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
     const bool busy = int(blockIdx.x) < ctas;
     // a copy brings the rows of one page that fall into a tile
