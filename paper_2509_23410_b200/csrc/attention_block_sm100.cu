@@ -125,11 +125,11 @@ __device__ __forceinline__ float top_of(const uint32_t (&v)[32], float top) {
     for (int c = 0; c < 32; ++c) t[c & 3] = fmaxf(t[c & 3], __uint_as_float(v[c]));
     return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
-// Maximum of the row's scores.
-__device__ __forceinline__ float row_top(uint32_t t_s, int left) {
+// Maximum of 32 n scores of the row.
+__device__ __forceinline__ float row_top(uint32_t t_s, int n, int left) {
     float top = -INFINITY;
 #pragma unroll 1
-    for (int q = 0; q < kKeys / 32; ++q) {
+    for (int q = 0; q < n; ++q) {
         uint32_t v[32];
         tmem_ld32(t_s + 32u * q, v);
         tmem_ld_wait();
@@ -138,28 +138,26 @@ __device__ __forceinline__ float row_top(uint32_t t_s, int left) {
     }
     return top;
 }
-// 2^(s scale + off) of the row's scores as bf16 and the sum of the unrounded values.  A quarter is on its way from TMEM while the
-// one before it is worked on.
-__device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool partly, float scale, float off, uint32_t (&pr)[2][32]) {
+// 2^(s scale + off) of 64 scores of the row as bf16 and the sum of the unrounded values.
+__device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool partly, float scale, float off, uint32_t (&pr)[32]) {
     const f2 scale2 = mk2(scale, scale), off2 = mk2(off, off);
     f2 sum[2] = {0ull, 0ull};
     uint32_t v[2][32];
     tmem_ld32(t_s, v[0]);
+    tmem_ld32(t_s + 32u, v[1]);
+    tmem_ld_wait();
+    if (partly) {
+        hide(v[0], left);
+        hide(v[1], left - 32);
+    }
 #pragma unroll
-    for (int q = 0; q < kKeys / 32; ++q) {
-        uint32_t (&s)[32] = v[q & 1];
-        tmem_ld_wait();
-        if (q + 1 < kKeys / 32) tmem_ld32(t_s + 32u * (q + 1), v[(q + 1) & 1]);
-        if (partly) hide(s, left - 32 * q);
-#pragma unroll
-        for (int c = 0; c < 32; c += 2) {
-            float e0, e1;
-            un2(fma2(mk2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, off2), e0, e1);
-            e0 = ex2(e0);
-            e1 = ex2(e1);
-            sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], mk2(e0, e1));
-            pr[q >> 1][(q & 1) * 16 + (c >> 1)] = pack2(e0, e1);
-        }
+    for (int c = 0; c < 64; c += 2) {
+        float e0, e1;
+        un2(fma2(mk2(__uint_as_float(v[c >> 5][c & 31]), __uint_as_float(v[c >> 5][(c & 31) + 1])), scale2, off2), e0, e1);
+        e0 = ex2(e0);
+        e1 = ex2(e1);
+        sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], mk2(e0, e1));
+        pr[c >> 1] = pack2(e0, e1);
     }
     float a, b;
     un2(add2(sum[0], sum[1]), a, b);
@@ -195,9 +193,10 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem = smem_raw + (base - smem_u32(smem_raw));
     const int ring = room.ring;
+    // per stream x, at 8 x: bar_s scores, bar_p probabilities (the second half's at 16 + 8 x), bar_h product of the first half
     const uint32_t bar_full = base + room.bars, bar_empty = bar_full + 8 * kMaxRing, bar_q = bar_empty + 8 * kMaxRing, bar_s = bar_q + 8,
-                   bar_p = bar_s + 16, bar_o = bar_p + 16;
-    uint32_t* misc = reinterpret_cast<uint32_t*>(smem + room.bars + 208);
+                   bar_p = bar_s + 16, bar_h = bar_p + 32, bar_o = bar_h + 16;
+    uint32_t* misc = reinterpret_cast<uint32_t*>(smem + room.bars + 224);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
     float* own_keys = reinterpret_cast<float*>(misc + 2);
     int* cum = reinterpret_cast<int*>(smem + room.cum);
@@ -208,7 +207,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (threadIdx.x == 32) {
         for (int i = 0; i < ring; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
         mbar_init(bar_q, 8);                                   // one arrival per softmax warp
-        for (int x = 0; x < 2; ++x) { mbar_init(bar_s + 8 * x, 1); mbar_init(bar_p + 8 * x, 4); }
+        for (int x = 0; x < 2; ++x) { mbar_init(bar_s + 8 * x, 1); mbar_init(bar_p + 8 * x, 4); mbar_init(bar_p + 16 + 8 * x, 4); mbar_init(bar_h + 8 * x, 1); }
         mbar_init(bar_o, 1);
         *abort_flag = 0;
         mbar_init_fence();
@@ -307,77 +306,70 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                           dk + uint64_t(((ks >> 2) * C::kAtom + (ks & 3) * 32) >> 4), idesc_s, ks != 0);
             mma_commit(bar_s + 8 * x);
         };
-        auto outputs = [&](int x, uint32_t v_tile, bool first) {
-            const uint64_t dv = desc_mnmajor_sw128(v_tile, C::kAtom);
+        auto outputs = [&](int x, uint32_t v_tile, bool first, int half) {          // of 64 keys
+            const uint64_t dv = desc_mnmajor_sw128(v_tile + half * 64 * 128, C::kAtom);
 #pragma unroll
-            for (int ks = 0; ks < kKeys / 16; ++ks)
-                mma_ta(tmem + 256u + 128u * x, tmem + 128u * x + 8u * ks, dv + uint64_t((ks * 2048) >> 4), idesc_o, !(first && ks == 0));
+            for (int ks = 0; ks < kKeys / 32; ++ks)
+                mma_ta(tmem + 256u + 128u * x, tmem + 128u * x + 32u * half + 8u * ks, dv + uint64_t((ks * 2048) >> 4), idesc_o, !(first && ks == 0));
         };
         // One thread runs an item from its first tile to its last (a vote of the warp at every wait cost 200 to 400 cycles each);
-        // only a tile with rows past the last key, an item's last, brings the warp together.
+        // only a tile with rows past the last key, an item's last, brings the warp together.  Loops stay rolled: this warp's few
+        // instructions compete with the softmax warps' for the instruction cache.
         for (bool have = s.start(u0, u1); have && ok; have = s.next()) {
             const bool dual = s.rows() - s.block * kBlockRows > 128;
             const int n = s.t1 - s.t0, lead = dual ? 1 : 2;
             const int valid = s.keys - (s.t1 - 1) * kKeys;     // rows of the last tile
             const uint32_t q0 = base + room.q, q1 = dual ? q0 + C::kQTile : q0;
             const bool leader = elect_one();
-            // products of tile i, and the scores of the tile that takes their place
-            auto tile = [&](int i, uint32_t v_stage) {
-                const bool more = i + lead < n;
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    if (y == 1 && !dual) break;
-                    const int x = dual ? y : i & 1;
-                    const bool last = !dual || y == 1;
-                    wait(bar_p + 8 * x, (phase_p >> x) & 1u);
-                    phase_p ^= 1u << x;
-                    if (!ok) return;
-                    outputs(x, base + v_stage * C::kTile, dual ? i == 0 : i < 2);
-                    if (last) mma_commit(bar_empty + 8 * v_stage);
-                    if (!more) continue;
-                    if (y == 0) wait(bar_full + 8 * stage, phase);
-                    if (!ok) return;
-                    scores(x, x ? q1 : q0, base + stage * C::kTile);
-                    if (last) mma_commit(bar_empty + 8 * stage);
-                }
-                if (more) advance();
-            };
-            uint32_t v_last = 0;
-            if (leader) {
-                wait(bar_q, phase_q);
-                for (int i = 0; i < lead && i < n && ok; ++i) {
-                    wait(bar_full + 8 * stage, phase);
-                    if (!ok) break;
-                    const uint32_t k_tile = base + stage * C::kTile;
-                    if (dual || i == 0) scores(0, q0, k_tile);
-                    if (dual || i == 1) scores(1, q1, k_tile);
-                    mma_commit(bar_empty + 8 * stage);
-                    advance();
-                }
-                for (int i = 0; i < n && ok; ++i) {
-                    wait(bar_full + 8 * stage, phase);
-                    if (!ok) break;
-                    const uint32_t v_stage = stage;
-                    advance();
-                    if (i == n - 1 && valid < kKeys) v_last = v_stage;
-                    else tile(i, v_stage);
-                }
-            }
+            int i = -lead;                                     // tile whose products are next; below 0: scores only
+            uint32_t v_stage = 0;
+            if (leader) wait(bar_q, phase_q);
             phase_q ^= 1u;
-            if (valid < kKeys) {                               // rows past the last key: zeros
+            for (bool zeroed = valid >= kKeys;; zeroed = true) {
+                if (leader) {
+#pragma unroll 1
+                    for (; i < n && ok; ++i) {
+                        if (i >= 0 && (i + 1 < n || !zeroed || valid >= kKeys)) {
+                            wait(bar_full + 8 * stage, phase);
+                            v_stage = stage;
+                            advance();
+                        }
+                        if (i + 1 == n && !zeroed) break;
+                        const bool more = i + lead < n;
+#pragma unroll 1
+                        for (int y = 0; y < (dual ? 2 : 1) && ok; ++y) {
+                            const int x = dual ? y : i & 1;
+                            const bool last = !dual || y == 1;
+                            if (i >= 0) {
+#pragma unroll 1
+                                for (int half = 0; half < 2 && ok; ++half) {
+                                    wait(bar_p + 16 * half + 8 * x, (phase_p >> x) & 1u);
+                                    if (ok) outputs(x, base + v_stage * C::kTile, (dual ? i == 0 : i < 2) && half == 0, half);
+                                    if (half == 0) mma_commit(bar_h + 8 * x);
+                                }
+                                phase_p ^= 1u << x;
+                                if (last) mma_commit(bar_empty + 8 * v_stage);
+                            }
+                            if (!more) continue;
+                            if (y == 0) wait(bar_full + 8 * stage, phase);
+                            if (ok) scores(x, x ? q1 : q0, base + stage * C::kTile);
+                            if (last) mma_commit(bar_empty + 8 * stage);
+                        }
+                        if (more) advance();
+                    }
+                    if (ok && zeroed) mma_commit(bar_o);
+                }
                 ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) break;
-                v_last = __reduce_max_sync(0xFFFFFFFFu, v_last);
+                if (zeroed || !ok) break;
+                // rows past the last key: zeros
+                v_stage = __reduce_max_sync(0xFFFFFFFFu, v_stage);
                 for (int j = valid * (D / 8) + lane; j < kKeys * (D / 8); j += 32) {
                     const int r = j / (D / 8), c = j - r * (D / 8);
-                    *reinterpret_cast<uint4*>(smem + v_last * C::kTile + (c >> 3) * C::kAtom + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4*>(smem + v_stage * C::kTile + (c >> 3) * C::kAtom + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
                 fence_async_shared();
                 __syncwarp();
-                if (leader) tile(n - 1, v_last);
             }
-            if (leader && ok) mma_commit(bar_o);
-            ok = __all_sync(0xFFFFFFFFu, ok);
         }
     } else if (warp >= 4) {
         // ---------------- softmax: thread = row of the stream ----------------
@@ -385,7 +377,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         const uint32_t lanes = uint32_t(quad * 32) << 16;
         const uint32_t t_s = tmem + lanes + 128u * x, t_o = tmem + lanes + 256u + 128u * x;
         float2* ml = reinterpret_cast<float2*>(smem + room.q);       // (m, l) of both streams' rows, where the queries were
-        uint32_t phase_s = 0, phase_o = 0;
+        uint32_t phase_s = 0, phase_h = 0, phase_o = 0;
         bool failed = false;
         for (bool have = s.start(u0, u1); have && !failed; have = s.next()) {
             const int rows = s.rows() - s.block * kBlockRows;  // of this block and the ones after it
@@ -419,37 +411,49 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 tc_fence_after();
                 const int left = see - (s.t0 + (dual ? j : 2 * j + x)) * kKeys;      // columns the row sees
                 const bool partly = __any_sync(0xFFFFFFFFu, left < kKeys);
-                if (j == 0) m = row_top(t_s, left) * p.scale_log2;
-                uint32_t pr[2][32];
-                for (;;) {
-                    const float sum = probabilities(t_s, left, partly, p.scale_log2, m == -INFINITY ? 0.0f : -m, pr);
-                    if (!__any_sync(0xFFFFFFFFu, sum > kMostSum && m != INFINITY)) {
-                        l += sum;
-                        break;
-                    }
-                    // a higher maximum, and the scores (still in TMEM) once more: afterwards the sum is at most the tile's keys
-                    const float up = fmaxf(m, row_top(t_s, left) * p.scale_log2), a = up == -INFINITY ? 1.0f : ex2(m - up);
-                    m = up;
-                    l *= a;
-                    if (j == 0) continue;
-                    // the scores were issued behind the stream's last product, which is therefore done
+                if (j == 0) m = row_top(t_s, kKeys / 32, left) * p.scale_log2;
+                // The products of the first half of the keys start while the second half is worked on.
 #pragma unroll 1
-                    for (int q = 0; q < D / 32; ++q) {
-                        uint32_t o[32];
-                        tmem_ld32(t_o + 32u * q, o);
-                        tmem_ld_wait();
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t t_h = t_s + 64u * half;
+                    uint32_t pr[32];
+                    for (;;) {
+                        const float sum = probabilities(t_h, left - 64 * half, partly, p.scale_log2, m == -INFINITY ? 0.0f : -m, pr);
+                        if (!__any_sync(0xFFFFFFFFu, sum > kMostSum && m != INFINITY)) {
+                            l += sum;
+                            break;
+                        }
+                        // a higher maximum, and the scores (still in TMEM) once more: afterwards the sum is at most the number of keys
+                        const float up = fmaxf(m, row_top(t_h, 2, left - 64 * half) * p.scale_log2), a = up == -INFINITY ? 1.0f : ex2(m - up);
+                        m = up;
+                        l *= a;
+                        if (j == 0 && half == 0) continue;
+                        // the scores were issued behind the stream's last product, which is therefore done; the first half's is waited for
+                        if (half == 1) {
+                            failed = __any_sync(0xFFFFFFFFu, !mbar_wait(bar_h + 8 * x, phase_h, abort_flag, p.status));
+                            if (failed) break;
+                            tc_fence_after();
+                        }
+#pragma unroll 1
+                        for (int q = 0; q < D / 32; ++q) {
+                            uint32_t o[32];
+                            tmem_ld32(t_o + 32u * q, o);
+                            tmem_ld_wait();
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * a);
-                        tmem_st32(t_o + 32u * q, o);
+                            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * a);
+                            tmem_st32(t_o + 32u * q, o);
+                        }
+                        tmem_st_wait();
                     }
+                    if (failed) break;
+                    tmem_st32(t_s + 32u * half, pr);
                     tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_p + 16 * half + 8 * x);
                 }
-                tmem_st32(t_s, pr[0]);
-                tmem_st32(t_s + 32u, pr[1]);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar_p + 8 * x);
+                phase_h ^= 1u;
+                if (failed) break;
             }
             if (!failed) failed = !mbar_wait(bar_o, phase_o, abort_flag, p.status);
             phase_o ^= 1u;
