@@ -8,6 +8,9 @@
 
 namespace patch {
 namespace attn {
+#ifndef V_MR
+#define V_MR 64
+#endif
 
 // Joins the partial results: one warp per query row and head.  Bound by the latency of three dependent reads (which CTAs, their
 // (m, l), their outputs); the (m, l) of up to 32 parts are read at once, one per lane, their outputs eight at a time.
@@ -85,8 +88,12 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
 // ---------------------------------------------------------------------------------------------
 // host side
 
-// Which kernel serves a phase, and its items' rows.  Up to 16 rows the decode kernel's tile (16 rows of mma.sync) holds them
-// and HBM is what it waits for; more rows would have it read the keys once per 16.
+// Which kernel serves a phase.  The prefix: the decode kernel where its 16 rows of mma.sync hold all rows (HBM is what it waits
+// for), else the block kernel (32 rows of two blocks on the decode kernel would read the prefix twice).  The suffixes: their
+// items are short, and an item costs the block kernel about 7 us (queries, first tile, result), so up to four blocks of 16 rows
+// stay on the decode kernel -- the keys come from L2 from the second block on (five tokens of four heads, 16 sequences of up to
+// 777 keys: V_T5A us against V_T5B us).
+constexpr int kMostDecodeRows = V_MR;
 struct Plan {
     bool block_p, block_s;                           // prefix / suffixes on the block kernel
     int blocks_p, blocks_s, rows_p, rows_s;          // row blocks per key head, rows of a slot
@@ -95,11 +102,13 @@ struct Plan {
 static Plan plan_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G) {
     Plan q;
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-    auto rows = [&](int64_t all, bool& block, int& blocks) {
-        block = all > kFewRows;
-        blocks = block ? int((all + kBlockRows - 1) / kBlockRows) : 1;
-        return int(all < kBlockRows ? all : kBlockRows);
+    auto rows = [&](int64_t all, bool block, int& blocks) {
+        const int most = block ? kBlockRows : kDecodeRows;
+        blocks = int((all + most - 1) / most);
+        return int(all < most ? all : most);
     };
+    q.block_p = B * T * G > kDecodeRows;
+    q.block_s = T * G > kMostDecodeRows;
     q.rows_p = rows(B * T * G, q.block_p, q.blocks_p);
     q.rows_s = rows(T * G, q.block_s, q.blocks_s);
     // a slot for every item and every CTA that may share one
@@ -166,7 +175,7 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
                         {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s}};
     const bool prefix = prefix_len > 0;
     auto tiles = [&](int keys) { return int((prefix_len + keys - 1) / keys); };
-    const Line dec = {prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : 1, tiles(kDecodeKeys), kDecodeCost};
+    const Line dec = {prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : q.blocks_s, tiles(kDecodeKeys), kDecodeCost};
     const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, tiles(kBlockKeys), kBlockCost};
     const bool use_block = blk.blocks_p || blk.blocks_s, use_decode = dec.blocks_p || dec.blocks_s;
     if (use_block && (rc = launch_attn_block(cache, p, blk, to, use_decode, s))) return rc;

@@ -3,7 +3,7 @@
 //
 // Work list.  An item is a set of query rows of one key head that read the same keys: rows of the batch against the shared
 // prefix, or one sequence's rows against its own keys.  An item's keys are cut into tiles; all tiles of all items,
-// item after item, form one line of U units, and CTA c of n owns units [c U / n, (c + 1) U / n): every CTA gets the same amount of
+// item after item, form one line of U units, and every CTA owns a stretch of it (of equal length, where all run at once): the same amount of
 // work whatever the lengths are, at the price of items that several CTAs share.  An item also has a few units without a tile, which
 // stand for what it costs by itself.  Each CTA writes one partial result (running maximum, sum and unnormalised output, fp32)
 // per item it has a share of.  Along the line the pair (item, CTA) changes one step at a time, so item + c numbers the partial
@@ -57,25 +57,32 @@ __device__ __forceinline__ int suffix_len(const Problem& p, int b) {
 }
 
 // Executed by one warp: where the kernel has suffix items, units before each sequence (one key head, one row block) and the clamped
-// lengths.  Returns the batch's own keys.
+// lengths.  Returns the batch's own keys.  (Every CTA waits for this: four groups of lengths are on their way at once.)
 __device__ __forceinline__ int64_t lay_out(const Problem& p, const Line& w, int tile_keys, int* cum, int* lens) {
+    constexpr int kAtOnce = 4;
     const int lane = threadIdx.x & 31;
     int before = 0;
     int64_t keys = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 32) {
-        const int b = b0 + lane, n = b < p.B ? suffix_len(p, b) : 0;
-        keys += n;
-        if (!w.blocks_s) continue;
-        int t = n / tile_keys + (n % tile_keys != 0);
-        if (t) t += w.cost;
-        if (b < p.B) lens[b] = n;
+    for (int g0 = 0; g0 < p.B; g0 += 32 * kAtOnce) {
+        int n[kAtOnce];
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xFFFFFFFFu, t, d);
-            if (lane >= d) t += o;
+        for (int i = 0; i < kAtOnce; ++i) n[i] = g0 + 32 * i + lane < p.B ? suffix_len(p, g0 + 32 * i + lane) : 0;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int b = g0 + 32 * i + lane;
+            keys += n[i];
+            if (!w.blocks_s || g0 + 32 * i >= p.B) continue;
+            int t = n[i] / tile_keys + (n[i] % tile_keys != 0);
+            if (t) t += w.cost;
+            if (b < p.B) lens[b] = n[i];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xFFFFFFFFu, t, d);
+                if (lane >= d) t += o;
+            }
+            if (b < p.B) cum[b + 1] = before + t;
+            before += __shfl_sync(0xFFFFFFFFu, t, 31);
         }
-        if (b < p.B) cum[b + 1] = before + t;
-        before += __shfl_sync(0xFFFFFFFFu, t, 31);
     }
     if (lane == 0 && w.blocks_s) cum[0] = 0;
 #pragma unroll
@@ -87,6 +94,13 @@ __host__ __device__ __forceinline__ int64_t prefix_units(const Line& w, int Hkv)
 __device__ __forceinline__ int64_t total_units(const Line& w, const Problem& p, const int* cum) {
     return prefix_units(w, p.Hkv) + (w.blocks_s ? int64_t(cum[p.B]) * p.Hkv * w.blocks_s : 0);
 }
+// First unit of CTA c's share of U units among n <= U CTAs: equal shares where all CTAs run at once (c U / n); where they take turns on
+// whatever SMs another kernel leaves free, shares that shrink from 7/4 to 1/4 of the average, so that the last ones to run are
+// short.  No share is empty: a CTA between an item's first and last one has a tile of it.
+__device__ __forceinline__ int64_t share_start(int64_t U, int c, int n, bool in_turns) {
+    return in_turns && U >= 4 * int64_t(n) ? U * c * (7 * n - 3 * c) / (4 * int64_t(n) * n) : U * c / n;
+}
+
 // One CTA's share of the line, item by item.
 struct Share {
     const Problem& p;
@@ -191,12 +205,14 @@ __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* m
         ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(bar), "l"(policy) : "memory");
 }
 
-// Items of at most kFewRows query rows per key head go to the decode kernel (attention_decode_sm100.cu), others to the block
-// kernel (attention_block_sm100.cu).
-constexpr int kFewRows = 16;
-constexpr int kBlockRows = 256;
+// The decode kernel (attention_decode_sm100.cu) takes rows in blocks of kDecodeRows, the block kernel (attention_block_sm100.cu) in
+// blocks of kBlockRows.
+constexpr int kDecodeRows = 16, kBlockRows = 256;
+#ifndef V_BC
+#define V_BC 3
+#endif
 constexpr int kDecodeKeys = 64, kBlockKeys = 128;     // keys of a tile
-constexpr int kDecodeCost = 1, kBlockCost = 1;        // Line::cost
+constexpr int kDecodeCost = 1, kBlockCost = V_BC;        // Line::cost
 constexpr int kMaxShares = 4 * kMaxSms;               // CTAs of one launch, at most
 int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool after_block, cudaStream_t s);
 int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool decode_follows, cudaStream_t s);

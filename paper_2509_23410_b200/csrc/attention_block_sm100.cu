@@ -1,4 +1,4 @@
-// Attention over the paged cache for items of more than 16 query rows: the batch's rows of one key head against the shared prefix,
+// Attention over the paged cache for items of more than 32 query rows: the batch's rows of one key head against the shared prefix,
 // or the drafted tokens of one sequence against its own keys (public header: patch_prefix_attention; the work list and the partial
 // results are described in attention.cuh).
 //
@@ -175,7 +175,7 @@ __device__ __forceinline__ int stream_tiles(int n, bool dual, int x) { return du
 template <int D>
 __device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w, float keys, int sms) {
     const float rows = float(p.B) * p.T * p.G, heads = float(p.Hkv);
-    const float mine = heads * w.tiles_p * V_TC * ceilf(rows / 128.0f);
+    const float mine = heads * w.tiles_p * (4000.0f * floorf(rows / 256.0f) + (fmodf(rows, 256.0f) > 128.0f ? 4000.0f : fmodf(rows, 256.0f) > 0.0f ? 3300.0f : 0.0f));
     const float theirs = heads * keys / kDecodeKeys * 700.0f;
     const float bytes = heads * (keys + float(p.prefix_len)) * D * 4.0f;
     const float time = fmaxf(bytes / 3420.0f, (mine + theirs) / sms);
@@ -228,7 +228,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
     if (share_gpu) ctas = min(ctas, sms_beside_decode<D>(p, w, *own_keys, gridDim.x));
     const bool busy = int(blockIdx.x) < ctas;
-    const int64_t u0 = busy ? total * blockIdx.x / ctas : 0, u1 = busy ? total * (blockIdx.x + 1) / ctas : 0;
+    const int64_t u0 = busy ? share_start(total, blockIdx.x, ctas, false) : 0, u1 = busy ? share_start(total, blockIdx.x + 1, ctas, false) : 0;
     Share s(p, w, cum, lens);
 
     if (warp == 0) {

@@ -1,4 +1,4 @@
-// Attention over the paged cache for items of at most 16 query rows (public header: patch_prefix_attention; the work list and the
+// Attention over the paged cache for items of few query rows, taken in blocks of at most 16 (public header: patch_prefix_attention; the work list and the
 // partial results are described in attention.cuh).
 //
 // Mathematics.  For every row the running maximum m of the scaled scores (in powers of two), the sum l of 2^(s - m) and the
@@ -20,7 +20,7 @@
 namespace patch {
 namespace attn {
 
-constexpr int kRows = kFewRows;               // query rows of an item
+constexpr int kRows = kDecodeRows;            // query rows of an item
 constexpr int kKeys = kDecodeKeys;
 constexpr int kStages = 2;
 constexpr int kWarps = 4;                     // consuming warps
@@ -43,7 +43,7 @@ template <int D> struct Cfg {
     static uint32_t smem_bytes(int B) { return kFixedBytes + uint32_t(2 * B + 1) * 4; }
 };
 // What a stage holds.
-struct Note { int slot, key0, keys, rows, flags, pad[3]; };
+struct Note { int slot, key0, keys, rows, block, flags, pad[2]; };
 constexpr int kFirst = 1, kLast = 2, kOwn = 4, kEnd = 8;   // first / last tile of the CTA's share of an item; the sequence's own keys; no tile: the end
 static_assert(sizeof(Note) == 32, "note");
 
@@ -104,7 +104,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         // this lane's page number of an item: entry page0 + lane of its list
         auto fetch = [&](const Share& s, int page0) { return page0 + lane < s.pages() ? s.list()[page0 + lane] : 0; };
         Share s(p, w, cum, lens), ahead(s);
-        bool have = s.start(total * blockIdx.x / ctas, total * (blockIdx.x + 1) / ctas);
+        bool have = s.start(share_start(total, blockIdx.x, ctas, AFTER), share_start(total, blockIdx.x + 1, ctas, AFTER));
         int page0 = have ? int((int64_t(s.t0) * kKeys) >> p.shift) : 0;
         int mine = have ? fetch(s, page0) : 0;
         while (have && ok) {
@@ -134,10 +134,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 if (!ok) break;
                 const uint32_t full = bar_full + 8 * stage;
                 const bool opens = i == s.t0;
-                const int rows = s.rows();
+                const int rows = s.rows() - s.block * kRows < kRows ? s.rows() - s.block * kRows : kRows;
                 if (lane == 0) {
-                    notes[stage] = Note{s.item + int(blockIdx.x), int(key0), s.keys, rows,
-                                        (opens ? kFirst : 0) | (i + 1 == s.t1 ? kLast : 0) | (s.b < 0 ? 0 : kOwn), {0, 0, 0}};
+                    notes[stage] = Note{s.item + int(blockIdx.x), int(key0), s.keys, rows, s.block,
+                                        (opens ? kFirst : 0) | (i + 1 == s.t1 ? kLast : 0) | (s.b < 0 ? 0 : kOwn), {0, 0}};
                     mbar_expect_tx(full, uint32_t(copies) * 2u * copy_bytes + (opens ? uint32_t(rows) * D * 2u : 0u));
                 }
                 __syncwarp();
@@ -146,9 +146,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     tma_load_page(dst, lane & 1 ? &map_v : &map_k, p.shift < 6 ? 0 : int(key0 & ((1 << p.shift) - 1)), 0, s.kvh, page, full, policy);
                 }
                 if (opens && lane >= 16 && lane - 16 < rows) {
-                    const int r = lane - 16;
+                    const int r = s.block * kRows + lane - 16;
                     const int64_t tok = (s.b < 0 ? 0 : int64_t(s.b) * p.T) + r / p.G;
-                    tma_bulk_load(base + C::kQOffset + stage * C::kQBytes + r * C::kQPitch,
+                    tma_bulk_load(base + C::kQOffset + stage * C::kQBytes + (lane - 16) * C::kQPitch,
                                   p.Q + tok * p.ldq + int64_t(s.kvh * p.G + r % p.G) * D, D * 2, full, policy);
                 }
                 ++issued;
@@ -201,8 +201,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             // rows past the item's are whatever lies there: their results are never stored
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) ldmatrix4(q_at + stage * C::kQBytes + i * 32, qa[i][0], qa[i][1], qa[i][2], qa[i][3]);
-            see0 = n.flags & kOwn ? n.keys - (p.T - 1 - g / p.G) : n.keys;
-            see1 = n.flags & kOwn ? n.keys - (p.T - 1 - (g + 8) / p.G) : n.keys;
+            const int r0 = n.block * kRows + g;
+            see0 = n.flags & kOwn ? n.keys - (p.T - 1 - r0 / p.G) : n.keys;
+            see1 = n.flags & kOwn ? n.keys - (p.T - 1 - (r0 + 8) / p.G) : n.keys;
             m0 = m1 = -INFINITY;
             l0 = l1 = 0.0f;
 #pragma unroll
@@ -332,8 +333,7 @@ static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, co
     if ((rc = allow_dynamic_smem(kern, Cfg<D>::smem_bytes(kMaxBatch), configured))) return rc;
     const int sms = sm_count() < kMaxSms ? sm_count() : kMaxSms;
     if (sms <= 0) return PATCH_ERR_CUDA;
-    // alone, one wave; beside the block kernel, which leaves an unknown part of the SMs free, shares half the size, so that
-    // the last ones do not run by themselves for long
+    // alone, one wave; beside the block kernel, more and ever smaller shares that run on whatever SMs it leaves free
     const int ctas = (AFTER ? 4 : 2) * sms;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
