@@ -28,19 +28,21 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
     if (!on) return;
 
     // slot of the item's first part, and the row's place in a slot
-    int count[2] = {0, 0};
+    int count[2] = {0, 0}, place[2] = {0, 0};
     int64_t at[2] = {0, 0};
     if (blocks_p) {
         const int r = tok * p.G + gq, blk = r / from.p.rows, item = kvh * blocks_p + blk;
         const int2 span = from.p.span[item];
         count[0] = span.y - span.x + 1;
-        at[0] = (int64_t(item) + span.x) * from.p.rows + (r - blk * from.p.rows);
+        at[0] = int64_t(item) + span.x;
+        place[0] = r - blk * from.p.rows;
     }
     if (own) {
         const int r = (tok - b * p.T) * p.G + gq, blk = r / from.s.rows, item = (b * p.Hkv + kvh) * blocks_s + blk;
         const int2 span = from.s.span[item];
         count[1] = span.y - span.x + 1;
-        at[1] = (int64_t(item) + span.x) * from.s.rows + (r - blk * from.s.rows);
+        at[1] = int64_t(item) + span.x;
+        place[1] = r - blk * from.s.rows;
     }
     float m = -INFINITY, l = 0.0f, acc[V];
 #pragma unroll
@@ -52,9 +54,9 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
         const int k = k0 + lane;
         const bool of_p = k < count[0];
         const Parts& part = of_p ? from.p : from.s;
-        const int64_t mine_at = of_p ? at[0] + int64_t(k) * part.rows : at[1] + int64_t(k - count[0]) * part.rows;
-        const float2 mine = lane < here ? part.ml[mine_at] : make_float2(-INFINITY, 0.0f);
-        const float* src = part.o + mine_at * D;
+        const int64_t slot = of_p ? at[0] + k : at[1] + (k - count[0]);
+        const int r = of_p ? place[0] : place[1];
+        const float2 mine = lane < here ? part.ml[slot * part.rows + r] : make_float2(-INFINITY, 0.0f);
         float mx = fmaxf(m, mine.x);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
@@ -70,7 +72,10 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
 #pragma unroll 8
         for (int q = 0; q < here; ++q) {
             const float fq = __shfl_sync(0xFFFFFFFFu, f, q);
-            const float* from_o = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(src), q)) + lane * V;
+            const bool q_of_p = k0 + q < count[0];
+            const Parts& q_part = q_of_p ? from.p : from.s;
+            const float* from_o = q_part.o + q_part.chunk<D>(q_of_p ? at[0] + k0 + q : at[1] + (k0 + q - count[0]), q_of_p ? place[0] : place[1],
+                                                             lane * V / 4) + (lane * V) % 4;
             float v[V];
             if constexpr (V == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(from_o);
             else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(from_o);
@@ -154,8 +159,6 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     if (rc) return rc;
     if (prefix_len < 0 || prefix_len > 0x7FFFFF00 || ld_table < 0 || !(scale > 0.0f) || scale > 3.0e38f) return PATCH_ERR_SHAPE;
     if (B == 0) return PATCH_OK;
-    // units of a sequence, summed over the batch, are counted in 32 bits (tiles of 64 keys or more, and each item's own cost)
-    if (ld_table > 0x7FFFFFFF || B * ((ld_table * cache->page_size + kDecodeKeys - 1) / kDecodeKeys + 8) > 0x7FFFFFFF) return PATCH_ERR_SHAPE;
     if (!Q || !O || !suffix_lens || (prefix_len && !prefix_pages) || (ld_table && !page_table)) return PATCH_ERR_NULL;
     const int D = cache->D;
     if (ldq < int64_t(Hq) * D || ldo < int64_t(Hq) * D || ldq % 8 || ldo % 8) return PATCH_ERR_SHAPE;
@@ -171,12 +174,16 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     while ((1 << p.shift) < cache->page_size) ++p.shift;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const Results to = {{reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float2*>(ws + q.ml_p), reinterpret_cast<int2*>(ws), q.rows_p},
-                        {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s}};
+    const Results to = {{reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float2*>(ws + q.ml_p), reinterpret_cast<int2*>(ws), q.rows_p, q.block_p},
+                        {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s, q.block_s}};
     const bool prefix = prefix_len > 0;
     auto tiles = [&](int keys) { return int((prefix_len + keys - 1) / keys); };
     const Line dec = {prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : q.blocks_s, tiles(kDecodeKeys), kDecodeCost};
     const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, tiles(kBlockKeys), kBlockCost};
+    // units are counted in 32 bits
+    const int64_t own = (ld_table * cache->page_size + kDecodeKeys - 1) / kDecodeKeys + 8;
+    if (ld_table > 0x7FFFFFFF || int64_t(cache->Hkv) * q.blocks_p * (int64_t(dec.tiles_p) + 8) + B * own * cache->Hkv * q.blocks_s > 0x7FFFFFFF)
+        return PATCH_ERR_SHAPE;
     const bool use_block = blk.blocks_p || blk.blocks_s, use_decode = dec.blocks_p || dec.blocks_s;
     if (use_block && (rc = launch_attn_block(cache, p, blk, to, use_decode, s))) return rc;
     if (use_decode && (rc = launch_attn_decode(cache, p, dec, to, use_block, s))) return rc;

@@ -39,10 +39,17 @@ struct Line {
 };
 // Where partial results go, of prefix items and of suffix items.
 struct Parts {
-    float* o;                                 // [slot][rows][D]
+    float* o;                                 // [slot][rows][D], see `quarters`
     float2* ml;                               // [slot][rows]: maximum (in powers of two), sum
     int2* span;                               // [item]: first and last CTA with a share of it
     int rows;                                 // rows of a slot
+    int quarters;                             // 0: rows of D; 1: by quarters of the columns, [slot][4][rows][D / 4], 16-byte chunk c of
+                                              // row r at chunk c ^ (r & (D / 16 - 1)) (how the block kernel's shared memory holds them)
+    template <int D> __device__ __forceinline__ int64_t chunk(int64_t slot, int r, int c) const {       // in elements, chunk c of row r
+        if (!quarters) return (slot * rows + r) * D + 4 * c;
+        const int q = c / (D / 16), cc = (c & (D / 16 - 1)) ^ (r & (D / 16 - 1));
+        return ((slot * 4 + q) * rows + r) * (D / 4) + 4 * cc;
+    }
 };
 struct Results { Parts p, s; };
 
@@ -90,15 +97,20 @@ __device__ __forceinline__ int64_t lay_out(const Problem& p, const Line& w, int 
     return keys;
 }
 
-__host__ __device__ __forceinline__ int64_t prefix_units(const Line& w, int Hkv) { return int64_t(Hkv) * w.blocks_p * (w.tiles_p + w.cost); }
-__device__ __forceinline__ int64_t total_units(const Line& w, const Problem& p, const int* cum) {
-    return prefix_units(w, p.Hkv) + (w.blocks_s ? int64_t(cum[p.B]) * p.Hkv * w.blocks_s : 0);
+// Units are counted in 32 bits (the host refuses what would not fit): a 64-bit division costs every CTA hundreds of cycles.
+__device__ __forceinline__ int prefix_units(const Line& w, int Hkv) { return Hkv * w.blocks_p * (w.tiles_p + w.cost); }
+__device__ __forceinline__ int total_units(const Line& w, const Problem& p, const int* cum) {
+    return prefix_units(w, p.Hkv) + (w.blocks_s ? cum[p.B] * p.Hkv * w.blocks_s : 0);
 }
-// First unit of CTA c's share of U units among n <= U CTAs: equal shares where all CTAs run at once (c U / n); where they take turns on
-// whatever SMs another kernel leaves free, shares that shrink from 7/4 to 1/4 of the average, so that the last ones to run are
-// short.  No share is empty: a CTA between an item's first and last one has a tile of it.
-__device__ __forceinline__ int64_t share_start(int64_t U, int c, int n, bool in_turns) {
-    return in_turns && U >= 4 * int64_t(n) ? U * c * (7 * n - 3 * c) / (4 * int64_t(n) * n) : U * c / n;
+// First unit of CTA c's share of U units among n <= U CTAs: equal shares where all CTAs run at once; where they take turns on whatever
+// SMs another kernel leaves free (`turns` = 1 / (4 n^2) then, else 0), shares that shrink from 7/4 to 1/4 of the average, so that
+// the last ones to run are short.  No share is empty: a CTA between an item's first and last one has a tile of it.
+__device__ __forceinline__ int share_start(int U, int c, int n, double turns) {
+    if (turns == 0.0 || U < 8 * n) {
+        const int each = U / n, more = U - each * n;
+        return c * each + min(c, more);
+    }
+    return c == n ? U : int(double(U) * (double(c) * double(7 * n - 3 * c)) * turns);
 }
 
 // One CTA's share of the line, item by item.
@@ -110,7 +122,7 @@ struct Share {
     int b, kvh, block, item;                  // b < 0: the prefix; item: number among the prefix's or the suffixes' items
     int tiles, keys;
     int t0, t1;                               // the share's tiles of the item
-    int64_t u, u1;                            // the item's first unit, the share's end
+    int u, u1;                                // the item's first unit, the share's end
 
     __device__ __forceinline__ Share(const Problem& p_, const Line& w_, const int* cum_, const int* len_)
         : p(p_), w(w_), cum(cum_), len(len_), b(-1), kvh(0), block(0), item(0), tiles(0), keys(0), t0(0), t1(0), u(0), u1(0) {}
@@ -122,36 +134,36 @@ struct Share {
         tiles = cum[b + 1] - cum[b] - w.cost;
         keys = len[b];
     }
-    __device__ __forceinline__ void clip() { const int64_t end = u1 - u - w.cost; t1 = end < tiles ? int(end) : tiles; }
+    __device__ __forceinline__ void clip() { t1 = min(tiles, u1 - u - w.cost); }
     // to the first item of units [u0, end) that has a tile among them; false: none
-    __device__ __forceinline__ bool start(int64_t u0, int64_t end) {
+    __device__ __forceinline__ bool start(int u0, int end) {
         if (u0 >= end) return false;
-        const int64_t before = prefix_units(w, p.Hkv);
+        const int before = prefix_units(w, p.Hkv);
         int place;                            // of u0 among its item's units
         if (u0 < before) {
             const int each = w.tiles_p + w.cost;
-            item = int(u0 / each);
+            item = u0 / each;
             b = -1;
             kvh = item / w.blocks_p;
             block = item - kvh * w.blocks_p;
             tiles = w.tiles_p;
             keys = p.prefix_len;
-            place = int(u0 - int64_t(item) * each);
+            place = u0 - item * each;
         } else {
             const int per = p.Hkv * w.blocks_s;
-            const int64_t v = u0 - before, q = v / per;
+            const int v = u0 - before, q = v / per;
             int lo = 0, hi = p.B;             // the sequence with cum[lo] <= q < cum[lo + 1]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (cum[mid] <= q) lo = mid; else hi = mid;
             }
             at_sequence(lo);
-            const int64_t r = v - int64_t(cum[lo]) * per;
-            const int each = tiles + w.cost, sub = int(r / each);
+            const int r = v - cum[lo] * per;
+            const int each = tiles + w.cost, sub = r / each;
             kvh = sub / w.blocks_s;
             block = sub - kvh * w.blocks_s;
             item = lo * per + sub;
-            place = int(r - int64_t(sub) * each);
+            place = r - sub * each;
         }
         u = u0 - place;
         u1 = end;
@@ -187,6 +199,17 @@ struct Share {
     __device__ __forceinline__ const int32_t* list() const { return b < 0 ? p.prefix_pages : p.table + b * p.ld_table; }
     __device__ __forceinline__ int pages() const { return int((int64_t(keys) + (1 << p.shift) - 1) >> p.shift); }
 };
+
+// The page lists on their way into L2 while the lengths are looked up (they are needed next; both come from HBM in a step of a
+// model whose weights have passed through L2 since).  Executed by `n` threads of every CTA.
+__device__ __forceinline__ void prefetch_lists(const Problem& p, const Line& w, int n, int t) {
+    const int64_t lines_p = w.blocks_p ? ((int64_t(p.prefix_len) >> p.shift) * 4 + 127) / 128 : 0;
+    const int64_t lines = lines_p + (w.blocks_s ? (p.B * p.ld_table * 4 + 127) / 128 : 0);
+    for (int64_t i = int64_t(blockIdx.x) * n + t; i < lines; i += int64_t(gridDim.x) * n) {
+        const char* at = i < lines_p ? reinterpret_cast<const char*>(p.prefix_pages) + i * 128 : reinterpret_cast<const char*>(p.table) + (i - lines_p) * 128;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+    }
+}
 
 __device__ __forceinline__ float ex2(float x) {
     float y;

@@ -95,11 +95,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32
 #undef PATCH_S32
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void st_global32(float* p, const float (&v)[8]) {
-    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]),
-                 "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
-}
-
 // true in one lane of the (converged) warp, always the same one
 __device__ __forceinline__ bool elect_one() {
     uint32_t pred;
@@ -224,11 +219,11 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     tc_fence_after();
     const uint32_t tmem = *misc;
 
-    const int64_t total = total_units(w, p, cum);
-    int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
+    const int total = total_units(w, p, cum);
+    int ctas = min(total, int(gridDim.x));
     if (share_gpu) ctas = min(ctas, sms_beside_decode<D>(p, w, *own_keys, gridDim.x));
     const bool busy = int(blockIdx.x) < ctas;
-    const int64_t u0 = busy ? share_start(total, blockIdx.x, ctas, false) : 0, u1 = busy ? share_start(total, blockIdx.x + 1, ctas, false) : 0;
+    const int u0 = busy ? share_start(total, blockIdx.x, ctas, 0.0) : 0, u1 = busy ? share_start(total, blockIdx.x + 1, ctas, 0.0) : 0;
     Share s(p, w, cum, lens);
 
     if (warp == 0) {
@@ -385,18 +380,25 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const int n = s.t1 - s.t0, mine = stream_tiles(n, dual, x);
             const int r = s.block * kBlockRows + (dual ? 128 * x : 0) + row;     // row of the item
             const bool valid = r < s.rows();
-            // the query rows, 16 bytes at a time, into the swizzled layout; rows past the item's are zeros
+            // this warp's 32 query rows into the swizzled layout, a row (256 bytes at D = 128) by D / 8 neighbouring lanes -- a lane per
+            // row would touch 32 lines with every load (6 100 cycles for 256 rows); rows past the item's are zeros
             if (dual || x == 0) {
-                const int64_t tok = (s.b < 0 ? 0 : int64_t(s.b) * p.T) + r / p.G;
-                const __nv_bfloat16* src = p.Q + tok * p.ldq + int64_t(s.kvh * p.G + r % p.G) * D;
-                uint8_t* dst = smem + room.q + x * C::kQTile;
+                constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+                const int c = lane & (kLanes - 1);
+                uint8_t* dst = smem + room.q + x * C::kQTile + (c >> 3) * C::kQAtom;
+                const int first = s.block * kBlockRows + (dual ? 128 * x : 0);
+                const __nv_bfloat16* from = p.Q + (s.b < 0 ? 0 : int64_t(s.b) * p.T) * p.ldq + int64_t(s.kvh) * p.G * D + 8 * c;
 #pragma unroll 1
-                for (int h = 0; h < D / 64; ++h) {
+                for (int h = 0; h < 32; h += 8 * kAtOnce) {
                     uint4 v[8];
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) v[c] = valid ? *reinterpret_cast<const uint4*>(src + 64 * h + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int i = 0; i < 8; ++i) {
+                        const int at = quad * 32 + h + i * kAtOnce + lane / kLanes, rr = first + at, tok = rr / p.G;
+                        v[i] = rr < s.rows() ? *reinterpret_cast<const uint4*>(from + tok * p.ldq + int64_t(rr - tok * p.G) * D) : make_uint4(0u, 0u, 0u, 0u);
+                    }
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(dst + h * C::kQAtom + atom_chunk_offset(row, c)) = v[c];
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<uint4*>(dst + atom_chunk_offset(quad * 32 + h + i * kAtOnce + lane / kLanes, c & 7)) = v[i];
                 }
                 fence_async_shared();
             }
@@ -460,56 +462,68 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             tc_fence_after();
             ml[128 * x + row] = make_float2(m, l);
             if (barrier_any(failed, 1, 256)) { failed = true; break; }
-            // ---- the partial result ----
+            // ---- the partial result: a quarter of the columns at a time through shared memory (where the queries were), from
+            // there in one copy; a lane's own row straight to memory would touch 32 lines with every store (6 800 cycles) ----
             const Parts& part = s.b < 0 ? to.p : to.s;
-            const int64_t at = (s.item + int64_t(blockIdx.x)) * part.rows + (dual ? 128 * x : 0) + row;
-            float* dst = part.o + at * D;
-            if (dual) {
-#pragma unroll 1
-                for (int q = 0; q < D / 32; ++q) {
-                    uint32_t o[32];
-                    tmem_ld32(t_o + 32u * q, o);
-                    tmem_ld_wait();
-                    if (valid) {
-#pragma unroll
-                        for (int c = 0; c < 32; c += 8) {
-                            float f[8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[c + i]);
-                            st_global32(dst + 32 * q + c, f);
-                        }
-                    }
-                }
-                if (valid) part.ml[at] = make_float2(m, l);
-            } else {
-                // both streams hold a part of the same rows: each takes half of the columns of both
+            const int64_t slot = s.item + int64_t(blockIdx.x);
+            const int base_row = dual ? 128 * x : 0, here = min(128, s.rows() - s.block * kBlockRows - base_row);
+            float fa = 1.0f, fb = 0.0f;
+            if (!dual) {                                       // both streams hold a part of the same rows: each takes half of the columns
                 const float2 a = ml[row], b = ml[128 + row];
                 const float mx = fmaxf(a.x, b.x);
-                const float fa = a.x == -INFINITY ? 0.0f : ex2(a.x - mx), fb = b.x == -INFINITY ? 0.0f : ex2(b.x - mx);
-#pragma unroll 1
-                for (int q = 0; q < D / 64; ++q) {
-                    const uint32_t col = uint32_t(x) * (D / 2) + 32u * q;
-                    uint32_t o0[32], o1[32];
-                    tmem_ld32(tmem + lanes + 256u + col, o0);
-                    if (n > 1) tmem_ld32(tmem + lanes + 384u + col, o1);
-                    tmem_ld_wait();
-                    if (valid) {
-#pragma unroll
-                        for (int c = 0; c < 32; c += 8) {
-                            float f[8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                f[i] = __uint_as_float(o0[c + i]) * fa + (n > 1 ? __uint_as_float(o1[c + i]) * fb : 0.0f);
-                            st_global32(dst + col + c, f);
-                        }
-                    }
-                }
-                if (valid && x == 0) part.ml[at] = make_float2(mx, a.y * fa + b.y * fb);
+                fa = a.x == -INFINITY ? 0.0f : ex2(a.x - mx);
+                fb = b.x == -INFINITY ? 0.0f : ex2(b.x - mx);
+                m = mx;
+                l = a.y * fa + b.y * fb;
             }
+            if (valid && (dual || x == 0)) part.ml[slot * part.rows + base_row + row] = make_float2(m, l);
+            barrier_any(false, 1, 256);                        // (m, l) have been read
+            constexpr uint32_t kQuarter = 128 * D;             // bytes of 128 rows
+            constexpr int kChunks = D / 16;                    // of a row
+            uint8_t* stage = smem + room.q + x * (dual ? C::kQTile : kQuarter);
+#pragma unroll 1
+            for (int q = dual ? 0 : 2 * x; q < (dual ? 4 : 2 * x + 2); ++q) {
+                uint32_t o[D / 4];
+                if (dual || n == 1) {
+                    if constexpr (D == 128) tmem_ld32(tmem + lanes + 256u + (dual ? 128u * x : 0u) + (D / 4) * q, o);
+                    else tmem_ld16(tmem + lanes + 256u + (dual ? 128u * x : 0u) + (D / 4) * q, o);
+                    tmem_ld_wait();
+                } else {
+                    uint32_t o1[D / 4];
+                    if constexpr (D == 128) {
+                        tmem_ld32(tmem + lanes + 256u + (D / 4) * q, o);
+                        tmem_ld32(tmem + lanes + 384u + (D / 4) * q, o1);
+                    } else {
+                        tmem_ld16(tmem + lanes + 256u + (D / 4) * q, o);
+                        tmem_ld16(tmem + lanes + 384u + (D / 4) * q, o1);
+                    }
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < D / 4; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * fa + __uint_as_float(o1[c]) * fb);
+                }
+                if (q & 1 && !dual || q == 2) {                // the buffer's last copy has been read
+                    if (row == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    barrier_any(false, 2 + x, 128);
+                }
+                uint8_t* to_row = stage + (dual ? (q & 1) * kQuarter : 0u) + row * D;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+                    *reinterpret_cast<uint4*>(to_row + ((c ^ (row & (kChunks - 1))) << 4)) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                fence_async_shared();
+                barrier_any(false, 2 + x, 128);
+                if (row == 0 && here > 0) {
+                    const uint32_t src = smem_u32(stage) + (dual ? (q & 1) * kQuarter : 0u);
+                    float* dst = part.o + ((slot * 4 + q) * part.rows + base_row) * (D / 4);
+                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(uint32_t(here) * D) : "memory");
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                }
+            }
+            if (row == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             tc_fence_before();
             if (barrier_any(false, 1, 256)) { failed = true; break; }             // nobody's accumulators are read any more
         }
     }
+    if (warp >= 4 && (threadIdx.x & 127) == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // results have been written
     tc_fence_before();
     __syncthreads();
     tc_fence_after();

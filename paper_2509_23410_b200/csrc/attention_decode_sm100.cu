@@ -62,7 +62,7 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
 template <int D, bool AFTER>
 __global__ void __launch_bounds__(kThreads, 2)
 attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const Line w,
-                   const Results to) {
+                   const Results to, const double turns) {
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -83,9 +83,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         tma_prefetch_map(&map_v);
     }
     if (warp == 0) lay_out(p, w, kKeys, cum, lens);
+    else if (warp < kWarps) prefetch_lists(p, w, 32 * (kWarps - 1), threadIdx.x - 32);
     __syncthreads();
-    const int64_t total = total_units(w, p, cum);
-    const int ctas = total < gridDim.x ? int(total) : int(gridDim.x);
+    const int total = total_units(w, p, cum), ctas = min(total, int(gridDim.x));
     const bool busy = int(blockIdx.x) < ctas;
     // a copy brings the rows of one page that fall into a tile
     const int rows_log2 = p.shift < 6 ? p.shift : 6;
@@ -104,7 +104,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         // this lane's page number of an item: entry page0 + lane of its list
         auto fetch = [&](const Share& s, int page0) { return page0 + lane < s.pages() ? s.list()[page0 + lane] : 0; };
         Share s(p, w, cum, lens), ahead(s);
-        bool have = s.start(share_start(total, blockIdx.x, ctas, AFTER), share_start(total, blockIdx.x + 1, ctas, AFTER));
+        bool have = s.start(share_start(total, blockIdx.x, ctas, turns), share_start(total, blockIdx.x + 1, ctas, turns));
         int page0 = have ? int((int64_t(s.t0) * kKeys) >> p.shift) : 0;
         int mine = have ? fetch(s, page0) : 0;
         while (have && ok) {
@@ -128,28 +128,28 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_FORMAT);
                     page = 0;
                 }
-                bool free_slot = true;
-                if (lane == 0 && issued >= kStages) free_slot = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status);
-                ok = __shfl_sync(0xFFFFFFFFu, free_slot ? 1 : 0, 0) != 0;
+                // everything is at hand before the slot is: between its release and the copies there are a wait and two instructions
+                const uint32_t full = bar_full + 8 * stage, dst = base + stage * C::kStageBytes + (lane & 1) * C::kOperandBytes + (lane >> 1) * copy_bytes;
+                const CUtensorMap* map = lane & 1 ? &map_v : &map_k;
+                const int row_in_page = p.shift < 6 ? 0 : int(key0 & ((1 << p.shift) - 1));
+                const bool opens = i == s.t0, on = lane < 2 * copies;
+                const int rows = opens ? min(kRows, s.rows() - s.block * kRows) : 0;
+                const uint32_t bytes = uint32_t(copies) * 2u * copy_bytes + uint32_t(rows) * D * 2u;
+                ok = __all_sync(0xFFFFFFFFu, issued < kStages || mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status));
                 if (!ok) break;
-                const uint32_t full = bar_full + 8 * stage;
-                const bool opens = i == s.t0;
-                const int rows = s.rows() - s.block * kRows < kRows ? s.rows() - s.block * kRows : kRows;
-                if (lane == 0) {
-                    notes[stage] = Note{s.item + int(blockIdx.x), int(key0), s.keys, rows, s.block,
-                                        (opens ? kFirst : 0) | (i + 1 == s.t1 ? kLast : 0) | (s.b < 0 ? 0 : kOwn), {0, 0}};
-                    mbar_expect_tx(full, uint32_t(copies) * 2u * copy_bytes + (opens ? uint32_t(rows) * D * 2u : 0u));
-                }
+                if (lane == 0) mbar_expect_tx_only(full, bytes);
                 __syncwarp();
-                if (lane < 2 * copies) {
-                    const uint32_t dst = base + stage * C::kStageBytes + (lane & 1) * C::kOperandBytes + (lane >> 1) * copy_bytes;
-                    tma_load_page(dst, lane & 1 ? &map_v : &map_k, p.shift < 6 ? 0 : int(key0 & ((1 << p.shift) - 1)), 0, s.kvh, page, full, policy);
-                }
+                if (on) tma_load_page(dst, map, row_in_page, 0, s.kvh, page, full, policy);
                 if (opens && lane >= 16 && lane - 16 < rows) {
                     const int r = s.block * kRows + lane - 16;
                     const int64_t tok = (s.b < 0 ? 0 : int64_t(s.b) * p.T) + r / p.G;
                     tma_bulk_load(base + C::kQOffset + stage * C::kQBytes + (lane - 16) * C::kQPitch,
                                   p.Q + tok * p.ldq + int64_t(s.kvh * p.G + r % p.G) * D, D * 2, full, policy);
+                }
+                if (lane == 0) {                     // the phase ends with this arrival and the bytes: the note is there by then
+                    notes[stage] = Note{s.item + int(blockIdx.x), int(key0), s.keys, min(kRows, s.rows() - s.block * kRows), s.block,
+                                        (opens ? kFirst : 0) | (i + 1 == s.t1 ? kLast : 0) | (s.b < 0 ? 0 : kOwn), {0, 0}};
+                    mbar_arrive(full);
                 }
                 ++issued;
                 if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -345,7 +345,7 @@ static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, co
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = AFTER ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, mk, mv, p, w, to) == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kern, mk, mv, p, w, to, AFTER ? 0.25 / ctas / ctas : 0.0) == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
 }
 
 int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool after_block, cudaStream_t s) {
