@@ -44,13 +44,17 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
         at[1] = int64_t(item) + span.x;
         place[1] = r - blk * from.s.rows;
     }
+    // this lane's elements of the first part, and from part to part
+    const int c = lane * V / 4, in_chunk = lane * V % 4;
+    const float* src[2] = {from.p.o + from.p.chunk<D>(at[0], place[0], c) + in_chunk, from.s.o + from.s.chunk<D>(at[1], place[1], c) + in_chunk};
+    const int64_t step[2] = {int64_t(from.p.rows) * D, int64_t(from.s.rows) * D};
     float m = -INFINITY, l = 0.0f, acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.0f;
     const int all = count[0] + count[1];
     for (int k0 = 0; k0 < all; k0 += 32) {
         const int here = all - k0 < 32 ? all - k0 : 32;
-        // this lane's part: its row in the outputs, and (m, l)
+        // this lane's part: its (m, l)
         const int k = k0 + lane;
         const bool of_p = k < count[0];
         const Parts& part = of_p ? from.p : from.s;
@@ -72,10 +76,8 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
 #pragma unroll 8
         for (int q = 0; q < here; ++q) {
             const float fq = __shfl_sync(0xFFFFFFFFu, f, q);
-            const bool q_of_p = k0 + q < count[0];
-            const Parts& q_part = q_of_p ? from.p : from.s;
-            const float* from_o = q_part.o + q_part.chunk<D>(q_of_p ? at[0] + k0 + q : at[1] + (k0 + q - count[0]), q_of_p ? place[0] : place[1],
-                                                             lane * V / 4) + (lane * V) % 4;
+            const int k1 = k0 + q;
+            const float* from_o = k1 < count[0] ? src[0] + k1 * step[0] : src[1] + (k1 - count[0]) * step[1];
             float v[V];
             if constexpr (V == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(from_o);
             else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(from_o);
@@ -170,8 +172,10 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PATCH_ERR_ALIGN;
     if ((rc = check_device())) return rc;
     Problem p = {static_cast<const __nv_bfloat16*>(Q), ldq, int(B), T, cache->Hkv, G, prefix_pages, int(prefix_len), page_table,
-                 ld_table, suffix_lens, 0, int(cache->num_pages), scale * 1.4426950408889634f, status_dev};
+                 ld_table, suffix_lens, 0, int(cache->num_pages), scale * 1.4426950408889634f, status_dev, 0u};
     while ((1 << p.shift) < cache->page_size) ++p.shift;
+    // r * ceil(2^32 / G) is at most r G above r 2^32 / G: exact while that stays below 2^32
+    if (G > 1 && B * T * G * int64_t(G) < (int64_t(1) << 32)) p.g_mul = uint32_t(((uint64_t(1) << 32) + G - 1) / G);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const Results to = {{reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float2*>(ws + q.ml_p), reinterpret_cast<int2*>(ws), q.rows_p, q.block_p},

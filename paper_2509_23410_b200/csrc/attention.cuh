@@ -29,6 +29,9 @@ struct Problem {
     int shift, num_pages;                     // log2(page_size)
     float scale_log2;                         // scale * log2(e): scores are kept in powers of two
     int* status;
+    uint32_t g_mul;                           // ceil(2^32 / G) where the product below is exact for every row, else 0
+    // token of row r of a key head's rows; one multiplication instead of a division's thirty instructions
+    __device__ __forceinline__ int token(int r) const { return g_mul ? int(__umulhi(uint32_t(r), g_mul)) : G == 1 ? r : r / G; }
 };
 
 // The line of units of one kernel.  Blocks of query rows are items of their own.
@@ -106,7 +109,7 @@ __device__ __forceinline__ int total_units(const Line& w, const Problem& p, cons
 // SMs another kernel leaves free (`turns` = 1 / (4 n^2) then, else 0), shares that shrink from 7/4 to 1/4 of the average, so that
 // the last ones to run are short.  No share is empty: a CTA between an item's first and last one has a tile of it.
 __device__ __forceinline__ int share_start(int U, int c, int n, double turns) {
-    if (turns == 0.0 || U < 8 * n) {
+    if (turns == 0.0 || U < 8 * n) {              // (also where the launch has more CTAs than there is work for)
         const int each = U / n, more = U - each * n;
         return c * each + min(c, more);
     }

@@ -214,17 +214,28 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         if (lane == 0) *own_keys = keys;
     }
     if (warp == 2) tmem_alloc(smem_u32(misc), kTmemCols);
+    if (warp >= 4) prefetch_lists(p, w, 256, threadIdx.x - 128);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *misc;
 
-    const int total = total_units(w, p, cum);
-    int ctas = min(total, int(gridDim.x));
-    if (share_gpu) ctas = min(ctas, sms_beside_decode<D>(p, w, *own_keys, gridDim.x));
+    // Shares: where every prefix item can have two CTAs or more to itself, as many for each and equal parts of its tiles (an item
+    // that a CTA has to share with another one costs it queries and a result twice); else equal stretches of the line.
+    Line line = w;
+    const int sms = share_gpu ? sms_beside_decode<D>(p, w, *own_keys, gridDim.x) : int(gridDim.x), items = p.Hkv * w.blocks_p;
+    const bool aligned = !w.blocks_s && 2 * items <= sms;
+    if (aligned) line.cost = 0;
+    const int total = total_units(line, p, cum), each = aligned ? min(sms / items, w.tiles_p) : 0;
+    const int ctas = aligned ? each * items : min(total, sms);
+    auto start_of = [&](int c) {
+        if (!aligned) return share_start(total, c, ctas, 0.0);
+        const int item = c / each;
+        return item * w.tiles_p + share_start(w.tiles_p, c - item * each, each, 0.0);
+    };
     const bool busy = int(blockIdx.x) < ctas;
-    const int u0 = busy ? share_start(total, blockIdx.x, ctas, 0.0) : 0, u1 = busy ? share_start(total, blockIdx.x + 1, ctas, 0.0) : 0;
-    Share s(p, w, cum, lens);
+    const int u0 = busy ? start_of(blockIdx.x) : 0, u1 = busy ? start_of(blockIdx.x + 1) : 0;
+    Share s(p, line, cum, lens);
 
     if (warp == 0) {
         // ---------------- producer: the first keys, then V0 K(lead) V1 K(lead + 1) ... as they are consumed ----------------
@@ -257,16 +268,15 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_FORMAT);
                     page = 0;
                 }
-                bool free_slot = true;
-                if (lane == 0 && issued >= ring) free_slot = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status);
-                ok = __shfl_sync(0xFFFFFFFFu, free_slot ? 1 : 0, 0) != 0;
+                // everything is at hand before the slot is
+                const uint32_t full = bar_full + 8 * stage, dst = base + stage * C::kTile + (lane & 1) * C::kAtom + box * box_bytes;
+                const CUtensorMap* map = v ? &map_v : &map_k;
+                const int row_in_page = p.shift < 7 ? 0 : int(key0 & ((1 << p.shift) - 1));
+                ok = __all_sync(0xFFFFFFFFu, issued < ring || mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status));
                 if (!ok) return;
-                const uint32_t full = bar_full + 8 * stage;
                 if (lane == 0) mbar_expect_tx(full, uint32_t(boxes) * uint32_t(D / 64) * box_bytes);
                 __syncwarp();
-                if (on)
-                    tma_load_page(base + stage * C::kTile + (lane & 1) * C::kAtom + box * box_bytes, v ? &map_v : &map_k,
-                                  p.shift < 7 ? 0 : int(key0 & ((1 << p.shift) - 1)), lane & 1, s.kvh, page, full, policy);
+                if (on) tma_load_page(dst, map, row_in_page, lane & 1, s.kvh, page, full, policy);
                 ++issued;
                 if (++stage == ring) { stage = 0; phase ^= 1u; }
             };
@@ -393,7 +403,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     uint4 v[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int at = quad * 32 + h + i * kAtOnce + lane / kLanes, rr = first + at, tok = rr / p.G;
+                        const int at = quad * 32 + h + i * kAtOnce + lane / kLanes, rr = first + at, tok = p.token(rr);
                         v[i] = rr < s.rows() ? *reinterpret_cast<const uint4*>(from + tok * p.ldq + int64_t(rr - tok * p.G) * D) : make_uint4(0u, 0u, 0u, 0u);
                     }
 #pragma unroll
@@ -404,7 +414,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_q);
-            const int see = s.b < 0 ? s.keys : s.keys - (p.T - 1 - r / p.G);      // keys the row sees
+            const int see = s.b < 0 ? s.keys : s.keys - (p.T - 1 - p.token(r));      // keys the row sees
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < mine; ++j) {
                 failed = __any_sync(0xFFFFFFFFu, !mbar_wait(bar_s + 8 * x, phase_s, abort_flag, p.status));

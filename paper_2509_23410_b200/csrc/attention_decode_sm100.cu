@@ -85,7 +85,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (warp == 0) lay_out(p, w, kKeys, cum, lens);
     else if (warp < kWarps) prefetch_lists(p, w, 32 * (kWarps - 1), threadIdx.x - 32);
     __syncthreads();
-    const int total = total_units(w, p, cum), ctas = min(total, int(gridDim.x));
+    const int total = total_units(w, p, cum);
+    // a CTA costs about as much as half a dozen tiles: the second half of the launch's CTAs is for work that is worth them
+    int ctas = gridDim.x;
+    if (AFTER) ctas = max(ctas / 2, min(ctas, total / 6));
+    ctas = min(ctas, total);
     const bool busy = int(blockIdx.x) < ctas;
     // a copy brings the rows of one page that fall into a tile
     const int rows_log2 = p.shift < 6 ? p.shift : 6;
@@ -104,7 +108,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         // this lane's page number of an item: entry page0 + lane of its list
         auto fetch = [&](const Share& s, int page0) { return page0 + lane < s.pages() ? s.list()[page0 + lane] : 0; };
         Share s(p, w, cum, lens), ahead(s);
-        bool have = s.start(share_start(total, blockIdx.x, ctas, turns), share_start(total, blockIdx.x + 1, ctas, turns));
+        bool have = s.start(share_start(total, blockIdx.x, ctas, ctas == gridDim.x ? turns : 0.0),
+                            share_start(total, blockIdx.x + 1, ctas, ctas == gridDim.x ? turns : 0.0));
         int page0 = have ? int((int64_t(s.t0) * kKeys) >> p.shift) : 0;
         int mine = have ? fetch(s, page0) : 0;
         while (have && ok) {
@@ -142,9 +147,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 if (on) tma_load_page(dst, map, row_in_page, 0, s.kvh, page, full, policy);
                 if (opens && lane >= 16 && lane - 16 < rows) {
                     const int r = s.block * kRows + lane - 16;
-                    const int64_t tok = (s.b < 0 ? 0 : int64_t(s.b) * p.T) + r / p.G;
+                    const int t = p.token(r);
+                    const int64_t tok = (s.b < 0 ? 0 : int64_t(s.b) * p.T) + t;
                     tma_bulk_load(base + C::kQOffset + stage * C::kQBytes + (lane - 16) * C::kQPitch,
-                                  p.Q + tok * p.ldq + int64_t(s.kvh * p.G + r % p.G) * D, D * 2, full, policy);
+                                  p.Q + tok * p.ldq + int64_t(s.kvh * p.G + r - t * p.G) * D, D * 2, full, policy);
                 }
                 if (lane == 0) {                     // the phase ends with this arrival and the bytes: the note is there by then
                     notes[stage] = Note{s.item + int(blockIdx.x), int(key0), s.keys, min(kRows, s.rows() - s.block * kRows), s.block,
@@ -202,8 +208,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) ldmatrix4(q_at + stage * C::kQBytes + i * 32, qa[i][0], qa[i][1], qa[i][2], qa[i][3]);
             const int r0 = n.block * kRows + g;
-            see0 = n.flags & kOwn ? n.keys - (p.T - 1 - r0 / p.G) : n.keys;
-            see1 = n.flags & kOwn ? n.keys - (p.T - 1 - (r0 + 8) / p.G) : n.keys;
+            see0 = n.flags & kOwn ? n.keys - (p.T - 1 - p.token(r0)) : n.keys;
+            see1 = n.flags & kOwn ? n.keys - (p.T - 1 - p.token(r0 + 8)) : n.keys;
             m0 = m1 = -INFINITY;
             l0 = l1 = 0.0f;
 #pragma unroll
