@@ -8,9 +8,6 @@
 
 namespace patch {
 namespace attn {
-#ifndef V_MR
-#define V_MR 64
-#endif
 
 // Joins the partial results: one warp per query row and head.  Bound by the latency of three dependent reads (which CTAs, their
 // (m, l), their outputs); the (m, l) of up to 32 parts are read at once, one per lane, their outputs eight at a time.
@@ -96,17 +93,20 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
 // host side
 
 // Which kernel serves a phase.  The prefix: the decode kernel where its 16 rows of mma.sync hold all rows (HBM is what it waits
-// for), else the block kernel (32 rows of two blocks on the decode kernel would read the prefix twice).  The suffixes: their
-// items are short, and an item costs the block kernel about 7 us (queries, first tile, result), so up to four blocks of 16 rows
-// stay on the decode kernel -- the keys come from L2 from the second block on (five tokens of four heads, 16 sequences of up to
-// 777 keys: V_T5A us against V_T5B us).
-constexpr int kMostDecodeRows = V_MR;
+// for), else the block kernel (two blocks on the decode kernel would read the prefix twice; one CTA holding both took 112 us against
+// 77 for 32 rows and 8192 keys of the 13B shape).  A sequence's own keys, where its T G rows are more than 16: items are short, and
+// an item costs the block kernel about 7 us (queries, first tile, result), so where page tables end at 1024 keys up to four blocks of 16
+// rows stay on the decode kernel, with the keys from L2 from the second block on.  Measured, 16 sequences, 28 rows, 8 key heads:
+// 200 keys 13.6 us there against 17.3, 800 keys 21.6 against 28.0, 4096 keys 85.4 against 52.8.
+constexpr int kMostDecodeRows = 64, kMostDecodeKeys = 1024;
+static bool block_suffixes(int64_t rows, int64_t keys) { return rows > kMostDecodeRows || (rows > kDecodeRows && keys > kMostDecodeKeys); }
+
 struct Plan {
     bool block_p, block_s;                           // prefix / suffixes on the block kernel
     int blocks_p, blocks_s, rows_p, rows_s;          // row blocks per key head, rows of a slot
     size_t span_s, ml_p, ml_s, o_p, o_s, bytes;      // workspace: [spans of prefix items | of suffix items | (m, l) | outputs]
 };
-static Plan plan_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G) {
+static Plan plan_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G, int64_t table_keys) {
     Plan q;
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     auto rows = [&](int64_t all, bool block, int& blocks) {
@@ -115,7 +115,7 @@ static Plan plan_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G) 
         return int(all < most ? all : most);
     };
     q.block_p = B * T * G > kDecodeRows;
-    q.block_s = T * G > kMostDecodeRows;
+    q.block_s = block_suffixes(T * G, table_keys);
     q.rows_p = rows(B * T * G, q.block_p, q.blocks_p);
     q.rows_s = rows(T * G, q.block_s, q.blocks_s);
     // a slot for every item and every CTA that may share one
@@ -148,7 +148,10 @@ extern "C" int patch_prefix_attention_workspace_size(const patch_kv_cache_t* cac
     if (!bytes_out) return PATCH_ERR_NULL;
     int rc = attn::check_batch(cache, B, T, Hq);
     if (rc) return rc;
-    *bytes_out = attn::plan_of(cache, B, T, Hq / cache->Hkv).bytes;
+    // whatever the tables' width will be
+    const int64_t G = Hq / cache->Hkv;
+    const size_t few = attn::plan_of(cache, B, T, G, 0).bytes, many = attn::plan_of(cache, B, T, G, int64_t(1) << 40).bytes;
+    *bytes_out = few > many ? few : many;
     return PATCH_OK;
 }
 
@@ -159,16 +162,17 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     using namespace attn;
     int rc = check_batch(cache, B, T, Hq);
     if (rc) return rc;
-    if (prefix_len < 0 || prefix_len > 0x7FFFFF00 || ld_table < 0 || !(scale > 0.0f) || scale > 3.0e38f) return PATCH_ERR_SHAPE;
+    if (prefix_len < 0 || prefix_len > 0x7FFFFF00 || ld_table < 0 || ld_table > 0x7FFFFFFF || !(scale > 0.0f) || scale > 3.0e38f) return PATCH_ERR_SHAPE;
     if (B == 0) return PATCH_OK;
     if (!Q || !O || !suffix_lens || (prefix_len && !prefix_pages) || (ld_table && !page_table)) return PATCH_ERR_NULL;
     const int D = cache->D;
     if (ldq < int64_t(Hq) * D || ldo < int64_t(Hq) * D || ldq % 8 || ldo % 8) return PATCH_ERR_SHAPE;
     if (!aligned16(Q) || !aligned16(O)) return PATCH_ERR_ALIGN;
     const int G = Hq / cache->Hkv;
-    const Plan q = plan_of(cache, B, T, G);
+    size_t need = 0;
+    if ((rc = patch_prefix_attention_workspace_size(cache, B, T, Hq, &need))) return rc;
     if (!workspace) return PATCH_ERR_NULL;
-    if (workspace_bytes < q.bytes) return PATCH_ERR_SIZE;
+    if (workspace_bytes < need) return PATCH_ERR_SIZE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PATCH_ERR_ALIGN;
     if ((rc = check_device())) return rc;
     Problem p = {static_cast<const __nv_bfloat16*>(Q), ldq, int(B), T, cache->Hkv, G, prefix_pages, int(prefix_len), page_table,
@@ -178,6 +182,7 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     if (G > 1 && B * T * G * int64_t(G) < (int64_t(1) << 32)) p.g_mul = uint32_t(((uint64_t(1) << 32) + G - 1) / G);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const Plan q = plan_of(cache, B, T, G, ld_table * cache->page_size);
     const Results to = {{reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float2*>(ws + q.ml_p), reinterpret_cast<int2*>(ws), q.rows_p, q.block_p},
                         {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s, q.block_s}};
     const bool prefix = prefix_len > 0;
@@ -186,7 +191,7 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, tiles(kBlockKeys), kBlockCost};
     // units are counted in 32 bits
     const int64_t own = (ld_table * cache->page_size + kDecodeKeys - 1) / kDecodeKeys + 8;
-    if (ld_table > 0x7FFFFFFF || int64_t(cache->Hkv) * q.blocks_p * (int64_t(dec.tiles_p) + 8) + B * own * cache->Hkv * q.blocks_s > 0x7FFFFFFF)
+    if (int64_t(cache->Hkv) * q.blocks_p * (int64_t(dec.tiles_p) + 8) + B * own * cache->Hkv * q.blocks_s > 0x7FFFFFFF)
         return PATCH_ERR_SHAPE;
     const bool use_block = blk.blocks_p || blk.blocks_s, use_decode = dec.blocks_p || dec.blocks_s;
     if (use_block && (rc = launch_attn_block(cache, p, blk, to, use_decode, s))) return rc;

@@ -234,11 +234,8 @@ __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* m
 // The decode kernel (attention_decode_sm100.cu) takes rows in blocks of kDecodeRows, the block kernel (attention_block_sm100.cu) in
 // blocks of kBlockRows.
 constexpr int kDecodeRows = 16, kBlockRows = 256;
-#ifndef V_BC
-#define V_BC 3
-#endif
 constexpr int kDecodeKeys = 64, kBlockKeys = 128;     // keys of a tile
-constexpr int kDecodeCost = 1, kBlockCost = V_BC;        // Line::cost
+constexpr int kDecodeCost = 1, kBlockCost = 3;        // Line::cost
 constexpr int kMaxShares = 4 * kMaxSms;               // CTAs of one launch, at most
 int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool after_block, cudaStream_t s);
 int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool decode_follows, cudaStream_t s);

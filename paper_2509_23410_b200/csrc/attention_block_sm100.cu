@@ -27,9 +27,6 @@
 namespace patch {
 namespace attn {
 namespace blk {
-#ifndef V_TC
-#define V_TC 2000.0f
-#endif
 
 constexpr int kKeys = kBlockKeys;
 constexpr int kMaxRing = 8;
@@ -165,8 +162,9 @@ __device__ __forceinline__ int stream_tiles(int n, bool dual, int x) { return du
 // How many SMs the block kernel takes where the decode kernel has the suffixes.  Together they are done no sooner than HBM has
 // delivered the keys and values and the SMs have done their cycles; with as many SMs as its own cycles need in that time, the block
 // kernel ends with the decode kernel, which streams from the other SMs meanwhile -- one is short of arithmetic, the other of
-// bandwidth.  Cycles measured: 4 000 for a key tile and 256 rows, 2 000 for one and 128 rows, 700 for a tile of the decode kernel (two
-// CTAs share its latencies); bandwidth in bytes per cycle of 6.5 TB/s at 1.9 GHz.
+// bandwidth.  Cycles measured: 4 000 for a key tile and 256 rows, 3 300 for one and 128 rows (two tiles at a time, waiting for HBM),
+// 700 for a tile of the decode kernel (two CTAs share its latencies); bandwidth in bytes per cycle of 6.5 TB/s at 1.9 GHz.  64
+// sequences behind 32768 keys: 82 us against 101 with the block kernel on all SMs first.
 template <int D>
 __device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w, float keys, int sms) {
     const float rows = float(p.B) * p.T * p.G, heads = float(p.Hkv);
