@@ -118,6 +118,9 @@ def load(path: str) -> ctypes.CDLL:
         for name in EXPORTS:
             if name != "patch_strerror":
                 getattr(L, name).restype = ctypes.c_int
+        # addresses for the calls that do not go through ctypes (see csrc/marshal.cpp)
+        for name in ("patch_qk_norm_rope", "patch_qk_norm_rope_backward", "patch_kv_append", "patch_prefix_attention"):
+            setattr(L, "at_" + name, ctypes.cast(getattr(L, name), vp).value)
     return L
 
 
@@ -433,15 +436,19 @@ def patch_read_layout(packed, stream=None) -> Layout:
 # Between the linear layers: norms and rotation of queries and keys, the paged cache, attention behind a shared prefix.
 #
 # These calls take a few microseconds on the GPU for a decode step's handful of tokens, so what the host does for each of them
-# counts: tensors are taken apart with one unpacking of shape and strides each.
+# counts: the tensors are checked and taken apart by a CPython module (csrc/marshal.cpp), which calls the library by address.
 
-_torch = _bf16 = _f32 = _i32 = _i64 = _raw_stream = None
+_torch = _bf16 = _raw_stream = _marshal = None
 
 
 def _use_torch():
-    global _torch, _bf16, _f32, _i32, _i64, _raw_stream
+    global _torch, _bf16, _raw_stream, _marshal
     import torch
-    _torch, _bf16, _f32, _i32, _i64 = torch, torch.bfloat16, torch.float32, torch.int32, torch.int64
+    try:
+        from . import _marshal as m
+    except ImportError as e:
+        raise RuntimeError("_marshal.so is missing or was built for another torch: run `python -m paper_2509_23410_b200.build`") from e
+    _torch, _bf16, _marshal = torch, torch.bfloat16, m
     # the current stream's handle without a Stream object around it (five times quicker); device index -> handle
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
@@ -450,31 +457,12 @@ def _stream_of(x, stream):
     return _raw_stream(x.get_device()) if stream is None else stream.cuda_stream
 
 
-def _rows(x, M, D):
-    """Rows of heads [M, H, D]: bf16, heads side by side, any row pitch -> (pointer, pitch, H)."""
-    m, H, d = x.shape
-    sm, sh, sd = x.stride()
-    assert x.dtype is _bf16 and x.is_cuda and m == M and d == D and sd == 1 and (sh == D or H == 1), \
-        "heads are bf16 CUDA tensors [tokens, heads, D] whose rows hold the heads side by side"
-    return x.data_ptr(), sm if M > 1 else H * D, H
-
-
-def _vec(x, dtype, n):
-    if x is None:
-        return None
-    assert x.dtype is dtype and x.is_cuda and x.is_contiguous() and x.numel() == n, f"expected {n} contiguous {dtype} values on the GPU"
-    return x.data_ptr()
-
-
-_NONE = (None, 0, 0)
-
-
 def patch_rope(cos_sin, interleaved: bool = False) -> Rope:
     """Rotation by a table float32 [max_positions, rotary_dim]: a position's cosines, then its sines."""
     _use_torch()
-    assert cos_sin.is_cuda and cos_sin.dtype is _f32 and cos_sin.dim() == 2 and cos_sin.is_contiguous()
+    assert cos_sin.is_cuda and cos_sin.dtype is _torch.float32 and cos_sin.dim() == 2 and cos_sin.is_contiguous()
     r = Rope(cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], 1 if interleaved else 0)
-    r.table = cos_sin
+    r.table, r.at = cos_sin, ctypes.addressof(r)
     return r
 
 
@@ -486,7 +474,7 @@ def patch_kv_cache(k, v) -> KVCache:
     pages, H, page, D = k.shape
     assert k.stride()[1:] == (page * D, D, 1), "a page holds [Hkv, page_size, D] without gaps"
     c = KVCache(k.data_ptr(), v.data_ptr(), pages, k.stride(0) if pages > 1 else H * page * D, page, H, D, 0)
-    c.buffers, c.shape = (k, v), (H, page, D)
+    c.buffers, c.at = (k, v), ctypes.addressof(c)
     return c
 
 
@@ -495,21 +483,12 @@ def patch_qk_norm_rope(Q, K, rope: Rope | None, positions, wq=None, wk=None, eps
     """Norms of queries [M, Hq, D] and keys [M, Hkv, D] (either may be None) and the rotation: returns (Q_out, K_out)."""
     if _torch is None:
         _use_torch()
-    some = Q if Q is not None else K
-    M, _, D = some.shape
-    q = k = qo = ko = _NONE
-    if Q is not None:
-        if Q_out is None:
-            Q_out = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
-        q, qo = _rows(Q, M, D), _rows(Q_out, M, D)
-    if K is not None:
-        if K_out is None:
-            K_out = _torch.empty(K.shape, dtype=_bf16, device=K.device)
-        k, ko = _rows(K, M, D), _rows(K_out, M, D)
-    assert qo[2] == q[2] and ko[2] == k[2]
-    rc = lib().patch_qk_norm_rope(q[0], q[1], q[2], k[0], k[1], k[2], M, D, _vec(wq, _bf16, D), _vec(wk, _bf16, D), eps,
-                                  rope, _vec(positions, _i32, M), qo[0], qo[1], ko[0], ko[1],
-                                  status.data_ptr() if status is not None else None, _stream_of(some, stream))
+    if Q_out is None and Q is not None:
+        Q_out = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
+    if K_out is None and K is not None:
+        K_out = _torch.empty(K.shape, dtype=_bf16, device=K.device)
+    rc = _marshal.qk_norm_rope((_lib or lib()).at_patch_qk_norm_rope, Q, K, wq, wk, eps, rope.at if rope is not None else None, positions,
+                               Q_out, K_out, status, _stream_of(Q if Q is not None else K, stream))
     if rc:
         _check(rc, "patch_qk_norm_rope")
     return Q_out, K_out
@@ -528,33 +507,21 @@ def patch_qk_norm_rope_backward(gQ_out, gK_out, rope: Rope | None, positions, Q=
     if _torch is None:
         _use_torch()
     some = gQ_out if gQ_out is not None else gK_out
-    M, _, D = some.shape
-    dev = some.device
-    q = k = gqo = gko = gq = gk = _NONE
-    if gQ_out is not None:
-        if gQ is None:
-            gQ = _torch.empty(gQ_out.shape, dtype=_bf16, device=dev)
-        gqo, gq = _rows(gQ_out, M, D), _rows(gQ, M, D)
-        if wq is not None:
-            q = _rows(Q, M, D)
-            gwq = gwq if gwq is not None else _torch.empty(D, dtype=_f32, device=dev)
-    if gK_out is not None:
-        if gK is None:
-            gK = _torch.empty(gK_out.shape, dtype=_bf16, device=dev)
-        gko, gk = _rows(gK_out, M, D), _rows(gK, M, D)
-        if wk is not None:
-            k = _rows(K, M, D)
-            gwk = gwk if gwk is not None else _torch.empty(D, dtype=_f32, device=dev)
-    Hq, Hkv = gqo[2], gko[2]
-    assert gq[2] == Hq and gk[2] == Hkv and q[2] in (0, Hq) and k[2] in (0, Hkv)
+    if gQ is None and gQ_out is not None:
+        gQ = _torch.empty(gQ_out.shape, dtype=_bf16, device=some.device)
+    if gK is None and gK_out is not None:
+        gK = _torch.empty(gK_out.shape, dtype=_bf16, device=some.device)
+    if gwq is None and wq is not None:
+        gwq = _torch.empty(some.shape[2], dtype=_torch.float32, device=some.device)
+    if gwk is None and wk is not None:
+        gwk = _torch.empty(some.shape[2], dtype=_torch.float32, device=some.device)
     if workspace is None and (wq is not None or wk is not None):
-        workspace = _torch.empty(patch_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D), dtype=_torch.uint8, device=dev)
-    rc = lib().patch_qk_norm_rope_backward(gqo[0], gqo[1], gko[0], gko[1], q[0], q[1], Hq, k[0], k[1], Hkv, M, D, _vec(wq, _bf16, D),
-                                           _vec(wk, _bf16, D), eps, rope, _vec(positions, _i32, M),
-                                           gq[0], gq[1], gk[0], gk[1], _vec(gwq, _f32, D), _vec(gwk, _f32, D),
-                                           workspace.data_ptr() if workspace is not None else None,
-                                           workspace.numel() if workspace is not None else 0,
-                                           status.data_ptr() if status is not None else None, _stream_of(some, stream))
+        n = patch_qk_norm_rope_backward_workspace_size(some.shape[0], gQ_out.shape[1] if gQ_out is not None else 0,
+                                                       gK_out.shape[1] if gK_out is not None else 0, some.shape[2])
+        workspace = _torch.empty(n, dtype=_torch.uint8, device=some.device)
+    rc = _marshal.qk_norm_rope_backward((_lib or lib()).at_patch_qk_norm_rope_backward, gQ_out, gK_out, Q if wq is not None else None,
+                                        K if wk is not None else None, wq, wk, eps, rope.at if rope is not None else None, positions, gQ, gK,
+                                        gwq, gwk, workspace, status, _stream_of(some, stream))
     if rc:
         _check(rc, "patch_qk_norm_rope_backward")
     return gQ, gK, gwq, gwk
@@ -564,19 +531,10 @@ def patch_kv_append(cache: KVCache, K, V, slots, rope: Rope | None = None, posit
                     wq=None, Q_out=None, status=None, stream=None):
     """Keys (normed and rotated) and values [M, Hkv, D] into the cache's slots (int64 [M]; negative: not stored); with Q
     [M, Hq, D] also the queries, normed and rotated: returns Q_out (None without Q)."""
-    Hkv, _, D = cache.shape
-    M = K.shape[0]
-    k, v = _rows(K, M, D), _rows(V, M, D)
-    q = qo = _NONE
-    if Q is not None:
-        if Q_out is None:
-            Q_out = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
-        q, qo = _rows(Q, M, D), _rows(Q_out, M, D)
-    assert k[2] == v[2] == Hkv and qo[2] == q[2]
-    rc = lib().patch_kv_append(cache, k[0], k[1], v[0], v[1], _vec(slots, _i64, M), M, _vec(wk, _bf16, D), eps,
-                               rope, _vec(positions, _i32, M), q[0], q[1], q[2],
-                               _vec(wq, _bf16, D), qo[0], qo[1], status.data_ptr() if status is not None else None,
-                               _stream_of(K, stream))
+    if Q_out is None and Q is not None:
+        Q_out = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
+    rc = _marshal.kv_append((_lib or lib()).at_patch_kv_append, cache.at, K, V, slots, wk, eps, rope.at if rope is not None else None,
+                            positions, Q, wq, Q_out, status, _stream_of(K, stream))
     if rc:
         _check(rc, "patch_kv_append")
     return Q_out
@@ -584,8 +542,7 @@ def patch_kv_append(cache: KVCache, K, V, slots, rope: Rope | None = None, posit
 
 def patch_prefix_attention_workspace_size(cache: KVCache, B: int, T: int, Hq: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(lib().patch_prefix_attention_workspace_size(cache, B, T, Hq, ctypes.byref(n)),
-           "patch_prefix_attention_workspace_size")
+    _check(lib().patch_prefix_attention_workspace_size(cache, B, T, Hq, ctypes.byref(n)), "patch_prefix_attention_workspace_size")
     return int(n.value)
 
 
@@ -594,24 +551,14 @@ def patch_prefix_attention(cache: KVCache, Q, prefix_pages, prefix_len: int, pag
     """Attention of Q [B T, Hq, D] over the shared prefix (int32 ``prefix_pages``, ``prefix_len`` keys) and each sequence's own
     keys (int32 ``page_table`` [B, n], int32 ``suffix_lens`` [B]): returns O; ``lse`` float32 [B T, Hq] is written if given.
     ``scale`` defaults to 1 / sqrt(D)."""
-    _, page, D = cache.shape
-    B, ld = page_table.shape
-    M, Hq, _ = Q.shape
-    T = M // B if B else 1
-    need = -(-prefix_len // page)
-    assert M == B * T and (T > 0 or B == 0) and page_table.dtype is _i32 and page_table.is_cuda and page_table.is_contiguous()
-    assert need == 0 or (prefix_pages.dtype is _i32 and prefix_pages.is_cuda and prefix_pages.is_contiguous()
-                         and prefix_pages.numel() >= need), "prefix_pages does not cover prefix_len"
     if O is None:
         O = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
     if workspace is None:
-        workspace = _torch.empty(patch_prefix_attention_workspace_size(cache, B, T, Hq), dtype=_torch.uint8, device=Q.device)
-    q, o = _rows(Q, M, D), _rows(O, M, D)
-    assert o[2] == Hq
-    rc = lib().patch_prefix_attention(cache, q[0], q[1], B, T, Hq, prefix_pages.data_ptr() if need else None, prefix_len,
-                                      page_table.data_ptr(), ld, _vec(suffix_lens, _i32, B), D ** -0.5 if scale is None else scale,
-                                      o[0], o[1], _vec(lse, _f32, M * Hq), workspace.data_ptr(), workspace.numel(),
-                                      status.data_ptr() if status is not None else None, _stream_of(Q, stream))
+        B = page_table.shape[0]
+        workspace = _torch.empty(patch_prefix_attention_workspace_size(cache, B, Q.shape[0] // B if B else 1, Q.shape[1]),
+                                 dtype=_torch.uint8, device=Q.device)
+    rc = _marshal.prefix_attention((_lib or lib()).at_patch_prefix_attention, cache.at, Q, prefix_pages, prefix_len, page_table, suffix_lens,
+                                   scale, O, lse, workspace, status, _stream_of(Q, stream))
     if rc:
         _check(rc, "patch_prefix_attention")
     return O

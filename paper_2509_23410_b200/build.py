@@ -13,19 +13,41 @@ SOURCES = ["pack.cu", "masks.cu", "gemv.cu", "gemm_decode_sm100.cu", "gemm_decod
            "qk_rope.cu", "attention.cu", "attention_decode_sm100.cu", "attention_block_sm100.cu", "api.cu"]
 
 
+MARSHAL = os.path.join(HERE, "_marshal.so")
+
+
 def _stale(lib: str = LIB) -> bool:
     if not os.path.exists(lib):
         return True
     t = os.path.getmtime(lib)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if os.path.isfile(os.path.join(CSRC, f))]
+    if lib == MARSHAL:
+        deps = [os.path.join(CSRC, "marshal.cpp")]
+    else:
+        deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if os.path.isfile(os.path.join(CSRC, f)) and not f.endswith(".cpp")]
     deps.append(os.path.join(os.path.dirname(HERE), "include", "patch.h"))
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def build_marshal(force: bool = False) -> str:
+    """The CPython module that takes torch tensors apart for the calls of a few microseconds (g++, torch's headers)."""
+    if not (force or _stale(MARSHAL)):
+        return MARSHAL
+    import sysconfig
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc, lib = os.path.join(root, "include"), os.path.join(root, "lib")
+    abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={abi}", f"-I{inc}",
+                    "-I" + os.path.join(inc, "torch", "csrc", "api", "include"), "-I" + sysconfig.get_paths()["include"], "-o", MARSHAL,
+                    os.path.join(CSRC, "marshal.cpp"), f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10", f"-Wl,-rpath,{lib}"], check=True)
+    return MARSHAL
 
 
 def build(force: bool = False, verbose: bool = False, fault_injection: bool = False) -> str:
     """The library; with ``fault_injection`` the test build ``libpatch_b200_fi.so`` (same sources with
     -DPATCH_FAULT_INJECTION: device-side waits give up after 300 us, and the stream-K decode kernel can be told,
     through its status word, to announce bytes that never arrive -- how the tests make a bounded wait run out)."""
+    build_marshal(force and not fault_injection)
     lib = LIB_FI if fault_injection else LIB
     if not (force or _stale(lib)):
         return lib
