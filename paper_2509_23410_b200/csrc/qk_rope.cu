@@ -253,6 +253,7 @@ rope_backward_kernel(const GradHeads q, const GradHeads k, const Turn turn, int6
     __shared__ float sums[kGroups][LANES * 8];
     __shared__ int kinds[kGroups];
     const int D = DT ? DT : d;
+    grid_launch_dependents();                 // the kernel that adds up the partial sums waits for this one's end by itself
     const int per_token = q.groups + k.groups;
     const int group = threadIdx.x / LANES;
     const int64_t idx = int64_t(blockIdx.x) * kGroups + group;
@@ -339,6 +340,7 @@ rope_weight_sum_kernel(const float* __restrict__ partial, int rows, int D, float
     __shared__ float sums[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
     float s = 0.0f;
+    grid_dependency_wait();
     if (j < 2 * D)
         for (int r = warp; r < rows; r += 32) s += partial[int64_t(r) * 2 * D + j];
     sums[warp][lane] = s;
@@ -454,8 +456,18 @@ struct Backward {
         if (blocks < least) blocks = least;
         const int64_t stride = int64_t(blocks) * (kThreads / LANES) / per_token;
         rope_backward_kernel<LANES, DT, INTER, FULL><<<blocks, kThreads, 0, s>>>(q, k, t, M, D, eps, stride, partial, status_dev);
-        if (partial) rope_weight_sum_kernel<<<(2 * D + 31) / 32, 1024, 0, s>>>(partial, blocks, D, gwq, gwk);
-        return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+        if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
+        if (!partial) return PATCH_OK;
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        cfg.gridDim = dim3(unsigned(2 * D + 31) / 32, 1, 1);
+        cfg.blockDim = dim3(1024, 1, 1);
+        cfg.stream = s;
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, rope_weight_sum_kernel, static_cast<const float*>(partial), blocks, D, gwq, gwk) == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
     }
 };
 
