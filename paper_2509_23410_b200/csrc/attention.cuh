@@ -233,7 +233,7 @@ __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* m
 
 // The decode kernel (attention_decode_sm100.cu) takes rows in blocks of kDecodeRows, the block kernel (attention_block_sm100.cu) in
 // blocks of kBlockRows.
-constexpr int kDecodeRows = 16, kBlockRows = 256;
+constexpr int kDecodeRows = 16, kBlockRows = 128;
 constexpr int kDecodeKeys = 64, kBlockKeys = 128;     // keys of a tile
 constexpr int kDecodeCost = 1, kBlockCost = 3;        // Line::cost
 constexpr int kMaxShares = 4 * kMaxSms;               // CTAs of one launch, at most

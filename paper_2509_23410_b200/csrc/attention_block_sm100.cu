@@ -7,19 +7,21 @@
 // sum of 2^(s - m) passes 256: the sum is needed anyway, no maximum is taken of the other tiles, and the accumulator is rarely
 // rescaled.  (The relative rounding of the bf16 probabilities does not depend on their size.)
 //
-// Kernel.  One CTA per SM, 128 query rows and 128 keys per tile, two streams x = 0, 1 of
-//     S_x = Q_x K^T (shared x shared -> TMEM),  P_x = 2^(S_x - m) (TMEM -> registers -> TMEM, over S_x),  O_x += P_x V (TMEM x shared)
-// so that one stream multiplies while the other is in its softmax.  An item of more than 128 rows gives each stream 128 rows, both
-// read the same keys; an item of fewer gives both streams the same rows and every second tile, and the two results are joined in
-// TMEM at the end.
+// Kernel.  One CTA per SM, an item is at most 128 query rows, a tile 128 keys; two streams x = 0, 1 take every second tile with the same
+// rows:
+//     S_x = Q K^T (shared x shared -> TMEM),  P_x = 2^(S_x - m_x) (TMEM -> registers -> TMEM, over S_x),  O_x += P_x V (TMEM x shared)
+// so that one stream multiplies while the other is in its softmax; the two results are joined in TMEM at the end.  (256 rows to an
+// item, a stream for each half, reads the keys once instead of twice, the second time from L2, but was the slower one
+// throughout: 52 us against 44 for 256 rows and 32768 keys of 8 heads, 76 against 74 for 512 rows.)
 //   warp 0       producer: tiles of keys and values, one TMA box per page and 64-element half, into a ring of 32 KB stages (D = 128),
 //                as many as fit beside the query tiles
 //   warp 1       issues the MMAs; zeroes the rows of V past the item's last key (a probability of 0 times whatever the
 //                cache holds there is not always 0)
 //   warps 4..7   softmax of stream 0, one thread per row; warps 8..11 stream 1.  They also bring an item's query rows into the
-//                swizzled layout (any head count per key head, any row pitch) and write its partial result.
-// What bounds it: HBM up to about 256 rows per key head -- 64 KB of keys and values per tile and SM take 2 850 cycles, its
-// four products (two streams) 2 048, the exponentials 2 048.
+//                swizzled layout (any head count per key head, any row pitch) and write its partial result, half of the columns each.
+// What bounds it: a tile's 64 KB of keys and values take an SM 2 850 cycles of HBM, its two products 1 024 and its exponentials 1 024,
+// but a stream's tile is a chain -- scores, softmax, products -- of 4 000 cycles, so two streams need 2 000 a tile: HBM bounds one block of
+// 128 rows, the chain more of them.
 // Tried: tiles of 64 keys with two score buffers per stream, so that no stream waits for its own products: 5 600 cycles per 128
 // keys and two streams -- twice the MMAs of the scores and twice the waits, and the warp that issues them became the bottleneck.
 #include "attention.cuh"
@@ -41,18 +43,17 @@ template <int D> struct Cfg {
     static constexpr uint32_t kQTile = 128 * D * 2;
     static constexpr uint32_t kBarBytes = 256;
 };
-// Shared memory: [ring | query tiles | barriers | units and lengths of the sequences, where the kernel has suffix items].
-struct Room { int ring, q_tiles; uint32_t q, bars, cum, bytes; };
+// Shared memory: [ring | query tile | barriers | units and lengths of the sequences, where the kernel has suffix items].
+struct Room { int ring; uint32_t q, bars, cum, bytes; };
 template <int D>
-static Room room_of(const Line& w, int B, int rows) {
+static Room room_of(const Line& w, int B) {
     using C = Cfg<D>;
     Room r;
-    r.q_tiles = rows > 128 ? 2 : 1;
-    const uint32_t cum = w.blocks_s ? uint32_t(2 * B + 1) * 4 : 0, rest = r.q_tiles * C::kQTile + C::kBarBytes + cum + 1024;
+    const uint32_t cum = w.blocks_s ? uint32_t(2 * B + 1) * 4 : 0, rest = C::kQTile + C::kBarBytes + cum + 1024;
     r.ring = int((227u * 1024 - rest) / C::kTile);
     if (r.ring > kMaxRing) r.ring = kMaxRing;
     r.q = r.ring * C::kTile;
-    r.bars = r.q + r.q_tiles * C::kQTile;
+    r.bars = r.q + C::kQTile;
     r.cum = r.bars + C::kBarBytes;
     r.bytes = rest + r.ring * C::kTile;
     return r;
@@ -92,6 +93,9 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32
 #undef PATCH_S32
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// n consecutive columns, n = 16 or 32
+__device__ __forceinline__ void load_quarter(uint32_t taddr, uint32_t (&v)[32]) { tmem_ld32(taddr, v); }
+__device__ __forceinline__ void load_quarter(uint32_t taddr, uint32_t (&v)[16]) { tmem_ld16(taddr, v); }
 // true in one lane of the (converged) warp, always the same one
 __device__ __forceinline__ bool elect_one() {
     uint32_t pred;
@@ -156,19 +160,16 @@ __device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool part
     return a + b;
 }
 
-// Number of a stream's tiles among n: all of them where each stream has rows of its own, else every second.
-__device__ __forceinline__ int stream_tiles(int n, bool dual, int x) { return dual ? n : (n + 1 - x) >> 1; }
-
 // How many SMs the block kernel takes where the decode kernel has the suffixes.  Together they are done no sooner than HBM has
 // delivered the keys and values and the SMs have done their cycles; with as many SMs as its own cycles need in that time, the block
 // kernel ends with the decode kernel, which streams from the other SMs meanwhile -- one is short of arithmetic, the other of
-// bandwidth.  Cycles measured: 4 000 for a key tile and 256 rows, 3 300 for one and 128 rows (two tiles at a time, waiting for HBM),
+// bandwidth.  Cycles measured: 2 000 for a tile, 3 300 where HBM is waited for (one block of rows),
 // 700 for a tile of the decode kernel (two CTAs share its latencies); bandwidth in bytes per cycle of 6.5 TB/s at 1.9 GHz.  64
 // sequences behind 32768 keys: 82 us against 101 with the block kernel on all SMs first.
 template <int D>
 __device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w, float keys, int sms) {
-    const float rows = float(p.B) * p.T * p.G, heads = float(p.Hkv);
-    const float mine = heads * w.tiles_p * (4000.0f * floorf(rows / 256.0f) + (fmodf(rows, 256.0f) > 128.0f ? 4000.0f : fmodf(rows, 256.0f) > 0.0f ? 3300.0f : 0.0f));
+    const float heads = float(p.Hkv);
+    const float mine = heads * w.tiles_p * (w.blocks_p == 1 ? 3300.0f : 2000.0f * w.blocks_p);
     const float theirs = heads * keys / kDecodeKeys * 700.0f;
     const float bytes = heads * (keys + float(p.prefix_len)) * D * 4.0f;
     const float time = fmaxf(bytes / 3420.0f, (mine + theirs) / sms);
@@ -236,7 +237,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     Share s(p, line, cum, lens);
 
     if (warp == 0) {
-        // ---------------- producer: the first keys, then V0 K(lead) V1 K(lead + 1) ... as they are consumed ----------------
+        // ---------------- producer: K0 K1, then V0 K2 V1 K3 ... as they are consumed ----------------
         const uint64_t policy = l2_policy_evict_first();
         const int rows_log2 = p.shift < 7 ? p.shift : 7;       // rows of a box: what one page gives to a tile
         const uint32_t box_bytes = 128u << rows_log2;
@@ -246,9 +247,8 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         for (bool have = s.start(u0, u1); have && ok; have = s.next()) {
             if (lane == 0) s.note(to, blockIdx.x);
             const int n_pages = s.pages();
-            const bool dual = s.rows() - s.block * kBlockRows > 128;
             const int n = s.t1 - s.t0;
-            // page numbers of the item's K tiles and V tiles, one per lane; the two run one or two tiles apart
+            // page numbers of the item's K tiles and V tiles, one per lane; the two run two tiles apart
             int at[2] = {-64, -64}, mine[2] = {0, 0};
             auto load = [&](int i, int v) {                    // tile i of the share, v = 0: keys, 1: values
                 const int64_t key0 = int64_t(s.t0 + i) * kKeys;
@@ -278,11 +278,10 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 ++issued;
                 if (++stage == ring) { stage = 0; phase ^= 1u; }
             };
-            const int lead = dual ? 1 : 2;
-            for (int i = 0; i < lead && i < n && ok; ++i) load(i, 0);
+            for (int i = 0; i < 2 && i < n && ok; ++i) load(i, 0);
             for (int i = 0; i < n && ok; ++i) {
                 load(i, 1);
-                if (i + lead < n && ok) load(i + lead, 0);
+                if (i + 2 < n && ok) load(i + 2, 0);
             }
         }
         if (*abort_flag) {
@@ -319,12 +318,10 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         // only a tile with rows past the last key, an item's last, brings the warp together.  Loops stay rolled: this warp's few
         // instructions compete with the softmax warps' for the instruction cache.
         for (bool have = s.start(u0, u1); have && ok; have = s.next()) {
-            const bool dual = s.rows() - s.block * kBlockRows > 128;
-            const int n = s.t1 - s.t0, lead = dual ? 1 : 2;
-            const int valid = s.keys - (s.t1 - 1) * kKeys;     // rows of the last tile
-            const uint32_t q0 = base + room.q, q1 = dual ? q0 + C::kQTile : q0;
+            const int n = s.t1 - s.t0, valid = s.keys - (s.t1 - 1) * kKeys;          // valid: rows of the last tile
+            const uint32_t q_tile = base + room.q;
             const bool leader = elect_one();
-            int i = -lead;                                     // tile whose products are next; below 0: scores only
+            int i = -2;                                        // tile whose products are next; below 0: scores only
             uint32_t v_stage = 0;
             if (leader) wait(bar_q, phase_q);
             phase_q ^= 1u;
@@ -332,33 +329,29 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 if (leader) {
 #pragma unroll 1
                     for (; i < n && ok; ++i) {
-                        if (i >= 0 && (i + 1 < n || !zeroed || valid >= kKeys)) {
+                        const int x = i & 1;
+                        if (i >= 0) {
+                            if (i + 1 < n || !zeroed || valid >= kKeys) {            // else the tile is here and its rows are zeroed
+                                wait(bar_full + 8 * stage, phase);
+                                v_stage = stage;
+                                advance();
+                            }
+                            if (i + 1 == n && !zeroed) break;
+#pragma unroll 1
+                            for (int half = 0; half < 2 && ok; ++half) {
+                                wait(bar_p + 16 * half + 8 * x, (phase_p >> x) & 1u);
+                                if (ok) outputs(x, base + v_stage * C::kTile, i < 2 && half == 0, half);
+                                if (half == 0) mma_commit(bar_h + 8 * x);
+                            }
+                            phase_p ^= 1u << x;
+                            mma_commit(bar_empty + 8 * v_stage);
+                        }
+                        if (i + 2 < n) {                       // the scores of the tile that takes this one's place
                             wait(bar_full + 8 * stage, phase);
-                            v_stage = stage;
+                            if (ok) scores(x, q_tile, base + stage * C::kTile);
+                            mma_commit(bar_empty + 8 * stage);
                             advance();
                         }
-                        if (i + 1 == n && !zeroed) break;
-                        const bool more = i + lead < n;
-#pragma unroll 1
-                        for (int y = 0; y < (dual ? 2 : 1) && ok; ++y) {
-                            const int x = dual ? y : i & 1;
-                            const bool last = !dual || y == 1;
-                            if (i >= 0) {
-#pragma unroll 1
-                                for (int half = 0; half < 2 && ok; ++half) {
-                                    wait(bar_p + 16 * half + 8 * x, (phase_p >> x) & 1u);
-                                    if (ok) outputs(x, base + v_stage * C::kTile, (dual ? i == 0 : i < 2) && half == 0, half);
-                                    if (half == 0) mma_commit(bar_h + 8 * x);
-                                }
-                                phase_p ^= 1u << x;
-                                if (last) mma_commit(bar_empty + 8 * v_stage);
-                            }
-                            if (!more) continue;
-                            if (y == 0) wait(bar_full + 8 * stage, phase);
-                            if (ok) scores(x, x ? q1 : q0, base + stage * C::kTile);
-                            if (last) mma_commit(bar_empty + 8 * stage);
-                        }
-                        if (more) advance();
                     }
                     if (ok && zeroed) mma_commit(bar_o);
                 }
@@ -383,43 +376,35 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         uint32_t phase_s = 0, phase_h = 0, phase_o = 0;
         bool failed = false;
         for (bool have = s.start(u0, u1); have && !failed; have = s.next()) {
-            const int rows = s.rows() - s.block * kBlockRows;  // of this block and the ones after it
-            const bool dual = rows > 128;
-            const int n = s.t1 - s.t0, mine = stream_tiles(n, dual, x);
-            const int r = s.block * kBlockRows + (dual ? 128 * x : 0) + row;     // row of the item
-            const bool valid = r < s.rows();
-            // this warp's 32 query rows into the swizzled layout, a row (256 bytes at D = 128) by D / 8 neighbouring lanes -- a lane per
-            // row would touch 32 lines with every load (6 100 cycles for 256 rows); rows past the item's are zeros
-            if (dual || x == 0) {
+            const int n = s.t1 - s.t0, first = s.block * kBlockRows, here = min(kBlockRows, s.rows() - first);
+            const bool valid = row < here;
+            // query rows into the swizzled layout, 16 of them by every warp, a row (256 bytes at D = 128) by D / 8 neighbouring lanes --
+            // a lane per row would touch 32 lines with every load; rows past the item's are zeros
+            {
                 constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
-                const int c = lane & (kLanes - 1);
-                uint8_t* dst = smem + room.q + x * C::kQTile + (c >> 3) * C::kQAtom;
-                const int first = s.block * kBlockRows + (dual ? 128 * x : 0);
+                const int c = lane & (kLanes - 1), warp_row = 16 * (warp - 4) + lane / kLanes;
+                uint8_t* dst = smem + room.q + (c >> 3) * C::kQAtom;
                 const __nv_bfloat16* from = p.Q + (s.b < 0 ? 0 : int64_t(s.b) * p.T) * p.ldq + int64_t(s.kvh) * p.G * D + 8 * c;
-#pragma unroll 1
-                for (int h = 0; h < 32; h += 8 * kAtOnce) {
-                    uint4 v[8];
+                uint4 v[16 / kAtOnce];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int at = quad * 32 + h + i * kAtOnce + lane / kLanes, rr = first + at, tok = p.token(rr);
-                        v[i] = rr < s.rows() ? *reinterpret_cast<const uint4*>(from + tok * p.ldq + int64_t(rr - tok * p.G) * D) : make_uint4(0u, 0u, 0u, 0u);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<uint4*>(dst + atom_chunk_offset(quad * 32 + h + i * kAtOnce + lane / kLanes, c & 7)) = v[i];
+                for (int i = 0; i < 16 / kAtOnce; ++i) {
+                    const int rr = first + warp_row + i * kAtOnce, tok = p.token(rr);
+                    v[i] = rr < s.rows() ? *reinterpret_cast<const uint4*>(from + tok * p.ldq + int64_t(rr - tok * p.G) * D) : make_uint4(0u, 0u, 0u, 0u);
                 }
+#pragma unroll
+                for (int i = 0; i < 16 / kAtOnce; ++i) *reinterpret_cast<uint4*>(dst + atom_chunk_offset(warp_row + i * kAtOnce, c & 7)) = v[i];
                 fence_async_shared();
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_q);
-            const int see = s.b < 0 ? s.keys : s.keys - (p.T - 1 - p.token(r));      // keys the row sees
+            const int see = s.b < 0 ? s.keys : s.keys - (p.T - 1 - p.token(first + row));      // keys the row sees
             float m = -INFINITY, l = 0.0f;
-            for (int j = 0; j < mine; ++j) {
+            for (int j = 0; 2 * j + x < n; ++j) {
                 failed = __any_sync(0xFFFFFFFFu, !mbar_wait(bar_s + 8 * x, phase_s, abort_flag, p.status));
                 if (failed) break;
                 phase_s ^= 1u;
                 tc_fence_after();
-                const int left = see - (s.t0 + (dual ? j : 2 * j + x)) * kKeys;      // columns the row sees
+                const int left = see - (s.t0 + 2 * j + x) * kKeys;      // columns the row sees
                 const bool partly = __any_sync(0xFFFFFFFFu, left < kKeys);
                 if (j == 0) m = row_top(t_s, kKeys / 32, left) * p.scale_log2;
                 // The products of the first half of the keys start while the second half is worked on.
@@ -470,59 +455,41 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             tc_fence_after();
             ml[128 * x + row] = make_float2(m, l);
             if (barrier_any(failed, 1, 256)) { failed = true; break; }
-            // ---- the partial result: a quarter of the columns at a time through shared memory (where the queries were), from
-            // there in one copy; a lane's own row straight to memory would touch 32 lines with every store (6 800 cycles) ----
+            // ---- the partial result: both streams hold a part of the same rows, each joins half of the columns, a quarter at a time
+            // through shared memory (where the queries were) and from there in one copy ----
             const Parts& part = s.b < 0 ? to.p : to.s;
             const int64_t slot = s.item + int64_t(blockIdx.x);
-            const int base_row = dual ? 128 * x : 0, here = min(128, s.rows() - s.block * kBlockRows - base_row);
-            float fa = 1.0f, fb = 0.0f;
-            if (!dual) {                                       // both streams hold a part of the same rows: each takes half of the columns
-                const float2 a = ml[row], b = ml[128 + row];
-                const float mx = fmaxf(a.x, b.x);
-                fa = a.x == -INFINITY ? 0.0f : ex2(a.x - mx);
-                fb = b.x == -INFINITY ? 0.0f : ex2(b.x - mx);
-                m = mx;
-                l = a.y * fa + b.y * fb;
-            }
-            if (valid && (dual || x == 0)) part.ml[slot * part.rows + base_row + row] = make_float2(m, l);
+            const float2 a = ml[row], b = ml[128 + row];
+            const float mx = fmaxf(a.x, b.x);
+            const float fa = a.x == -INFINITY ? 0.0f : ex2(a.x - mx), fb = b.x == -INFINITY ? 0.0f : ex2(b.x - mx);
+            if (valid && x == 0) part.ml[slot * part.rows + row] = make_float2(mx, a.y * fa + b.y * fb);
             barrier_any(false, 1, 256);                        // (m, l) have been read
             constexpr uint32_t kQuarter = 128 * D;             // bytes of 128 rows
             constexpr int kChunks = D / 16;                    // of a row
-            uint8_t* stage = smem + room.q + x * (dual ? C::kQTile : kQuarter);
+            uint8_t* const stage = smem + room.q + x * kQuarter;
 #pragma unroll 1
-            for (int q = dual ? 0 : 2 * x; q < (dual ? 4 : 2 * x + 2); ++q) {
-                uint32_t o[D / 4];
-                if (dual || n == 1) {
-                    if constexpr (D == 128) tmem_ld32(tmem + lanes + 256u + (dual ? 128u * x : 0u) + (D / 4) * q, o);
-                    else tmem_ld16(tmem + lanes + 256u + (dual ? 128u * x : 0u) + (D / 4) * q, o);
-                    tmem_ld_wait();
-                } else {
-                    uint32_t o1[D / 4];
-                    if constexpr (D == 128) {
-                        tmem_ld32(tmem + lanes + 256u + (D / 4) * q, o);
-                        tmem_ld32(tmem + lanes + 384u + (D / 4) * q, o1);
-                    } else {
-                        tmem_ld16(tmem + lanes + 256u + (D / 4) * q, o);
-                        tmem_ld16(tmem + lanes + 384u + (D / 4) * q, o1);
-                    }
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int c = 0; c < D / 4; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * fa + __uint_as_float(o1[c]) * fb);
-                }
-                if (q & 1 && !dual || q == 2) {                // the buffer's last copy has been read
+            for (int q = 2 * x; q < 2 * x + 2; ++q) {
+                uint32_t o[D / 4], o1[D / 4];
+                load_quarter(tmem + lanes + 256u + (D / 4) * q, o);
+                if (n > 1) load_quarter(tmem + lanes + 384u + (D / 4) * q, o1);
+                tmem_ld_wait();
+                if (q & 1) {                                   // the first copy has read the buffer
                     if (row == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     barrier_any(false, 2 + x, 128);
                 }
-                uint8_t* to_row = stage + (dual ? (q & 1) * kQuarter : 0u) + row * D;
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c)
-                    *reinterpret_cast<uint4*>(to_row + ((c ^ (row & (kChunks - 1))) << 4)) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                for (int c = 0; c < kChunks; ++c) {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        v[i] = __float_as_uint(__uint_as_float(o[4 * c + i]) * fa + (n > 1 ? __uint_as_float(o1[4 * c + i]) * fb : 0.0f));
+                    *reinterpret_cast<uint4*>(stage + row * D + ((c ^ (row & (kChunks - 1))) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                }
                 fence_async_shared();
                 barrier_any(false, 2 + x, 128);
-                if (row == 0 && here > 0) {
-                    const uint32_t src = smem_u32(stage) + (dual ? (q & 1) * kQuarter : 0u);
-                    float* dst = part.o + ((slot * 4 + q) * part.rows + base_row) * (D / 4);
-                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(uint32_t(here) * D) : "memory");
+                if (row == 0) {
+                    float* dst = part.o + (slot * 4 + q) * part.rows * (D / 4);
+                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(stage)), "r"(uint32_t(here) * D) : "memory");
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
             }
@@ -548,7 +515,7 @@ static int launch_block(const patch_kv_cache_t* c, const Problem& p, const Line&
     auto kern = attn_block_kernel<D>;
     static std::atomic<uint64_t> configured{0};
     if ((rc = allow_dynamic_smem(kern, 227 * 1024, configured))) return rc;
-    const blk::Room room = blk::room_of<D>(w, p.B, w.blocks_p ? to.p.rows : to.s.rows);
+    const blk::Room room = blk::room_of<D>(w, p.B);
     const int sms = sm_count();
     if (sms <= 0) return PATCH_ERR_CUDA;
     kern<<<sms < kMaxSms ? sms : kMaxSms, blk::kThreads, room.bytes, stream>>>(mk, mv, p, w, to, room, share_gpu);
