@@ -9,6 +9,12 @@
 namespace patch {
 namespace attn {
 
+// Number of an item's parts.  A launch that gave up (PATCH_ERR_TIMEOUT) may have left items without a note: whatever lies there then
+// must not lead out of the workspace.
+__device__ __forceinline__ int parts_of(int2 span) {
+    return unsigned(span.x) < unsigned(kMaxShares) && unsigned(span.y) < unsigned(kMaxShares) && span.x <= span.y ? span.y - span.x + 1 : 0;
+}
+
 // Joins the partial results: one warp per query row and head.  Bound by the latency of three dependent reads (which CTAs, their
 // (m, l), their outputs); the (m, l) of up to 32 parts are read at once, one per lane, their outputs eight at a time.
 template <int D>
@@ -30,14 +36,14 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
     if (blocks_p) {
         const int r = tok * p.G + gq, blk = r / from.p.rows, item = kvh * blocks_p + blk;
         const int2 span = from.p.span[item];
-        count[0] = span.y - span.x + 1;
+        count[0] = parts_of(span);
         at[0] = int64_t(item) + span.x;
         place[0] = r - blk * from.p.rows;
     }
     if (own) {
         const int r = (tok - b * p.T) * p.G + gq, blk = r / from.s.rows, item = (b * p.Hkv + kvh) * blocks_s + blk;
         const int2 span = from.s.span[item];
-        count[1] = span.y - span.x + 1;
+        count[1] = parts_of(span);
         at[1] = int64_t(item) + span.x;
         place[1] = r - blk * from.s.rows;
     }

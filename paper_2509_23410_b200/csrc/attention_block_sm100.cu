@@ -244,6 +244,16 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         int stage = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
+#ifdef PATCH_FAULT_INJECTION
+        uint32_t inject = 0u;                                  // as in the decode kernel
+        if (blockIdx.x == 0 && p.status && *p.status == kInjectMagic) {
+            inject = 16u;
+            __syncwarp();
+            if (lane == 0) *p.status = PATCH_OK;
+        }
+#else
+        constexpr uint32_t inject = 0u;
+#endif
         for (bool have = s.start(u0, u1); have && ok; have = s.next()) {
             if (lane == 0) s.note(to, blockIdx.x);
             const int n_pages = s.pages();
@@ -272,7 +282,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 const int row_in_page = p.shift < 7 ? 0 : int(key0 & ((1 << p.shift) - 1));
                 ok = __all_sync(0xFFFFFFFFu, issued < ring || mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status));
                 if (!ok) return;
-                if (lane == 0) mbar_expect_tx(full, uint32_t(boxes) * uint32_t(D / 64) * box_bytes);
+                if (lane == 0) mbar_expect_tx(full, uint32_t(boxes) * uint32_t(D / 64) * box_bytes + (issued == 0 ? inject : 0u));
                 __syncwarp();
                 if (on) tma_load_page(dst, map, row_in_page, lane & 1, s.kvh, page, full, policy);
                 ++issued;

@@ -105,6 +105,18 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         int stage = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
+#ifdef PATCH_FAULT_INJECTION
+        // test build: a status word holding kInjectMagic makes CTA 1 (CTA 0 may have no tile) announce sixteen bytes more
+        // than its first stage will ever receive
+        uint32_t inject = 0u;
+        if (blockIdx.x == 1 && p.status && *p.status == kInjectMagic) {
+            inject = 16u;
+            __syncwarp();
+            if (lane == 0) *p.status = PATCH_OK;
+        }
+#else
+        constexpr uint32_t inject = 0u;
+#endif
         // this lane's page number of an item: entry page0 + lane of its list
         auto fetch = [&](const Share& s, int page0) { return page0 + lane < s.pages() ? s.list()[page0 + lane] : 0; };
         Share s(p, w, cum, lens), ahead(s);
@@ -142,7 +154,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 const uint32_t bytes = uint32_t(copies) * 2u * copy_bytes + uint32_t(rows) * D * 2u;
                 ok = __all_sync(0xFFFFFFFFu, issued < kStages || mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, p.status));
                 if (!ok) break;
-                if (lane == 0) mbar_expect_tx_only(full, bytes);
+                if (lane == 0) mbar_expect_tx_only(full, bytes + (issued == 0 ? inject : 0u));
                 __syncwarp();
                 if (on) tma_load_page(dst, map, row_in_page, 0, s.kvh, page, full, policy);
                 if (opens && lane >= 16 && lane - 16 < rows) {

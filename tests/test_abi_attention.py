@@ -137,3 +137,26 @@ def test_attention_refusals(B):
     assert L.patch_prefix_attention_workspace_size(c, 3, 1, 8, None) == B.ERR_NULL
     with pytest.raises(B.PatchError):
         B.patch_prefix_attention_workspace_size(c, 3, 1, 9)
+
+
+def test_tensors_are_checked_before_the_library_is_called(B):
+    """The module that takes tensors apart: wrong types, shapes, layouts and devices are refused (a null function would be called last)."""
+    torch = pytest.importorskip("torch")
+    from paper_2509_23410_b200 import _marshal as m
+    x = torch.zeros(4, 2, 128, dtype=torch.bfloat16)
+    c = cache(B)
+    at = ctypes.addressof(c)
+    for bad in (x, x.float(), x[:, :, ::2], x[0], 5, "x", x.transpose(0, 1)):
+        with pytest.raises(AssertionError):
+            m.kv_append(0, at, bad, bad, None, None, 1e-6, None, None, None, None, None, None, 0)
+        with pytest.raises(AssertionError):
+            m.qk_norm_rope(0, bad, None, None, None, 1e-6, None, None, bad, None, None, 0)
+        with pytest.raises(AssertionError):
+            m.qk_norm_rope_backward(0, bad, None, None, None, None, None, 1e-6, None, None, bad, None, None, None, None, None, 0)
+        with pytest.raises(AssertionError):
+            m.prefix_attention(0, at, bad, None, 0, bad, bad, None, bad, None, None, None, 0)
+    with pytest.raises(AssertionError):
+        m.qk_norm_rope(0, None, None, None, None, 1e-6, None, None, None, None, None, 0)
+    for f in (m.kv_append, m.qk_norm_rope, m.qk_norm_rope_backward, m.prefix_attention):
+        with pytest.raises(TypeError):
+            f(0)
