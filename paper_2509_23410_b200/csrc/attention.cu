@@ -107,6 +107,22 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
 constexpr int kMostDecodeRows = 64, kMostDecodeKeys = 1024;
 static bool block_suffixes(int64_t rows, int64_t keys) { return rows > kMostDecodeRows || (rows > kDecodeRows && keys > kMostDecodeKeys); }
 
+// CTAs of a cluster for each item of the small problems that take one launch of their own (attn_direct_kernel), 0 for the others.
+// There every item reads the prefix for itself, so it is a matter of how many tiles there are in all (by the tables' width): up to
+// eight for each CTA that can run at once.  Measured, one launch against two or three, 13B heads: one sequence, 128 + 100 keys 5.1 us
+// against 8.3, 4096 + 100 keys (7 tiles a slot) 15.4 against 18.0, 4 x (1024 + 100) (8 a slot) 11.9 against 11.9; 8 key heads of 4
+// rows, 16 x (64 + 500) 9.0 us against 26.1 (32 rows or more of a prefix are the block kernel's otherwise).  A second wave of items
+// is worth it only where a prefix would be a launch of its own: 2 items a slot 14.6 us against 32.8 with one, 3 items a slot without 14.1
+// against 12.2.  Clusters of 16 (more than the portable 8) pay from four tiles a CTA: 71 tiles an item 10.4 us against 11.4, 16
+// tiles 7.7 against 6.8.
+static int direct_split(int64_t rows, int64_t items, int64_t prefix_len, int64_t table_keys) {
+    const int64_t slots = 2 * sm_count(), tiles = (prefix_len + kDecodeKeys - 1) / kDecodeKeys + (table_keys + kDecodeKeys - 1) / kDecodeKeys;
+    if (rows > kDecodeRows || tiles > 8 * slots || items * tiles > 8 * slots || items > (prefix_len ? 2 : 1) * slots) return 0;
+    int split = 1;                                   // all CTAs at once, and each with a tile at least
+    while (split < 16 && 2 * split * items <= slots && tiles >= (split < 8 ? 2 * split : 64)) split *= 2;
+    return split;
+}
+
 struct Plan {
     bool block_p, block_s;                           // prefix / suffixes on the block kernel
     int blocks_p, blocks_s, rows_p, rows_s;          // row blocks per key head, rows of a slot
@@ -188,6 +204,8 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     if (G > 1 && B * T * G * int64_t(G) < (int64_t(1) << 32)) p.g_mul = uint32_t(((uint64_t(1) << 32) + G - 1) / G);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
+    if (const int split = direct_split(int64_t(T) * G, B * cache->Hkv, prefix_len, ld_table * cache->page_size))
+        return launch_attn_direct(cache, p, split, static_cast<__nv_bfloat16*>(O), ldo, lse, s);
     const Plan q = plan_of(cache, B, T, G, ld_table * cache->page_size);
     const Results to = {{reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float2*>(ws + q.ml_p), reinterpret_cast<int2*>(ws), q.rows_p, q.block_p},
                         {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s, q.block_s}};

@@ -136,6 +136,41 @@ def test_against_the_definition(B, case, layout):
     assert torch.equal(o, o2), "equal calls give equal bits"
 
 
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_behind_wide_tables(B, case):
+    """The kernels are chosen by the width of the page table: the same batches with room for 160000 keys a sequence, which takes none
+    of them into the single launch of small problems."""
+    lens, T, Hq, Hkv, D, P, page = CASES[case]
+    x = Batch(B, lens, T, Hq, Hkv, D, P, page, seed=case, extra=160000 // page)
+    o, l = x.run(B)
+    x.check(o, l)
+    o2, _ = x.run(B, lse=False)
+    assert torch.equal(o, o2), "equal calls give equal bits"
+
+
+SMALL = [  # lens, T, Hq, Hkv, D, P, page: from one CTA to sixteen an item, items beyond the CTAs that run at once
+    ([8000], 1, 8, 1, 128, 0, 16),
+    ([500], 1, 16, 2, 128, 4000, 64),
+    ([16000, 3, 0, 5000], 4, 8, 2, 64, 0, 256),
+    ([1] * 37, 1, 8, 8, 128, 1, 16),
+    ([0, 100] * 37, 1, 32, 8, 128, 100, 32),
+    ([64 * i + i % 3 for i in range(9)], 2, 8, 1, 64, 64, 128),
+    ([65] * 4, 3, 15, 3, 128, 127, 64),
+]
+
+
+@pytest.mark.parametrize("case", range(len(SMALL)))
+@pytest.mark.parametrize("layout", ["plain", "strided"])
+def test_small_problems(B, case, layout):
+    lens, T, Hq, Hkv, D, P, page = SMALL[case]
+    kw = dict(shared_buffer=True, pitch=2 * Hkv * D, extra=3) if layout == "strided" else {}
+    x = Batch(B, lens, T, Hq, Hkv, D, P, page, seed=case, **kw)
+    o, l = x.run(B)
+    x.check(o, l)
+    o2, _ = x.run(B, lse=False)
+    assert torch.equal(o, o2), "equal calls give equal bits"
+
+
 def test_result_pitch_scale_and_peaked_scores(B):
     """A strided result leaves its gaps alone; a scale of one's own; scores far apart (the maximum moves and parts differ by
     hundreds of powers of two)."""

@@ -28,10 +28,12 @@ def test_offsets_beyond_32_bits(B):
         assert torch.equal(k[p], x[p * page : (p + 1) * page, Hkv : 2 * Hkv].transpose(0, 1))
         assert torch.equal(v[p], x[p * page : (p + 1) * page, 2 * Hkv :].transpose(0, 1))
     assert torch.equal(q, x[:, :Hkv])
-    # attention: prefix in the last two pages, own keys in the first ones; one row (decode kernel) and 33 (block kernel)
+    # attention: prefix in the last two pages, own keys in the first ones; tables as wide as needed (one launch for all)
+    # and wider (one row: decode kernel; 33: block kernel)
     prefix = torch.tensor([pages - 1, pages - 2], dtype=torch.int32, device="cuda")
-    for n in (1, 33):
-        table = torch.arange(2, dtype=torch.int32, device="cuda").repeat(n, 1)
+    for n, width in ((1, 2), (33, 2), (1, 10000), (33, 10000)):
+        table = torch.full((n, width), -1, dtype=torch.int32, device="cuda")
+        table[:, :2] = torch.arange(2, dtype=torch.int32, device="cuda")
         lens = torch.full((n,), 20, dtype=torch.int32, device="cuda")
         qq = x[:n, :Hkv].contiguous()
         o = B.patch_prefix_attention(cache, qq, prefix, 30, table, lens)
@@ -58,13 +60,15 @@ def test_largest_batch(B):
 
 
 @pytest.mark.parametrize("shape", [(1, 4, 4, 0), (1, 4, 4, 300), (40, 4, 1, 300)])
-def test_a_wait_that_runs_out_is_reported_and_survivable(B, shape):
-    """A CTA of the call's first kernel (the decode kernel; the block kernel for the 160 rows of the last shape) waits for bytes that
-    never come: it gives up, the launch completes with PATCH_ERR_TIMEOUT, the next call is right."""
+@pytest.mark.parametrize("extra", [0, 10000])
+def test_a_wait_that_runs_out_is_reported_and_survivable(B, shape, extra):
+    """A CTA of the call's first kernel (the kernel of small problems; with wide tables the decode kernel, or the block kernel for the
+    160 rows of the last shape) waits for bytes that never come: it gives up, the launch completes with PATCH_ERR_TIMEOUT, the next
+    call is right."""
     from paper_2509_23410_b200 import build
     n, Hq, Hkv, P = shape
     fi = B.load(build.build(fault_injection=True))
-    x = Batch(B, [70] * n, 1, Hq, Hkv, 128, P, 16, seed=5)
+    x = Batch(B, [70] * n, 1, Hq, Hkv, 128, P, 16, seed=5, extra=extra)
     want, _ = x.run(B)
     ws = torch.full((B.patch_prefix_attention_workspace_size(x.cache, n, 1, Hq),), 0xFF, dtype=torch.uint8, device="cuda")
     o = torch.zeros_like(want)
