@@ -229,8 +229,8 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
                         {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s, q.block_s}};
     const bool prefix = prefix_len > 0;
     auto tiles = [&](int keys) { return int((prefix_len + keys - 1) / keys); };
-    const Line dec = {prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : q.blocks_s, tiles(kDecodeKeys), kDecodeCost};
-    const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, tiles(kBlockKeys), kBlockCost};
+    const Line dec = {prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : q.blocks_s, tiles(kDecodeKeys), kDecodeCost, 6};
+    const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, tiles(kBlockKeys), kBlockCost, 7};
     // units are counted in 32 bits
     const int64_t own = (ld_table * cache->page_size + kDecodeKeys - 1) / kDecodeKeys + 8;
     if (int64_t(cache->Hkv) * q.blocks_p * (int64_t(dec.tiles_p) + 8) + B * own * cache->Hkv * q.blocks_s > 0x7FFFFFFF)

@@ -177,7 +177,7 @@ __device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w
 }
 }  // namespace blk
 
-template <int D>
+template <int D, bool STEPS>
 __global__ void __launch_bounds__(blk::kThreads, 1)
 attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const Line w,
                   const Results to, const blk::Room room, const bool share_gpu) {
@@ -209,7 +209,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         tma_prefetch_map(&map_v);
     }
     if (warp == 0) {
-        const float keys = float(lay_out(p, w, kKeys, cum, lens));
+        const float keys = float(lay_out<STEPS>(p, w, cum, lens));
         if (lane == 0) *own_keys = keys;
     }
     if (warp == 2) tmem_alloc(smem_u32(misc), kTmemCols);
@@ -234,7 +234,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     };
     const bool busy = int(blockIdx.x) < ctas;
     const int u0 = busy ? start_of(blockIdx.x) : 0, u1 = busy ? start_of(blockIdx.x + 1) : 0;
-    Share s(p, line, cum, lens);
+    Share<STEPS> s(p, line, cum, lens);
 
     if (warp == 0) {
         // ---------------- producer: K0 K1, then V0 K2 V1 K3 ... as they are consumed ----------------
@@ -515,14 +515,14 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (warp == 2) tmem_dealloc(tmem, blk::kTmemCols);
 }
 
-template <int D>
+template <int D, bool STEPS>
 static int launch_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool share_gpu, cudaStream_t stream) {
     CUtensorMap mk, mv;
     const int rows = c->page_size < blk::kKeys ? c->page_size : blk::kKeys;
     int rc = make_kv_tensor_map(&mk, c, c->k_dev, rows, 1);
     if (!rc) rc = make_kv_tensor_map(&mv, c, c->v_dev, rows, 1);
     if (rc) return rc;
-    auto kern = attn_block_kernel<D>;
+    auto kern = attn_block_kernel<D, STEPS>;
     static std::atomic<uint64_t> configured{0};
     if ((rc = allow_dynamic_smem(kern, 227 * 1024, configured))) return rc;
     const blk::Room room = blk::room_of<D>(w, p.B);
@@ -533,7 +533,9 @@ static int launch_block(const patch_kv_cache_t* c, const Problem& p, const Line&
 }
 
 int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool decode_follows, cudaStream_t s) {
-    return c->D == 128 ? launch_block<128>(c, p, w, to, decode_follows, s) : launch_block<64>(c, p, w, to, decode_follows, s);
+    if (w.blocks_s && p.T > kMostLevelTokens)
+        return c->D == 128 ? launch_block<128, true>(c, p, w, to, decode_follows, s) : launch_block<64, true>(c, p, w, to, decode_follows, s);
+    return c->D == 128 ? launch_block<128, false>(c, p, w, to, decode_follows, s) : launch_block<64, false>(c, p, w, to, decode_follows, s);
 }
 
 }  // namespace attn

@@ -228,7 +228,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         tma_prefetch_map(&map_k);
         tma_prefetch_map(&map_v);
     }
-    if (warp == 0) lay_out(p, w, kKeys, cum, lens);
+    if (warp == 0) lay_out<false>(p, w, cum, lens);
     else if (warp < kWarps) prefetch_lists(p, w, 32 * (kWarps - 1), threadIdx.x - 32);
     __syncthreads();
     const int total = total_units(w, p, cum);
@@ -264,8 +264,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         constexpr uint32_t inject = 0u;
 #endif
         // this lane's page number of an item: entry page0 + lane of its list
-        auto fetch = [&](const Share& s, int page0) { return page0 + lane < s.pages() ? s.list()[page0 + lane] : 0; };
-        Share s(p, w, cum, lens), ahead(s);
+        auto fetch = [&](const Share<false>& s, int page0) { return page0 + lane < s.pages() ? s.list()[page0 + lane] : 0; };
+        Share<false> s(p, w, cum, lens), ahead(s);
         bool have = s.start(share_start(total, blockIdx.x, ctas, ctas == gridDim.x ? turns : 0.0),
                             share_start(total, blockIdx.x + 1, ctas, ctas == gridDim.x ? turns : 0.0));
         int page0 = have ? int((int64_t(s.t0) * kKeys) >> p.shift) : 0;

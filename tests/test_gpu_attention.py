@@ -171,6 +171,25 @@ def test_small_problems(B, case, layout):
     assert torch.equal(o, o2), "equal calls give equal bits"
 
 
+PROMPTS = [  # many tokens a sequence: row blocks that see different numbers of tiles
+    ([513], 513, 4, 1, 64, 0, 32),
+    ([600, 65, 0, 10], 530, 4, 2, 128, 70, 16),            # more tokens than keys: the first ones see nothing
+    ([1500, 640, 639], 640, 3, 1, 128, 200, 64),           # blocks of 128 rows that begin within a token
+    ([257] * 5, 65, 16, 2, 128, 0, 128),
+    ([600, 1, 128, 127], 520, 3, 3, 64, 129, 16),
+]
+
+
+@pytest.mark.parametrize("case", range(len(PROMPTS)))
+def test_prompts(B, case):
+    lens, T, Hq, Hkv, D, P, page = PROMPTS[case]
+    x = Batch(B, lens, T, Hq, Hkv, D, P, page, seed=case)
+    o, l = x.run(B)
+    x.check(o, l)
+    o2, _ = x.run(B, lse=False)
+    assert torch.equal(o, o2), "equal calls give equal bits"
+
+
 def test_result_pitch_scale_and_peaked_scores(B):
     """A strided result leaves its gaps alone; a scale of one's own; scores far apart (the maximum moves and parts differ by
     hundreds of powers of two)."""
