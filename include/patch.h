@@ -579,8 +579,8 @@ int patch_kv_append(const patch_kv_cache_t* cache, const void* K_dev, int64_t ld
  *     query token t sees the whole prefix and the first max(0, suffix_lens[b] - (T - 1 - t)) of the own keys;
  *     O = softmax(scale q k^T) v over what it sees,  lse = ln sum exp(scale q k^T);  nothing seen: O = 0, lse = -inf.
  * Query head h reads key head h / (Hq / Hkv).  The prefix is read once for all sequences (the batch's rows of one key
- * head are one operand), and no key or value past a length is used, whatever the cache holds there; keys and values that some query token of a
- * sequence sees are assumed finite.
+ * head are one operand; only problems of a few microseconds read it for each, from L2), and no key or value past a length is
+ * used, whatever the cache holds there; keys and values that some query token of a sequence sees are assumed finite.
  *   cache             D = 64 or 128
  *   Q_dev, O_dev      [B T x Hq heads of D], pitches ldq, ldo;  Hq a multiple of the cache's Hkv
  *   prefix_pages_dev  int32 [ceil(prefix_len / page_size)] pages of the prefix, in order (NULL if prefix_len is 0)

@@ -2,7 +2,8 @@
 
 Argument marshalling only: every step of the path (mask selection, packing, the matmul, its
 split-K reduction and the bf16 epilogue) runs in the CUDA library.  There is no CPU fallback:
-if ``libpatch_b200.so`` is missing this module raises on first use.
+if ``libpatch_b200.so`` is missing this module raises on first use.  The calls between the linear layers (a few
+microseconds of kernel) hand their tensors to the CPython module ``_marshal``, which calls the same C entry points.
 
 Tensors are torch CUDA tensors used purely as device buffers (``data_ptr()``); weights,
 activations and results are ``torch.bfloat16``; packed blobs and workspaces are ``torch.uint8``.

@@ -1,6 +1,6 @@
-// Attention over the paged cache for items of more than 32 query rows: the batch's rows of one key head against the shared prefix,
-// or the drafted tokens of one sequence against its own keys (public header: patch_prefix_attention; the work list and the partial
-// results are described in attention.cuh).
+// Attention over the paged cache for items of more than 16 query rows: the batch's rows of one key head against the shared prefix,
+// or a sequence's many tokens (a prompt, drafted tokens) against its own keys (the rule is in attention.cu; public header:
+// patch_prefix_attention; the work list and the partial results are described in attention.cuh).
 //
 // Mathematics.  As in the decode kernel: running maximum m, sum l and unnormalised output o of every row, fp32, scores in powers of
 // two.  Any m serves as long as nothing overflows, so it is the maximum of the row's first tile and is raised only when a tile's
@@ -20,8 +20,9 @@
 //   warps 4..7   softmax of stream 0, one thread per row; warps 8..11 stream 1.  They also bring an item's query rows into the
 //                swizzled layout (any head count per key head, any row pitch) and write its partial result, half of the columns each.
 // What bounds it: a tile's 64 KB of keys and values take an SM 2 850 cycles of HBM, its two products 1 024 and its exponentials 1 024,
-// but a stream's tile is a chain -- scores, softmax, products -- of 4 000 cycles, so two streams need 2 000 a tile: HBM bounds one block of
-// 128 rows, the chain more of them.
+// but a stream's tile is a chain -- scores, softmax, products -- of 4 000 to 5 000 cycles, so two streams need 2 000 to 2 500 a tile: HBM
+// bounds one block of 128 rows, the chain more of them.  An item costs 7 000 cycles before its first scores and 4 200 for its result
+// (24 items of 320 rows and 4093 keys: 17 us).
 // Tried: tiles of 64 keys with two score buffers per stream, so that no stream waits for its own products: 5 600 cycles per 128
 // keys and two streams -- twice the MMAs of the scores and twice the waits, and the warp that issues them became the bottleneck.
 #include "attention.cuh"
@@ -165,7 +166,7 @@ __device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool part
 // kernel ends with the decode kernel, which streams from the other SMs meanwhile -- one is short of arithmetic, the other of
 // bandwidth.  Cycles measured: 2 000 for a tile, 3 300 where HBM is waited for (one block of rows),
 // 700 for a tile of the decode kernel (two CTAs share its latencies); bandwidth in bytes per cycle of 6.5 TB/s at 1.9 GHz.  64
-// sequences behind 32768 keys: 82 us against 101 with the block kernel on all SMs first.
+// sequences behind 32768 keys (8 key heads): 80 us against 101 with the block kernel on all SMs first.
 template <int D>
 __device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w, float keys, int sms) {
     const float heads = float(p.Hkv);

@@ -1,20 +1,21 @@
-// Attention over the paged cache for items of few query rows, taken in blocks of at most 16 (public header: patch_prefix_attention; the work list and the
-// partial results are described in attention.cuh).
+// Attention over the paged cache for items of few query rows, taken in blocks of at most 16, and for small problems in one launch
+// (public header: patch_prefix_attention; the work list and the partial results are described in attention.cuh).
 //
 // Mathematics.  For every row the running maximum m of the scaled scores (in powers of two), the sum l of 2^(s - m) and the
 // unnormalised output o = sum 2^(s - m) v; parts of the keys are joined with weights 2^(m_i - m).  All three are fp32; the
 // probabilities are rounded to bf16 for the product with V (they are at most 1; the sum takes them unrounded).
 //
-// Kernel.  One CTA per SM walks over its share of the work list (attention.cuh).  Warp 4 alone knows the list: it requests tiles
+// Kernel.  Every CTA, two to an SM, walks over its share of the work list (attention.cuh).  Warp 4 alone knows the list: it requests tiles
 // of 64 keys and values with TMA, one copy per page and operand, into a ring of stages, and with an item's first tile the
 // item's query rows; a note in the stage says what the tile is.  Warps 0..3 each take 16 of the 64 keys: S = Q K^T
 // (16 rows x 16 keys), probabilities in registers, O += P V, with a maximum of their own, so that within an item no warp waits
-// for another.  At the end of a share the four warps' results are joined in shared memory.  Two CTAs share an SM, so that one
-// streams while the other hands an item over.
+// for another.  At the end of a share the four warps' results are joined in shared memory, while the SM's other CTA
+// streams.
 // What bounds it: HBM.  A 64-key tile is 32 KB (D = 128), about 1 430 cycles of an SM's share of the bandwidth; its
 // 32 + 32 products of 16 x 8 x 16 per warp and the softmax of 16 x 16 scores take half of that.  Batches with many short
 // items live off the hand-over between items: with every warp looking its items up and fetching their queries itself, an
-// item cost about 1.5 us on top of its tiles (16 sequences of up to 1024 keys, 32 heads: 59 us against a floor of 27).
+// item cost about 1.5 us on top of its tiles (16 sequences of up to 1024 keys behind 2048, 32 heads: 59 us against a floor of
+// 27; now 34: 28 in this kernel, 6 from its end to the joining kernel's).
 #include "attention.cuh"
 
 namespace patch {
