@@ -117,12 +117,20 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
 // host side
 
 // Which kernel serves a phase.  The prefix: the decode kernel where its 16 rows of mma.sync hold all rows (HBM is what it waits
-// for), else the block kernel (two blocks on the decode kernel would read the prefix twice; one CTA holding both took 112 us against
-// 77 for 32 rows and 8192 keys of the 13B shape).  A sequence's own keys, where its T G rows are more than 16: items are short, and
-// an item costs the block kernel about 7 us (queries, first tile, result), so where page tables end at 1024 keys up to four blocks of 16
-// rows stay on the decode kernel, with the keys from L2 from the second block on.  Measured, 16 sequences, 28 rows, 8 key heads:
-// 200 keys 13.6 us there against 17.3, 800 keys 21.6 against 28.0, 4096 keys 85.4 against 52.8.
+// for).  More rows are more blocks there, all of which read the keys (from L2 but for the first), so that is for work so small that it
+// ends before the block kernel, whose chain of queries, tiles and result takes 12 us at least, would: up to 4000 tiles of 64 keys and
+// 16 rows.  Measured, decode kernel against block kernel: 16 sequences, 40 heads of 7 rows, 4 + 900 keys 56 us against 62; 7
+// sequences, 40 heads of 4 rows, 1454 + 10 keys 16.7 against 22.0 (1 920 tiles); 19 sequences, 8 heads of 16 rows, 929 + 40 keys 17.7
+// against 20.6 (2 432); 29 sequences, 8 heads of 4 rows, 4478 + 500 keys 28.9 against 27.6 (4 544).  A sequence's own keys, where its
+// T G rows are more than 16: items are short, and an item costs the block kernel about 6 us (queries, first tile, result), so where page
+// tables end at 1024 keys up to four blocks of 16 rows stay on the decode kernel, with the keys from L2 from the second block on.
+// Measured, 16 sequences, 28 rows, 8 key heads: 200 keys 13.6 us there against 17.3, 800 keys 21.6 against 28.0, 4096 keys 85.4
+// against 52.8.  Where suffixes go to the block kernel the prefix does too, so that there is one kernel less.
+constexpr int64_t kMostPrefixUnits = 4000;
 constexpr int kMostDecodeRows = 64, kMostDecodeKeys = 1024;
+static bool block_prefix(int64_t rows, int64_t Hkv, int64_t prefix_len) {
+    return rows > kDecodeRows && (rows + kDecodeRows - 1) / kDecodeRows * Hkv * ((prefix_len + kDecodeKeys - 1) / kDecodeKeys + kDecodeCost) > kMostPrefixUnits;
+}
 static bool block_suffixes(int64_t rows, int64_t keys) { return rows > kMostDecodeRows || (rows > kDecodeRows && keys > kMostDecodeKeys); }
 
 // CTAs of a cluster for each item of the small problems that take one launch of their own (attn_direct_kernel), 0 for the others.
@@ -133,9 +141,10 @@ static bool block_suffixes(int64_t rows, int64_t keys) { return rows > kMostDeco
 // is worth it only where a prefix would be a launch of its own: 2 items a slot 14.6 us against 32.8 with one, 3 items a slot without 14.1
 // against 12.2.  Clusters of 16 (more than the portable 8) pay from four tiles a CTA: 71 tiles an item 10.4 us against 11.4, 16
 // tiles 7.7 against 6.8.
-static int direct_split(int64_t rows, int64_t items, int64_t prefix_len, int64_t table_keys) {
-    const int64_t slots = 2 * sm_count(), tiles = (prefix_len + kDecodeKeys - 1) / kDecodeKeys + (table_keys + kDecodeKeys - 1) / kDecodeKeys;
-    if (rows > kDecodeRows || tiles > 8 * slots || items * tiles > 8 * slots || items > (prefix_len ? 2 : 1) * slots) return 0;
+static int direct_split(int64_t rows, int64_t heads, int64_t prefix_len, int64_t table_keys) {
+    const int64_t slots = 2 * sm_count(), items = heads * ((rows + kDecodeRows - 1) / kDecodeRows);
+    const int64_t tiles = (prefix_len + kDecodeKeys - 1) / kDecodeKeys + (table_keys + kDecodeKeys - 1) / kDecodeKeys;
+    if (tiles > 8 * slots || items * tiles > 8 * slots || items > (prefix_len ? 2 : 1) * slots) return 0;
     int split = 1;                                   // all CTAs at once, and each with a tile at least
     while (split < 16 && 2 * split * items <= slots && tiles >= (split < 8 ? 2 * split : 64)) split *= 2;
     return split;
@@ -146,7 +155,7 @@ struct Plan {
     int blocks_p, blocks_s, rows_p, rows_s;          // row blocks per key head, rows of a slot
     size_t span_s, ml_p, ml_s, o_p, o_s, bytes;      // workspace: [spans of prefix items | of suffix items | (m, l) | outputs]
 };
-static Plan plan_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G, int64_t table_keys) {
+static Plan plan_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G, int64_t prefix_len, int64_t table_keys) {
     Plan q;
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     auto rows = [&](int64_t all, bool block, int& blocks) {
@@ -154,8 +163,8 @@ static Plan plan_of(const patch_kv_cache_t* c, int64_t B, int64_t T, int64_t G, 
         blocks = int((all + most - 1) / most);
         return int(all < most ? all : most);
     };
-    q.block_p = B * T * G > kDecodeRows;
     q.block_s = block_suffixes(T * G, table_keys);
+    q.block_p = q.block_s ? B * T * G > kDecodeRows : block_prefix(B * T * G, c->Hkv, prefix_len);
     q.rows_p = rows(B * T * G, q.block_p, q.blocks_p);
     q.rows_s = rows(T * G, q.block_s, q.blocks_s);
     // a slot for every item and every CTA that may share one
@@ -188,10 +197,14 @@ extern "C" int patch_prefix_attention_workspace_size(const patch_kv_cache_t* cac
     if (!bytes_out) return PATCH_ERR_NULL;
     int rc = attn::check_batch(cache, B, T, Hq);
     if (rc) return rc;
-    // whatever the tables' width will be
+    // whatever the prefix's length and the tables' width will be
     const int64_t G = Hq / cache->Hkv;
-    const size_t few = attn::plan_of(cache, B, T, G, 0).bytes, many = attn::plan_of(cache, B, T, G, int64_t(1) << 40).bytes;
-    *bytes_out = few > many ? few : many;
+    *bytes_out = 0;
+    for (int64_t prefix : {int64_t(0), int64_t(1) << 30})
+        for (int64_t keys : {int64_t(0), int64_t(1) << 40}) {
+            const size_t n = attn::plan_of(cache, B, T, G, prefix, keys).bytes;
+            if (n > *bytes_out) *bytes_out = n;
+        }
     return PATCH_OK;
 }
 
@@ -224,12 +237,12 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     if (const int split = direct_split(int64_t(T) * G, B * cache->Hkv, prefix_len, ld_table * cache->page_size))
         return launch_attn_direct(cache, p, split, static_cast<__nv_bfloat16*>(O), ldo, lse, s);
-    const Plan q = plan_of(cache, B, T, G, ld_table * cache->page_size);
+    const Plan q = plan_of(cache, B, T, G, prefix_len, ld_table * cache->page_size);
     const Results to = {{reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float2*>(ws + q.ml_p), reinterpret_cast<int2*>(ws), q.rows_p, q.block_p},
                         {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s, q.block_s}};
     const bool prefix = prefix_len > 0;
     auto tiles = [&](int keys) { return int((prefix_len + keys - 1) / keys); };
-    const Line dec = {prefix && !q.block_p ? 1 : 0, q.block_s ? 0 : q.blocks_s, tiles(kDecodeKeys), kDecodeCost, 6};
+    const Line dec = {prefix && !q.block_p ? q.blocks_p : 0, q.block_s ? 0 : q.blocks_s, tiles(kDecodeKeys), kDecodeCost, 6};
     const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, tiles(kBlockKeys), kBlockCost, 7};
     // units are counted in 32 bits
     const int64_t own = (ld_table * cache->page_size + kDecodeKeys - 1) / kDecodeKeys + 8;

@@ -164,13 +164,14 @@ __device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool part
 // How many SMs the block kernel takes where the decode kernel has the suffixes.  Together they are done no sooner than HBM has
 // delivered the keys and values and the SMs have done their cycles; with as many SMs as its own cycles need in that time, the block
 // kernel ends with the decode kernel, which streams from the other SMs meanwhile -- one is short of arithmetic, the other of
-// bandwidth.  Cycles measured: 2 000 for a tile, 3 300 where HBM is waited for (one block of rows),
+// bandwidth.  Cycles measured: 2 000 for a tile, 3 300 where HBM is waited for (one block of rows), 11 000 for an
+// item's queries and result (left out, 16 sequences of 40 heads behind 4 keys took 167 us instead of 62: forty items on four SMs),
 // 700 for a tile of the decode kernel (two CTAs share its latencies); bandwidth in bytes per cycle of 6.5 TB/s at 1.9 GHz.  64
 // sequences behind 32768 keys (8 key heads): 80 us against 101 with the block kernel on all SMs first.
 template <int D>
 __device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w, float keys, int sms) {
     const float heads = float(p.Hkv);
-    const float mine = heads * w.tiles_p * (w.blocks_p == 1 ? 3300.0f : 2000.0f * w.blocks_p);
+    const float mine = heads * (w.tiles_p * (w.blocks_p == 1 ? 3300.0f : 2000.0f * w.blocks_p) + 11000.0f * w.blocks_p);
     const float theirs = heads * keys / kDecodeKeys * 700.0f;
     const float bytes = heads * (keys + float(p.prefix_len)) * D * 4.0f;
     const float time = fmaxf(bytes / 3420.0f, (mine + theirs) / sms);

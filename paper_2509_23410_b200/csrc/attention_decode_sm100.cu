@@ -377,8 +377,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (failed) barrier_any(true, 1, 32 * kWarps);
 }
 
-// Small problems, in one launch and without partial results in memory: a cluster of CTAs owns one sequence's rows of a key head, its
-// CTAs take equal parts of the tiles of the prefix and of the sequence's own keys, and join in distributed shared memory.  The
+// Small problems, in one launch and without partial results in memory: a cluster of CTAs owns a block of one sequence's rows of a key
+// head, its CTAs take equal parts of the tiles of the prefix and of the sequence's own keys, and join in distributed shared memory.  The
 // prefix is read by every sequence (from L2 after the first), which is cheap as long as all there is to read is a few tiles per CTA:
 // one sequence behind 128 keys of the 7B shape 8.3 us -> 5.1.  What is left is one chain: barriers, page numbers, a tile from HBM, its products, two joins.
 template <int D>
@@ -393,7 +393,9 @@ attn_direct_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kBarOffset + 16 * kStages);
     Note* notes = reinterpret_cast<Note*>(smem + C::kNoteOffset);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int item = blockIdx.x / split, rank = int(cluster_ctarank()), b = item / p.Hkv, kvh = item - b * p.Hkv, rows_n = p.T * p.G;
+    const int item = blockIdx.x / split, rank = int(cluster_ctarank()), blocks = (p.T * p.G + kRows - 1) / kRows;
+    const int b = item / (p.Hkv * blocks), head_block = item - b * p.Hkv * blocks, kvh = head_block / blocks, row0 = (head_block - kvh * blocks) * kRows;
+    const int rows_n = min(kRows, p.T * p.G - row0);
     const int rows_log2 = p.shift < 6 ? p.shift : 6;
     const uint32_t copy_bytes = uint32_t(D * 2) << rows_log2;
 
@@ -446,8 +448,8 @@ attn_direct_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             __syncwarp();
             if (on) tma_load_page(dst, lane & 1 ? &map_v : &map_k, p.shift < 6 ? 0 : int(key0 & ((1 << p.shift) - 1)), 0, kvh, page, full, policy);
             if (opens && lane >= 16 && lane - 16 < rows_n) {
-                const int r = lane - 16, t = p.token(r);
-                tma_bulk_load(base + C::kQOffset + stage * C::kQBytes + r * C::kQPitch,
+                const int r = row0 + lane - 16, t = p.token(r);
+                tma_bulk_load(base + C::kQOffset + stage * C::kQBytes + (lane - 16) * C::kQPitch,
                               p.Q + (int64_t(b) * p.T + t) * p.ldq + int64_t(kvh * p.G + r - t * p.G) * D, D * 2, full, policy);
             }
             if (lane == 0) {
@@ -480,7 +482,7 @@ attn_direct_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             const Note n = notes[stage];
             if (n.flags & kEnd) break;
             if (n.flags & kFirst) rows.queries(base + C::kQOffset + stage * C::kQBytes, lane);
-            if (n.flags & kTurns) rows.sees(p, 0, n.keys, n.flags & kOwn);
+            if (n.flags & kTurns) rows.sees(p, row0, n.keys, n.flags & kOwn);
             rows.tile(base + stage * C::kStageBytes, n.key0, n.keys, p.scale_log2);
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_empty + 8 * stage);
@@ -518,7 +520,7 @@ attn_direct_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 m = mx;
             }
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;       // nothing seen: 0
-            const int t = p.token(r), head = kvh * p.G + r - t * p.G;
+            const int t = p.token(row0 + r), head = kvh * p.G + row0 + r - t * p.G;
             const int64_t tok = int64_t(b) * p.T + t;
             *reinterpret_cast<uint2*>(O + tok * ldo + int64_t(head) * D + 4 * c) = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
             if (lse && c == 0) lse[tok * (p.Hkv * p.G) + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
@@ -543,7 +545,7 @@ static int launch_direct(const patch_kv_cache_t* c, const Problem& p, int split,
     if ((rc = allow_dynamic_smem(kern, Cfg<D>::kFixedBytes, configured))) return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
-    cfg.gridDim = dim3(unsigned(p.B * p.Hkv * split), 1, 1);
+    cfg.gridDim = dim3(unsigned(p.B * p.Hkv * ((p.T * p.G + kRows - 1) / kRows) * split), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = Cfg<D>::kFixedBytes;
     cfg.stream = stream;

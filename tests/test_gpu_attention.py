@@ -148,6 +148,25 @@ def test_behind_wide_tables(B, case):
     assert torch.equal(o, o2), "equal calls give equal bits"
 
 
+LONG = [  # prefixes whose rows and keys are the block kernel's
+    ([5] * 33, 1, 8, 2, 128, 20000, 16),
+    ([1 + 37 * i % 301 for i in range(64)], 1, 4, 1, 128, 17001, 16),
+    ([129] * 40, 1, 8, 1, 64, 16000, 64),
+    ([300, 2, 31, 33] * 4, 3, 12, 4, 64, 9000, 256),
+    ([0] * 300, 1, 4, 4, 64, 13000, 16),
+]
+
+
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_long_prefixes(B, case):
+    lens, T, Hq, Hkv, D, P, page = LONG[case]
+    x = Batch(B, lens, T, Hq, Hkv, D, P, page, seed=case)
+    o, l = x.run(B)
+    x.check(o, l)
+    o2, _ = x.run(B, lse=False)
+    assert torch.equal(o, o2), "equal calls give equal bits"
+
+
 SMALL = [  # lens, T, Hq, Hkv, D, P, page: from one CTA to sixteen an item, items beyond the CTAs that run at once
     ([8000], 1, 8, 1, 128, 0, 16),
     ([500], 1, 16, 2, 128, 4000, 64),
@@ -156,6 +175,8 @@ SMALL = [  # lens, T, Hq, Hkv, D, P, page: from one CTA to sixteen an item, item
     ([0, 100] * 37, 1, 32, 8, 128, 100, 32),
     ([64 * i + i % 3 for i in range(9)], 2, 8, 1, 64, 64, 128),
     ([65] * 4, 3, 15, 3, 128, 127, 64),
+    ([40, 700], 7, 16, 2, 128, 300, 16),                   # 56 rows: four blocks of them
+    ([90], 64, 3, 3, 64, 5, 32),
 ]
 
 

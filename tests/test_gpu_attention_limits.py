@@ -28,16 +28,17 @@ def test_offsets_beyond_32_bits(B):
         assert torch.equal(k[p], x[p * page : (p + 1) * page, Hkv : 2 * Hkv].transpose(0, 1))
         assert torch.equal(v[p], x[p * page : (p + 1) * page, 2 * Hkv :].transpose(0, 1))
     assert torch.equal(q, x[:, :Hkv])
-    # attention: prefix in the last two pages, own keys in the first ones; tables as wide as needed (one launch for all)
-    # and wider (one row: decode kernel; 33: block kernel)
-    prefix = torch.tensor([pages - 1, pages - 2], dtype=torch.int32, device="cuda")
-    for n, width in ((1, 2), (33, 2), (1, 10000), (33, 10000)):
+    # attention: prefix in the last two pages (again and again), own keys in the first ones; tables as wide as needed (one launch for all)
+    # and wider (decode kernel; block kernel for the long prefix)
+    for n, width, times in ((1, 2, 1), (33, 2, 1), (1, 10000, 1), (33, 10000, 1), (33, 2, 1400)):
+        prefix = torch.tensor([pages - 1, pages - 2] * times, dtype=torch.int32, device="cuda")
+        P = 2 * page * times - 2
         table = torch.full((n, width), -1, dtype=torch.int32, device="cuda")
         table[:, :2] = torch.arange(2, dtype=torch.int32, device="cuda")
         lens = torch.full((n,), 20, dtype=torch.int32, device="cuda")
         qq = x[:n, :Hkv].contiguous()
-        o = B.patch_prefix_attention(cache, qq, prefix, 30, table, lens)
-        order = torch.cat((slots[(pages - 1) * page :], slots[(pages - 2) * page : (pages - 2) * page + 14], slots[:20]))
+        o = B.patch_prefix_attention(cache, qq, prefix, P, table, lens)
+        order = torch.cat((torch.cat((slots[(pages - 1) * page :], slots[(pages - 2) * page : (pages - 1) * page])).repeat(times)[:P], slots[:20]))
         kk, vv = x[order, Hkv : 2 * Hkv].double().transpose(0, 1), x[order, 2 * Hkv :].double().transpose(0, 1)
         p = torch.softmax(torch.einsum("bhd,hnd->bhn", qq.double(), kk) * D ** -0.5, -1)
         ref, size = torch.einsum("bhn,hnd->bhd", p, vv), torch.einsum("bhn,hnd->bhd", p, vv.abs())
@@ -59,11 +60,11 @@ def test_largest_batch(B):
         assert bool(((o[b].double() - ref).abs() <= ref.abs() * 2.0 ** -8 * 1.01 + size * (2.0 ** -8 + 2.0 ** -12)).all()), b
 
 
-@pytest.mark.parametrize("shape", [(1, 4, 4, 0), (1, 4, 4, 300), (40, 4, 1, 300)])
+@pytest.mark.parametrize("shape", [(1, 4, 4, 0), (1, 4, 4, 300), (40, 4, 1, 26000)])
 @pytest.mark.parametrize("extra", [0, 10000])
 def test_a_wait_that_runs_out_is_reported_and_survivable(B, shape, extra):
-    """A CTA of the call's first kernel (the kernel of small problems; with wide tables the decode kernel, or the block kernel for the
-    160 rows of the last shape) waits for bytes that never come: it gives up, the launch completes with PATCH_ERR_TIMEOUT, the next
+    """A CTA of the call's first kernel (the kernel of small problems; with wide tables the decode kernel; the block kernel for the 160
+    rows of the last shape) waits for bytes that never come: it gives up, the launch completes with PATCH_ERR_TIMEOUT, the next
     call is right."""
     from paper_2509_23410_b200 import build
     n, Hq, Hkv, P = shape
