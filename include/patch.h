@@ -592,7 +592,7 @@ int patch_kv_append(const patch_kv_cache_t* cache, const void* K_dev, int64_t ld
  *                     aligned, no initialisation needed
  *   status_dev        PATCH_ERR_SIZE: a length outside its range (clamped); PATCH_ERR_FORMAT: a page outside the cache (page 0
  *                     is read in its place); PATCH_ERR_TIMEOUT: a bounded wait expired.  O is undefined in the last two.
- * B <= 2048, B T Hq D < 2^31, scale > 0.  Fixed lengths give fixed bits.  At most three launches, no host synchronisation.
+ * B <= 2048, B T Hq D < 2^31, 0 < scale <= 2e38 (scale log2(e) is an fp32 number).  Finite scores q.k may have any size.  Fixed lengths give fixed bits.  At most three launches, no host synchronisation.
  */
 int patch_prefix_attention_workspace_size(const patch_kv_cache_t* cache, int64_t B, int T, int Hq, size_t* bytes_out);
 int patch_prefix_attention(const patch_kv_cache_t* cache, const void* Q_dev, int64_t ldq, int64_t B, int T, int Hq,

@@ -2,8 +2,8 @@
 // header: patch_prefix_attention; kernels: attention_decode_sm100.cu, attention_block_sm100.cu; work list: attention.cuh).
 //
 // The batch's query rows of one key head are one operand against the shared prefix (B T G rows), a sequence's rows (T G) one
-// against its own keys.  Softmax parts over disjoint keys join exactly: with m = max m_i, o = sum 2^(m_i - m) o_i and
-// l = sum 2^(m_i - m) l_i, the result is o / l.
+// against its own keys.  Softmax parts over disjoint keys join exactly: with m = max m_i and w_i = 2^((m_i - m) scale),
+// o = sum w_i o_i and l = sum w_i l_i, the result is o / l.
 #include "attention.cuh"
 
 namespace patch {
@@ -83,7 +83,7 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
         if (mx == -INFINITY) continue;
-        const float f = ex2(mine.x - mx), a = ex2(m - mx);
+        const float f = ex2(exponent(mine.x, mx, p.scale_log2)), a = ex2(exponent(m, mx, p.scale_log2));
         float add = mine.y * f;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, d);
@@ -110,7 +110,7 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
     __nv_bfloat16* dst = O + int64_t(tok) * ldo + int64_t(hq) * D + lane * V;
     if constexpr (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(acc[0] * inv, acc[1] * inv), pack2(acc[2] * inv, acc[3] * inv));
     else *reinterpret_cast<uint32_t*>(dst) = pack2(acc[0] * inv, acc[1] * inv);
-    if (lse && lane == 0) lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    if (lse && lane == 0) lse[row] = l == 0.0f ? -INFINITY : (m * p.scale_log2 + log2f(l)) * 0.6931471805599453f;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -215,7 +215,7 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     using namespace attn;
     int rc = check_batch(cache, B, T, Hq);
     if (rc) return rc;
-    if (prefix_len < 0 || prefix_len > 0x7FFFFF00 || ld_table < 0 || ld_table > 0x7FFFFFFF || !(scale > 0.0f) || scale > 3.0e38f) return PATCH_ERR_SHAPE;
+    if (prefix_len < 0 || prefix_len > 0x7FFFFF00 || ld_table < 0 || ld_table > 0x7FFFFFFF || !(scale > 0.0f) || scale > 2.0e38f) return PATCH_ERR_SHAPE;
     if (B == 0) return PATCH_OK;
     if (!Q || !O || !suffix_lens || (prefix_len && !prefix_pages) || (ld_table && !page_table)) return PATCH_ERR_NULL;
     const int D = cache->D;

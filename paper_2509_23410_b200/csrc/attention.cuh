@@ -10,6 +10,7 @@
 // results; the CTAs with an item's first and last tile note their numbers for the joining kernel.
 #pragma once
 #include "sm100_ptx.cuh"
+#include "softmax_rule.cuh"
 
 namespace patch {
 namespace attn {
@@ -27,7 +28,7 @@ struct Problem {
     int64_t ld_table;
     const int32_t* lens;
     int shift, num_pages;                     // log2(page_size)
-    float scale_log2;                         // scale * log2(e): scores are kept in powers of two
+    float scale_log2;                         // scale * log2(e): 2^(s scale_log2) = e^(s scale)
     int* status;
     uint32_t g_mul;                           // ceil(2^32 / G) where the product below is exact for every row, else 0
     // token of row r of a key head's rows; one multiplication instead of a division's thirty instructions
@@ -69,7 +70,7 @@ template <bool STEPS> __device__ __forceinline__ int head_units(const Problem& p
 // Where partial results go, of prefix items and of suffix items.
 struct Parts {
     float* o;                                 // [slot][rows][D], see `quarters`
-    float2* ml;                               // [slot][rows]: maximum (in powers of two), sum
+    float2* ml;                               // [slot][rows]: maximum of the scores (unscaled), sum
     int2* span;                               // [item]: first and last CTA with a share of it
     int rows;                                 // rows of a slot
     int quarters;                             // 0: rows of D; 1: by quarters of the columns, [slot][4][rows][D / 4], 16-byte chunk c of

@@ -2,14 +2,14 @@
 // or a sequence's many tokens (a prompt, drafted tokens) against its own keys (the rule is in attention.cu; public header:
 // patch_prefix_attention; the work list and the partial results are described in attention.cuh).
 //
-// Mathematics.  As in the decode kernel: running maximum m, sum l and unnormalised output o of every row, fp32, scores in powers of
-// two.  Any m serves as long as nothing overflows, so it is the maximum of the row's first tile and is raised only when a tile's
-// sum of 2^(s - m) passes 256: the sum is needed anyway, no maximum is taken of the other tiles, and the accumulator is rarely
+// Mathematics.  As in the decode kernel: running maximum m, sum l and unnormalised output o of every row, fp32, probabilities
+// 2^((s - m) scale).  Any m serves as long as nothing overflows, so it is the maximum of the row's first tile and is raised only when half
+// a tile's sum of probabilities passes 256: the sum is needed anyway, no maximum is taken of the other tiles, and the accumulator is rarely
 // rescaled.  (The relative rounding of the bf16 probabilities does not depend on their size.)
 //
 // Kernel.  One CTA per SM, an item is at most 128 query rows, a tile 128 keys; two streams x = 0, 1 take every second tile with the same
 // rows:
-//     S_x = Q K^T (shared x shared -> TMEM),  P_x = 2^(S_x - m_x) (TMEM -> registers -> TMEM, over S_x),  O_x += P_x V (TMEM x shared)
+//     S_x = Q K^T (shared x shared -> TMEM),  P_x = 2^((S_x - m_x) scale) (TMEM -> registers -> TMEM, over S_x),  O_x += P_x V (TMEM x shared)
 // so that one stream multiplies while the other is in its softmax; the two results are joined in TMEM at the end.  (256 rows to an
 // item, a stream for each half, reads the keys once instead of twice, the second time from L2, but was the slower one
 // throughout: 52 us against 44 for 256 rows and 32768 keys of 8 heads, 76 against 74 for 512 rows.)
@@ -35,7 +35,6 @@ constexpr int kKeys = kBlockKeys;
 constexpr int kMaxRing = 8;
 constexpr int kThreads = 384;
 constexpr uint32_t kTmemCols = 512;                   // S_x at 128 x, O_x at 256 + 128 x
-constexpr float kMostSum = 256.0f;                    // of a tile's probabilities, before the maximum is raised
 
 template <int D> struct Cfg {
     static constexpr uint32_t kAtom = kKeys * 128;    // 64 elements of every key
@@ -107,8 +106,8 @@ __device__ __forceinline__ bool elect_one() {
 typedef unsigned long long f2;
 __device__ __forceinline__ f2 mk2(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ void un2(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 
 // scores past the row's last column: -inf
 __device__ __forceinline__ void hide(uint32_t (&v)[32], int left) {
@@ -122,9 +121,8 @@ __device__ __forceinline__ float top_of(const uint32_t (&v)[32], float top) {
     for (int c = 0; c < 32; ++c) t[c & 3] = fmaxf(t[c & 3], __uint_as_float(v[c]));
     return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
-// Maximum of 32 n scores of the row.
-__device__ __forceinline__ float row_top(uint32_t t_s, int n, int left) {
-    float top = -INFINITY;
+// Maximum of 32 n scores of the row and `top`.
+__device__ __forceinline__ float row_top(uint32_t t_s, int n, int left, float top = -INFINITY) {
 #pragma unroll 1
     for (int q = 0; q < n; ++q) {
         uint32_t v[32];
@@ -135,9 +133,9 @@ __device__ __forceinline__ float row_top(uint32_t t_s, int n, int left) {
     }
     return top;
 }
-// 2^(s scale + off) of 64 scores of the row as bf16 and the sum of the unrounded values.
-__device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool partly, float scale, float off, uint32_t (&pr)[32]) {
-    const f2 scale2 = mk2(scale, scale), off2 = mk2(off, off);
+// 2^exponent(s, base, scale) of 64 scores of the row (softmax_rule.cuh, two at a time) as bf16 and the sum of the unrounded values.
+__device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool partly, float scale, float base, uint32_t (&pr)[32]) {
+    const f2 scale2 = mk2(scale, scale), base2 = mk2(-base, -base);
     f2 sum[2] = {0ull, 0ull};
     uint32_t v[2][32];
     tmem_ld32(t_s, v[0]);
@@ -150,7 +148,7 @@ __device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool part
 #pragma unroll
     for (int c = 0; c < 64; c += 2) {
         float e0, e1;
-        un2(fma2(mk2(__uint_as_float(v[c >> 5][c & 31]), __uint_as_float(v[c >> 5][(c & 31) + 1])), scale2, off2), e0, e1);
+        un2(mul2(add2(mk2(__uint_as_float(v[c >> 5][c & 31]), __uint_as_float(v[c >> 5][(c & 31) + 1])), base2), scale2), e0, e1);
         e0 = ex2(e0);
         e1 = ex2(e1);
         sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], mk2(e0, e1));
@@ -418,20 +416,20 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 tc_fence_after();
                 const int left = see - (s.t0 + 2 * j + x) * kKeys;      // columns the row sees
                 const bool partly = __any_sync(0xFFFFFFFFu, left < kKeys);
-                if (j == 0) m = row_top(t_s, kKeys / 32, left) * p.scale_log2;
+                if (j == 0) m = row_top(t_s, kKeys / 32, left);
                 // The products of the first half of the keys start while the second half is worked on.
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
                     const uint32_t t_h = t_s + 64u * half;
                     uint32_t pr[32];
-                    for (;;) {
-                        const float sum = probabilities(t_h, left - 64 * half, partly, p.scale_log2, m == -INFINITY ? 0.0f : -m, pr);
-                        if (!__any_sync(0xFFFFFFFFu, sum > kMostSum && m != INFINITY)) {
+                    for (bool raised = false;; raised = true) {
+                        const float sum = probabilities(t_h, left - 64 * half, partly, p.scale_log2, base_of(m), pr);
+                        if (!__any_sync(0xFFFFFFFFu, raise_maximum(sum, m, raised))) {
                             l += sum;
                             break;
                         }
-                        // a higher maximum, and the scores (still in TMEM) once more: afterwards the sum is at most the number of keys
-                        const float up = fmaxf(m, row_top(t_h, 2, left - 64 * half) * p.scale_log2), a = up == -INFINITY ? 1.0f : ex2(m - up);
+                        // a higher maximum, and the scores (still in TMEM) once more: then the sum is at most the number of keys
+                        const float up = row_top(t_h, 2, left - 64 * half, m), a = up == -INFINITY ? 1.0f : ex2(exponent(m, up, p.scale_log2));
                         m = up;
                         l *= a;
                         if (j == 0 && half == 0) continue;
@@ -473,7 +471,7 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const int64_t slot = s.item + int64_t(blockIdx.x);
             const float2 a = ml[row], b = ml[128 + row];
             const float mx = fmaxf(a.x, b.x);
-            const float fa = a.x == -INFINITY ? 0.0f : ex2(a.x - mx), fb = b.x == -INFINITY ? 0.0f : ex2(b.x - mx);
+            const float fa = a.x == -INFINITY ? 0.0f : ex2(exponent(a.x, mx, p.scale_log2)), fb = b.x == -INFINITY ? 0.0f : ex2(exponent(b.x, mx, p.scale_log2));
             if (valid && x == 0) part.ml[slot * part.rows + row] = make_float2(mx, a.y * fa + b.y * fb);
             barrier_any(false, 1, 256);                        // (m, l) have been read
             constexpr uint32_t kQuarter = 128 * D;             // bytes of 128 rows

@@ -1,8 +1,8 @@
 // Attention over the paged cache for items of few query rows, taken in blocks of at most 16, and for small problems in one launch
 // (public header: patch_prefix_attention; the work list and the partial results are described in attention.cuh).
 //
-// Mathematics.  For every row the running maximum m of the scaled scores (in powers of two), the sum l of 2^(s - m) and the
-// unnormalised output o = sum 2^(s - m) v; parts of the keys are joined with weights 2^(m_i - m).  All three are fp32; the
+// Mathematics.  For every row the running maximum m of the scores s = q.k, the sum l of 2^((s - m) scale) and the unnormalised output
+// o = sum 2^((s - m) scale) v; parts of the keys are joined with weights 2^((m_i - m) scale) (softmax_rule.cuh).  All three are fp32; the
 // probabilities are rounded to bf16 for the product with V (they are at most 1; the sum takes them unrounded).
 //
 // Kernel.  Every CTA, two to an SM, walks over its share of the work list (attention.cuh).  Warp 4 alone knows the list: it requests tiles
@@ -130,11 +130,11 @@ template <int D> struct Rows {
         float x1 = fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]));
         x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1));
         x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
-        x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2)) * scale_log2;
-        x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2)) * scale_log2;
+        x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2));
+        x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
         if (__any_sync(0xFFFFFFFFu, x0 > m0 || x1 > m1)) {
             const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
-            const float a0 = n0 == -INFINITY ? 1.0f : ex2(m0 - n0), a1 = n1 == -INFINITY ? 1.0f : ex2(m1 - n1);
+            const float a0 = n0 == -INFINITY ? 1.0f : ex2(exponent(m0, n0, scale_log2)), a1 = n1 == -INFINITY ? 1.0f : ex2(exponent(m1, n1, scale_log2));
             m0 = n0;
             m1 = n1;
             l0 *= a0;
@@ -142,13 +142,13 @@ template <int D> struct Rows {
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) { o[i][0] *= a0; o[i][1] *= a0; o[i][2] *= a1; o[i][3] *= a1; }
         }
-        const float c0 = m0 == -INFINITY ? 0.0f : m0, c1 = m1 == -INFINITY ? 0.0f : m1;
+        const float c0 = base_of(m0), c1 = base_of(m1);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            sc[j][0] = ex2(fmaf(sc[j][0], scale_log2, -c0));
-            sc[j][1] = ex2(fmaf(sc[j][1], scale_log2, -c0));
-            sc[j][2] = ex2(fmaf(sc[j][2], scale_log2, -c1));
-            sc[j][3] = ex2(fmaf(sc[j][3], scale_log2, -c1));
+            sc[j][0] = ex2(exponent(sc[j][0], c0, scale_log2));
+            sc[j][1] = ex2(exponent(sc[j][1], c0, scale_log2));
+            sc[j][2] = ex2(exponent(sc[j][2], c1, scale_log2));
+            sc[j][3] = ex2(exponent(sc[j][3], c1, scale_log2));
             l0 += sc[j][0] + sc[j][1];
             l1 += sc[j][2] + sc[j][3];
         }
@@ -188,7 +188,7 @@ template <int D> struct Rows {
     }
 };
 // Four elements (chunk c) of row r from the four warps' parts in the join buffer, and the row's (m, l).
-template <int D> __device__ __forceinline__ float4 joined(const float* join_o, const float2* join_ml, int r, int c, float2& ml_out) {
+template <int D> __device__ __forceinline__ float4 joined(const float* join_o, const float2* join_ml, int r, int c, float scale_log2, float2& ml_out) {
     float mx = -INFINITY, ls = 0.0f;
 #pragma unroll
     for (int q = 0; q < kWarps; ++q) mx = fmaxf(mx, join_ml[q * kRows + r].x);
@@ -196,7 +196,7 @@ template <int D> __device__ __forceinline__ float4 joined(const float* join_o, c
 #pragma unroll
     for (int q = 0; q < kWarps; ++q) {
         const float2 ml = join_ml[q * kRows + r];
-        const float a = ml.x == -INFINITY ? 0.0f : ex2(ml.x - mx);
+        const float a = ml.x == -INFINITY ? 0.0f : ex2(exponent(ml.x, mx, scale_log2));
         const float4 v = *reinterpret_cast<const float4*>(join_o + (q * kRows + r) * Cfg<D>::kJoinPitch + 4 * c);
         ls = fmaf(ml.y, a, ls);
         sum.x = fmaf(v.x, a, sum.x); sum.y = fmaf(v.y, a, sum.y); sum.z = fmaf(v.z, a, sum.z); sum.w = fmaf(v.w, a, sum.w);
@@ -370,7 +370,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         for (int i = threadIdx.x; i < n.rows * (D / 4); i += 32 * kWarps) {
             const int r = i / (D / 4), c = i - r * (D / 4);
             float2 ml;
-            *reinterpret_cast<float4*>(part.o + (row0 + r) * D + 4 * c) = joined<D>(join_o, join_ml, r, c, ml);
+            *reinterpret_cast<float4*>(part.o + (row0 + r) * D + 4 * c) = joined<D>(join_o, join_ml, r, c, p.scale_log2, ml);
             if (c == 0) part.ml[row0 + r] = ml;
         }
     }
@@ -496,7 +496,7 @@ attn_direct_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             for (int i = threadIdx.x; i < rows_n * (D / 4); i += 32 * kWarps) {
                 const int r = i / (D / 4), c = i - r * (D / 4);
                 float2 ml;
-                *reinterpret_cast<float4*>(part_o + r * D + 4 * c) = joined<D>(join_o, join_ml, r, c, ml);
+                *reinterpret_cast<float4*>(part_o + r * D + 4 * c) = joined<D>(join_o, join_ml, r, c, p.scale_log2, ml);
                 if (c == 0) part_ml[r] = ml;
             }
         }
@@ -514,7 +514,7 @@ attn_direct_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(ml.x), "=f"(ml.y) : "r"(map_to_rank(base + kRows * D * 4 + r * 8, q)) : "memory");
                 asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(map_to_rank(base + r * D * 4 + c * 16, q)) : "memory");
                 if (ml.x == -INFINITY) continue;
-                const float mx = fmaxf(m, ml.x), a = m == -INFINITY ? 0.0f : ex2(m - mx), f = ex2(ml.x - mx);
+                const float mx = fmaxf(m, ml.x), a = m == -INFINITY ? 0.0f : ex2(exponent(m, mx, p.scale_log2)), f = ex2(exponent(ml.x, mx, p.scale_log2));
                 acc.x = acc.x * a + v.x * f; acc.y = acc.y * a + v.y * f; acc.z = acc.z * a + v.z * f; acc.w = acc.w * a + v.w * f;
                 l = l * a + ml.y * f;
                 m = mx;
@@ -523,7 +523,7 @@ attn_direct_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             const int t = p.token(row0 + r), head = kvh * p.G + row0 + r - t * p.G;
             const int64_t tok = int64_t(b) * p.T + t;
             *reinterpret_cast<uint2*>(O + tok * ldo + int64_t(head) * D + 4 * c) = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
-            if (lse && c == 0) lse[tok * (p.Hkv * p.G) + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+            if (lse && c == 0) lse[tok * (p.Hkv * p.G) + head] = l == 0.0f ? -INFINITY : (m * p.scale_log2 + log2f(l)) * 0.6931471805599453f;
         }
     }
     __syncwarp();

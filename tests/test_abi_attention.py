@@ -160,3 +160,11 @@ def test_tensors_are_checked_before_the_library_is_called(B):
     for f in (m.kv_append, m.qk_norm_rope, m.qk_norm_rope_backward, m.prefix_attention):
         with pytest.raises(TypeError):
             f(0)
+
+
+def test_attention_scale_bound(B):
+    """scale log2(e) has to be an fp32 number: twice that would be an infinity in every exponent."""
+    L, c = B.lib(), cache(B)
+    need = B.patch_prefix_attention_workspace_size(c, 3, 1, 8)
+    call = lambda scale: L.patch_prefix_attention(c, FAKE, 1024, 3, 1, 8, FAKE, 100, FAKE, 4, FAKE, scale, FAKE, 1024, None, FAKE, need - 1, None, None)  # noqa: E731
+    assert call(2.5e38) == B.ERR_SHAPE and call(1.9e38) == B.ERR_SIZE
