@@ -256,7 +256,9 @@ rope_backward_kernel(const GradHeads q, const GradHeads k, const Turn turn, int6
     __shared__ float sums[kGroups][LANES * 8];
     __shared__ int kinds[kGroups];
     const int D = DT ? DT : d;
-    grid_launch_dependents();                 // the kernel that adds up the partial sums waits for this one's end by itself
+    // The kernel that adds up the partial sums waits for this one's end by itself.  Without weights there is none: what follows then is the
+    // caller's, and a GEMM whose input is promised to be there would not wait.
+    if (partial) grid_launch_dependents();
     const int per_token = q.groups + k.groups;
     const int group = threadIdx.x / LANES;
     const int64_t idx = int64_t(blockIdx.x) * kGroups + group;

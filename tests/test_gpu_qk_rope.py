@@ -269,3 +269,31 @@ def test_on_another_stream_and_in_a_graph(B):
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("M", [64, 4096, 16384])
+@pytest.mark.parametrize("weights", [False, True])
+def test_a_gemm_behind_the_gradient(B, M, weights):
+    """The gradient has completed when the next kernel starts: a GEMM whose weight and input are promised not to be written in its overlap
+    window reads gQ without waiting, and one whose result is promised writes over an operand of the gradient."""
+    H, D, N = 16, 128, 256
+    g = torch.Generator(device="cuda").manual_seed(M)
+    packed, layout = B.patch_pack((torch.randn(N, H * D, generator=g, device="cuda") * 0.05).to(BF), np.zeros((N // 128, H * D // 128), np.uint8))
+    ws = torch.zeros(B.patch_gemm_workspace_size(layout, max(M, 64)), dtype=torch.uint8, device="cuda")
+    q, gy = make(M, H, D, 1).contiguous(), make(M, H, D, 2).contiguous()
+    w = weight(D, 3) if weights else None
+    rope, pos = B.patch_rope(table(512, D)), (torch.arange(M, device="cuda") % 512).int()
+    promised = B.VARIANT_AUTO | B.WEIGHTS_STATIC | B.INPUT_STATIC | (B.OUTPUT_STATIC if M <= 64 else 0)
+    want, _, _, _ = B.patch_qk_norm_rope_backward(gy, None, rope, pos, Q=q, wq=w)
+    torch.cuda.synchronize()
+    want_y = B.patch_gemm(want.view(M, H * D), layout, packed, workspace=ws, variant=promised)
+    torch.cuda.synchronize()
+    gq, status = torch.empty_like(want), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for _ in range(8):
+        gq.fill_(float("nan"))
+        operand = gy.clone()                                    # the GEMM's result goes where the gradient's operand was
+        y = operand.view(-1)[: M * N].view(M, N)
+        B.patch_qk_norm_rope_backward(operand, None, rope, pos, Q=q, wq=w, gQ=gq, status=status)
+        B.patch_gemm(gq.view(M, H * D), layout, packed, Y=y, workspace=ws, variant=promised)
+        torch.cuda.synchronize()
+        assert torch.equal(gq, want) and torch.equal(y, want_y) and int(status.item()) == 0
