@@ -458,6 +458,15 @@ def _stream_of(x, stream):
     return _raw_stream(x.get_device()) if stream is None else stream.cuda_stream
 
 
+def _empty(stream, shape, dtype, device):
+    """Memory for a call that runs on ``stream``, from that stream's share of torch's allocator.  From the current stream's it could be in use
+    there still, and be given away there when the last reference goes (a workspace's: on return), while the kernels run on ``stream``."""
+    if stream is None:
+        return _torch.empty(shape, dtype=dtype, device=device)
+    with _torch.cuda.stream(stream):
+        return _torch.empty(shape, dtype=dtype, device=device)
+
+
 def patch_rope(cos_sin, interleaved: bool = False) -> Rope:
     """Rotation by a table float32 [max_positions, rotary_dim]: a position's cosines, then its sines."""
     _use_torch()
@@ -485,9 +494,9 @@ def patch_qk_norm_rope(Q, K, rope: Rope | None, positions, wq=None, wk=None, eps
     if _torch is None:
         _use_torch()
     if Q_out is None and Q is not None:
-        Q_out = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
+        Q_out = _empty(stream, Q.shape, _bf16, Q.device)
     if K_out is None and K is not None:
-        K_out = _torch.empty(K.shape, dtype=_bf16, device=K.device)
+        K_out = _empty(stream, K.shape, _bf16, K.device)
     rc = _marshal.qk_norm_rope((_lib or lib()).at_patch_qk_norm_rope, Q, K, wq, wk, eps, rope.at if rope is not None else None, positions,
                                Q_out, K_out, status, _stream_of(Q if Q is not None else K, stream))
     if rc:
@@ -509,17 +518,17 @@ def patch_qk_norm_rope_backward(gQ_out, gK_out, rope: Rope | None, positions, Q=
         _use_torch()
     some = gQ_out if gQ_out is not None else gK_out
     if gQ is None and gQ_out is not None:
-        gQ = _torch.empty(gQ_out.shape, dtype=_bf16, device=some.device)
+        gQ = _empty(stream, gQ_out.shape, _bf16, some.device)
     if gK is None and gK_out is not None:
-        gK = _torch.empty(gK_out.shape, dtype=_bf16, device=some.device)
+        gK = _empty(stream, gK_out.shape, _bf16, some.device)
     if gwq is None and wq is not None:
-        gwq = _torch.empty(some.shape[2], dtype=_torch.float32, device=some.device)
+        gwq = _empty(stream, some.shape[2], _torch.float32, some.device)
     if gwk is None and wk is not None:
-        gwk = _torch.empty(some.shape[2], dtype=_torch.float32, device=some.device)
+        gwk = _empty(stream, some.shape[2], _torch.float32, some.device)
     if workspace is None and (wq is not None or wk is not None):
         n = patch_qk_norm_rope_backward_workspace_size(some.shape[0], gQ_out.shape[1] if gQ_out is not None else 0,
                                                        gK_out.shape[1] if gK_out is not None else 0, some.shape[2])
-        workspace = _torch.empty(n, dtype=_torch.uint8, device=some.device)
+        workspace = _empty(stream, n, _torch.uint8, some.device)
     rc = _marshal.qk_norm_rope_backward((_lib or lib()).at_patch_qk_norm_rope_backward, gQ_out, gK_out, Q if wq is not None else None,
                                         K if wk is not None else None, wq, wk, eps, rope.at if rope is not None else None, positions, gQ, gK,
                                         gwq, gwk, workspace, status, _stream_of(some, stream))
@@ -533,7 +542,7 @@ def patch_kv_append(cache: KVCache, K, V, slots, rope: Rope | None = None, posit
     """Keys (normed and rotated) and values [M, Hkv, D] into the cache's slots (int64 [M]; negative: not stored); with Q
     [M, Hq, D] also the queries, normed and rotated: returns Q_out (None without Q)."""
     if Q_out is None and Q is not None:
-        Q_out = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
+        Q_out = _empty(stream, Q.shape, _bf16, Q.device)
     rc = _marshal.kv_append((_lib or lib()).at_patch_kv_append, cache.at, K, V, slots, wk, eps, rope.at if rope is not None else None,
                             positions, Q, wq, Q_out, status, _stream_of(K, stream))
     if rc:
@@ -553,11 +562,10 @@ def patch_prefix_attention(cache: KVCache, Q, prefix_pages, prefix_len: int, pag
     keys (int32 ``page_table`` [B, n], int32 ``suffix_lens`` [B]): returns O; ``lse`` float32 [B T, Hq] is written if given.
     ``scale`` defaults to 1 / sqrt(D)."""
     if O is None:
-        O = _torch.empty(Q.shape, dtype=_bf16, device=Q.device)
+        O = _empty(stream, Q.shape, _bf16, Q.device)
     if workspace is None:
         B = page_table.shape[0]
-        workspace = _torch.empty(patch_prefix_attention_workspace_size(cache, B, Q.shape[0] // B if B else 1, Q.shape[1]),
-                                 dtype=_torch.uint8, device=Q.device)
+        workspace = _empty(stream, patch_prefix_attention_workspace_size(cache, B, Q.shape[0] // B if B else 1, Q.shape[1]), _torch.uint8, Q.device)
     rc = _marshal.prefix_attention((_lib or lib()).at_patch_prefix_attention, cache.at, Q, prefix_pages, prefix_len, page_table, suffix_lens,
                                    scale, O, lse, workspace, status, _stream_of(Q, stream))
     if rc:
