@@ -580,7 +580,8 @@ int patch_kv_append(const patch_kv_cache_t* cache, const void* K_dev, int64_t ld
  *     O = softmax(scale q k^T) v over what it sees,  lse = ln sum exp(scale q k^T);  nothing seen: O = 0, lse = -inf.
  * Query head h reads key head h / (Hq / Hkv).  The prefix is read once for all sequences (the batch's rows of one key
  * head are one operand; only problems of a few microseconds read it for each, from L2), and no key or value past a length is
- * used, whatever the cache holds there; keys and values that some query token of a sequence sees are assumed finite.
+ * used, whatever the cache holds there; keys and values that some query token of a sequence sees are assumed finite.  NaN in a
+ * query head makes its row of O and its lse NaN and no other.
  *   cache             D = 64 or 128
  *   Q_dev, O_dev      [B T x Hq heads of D], pitches ldq, ldo;  Hq a multiple of the cache's Hkv
  *   prefix_pages_dev  int32 [ceil(prefix_len / page_size)] pages of the prefix, in order (NULL if prefix_len is 0)

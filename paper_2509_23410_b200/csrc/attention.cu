@@ -82,7 +82,7 @@ attn_join_kernel(const Problem p, const Results from, const int blocks_p, const 
         float mx = fmaxf(m, mine.x);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
-        if (mx == -INFINITY) continue;
+        if (!__any_sync(0xFFFFFFFFu, mine.y != 0.0f)) continue;      // saw nothing (a row of NaN has seen something: its sum is NaN)
         const float f = ex2(exponent(mine.x, mx, p.scale_log2)), a = ex2(exponent(m, mx, p.scale_log2));
         float add = mine.y * f;
 #pragma unroll

@@ -513,7 +513,7 @@ attn_direct_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 float4 v;
                 asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(ml.x), "=f"(ml.y) : "r"(map_to_rank(base + kRows * D * 4 + r * 8, q)) : "memory");
                 asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(map_to_rank(base + r * D * 4 + c * 16, q)) : "memory");
-                if (ml.x == -INFINITY) continue;
+                if (ml.y == 0.0f) continue;          // saw nothing (a row of NaN has seen something: its sum is NaN)
                 const float mx = fmaxf(m, ml.x), a = m == -INFINITY ? 0.0f : ex2(exponent(m, mx, p.scale_log2)), f = ex2(exponent(ml.x, mx, p.scale_log2));
                 acc.x = acc.x * a + v.x * f; acc.y = acc.y * a + v.y * f; acc.z = acc.z * a + v.z * f; acc.w = acc.w * a + v.w * f;
                 l = l * a + ml.y * f;

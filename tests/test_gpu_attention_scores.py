@@ -152,3 +152,20 @@ def test_moving_maximum(B, case):
     stairs(x, case)
     o, l = x.run(B)
     x.check(o, l)
+
+
+@pytest.mark.parametrize("case", range(len(SHAPES)))
+def test_a_query_that_is_not_a_number_shows(B, case):
+    """NaN in a query makes its result and its lse NaN (not the 0 and -inf of a row that sees nothing) and leaves all others alone."""
+    lens, T, Hq, Hkv, D, P, page, extra = SHAPES[case]
+    x = Batch(B, lens, T, Hq, Hkv, D, P, page, seed=case, extra=extra)
+    want, want_l = x.run(B)
+    rows = {(b * T + t, (b + t) % Hq) for b in range(len(lens)) for t in (0, T - 1)}
+    mask = torch.zeros(x.q.shape[:2], dtype=torch.bool, device="cuda")
+    for row, h in rows:
+        x.q[row, h, (7 * row) % D] = float("nan")
+        b, t = divmod(row, T)
+        mask[row, h] = P + max(0, lens[b] - (T - 1 - t)) > 0          # a row without keys stays 0
+    o, l = x.run(B)
+    assert bool(mask.any()) and bool(o[mask].isnan().all()) and bool(l[mask].isnan().all())
+    assert torch.equal(o[~mask], want[~mask]) and torch.equal(l[~mask], want_l[~mask])
