@@ -80,6 +80,7 @@ template <class F> PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F&& f) {
     return nullptr;
 }
 template <class F> int unlocked(F&& f) {          // the launch itself, without the interpreter's lock
+    if (PyErr_Occurred()) return -1;              // a number was none: nothing is launched
     PyThreadState* s = PyEval_SaveThread();
     const int rc = f();
     PyEval_RestoreThread(s);
