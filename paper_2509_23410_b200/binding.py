@@ -449,6 +449,8 @@ def _use_torch():
         from . import _marshal as m
     except ImportError as e:
         raise RuntimeError("_marshal.so is missing or was built for another torch: run `python -m paper_2509_23410_b200.build`") from e
+    if m.built != f"for torch {torch.__version__}":
+        raise RuntimeError(f"_marshal.so was built {m.built}, this is {torch.__version__}: run `python -m paper_2509_23410_b200.build`")
     _torch, _bf16, _marshal = torch, torch.bfloat16, m
     # the current stream's handle without a Stream object around it (five times quicker); device index -> handle
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)

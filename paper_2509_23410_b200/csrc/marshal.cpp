@@ -197,4 +197,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&module); }
+// PATCH_BUILT: which torch this was compiled against (build.py), looked at before anything is called
+PyMODINIT_FUNC PyInit__marshal() {
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built", PATCH_BUILT) < 0) Py_CLEAR(m);
+    return m;
+}
