@@ -297,3 +297,32 @@ def test_a_gemm_behind_the_gradient(B, M, weights):
         B.patch_gemm(gq.view(M, H * D), layout, packed, Y=y, workspace=ws, variant=promised)
         torch.cuda.synchronize()
         assert torch.equal(gq, want) and torch.equal(y, want_y) and int(status.item()) == 0
+
+
+@pytest.mark.parametrize("case", [(9, 4, 2, 64, 32, True), (70, 6, 3, 128, 128, False), (33, 2, 5, 256, 64, False)])
+def test_gradient_against_autograd(B, case):
+    """The gradient kernel against torch's own differentiation of the definition in 64 bits."""
+    M, Hq, Hkv, D, R, inter = case
+    tab, pos = table(200, R), torch.randint(0, 200, (M,), device="cuda", dtype=torch.int32, generator=torch.Generator(device="cuda").manual_seed(5))
+    c, s = tab[pos.long(), : R // 2].double()[:, None], tab[pos.long(), R // 2 :].double()[:, None]
+    rope = B.patch_rope(tab, interleaved=inter)
+    ins = [make(M, Hq, D, 1), make(M, Hkv, D, 2), weight(D, 3), weight(D, 4)]
+    gy = [make(M, Hq, D, 6), make(M, Hkv, D, 7)]
+    got = B.patch_qk_norm_rope_backward(*gy, rope, pos, Q=ins[0], K=ins[1], wq=ins[2], wk=ins[3], eps=1e-5)
+    leaves = [t.double().requires_grad_() for t in ins]
+    loss = 0.0
+    for x, w, g in zip(leaves[:2], leaves[2:], gy):
+        y = x / torch.sqrt((x * x).mean(-1, keepdim=True) + 1e-5) * w
+        a, b = (y[..., 0:R:2], y[..., 1:R:2]) if inter else (y[..., : R // 2], y[..., R // 2 : R])
+        pair = (a * c - b * s, b * c + a * s)
+        turned = torch.stack(pair, -1).flatten(-2) if inter else torch.cat(pair, -1)
+        loss = loss + (torch.cat((turned, y[..., R:]), -1) * g.double()).sum()
+    want = torch.autograd.grad(loss, leaves)
+    for x, w, g, a, b in zip(ins, ins[2:], gy, got, want):
+        x = x.double()
+        r = 1 / torch.sqrt((x * x).mean(-1, keepdim=True) + 1e-5)
+        most = 2 * g.double().abs().amax(-1, keepdim=True) * w.double().abs().max()
+        check(a, b, r * (most + (x * r).abs() * most * (x * r).abs().mean(-1, keepdim=True)), "gradient")
+    for x, g, a, b in zip(ins, gy, got[2:], want[2:]):
+        xh = x.double() / torch.sqrt((x.double() ** 2).mean(-1, keepdim=True) + 1e-5)
+        assert bool(((a.double() - b).abs() <= (2 * g.double().abs().amax(-1, keepdim=True) * xh.abs()).sum((0, 1)) * 2.0 ** -12).all())
