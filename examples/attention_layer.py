@@ -30,19 +30,20 @@ def rope_table(positions: int, rotary_dim: int, base: float = 10000.0) -> torch.
 
 
 class QKNormRope(torch.autograd.Function):
-    """(Q, K, wq, wk) -> normed and rotated (Q, K), with the gradient kernel behind it."""
+    """(Q, K, wq, wk) -> normed and rotated (Q, K), with the gradient kernel behind it; a weight may be None (rotation alone)."""
 
     @staticmethod
     def forward(ctx, Q, K, wq, wk, rope, positions, eps):
-        ctx.save_for_backward(Q, K, wq, wk, positions)
+        ctx.save_for_backward(Q if wq is not None else None, K if wk is not None else None, wq, wk, positions)
         ctx.rope, ctx.eps = rope, eps
         return B.patch_qk_norm_rope(Q, K, rope, positions, wq=wq, wk=wk, eps=eps)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable          # the gradient kernel is not differentiated in turn
     def backward(ctx, gQ, gK):
         Q, K, wq, wk, positions = ctx.saved_tensors
-        gQ, gK, gwq, gwk = B.patch_qk_norm_rope_backward(gQ.contiguous(), gK.contiguous(), ctx.rope, positions, Q=Q, K=K, wq=wq, wk=wk, eps=ctx.eps)
-        return gQ, gK, gwq.to(BF), gwk.to(BF), None, None, None
+        gQ, gK, *gw = B.patch_qk_norm_rope_backward(gQ.contiguous(), gK.contiguous(), ctx.rope, positions, Q=Q, K=K, wq=wq, wk=wk, eps=ctx.eps)
+        return gQ, gK, *(g if g is None else g.to(BF) for g in gw), None, None, None
 
 
 class Layer:

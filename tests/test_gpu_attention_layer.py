@@ -33,3 +33,31 @@ def test_prompt_and_steps(example, shape):
 def test_training(example):
     losses = example.train_step()
     assert losses[-1] < 0.2 * losses[0] and all(b < a for a, b in zip(losses, losses[1:]))
+
+
+@pytest.mark.parametrize("norms", [(False, False), (True, False), (False, True), (True, True)])
+def test_autograd_function(example, norms):
+    """With either weight left out, and differentiated once only.  Results and gradients are rounded to bf16: 2^-8 each."""
+    M, Hq, Hkv, D = 20, 4, 2, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    tab = example.rope_table(M, D)
+    rope, pos = example.B.patch_rope(tab), torch.arange(M, dtype=torch.int32, device="cuda")
+    x = [rand(M, Hq, D).requires_grad_(), rand(M, Hkv, D).requires_grad_()]
+    w = [(1 + 0.1 * rand(D)).requires_grad_() if n else None for n in norms]
+    gy = [rand(M, Hq, D), rand(M, Hkv, D)]
+    leaves = x + [t for t in w if t is not None]
+    got = torch.autograd.grad(sum((y * t).sum() for y, t in zip(example.QKNormRope.apply(*x, *w, rope, pos, 1e-6), gy)), leaves)
+    leaves64 = [t.detach().double().requires_grad_() for t in leaves]
+    loss, weights, c, s = 0.0, iter(leaves64[2:]), tab[:, None, : D // 2].double(), tab[:, None, D // 2 :].double()
+    for y, norm, t in zip(leaves64[:2], norms, gy):
+        if norm:
+            y = y / torch.sqrt(y.square().mean(-1, keepdim=True) + 1e-6) * next(weights)
+        a, b = y[..., : D // 2], y[..., D // 2 :]
+        loss = loss + (torch.cat((a * c - b * s, b * c + a * s), -1) * t.double()).sum()
+    for a, b in zip(got, torch.autograd.grad(loss, leaves64)):
+        assert float((a.double() - b).norm() / b.norm()) < 1e-2
+    y, _ = example.QKNormRope.apply(*x, *w, rope, pos, 1e-6)
+    (gx,) = torch.autograd.grad(y.float().square().sum(), x[:1], create_graph=True)
+    with pytest.raises(RuntimeError):
+        gx.float().square().sum().backward()
