@@ -94,7 +94,8 @@ __device__ __forceinline__ int suffix_len(const Problem& p, int b) {
 }
 
 // Executed by one warp: where the kernel has suffix items, units before each sequence (of one key head) and the clamped
-// lengths.  Returns the batch's own keys.  (Every CTA waits for this: four groups of lengths are on their way at once.)
+// lengths (unless `lens` is null).  Returns the batch's own keys.  (Every CTA waits for this: four groups of lengths are on their way at
+// once.)
 template <bool STEPS> __device__ __forceinline__ int64_t lay_out(const Problem& p, const Line& w, int* cum, int* lens) {
     constexpr int kAtOnce = 4;
     const int lane = threadIdx.x & 31;
@@ -110,7 +111,7 @@ template <bool STEPS> __device__ __forceinline__ int64_t lay_out(const Problem& 
             keys += n[i];
             if (!w.blocks_s || g0 + 32 * i >= p.B) continue;
             int t = head_units<STEPS>(p, w, n[i]);
-            if (b < p.B) lens[b] = n[i];
+            if (lens && b < p.B) lens[b] = n[i];
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int o = __shfl_up_sync(0xFFFFFFFFu, t, d);
@@ -147,7 +148,7 @@ template <bool STEPS> struct Share {
     const Problem& p;
     const Line& w;
     const int* cum;
-    const int* len;
+    const int* len;                           // null: looked up where they came from
     int b, kvh, block, item;                  // b < 0: the prefix; item: number among the prefix's or the suffixes' items
     int tiles, keys;
     int t0, t1;                               // the share's tiles of the item
@@ -160,7 +161,7 @@ template <bool STEPS> struct Share {
     }
     __device__ __forceinline__ void at_sequence(int b_) {
         b = b_;
-        keys = len[b];
+        keys = len ? len[b] : suffix_len(p, b);
         tiles = tiles_of<STEPS>(p, w, keys, 0);
     }
     __device__ __forceinline__ void clip() { t1 = min(tiles, u1 - u - w.cost); }

@@ -41,7 +41,12 @@ template <int D> struct Cfg {
     static constexpr uint32_t kBarOffset = kNoteOffset + kStages * 32;
     static constexpr uint32_t kCumOffset = kBarOffset + 128;
     static constexpr uint32_t kFixedBytes = kCumOffset + 1024;               // + alignment of the ring
-    static uint32_t smem_bytes(int B) { return kFixedBytes + uint32_t(2 * B + 1) * 4; }
+    // The sequences' units and lengths are kept behind that.  Where with both of them two CTAs no longer fit an SM, lengths are not kept but
+    // looked up again (in L1): at D = 128 two CTAs fit up to 1231 sequences instead of 615.  616 sequences of up to 1024 keys of 2 heads
+    // took 115 us with one CTA per SM, 85 with two; for fewer sequences the look-up costs the launches beside the block kernel 0.6 us.
+    static constexpr uint32_t kMostForTwo = 228 * 1024 / 2 - 1024;          // the hardware takes 1 KB for each CTA
+    __host__ __device__ static constexpr bool keeps_lengths(int B) { return kFixedBytes + uint32_t(2 * B + 1) * 4 <= kMostForTwo; }
+    static constexpr uint32_t smem_bytes(int B) { return kFixedBytes + uint32_t(keeps_lengths(B) ? 2 * B + 1 : B + 1) * 4; }
 };
 // What a stage holds.
 struct Note { int slot, key0, keys, rows, block, flags, pad[2]; };
@@ -218,7 +223,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kBarOffset + 16 * kStages);
     Note* notes = reinterpret_cast<Note*>(smem + C::kNoteOffset);
     int* cum = reinterpret_cast<int*>(smem + C::kCumOffset);
-    int* lens = cum + p.B + 1;
+    int* lens = C::keeps_lengths(p.B) ? cum + p.B + 1 : nullptr;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     grid_launch_dependents();                        // the joining kernel waits for this one's end by itself
@@ -573,8 +578,10 @@ static int launch(const patch_kv_cache_t* c, const Problem& p, const Line& w, co
     if ((rc = allow_dynamic_smem(kern, Cfg<D>::smem_bytes(kMaxBatch), configured))) return rc;
     const int sms = sm_count() < kMaxSms ? sm_count() : kMaxSms;
     if (sms <= 0) return PATCH_ERR_CUDA;
-    // alone, one wave; beside the block kernel, more and ever smaller shares that run on whatever SMs it leaves free
-    const int ctas = (AFTER ? 4 : 2) * sms;
+    // Alone, one wave: two CTAs per SM where they fit, else one (two waves of equal shares would follow one another: 2048 sequences of up to
+    // 1024 keys of 2 heads 356 us, 336 in one wave).  Beside the block kernel, more and ever smaller shares that run on whatever SMs
+    // it leaves free.
+    const int ctas = (AFTER ? 4 : Cfg<D>::smem_bytes(p.B) > Cfg<D>::kMostForTwo ? 1 : 2) * sms;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     cfg.gridDim = dim3(unsigned(ctas), 1, 1);

@@ -88,3 +88,20 @@ def test_a_wait_that_runs_out_is_reported_and_survivable(B, shape, extra):
     assert call(status) == B.ERR_TIMEOUT
     status.zero_()
     assert call(status) == B.OK and torch.equal(o, want)
+
+
+@pytest.mark.parametrize("n", [615, 616, 1231, 1232, 2048])
+@pytest.mark.parametrize("P", [0, 100, 4100])
+def test_batches_around_the_limits_of_shared_memory(B, n, P):
+    """Up to 615 sequences the decode kernel keeps their lengths, up to 1231 two of its CTAs fit an SM (heads of 128); alone, and beside the
+    block kernel, which has the longer prefix."""
+    lens = [(1 + 7 * i % 150) * (i % 11 != 3) for i in range(n)]
+    x = Batch(B, lens, 1, 2, 1, 128, P, 16, seed=n)
+    o, l = x.run(B)
+    if P == 0:
+        assert float(o[3].float().abs().max()) == 0.0 and bool((l[3] == -float("inf")).all())
+    # a sample of the sequences: the check walks them one by one
+    rows = [b for b in range(0, n, 41) if P or lens[b]] + [n - 1]
+    x.lens, x.ks, x.vs = [lens[b] for b in rows], [x.ks[b] for b in rows], [x.vs[b] for b in rows]
+    x.q = x.q[rows]
+    x.check(o[rows], l[rows])
