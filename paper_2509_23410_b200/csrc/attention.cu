@@ -189,6 +189,21 @@ static int check_batch(const patch_kv_cache_t* c, int64_t B, int T, int Hq) {
 }
 
 }  // namespace attn
+
+int make_kv_tensor_map(CUtensorMap* map, const patch_kv_cache_t* c, const void* base, int rows, int halves) {
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return PATCH_ERR_CUDA;
+    const cuuint64_t row = cuuint64_t(c->D) * 2;
+    const cuuint64_t dims[5] = {64, cuuint64_t(c->page_size), cuuint64_t(c->D / 64), cuuint64_t(c->Hkv), cuuint64_t(c->num_pages)};
+    const cuuint64_t strides[4] = {row, 128, row * c->page_size, cuuint64_t(c->page_stride) * 2};
+    const cuuint32_t box[5] = {64, cuuint32_t(rows), cuuint32_t(halves), 1, 1};
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? PATCH_OK : PATCH_ERR_CUDA;
+}
+
 }  // namespace patch
 
 using namespace patch;

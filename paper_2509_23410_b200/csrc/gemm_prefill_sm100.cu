@@ -19,7 +19,7 @@
 //
 // Every mbarrier wait is bounded; on expiry the CTA raises an abort flag, reports
 // PATCH_ERR_TIMEOUT through status_dev, drains its copies in flight, frees TMEM and returns.
-#include "attention.cuh"
+#include "sm100_ptx.cuh"
 
 namespace patch {
 
@@ -188,11 +188,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmap_x, const uint8_t* __rest
 // ---------------------------------------------------------------------------------------------
 // host side
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_tiled_fn() {
+EncodeTiledFn encode_tiled_fn() {
     static EncodeTiledFn fn = [] {
         void* p = nullptr;
         cudaDriverEntryPointQueryResult q;
@@ -214,20 +210,6 @@ int make_x_tensor_map(CUtensorMap* map, const __nv_bfloat16* X, int64_t ldx, int
     CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<__nv_bfloat16*>(X), dims, strides, box,
                      estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? PATCH_OK : PATCH_ERR_CUDA;
-}
-
-int make_kv_tensor_map(CUtensorMap* map, const patch_kv_cache_t* c, const void* base, int rows, int halves) {
-    EncodeTiledFn enc = encode_tiled_fn();
-    if (!enc) return PATCH_ERR_CUDA;
-    const cuuint64_t row = cuuint64_t(c->D) * 2;
-    const cuuint64_t dims[5] = {64, cuuint64_t(c->page_size), cuuint64_t(c->D / 64), cuuint64_t(c->Hkv), cuuint64_t(c->num_pages)};
-    const cuuint64_t strides[4] = {row, 128, row * c->page_size, cuuint64_t(c->page_stride) * 2};
-    const cuuint32_t box[5] = {64, cuuint32_t(rows), cuuint32_t(halves), 1, 1};
-    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-    CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? PATCH_OK : PATCH_ERR_CUDA;
 }
 

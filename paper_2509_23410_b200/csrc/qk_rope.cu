@@ -22,6 +22,7 @@
 // TB/s).  One token appended takes 3.0 us, which is a launch and three dependent reads.
 #include "patch_internal.cuh"
 #include "sm100_ptx.cuh"
+#include "f32x2.cuh"
 
 namespace patch {
 namespace rope {
@@ -57,26 +58,9 @@ struct Turn {
     int R;
 };
 
-// ---- pairs of fp32 in a 64-bit register ----
-typedef unsigned long long f2;
-__device__ __forceinline__ f2 mk2(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void un2(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ f2 swap2(f2 v) { float a, b; un2(v, a, b); return mk2(b, a); }
-__device__ __forceinline__ float sum2(f2 v) { float a, b; un2(v, a, b); return a + b; }
-// two bf16 -> two fp32 and back
-__device__ __forceinline__ f2 widen(uint32_t u) { return mk2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u)); }
-__device__ __forceinline__ uint32_t narrow(f2 v) {
-    float a, b;
-    un2(v, a, b);
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 struct Raw { uint2 a, b; };               // a lane's eight bf16 of a head
 __device__ __forceinline__ void widen(const Raw& r, f2 (&v)[4]) {
-    v[0] = widen(r.a.x); v[1] = widen(r.a.y); v[2] = widen(r.b.x); v[3] = widen(r.b.y);
+    v[0] = widen2(r.a.x); v[1] = widen2(r.a.y); v[2] = widen2(r.b.x); v[3] = widen2(r.b.y);
 }
 
 // One group of lanes.  DT: head size known at compile time (then every lane is inside the head), 0: given at run time.
@@ -106,8 +90,8 @@ struct Group {
     }
     __device__ __forceinline__ void store(__nv_bfloat16* head, const f2 (&v)[4]) const {
         if (!on) return;
-        *reinterpret_cast<uint2*>(head + o0) = make_uint2(narrow(v[0]), narrow(v[1]));
-        *reinterpret_cast<uint2*>(head + o1) = make_uint2(narrow(v[2]), narrow(v[3]));
+        *reinterpret_cast<uint2*>(head + o0) = make_uint2(narrow2(v[0]), narrow2(v[1]));
+        *reinterpret_cast<uint2*>(head + o1) = make_uint2(narrow2(v[2]), narrow2(v[3]));
     }
     // the pairs' other elements; zeros where nothing is rotated (an infinity there must not meet a zero sine)
     __device__ __forceinline__ void other(const f2 (&v)[4], f2 (&o)[4]) const {

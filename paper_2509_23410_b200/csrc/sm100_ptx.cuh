@@ -381,6 +381,11 @@ __device__ __forceinline__ void store_fragment_transposed(const uint32_t (&v)[16
     __syncwarp();
 }
 
+// The driver's encoder of tensor maps (null: not to be had).
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn();
 // Host: tensor map over X [M x ldx] bf16 with a box of 64 columns (128 B) x n_tok rows,
 // 128-byte swizzle, zero fill outside the matrix.
 int make_x_tensor_map(CUtensorMap* map, const __nv_bfloat16* X, int64_t ldx, int64_t M, int64_t K, int n_tok);
