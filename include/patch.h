@@ -483,7 +483,9 @@ int patch_soft_mask_backward(const void* W_dev, int64_t ldw, const float* P_tile
  * Between the linear layers: what a decoder does with the q/k/v projection before the o projection.
  * Queries, keys and values are rows of heads: head h of token m starts at element m * ld + h * D, so the
  * column ranges of one stacked q/k/v projection are passed as they are (pointer to the range, ld = the stack's pitch).
- * Everything is bf16; arithmetic is fp32 with one rounding at the end.  The launches are ordinary ones as far as
+ * Everything is bf16; arithmetic, sums and maxima are fp32, and results are rounded once, at the end.  One rounding more lies inside the
+ * attention: its probabilities are rounded to bf16 for their product with V (the sum that divides takes them unrounded), which is what
+ * the tensor cores multiply; a result may be off by 2^-8 of sum p |v| for it.  The launches are ordinary ones as far as
  * the GEMMs' overlap window goes: they start when everything before them on the stream has completed, and they have
  * completed when the next kernel starts.
  * ========================================================================================= */
@@ -562,7 +564,7 @@ int patch_qk_norm_rope_backward(const void* gQo_dev, int64_t ldgqo, const void* 
  * projection and its attention.  Serves a decode step (one token of each sequence) and a prompt alike.
  *   K_dev, V_dev  [M x Hkv heads of D] (the cache's), pitches ldk, ldv
  *   slots_dev     int64 [M], the slot number of each token; negative: the token's key and value are not stored (padding).
- *                 Two tokens with one slot leave either's row there.
+ *                 What two tokens with one slot leave there is undefined (rows of either, head by head).
  *   Q_dev         NULL (Hq = 0), or [M x Hq heads of D];  Qo_dev as in patch_qk_norm_rope
  *   status_dev    PATCH_ERR_SIZE for a position outside the table (taken as 0) or a slot outside the cache (not stored)
  * One kernel.
@@ -584,6 +586,7 @@ int patch_kv_append(const patch_kv_cache_t* cache, const void* K_dev, int64_t ld
  * query head makes its row of O and its lse NaN and no other.
  *   cache             D = 64 or 128
  *   Q_dev, O_dev      [B T x Hq heads of D], pitches ldq, ldo;  Hq a multiple of the cache's Hkv
+ *   prefix_len        0 <= prefix_len <= 2^31 - 256
  *   prefix_pages_dev  int32 [ceil(prefix_len / page_size)] pages of the prefix, in order (NULL if prefix_len is 0)
  *   page_table_dev    int32 [B x ld_table]: row b lists the pages of sequence b's own keys, which start at slot 0 of the first
  *                     (entries past its length are not used)
@@ -593,7 +596,10 @@ int patch_kv_append(const patch_kv_cache_t* cache, const void* K_dev, int64_t ld
  *                     aligned, no initialisation needed
  *   status_dev        PATCH_ERR_SIZE: a length outside its range (clamped); PATCH_ERR_FORMAT: a page outside the cache (page 0
  *                     is read in its place); PATCH_ERR_TIMEOUT: a bounded wait expired.  O is undefined in the last two.
- * B <= 2048, B T Hq D < 2^31, 0 < scale <= 2e38 (scale log2(e) is an fp32 number).  Finite scores q.k may have any size.  Fixed lengths give fixed bits.  At most three launches, no host synchronisation.
+ * B <= 2048, B T Hq D < 2^31, 0 < scale <= 2e38 (scale log2(e) is an fp32 number).  Finite scores q.k may have any size.  Tiles are counted
+ * in 32 bits: PATCH_ERR_SHAPE where prefix and tables could hold 2^31 tiles of 64 keys over all key heads and blocks of query rows (it goes by
+ * the tables' width; 2048 sequences of 8 key heads may be 8 million keys wide each).  Fixed lengths give fixed bits.  At most three launches,
+ * no host synchronisation.
  */
 int patch_prefix_attention_workspace_size(const patch_kv_cache_t* cache, int64_t B, int T, int Hq, size_t* bytes_out);
 int patch_prefix_attention(const patch_kv_cache_t* cache, const void* Q_dev, int64_t ldq, int64_t B, int T, int Hq,

@@ -135,8 +135,8 @@ static bool block_suffixes(int64_t rows, int64_t keys) { return rows > kMostDeco
 
 // CTAs of a cluster for each item of the small problems that take one launch of their own (attn_direct_kernel), 0 for the others.
 // There every item reads the prefix for itself, so it is a matter of how many tiles there are in all (by the tables' width): up to
-// eight for each CTA that can run at once.  Measured, one launch against two or three, 13B heads: one sequence, 128 + 100 keys 5.1 us
-// against 8.3, 4096 + 100 keys (7 tiles a slot) 15.4 against 18.0, 4 x (1024 + 100) (8 a slot) 11.9 against 11.9; 8 key heads of 4
+// eight for each CTA that can run at once.  Measured on the same inputs call after call (from L2; one sequence of 128 + 64 keys that come
+// from HBM takes 5.9 us), one launch against two or three, 7B heads: one sequence, 128 + 100 keys 5.2 us against 8.3, 4096 + 100 keys (7 tiles a slot) 15.4 against 18.0, 4 x (1024 + 100) (8 a slot) 11.9 against 11.9; 8 key heads of 4
 // rows, 16 x (64 + 500) 9.0 us against 26.1 (32 rows or more of a prefix are the block kernel's otherwise).  A second wave of items
 // is worth it only where a prefix would be a launch of its own: 2 items a slot 14.6 us against 32.8 with one, 3 items a slot without 14.1
 // against 12.2.  Clusters of 16 (more than the portable 8) pay from four tiles a CTA: 71 tiles an item 10.4 us against 11.4, 16
@@ -242,6 +242,11 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     if (!workspace) return PATCH_ERR_NULL;
     if (workspace_bytes < need) return PATCH_ERR_SIZE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PATCH_ERR_ALIGN;
+    const Plan q = plan_of(cache, B, T, G, prefix_len, ld_table * cache->page_size);
+    auto tiles = [&](int keys) { return int((prefix_len + keys - 1) / keys); };
+    // units are counted in 32 bits
+    const int64_t own = (ld_table * cache->page_size + kDecodeKeys - 1) / kDecodeKeys + 8;
+    if (int64_t(cache->Hkv) * q.blocks_p * (int64_t(tiles(kDecodeKeys)) + 8) + B * own * cache->Hkv * q.blocks_s > 0x7FFFFFFF) return PATCH_ERR_SHAPE;
     if ((rc = check_device())) return rc;
     Problem p = {static_cast<const __nv_bfloat16*>(Q), ldq, int(B), T, cache->Hkv, G, prefix_pages, int(prefix_len), page_table,
                  ld_table, suffix_lens, 0, int(cache->num_pages), scale * 1.4426950408889634f, status_dev, 0u};
@@ -252,17 +257,11 @@ extern "C" int patch_prefix_attention(const patch_kv_cache_t* cache, const void*
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     if (const int split = direct_split(int64_t(T) * G, B * cache->Hkv, prefix_len, ld_table * cache->page_size))
         return launch_attn_direct(cache, p, split, static_cast<__nv_bfloat16*>(O), ldo, lse, s);
-    const Plan q = plan_of(cache, B, T, G, prefix_len, ld_table * cache->page_size);
     const Results to = {{reinterpret_cast<float*>(ws + q.o_p), reinterpret_cast<float2*>(ws + q.ml_p), reinterpret_cast<int2*>(ws), q.rows_p, q.block_p},
                         {reinterpret_cast<float*>(ws + q.o_s), reinterpret_cast<float2*>(ws + q.ml_s), reinterpret_cast<int2*>(ws + q.span_s), q.rows_s, q.block_s}};
     const bool prefix = prefix_len > 0;
-    auto tiles = [&](int keys) { return int((prefix_len + keys - 1) / keys); };
     const Line dec = {prefix && !q.block_p ? q.blocks_p : 0, q.block_s ? 0 : q.blocks_s, tiles(kDecodeKeys), kDecodeCost, 6};
     const Line blk = {prefix && q.block_p ? q.blocks_p : 0, q.block_s ? q.blocks_s : 0, tiles(kBlockKeys), kBlockCost, 7};
-    // units are counted in 32 bits
-    const int64_t own = (ld_table * cache->page_size + kDecodeKeys - 1) / kDecodeKeys + 8;
-    if (int64_t(cache->Hkv) * q.blocks_p * (int64_t(dec.tiles_p) + 8) + B * own * cache->Hkv * q.blocks_s > 0x7FFFFFFF)
-        return PATCH_ERR_SHAPE;
     const bool use_block = blk.blocks_p || blk.blocks_s, use_decode = dec.blocks_p || dec.blocks_s;
     if (use_block && (rc = launch_attn_block(cache, p, blk, to, use_decode, s))) return rc;
     if (use_decode && (rc = launch_attn_decode(cache, p, dec, to, use_block, s))) return rc;

@@ -266,7 +266,7 @@ constexpr int kDecodeKeys = 64, kBlockKeys = 128;     // keys of a tile
 constexpr int kDecodeCost = 1, kBlockCost = 3;        // Line::cost
 constexpr int kMaxShares = 4 * kMaxSms;               // CTAs of one launch, at most
 int launch_attn_decode(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool after_block, cudaStream_t s);
-// one launch for everything: clusters of `split` CTAs (1, 2, 4 or 8)
+// one launch for everything: clusters of `split` CTAs (1, 2, 4, 8 or 16; 16 is more than the portable size and allowed explicitly)
 int launch_attn_direct(const patch_kv_cache_t* c, const Problem& p, int split, __nv_bfloat16* O, int64_t ldo, float* lse, cudaStream_t s);
 int launch_attn_block(const patch_kv_cache_t* c, const Problem& p, const Line& w, const Results& to, bool decode_follows, cudaStream_t s);
 

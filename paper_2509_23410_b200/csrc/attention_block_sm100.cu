@@ -158,7 +158,8 @@ __device__ __forceinline__ float probabilities(uint32_t t_s, int left, bool part
 // kernel ends with the decode kernel, which streams from the other SMs meanwhile -- one is short of arithmetic, the other of
 // bandwidth.  Cycles measured: 2 000 for a tile, 3 300 where HBM is waited for (one block of rows), 11 000 for an
 // item's queries and result (left out, 16 sequences of 40 heads behind 4 keys took 167 us instead of 62: forty items on four SMs),
-// 700 for a tile of the decode kernel (two CTAs share its latencies); bandwidth in bytes per cycle of 6.5 TB/s at 1.9 GHz.  64
+// 700 for a tile of the decode kernel (two CTAs share its latencies; each sequence's keys are counted once, though for 17 to 64 rows of
+// a sequence the decode kernel walks them once per 16 rows, from L2: its work is then taken for less than it is); bandwidth in bytes per cycle of 6.5 TB/s at 1.9 GHz.  64
 // sequences behind 32768 keys (8 key heads): 80 us against 101 with the block kernel on all SMs first.
 template <int D>
 __device__ __forceinline__ int sms_beside_decode(const Problem& p, const Line& w, float keys, int sms) {

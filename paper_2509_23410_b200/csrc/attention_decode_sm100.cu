@@ -5,7 +5,7 @@
 // o = sum 2^((s - m) scale) v; parts of the keys are joined with weights 2^((m_i - m) scale) (softmax_rule.cuh).  All three are fp32; the
 // probabilities are rounded to bf16 for the product with V (they are at most 1; the sum takes them unrounded).
 //
-// Kernel.  Every CTA, two to an SM, walks over its share of the work list (attention.cuh).  Warp 4 alone knows the list: it requests tiles
+// Kernel.  Every CTA, two to an SM (one for more than 1231 sequences of heads of 128), walks over its share of the work list (attention.cuh).  Warp 4 alone knows the list: it requests tiles
 // of 64 keys and values with TMA, one copy per page and operand, into a ring of stages, and with an item's first tile the
 // item's query rows; a note in the stage says what the tile is.  Warps 0..3 each take 16 of the 64 keys: S = Q K^T
 // (16 rows x 16 keys), probabilities in registers, O += P V, with a maximum of their own, so that within an item no warp waits
@@ -385,7 +385,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 // Small problems, in one launch and without partial results in memory: a cluster of CTAs owns a block of one sequence's rows of a key
 // head, its CTAs take equal parts of the tiles of the prefix and of the sequence's own keys, and join in distributed shared memory.  The
 // prefix is read by every sequence (from L2 after the first), which is cheap as long as all there is to read is a few tiles per CTA:
-// one sequence behind 128 keys of the 7B shape 8.3 us -> 5.1.  What is left is one chain: barriers, page numbers, a tile from HBM, its products, two joins.
+// one sequence behind 128 keys of the 7B shape 8.3 us -> 5.2 with its inputs in L2.  What is left is one chain: barriers, page numbers, a tile from HBM, its products, two joins.
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2)
 attn_direct_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p, const int split,

@@ -168,3 +168,17 @@ def test_attention_scale_bound(B):
     need = B.patch_prefix_attention_workspace_size(c, 3, 1, 8)
     call = lambda scale: L.patch_prefix_attention(c, FAKE, 1024, 3, 1, 8, FAKE, 100, FAKE, 4, FAKE, scale, FAKE, 1024, None, FAKE, need - 1, None, None)  # noqa: E731
     assert call(2.5e38) == B.ERR_SHAPE and call(1.9e38) == B.ERR_SIZE
+
+
+def test_attention_counts_tiles_in_32_bits(B):
+    """Refused before a device is touched, and only where the count would not fit."""
+    L, c = B.lib(), cache(B, Hkv=8, page_stride=8 * 16 * 128)
+    need = B.patch_prefix_attention_workspace_size(c, 2048, 1, 8)
+    call = lambda n, P, ld: L.patch_prefix_attention(c, FAKE, 1024, n, 1, 8, FAKE, P, FAKE, ld, FAKE, 0.1, FAKE, 1024, None, FAKE, need, FAKE, None)  # noqa: E731
+    wide = 8 * 1024 * 1024 // 16                              # pages of 16 keys: 8 million keys
+    assert call(2048, 0, wide) == B.ERR_SHAPE and call(2048, 1 << 30, 4) == B.ERR_SHAPE and call(1, 100, 0x7FFFFFFF) == B.ERR_SHAPE
+    import torch
+    if not torch.cuda.is_available():                         # these are let through: the missing device is what is reported
+        for args in ((2048, 0, wide - 600), (2047, 1 << 23, wide - 4200), (1, 0x7FFFFF00, 4)):
+            assert call(*args) in (B.ERR_CUDA, B.ERR_ARCH), args
+    assert call(1, 0x7FFFFF01, 4) == B.ERR_SHAPE
