@@ -510,7 +510,7 @@ typedef struct patch_rope_t {
  * so a page holds, head by head, page_size rows of D.  Keys and values may share one buffer (page_stride counts the
  * elements from one page of keys to the next).
  *   page_size  a power of two, 16 .. 256;  page_stride >= Hkv * page_size * D, a multiple of 8;  D a multiple of 8, <= 256
- * "Slot number" below means p * page_size + s.
+ * "Slot number" below means p * page_size + s.  (patch_prefix_attention reads caches of D = 64 and 128.)
  */
 typedef struct patch_kv_cache_t {
     void* k_dev;
