@@ -152,6 +152,20 @@ def _stream(stream=None):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _empty(stream, shape, dtype, device):
+    """Memory for a call that runs on ``stream``, from that stream's share of torch's allocator.  From the current stream's it could be in use
+    there still, and be given away there when the last reference goes (a workspace's: on return), while the kernels run on ``stream``."""
+    torch = _torch
+    if torch is None:
+        import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):             # any object with a handle will do for the launch
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _flags_buf(flags):
     import numpy as np
     f = np.ascontiguousarray(flags, dtype=np.uint8).reshape(-1)
@@ -173,7 +187,7 @@ def patch_pack(W, flags, layout: Layout | None = None, out=None, stream=None):
     if layout is None:
         layout = patch_packed_size(N, K, flags)
     if out is None:
-        out = torch.empty(layout.total_bytes, dtype=torch.uint8, device=W.device)
+        out = _empty(stream, layout.total_bytes, torch.uint8, W.device)
     f, fp = _flags_buf(flags)
     _check(lib().patch_pack(_ptr(W), W.stride(0), fp, ctypes.byref(layout), _ptr(out), out.numel(),
                             _stream(stream)), "patch_pack")
@@ -183,7 +197,7 @@ def patch_pack(W, flags, layout: Layout | None = None, out=None, stream=None):
 def patch_unpack(layout: Layout, packed, out=None, stream=None):
     import torch
     if out is None:
-        out = torch.empty((layout.N, layout.K), dtype=torch.bfloat16, device=packed.device)
+        out = _empty(stream, (layout.N, layout.K), torch.bfloat16, packed.device)
     _check(lib().patch_unpack(ctypes.byref(layout), _ptr(packed), _ptr(out), out.stride(0), _stream(stream)),
            "patch_unpack")
     return out
@@ -207,7 +221,7 @@ def patch_gemm(X, layout: Layout, packed, Y=None, workspace=None, status=None, s
     assert X.is_cuda and X.dtype == torch.bfloat16 and X.dim() == 2 and (X.shape[0] == 0 or X.stride(1) == 1)
     M = X.shape[0]
     if Y is None:
-        Y = torch.empty((M, layout.N), dtype=torch.bfloat16, device=X.device)
+        Y = _empty(stream, (M, layout.N), torch.bfloat16, X.device)
     ws_bytes = workspace.numel() if workspace is not None else 0
     _check(lib().patch_gemm_ex(_ptr(X), X.stride(0) if M else layout.K, M, ctypes.byref(layout), _ptr(packed),
                                _ptr(Y), Y.stride(0) if M else layout.N, _ptr(workspace), ws_bytes,
@@ -239,7 +253,7 @@ def patch_gemm_gated(X, layout: Layout, packed, Y=None, workspace=None, status=N
     import torch
     M = X.shape[0]
     if Y is None:
-        Y = torch.empty((M, layout.N // 2), dtype=torch.bfloat16, device=X.device)
+        Y = _empty(stream, (M, layout.N // 2), torch.bfloat16, X.device)
     ws_bytes = workspace.numel() if workspace is not None else 0
     _check(lib().patch_gemm_gated(_ptr(X), X.stride(0) if M else layout.K, M, ctypes.byref(layout), _ptr(packed),
                                   _ptr(Y), Y.stride(0) if M else layout.N // 2, _ptr(workspace), ws_bytes,
@@ -316,9 +330,9 @@ def patch_hard_mask(P_tile, P24, N: int, K: int, flags_out=None, patterns_out=No
     assert P_tile.is_cuda and P_tile.dtype == torch.float32 and P_tile.is_contiguous()
     assert P24.is_cuda and P24.dtype == torch.float32 and P24.is_contiguous() and tuple(P24.shape) == (6, N * K // 4)
     if flags_out is None:
-        flags_out = torch.empty((N // 128) * (K // 128), dtype=torch.uint8, device=P24.device)
+        flags_out = _empty(stream, (N // 128) * (K // 128), torch.uint8, P24.device)
     if patterns_out is None:
-        patterns_out = torch.empty(N * K // 4, dtype=torch.uint8, device=P24.device)
+        patterns_out = _empty(stream, N * K // 4, torch.uint8, P24.device)
     _check(lib().patch_hard_mask(_ptr(P_tile), _ptr(P24), N, K, 128, 128, _ptr(flags_out), _ptr(patterns_out),
                                  _stream(stream)), "patch_hard_mask")
     return flags_out, patterns_out
@@ -334,7 +348,7 @@ def patch_pack_patterns(W, flags, patterns, layout: Layout | None = None, out=No
     if layout is None:
         layout = patch_packed_size(N, K, flags)
     if out is None:
-        out = torch.empty(layout.total_bytes, dtype=torch.uint8, device=W.device)
+        out = _empty(stream, layout.total_bytes, torch.uint8, W.device)
     f, fp = _flags_buf(flags)
     _check(lib().patch_pack_patterns(_ptr(W), W.stride(0), fp, _ptr(patterns), ctypes.byref(layout), _ptr(out),
                                      out.numel(), _ptr(status), _stream(stream)), "patch_pack_patterns")
@@ -357,11 +371,11 @@ def patch_soft_mask(W, P_tile, P24, tau: float, kappa: float, seed: int = 0, fla
     assert P_tile.is_cuda and P_tile.dtype == torch.float32 and P_tile.is_contiguous()
     assert P24.is_cuda and P24.dtype == torch.float32 and P24.is_contiguous() and tuple(P24.shape) == (6, N * K // 4)
     if Wt is None:
-        Wt = torch.empty((N, K), dtype=torch.bfloat16, device=W.device)
+        Wt = _empty(stream, (N, K), torch.bfloat16, W.device)
     if sums is None:
-        sums = torch.empty(4, dtype=torch.float64, device=W.device)
+        sums = _empty(stream, 4, torch.float64, W.device)
     if workspace is None:
-        workspace = torch.empty(patch_soft_mask_workspace_size(N, K), dtype=torch.uint8, device=W.device)
+        workspace = _empty(stream, patch_soft_mask_workspace_size(N, K), torch.uint8, W.device)
     assert Mt is None or (Mt.is_cuda and Mt.dtype == torch.float32 and Mt.stride(1) == 1)
     _check(lib().patch_soft_mask(_ptr(W), W.stride(0), _ptr(P_tile), _ptr(P24), N, K, 128, 128, float(tau),
                                  float(kappa), int(seed) & 0xFFFFFFFFFFFFFFFF, int(flags), _ptr(Wt), Wt.stride(0),
@@ -401,9 +415,9 @@ def patch_soft_mask_backward(W, P_tile, P24, tau: float, kappa: float, Gw, c1: f
     assert P_tile.is_cuda and P_tile.dtype == torch.float32 and P_tile.is_contiguous()
     assert P24.is_cuda and P24.dtype == torch.float32 and P24.is_contiguous() and tuple(P24.shape) == (6, N * K // 4)
     if gP_tile is None:
-        gP_tile = torch.empty_like(P_tile)
+        gP_tile = _empty(stream, P_tile.shape, torch.float32, P_tile.device)
     if gP24 is None:
-        gP24 = torch.empty_like(P24)
+        gP24 = _empty(stream, P24.shape, torch.float32, P24.device)
     _check(lib().patch_soft_mask_backward(_ptr(W), W.stride(0), _ptr(P_tile), _ptr(P24), N, K, 128, 128, float(tau),
                                           float(kappa), int(seed) & 0xFFFFFFFFFFFFFFFF, int(flags), _ptr(Gw), Gw.stride(0),
                                           float(c1), float(c2), _ptr(gP_tile), _ptr(gP24), _stream(stream)),
@@ -421,7 +435,7 @@ def patch_pack_dev(W, flags_dev, patterns=None, out=None, status=None, stream=No
     T = (N // 128) * (K // 128)
     assert flags_dev.numel() == T
     if out is None:
-        out = torch.empty((256 + 16 * T + 1023) // 1024 * 1024 + T * 32768, dtype=torch.uint8, device=W.device)
+        out = _empty(stream, (256 + 16 * T + 1023) // 1024 * 1024 + T * 32768, torch.uint8, W.device)
     _check(lib().patch_pack_dev(_ptr(W), W.stride(0), _ptr(flags_dev), _ptr(patterns), N, K, 128, 128, _ptr(out),
                                 out.numel(), _ptr(status), _stream(stream)), "patch_pack_dev")
     return out
@@ -458,15 +472,6 @@ def _use_torch():
 
 def _stream_of(x, stream):
     return _raw_stream(x.get_device()) if stream is None else stream.cuda_stream
-
-
-def _empty(stream, shape, dtype, device):
-    """Memory for a call that runs on ``stream``, from that stream's share of torch's allocator.  From the current stream's it could be in use
-    there still, and be given away there when the last reference goes (a workspace's: on return), while the kernels run on ``stream``."""
-    if stream is None:
-        return _torch.empty(shape, dtype=dtype, device=device)
-    with _torch.cuda.stream(stream):
-        return _torch.empty(shape, dtype=dtype, device=device)
 
 
 def patch_rope(cos_sin, interleaved: bool = False) -> Rope:

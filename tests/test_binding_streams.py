@@ -8,6 +8,14 @@ import pytest
 torch = pytest.importorskip("torch")
 
 
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+    def __eq__(self, other):
+        return isinstance(other, Stream) and other.cuda_stream == self.cuda_stream
+
+
 class Recorder:
     """What torch.empty and torch.cuda.stream do, as far as the binding uses them: a tensor knows the stream it was allocated for."""
 
@@ -24,7 +32,7 @@ class Recorder:
 
             def __exit__(self, *a):
                 rec.now = self.before
-        self.cuda = types.SimpleNamespace(stream=On)
+        self.cuda = types.SimpleNamespace(stream=On, Stream=Stream, ExternalStream=lambda handle, device: Stream(handle))
         self.uint8, self.float32 = torch.uint8, torch.float32
 
     def empty(self, shape, dtype=None, device=None):
@@ -32,7 +40,7 @@ class Recorder:
         return types.SimpleNamespace(shape=shape)
 
 
-@pytest.mark.parametrize("stream", [None, types.SimpleNamespace(cuda_stream=77)])
+@pytest.mark.parametrize("stream", [None, Stream(77), types.SimpleNamespace(cuda_stream=77)])
 def test_own_memory_belongs_to_the_calls_stream(monkeypatch, stream):
     from paper_2509_23410_b200 import build
     build.build()
@@ -56,7 +64,7 @@ def test_own_memory_belongs_to_the_calls_stream(monkeypatch, stream):
     B.patch_kv_append(cache, x, x, None, Q=x, stream=stream)                             # the queries
     B.patch_prefix_attention(cache, x, None, 0, table, None, stream=stream)              # the result, a workspace
     assert launched == [5 if stream is None else 77] * 4
-    assert rec.made == ["current" if stream is None else stream] * 10
+    assert rec.made == ["current" if stream is None else Stream(77)] * 10
 
 
 @pytest.mark.gpu
@@ -86,3 +94,47 @@ def test_streams_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     for i, *r in got:
         assert all(torch.equal(a, b) for a, b in zip(r, want[i]))
+
+
+@pytest.mark.gpu
+def test_every_call_allocates_for_its_stream(monkeypatch):
+    """The calls on weights and masks as well: each of them asks for its memory with the stream that it runs on, and is right there."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2509_23410_b200 import build, binding as B
+    build.build()
+    real, seen = B._empty, []
+
+    def empty(stream, *a):
+        seen.append(stream)
+        return real(stream, *a)
+    monkeypatch.setattr(B, "_empty", empty)
+    N = K = 256
+    g = torch.Generator(device="cuda").manual_seed(1)
+    W, X, Gw = (torch.randn(r, K, generator=g, device="cuda").bfloat16() for r in (N, 5, N))
+    P_tile, P24 = torch.randn(2, 2, generator=g, device="cuda"), torch.randn(6, N * K // 4, generator=g, device="cuda")
+    flags = [0, 1, 1, 0]
+    workspace = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    flags_dev = torch.tensor(flags, dtype=torch.uint8, device="cuda")
+
+    def calls(stream):
+        packed, layout = B.patch_pack(W, flags, stream=stream)
+        kw = dict(workspace=workspace, stream=stream)
+        hard, patterns = B.patch_hard_mask(P_tile, P24, N, K, stream=stream)
+        return [packed, B.patch_unpack(layout, packed, stream=stream), B.patch_gemm(X, layout, packed, **kw),
+                B.patch_gemm_gated(X, layout, packed, **kw), hard, patterns, B.patch_pack_patterns(W, flags, patterns, stream=stream)[0],
+                *B.patch_soft_mask(W, P_tile, P24, 1.0, 1.0, stream=stream),
+                *B.patch_soft_mask_backward(W, P_tile, P24, 1.0, 1.0, Gw, 0.1, 0.1, stream=stream),
+                B.patch_unpack(layout, B.patch_pack_dev(W, flags_dev, stream=stream), stream=stream)]
+    want = calls(None)
+    torch.cuda.synchronize()
+    count = len(seen)
+    assert seen == [None] * count and count >= len(want)
+    s = torch.cuda.Stream()
+    for stream in (s, types.SimpleNamespace(cuda_stream=s.cuda_stream)):
+        seen.clear()
+        s.wait_stream(torch.cuda.current_stream())
+        got = calls(stream)
+        torch.cuda.synchronize()
+        assert len(seen) == count and all(t is stream for t in seen)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
