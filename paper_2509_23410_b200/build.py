@@ -49,8 +49,8 @@ def build_marshal(force: bool = False) -> str:
 
 def build(force: bool = False, verbose: bool = False, fault_injection: bool = False) -> str:
     """The library; with ``fault_injection`` the test build ``libpatch_b200_fi.so`` (same sources with
-    -DPATCH_FAULT_INJECTION: device-side waits give up after 300 us, and the stream-K decode kernel can be told,
-    through its status word, to announce bytes that never arrive -- how the tests make a bounded wait run out).  The library
+    -DPATCH_FAULT_INJECTION: device-side waits give up after 300 us, and decode and attention kernels can be told,
+    through their status word, to announce bytes that never arrive -- how the tests make a bounded wait run out).  The library
     needs nvcc alone.  The module for torch's tensors is built along with it where torch and its headers are; where it cannot be, that is
     said on stderr and the binding's calls that use it raise."""
     lib = LIB_FI if fault_injection else LIB
