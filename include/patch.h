@@ -607,6 +607,76 @@ int patch_prefix_attention(const patch_kv_cache_t* cache, const void* Q_dev, int
                            int64_t ld_table, const int32_t* suffix_lens_dev, float scale, void* O_dev, int64_t ldo,
                            float* lse_dev, void* workspace_dev, size_t workspace_bytes, int* status_dev, void* stream);
 
+/* =========================================================================================
+ * From logits to a loss: L_LM of Eq. 5 and its gradient, evaluation, and distillation from the dense model.
+ * Logits are rows of V values, bf16 or fp32, with a pitch (ld) that is a multiple of 8 elements; columns from V on are neither
+ * read nor written.  1 <= V <= 2^20, M < 2^31.  Arithmetic, sums and results other than gradients (which have the logits' type and are rounded
+ * once) are fp32; sums are taken in an order that depends on the arguments only: equal calls give equal bits.  The distribution of a row z is
+ * p = softmax(z / temperature), 0 < temperature < inf (and its reciprocal an fp32 number).  Logits of -inf are masked: probability 0,
+ * gradient 0.  A row of nothing but -inf has no distribution: lse and log probabilities -inf, entropy 0, gradients 0.  NaN or +inf in a
+ * row makes that row's results NaN and no other's.  The launches are ordinary ones in the sense of the section above.
+ * ========================================================================================= */
+enum { PATCH_LOGITS_BF16 = 0, PATCH_LOGITS_F32 = 1 };
+
+/*
+ * Log probabilities of given tokens, entropies and the most likely alternatives of M rows, in one pass over the logits:
+ *     lse = ln sum exp(z / T),   logp = z_token / T - lse,   entropy = - sum p ln p,
+ *     top_ids: the k largest logits' columns, largest first, equal ones by the lower column (NaN counts as -inf);  top_logp: their log probabilities.
+ *   tokens_dev   int64 [M] or NULL; negative: the row does not count, logp 0.  logp_dev fp32 [M], given exactly if tokens are
+ *   entropy_dev, lse_dev   fp32 [M] or NULL (lse is what the gradient reads)
+ *   k            0 .. 256, at most V;  top_ids_dev int32 [M x k], top_logp_dev fp32 [M x k] (NULL where k is 0)
+ *   status_dev   optional device int (zero before the call): PATCH_ERR_SIZE if a token is V or more (the row then does not count)
+ * One kernel, no workspace.
+ */
+int patch_token_logprobs(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int64_t V, const int64_t* tokens_dev, int k,
+                         float temperature, float* logp_dev, float* entropy_dev, float* lse_dev, int32_t* top_ids_dev,
+                         float* top_logp_dev, int* status_dev, void* stream);
+
+/*
+ * Gradient of sum_m glogp[m] logp[m] + gentropy[m] entropy[m] with respect to the logits:
+ *     gz_v = (1 / T) [ glogp (1[v = token] - p_v) - gentropy p_v (ln p_v + entropy) ]
+ *   glogp_dev    fp32 [M] or NULL; with it tokens_dev as in the forward call (rows that do not count have no gradient from it)
+ *   gentropy_dev fp32 [M] or NULL; with it entropy_dev, the forward call's
+ *   lse_dev      the forward call's
+ *   gZ_dev       same type as Z; may be Z_dev itself with the same pitch.  Rows whose two factors are 0 become 0, whatever their logits.
+ */
+int patch_token_logprobs_backward(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int64_t V, const int64_t* tokens_dev,
+                                  float temperature, const float* lse_dev, const float* glogp_dev, const float* entropy_dev,
+                                  const float* gentropy_dev, void* gZ_dev, int64_t ldg, int* status_dev, void* stream);
+
+/* patch_distill_loss flag: what the teacher's list leaves of its probability is one more class. */
+enum { PATCH_DISTILL_REST = 1 };
+
+/*
+ * Distillation from a teacher's top logits: the cross entropy of the student's rows with the teacher's listed probabilities.  (It differs from
+ * the divergence by the teacher's entropy, which has no gradient and whose subtraction would leave nothing of a small divergence in fp32.)
+ * Entry i of a row is a column id_i and the teacher's logit or log probability t_i, already divided by the temperature:
+ *     without PATCH_DISTILL_REST   q_i = exp(t_i) / sum_j exp(t_j),   loss = - sum_i q_i ln p_{id_i}
+ *     with PATCH_DISTILL_REST      q_i = exp(t_i),  q_r = max(0, 1 - sum_i q_i),  p_r = sum of p_v over the columns not listed,
+ *                                  loss = - sum_i q_i ln p_{id_i} - q_r ln p_r
+ * patch_token_logprobs of the teacher's logits at the same temperature writes such lists (its log probabilities serve both forms).  One entry of
+ * log probability 0 per row is the ordinary cross entropy.
+ *   ids_dev      int32 [M x K], 1 <= K <= 256; negative: no entry.  Entries with one id add up.  A row without entries (or with
+ *                t = -inf in all of them) has loss and gradient 0 in the first form.
+ *   t_dev        fp32 [M x K]
+ *   loss_dev     fp32 [M]
+ *   stats_dev    NULL or fp32 [M x 2], what the gradient's own call reads
+ *   gZ_dev       NULL, or the gradient of sum_m gloss[m] loss[m] in the same launch (the logits are read from HBM once): same type as
+ *                Z, pitch ldg; may be Z_dev itself with the same pitch.  Rows with gloss = 0 become 0, whatever their logits
+ *   gloss_dev    fp32 [M], NULL: all 1
+ *   status_dev   PATCH_ERR_SIZE if an id is V or more (no entry then)
+ * One kernel, no workspace.
+ */
+int patch_distill_loss(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int64_t V, const int32_t* ids_dev, const float* t_dev,
+                       int K, float temperature, int flags, float* loss_dev, float* stats_dev, const float* gloss_dev,
+                       void* gZ_dev, int64_t ldg, int* status_dev, void* stream);
+
+/* The gradient by itself, for a gloss that is known only later: from the stats of the forward call.  gZ_dev is not Z_dev
+ * (PATCH_ERR_SHAPE). */
+int patch_distill_loss_backward(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int64_t V, const int32_t* ids_dev,
+                                const float* t_dev, int K, float temperature, int flags, const float* stats_dev,
+                                const float* gloss_dev, void* gZ_dev, int64_t ldg, int* status_dev, void* stream);
+
 /* Human-readable text for a status code (static storage). */
 const char* patch_strerror(int status);
 

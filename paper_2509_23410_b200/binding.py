@@ -32,8 +32,11 @@ EXPORTS = ["patch_packed_size", "patch_pack", "patch_unpack", "patch_gemm_worksp
            "patch_mask_regularizers", "patch_mask_regularizer_coefficients", "patch_soft_mask_backward",
            "patch_qk_norm_rope", "patch_qk_norm_rope_backward_workspace_size", "patch_qk_norm_rope_backward",
            "patch_kv_append", "patch_prefix_attention_workspace_size", "patch_prefix_attention",
+           "patch_token_logprobs", "patch_token_logprobs_backward", "patch_distill_loss", "patch_distill_loss_backward",
            "patch_strerror", "patch_version"]
 MASK_NO_NOISE = 1
+LOGITS_BF16, LOGITS_F32 = 0, 1
+DISTILL_REST = 1
 
 
 class Layout(ctypes.Structure):
@@ -114,13 +117,18 @@ def load(path: str) -> ctypes.CDLL:
         L.patch_kv_append.argtypes = [cp, vp, i64, vp, i64, vp, i64, vp, f32, rp, vp, vp, i64, i32, vp, vp, i64, vp, vp]
         L.patch_prefix_attention_workspace_size.argtypes = [cp, i64, i32, i32, ctypes.POINTER(sz)]
         L.patch_prefix_attention.argtypes = [cp, vp, i64, i64, i32, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, vp, sz, vp, vp]
+        L.patch_token_logprobs.argtypes = [vp, i64, i32, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp, vp, vp]
+        L.patch_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp, vp]
+        L.patch_distill_loss.argtypes = [vp, i64, i32, i64, i64, vp, vp, i32, f32, i32, vp, vp, vp, vp, i64, vp, vp]
+        L.patch_distill_loss_backward.argtypes = [vp, i64, i32, i64, i64, vp, vp, i32, f32, i32, vp, vp, vp, i64, vp, vp]
         L.patch_strerror.argtypes = [ctypes.c_int]
         L.patch_strerror.restype = ctypes.c_char_p
         for name in EXPORTS:
             if name != "patch_strerror":
                 getattr(L, name).restype = ctypes.c_int
         # addresses for the calls that do not go through ctypes (see csrc/marshal.cpp)
-        for name in ("patch_qk_norm_rope", "patch_qk_norm_rope_backward", "patch_kv_append", "patch_prefix_attention"):
+        for name in ("patch_qk_norm_rope", "patch_qk_norm_rope_backward", "patch_kv_append", "patch_prefix_attention",
+                     "patch_token_logprobs", "patch_token_logprobs_backward", "patch_distill_loss", "patch_distill_loss_backward"):
             setattr(L, "at_" + name, ctypes.cast(getattr(L, name), vp).value)
     return L
 
@@ -578,3 +586,89 @@ def patch_prefix_attention(cache: KVCache, Q, prefix_pages, prefix_len: int, pag
     if rc:
         _check(rc, "patch_prefix_attention")
     return O
+
+
+# ---------------------------------------------------------------------------------------------
+# From logits to a loss: log probabilities of tokens, entropy, alternatives; distillation from a teacher's list.
+#
+# Logits are bf16 or float32 [M, V] with contiguous rows, any pitch that is a multiple of eight elements.  The calls run on the tensors'
+# device, whichever is the current one.
+
+def _rows_like(Z, stream):
+    """Memory for a gradient of Z [M, V]: rows of a pitch that the library takes."""
+    M, V = Z.shape
+    return _empty(stream, (M, (V + 7) // 8 * 8), Z.dtype, Z.device)[:, :V]
+
+
+def patch_token_logprobs(Z, tokens=None, k: int = 0, temperature: float = 1.0, logp=None, entropy=None, lse=None, top_ids=None,
+                         top_logp=None, status=None, stream=None):
+    """Log probabilities of ``tokens`` (int64 [M]; negative: the row does not count, 0) under softmax(Z / temperature), and the ``k`` most
+    likely alternatives of every row: returns (logp, entropy, lse, top_ids, top_logp).  ``logp`` is None without tokens, ``top_ids`` (int32) and
+    ``top_logp`` [M, k] without k; ``entropy`` and ``lse`` (float32 [M]) are written if given, made if True."""
+    if _torch is None:
+        _use_torch()
+    assert Z.is_cuda and Z.dim() == 2, "logits are CUDA tensors [rows, columns]"
+    M = Z.shape[0]
+    if logp is None and tokens is not None:
+        logp = _empty(stream, M, _torch.float32, Z.device)
+    if entropy is True:
+        entropy = _empty(stream, M, _torch.float32, Z.device)
+    if lse is True:
+        lse = _empty(stream, M, _torch.float32, Z.device)
+    if k > 0 and top_ids is None:
+        top_ids = _empty(stream, (M, k), _torch.int32, Z.device)
+    if k > 0 and top_logp is None:
+        top_logp = _empty(stream, (M, k), _torch.float32, Z.device)
+    rc = _marshal.token_logprobs((_lib or lib()).at_patch_token_logprobs, Z, tokens, k, temperature, logp, entropy, lse, top_ids, top_logp, status,
+                                 _stream_of(Z, stream))
+    if rc:
+        _check(rc, "patch_token_logprobs")
+    return logp, entropy, lse, top_ids, top_logp
+
+
+def patch_token_logprobs_backward(Z, tokens, lse, glogp=None, entropy=None, gentropy=None, temperature: float = 1.0, gZ=None, status=None,
+                                  stream=None):
+    """Gradient of sum(glogp * logp) + sum(gentropy * entropy) with respect to the logits, from the forward call's ``lse`` (and
+    ``entropy``): returns gZ (which may be Z itself)."""
+    if _torch is None:
+        _use_torch()
+    assert Z.is_cuda and Z.dim() == 2, "logits are CUDA tensors [rows, columns]"
+    if gZ is None:
+        gZ = _rows_like(Z, stream)
+    rc = _marshal.token_logprobs_backward((_lib or lib()).at_patch_token_logprobs_backward, Z, tokens, temperature, lse, glogp, entropy, gentropy, gZ,
+                                          status, _stream_of(Z, stream))
+    if rc:
+        _check(rc, "patch_token_logprobs_backward")
+    return gZ
+
+
+def patch_distill_loss(Z, top_ids, top_logp, temperature: float = 1.0, rest: bool = False, loss=None, stats=None, gloss=None, gZ=None, status=None,
+                       stream=None):
+    """Cross entropy of the rows of Z [M, V] with a teacher's list (int32 ``top_ids`` and float32 ``top_logp`` [M, K], at the same
+    temperature), renormalised or, with ``rest``, with what the list leaves as one more class: returns loss float32 [M].  ``gZ`` takes the gradient of
+    sum(gloss * loss) if given (it may be Z itself); ``stats`` float32 [M, 2] what ``patch_distill_loss_backward`` reads."""
+    if _torch is None:
+        _use_torch()
+    assert Z.is_cuda and Z.dim() == 2, "logits are CUDA tensors [rows, columns]"
+    if loss is None:
+        loss = _empty(stream, Z.shape[0], _torch.float32, Z.device)
+    rc = _marshal.distill_loss((_lib or lib()).at_patch_distill_loss, Z, top_ids, top_logp, temperature, DISTILL_REST if rest else 0, loss, stats, gloss,
+                               gZ, status, _stream_of(Z, stream))
+    if rc:
+        _check(rc, "patch_distill_loss")
+    return loss
+
+
+def patch_distill_loss_backward(Z, top_ids, top_logp, stats, gloss=None, temperature: float = 1.0, rest: bool = False, gZ=None, status=None,
+                                stream=None):
+    """Gradient of sum(gloss * loss) with respect to the logits from the forward call's ``stats``: returns gZ (not Z itself)."""
+    if _torch is None:
+        _use_torch()
+    assert Z.is_cuda and Z.dim() == 2, "logits are CUDA tensors [rows, columns]"
+    if gZ is None:
+        gZ = _rows_like(Z, stream)
+    rc = _marshal.distill_loss_backward((_lib or lib()).at_patch_distill_loss_backward, Z, top_ids, top_logp, temperature, DISTILL_REST if rest else 0,
+                                        stats, gloss, gZ, status, _stream_of(Z, stream))
+    if rc:
+        _check(rc, "patch_distill_loss_backward")
+    return gZ

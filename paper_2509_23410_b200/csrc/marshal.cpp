@@ -1,11 +1,12 @@
 // Takes torch tensors apart for the calls whose kernels run only a few microseconds (patch_qk_norm_rope, its gradient,
-// patch_kv_append, patch_prefix_attention): a CPython module that checks types, shapes and strides and calls the C ABI by address.
+// patch_kv_append, patch_prefix_attention, and those from logits to a loss): a CPython module that checks types, shapes and strides and calls the C ABI by address.
 // Nothing else happens here -- no allocation, no kernels; the checks of sizes, alignment and device are the library's own.
 // Why not ctypes: a call with four tensors of heads and twenty arguments spent 4 us in Python attribute look-ups and argument
 // conversion, as much again as the launch (8.8 us against 4.6 us for a decode step's 64 tokens appended, whose kernel takes 3.4).
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <ATen/core/Tensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include "../../include/patch.h"
 
@@ -187,11 +188,145 @@ PyObject* prefix_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// Rows of logits [M, V], bf16 or fp32, any pitch.
+constexpr const char* kLogits = "logits are bf16 or float32 CUDA tensors [rows, columns] whose rows are contiguous";
+struct Logits { void* p = nullptr; int64_t ld = 0, M = -1, V = -1; int type = -1; };
+Logits logits(PyObject* o) {
+    Logits r;
+    const at::Tensor* t = tensor(o, kLogits);
+    if (!t) return r;
+    if (!t->is_cuda() || t->dim() != 2 || (t->scalar_type() != at::kBFloat16 && t->scalar_type() != at::kFloat)) throw Bad{kLogits};
+    r.type = t->scalar_type() == at::kFloat ? PATCH_LOGITS_F32 : PATCH_LOGITS_BF16;
+    r.M = t->size(0);
+    r.V = t->size(1);
+    if (r.V > 1 && t->stride(1) != 1) throw Bad{kLogits};
+    r.p = t->data_ptr();
+    r.ld = r.M > 1 ? t->stride(0) : (r.V + 7) / 8 * 8;
+    return r;
+}
+void same(const Logits& a, const Logits& b) {
+    if (b.p && (a.M != b.M || a.V != b.V || a.type != b.type)) throw Bad{"gradients have the logits' shape and type"};
+}
+int whole(PyObject* o, const char* what) {
+    const long v = PyLong_AsLong(o);
+    if (v < -(1l << 30) || v > (1l << 30)) throw Bad{what};
+    return int(v);
+}
+// All tensors among the arguments are on the first one's device, which is the current one while the guard lives.
+class OnDevice {
+    c10::OptionalDeviceGuard guard;
+public:
+    OnDevice(PyObject* const* a, Py_ssize_t n) {
+        const at::Tensor* first = nullptr;
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            if (!THPVariable_Check(a[i])) continue;
+            const at::Tensor& t = THPVariable_Unpack(a[i]);
+            if (!t.is_cuda()) throw Bad{"tensors are on the GPU"};
+            if (!first) first = &t;
+            else if (t.device() != first->device()) throw Bad{"tensors are on one device"};
+        }
+        if (first) guard.reset_device(first->device());
+    }
+};
+
+// (function, Z, tokens, k, temperature, logp, entropy, lse, top_ids, top_logp, status, stream)
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&] {
+        const OnDevice on(a, n);
+        const Logits z = logits(a[1]);
+        if (z.M < 0) throw Bad{kLogits};
+        const int k = whole(a[3], "k: 0 to 256 alternatives");
+        const auto* tokens = static_cast<const int64_t*>(values(a[2], at::kLong, z.M, "tokens: an int64 value on the GPU for every row"));
+        const float temperature = float(PyFloat_AsDouble(a[4]));
+        auto* logp = static_cast<float*>(values(a[5], at::kFloat, z.M, "logp: a float32 value on the GPU for every row"));
+        auto* entropy = static_cast<float*>(values(a[6], at::kFloat, z.M, "entropy: a float32 value on the GPU for every row"));
+        auto* lse = static_cast<float*>(values(a[7], at::kFloat, z.M, "lse: a float32 value on the GPU for every row"));
+        auto* ids = static_cast<int32_t*>(values(a[8], at::kInt, z.M * k, "top_ids: contiguous int32 [rows, k] on the GPU"));
+        auto* top = static_cast<float*>(values(a[9], at::kFloat, z.M * k, "top_logp: contiguous float32 [rows, k] on the GPU"));
+        int* status = static_cast<int*>(status_word(a[10]));
+        void* stream = address(a[11]);
+        auto f = function<decltype(&patch_token_logprobs)>(a[0]);
+        return unlocked([&] { return f(z.p, z.ld, z.type, z.M, z.V, tokens, k, temperature, logp, entropy, lse, ids, top, status, stream); });
+    });
+}
+
+// (function, Z, tokens, temperature, lse, glogp, entropy, gentropy, gZ, status, stream)
+PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&] {
+        const OnDevice on(a, n);
+        const Logits z = logits(a[1]), g = logits(a[8]);
+        if (z.M < 0 || g.M < 0) throw Bad{kLogits};
+        same(z, g);
+        const auto* tokens = static_cast<const int64_t*>(values(a[2], at::kLong, z.M, "tokens: an int64 value on the GPU for every row"));
+        const float temperature = float(PyFloat_AsDouble(a[3]));
+        auto* lse = static_cast<float*>(values(a[4], at::kFloat, z.M, "lse: a float32 value on the GPU for every row"));
+        auto* glogp = static_cast<float*>(values(a[5], at::kFloat, z.M, "glogp: a float32 value on the GPU for every row"));
+        auto* entropy = static_cast<float*>(values(a[6], at::kFloat, z.M, "entropy: a float32 value on the GPU for every row"));
+        auto* gentropy = static_cast<float*>(values(a[7], at::kFloat, z.M, "gentropy: a float32 value on the GPU for every row"));
+        int* status = static_cast<int*>(status_word(a[9]));
+        void* stream = address(a[10]);
+        auto f = function<decltype(&patch_token_logprobs_backward)>(a[0]);
+        return unlocked([&] { return f(z.p, z.ld, z.type, z.M, z.V, tokens, temperature, lse, glogp, entropy, gentropy, g.p, g.ld, status, stream); });
+    });
+}
+
+struct Teacher { const int32_t* ids; const float* t; int K; };
+Teacher teacher(PyObject* ids, PyObject* t, int64_t M) {
+    constexpr const char* what = "the teacher's list: contiguous int32 ids and float32 log probabilities [rows, entries] on the GPU";
+    const at::Tensor *i = tensor(ids, what), *l = tensor(t, what);
+    if (!i || !l || i->dim() != 2 || l->dim() != 2 || i->sizes() != l->sizes() || i->size(0) != M || i->size(1) > (1 << 20)) throw Bad{what};
+    const int64_t n = i->numel();
+    return {static_cast<const int32_t*>(values(ids, at::kInt, n, what)), static_cast<const float*>(values(t, at::kFloat, n, what)), int(i->size(1))};
+}
+
+// (function, Z, ids, t, temperature, flags, loss, stats, gloss, gZ, status, stream)
+PyObject* distill_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&] {
+        const OnDevice on(a, n);
+        const Logits z = logits(a[1]), g = logits(a[9]);
+        if (z.M < 0) throw Bad{kLogits};
+        if (g.M >= 0) same(z, g);
+        const Teacher t = teacher(a[2], a[3], z.M);
+        const float temperature = float(PyFloat_AsDouble(a[4]));
+        const int flags = whole(a[5], "flags");
+        auto* loss = static_cast<float*>(values(a[6], at::kFloat, z.M, "loss: a float32 value on the GPU for every row"));
+        auto* stats = static_cast<float*>(values(a[7], at::kFloat, 2 * z.M, "stats: contiguous float32 [rows, 2] on the GPU"));
+        auto* gloss = static_cast<float*>(values(a[8], at::kFloat, z.M, "gloss: a float32 value on the GPU for every row"));
+        int* status = static_cast<int*>(status_word(a[10]));
+        void* stream = address(a[11]);
+        auto f = function<decltype(&patch_distill_loss)>(a[0]);
+        return unlocked([&] { return f(z.p, z.ld, z.type, z.M, z.V, t.ids, t.t, t.K, temperature, flags, loss, stats, gloss, g.p, g.ld, status, stream); });
+    });
+}
+
+// (function, Z, ids, t, temperature, flags, stats, gloss, gZ, status, stream)
+PyObject* distill_loss_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&] {
+        const OnDevice on(a, n);
+        const Logits z = logits(a[1]), g = logits(a[8]);
+        if (z.M < 0 || g.M < 0) throw Bad{kLogits};
+        same(z, g);
+        const Teacher t = teacher(a[2], a[3], z.M);
+        const float temperature = float(PyFloat_AsDouble(a[4]));
+        const int flags = whole(a[5], "flags");
+        auto* stats = static_cast<float*>(values(a[6], at::kFloat, 2 * z.M, "stats: contiguous float32 [rows, 2] on the GPU"));
+        auto* gloss = static_cast<float*>(values(a[7], at::kFloat, z.M, "gloss: a float32 value on the GPU for every row"));
+        int* status = static_cast<int*>(status_word(a[9]));
+        void* stream = address(a[10]);
+        auto f = function<decltype(&patch_distill_loss_backward)>(a[0]);
+        return unlocked([&] { return f(z.p, z.ld, z.type, z.M, z.V, t.ids, t.t, t.K, temperature, flags, stats, gloss, g.p, g.ld, status, stream); });
+    });
+}
+
 PyMethodDef methods[] = {
     {"qk_norm_rope", reinterpret_cast<PyCFunction>(qk_norm_rope), METH_FASTCALL, nullptr},
     {"qk_norm_rope_backward", reinterpret_cast<PyCFunction>(qk_norm_rope_backward), METH_FASTCALL, nullptr},
     {"kv_append", reinterpret_cast<PyCFunction>(kv_append), METH_FASTCALL, nullptr},
     {"prefix_attention", reinterpret_cast<PyCFunction>(prefix_attention), METH_FASTCALL, nullptr},
+    {"token_logprobs", reinterpret_cast<PyCFunction>(token_logprobs), METH_FASTCALL, nullptr},
+    {"token_logprobs_backward", reinterpret_cast<PyCFunction>(token_logprobs_backward), METH_FASTCALL, nullptr},
+    {"distill_loss", reinterpret_cast<PyCFunction>(distill_loss), METH_FASTCALL, nullptr},
+    {"distill_loss_backward", reinterpret_cast<PyCFunction>(distill_loss_backward), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
