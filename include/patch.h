@@ -607,6 +607,41 @@ int patch_prefix_attention(const patch_kv_cache_t* cache, const void* Q_dev, int
                            int64_t ld_table, const int32_t* suffix_lens_dev, float scale, void* O_dev, int64_t ldo,
                            float* lse_dev, void* workspace_dev, size_t workspace_bytes, int* status_dev, void* stream);
 
+/*
+ * Causal attention within sequences packed one after the other, as prompts and training batches are: rows starts[b] .. starts[b + 1] - 1 of
+ * Q, K, V and O are sequence b, and its row i sees its rows up to i:
+ *     s_ij = q_i . k_j (j <= i),   O_i = sum_j softmax_j(scale s_ij) v_j,   lse_i = ln sum_j exp(scale s_ij).
+ * Query head h reads key head h / (Hq / Hkv).  Sequences may be of any length, 0 and 1 included; rows before the first and behind the last one
+ * are neither read into a result nor written.  Values of a sequence are assumed finite; whatever the rows of other sequences and
+ * around them hold shows in no result of it.
+ *   Q_dev, O_dev  [M x Hq heads of D], pitches ldq, ldo;  K_dev, V_dev [M x Hkv heads of D], pitches ldk, ldv;  D = 64 or 128, Hq a multiple of Hkv, at
+ *                 most 4096;  pitches at most 2^28
+ *   starts_dev    int32 [B + 1], 0 <= starts[0] <= .. <= starts[B] <= M, in device memory: a captured launch follows it.  B <= 2^20
+ *   lse_dev       NULL or fp32 [M x Hq], what the gradient reads
+ *   status_dev    PATCH_ERR_SIZE: starts out of order or out of range (nothing out of range is read or written; results are undefined);
+ *                 PATCH_ERR_TIMEOUT: a bounded wait expired (O is undefined)
+ * 0 < scale <= 2e38, M <= 2^31 - 257.  M == 0 or B == 0 returns PATCH_OK without launching.  Equal calls give equal bits.  No workspace.
+ */
+int patch_sequence_attention(const void* Q_dev, int64_t ldq, const void* K_dev, int64_t ldk, const void* V_dev, int64_t ldv, int64_t M,
+                             int Hq, int Hkv, int D, const int32_t* starts_dev, int64_t B, float scale, void* O_dev, int64_t ldo,
+                             float* lse_dev, int* status_dev, void* stream);
+
+/*
+ * Gradient of patch_sequence_attention, from its inputs and results.  With p_ij = exp(scale s_ij - lse_i), delta_i = gO_i . O_i:
+ *     gs_ij = scale p_ij (gO_i . v_j - delta_i),   gQ_i = sum_j gs_ij k_j,   gK_j = sum_i gs_ij q_i,   gV_j = sum_i p_ij gO_i,
+ * gK and gV summed over the query heads of a key head too.  Products take p and gs rounded to bf16.
+ *   gQ_dev [M x Hq heads], gK_dev, gV_dev [M x Hkv heads]: results, column ranges of one stacked gradient if wanted; they overlap no input.
+ *                 Rows outside the sequences stay as they are.
+ *   workspace_dev at least patch_sequence_attention_backward_workspace_size bytes, 256-byte aligned, no initialisation needed
+ * Everything else as above.  Equal calls give equal bits (no atomics).
+ */
+int patch_sequence_attention_backward_workspace_size(int64_t M, int64_t B, int Hq, int Hkv, int D, size_t* bytes_out);
+int patch_sequence_attention_backward(const void* gO_dev, int64_t ldgo, const void* Q_dev, int64_t ldq, const void* K_dev, int64_t ldk,
+                                      const void* V_dev, int64_t ldv, const void* O_dev, int64_t ldo, const float* lse_dev, int64_t M,
+                                      int Hq, int Hkv, int D, const int32_t* starts_dev, int64_t B, float scale, void* gQ_dev,
+                                      int64_t ldgq, void* gK_dev, int64_t ldgk, void* gV_dev, int64_t ldgv, void* workspace_dev,
+                                      size_t workspace_bytes, int* status_dev, void* stream);
+
 /* =========================================================================================
  * From logits to a loss: L_LM of Eq. 5 and its gradient, evaluation, and distillation from the dense model.
  * Logits are rows of V values, bf16 or fp32, with a pitch (ld) that is a multiple of 8 elements; columns from V on are neither

@@ -32,6 +32,7 @@ EXPORTS = ["patch_packed_size", "patch_pack", "patch_unpack", "patch_gemm_worksp
            "patch_mask_regularizers", "patch_mask_regularizer_coefficients", "patch_soft_mask_backward",
            "patch_qk_norm_rope", "patch_qk_norm_rope_backward_workspace_size", "patch_qk_norm_rope_backward",
            "patch_kv_append", "patch_prefix_attention_workspace_size", "patch_prefix_attention",
+           "patch_sequence_attention", "patch_sequence_attention_backward_workspace_size", "patch_sequence_attention_backward",
            "patch_token_logprobs", "patch_token_logprobs_backward", "patch_distill_loss", "patch_distill_loss_backward",
            "patch_strerror", "patch_version"]
 MASK_NO_NOISE = 1
@@ -117,6 +118,10 @@ def load(path: str) -> ctypes.CDLL:
         L.patch_kv_append.argtypes = [cp, vp, i64, vp, i64, vp, i64, vp, f32, rp, vp, vp, i64, i32, vp, vp, i64, vp, vp]
         L.patch_prefix_attention_workspace_size.argtypes = [cp, i64, i32, i32, ctypes.POINTER(sz)]
         L.patch_prefix_attention.argtypes = [cp, vp, i64, i64, i32, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, vp, sz, vp, vp]
+        L.patch_sequence_attention.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, vp, i64, f32, vp, i64, vp, vp, vp]
+        L.patch_sequence_attention_backward_workspace_size.argtypes = [i64, i64, i32, i32, i32, ctypes.POINTER(sz)]
+        L.patch_sequence_attention_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, vp, i64, f32, vp, i64, vp, i64,
+                                                        vp, i64, vp, sz, vp, vp]
         L.patch_token_logprobs.argtypes = [vp, i64, i32, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp, vp, vp]
         L.patch_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp, vp]
         L.patch_distill_loss.argtypes = [vp, i64, i32, i64, i64, vp, vp, i32, f32, i32, vp, vp, vp, vp, i64, vp, vp]
@@ -128,6 +133,7 @@ def load(path: str) -> ctypes.CDLL:
                 getattr(L, name).restype = ctypes.c_int
         # addresses for the calls that do not go through ctypes (see csrc/marshal.cpp)
         for name in ("patch_qk_norm_rope", "patch_qk_norm_rope_backward", "patch_kv_append", "patch_prefix_attention",
+                     "patch_sequence_attention", "patch_sequence_attention_backward",
                      "patch_token_logprobs", "patch_token_logprobs_backward", "patch_distill_loss", "patch_distill_loss_backward"):
             setattr(L, "at_" + name, ctypes.cast(getattr(L, name), vp).value)
     return L
@@ -586,6 +592,49 @@ def patch_prefix_attention(cache: KVCache, Q, prefix_pages, prefix_len: int, pag
     if rc:
         _check(rc, "patch_prefix_attention")
     return O
+
+
+def patch_sequence_attention(Q, K, V, starts, scale: float | None = None, O=None, lse=None, status=None, stream=None):
+    """Causal attention within packed sequences: Q [M, Hq, D], K and V [M, Hkv, D], sequence b in rows starts[b] .. starts[b + 1] - 1 (int32
+    [B + 1]): returns O; ``lse`` float32 [M, Hq] is written if given.  ``scale`` defaults to 1 / sqrt(D).  Rows outside the sequences are
+    not written (where O is made here: they hold whatever the memory did)."""
+    if _torch is None:
+        _use_torch()
+    assert Q.is_cuda, "heads are on the GPU"
+    if O is None:
+        O = _empty(stream, Q.shape, _bf16, Q.device)
+    rc = _marshal.sequence_attention((_lib or lib()).at_patch_sequence_attention, Q, K, V, starts, scale, O, lse, status, _stream_of(Q, stream))
+    if rc:
+        _check(rc, "patch_sequence_attention")
+    return O
+
+
+def patch_sequence_attention_backward_workspace_size(M: int, B: int, Hq: int, Hkv: int, D: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().patch_sequence_attention_backward_workspace_size(M, B, Hq, Hkv, D, ctypes.byref(n)), "patch_sequence_attention_backward_workspace_size")
+    return int(n.value)
+
+
+def patch_sequence_attention_backward(gO, Q, K, V, O, lse, starts, scale: float | None = None, gQ=None, gK=None, gV=None, workspace=None, status=None,
+                                      stream=None):
+    """Gradient of ``patch_sequence_attention`` from its inputs and results: returns (gQ, gK, gV).  Rows outside the sequences are not written."""
+    if _torch is None:
+        _use_torch()
+    assert Q.is_cuda and Q.dim() == 3 and K.dim() == 3, "heads are CUDA tensors [rows, heads, D]"
+    if gQ is None:
+        gQ = _empty(stream, Q.shape, _bf16, Q.device)
+    if gK is None:
+        gK = _empty(stream, K.shape, _bf16, Q.device)
+    if gV is None:
+        gV = _empty(stream, V.shape, _bf16, Q.device)
+    if workspace is None:
+        n = patch_sequence_attention_backward_workspace_size(Q.shape[0], max(0, starts.shape[0] - 1), Q.shape[1], K.shape[1], Q.shape[2])
+        workspace = _empty(stream, n, _torch.uint8, Q.device)
+    rc = _marshal.sequence_attention_backward((_lib or lib()).at_patch_sequence_attention_backward, gO, Q, K, V, O, lse, starts, scale, gQ, gK, gV, workspace,
+                                              status, _stream_of(Q, stream))
+    if rc:
+        _check(rc, "patch_sequence_attention_backward")
+    return gQ, gK, gV
 
 
 # ---------------------------------------------------------------------------------------------

@@ -1,5 +1,5 @@
 // Takes torch tensors apart for the calls whose kernels run only a few microseconds (patch_qk_norm_rope, its gradient,
-// patch_kv_append, patch_prefix_attention, and those from logits to a loss): a CPython module that checks types, shapes and strides and calls the C ABI by address.
+// patch_kv_append, the attentions, and those from logits to a loss): a CPython module that checks types, shapes and strides and calls the C ABI by address.
 // Nothing else happens here -- no allocation, no kernels; the checks of sizes, alignment and device are the library's own.
 // Why not ctypes: a call with four tensors of heads and twenty arguments spent 4 us in Python attribute look-ups and argument
 // conversion, as much again as the launch (8.8 us against 4.6 us for a decode step's 64 tokens appended, whose kernel takes 3.4).
@@ -318,11 +318,71 @@ PyObject* distill_loss_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+struct Starts { const int32_t* p; int64_t B; };
+Starts starts_of(PyObject* o) {
+    constexpr const char* what = "starts: contiguous int32 [sequences + 1] on the GPU";
+    const at::Tensor* t = tensor(o, what);
+    if (!t || t->dim() != 1 || t->numel() < 1) throw Bad{what};
+    return {static_cast<const int32_t*>(values(o, at::kInt, t->numel(), what)), t->numel() - 1};
+}
+// Q, K, V (and what has their shapes) of one call
+void alike(const Rows& q, const Rows& k, const Rows& v) {
+    if (q.M < 0 || k.M != q.M || v.M != q.M || k.D != q.D || v.D != q.D || k.H != v.H) throw Bad{"queries, keys and values have the same rows and D, keys and values the same heads"};
+}
+void as_shaped(const Rows& a, const Rows& b) {
+    if (a.M != b.M || a.H != b.H || a.D != b.D) throw Bad{"results and gradients have the shapes of what they belong to"};
+}
+
+// (function, Q, K, V, starts, scale, O, lse, status, stream)
+PyObject* sequence_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&] {
+        const OnDevice on(a, n);
+        const Rows q = rows(a[1]), k = rows(a[2]), v = rows(a[3]), o = rows(a[6]);
+        alike(q, k, v);
+        as_shaped(o, q);
+        const Starts s = starts_of(a[4]);
+        const float scale = a[5] == Py_None ? 1.0f / std::sqrt(float(q.D)) : float(PyFloat_AsDouble(a[5]));
+        auto* lse = static_cast<float*>(values(a[7], at::kFloat, q.M * q.H, "lse: contiguous float32 [rows, heads] on the GPU"));
+        int* status = static_cast<int*>(status_word(a[8]));
+        void* stream = address(a[9]);
+        auto f = function<decltype(&patch_sequence_attention)>(a[0]);
+        return unlocked([&] { return f(q.p, q.ld, k.p, k.ld, v.p, v.ld, q.M, q.H, k.H, int(q.D), s.p, s.B, scale, o.p, o.ld, lse, status, stream); });
+    });
+}
+
+// (function, gO, Q, K, V, O, lse, starts, scale, gQ, gK, gV, workspace, status, stream)
+PyObject* sequence_attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 15, [&] {
+        const OnDevice on(a, n);
+        const Rows go = rows(a[1]), q = rows(a[2]), k = rows(a[3]), v = rows(a[4]), o = rows(a[5]), gq = rows(a[9]), gk = rows(a[10]), gv = rows(a[11]);
+        alike(q, k, v);
+        as_shaped(o, q);
+        as_shaped(go, q);
+        as_shaped(gq, q);
+        as_shaped(gk, k);
+        as_shaped(gv, v);
+        const auto* lse = static_cast<const float*>(values(a[6], at::kFloat, q.M * q.H, "lse: contiguous float32 [rows, heads] on the GPU"));
+        const Starts s = starts_of(a[7]);
+        const float scale = a[8] == Py_None ? 1.0f / std::sqrt(float(q.D)) : float(PyFloat_AsDouble(a[8]));
+        size_t bytes;
+        void* ws = workspace_of(a[12], bytes);
+        int* status = static_cast<int*>(status_word(a[13]));
+        void* stream = address(a[14]);
+        auto f = function<decltype(&patch_sequence_attention_backward)>(a[0]);
+        return unlocked([&] {
+            return f(go.p, go.ld, q.p, q.ld, k.p, k.ld, v.p, v.ld, o.p, o.ld, lse, q.M, q.H, k.H, int(q.D), s.p, s.B, scale, gq.p, gq.ld, gk.p, gk.ld, gv.p, gv.ld,
+                     ws, bytes, status, stream);
+        });
+    });
+}
+
 PyMethodDef methods[] = {
     {"qk_norm_rope", reinterpret_cast<PyCFunction>(qk_norm_rope), METH_FASTCALL, nullptr},
     {"qk_norm_rope_backward", reinterpret_cast<PyCFunction>(qk_norm_rope_backward), METH_FASTCALL, nullptr},
     {"kv_append", reinterpret_cast<PyCFunction>(kv_append), METH_FASTCALL, nullptr},
     {"prefix_attention", reinterpret_cast<PyCFunction>(prefix_attention), METH_FASTCALL, nullptr},
+    {"sequence_attention", reinterpret_cast<PyCFunction>(sequence_attention), METH_FASTCALL, nullptr},
+    {"sequence_attention_backward", reinterpret_cast<PyCFunction>(sequence_attention_backward), METH_FASTCALL, nullptr},
     {"token_logprobs", reinterpret_cast<PyCFunction>(token_logprobs), METH_FASTCALL, nullptr},
     {"token_logprobs_backward", reinterpret_cast<PyCFunction>(token_logprobs_backward), METH_FASTCALL, nullptr},
     {"distill_loss", reinterpret_cast<PyCFunction>(distill_loss), METH_FASTCALL, nullptr},
