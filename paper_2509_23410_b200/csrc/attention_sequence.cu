@@ -9,7 +9,7 @@
 // A CTA owns 64 rows of a sequence: queries of one head (result, gq) or keys of one key head (gk, gv; it walks over the group's query
 // heads, so that shared heads need no atomics and equal calls give equal bits).
 #include <math.h>
-#include "attention.cuh"
+#include "attention_sequence.cuh"
 
 namespace patch {
 namespace seq {
@@ -19,41 +19,6 @@ using attn::pack2;
 
 constexpr int kRows = 64;                    // of a tile of queries or keys
 constexpr int kThreads = 128;
-
-struct Problem {
-    const __nv_bfloat16 *q, *k, *v, *o, *go;
-    int64_t ldq, ldk, ldv, ldo, ldgo;
-    const int32_t* starts;
-    int B, M, Hq, Hkv, G;
-    float scale, scale_log2;
-    int* status;
-};
-
-// Tiles of all sequences in one line: sequence b's first tile is number starts[b] / kRows + b, and it has at most as many as lie before
-// the next one's first.
-struct Tile { int begin, end, first; };      // rows of the sequence; the tile's first row, counted from `begin` (-1: no tile)
-__device__ __forceinline__ int clamped(const Problem& p, int b) { return min(max(p.starts[b], 0), p.M); }
-__device__ __forceinline__ Tile tile_of(const Problem& p, int slot) {
-    int lo = -1, hi = p.B;                   // the last sequence whose first tile is at or before `slot`
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (clamped(p, mid) / kRows + mid <= slot) lo = mid; else hi = mid;
-    }
-    Tile t = {0, 0, -1};
-    if (lo < 0) return t;
-    t.begin = clamped(p, lo);
-    t.end = max(clamped(p, lo + 1), t.begin);
-    const int first = (slot - (t.begin / kRows + lo)) * kRows;
-    if (first >= 0 && first < t.end - t.begin) t.first = first;
-    return t;
-}
-// starts out of order or out of range are reported (every tile stays within the rows all the same)
-__device__ __forceinline__ void check_starts(const Problem& p) {
-    if (blockIdx.x || blockIdx.y || !p.status) return;
-    bool bad = false;
-    for (int b = threadIdx.x; b <= p.B; b += blockDim.x) bad |= p.starts[b] < 0 || p.starts[b] > p.M || (b && p.starts[b] < p.starts[b - 1]);
-    if (bad) atomicCAS(p.status, PATCH_OK, PATCH_ERR_SIZE);
-}
 
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -124,61 +89,6 @@ __device__ __forceinline__ void store_rows(__nv_bfloat16* to, int64_t ld, int ro
     }
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) forward_kernel(const Problem p, __nv_bfloat16* o, int64_t ldo, float* lse) {
-    extern __shared__ __align__(16) __nv_bfloat16 sm[];
-    __nv_bfloat16 *sq = sm, *sk = sq + kTileElements<D>, *sv = sk + kTileElements<D>;
-    check_starts(p);
-    const Tile t = tile_of(p, gridDim.x - 1 - blockIdx.x);         // a sequence's last rows, which see most keys, first
-    if (t.first < 0) return;
-    const int h = blockIdx.y, kvh = h / p.G, lane = threadIdx.x & 31, row = t.begin + t.first;
-    load_tile<D>(sq, p.q + int64_t(h) * D, p.ldq, row, t.end);
-    float acc[D / 8][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-    const int mine = row + 16 * (threadIdx.x >> 5) + (lane >> 2);
-    for (int key = t.begin; key <= row; key += kRows) {
-        __syncthreads();
-        load_tile<D>(sk, p.k + int64_t(kvh) * D, p.ldk, key, t.end);
-        load_tile<D>(sv, p.v + int64_t(kvh) * D, p.ldv, key, t.end);
-        __syncthreads();
-        float s[8][4];
-        product<D>(s, sq, sk);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            float top = m[x];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int i = 2 * x; i < 2 * x + 2; ++i) {
-                    if (key + 8 * j + 2 * (lane & 3) + (i & 1) > mine + 8 * x) s[j][i] = -INFINITY;
-                    top = fmaxf(top, s[j][i]);
-                }
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const float f = top == m[x] ? 1.0f : ex2(attn::exponent(m[x], attn::base_of(top), p.scale_log2)), base = attn::base_of(top);
-            float sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int i = 2 * x; i < 2 * x + 2; ++i) {
-                    s[j][i] = ex2(attn::exponent(s[j][i], base, p.scale_log2));
-                    sum += s[j][i];
-                }
-            l[x] = l[x] * f + sum;
-            m[x] = top;
-#pragma unroll
-            for (int j = 0; j < D / 8; ++j) { acc[j][2 * x] *= f; acc[j][2 * x + 1] *= f; }
-        }
-        accumulate<D>(acc, s, sv);
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        l[x] += __shfl_xor_sync(0xFFFFFFFFu, l[x], 1);
-        l[x] += __shfl_xor_sync(0xFFFFFFFFu, l[x], 2);
-        if (lse && !(lane & 3) && mine + 8 * x < t.end) lse[int64_t(mine + 8 * x) * p.Hq + h] = m[x] * p.scale + logf(l[x]);
-    }
-    store_rows<D>(o + int64_t(h) * D, ldo, row, t.end, acc, 1.0f / l[0], 1.0f / l[1]);
-}
-
 // (lse log2 e, delta) of every row and head, [Hq][M]
 template <int D>
 __global__ void __launch_bounds__(256) delta_kernel(const Problem p, const float* lse, float2* stats) {
@@ -204,8 +114,8 @@ template <int D>
 __global__ void __launch_bounds__(kThreads) query_grad_kernel(const Problem p, const float2* stats, __nv_bfloat16* gq, int64_t ldgq) {
     extern __shared__ __align__(16) __nv_bfloat16 sm[];
     __nv_bfloat16 *sq = sm, *sgo = sq + kTileElements<D>, *sk = sgo + kTileElements<D>, *sv = sk + kTileElements<D>;
-    check_starts(p);
-    const Tile t = tile_of(p, gridDim.x - 1 - blockIdx.x);
+    if (blockIdx.x == 0 && blockIdx.y == 0) check_starts(p, threadIdx.x, kThreads);
+    const Tile t = tile_of<kRows>(p, gridDim.x - 1 - blockIdx.x);
     if (t.first < 0) return;
     const int h = blockIdx.y, kvh = h / p.G, lane = threadIdx.x & 31, row = t.begin + t.first;
     load_tile<D>(sq, p.q + int64_t(h) * D, p.ldq, row, t.end);
@@ -240,7 +150,7 @@ __global__ void __launch_bounds__(kThreads) key_grad_kernel(const Problem p, con
     extern __shared__ __align__(16) __nv_bfloat16 sm[];
     __nv_bfloat16 *sk = sm, *sv = sk + kTileElements<D>, *sq = sv + kTileElements<D>, *sgo = sq + kTileElements<D>;
     __shared__ float2 st[kRows];
-    const Tile t = tile_of(p, blockIdx.x);                         // a sequence's first keys, which most rows see, first
+    const Tile t = tile_of<kRows>(p, blockIdx.x);                         // a sequence's first keys, which most rows see, first
     if (t.first < 0) return;
     const int kvh = blockIdx.y, lane = threadIdx.x & 31, row = t.begin + t.first;
     load_tile<D>(sk, p.k + int64_t(kvh) * D, p.ldk, row, t.end);
@@ -276,14 +186,6 @@ __global__ void __launch_bounds__(kThreads) key_grad_kernel(const Problem p, con
 }
 
 template <int D>
-static int forward(const Problem& p, __nv_bfloat16* o, int64_t ldo, float* lse, cudaStream_t s) {
-    static std::atomic<uint64_t> configured{0};
-    const uint32_t smem = 3 * kTileElements<D> * 2;
-    if (int rc = allow_dynamic_smem(forward_kernel<D>, smem, configured)) return rc;
-    forward_kernel<D><<<dim3(unsigned(p.M / kRows + p.B), unsigned(p.Hq)), kThreads, smem, s>>>(p, o, ldo, lse);
-    return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
-}
-template <int D>
 static int backward(const Problem& p, const float* lse, float2* stats, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
                     int64_t ldgv, cudaStream_t s) {
     static std::atomic<uint64_t> configured_q{0}, configured_k{0};
@@ -294,7 +196,7 @@ static int backward(const Problem& p, const float* lse, float2* stats, __nv_bflo
     const int64_t groups = int64_t(p.M) * p.Hq;
     delta_kernel<D><<<unsigned((groups * (D / 8) + 255) / 256), 256, 0, s>>>(p, lse, stats);
     if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
-    const unsigned tiles = unsigned(p.M / kRows + p.B);
+    const unsigned tiles = unsigned(most_tiles(p.M, p.B, kRows));
     query_grad_kernel<D><<<dim3(tiles, unsigned(p.Hq)), kThreads, smem, s>>>(p, stats, gq, ldgq);
     if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
     key_grad_kernel<D><<<dim3(tiles, unsigned(p.Hkv)), kThreads, smem, s>>>(p, stats, gk, ldgk, gv, ldgv);
@@ -304,7 +206,8 @@ static int backward(const Problem& p, const float* lse, float2* stats, __nv_bflo
 // ---- checks of arguments ----
 static int check_shape(int64_t M, int Hq, int Hkv, int D, int64_t B) {
     if (M < 0 || M > 0x7FFFFFFF - 256 || B < 0 || B > (1 << 20) || (D != 64 && D != 128) || Hkv < 1 || Hq < Hkv || Hq % Hkv || Hq > 4096) return PATCH_ERR_SHAPE;
-    return M * Hq * (D / 8) > (int64_t(1) << 38) ? PATCH_ERR_SHAPE : PATCH_OK;        // CTAs of a launch are counted in 31 bits
+    // CTAs of a launch are counted in 31 bits
+    return M * Hq * (D / 8) > (int64_t(1) << 38) || most_tiles(M, B, kRows) * Hq > 0x7FFFFFFF ? PATCH_ERR_SHAPE : PATCH_OK;
 }
 static int check_rows(const void* x, int64_t ld, int64_t H, int64_t D) {
     if (!x) return PATCH_ERR_NULL;
@@ -333,7 +236,7 @@ extern "C" int patch_sequence_attention(const void* Q, int64_t ldq, const void* 
     const seq::Problem p = {static_cast<const B16*>(Q), static_cast<const B16*>(K), static_cast<const B16*>(V), nullptr, nullptr, ldq, ldk, ldv, 0, 0, starts,
                             int(B), int(M), Hq, Hkv, Hq / Hkv, scale, scale * 1.44269504f, status_dev};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return D == 128 ? seq::forward<128>(p, static_cast<B16*>(O), ldo, lse, s) : seq::forward<64>(p, static_cast<B16*>(O), ldo, lse, s);
+    return seq::launch_forward(p, D, static_cast<B16*>(O), ldo, lse, s);
 }
 
 extern "C" int patch_sequence_attention_backward_workspace_size(int64_t M, int64_t B, int Hq, int Hkv, int D, size_t* bytes_out) {
