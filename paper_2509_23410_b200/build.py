@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpatch_b200.so")
 LIB_FI = os.path.join(HERE, "libpatch_b200_fi.so")
 SOURCES = ["pack.cu", "masks.cu", "gemv.cu", "gemm_decode_sm100.cu", "gemm_decode_cluster_sm100.cu", "gemm_prefill_sm100.cu", "gemm_prefill2_sm100.cu", "gemm_prefill_pair_sm100.cu", "gemm_prefill_pair_mixed_sm100.cu", "gemm_decode_q4_sm100.cu",
-           "qk_rope.cu", "attention.cu", "attention_decode_sm100.cu", "attention_block_sm100.cu", "attention_sequence.cu", "attention_sequence_sm100.cu", "logits.cu", "api.cu"]
+           "qk_rope.cu", "attention.cu", "attention_decode_sm100.cu", "attention_block_sm100.cu", "attention_sequence.cu", "attention_sequence_sm100.cu", "attention_sequence_grad_sm100.cu", "logits.cu", "api.cu"]
 
 
 MARSHAL = os.path.join(HERE, "_marshal.so")

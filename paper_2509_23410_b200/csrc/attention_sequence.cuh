@@ -43,7 +43,82 @@ __device__ __forceinline__ void check_starts(const Problem& p, int thread, int t
     if (bad) atomicCAS(p.status, PATCH_OK, PATCH_ERR_SIZE);
 }
 
+// A CTA that has started takes the place of one that has not: asked for ahead, answered in shared memory.  Launch order is kept, and what is left
+// over is balanced by itself, whatever the lengths in device memory are.  One question at a time; its answer is waited for before the CTA ends.
+__device__ __forceinline__ void ask_for_next(uint4* answer, uint64_t* bar) {
+    mbar_expect_tx(smem_u32(bar), 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(answer)), "r"(smem_u32(bar)) : "memory");
+}
+// the CTA number taken over; false: none is left (do not ask again)
+__device__ __forceinline__ bool answered(const uint4* answer, unsigned& next) {
+    uint32_t there;
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b128 r;\n\tld.shared.b128 r, [%2];\n\tclusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+                 "selp.u32 %1, 1, 0, p;\n\tmov.u32 %0, 0;\n\t@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, _, _, _}, r;\n\t}"
+                 : "=r"(next), "=r"(there) : "r"(smem_u32(answer)) : "memory");
+    attn::blk::fence_async_shared();                    // read before the next answer is written
+    return there != 0;
+}
+
+constexpr int kTileRows = 128;               // of a tile in shared memory: [64-element half][row][128 bytes, swizzled]
+template <int D> constexpr uint32_t kTileBytes = kTileRows * D * 2;
+
+// The producer warp's side of a ring of tiles.  All lanes call together.
+template <int D, int RING>
+struct Loader {
+    uint8_t* smem;                           // the ring
+    uint64_t *full, *empty, *tail;           // tail: a barrier of its own for tiles that need work behind the copy
+    volatile int* abort_flag;
+    int* status;
+    int stage = 0, issued = 0;
+    uint32_t phase = 0, phase_tail = 0;
+    bool ok = true;
+
+    __device__ __forceinline__ Loader(uint8_t* smem_, uint64_t* full_, uint64_t* empty_, uint64_t* tail_, volatile int* abort_, int* status_)
+        : smem(smem_), full(full_), empty(empty_), tail(tail_), abort_flag(abort_), status(status_) {}
+    __device__ __forceinline__ void wait(uint64_t& bar, uint32_t parity) {
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bar), parity, abort_flag, status)) && ok;
+    }
+    // 128 rows from `row` on of one head into the next stage; `left` < 128: rows from there on become zeros
+    __device__ __forceinline__ void load(const CUtensorMap* map, int row, int chunk, int left, uint64_t policy) {
+        if (issued >= RING) wait(empty[stage], phase ^ 1u);
+        if (!ok) return;
+        const int lane = threadIdx.x & 31;
+        uint8_t* const tile = smem + stage * kTileBytes<D>;
+        const bool partly = left < kTileRows;
+        if (lane == 0) {
+            const uint32_t bar = smem_u32(partly ? tail : &full[stage]);
+            mbar_expect_tx(bar, kTileBytes<D>);
+            tma_tile_load_3d(smem_u32(tile), map, 0, row, chunk, bar, policy);
+        }
+        __syncwarp();
+        ++issued;
+        if (partly) {
+            wait(*tail, phase_tail);
+            if (!ok) return;
+            phase_tail ^= 1u;
+            for (int i = left * (D / 8) + lane; i < kTileRows * (D / 8); i += 32) {
+                const int r = i / (D / 8), c = i - r * (D / 8);
+                *reinterpret_cast<uint4*>(tile + (c >> 3) * (kTileRows * 128) + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            attn::blk::fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
+        }
+        if (++stage == RING) { stage = 0; phase ^= 1u; }
+    }
+    // after a failure: copies on their way end before the CTA does
+    __device__ __forceinline__ void drain() {
+        const uint64_t t0 = global_timer_ns();
+        for (int j = issued > RING ? issued - RING : 0; j < issued; ++j)
+            while (!mbar_try_wait(smem_u32(&full[j % RING]), uint32_t(j / RING) & 1u) && global_timer_ns() - t0 < kDrainLimitNs) {}
+        while (global_timer_ns() - t0 < kDrainLimitNs) {}                    // those with barriers of their own
+    }
+};
+
 int launch_forward(const Problem& p, int D, __nv_bfloat16* o, int64_t ldo, float* lse, cudaStream_t s);
+// stats: [Hq][M] of scratch
+int launch_backward(const Problem& p, int D, const float* lse, float2* stats, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
+                    int64_t ldgv, cudaStream_t s);
 
 }  // namespace seq
 }  // namespace patch

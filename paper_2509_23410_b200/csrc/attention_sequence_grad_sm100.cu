@@ -1,0 +1,672 @@
+// Gradient of the causal attention within packed sequences on tcgen05 (public header: patch_sequence_attention_backward; mathematics in
+// attention_sequence.cu).
+//
+// Two kernels, so that every sum has one owner and an order of its own: gq by blocks of 128 queries over their keys (three products a tile), gk and
+// gv by blocks of 128 keys of a key head over the queries that see them, head by head of the group (four products a tile).  The scores are computed in
+// both, seven products instead of five; the price of sums in fp32 atomics would be an order that changes from call to call, and their traffic.
+// A CTA owns an SM; roles, rings and the taking of items are the forward kernel's.  Eight warps do the elementwise part of a tile of 128 x 128,
+// a thread 64 columns of a row.
+//
+//   gq:      S = Q K^T (two buffers), GP = GO V^T,   GS = P (GP - delta) (over S),   GQ += GS K
+//            order of the MMAs: GQ(j), GP(j + 1), S(j + 2): the exponentials of j + 1 run beside the first two
+//   gk, gv:  S^T = K Q^T,  GP^T = V GO^T (lane = key, column = query),  P^T (over S^T),  GS^T (over GP^T),  GV += P^T GO,  GK += GS^T Q
+//            order of the MMAs: GV(t), S(t + 1), GK(t), GP(t + 1): the exponentials of t + 1 run beside the last two
+// TMEM: 512 columns in both (two of scores or one, one of GP, the accumulators).
+#include "attention_sequence.cuh"
+
+namespace patch {
+namespace seq {
+
+using namespace attn;
+using namespace attn::blk;
+
+namespace bwd {
+
+constexpr int kRows = 128;                   // of an item and of a tile
+constexpr int kThreads = 384;
+constexpr uint32_t kTmemCols = 512;
+
+struct Item { int head, begin, end, first; };         // head < 0: no more
+
+template <int D> struct Cfg {
+    static constexpr int kRing = D == 128 ? 5 : 8;
+    static constexpr uint32_t kAtom = 128 * 128;       // 64 elements of 128 rows
+    static constexpr uint32_t kTile = kTileBytes<D>;
+    static constexpr uint32_t kOwn = kRing * kTile;    // the item's own two tiles
+    static constexpr uint32_t kMisc = kOwn + 2 * kTile;
+    static constexpr uint32_t kStats = kMisc + 384;    // of two tiles of queries: [lse log2 e: 128 | delta: 128]
+    static constexpr uint32_t kBytes = kStats + 2 * 1024;                      // the array itself is aligned: 227 KB leave nothing to round
+    static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
+};
+
+struct Misc {
+    uint64_t full[8], empty[8];
+    uint64_t own_full, own_empty, s[2], gp, p[2], gs[2], done, read;          // p, gs: by half of the columns; s: by buffer
+    uint64_t item_full[2], item_empty[2], stats_full[2], stats_empty[2], taken, tail;
+    alignas(16) uint4 answer;
+    Item item[2];
+    uint32_t tmem;
+    int abort;
+};
+static_assert(sizeof(Misc) <= 384, "fits behind the tiles");
+
+__device__ __forceinline__ void init(Misc& sh, int ring, int readers) {
+    for (int i = 0; i < ring; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); }
+    for (int x = 0; x < 2; ++x) {
+        mbar_init(smem_u32(&sh.s[x]), 1);
+        mbar_init(smem_u32(&sh.p[x]), 4);
+        mbar_init(smem_u32(&sh.gs[x]), 4);
+        mbar_init(smem_u32(&sh.item_full[x]), 1);
+        mbar_init(smem_u32(&sh.item_empty[x]), readers);
+        mbar_init(smem_u32(&sh.stats_full[x]), 1);
+        mbar_init(smem_u32(&sh.stats_empty[x]), 8);
+    }
+    mbar_init(smem_u32(&sh.own_full), 1);
+    mbar_init(smem_u32(&sh.own_empty), 1);
+    mbar_init(smem_u32(&sh.gp), 1);
+    mbar_init(smem_u32(&sh.done), 1);
+    mbar_init(smem_u32(&sh.read), 8);
+    mbar_init(smem_u32(&sh.taken), 1);
+    mbar_init(smem_u32(&sh.tail), 1);
+    sh.abort = 0;
+    mbar_init_fence();
+}
+
+// D[128 x 128] = A B^T, both K-major tiles of shared memory
+template <int D>
+__device__ __forceinline__ void product(uint32_t d_tmem, uint32_t a, uint32_t b) {
+    const uint64_t da = desc_kmajor_sw128(a), db = desc_kmajor_sw128(b);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        const uint64_t off = uint64_t(((ks >> 2) * Cfg<D>::kAtom + (ks & 3) * 32) >> 4);
+        mma_dense(d_tmem, da + off, db + off, instr_desc(128, false), ks != 0);
+    }
+}
+// D[128 x D] (+)= A[128 x 64, bf16 in TMEM] B[64 rows of a tile]
+template <int D>
+__device__ __forceinline__ void accumulate(uint32_t d_tmem, uint32_t a_tmem, uint32_t b, int half, bool first) {
+    const uint64_t db = desc_mnmajor_sw128(b + half * 64 * 128, Cfg<D>::kAtom);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) mma_ta(d_tmem, a_tmem + 8u * ks, db + uint64_t((ks * 2048) >> 4), instr_desc(D, false) | (1u << 16), !(first && ks == 0));
+}
+// a row of COLS fp32 columns of TMEM, times f, as bf16
+template <int COLS>
+__device__ __forceinline__ void store_row(uint32_t t, __nv_bfloat16* to, bool valid, float f) {
+#pragma unroll 1
+    for (int q = 0; q < COLS / 32; ++q) {
+        uint32_t v[32];
+        tmem_ld32(t + 32u * q, v);
+        tmem_ld_wait();
+        if (!valid) continue;
+#pragma unroll
+        for (int c = 0; c < 32; c += 8) {
+            uint4 w;
+            w.x = pack2(__uint_as_float(v[c]) * f, __uint_as_float(v[c + 1]) * f);
+            w.y = pack2(__uint_as_float(v[c + 2]) * f, __uint_as_float(v[c + 3]) * f);
+            w.z = pack2(__uint_as_float(v[c + 4]) * f, __uint_as_float(v[c + 5]) * f);
+            w.w = pack2(__uint_as_float(v[c + 6]) * f, __uint_as_float(v[c + 7]) * f);
+            *reinterpret_cast<uint4*>(to + 32 * q + c) = w;
+        }
+    }
+}
+
+}  // namespace bwd
+
+// (lse log2 e, delta) of every row and head, [Hq][M]
+template <int D>
+__global__ void __launch_bounds__(256) delta_kernel(const Problem p, const float* lse, float2* stats) {
+    const int64_t group = (int64_t(blockIdx.x) * 256 + threadIdx.x) / (D / 8);
+    const int c = threadIdx.x & (D / 8 - 1);
+    if (group >= int64_t(p.M) * p.Hq) return;
+    const int64_t row = group / p.Hq;
+    const int h = int(group - row * p.Hq);
+    const uint4 a = *reinterpret_cast<const uint4*>(p.o + row * p.ldo + h * D + 8 * c), b = *reinterpret_cast<const uint4*>(p.go + row * p.ldgo + h * D + 8 * c);
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        sum = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum);
+        sum = fmaf(__uint_as_float(x[i] & 0xFFFF0000u), __uint_as_float(y[i] & 0xFFFF0000u), sum);
+    }
+#pragma unroll
+    for (int d = D / 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+    if (c == 0) stats[int64_t(h) * p.M + row] = make_float2(lse[group] * 1.44269504f, sum);
+}
+
+// ---------------------------------------------------------------------------------------------
+// gq
+template <int D>
+__global__ void __launch_bounds__(bwd::kThreads, 1)
+sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUtensorMap map_k,
+                           const __grid_constant__ CUtensorMap map_v, const Problem p, const float2* const stats, __nv_bfloat16* const gq, const int64_t ldgq) {
+    using namespace bwd;
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t base = smem_u32(smem);
+    Misc& sh = *reinterpret_cast<Misc*>(smem + C::kMisc);
+    volatile int* abort_flag = &sh.abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 32) {
+        init(sh, C::kRing, 9);                                     // an item's readers: the MMA thread, eight warps
+        tma_prefetch_map(&map_q);
+        tma_prefetch_map(&map_go);
+        tma_prefetch_map(&map_k);
+        tma_prefetch_map(&map_v);
+    }
+    if (warp == 2) tmem_alloc(smem_u32(&sh.tmem), kTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem, t_gp = tmem + 256, t_gq = tmem + 384;      // scores: tmem + 128 (j & 1)
+
+    if (warp == 0) {
+        // ---------------- producer ----------------
+        const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
+        const int slots = int(most_tiles(p.M, p.B, kRows));
+        Loader<D, C::kRing> ring(smem, sh.full, sh.empty, &sh.tail, abort_flag, p.status);
+        int items = 0;
+        uint32_t phase_own = 0, phase_taken = 0;
+        unsigned at = blockIdx.x;
+        for (;;) {
+            if (lane == 0) ask_for_next(&sh.answer, &sh.taken);
+            __syncwarp();
+            if (at == 0) check_starts(p, lane, 32);
+            const int slot = slots - 1 - int(at / unsigned(p.Hq)), head = int(at % unsigned(p.Hq));
+            const Tile t = tile_of<kRows>(p, slot);
+            if (t.first >= 0) {
+                const Item it = {head, t.begin, t.end, t.first};
+                if (items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
+                if (ring.ok && lane == 0) {
+                    sh.item[items & 1] = it;
+                    mbar_arrive(smem_u32(&sh.item_full[items & 1]));
+                }
+                if (ring.ok && items >= 1) {
+                    ring.wait(sh.own_empty, phase_own);
+                    phase_own ^= 1u;
+                }
+                ++items;
+                if (ring.ok && lane == 0) {
+                    const uint32_t bar = smem_u32(&sh.own_full);
+                    mbar_expect_tx(bar, 2 * C::kTile);
+                    tma_tile_load_3d(base + C::kOwn, &map_q, 0, it.begin + it.first, head * (D / 64), bar, once);
+                    tma_tile_load_3d(base + C::kOwn + C::kTile, &map_go, 0, it.begin + it.first, head * (D / 64), bar, once);
+                }
+                __syncwarp();
+                const int n = it.first / kRows + 1, chunk = head / p.G * (D / 64);
+                for (int j = 0; j < n && ring.ok; ++j) {
+                    const int row = it.begin + j * kRows;
+                    ring.load(&map_k, row, chunk, it.end - row, keep);
+                    if (ring.ok) ring.load(&map_v, row, chunk, kRows, keep);
+                }
+            }
+            const bool before = ring.ok;
+            ring.ok = true;
+            ring.wait(sh.taken, phase_taken);
+            phase_taken ^= 1u;
+            const bool more = ring.ok && answered(&sh.answer, at);
+            ring.ok = ring.ok && before;
+            __syncwarp();
+            if (!ring.ok || !more) break;
+        }
+        if (ring.ok && items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
+        if (ring.ok && lane == 0) {
+            sh.item[items & 1].head = -1;
+            mbar_arrive(smem_u32(&sh.item_full[items & 1]));
+        }
+        if (*abort_flag) ring.drain();
+    } else if (warp == 1) {
+        // ---------------- MMAs: one thread ----------------
+        if (elect_one()) {
+            // stages of the ring: keys of tile j in number `k0 + 2 j` of the item, values behind them
+            int at = 0;                                            // tiles used before this item
+            uint32_t phase_own = 0, phase_gs = 0, phase_read = 0;
+            bool ok = true, began = false;
+            auto wait = [&](uint64_t& bar, uint32_t parity) {
+                ok = ok && mbar_wait(smem_u32(&bar), parity, abort_flag, p.status);
+                tc_fence_after();
+            };
+            auto arrived = [&](int i) { wait(sh.full[i % C::kRing], uint32_t(i / C::kRing) & 1u); return base + (i % C::kRing) * C::kTile; };
+            auto release = [&](int i) { mma_commit(smem_u32(&sh.empty[i % C::kRing])); };
+            const uint32_t q_tile = base + C::kOwn, go_tile = q_tile + C::kTile;
+            for (int item = 0; ok; ++item) {
+                wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
+                if (!ok) break;
+                const Item it = sh.item[item & 1];
+                mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+                if (it.head < 0) break;
+                const int n = it.first / kRows + 1;
+                wait(sh.own_full, phase_own);
+                phase_own ^= 1u;
+                auto scores = [&](int j) {
+                    const uint32_t k_tile = arrived(at + 2 * j);
+                    if (ok) product<D>(tmem + 128u * (j & 1), q_tile, k_tile);
+                    mma_commit(smem_u32(&sh.s[j & 1]));
+                };
+                auto gps = [&](int j) {
+                    const uint32_t v_tile = arrived(at + 2 * j + 1);
+                    if (ok) product<D>(t_gp, go_tile, v_tile);
+                    mma_commit(smem_u32(&sh.gp));
+                    release(at + 2 * j + 1);
+                };
+                if (ok) scores(0);
+                if (ok) gps(0);
+                if (ok && n > 1) scores(1);
+                if (n == 1) mma_commit(smem_u32(&sh.own_empty));
+#pragma unroll 1
+                for (int j = 0; j < n && ok; ++j) {
+                    const uint32_t k_tile = base + ((at + 2 * j) % C::kRing) * C::kTile;
+                    if (j == 0) {
+                        if (began) {
+                            wait(sh.read, phase_read);             // the last item's result has been read
+                            phase_read ^= 1u;
+                        }
+                        began = true;
+                    }
+#pragma unroll 1
+                    for (int half = 0; half < 2 && ok; ++half) {
+                        wait(sh.gs[half], phase_gs);
+                        if (ok) accumulate<D>(t_gq, tmem + 128u * (j & 1) + 64u * half, k_tile, half, j == 0 && half == 0);
+                    }
+                    phase_gs ^= 1u;
+                    release(at + 2 * j);
+                    if (j + 1 == n) mma_commit(smem_u32(&sh.done));
+                    if (ok && j + 1 < n) gps(j + 1);
+                    if (ok && j + 2 < n) scores(j + 2);
+                    if (j + 2 == n) mma_commit(smem_u32(&sh.own_empty));       // the last products with the item's own tiles
+                }
+                at += 2 * n;
+            }
+        }
+    } else if (warp >= 4) {
+        // ---------------- elementwise: thread = row, half of the columns ----------------
+        const int half = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t lanes = uint32_t(quad * 32) << 16;
+        uint32_t phase_s = 0, phase_gp = 0, phase_done = 0;        // phase_s: bit of the buffer
+        bool failed = false;
+        auto wait = [&](uint64_t& bar, uint32_t parity) {
+            failed = __any_sync(0xFFFFFFFFu, !mbar_wait(smem_u32(&bar), parity, abort_flag, p.status)) || failed;
+            tc_fence_after();
+        };
+        const f2 scale2 = mk2(p.scale_log2, p.scale_log2);
+        for (int item = 0;; ++item) {
+            wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
+            if (failed) break;
+            const Item it = sh.item[item & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+            if (it.head < 0) break;
+            const int n = it.first / kRows + 1, r = it.first + row;
+            const bool valid = r < it.end - it.begin;
+            const float2 st = valid ? stats[int64_t(it.head) * p.M + it.begin + r] : make_float2(0.0f, 0.0f);
+            const f2 lse2 = mk2(-st.x, -st.x), delta2 = mk2(-st.y, -st.y);
+            for (int j = 0; j < n; ++j) {
+                const uint32_t t_s = tmem + lanes + 128u * (j & 1) + 64u * half;
+                wait(sh.s[j & 1], (phase_s >> (j & 1)) & 1u);
+                if (failed) break;
+                phase_s ^= 1u << (j & 1);
+                const bool partly = j == n - 1;                    // the tile on the diagonal
+                const int left = row + 1 - 64 * half;              // columns the row sees there
+                uint32_t e[2][32];
+                tmem_ld32(t_s, e[0]);
+                tmem_ld32(t_s + 32u, e[1]);
+                tmem_ld_wait();
+                if (partly) {
+                    hide(e[0], left);
+                    hide(e[1], left - 32);
+                }
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) {
+                    float a, b;
+                    un2(fma2(mk2(__uint_as_float(e[c >> 5][c & 31]), __uint_as_float(e[c >> 5][(c & 31) + 1])), scale2, lse2), a, b);
+                    e[c >> 5][c & 31] = __float_as_uint(ex2(a));
+                    e[c >> 5][(c & 31) + 1] = __float_as_uint(ex2(b));
+                }
+                wait(sh.gp, phase_gp);
+                if (failed) break;
+                phase_gp ^= 1u;
+                uint32_t gs[32];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t v[32];
+                    tmem_ld32(tmem + lanes + 256u + 64u * half + 32u * i, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        float a, b;
+                        un2(mul2(mk2(__uint_as_float(e[i][c]), __uint_as_float(e[i][c + 1])),
+                                 add2(mk2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), delta2)), a, b);
+                        if (partly) {                              // values behind the sequence's end may be anything
+                            if (32 * i + c >= left) a = 0.0f;
+                            if (32 * i + c + 1 >= left) b = 0.0f;
+                        }
+                        gs[16 * i + (c >> 1)] = pack2(a, b);
+                    }
+                }
+                tmem_st32(t_s, gs);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.gs[half]));
+            }
+            if (failed) break;
+            wait(sh.done, phase_done);
+            if (failed) break;
+            phase_done ^= 1u;
+            store_row<D / 2>(t_gq + lanes + half * (D / 2), gq + int64_t(it.begin + r) * ldgq + int64_t(it.head) * D + half * (D / 2), valid, p.scale);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.read));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 2) tmem_dealloc(tmem, kTmemCols);
+}
+
+// ---------------------------------------------------------------------------------------------
+// gk, gv
+template <int D>
+__global__ void __launch_bounds__(bwd::kThreads, 1)
+sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUtensorMap map_k,
+                         const __grid_constant__ CUtensorMap map_v, const Problem p, const float2* const stats, __nv_bfloat16* const gk, const int64_t ldgk,
+                         __nv_bfloat16* const gv, const int64_t ldgv) {
+    using namespace bwd;
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t base = smem_u32(smem);
+    Misc& sh = *reinterpret_cast<Misc*>(smem + C::kMisc);
+    float* const stats_sh = reinterpret_cast<float*>(smem + C::kStats);
+    volatile int* abort_flag = &sh.abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 32) {
+        init(sh, C::kRing, 10);                                    // an item's readers: the MMA thread, the warp of the statistics, eight warps
+        tma_prefetch_map(&map_q);
+        tma_prefetch_map(&map_go);
+        tma_prefetch_map(&map_k);
+        tma_prefetch_map(&map_v);
+    }
+    if (warp == 2) tmem_alloc(smem_u32(&sh.tmem), kTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem, t_gp = tmem + 128, t_gv = tmem + 256, t_gk = tmem + 384;
+    // tiles of queries that see the item's keys, of one head; tile i of the item is tile first / kRows + i % tiles of head i / tiles
+    auto tiles_of_item = [](const Item& it) { return (it.end - it.begin + kRows - 1) / kRows - it.first / kRows; };
+
+    if (warp == 0) {
+        // ---------------- producer ----------------
+        const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
+        Loader<D, C::kRing> ring(smem, sh.full, sh.empty, &sh.tail, abort_flag, p.status);
+        int items = 0;
+        uint32_t phase_own = 0, phase_taken = 0;
+        unsigned at = blockIdx.x;
+        for (;;) {
+            if (lane == 0) ask_for_next(&sh.answer, &sh.taken);
+            __syncwarp();
+            const int slot = int(at / unsigned(p.Hkv)), kvh = int(at % unsigned(p.Hkv));       // a sequence's first keys, which most rows see, first
+            const Tile t = tile_of<kRows>(p, slot);
+            if (t.first >= 0) {
+                const Item it = {kvh, t.begin, t.end, t.first};
+                if (items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
+                if (ring.ok && lane == 0) {
+                    sh.item[items & 1] = it;
+                    mbar_arrive(smem_u32(&sh.item_full[items & 1]));
+                }
+                if (ring.ok && items >= 1) {
+                    ring.wait(sh.own_empty, phase_own);
+                    phase_own ^= 1u;
+                }
+                ++items;
+                if (ring.ok && lane == 0) {
+                    const uint32_t bar = smem_u32(&sh.own_full);
+                    mbar_expect_tx(bar, 2 * C::kTile);
+                    tma_tile_load_3d(base + C::kOwn, &map_k, 0, it.begin + it.first, kvh * (D / 64), bar, once);
+                    tma_tile_load_3d(base + C::kOwn + C::kTile, &map_v, 0, it.begin + it.first, kvh * (D / 64), bar, once);
+                }
+                __syncwarp();
+                for (int h = kvh * p.G; h < (kvh + 1) * p.G && ring.ok; ++h)
+                    for (int row = it.begin + it.first; row < it.end && ring.ok; row += kRows) {
+                        ring.load(&map_q, row, h * (D / 64), it.end - row, keep);
+                        if (ring.ok) ring.load(&map_go, row, h * (D / 64), it.end - row, keep);
+                    }
+            }
+            const bool before = ring.ok;
+            ring.ok = true;
+            ring.wait(sh.taken, phase_taken);
+            phase_taken ^= 1u;
+            const bool more = ring.ok && answered(&sh.answer, at);
+            ring.ok = ring.ok && before;
+            __syncwarp();
+            if (!ring.ok || !more) break;
+        }
+        if (ring.ok && items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
+        if (ring.ok && lane == 0) {
+            sh.item[items & 1].head = -1;
+            mbar_arrive(smem_u32(&sh.item_full[items & 1]));
+        }
+        if (*abort_flag) ring.drain();
+    } else if (warp == 1) {
+        // ---------------- MMAs: one thread ----------------
+        if (elect_one()) {
+            int at = 0;                                            // tiles used before this item; queries of its tile t in number at + 2 t, gradients behind them
+            uint32_t phase_own = 0, phase_p = 0, phase_read = 0;
+            bool ok = true, began = false;
+            auto wait = [&](uint64_t& bar, uint32_t parity) {
+                ok = ok && mbar_wait(smem_u32(&bar), parity, abort_flag, p.status);
+                tc_fence_after();
+            };
+            auto place = [&](int i) { return base + (i % C::kRing) * C::kTile; };
+            auto arrived = [&](int i) { wait(sh.full[i % C::kRing], uint32_t(i / C::kRing) & 1u); return place(i); };
+            auto release = [&](int i) { mma_commit(smem_u32(&sh.empty[i % C::kRing])); };
+            const uint32_t k_tile = base + C::kOwn, v_tile = k_tile + C::kTile;
+            for (int item = 0; ok; ++item) {
+                wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
+                if (!ok) break;
+                const Item it = sh.item[item & 1];
+                mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+                if (it.head < 0) break;
+                const int n = tiles_of_item(it) * p.G;
+                wait(sh.own_full, phase_own);
+                phase_own ^= 1u;
+                auto scores = [&](int t) {
+                    const uint32_t q_tile = arrived(at + 2 * t);
+                    if (ok) product<D>(tmem, k_tile, q_tile);
+                    mma_commit(smem_u32(&sh.s[0]));
+                };
+                auto gps = [&](int t) {
+                    const uint32_t go_tile = arrived(at + 2 * t + 1);
+                    if (ok) product<D>(t_gp, v_tile, go_tile);
+                    mma_commit(smem_u32(&sh.gp));
+                };
+                if (ok) scores(0);
+                if (ok) gps(0);
+#pragma unroll 1
+                for (int t = 0; t < n && ok; ++t) {
+                    if (t == 0) {
+                        if (began) {
+                            wait(sh.read, phase_read);             // the last item's results have been read
+                            phase_read ^= 1u;
+                        }
+                        began = true;
+                    }
+#pragma unroll 1
+                    for (int half = 0; half < 2 && ok; ++half) {
+                        wait(sh.p[half], phase_p);
+                        if (ok) accumulate<D>(t_gv, tmem + 64u * half, place(at + 2 * t + 1), half, t == 0 && half == 0);
+                    }
+                    release(at + 2 * t + 1);
+                    if (ok && t + 1 < n) scores(t + 1);
+#pragma unroll 1
+                    for (int half = 0; half < 2 && ok; ++half) {
+                        wait(sh.gs[half], phase_p);
+                        if (ok) accumulate<D>(t_gk, t_gp + 64u * half, place(at + 2 * t), half, t == 0 && half == 0);
+                    }
+                    phase_p ^= 1u;
+                    release(at + 2 * t);
+                    if (ok && t + 1 < n) gps(t + 1);
+                }
+                mma_commit(smem_u32(&sh.own_empty));
+                mma_commit(smem_u32(&sh.done));
+                at += 2 * n;
+            }
+        }
+    } else if (warp == 3) {
+        // ---------------- statistics of the tiles' queries ----------------
+        bool ok = true;
+        auto wait = [&](uint64_t& bar, uint32_t parity) { ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspended(smem_u32(&bar), parity, abort_flag, p.status)) && ok; };
+        int k = 0;                                                 // tiles so far
+        for (int item = 0; ok; ++item) {
+            wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
+            if (!ok) break;
+            const Item it = sh.item[item & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+            if (it.head < 0) break;
+            for (int h = it.head * p.G; h < (it.head + 1) * p.G && ok; ++h)
+                for (int row = it.begin + it.first; row < it.end && ok; row += kRows, ++k) {
+                    float2 v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)                    // behind the end: probability 0
+                        v[i] = row + lane + 32 * i < it.end ? stats[int64_t(h) * p.M + row + lane + 32 * i] : make_float2(INFINITY, 0.0f);
+                    if (k >= 2) wait(sh.stats_empty[k & 1], uint32_t((k >> 1) - 1) & 1u);
+                    if (!ok) break;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        stats_sh[256 * (k & 1) + lane + 32 * i] = -v[i].x;
+                        stats_sh[256 * (k & 1) + 128 + lane + 32 * i] = -v[i].y;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sh.stats_full[k & 1]));
+                }
+        }
+    } else if (warp >= 4) {
+        // ---------------- elementwise: thread = key, half of the queries ----------------
+        const int half = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t lanes = uint32_t(quad * 32) << 16, t_s = tmem + lanes + 64u * half, t_g = t_gp + lanes + 64u * half;
+        uint32_t phase = 0, phase_done = 0;
+        int k = 0;
+        bool failed = false;
+        auto wait = [&](uint64_t& bar, uint32_t parity) {
+            failed = __any_sync(0xFFFFFFFFu, !mbar_wait(smem_u32(&bar), parity, abort_flag, p.status)) || failed;
+            tc_fence_after();
+        };
+        const f2 scale2 = mk2(p.scale_log2, p.scale_log2);
+        for (int item = 0;; ++item) {
+            wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
+            if (failed) break;
+            const Item it = sh.item[item & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+            if (it.head < 0) break;
+            const int tiles = tiles_of_item(it), n = tiles * p.G;
+            int of_head = 0;
+            for (int t = 0; t < n; ++t, ++k) {
+                const bool partly = of_head == 0;                  // the tile on the diagonal
+                if (++of_head == tiles) of_head = 0;
+                wait(sh.stats_full[k & 1], uint32_t(k >> 1) & 1u);
+                if (!failed) wait(sh.s[0], phase);
+                if (failed) break;
+                const float4* lse4 = reinterpret_cast<const float4*>(stats_sh + 256 * (k & 1) + 64 * half);
+                const float4* delta4 = lse4 + 32;
+                uint32_t e[2][32], out[32];
+                tmem_ld32(t_s, e[0]);
+                tmem_ld32(t_s + 32u, e[1]);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 64; c += 4) {
+                    const float4 l = lse4[c >> 2];
+                    float a[4];
+                    un2(fma2(mk2(__uint_as_float(e[c >> 5][c & 31]), __uint_as_float(e[c >> 5][(c & 31) + 1])), scale2, mk2(l.x, l.y)), a[0], a[1]);
+                    un2(fma2(mk2(__uint_as_float(e[c >> 5][(c & 31) + 2]), __uint_as_float(e[c >> 5][(c & 31) + 3])), scale2, mk2(l.z, l.w)), a[2], a[3]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float x = ex2(a[i]);
+                        if (partly && 64 * half + c + i < row) x = 0.0f;       // queries before the key
+                        e[c >> 5][(c & 31) + i] = __float_as_uint(x);
+                    }
+                    out[c >> 1] = pack2(__uint_as_float(e[c >> 5][c & 31]), __uint_as_float(e[c >> 5][(c & 31) + 1]));
+                    out[(c >> 1) + 1] = pack2(__uint_as_float(e[c >> 5][(c & 31) + 2]), __uint_as_float(e[c >> 5][(c & 31) + 3]));
+                }
+                tmem_st32(t_s, out);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.p[half]));
+                wait(sh.gp, phase);
+                if (failed) break;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t v[32];
+                    tmem_ld32(t_g + 32u * i, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        const float4 d = delta4[8 * i + (c >> 2)];
+                        float a, b;
+                        un2(mul2(mk2(__uint_as_float(e[i][c]), __uint_as_float(e[i][c + 1])), add2(mk2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), mk2(d.x, d.y))), a, b);
+                        out[16 * i + (c >> 1)] = pack2(a, b);
+                        un2(mul2(mk2(__uint_as_float(e[i][c + 2]), __uint_as_float(e[i][c + 3])),
+                                 add2(mk2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), mk2(d.z, d.w))), a, b);
+                        out[16 * i + (c >> 1) + 1] = pack2(a, b);
+                    }
+                }
+                tmem_st32(t_g, out);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&sh.gs[half]));
+                    mbar_arrive(smem_u32(&sh.stats_empty[k & 1]));
+                }
+                phase ^= 1u;
+            }
+            if (failed) break;
+            wait(sh.done, phase_done);
+            if (failed) break;
+            phase_done ^= 1u;
+            const int r = it.first + row;
+            const bool valid = r < it.end - it.begin;
+            if (half == 0) store_row<D>(t_gv + lanes, gv + int64_t(it.begin + r) * ldgv + int64_t(it.head) * D, valid, 1.0f);
+            else store_row<D>(t_gk + lanes, gk + int64_t(it.begin + r) * ldgk + int64_t(it.head) * D, valid, p.scale);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.read));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 2) tmem_dealloc(tmem, kTmemCols);
+}
+
+template <int D>
+static int launch(const Problem& p, const float* lse, float2* stats, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
+                  int64_t ldgv, cudaStream_t s) {
+    using C = bwd::Cfg<D>;
+    CUtensorMap mq, mgo, mk, mv;
+    int rc = make_x_chunk_tensor_map(&mq, p.q, p.ldq, p.M, int64_t(p.Hq) * D, 128, D / 64);
+    if (!rc) rc = make_x_chunk_tensor_map(&mgo, p.go, p.ldgo, p.M, int64_t(p.Hq) * D, 128, D / 64);
+    if (!rc) rc = make_x_chunk_tensor_map(&mk, p.k, p.ldk, p.M, int64_t(p.Hkv) * D, 128, D / 64);
+    if (!rc) rc = make_x_chunk_tensor_map(&mv, p.v, p.ldv, p.M, int64_t(p.Hkv) * D, 128, D / 64);
+    static std::atomic<uint64_t> configured_q{0}, configured_k{0};
+    if (!rc) rc = allow_dynamic_smem(sequence_query_grad_kernel<D>, C::kBytes, configured_q);
+    if (!rc) rc = allow_dynamic_smem(sequence_key_grad_kernel<D>, C::kBytes, configured_k);
+    if (rc) return rc;
+    const int64_t groups = int64_t(p.M) * p.Hq, tiles = most_tiles(p.M, p.B, bwd::kRows);
+    delta_kernel<D><<<unsigned((groups * (D / 8) + 255) / 256), 256, 0, s>>>(p, lse, stats);
+    if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
+    sequence_query_grad_kernel<D><<<unsigned(tiles * p.Hq), bwd::kThreads, C::kBytes, s>>>(mq, mgo, mk, mv, p, stats, gq, ldgq);
+    if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
+    sequence_key_grad_kernel<D><<<unsigned(tiles * p.Hkv), bwd::kThreads, C::kBytes, s>>>(mq, mgo, mk, mv, p, stats, gk, ldgk, gv, ldgv);
+    return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+}
+int launch_backward(const Problem& p, int D, const float* lse, float2* stats, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
+                    int64_t ldgv, cudaStream_t s) {
+    return D == 128 ? launch<128>(p, lse, stats, gq, ldgq, gk, ldgk, gv, ldgv, s) : launch<64>(p, lse, stats, gq, ldgq, gk, ldgk, gv, ldgv, s);
+}
+
+}  // namespace seq
+}  // namespace patch

@@ -101,17 +101,12 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
         const int slots = int(most_tiles(p.M, p.B, kRows));
-        int stage = 0, issued = 0, items = 0;
-        uint32_t phase = 0, used_q = 0, phase_q = 0, phase_taken = 0, phase_tail = 0;       // used_q, phase_q: bit x
-        bool ok = true;
+        Loader<D, kRing> ring(smem, sh.full, sh.empty, &sh.tail, abort_flag, p.status);
+        int items = 0;
+        uint32_t used_q = 0, phase_q = 0, phase_taken = 0;                   // used_q, phase_q: bit x
         unsigned at = blockIdx.x;
-        auto wait = [&](uint64_t& bar, uint32_t parity) { ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bar), parity, abort_flag, p.status)) && ok; };
         for (;;) {
-            if (lane == 0) {
-                mbar_expect_tx(smem_u32(&sh.taken), 16);
-                asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(&sh.answer)),
-                             "r"(smem_u32(&sh.taken)) : "memory");
-            }
+            if (lane == 0) ask_for_next(&sh.answer, &sh.taken);
             __syncwarp();
             if (at == 0) check_starts(p, lane, 32);
             // a sequence's last rows, which see most keys, first; heads that share keys side by side
@@ -119,85 +114,47 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             const Tile t = tile_of<kRows>(p, slot);
             if (t.first >= 0) {
                 const Item it = {head, t.begin, t.end, t.first};
-                if (items >= 2) wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
-                if (ok && lane == 0) {
+                if (items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
+                if (ring.ok && lane == 0) {
                     sh.item[items & 1] = it;
                     mbar_arrive(smem_u32(&sh.item_full[items & 1]));
                 }
                 ++items;
-                const int n = max(tiles_of_stream(it, 0), tiles_of_stream(it, 1)), len = it.end - it.begin, kv_chunk = head / p.G * (D / 64);
-                // tile of keys or values into the ring
-                auto load = [&](const CUtensorMap* map, int tile, bool values) {
-                    if (issued >= kRing) wait(sh.empty[stage], phase ^ 1u);
-                    if (!ok) return;
-                    const uint32_t dst = base + stage * C::kTile, full = smem_u32(&sh.full[stage]);
-                    const int left = len - tile * kKeys;           // rows of the tile that belong to the sequence
-                    const bool partly = values && left < kKeys;
-                    const uint32_t bar = partly ? smem_u32(&sh.tail) : full;
-                    if (lane == 0) {
-                        mbar_expect_tx(bar, C::kTile);
-                        tma_tile_load_3d(dst, map, 0, it.begin + tile * kKeys, kv_chunk, bar, keep);
-                    }
-                    __syncwarp();
-                    if (partly) {
-                        wait(sh.tail, phase_tail);
-                        phase_tail ^= 1u;
-                        for (int i = left * (D / 8) + lane; i < kKeys * (D / 8); i += 32) {
-                            const int r = i / (D / 8), c = i - r * (D / 8);
-                            *reinterpret_cast<uint4*>(smem + stage * C::kTile + (c >> 3) * C::kAtom + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                        }
-                        fence_async_shared();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(full);
-                    }
-                    ++issued;
-                    if (++stage == kRing) { stage = 0; phase ^= 1u; }
-                };
-                for (int x = 0; x < 2 && ok; ++x) {
+                for (int x = 0; x < 2 && ring.ok; ++x) {
                     if (!tiles_of_stream(it, x)) continue;
                     if ((used_q >> x) & 1u) {
-                        wait(sh.q_empty[x], (phase_q >> x) & 1u);
+                        ring.wait(sh.q_empty[x], (phase_q >> x) & 1u);
                         phase_q ^= 1u << x;
                     }
                     used_q |= 1u << x;
-                    if (ok && lane == 0) {
+                    if (ring.ok && lane == 0) {
                         mbar_expect_tx(smem_u32(&sh.q_full[x]), C::kTile);
                         tma_tile_load_3d(base + C::kQ + x * C::kTile, &map_q, 0, it.begin + it.first + 128 * x, head * (D / 64), smem_u32(&sh.q_full[x]), once);
                     }
                 }
-                for (int j = 0; j < n && ok; ++j) {
-                    load(&map_k, j, false);
-                    if (ok) load(&map_v, j, true);
+                const int n = max(tiles_of_stream(it, 0), tiles_of_stream(it, 1)), chunk = head / p.G * (D / 64);
+                for (int j = 0; j < n && ring.ok; ++j) {
+                    const int row = it.begin + j * kKeys;
+                    ring.load(&map_k, row, chunk, kKeys, keep);
+                    if (ring.ok) ring.load(&map_v, row, chunk, it.end - row, keep);
                 }
             }
-            // the next item, if there is one; an answer on its way is waited for whatever happened
-            const bool before = ok;
-            ok = true;
-            wait(sh.taken, phase_taken);
+            // the answer is waited for whatever happened
+            const bool before = ring.ok;
+            ring.ok = true;
+            ring.wait(sh.taken, phase_taken);
             phase_taken ^= 1u;
-            uint32_t next = 0, there = 0;
-            if (ok) {
-                asm volatile("{\n\t.reg .pred p;\n\t.reg .b128 r;\n\tld.shared.b128 r, [%2];\n\tclusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
-                             "selp.u32 %1, 1, 0, p;\n\tmov.u32 %0, 0;\n\t@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, _, _, _}, r;\n\t}"
-                             : "=r"(next), "=r"(there) : "r"(smem_u32(&sh.answer)) : "memory");
-                fence_async_shared();
-            }
-            ok = ok && before;
+            const bool more = ring.ok && answered(&sh.answer, at);
+            ring.ok = ring.ok && before;
             __syncwarp();
-            if (!ok || !there) break;
-            at = next;
+            if (!ring.ok || !more) break;
         }
-        if (ok && items >= 2) wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
-        if (ok && lane == 0) {
+        if (ring.ok && items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
+        if (ring.ok && lane == 0) {
             sh.item[items & 1].head = -1;
             mbar_arrive(smem_u32(&sh.item_full[items & 1]));
         }
-        if (*abort_flag) {                   // copies on their way end before the CTA does
-            const uint64_t t0 = global_timer_ns();
-            for (int j = issued > kRing ? issued - kRing : 0; j < issued; ++j)
-                while (!mbar_try_wait(smem_u32(&sh.full[j % kRing]), uint32_t(j / kRing) & 1u) && global_timer_ns() - t0 < kDrainLimitNs) {}
-            while (global_timer_ns() - t0 < kDrainLimitNs) {}                // queries
-        }
+        if (*abort_flag) ring.drain();
     } else if (warp == 1) {
         // ---------------- MMAs: one thread ----------------
         constexpr uint32_t idesc_s = instr_desc(kKeys, false), idesc_o = instr_desc(D, false) | (1u << 16);      // V is MN-major
