@@ -23,9 +23,13 @@ namespace logits {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kPerSm = 3;                    // CTAs that fit an SM: 80 registers a thread
 constexpr int kAhead = 4;                    // vectors of 16 bytes that a thread has on their way together
 constexpr int kMost = 256;                   // alternatives or teacher's entries of a row, at most; kMost <= kThreads
 constexpr int kCandidates = 2048;
+constexpr int kCells = 32;                   // see Cells, per thread
+constexpr int kFound = 2048;                 // cells that reach the border, most often k to 1.5 k
+constexpr size_t kListBytes = kCandidates * sizeof(uint64_t) + kFound * sizeof(uint32_t);
 constexpr int kMaxParts = 8;                 // CTAs of a cluster that share a row
 constexpr int64_t kMaxV = int64_t(1) << 20;  // a bit per element fits shared memory
 static_assert(kMost <= kThreads && kMaxParts * kMost <= kCandidates, "lists of all parts of a row fit the candidates");
@@ -52,6 +56,7 @@ template <> struct Vec<__nv_bfloat16> {
     static constexpr int N = 8;
     uint32_t w[4];
     __device__ __forceinline__ void set(uint4 v) { w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+    __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0xFF80FF80u; }          // -inf
     __device__ __forceinline__ void hide(uint32_t mask) {          // elements whose bit is set: -inf
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -70,6 +75,7 @@ template <> struct Vec<float> {
     static constexpr int N = 4;
     uint32_t w[4];
     __device__ __forceinline__ void set(uint4 v) { w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+    __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0xFF800000u; }
     __device__ __forceinline__ void hide(uint32_t mask) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -96,6 +102,8 @@ template <class T> __device__ __forceinline__ T rounded(float x);
 template <> __device__ __forceinline__ float rounded<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 rounded<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
+template <class T> struct Batch { Vec<T> v[kAhead]; };
+
 // A CTA's part of a row: vector numbers part * kThreads + thread, then every parts * kThreads-th.  The row's last vector may be short.
 template <class T> struct Row {
     static constexpr int N = Vec<T>::N;
@@ -111,8 +119,7 @@ template <class T> struct Row {
             x.set(load16(z + int64_t(v) * N));
             return x;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x.w[i] = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+        x.clear();
         if (v < count) {
             for (int i = v * N; i < V; ++i) {
                 if constexpr (sizeof(T) == 2) {
@@ -135,17 +142,30 @@ template <class T> struct Row {
                 if (v * N + i < V) g[v * N + i] = rounded<T>(y[i]);
         }
     }
-    // f(vector number, vector) for all vectors of this thread, kAhead of them loaded together
-    template <class F> __device__ __forceinline__ void each(F&& f) const {
-        int v = first;
-        for (; v + (kAhead - 1) * step < whole; v += kAhead * step) {
-            Vec<T> x[kAhead];
+    // A thread's vectors come in batches that are loaded together, one batch ahead of the arithmetic.  Batch b holds vectors
+    // at(b, 0) .. at(b, kAhead - 1); those that are not whole are -inf (the row's short last vector is the caller's: `rest`).
+    __device__ __forceinline__ int at(int b, int u) const { return first + (b * kAhead + u) * step; }
+    __device__ __forceinline__ int batches() const { return whole > first ? (whole - first + kAhead * step - 1) / (kAhead * step) : 0; }
+    __device__ __forceinline__ void fetch(Batch<T>& x, int b) const {
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) x[u].set(load16(z + int64_t(v + u * step) * N));
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) f(v + u * step, x[u]);
+        for (int u = 0; u < kAhead; ++u) {
+            const int v = at(b, u);
+            if (v < whole) x.v[u].set(load16(z + int64_t(v) * N));
+            else x.v[u].clear();
         }
-        for (; v < count; v += step) f(v, load(v));
+    }
+    __device__ __forceinline__ bool rest() const { return count > whole && whole >= first && (whole - first) % step == 0; }
+    // f(batch number, batch) for all of them; `ahead` holds the first one, and whatever next(ahead) fetches afterwards
+    template <class F, class Next> __device__ __forceinline__ void each(Batch<T>& ahead, F&& f, Next&& next) const {
+        const int n = batches();
+        if (n == 0) next(ahead);
+#pragma unroll 2
+        for (int b = 0; b < n; ++b) {
+            Batch<T> x = ahead;
+            if (b + 1 < n) fetch(ahead, b + 1);
+            else next(ahead);
+            f(b, x);
+        }
     }
 };
 
@@ -167,22 +187,30 @@ struct Shared {
     int scan[kWarps];
 };
 
+// Sums of 32 lanes, of the first N of them: the largest maximum, then every lane's sums times one factor, added up in a fixed order.
+template <int N> __device__ __forceinline__ Sums sum_of_lanes(Sums x, float c) {
+    float m = x.m;
+#pragma unroll
+    for (int d = N / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+    if (x.m > -INFINITY) {                   // else nothing, or NaN
+        const float d = fmaxf(x.m - m, -1e30f), f = ex2(d * c);
+        x.t = f * (x.t + d * x.s);
+        x.s *= f;
+    }
+#pragma unroll
+    for (int d = N / 2; d > 0; d >>= 1) {
+        x.s += __shfl_xor_sync(0xFFFFFFFFu, x.s, d);
+        x.t += __shfl_xor_sync(0xFFFFFFFFu, x.t, d);
+    }
+    return Sums{m, x.s, x.t};
+}
 // Sums of a row from those of every thread; all threads get them.  `c`: log2(e) / T.
 __device__ __forceinline__ Sums sum_up(Sums x, float c, Shared& sh, int parts) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        const Sums o = {__shfl_xor_sync(0xFFFFFFFFu, x.m, d), __shfl_xor_sync(0xFFFFFFFFu, x.s, d), __shfl_xor_sync(0xFFFFFFFFu, x.t, d)};
-        x = (lane & d) ? join(o, x, c) : join(x, o, c);                  // the same order in both lanes: the same bits
-    }
+    x = sum_of_lanes<32>(x, c);
     if (lane == 0) sh.warp[warp] = x;
     __syncthreads();
-    x = sh.warp[lane & (kWarps - 1)];
-#pragma unroll
-    for (int d = kWarps / 2; d > 0; d >>= 1) {
-        const Sums o = {__shfl_xor_sync(0xFFFFFFFFu, x.m, d), __shfl_xor_sync(0xFFFFFFFFu, x.s, d), __shfl_xor_sync(0xFFFFFFFFu, x.t, d)};
-        x = (lane & d) ? join(o, x, c) : join(x, o, c);
-    }
+    x = sum_of_lanes<kWarps>(sh.warp[lane & (kWarps - 1)], c);
     if (parts == 1) {
         __syncthreads();                     // sh.warp may be written again
         return x;
@@ -200,45 +228,85 @@ __device__ __forceinline__ Sums sum_up(Sums x, float c, Shared& sh, int parts) {
     return x;
 }
 
-// One pass over a thread's elements.  HIDE: elements whose bit is set in `bits` do not count.
-template <class T, bool ENTROPY, bool HIDE>
-__device__ __forceinline__ Sums scan_row(const Row<T>& row, float c, const uint32_t* bits) {
-    constexpr int N = Vec<T>::N;
-    Sums x = {-INFINITY, 0.0f, 0.0f};
+// One pass over a thread's elements, COUNT vectors at a time.  HIDE: elements whose bit is set in `bits` do not count.
+template <class T, bool ENTROPY>
+struct Scan {
+    static constexpr int N = Vec<T>::N;
+    float m = -INFINITY, c;
     f2 s2 = 0ull, t2 = 0ull;
-    const f2 c2 = mk2(c, c);
-    row.each([&](int v, Vec<T> e) {
-        if (HIDE) {
-            const uint32_t mask = (bits[v / (32 / N)] >> (v % (32 / N) * N)) & ((1u << N) - 1u);
-            if (mask) e.hide(mask);
-        }
-        const float top = e.top();
-        if (top > x.m) {
-            if (x.m > -INFINITY) {
-                const float d = fmaxf(x.m - top, -1e30f), f = ex2(d * c);
+    __device__ __forceinline__ explicit Scan(float c_) : c(c_) {}
+    template <int COUNT> __device__ __forceinline__ float take(const Vec<T> (&e)[COUNT]) {       // returns the largest element
+        float top = e[0].top();
+#pragma unroll
+        for (int u = 1; u < COUNT; ++u) top = fmaxf(top, e[u].top());
+        if (top > m) {
+            if (m > -INFINITY) {
+                const float d = fmaxf(m - top, -1e30f), f = ex2(d * c);
                 if (ENTROPY) t2 = mul2(mk2(f, f), fma2(mk2(d, d), s2, t2));
                 s2 = mul2(mk2(f, f), s2);
             }
-            x.m = top;
+            m = top;
         }
-        const float base = x.m == -INFINITY ? 0.0f : x.m;
-        const f2 b2 = mk2(-base, -base);
+        const float base = m == -INFINITY ? 0.0f : m;
+        const f2 b2 = mk2(-base, -base), c2 = mk2(c, c);
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const f2 d = add2(e.pair(i), b2);
-            float a, b;
-            un2(mul2(d, c2), a, b);
-            const f2 p = mk2(ex2(a), ex2(b));
-            s2 = add2(s2, p);
-            if (ENTROPY) {
-                un2(d, a, b);                // a masked element: 0 times a number, not times -inf
-                t2 = fma2(p, mk2(fmaxf(a, -1e30f), fmaxf(b, -1e30f)), t2);
+        for (int u = 0; u < COUNT; ++u)
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const f2 d = add2(e[u].pair(i), b2);
+                float a, b;
+                un2(mul2(d, c2), a, b);
+                const f2 p = mk2(ex2(a), ex2(b));
+                s2 = add2(s2, p);
+                if (ENTROPY) {
+                    un2(d, a, b);            // a masked element: 0 times a number, not times -inf
+                    t2 = fma2(p, mk2(fmaxf(a, -1e30f), fmaxf(b, -1e30f)), t2);
+                }
+            }
+        return top;
+    }
+    __device__ __forceinline__ Sums sums() const { return Sums{m, sum2(s2), sum2(t2)}; }
+};
+template <class T> __device__ __forceinline__ void hide_listed(Vec<T>& x, int v, const uint32_t* bits) {
+    constexpr int N = Vec<T>::N;
+    const uint32_t mask = (bits[v / (32 / N)] >> (v % (32 / N) * N)) & ((1u << N) - 1u);
+    if (mask) x.hide(mask);
+}
+// The largest element of every 2^shift batches of a thread, for the alternatives: cell [batch >> shift][thread].
+struct Cells {
+    float* at;
+    int shift;
+    static __host__ __device__ int shift_of(int batches) {
+        int s = 0;
+        while ((batches >> s) >= kCells) ++s;
+        return s;
+    }
+};
+template <class T, bool ENTROPY, bool HIDE, bool TOP, class Next>
+__device__ __forceinline__ Sums scan_row(const Row<T>& row, Batch<T>& ahead, float c, const uint32_t* bits, const Cells& cells, Next&& next) {
+    Scan<T, ENTROPY> scan(c);
+    float cell = -INFINITY;
+    row.each(ahead, [&](int b, Batch<T>& x) {
+        if (HIDE) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (row.at(b, u) < row.whole) hide_listed(x.v[u], row.at(b, u), bits);
+        }
+        const float top = scan.take(x.v);
+        if (TOP) {
+            cell = fmaxf(cell, top);
+            if (((b + 1) & ((1 << cells.shift) - 1)) == 0 || b + 1 == row.batches()) {
+                cells.at[(b >> cells.shift) * kThreads + threadIdx.x] = cell;
+                cell = -INFINITY;
             }
         }
-    });
-    x.s = sum2(s2);
-    x.t = sum2(t2);
-    return x;
+    }, next);
+    if (row.rest()) {
+        Vec<T> x[1] = {row.load(row.whole)};
+        if (HIDE) hide_listed(x[0], row.whole, bits);
+        scan.take(x);
+    }
+    return scan.sums();
 }
 
 // Order of the alternatives: larger value first, then lower index.  A value's sort key; NaN counts as -inf, -0 as 0.
@@ -260,20 +328,25 @@ __device__ __forceinline__ int block_sum(int n, Shared& sh) {
     return sum;
 }
 
-// The k first candidates of `list` [n], in order, to `out`.  Keys are distinct.
+// The k first candidates of `list` [n], in order, to `out`.  Keys are distinct.  Eight lanes count for one candidate.
 __device__ __forceinline__ void rank(const uint64_t* list, int n, int k, uint64_t* out) {
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const uint64_t mine = list[i];
+    const int sub = threadIdx.x & 7;
+    for (int i0 = 0; i0 < n; i0 += kThreads / 8) {
+        const int i = i0 + (threadIdx.x >> 3);
+        const uint64_t mine = i < n ? list[i] : 0ull;
         int before = 0;
-        for (int j = 0; j < n; ++j) before += list[j] > mine;
-        if (before < k) out[before] = mine;
+#pragma unroll 4
+        for (int j = sub; j < n; j += 8) before += list[j] > mine;
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1) before += __shfl_xor_sync(0xFFFFFFFFu, before, d);
+        if (sub == 0 && i < n && before < k) out[before] = mine;
     }
 }
 
-// The first k elements, in order, of this CTA's part of a row (which has k) -> top[k].  `best`: the largest of the thread's elements.
-// All threads of the CTA; ends with a barrier.
+// The first k elements, in order, of this CTA's part of a row (which has k) -> top[k].  `best`: the largest of the thread's elements; `cells`:
+// of its batches.  All threads of the CTA; ends with a barrier.
 template <class T>
-__device__ __forceinline__ void top_of_part(const Row<T>& row, float best, int k, uint64_t* list, uint64_t* top, Shared& sh) {
+__device__ __forceinline__ void top_of_part(const Row<T>& row, float best, const Cells& cells, int k, uint64_t* list, uint64_t* top, Shared& sh) {
     constexpr int N = Vec<T>::N;
     constexpr int kLowest = sizeof(T) == 2 ? 16 : 0;                      // bf16 keys differ in their high halves
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -285,31 +358,56 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, float best, int k
         if (n >= k) border = next;
         if (n == k) break;
     }
-    // elements of threads whose best reaches the border, by the whole warp; keys from `least` on
-    auto gather = [&](uint32_t least, bool all) {
-        if (threadIdx.x == 0) sh.n = 0;
-        __syncthreads();
-        for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, all ? row.first < row.count : mine >= least && mine); todo; todo &= todo - 1) {
-            const int who = __ffs(todo) - 1, from = row.first - lane + who;
-            for (int v0 = from + lane * row.step; v0 - lane * row.step < row.count; v0 += 32 * row.step) {
-                const Vec<T> x = row.load(v0);
+    // candidates of vector v whose keys are `least` or more
+    auto look = [&](int v, uint32_t least) {
+        const Vec<T> x = row.load(v);
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const uint32_t key = key_of(element(x, i));
-                    if ((key >> kLowest) >= least && int64_t(v0) * N + i < row.V) {
-                        const int at = atomicAdd(&sh.n, 1);
-                        if (at < kCandidates) list[at] = candidate(key, v0 * N + i);
-                    }
-                }
+        for (int i = 0; i < N; ++i) {
+            const uint32_t key = key_of(element(x, i));
+            if ((key >> kLowest) >= least && v * N + i < row.V) {
+                const int at = atomicAdd(&sh.n, 1);
+                if (at < kCandidates) list[at] = candidate(key, v * N + i);
             }
         }
-        __syncthreads();
-        const int n = sh.n;
-        __syncthreads();
-        return n;
     };
-    int n = gather(border, false);
-    if (n <= kCandidates) {
+    // cells that reach the border, and the short last vector
+    uint32_t* const found = reinterpret_cast<uint32_t*>(list + kCandidates);
+    if (threadIdx.x == 0) sh.n = sh.n2 = 0;
+    __syncthreads();
+    if (mine >= border && mine) {
+        const int n = (row.batches() + (1 << cells.shift) - 1) >> cells.shift;
+        for (int g = 0; g < n; ++g)
+            if ((key_of(cells.at[g * kThreads + threadIdx.x]) >> kLowest) >= border) {
+                const int at = atomicAdd(&sh.n2, 1);
+                if (at < kFound) found[at] = uint32_t(g) << 16 | threadIdx.x;
+            }
+        if (row.rest()) look(row.whole, border);
+    }
+    __syncthreads();
+    int n = sh.n2;
+    auto key_of_cell = [&](uint32_t f) { return key_of(cells.at[(f >> 16) * kThreads + (f & 0xFFFFu)]) >> kLowest; };
+    if (n > 2 * k && n <= kFound) {          // the threads' bests were few for a k of this size: the k-th cell is a better border
+        uint32_t better = 0;
+        for (int bit = 31 - kLowest; bit >= 0; --bit) {
+            int sum = 0;
+            for (int i = threadIdx.x; i < n; i += kThreads) sum += key_of_cell(found[i]) >= (better | (1u << bit));
+            if (block_sum(sum, sh) >= k) better |= 1u << bit;
+        }
+        border = max(border, better);
+    }
+    if (n <= kFound) {
+        const int each = kAhead << cells.shift;                    // vectors of a cell
+        for (int i = threadIdx.x; i < n * each; i += kThreads) {
+            const uint32_t f = found[i / each];
+            const int v = row.first - int(threadIdx.x) + int(f & 0xFFFFu) + (int(f >> 16) * each + i % each) * row.step;
+            if (v < row.whole && key_of_cell(f) >= border) look(v, border);
+        }
+    }
+    __syncthreads();
+    const bool few = n <= kFound && sh.n <= kCandidates;
+    n = sh.n;
+    __syncthreads();
+    if (few) {
         rank(list, n, k, top);
         __syncthreads();
         return;
@@ -329,8 +427,11 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, float best, int k
         for (int bit = 31 - kLowest; bit >= 0; --bit)
             if (count(border | (1u << bit)) >= k) border |= 1u << bit;
     }
-    n = gather(border + 1, true);            // fewer than k
-    int have = n;
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+    for (int v = row.first; v < row.count; v += row.step) look(v, border + 1);                   // fewer than k
+    __syncthreads();
+    int have = sh.n;
     for (int v0 = row.first - threadIdx.x; v0 < row.count && have < k; v0 += row.step) {         // and the first ones that equal it
         const int v = v0 + threadIdx.x;
         uint32_t equal = 0;
@@ -371,7 +472,7 @@ __device__ __forceinline__ void top_of_part(const Row<T>& row, float best, int k
 
 struct LogProbs {
     int64_t ldz, M;
-    int V, k, parts;
+    int V, k, parts, cell_shift;
     float c, temperature;
     const int64_t* tokens;
     float *logp, *entropy, *lse, *top_logp;
@@ -379,19 +480,25 @@ struct LogProbs {
     int* status;
 };
 
-template <class T, bool ENTROPY>
-__global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const T* z, const LogProbs p) {
+template <class T, bool ENTROPY, bool TOP>
+__global__ void __launch_bounds__(kThreads, kPerSm) logprobs_kernel(const T* z, const LogProbs p) {
     __shared__ Shared sh;
-    __shared__ uint64_t top[kMost];
-    extern __shared__ uint64_t list[];       // kCandidates, where k > 0
+    __shared__ uint64_t top[TOP ? kMost : 1];
+    extern __shared__ uint64_t list[];       // TOP: kCandidates, then numbers of kFound cells, then the cells
+    const Cells cells = {reinterpret_cast<float*>(list + kCandidates) + kFound, p.cell_shift};
     const int part = p.parts > 1 ? int(cluster_ctarank()) : 0;
-    for (int64_t m = blockIdx.x / p.parts; m < p.M; m += gridDim.x / p.parts) {
+    const int64_t rows = gridDim.x / p.parts;
+    Batch<T> ahead;
+    if (int64_t m = blockIdx.x / p.parts; m < p.M) Row<T>(z + m * p.ldz, p.V, part, p.parts).fetch(ahead, 0);
+    for (int64_t m = blockIdx.x / p.parts; m < p.M; m += rows) {
         const Row<T> row(z + m * p.ldz, p.V, part, p.parts);
-        const Sums own = scan_row<T, ENTROPY, false>(row, p.c, nullptr);
+        const Sums own = scan_row<T, ENTROPY, false, TOP>(row, ahead, p.c, nullptr, cells, [&](Batch<T>& x) {
+            if (m + rows < p.M) Row<T>(z + (m + rows) * p.ldz, p.V, part, p.parts).fetch(x, 0);
+        });
         const Sums x = sum_up(own, p.c, sh, p.parts);
         const float base = x.m == -INFINITY ? 0.0f : x.m;
         const bool none = x.m == -INFINITY && !(x.s != x.s);      // every element is -inf: no distribution
-        const float ln = logf(x.s);
+        const float ln = TOP || (part == 0 && threadIdx.x == 0) ? logf(x.s) : 0.0f;
         if (part == 0 && threadIdx.x == 0) {
             if (p.tokens) {
                 const int64_t t = p.tokens[m];
@@ -406,8 +513,8 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const T* z, const
             if (p.lse) p.lse[m] = none ? -INFINITY : base / p.temperature + ln;
             if (ENTROPY) p.entropy[m] = none ? 0.0f : ln - x.t / (x.s * p.temperature);
         }
-        if (p.k) {
-            top_of_part(row, own.m, p.k, list, top, sh);
+        if (TOP) {
+            top_of_part(row, own.m, cells, p.k, list, top, sh);
             if (p.parts > 1) {
                 cluster_sync_all();
                 if (part == 0) {
@@ -466,7 +573,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_grad_kernel(const T* z, T* 
     const float base = lse * p.temperature, h = ENTROPY ? p.entropy[m] : 0.0f, a = -up;
     const int tv = token >= 0 ? int(token) / N : -1;
     constexpr float kLn2 = 0.693147180559945f;
-    row.each([&](int v, const Vec<T>& x) {
+    auto one = [&](int v, const Vec<T>& x) {
         float y[N];
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
@@ -484,7 +591,15 @@ __global__ void __launch_bounds__(kThreads) logprobs_grad_kernel(const T* z, T* 
                 if (tv * N + i == token) y[i] += up;
         }
         row.store(g, v, y);
-    });
+    };
+    Batch<T> ahead;
+    row.fetch(ahead, 0);
+    row.each(ahead, [&](int b, const Batch<T>& x) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (row.at(b, u) < row.whole) one(row.at(b, u), x.v[u]);
+    }, [](Batch<T>&) {});
+    if (row.rest()) one(row.whole, row.load(row.whole));
 }
 
 struct Distill {
@@ -571,10 +686,11 @@ __device__ __forceinline__ Entry entry_of(const Distill& p, int64_t m, const T* 
 }
 // Gradient of a row's part: w_v (c p_rest - q_rest) g / T for elements that are not listed, w_v = 2^((x - base) c) / rest_s (all
 // elements where REST is false: p_v g / T), then the listed ones, which need the barrier.
-template <class T>
-__device__ __forceinline__ void write_gradient(const Row<T>& row, T* g, float base, float c, float factor, const Entry& e, float listed, int parts, int part) {
+template <class T, class Next>
+__device__ __forceinline__ void write_gradient(const Row<T>& row, Batch<T>& ahead, T* g, float base, float c, float factor, const Entry& e, float listed, int parts,
+                                               int part, Next&& next) {
     constexpr int N = Vec<T>::N;
-    row.each([&](int v, const Vec<T>& x) {
+    auto one = [&](int v, const Vec<T>& x) {
         float y[N];
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
@@ -583,7 +699,13 @@ __device__ __forceinline__ void write_gradient(const Row<T>& row, T* g, float ba
             un2(mul2(mk2(ex2(a), ex2(b)), mk2(factor, factor)), y[2 * i], y[2 * i + 1]);
         }
         row.store(g, v, y);
-    });
+    };
+    row.each(ahead, [&](int b, const Batch<T>& x) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (row.at(b, u) < row.whole) one(row.at(b, u), x.v[u]);
+    }, next);
+    if (row.rest()) one(row.whole, row.load(row.whole));
     __syncthreads();
     if (e.first && (e.id / N / kThreads) % parts == part) g[e.id] = rounded<T>(listed);
 }
@@ -594,7 +716,7 @@ __device__ __forceinline__ void write_zeros(const Row<T>& row, T* g) {
 }
 
 template <class T, bool REST, bool GRAD>
-__global__ void __launch_bounds__(kThreads, 4) distill_kernel(const T* z, T* gz, const Distill p) {
+__global__ void __launch_bounds__(kThreads, kPerSm) distill_kernel(const T* z, T* gz, const Distill p) {
     __shared__ Shared sh;
     extern __shared__ uint32_t bits[];       // REST: a bit per element, set where it is listed
     const int part = p.parts > 1 ? int(cluster_ctarank()) : 0;
@@ -602,15 +724,23 @@ __global__ void __launch_bounds__(kThreads, 4) distill_kernel(const T* z, T* gz,
         for (int i = threadIdx.x; i < (p.V + 31) / 32; i += kThreads) bits[i] = 0u;
         __syncthreads();
     }
-    for (int64_t m = blockIdx.x / p.parts; m < p.M; m += gridDim.x / p.parts) {
+    const int64_t rows = gridDim.x / p.parts;
+    Batch<T> ahead;
+    if (int64_t m = blockIdx.x / p.parts; m < p.M) Row<T>(z + m * p.ldz, p.V, part, p.parts).fetch(ahead, 0);
+    for (int64_t m = blockIdx.x / p.parts; m < p.M; m += rows) {
         const Row<T> row(z + m * p.ldz, p.V, part, p.parts);
+        auto next_row = [&](Batch<T>& x) {
+            if (m + rows < p.M) Row<T>(z + (m + rows) * p.ldz, p.V, part, p.parts).fetch(x, 0);
+        };
         float q_sum;
         const Entry e = entry_of<T, REST>(p, m, row.z, q_sum, sh);
         if (REST) {
             if (e.first) atomicOr(&bits[e.id >> 5], 1u << (e.id & 31));
             __syncthreads();
         }
-        const Sums x = sum_up(scan_row<T, false, REST>(row, p.c, bits), p.c, sh, p.parts);
+        const Sums x = sum_up(scan_row<T, false, REST, false>(row, ahead, p.c, bits, Cells{}, [&](Batch<T>& y) {
+                                  if (GRAD) row.fetch(y, 0); else next_row(y);
+                              }), p.c, sh, p.parts);
         if (REST && e.first) atomicAnd(&bits[e.id >> 5], ~(1u << (e.id & 31)));       // read again only behind the next row's barriers
         // the sums over all elements, and which part of them is not listed
         Sums all = x;
@@ -639,9 +769,10 @@ __global__ void __launch_bounds__(kThreads, 4) distill_kernel(const T* z, T* gz,
             T* const to = gz + m * p.ldg;
             if (g == 0.0f || none) {
                 write_zeros(row, to);
+                next_row(ahead);
             } else {
                 const float q_all = q_sum + q_rest, factor = x.s == 0.0f ? 0.0f : g * (q_all * p_rest - q_rest) / x.s;
-                write_gradient(row, to, x.m == -INFINITY ? 0.0f : x.m, p.c, factor, e, g * (q_all * expf(lnp) - e.q_all), p.parts, part);
+                write_gradient(row, ahead, to, x.m == -INFINITY ? 0.0f : x.m, p.c, factor, e, g * (q_all * expf(lnp) - e.q_all), p.parts, part, next_row);
             }
         }
         if (p.parts > 1) cluster_sync_all(); else __syncthreads();
@@ -664,14 +795,16 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(const T* z, T* g
     }
     const float q_rest = REST ? fmaxf(1.0f - q_sum, 0.0f) : 0.0f, q_all = q_sum + q_rest;
     const bool none = ln_rest == -INFINITY;                        // everything is listed, or masked
-    write_gradient(row, to, none ? 0.0f : (lse + ln_rest) * p.temperature, p.c, none ? 0.0f : g * (q_all * expf(ln_rest) - q_rest), e,
-                   g * (q_all * expf(e.x / p.temperature - lse) - e.q_all), p.parts, part);
+    Batch<T> ahead;
+    row.fetch(ahead, 0);
+    write_gradient(row, ahead, to, none ? 0.0f : (lse + ln_rest) * p.temperature, p.c, none ? 0.0f : g * (q_all * expf(ln_rest) - q_rest), e,
+                   g * (q_all * expf(e.x / p.temperature - lse) - e.q_all), p.parts, part, [](Batch<T>&) {});
 }
 
 // CTAs that share a row.  Four CTAs fit an SM; a row is shared (and read by a cluster, which joins its sums in distributed shared memory) where
 // rows alone would leave SMs empty, as long as every thread keeps a few vectors.
 static int parts_of(int64_t M, int64_t vectors) {
-    const int64_t room = 4 * int64_t(sm_count());
+    const int64_t room = kPerSm * int64_t(sm_count());
     int parts = 1;
     while (parts < kMaxParts && M * parts * 2 <= room && vectors >= int64_t(parts) * 2 * kThreads) parts *= 2;
     return parts;
@@ -683,7 +816,7 @@ static int64_t segments_of(int64_t vectors) {
 }
 template <class... A>
 static int launch_rows(void (*kern)(A...), int64_t M, int parts, size_t smem, cudaStream_t s, A... args) {
-    const int64_t most = (int64_t(sm_count()) * 4) / parts, clusters = M < most ? M : most;
+    const int64_t most = (int64_t(sm_count()) * kPerSm) / parts, clusters = M < most ? M : most;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     cfg.gridDim = dim3(unsigned(clusters * parts), 1, 1);
@@ -697,6 +830,26 @@ static int launch_rows(void (*kern)(A...), int64_t M, int parts, size_t smem, cu
     if (cudaLaunchKernelEx(&cfg, kern, args...) == cudaSuccess) return PATCH_OK;
     cudaGetLastError();                      // reported here, not by the next call
     return PATCH_ERR_CUDA;
+}
+
+template <class T, bool ENTROPY, bool TOP>
+static int launch_logprobs(const T* z, LogProbs p, cudaStream_t s) {
+    auto kern = logprobs_kernel<T, ENTROPY, TOP>;
+    size_t smem = 0;
+    if (TOP) {
+        const int vectors = p.V / Vec<T>::N, batches = (vectors + p.parts * kThreads * kAhead - 1) / (p.parts * kThreads * kAhead);
+        p.cell_shift = Cells::shift_of(batches);
+        smem = kListBytes + size_t((batches + (1 << p.cell_shift) - 1) >> p.cell_shift) * kThreads * sizeof(float);
+        static std::atomic<uint64_t> configured{0};
+        if (int rc = allow_dynamic_smem(kern, uint32_t(kListBytes + kCells * kThreads * sizeof(float)), configured)) return rc;
+    }
+    return launch_rows(kern, p.M, p.parts, smem, s, z, p);
+}
+template <class T>
+static int launch_logprobs(const void* Z, const LogProbs& p, cudaStream_t s) {
+    const T* z = static_cast<const T*>(Z);
+    if (p.k) return p.entropy ? launch_logprobs<T, true, true>(z, p, s) : launch_logprobs<T, false, true>(z, p, s);
+    return p.entropy ? launch_logprobs<T, true, false>(z, p, s) : launch_logprobs<T, false, false>(z, p, s);
 }
 
 // ---- checks of arguments ----
@@ -734,16 +887,9 @@ extern "C" int patch_token_logprobs(const void* Z, int64_t ldz, int dtype, int64
     if ((rc = check_device())) return rc;
     if (sm_count() <= 0) return PATCH_ERR_CUDA;
     const int parts = parts_of(M, V / (dtype == PATCH_LOGITS_BF16 ? 8 : 4));
-    const LogProbs p = {ldz, M, int(V), k, parts, 1.44269504f / temperature, temperature, tokens, logp, entropy, lse, top_logp, top_ids, status_dev};
-    const size_t smem = k ? kCandidates * sizeof(uint64_t) : 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (dtype == PATCH_LOGITS_BF16) {
-        const auto* z = static_cast<const __nv_bfloat16*>(Z);
-        return entropy ? launch_rows(logprobs_kernel<__nv_bfloat16, true>, M, parts, smem, s, z, p)
-                       : launch_rows(logprobs_kernel<__nv_bfloat16, false>, M, parts, smem, s, z, p);
-    }
-    const auto* z = static_cast<const float*>(Z);
-    return entropy ? launch_rows(logprobs_kernel<float, true>, M, parts, smem, s, z, p) : launch_rows(logprobs_kernel<float, false>, M, parts, smem, s, z, p);
+    LogProbs p = {ldz, M, int(V), k, parts, 0, 1.44269504f / temperature, temperature, tokens, logp, entropy, lse, top_logp, top_ids, status_dev};
+    return dtype == PATCH_LOGITS_BF16 ? launch_logprobs<__nv_bfloat16>(Z, p, s) : launch_logprobs<float>(Z, p, s);
 }
 
 extern "C" int patch_token_logprobs_backward(const void* Z, int64_t ldz, int dtype, int64_t M, int64_t V, const int64_t* tokens, float temperature,
