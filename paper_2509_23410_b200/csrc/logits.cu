@@ -31,6 +31,7 @@ constexpr int kCells = 32;                   // see Cells, per thread
 constexpr int kFound = 2048;                 // cells that reach the border, most often k to 1.5 k
 constexpr size_t kListBytes = kCandidates * sizeof(uint64_t) + kFound * sizeof(uint32_t);
 constexpr int kMaxParts = 8;                 // CTAs of a cluster that share a row
+constexpr int64_t kL2Share = 24 << 20;       // see launch_resident
 constexpr int64_t kMaxV = int64_t(1) << 20;  // a bit per element fits shared memory
 static_assert(kMost <= kThreads && kMaxParts * kMost <= kCandidates, "lists of all parts of a row fit the candidates");
 
@@ -57,6 +58,10 @@ template <> struct Vec<__nv_bfloat16> {
     uint32_t w[4];
     __device__ __forceinline__ void set(uint4 v) { w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
     __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0xFF80FF80u; }          // -inf
+    __device__ __forceinline__ void put(int i, __nv_bfloat16 x) {
+        const uint32_t h = __bfloat16_as_ushort(x);
+        w[i >> 1] = (i & 1) ? (w[i >> 1] & 0xFFFFu) | (h << 16) : (w[i >> 1] & 0xFFFF0000u) | h;
+    }
     __device__ __forceinline__ void hide(uint32_t mask) {          // elements whose bit is set: -inf
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -76,6 +81,7 @@ template <> struct Vec<float> {
     uint32_t w[4];
     __device__ __forceinline__ void set(uint4 v) { w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
     __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0xFF800000u; }
+    __device__ __forceinline__ void put(int i, float x) { w[i] = __float_as_uint(x); }
     __device__ __forceinline__ void hide(uint32_t mask) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -121,15 +127,9 @@ template <class T> struct Row {
         }
         x.clear();
         if (v < count) {
-            for (int i = v * N; i < V; ++i) {
-                if constexpr (sizeof(T) == 2) {
-                    const uint32_t h = *reinterpret_cast<const uint16_t*>(z + i);
-                    uint32_t& w = x.w[(i - v * N) >> 1];
-                    w = (i & 1) ? (w & 0xFFFFu) | (h << 16) : (w & 0xFFFF0000u) | h;
-                } else {
-                    x.w[i - v * N] = *reinterpret_cast<const uint32_t*>(z + i);
-                }
-            }
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (v * N + i < V) x.put(i, z[v * N + i]);
         }
         return x;
     }
@@ -267,10 +267,19 @@ struct Scan {
     }
     __device__ __forceinline__ Sums sums() const { return Sums{m, sum2(s2), sum2(t2)}; }
 };
-template <class T> __device__ __forceinline__ void hide_listed(Vec<T>& x, int v, const uint32_t* bits) {
-    constexpr int N = Vec<T>::N;
-    const uint32_t mask = (bits[v / (32 / N)] >> (v % (32 / N) * N)) & ((1u << N) - 1u);
-    if (mask) x.hide(mask);
+template <class T, int COUNT> __device__ __forceinline__ void hide_listed(Vec<T> (&x)[COUNT], int v, int step, const uint32_t* bits) {      // vectors v, v + step ..
+    const uint8_t* b = reinterpret_cast<const uint8_t*>(bits);
+    uint32_t mask[COUNT], any = 0;
+#pragma unroll
+    for (int u = 0; u < COUNT; ++u) {
+        const int at = v + u * step;
+        mask[u] = Vec<T>::N == 8 ? b[at] : (b[at >> 1] >> (at & 1) * 4) & 15u;
+        any |= mask[u];
+    }
+    if (any) {
+#pragma unroll
+        for (int u = 0; u < COUNT; ++u) x[u].hide(mask[u]);
+    }
 }
 // The largest element of every 2^shift batches of a thread, for the alternatives: cell [batch >> shift][thread].
 struct Cells {
@@ -287,11 +296,7 @@ __device__ __forceinline__ Sums scan_row(const Row<T>& row, Batch<T>& ahead, flo
     Scan<T, ENTROPY> scan(c);
     float cell = -INFINITY;
     row.each(ahead, [&](int b, Batch<T>& x) {
-        if (HIDE) {
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (row.at(b, u) < row.whole) hide_listed(x.v[u], row.at(b, u), bits);
-        }
+        if (HIDE) hide_listed(x.v, row.at(b, 0), row.step, bits);   // (bits behind the row are 0)
         const float top = scan.take(x.v);
         if (TOP) {
             cell = fmaxf(cell, top);
@@ -303,7 +308,7 @@ __device__ __forceinline__ Sums scan_row(const Row<T>& row, Batch<T>& ahead, flo
     }, next);
     if (row.rest()) {
         Vec<T> x[1] = {row.load(row.whole)};
-        if (HIDE) hide_listed(x[0], row.whole, bits);
+        if (HIDE) hide_listed(x, row.whole, 0, bits);
         scan.take(x);
     }
     return scan.sums();
@@ -614,6 +619,8 @@ struct Distill {
     int* status;
 };
 // What a row's entries say: of thread i < K.
+// Words of a bit per element; a batch of vectors past the row's end has bits too.
+template <class T> __host__ __device__ constexpr int bit_words(int V, int parts) { return (V + (kAhead + 1) * parts * kThreads * Vec<T>::N) / 32 + 1; }
 struct Entry {
     int id;                                  // -1: none
     float q, x;                              // teacher's probability; the student's logit
@@ -684,6 +691,41 @@ __device__ __forceinline__ Entry entry_of(const Distill& p, int64_t m, const T* 
     __syncthreads();                         // the lists may be written again
     return e;
 }
+// What a row's sums say.  x: over the elements that are not listed (all, where REST is false); listed: over the listed ones (their maximum, sum; REST); q_sum:
+// of the teacher's listed probabilities; a: sum of q_i (x_i - ref), ref the listed maximum, 0 where that is -inf.
+struct RowResult {
+    float g, factor;                         // gradient: factor 2^((x - x.m) c) for elements that are not listed,
+    float q_total, base, ln;                 // g (q_total p_i - q_i), ln p_i = (x_i - base) / T - ln for listed ones
+    bool zero;                               // the whole row's is 0
+};
+template <bool REST>
+__device__ __forceinline__ RowResult finish_row(const Distill& p, int64_t m, const Sums& x, const Sums& listed, float q_sum, float a, bool write) {
+    Sums all = x;
+    float p_rest = 1.0f, ln_rest = 0.0f;
+    if (REST) {
+        all = join(x, listed, p.c);
+        const float p_listed = listed.m == -INFINITY ? listed.s : ex2((listed.m - all.m) * p.c) * listed.s / all.s;
+        p_rest = x.m == -INFINITY ? x.s : ex2((x.m - all.m) * p.c) * x.s / all.s;
+        // ln p_rest without what a difference of two logarithms loses where it is near 0, and where p_rest is below the numbers of fp32
+        ln_rest = p_listed < 0.5f ? log1pf(-p_listed) : p_rest > 1e-30f ? logf(p_rest) : (x.m - all.m) / p.temperature + logf(x.s) - logf(all.s);
+    }
+    RowResult f;
+    const bool none = all.m == -INFINITY && !(all.s != all.s);              // every element is -inf: no distribution
+    f.ln = logf(all.s);
+    f.base = all.m == -INFINITY ? 0.0f : all.m;
+    const float q_rest = REST ? fmaxf(1.0f - q_sum, 0.0f) : 0.0f;
+    f.q_total = q_sum + q_rest;
+    if (write) {
+        const float ref = listed.m == -INFINITY ? 0.0f : listed.m;
+        const float ce = none ? (q_sum == 0.0f ? 0.0f : q_sum * INFINITY) : q_sum * f.ln - (a + q_sum * (ref - f.base)) / p.temperature;
+        p.loss[m] = ce + (q_rest > 0.0f ? -q_rest * (none ? -INFINITY : ln_rest) : 0.0f);
+        if (p.stats) { p.stats[2 * m] = none ? -INFINITY : f.base / p.temperature + f.ln; p.stats[2 * m + 1] = ln_rest; }
+    }
+    f.g = p.gloss ? p.gloss[m] / p.temperature : 1.0f / p.temperature;
+    f.zero = f.g == 0.0f || none;
+    f.factor = x.s == 0.0f ? 0.0f : f.g * (f.q_total * p_rest - q_rest) / x.s;
+    return f;
+}
 // Gradient of a row's part: w_v (c p_rest - q_rest) g / T for elements that are not listed, w_v = 2^((x - base) c) / rest_s (all
 // elements where REST is false: p_v g / T), then the listed ones, which need the barrier.
 template <class T, class Next>
@@ -721,7 +763,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) distill_kernel(const T* z, T
     extern __shared__ uint32_t bits[];       // REST: a bit per element, set where it is listed
     const int part = p.parts > 1 ? int(cluster_ctarank()) : 0;
     if (REST) {
-        for (int i = threadIdx.x; i < (p.V + 31) / 32; i += kThreads) bits[i] = 0u;
+        for (int i = threadIdx.x; i < bit_words<T>(p.V, p.parts); i += kThreads) bits[i] = 0u;
         __syncthreads();
     }
     const int64_t rows = gridDim.x / p.parts;
@@ -742,41 +784,376 @@ __global__ void __launch_bounds__(kThreads, kPerSm) distill_kernel(const T* z, T
                                   if (GRAD) row.fetch(y, 0); else next_row(y);
                               }), p.c, sh, p.parts);
         if (REST && e.first) atomicAnd(&bits[e.id >> 5], ~(1u << (e.id & 31)));       // read again only behind the next row's barriers
-        // the sums over all elements, and which part of them is not listed
-        Sums all = x;
-        float p_rest = 1.0f, ln_rest = 0.0f;
-        if (REST) {
-            const float mine = e.first ? e.x : -INFINITY, top = block_top(mine, sh);
-            const float nan = e.first && !(e.x == e.x) ? e.x : 0.0f;
-            const Sums listed = {top, block_total(top > -INFINITY && e.first ? ex2((e.x - top) * p.c) : nan, sh), 0.0f};
-            all = join(x, listed, p.c);
-            const float p_listed = listed.m == -INFINITY ? listed.s : ex2((listed.m - all.m) * p.c) * listed.s / all.s;
-            p_rest = x.m == -INFINITY ? x.s : ex2((x.m - all.m) * p.c) * x.s / all.s;
-            // ln p_rest without what a difference of two logarithms loses where it is near 0, and where p_rest is below the numbers of fp32
-            ln_rest = p_listed < 0.5f ? log1pf(-p_listed) : p_rest > 1e-30f ? logf(p_rest) : (x.m - all.m) / p.temperature + logf(x.s) - logf(all.s);
-        }
-        const bool none = all.m == -INFINITY && !(all.s != all.s);          // every element is -inf: no distribution
-        const float ln = logf(all.s), base = all.m == -INFINITY ? 0.0f : all.m;
-        const float q_rest = REST ? fmaxf(1.0f - q_sum, 0.0f) : 0.0f;
-        const float lnp = none ? -INFINITY : (e.x - base) / p.temperature - ln;
-        const float ce = block_total(e.q != 0.0f ? -e.q * lnp : 0.0f, sh);
-        if (part == 0 && threadIdx.x == 0) {
-            p.loss[m] = ce + (q_rest > 0.0f ? -q_rest * (none ? -INFINITY : ln_rest) : 0.0f);
-            if (p.stats) { p.stats[2 * m] = none ? -INFINITY : base / p.temperature + ln; p.stats[2 * m + 1] = ln_rest; }
-        }
+        const float top = block_top(e.first ? e.x : -INFINITY, sh), ref = top == -INFINITY ? 0.0f : top;
+        const float listed = REST ? block_total(e.first && (top > -INFINITY || e.x != e.x) ? ex2((e.x - ref) * p.c) : 0.0f, sh) : 0.0f;
+        const float a = block_total(e.q != 0.0f ? e.q * (e.x - ref) : 0.0f, sh);
+        const RowResult f = finish_row<REST>(p, m, x, Sums{top, listed, 0.0f}, q_sum, a, part == 0 && threadIdx.x == 0);
         if (GRAD) {
-            const float g = p.gloss ? p.gloss[m] / p.temperature : 1.0f / p.temperature;
             T* const to = gz + m * p.ldg;
-            if (g == 0.0f || none) {
+            if (f.zero) {
                 write_zeros(row, to);
                 next_row(ahead);
             } else {
-                const float q_all = q_sum + q_rest, factor = x.s == 0.0f ? 0.0f : g * (q_all * p_rest - q_rest) / x.s;
-                write_gradient(row, ahead, to, x.m == -INFINITY ? 0.0f : x.m, p.c, factor, e, g * (q_all * expf(lnp) - e.q_all), p.parts, part, next_row);
+                write_gradient(row, ahead, to, x.m == -INFINITY ? 0.0f : x.m, p.c, f.factor, e,
+                               f.g * (f.q_total * expf((e.x - f.base) / p.temperature - f.ln) - e.q_all), p.parts, part, next_row);
             }
         }
         if (p.parts > 1) cluster_sync_all(); else __syncthreads();
     }
+}
+
+// ---- loss and gradient of long rows: one read of the logits ----
+// A row whose second reading would miss L2 (all rows in flight together are larger than it keeps) stays in shared memory between the two
+// passes: a cluster of 1, 2, 4 or 8 CTAs holds a row in parts, in chunks that come by bulk copies into a ring and leave it as the gradient is
+// written; three CTAs share an SM, so that exponentials, reductions, copies and stores of different rows run beside each other.
+//   warps 0..7  the two passes     warp 8  copies     warp 9  the entries of the next row; it also writes -inf over the listed elements of a
+//                chunk that has come, which leaves the sums of the others to the first pass and is overwritten after the second one
+// The parts' sums go to all CTAs of the cluster by asynchronous stores that count on their barriers; nobody waits for the whole cluster.
+namespace resident {
+constexpr int kWorkers = 256;
+constexpr int kBlock = kWorkers + 64;
+constexpr int kEach = 4;                     // vectors of a chunk for every thread
+constexpr int kChunk = kEach * kWorkers;
+constexpr int kRing = 4;
+constexpr int kSegment = kRing * kChunk;     // vectors of a part, at most
+struct Table {                               // the entries of a row and what depends on them alone
+    float q_sum, top, s, a;                  // sum q; largest listed logit, sum 2^((x - top) c), sum q (x - top) (x itself where top is -inf)
+    int id[kMost];                           // of the first entry with this id, else -1
+    float x[kMost], q_all[kMost];
+};
+struct Shared {
+    uint64_t full[kRing], ready[kRing], empty[kRing], entries_full[2], entries_empty[2], inbox_full[2];
+    float4 inbox[2][kMaxParts];
+    Sums warp[kWorkers / 32];
+    RowResult result;
+    Sums sums;
+    int abort;
+    alignas(16) int all_id[kMost];           // of all entries, and their own probabilities
+    float q[kMost];
+    Table table[2];
+};
+constexpr size_t kBytes = size_t(kRing) * kChunk * 16 + sizeof(Shared);
+constexpr int kPerSm = 3;
+static_assert(kPerSm * (kBytes + 1024) <= 228 * 1024, "shared memory of an SM");
+__device__ __forceinline__ void workers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kWorkers) : "memory"); }
+}  // namespace resident
+
+template <class T, bool REST>
+__global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_resident_kernel(const T* z, T* gz, const Distill p) {
+    using namespace resident;
+    constexpr int N = Vec<T>::N;
+    extern __shared__ __align__(128) uint8_t smem[];
+    resident::Shared& sh = *reinterpret_cast<resident::Shared*>(smem + size_t(kRing) * kChunk * 16);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int part = p.parts > 1 ? int(cluster_ctarank()) : 0;
+    const int whole = p.V / N, segment = (whole + p.parts - 1) / p.parts, v0 = part * segment, n_v = min(segment, whole - v0);
+    const bool rest = part == p.parts - 1 && p.V % N != 0;         // this part has the row's short last vector too
+    const int chunks = (n_v + kChunk - 1) / kChunk;
+    const int64_t rows = gridDim.x / p.parts, m0 = blockIdx.x / p.parts;
+    volatile int* abort_flag = &sh.abort;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kRing; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.ready[i]), 1); mbar_init(smem_u32(&sh.empty[i]), kWorkers / 32); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sh.entries_full[i]), 1);
+            mbar_init(smem_u32(&sh.entries_empty[i]), kWorkers / 32);
+            mbar_init(smem_u32(&sh.inbox_full[i]), 1);
+        }
+        sh.abort = 0;
+        mbar_init_fence();
+    }
+    __syncthreads();
+    if (p.parts > 1) cluster_sync_all();     // barriers are there before anybody sends
+
+    if (warp == kWorkers / 32) {
+        // ---------------- copies ----------------
+        if (lane == 0) {
+            const uint64_t policy = l2_policy_evict_first();
+            int stage = 0, issued = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int64_t m = m0; m < p.M && ok; m += rows)
+                for (int i = 0; i < chunks && ok; ++i) {
+                    if (issued >= kRing) ok = mbar_wait_relaxed(smem_u32(&sh.empty[stage]), phase ^ 1u, abort_flag, p.status);
+                    if (!ok) break;
+                    const uint32_t bytes = uint32_t(min(kChunk, n_v - i * kChunk)) * 16u, bar = smem_u32(&sh.full[stage]);
+                    mbar_expect_tx(bar, bytes);
+                    tma_bulk_load(smem_u32(smem) + uint32_t(stage) * kChunk * 16u, z + m * p.ldz + int64_t(v0 + i * kChunk) * N, bytes, bar, policy);
+                    ++issued;
+                    if (++stage == kRing) { stage = 0; phase ^= 1u; }
+                }
+            if (*abort_flag) {
+                const uint64_t t0 = global_timer_ns();
+                for (int j = issued > kRing ? issued - kRing : 0; j < issued; ++j)
+                    while (!mbar_try_wait(smem_u32(&sh.full[j % kRing]), uint32_t(j / kRing) & 1u) && global_timer_ns() - t0 < kDrainLimitNs) {}
+            }
+        }
+    } else if (warp == kWorkers / 32 + 1) {
+        // ---------------- entries: lane + 32 j ----------------
+        bool ok = true;
+        auto wait = [&](uint64_t& bar, uint32_t parity) { ok = __all_sync(0xFFFFFFFFu, mbar_wait_relaxed(smem_u32(&bar), parity, abort_flag, p.status)) && ok; };
+        auto total = [](float x) {
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+            return x;
+        };
+        auto largest = [](float x) {
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
+            return x;
+        };
+        constexpr int kEach = kMost / 32;                          // entries of a lane
+        int stage = 0;
+        uint32_t phase = 0;
+        int r = 0, next[kEach];                                    // ids come a row ahead, what they point to in one go
+        auto fetch = [&](int64_t m) {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) next[j] = m < p.M && lane + 32 * j < p.K ? p.ids[m * p.K + lane + 32 * j] : -1;
+        };
+        fetch(m0);
+        for (int64_t m = m0; m < p.M && ok; m += rows, ++r) {
+            Table& t = sh.table[r & 1];
+            if (r >= 2) wait(sh.entries_empty[r & 1], uint32_t((r >> 1) - 1) & 1u);
+            if (!ok) break;
+            const T* row = z + m * p.ldz;
+            int id[kEach];
+            float q[kEach], x[kEach];
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                id[j] = next[j];
+                if (id[j] >= p.V) {
+                    if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_SIZE);
+                    id[j] = -1;
+                }
+                q[j] = id[j] >= 0 ? p.t[m * p.K + lane + 32 * j] : -INFINITY;
+                x[j] = id[j] >= 0 ? as_float(row[id[j]]) : 0.0f;
+                if (id[j] < 0) id[j] = -1 - j;                     // equal to nobody's
+                sh.all_id[lane + 32 * j] = id[j];
+            }
+            fetch(m + rows);
+            __syncwarp();
+            // the same id twice?  (rarely: the lists of a teacher's largest logits have none)
+            bool twice = false;
+            for (int j = 0; j < p.K; j += 4) {
+                const int4 o = *reinterpret_cast<const int4*>(sh.all_id + j);
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    if (32 * i >= p.K) break;
+                    const int d = lane + 32 * i - j;               // its own place among the four
+                    twice |= id[i] >= 0 && ((o.x == id[i] && d != 0) || (o.y == id[i] && d != 1) || (o.z == id[i] && d != 2) || (o.w == id[i] && d != 3));
+                }
+            }
+            twice = __any_sync(0xFFFFFFFFu, twice);
+            float top_t = -INFINITY, sum = 0.0f, top = -INFINITY, s = 0.0f, a = 0.0f;
+            if (!REST) {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) top_t = fmaxf(top_t, q[j]);
+                top_t = largest(top_t);
+            }
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (32 * j >= p.K) break;
+                q[j] = id[j] < 0 || q[j] == -INFINITY ? 0.0f : expf(REST ? q[j] : q[j] - top_t);
+                sum += q[j];
+            }
+            sum = total(sum);
+            const float by = REST || sum == 0.0f ? 1.0f : 1.0f / sum;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (32 * j >= p.K) break;
+                q[j] *= by;
+                sh.q[lane + 32 * j] = q[j];
+            }
+            if (twice) {                                           // of every id the first entry stays, with the probabilities of all of them
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    const int i = lane + 32 * j;
+                    float sum_q = 0.0f;
+                    bool first = true;
+                    for (int o = 0; o < p.K && id[j] >= 0; ++o)
+                        if (sh.all_id[o] == id[j]) {
+                            sum_q += sh.q[o];
+                            first = first && o >= i;
+                        }
+                    q[j] = sum_q;
+                    if (!first) id[j] = -1;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (32 * j >= p.K) break;
+                t.id[lane + 32 * j] = id[j] >= 0 ? id[j] : -1;
+                t.x[lane + 32 * j] = x[j];
+                t.q_all[lane + 32 * j] = q[j];
+                if (id[j] >= 0) top = fmaxf(top, x[j]);
+            }
+            top = largest(top);
+            const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (32 * j >= p.K) break;
+                if (id[j] < 0) continue;
+                if (top > -INFINITY || x[j] != x[j]) s += ex2((x[j] - ref) * p.c);
+                if (q[j] != 0.0f) a += q[j] * (x[j] - ref);
+            }
+            s = total(s);
+            a = total(a);
+            if (lane == 0) {
+                t.q_sum = REST ? sum : sum == 0.0f ? 0.0f : 1.0f;
+                t.top = top;
+                t.s = s;
+                t.a = a;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.entries_full[r & 1]));
+            if (!REST) continue;
+            for (int i = 0; i < chunks && ok; ++i) {
+                wait(sh.full[stage], phase);
+                T* const chunk = reinterpret_cast<T*>(smem) + stage * kChunk * N;
+                const int from = (v0 + i * kChunk) * N, count = min(kChunk, n_v - i * kChunk) * N;
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    if (32 * j >= p.K) break;
+                    if (id[j] >= from && id[j] < from + count) chunk[id[j] - from] = rounded<T>(-INFINITY);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.ready[stage]));
+                if (++stage == kRing) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else {
+        // ---------------- the two passes ----------------
+        bool ok = true;
+        auto wait = [&](uint64_t& bar, uint32_t parity) { ok = ok && mbar_wait(smem_u32(&bar), parity, abort_flag, p.status); };
+        int r = 0, begin = 0;                                      // stage of the row's first chunk
+        uint32_t begin_phase = 0;
+        for (int64_t m = m0; m < p.M; m += rows, ++r) {
+            const Table& t = sh.table[r & 1];
+            Scan<T, false> scan(p.c);
+            // a thread's vectors of chunk i in a stage, -inf past the part's end; f(vector of the part)
+            auto load = [&](Vec<T> (&x)[kEach], int i, int stage) {
+                const uint4* from = reinterpret_cast<const uint4*>(smem) + stage * kChunk + threadIdx.x;
+                const int left = n_v - i * kChunk;
+                if (left >= kChunk) {
+#pragma unroll
+                    for (int u = 0; u < kEach; ++u) x[u].set(from[u * kWorkers]);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kEach; ++u) {
+                        if (left > u * kWorkers + int(threadIdx.x)) x[u].set(from[u * kWorkers]);
+                        else x[u].clear();
+                    }
+                }
+            };
+            auto advance = [&](int& stage, uint32_t& phase) { if (++stage == kRing) { stage = 0; phase ^= 1u; } };
+            const T* row = z + m * p.ldz;
+            int stage = begin;
+            uint32_t phase = begin_phase;
+            for (int i = 0; i < chunks && ok; ++i) {
+                wait(REST ? sh.ready[stage] : sh.full[stage], phase);
+                Vec<T> x[kEach];
+                load(x, i, stage);
+                scan.take(x);
+                advance(stage, phase);
+            }
+            wait(sh.entries_full[r & 1], uint32_t(r >> 1) & 1u);
+            Vec<T> last[1];
+            if (rest && threadIdx.x == 0) {
+                last[0].clear();
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (whole * N + i < p.V) last[0].put(i, row[whole * N + i]);
+                if (REST)
+                    for (int j = 0; j < p.K; ++j)
+                        if (t.id[j] >= whole * N) last[0].hide(1u << (t.id[j] - whole * N));
+                scan.take(last);
+            }
+            Sums x = sum_of_lanes<32>(scan.sums(), p.c);
+            if (lane == 0) sh.warp[warp] = x;
+            workers_sync();
+            if (warp == 0) {                                       // one warp finishes the sums for all
+                x = sum_of_lanes<kWorkers / 32>(sh.warp[lane & (kWorkers / 32 - 1)], p.c);
+                if (p.parts > 1) {
+                    if (lane < p.parts) {                          // lane i sends to CTA i
+                        if (lane == 0) mbar_expect_tx(smem_u32(&sh.inbox_full[r & 1]), 16u * p.parts);
+                        asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                                     ::"r"(map_to_rank(smem_u32(&sh.inbox[r & 1][part]), lane)), "f"(x.m), "f"(x.s), "f"(0.0f), "f"(0.0f),
+                                     "r"(map_to_rank(smem_u32(&sh.inbox_full[r & 1]), lane)) : "memory");
+                    }
+                    __syncwarp();
+                    wait(sh.inbox_full[r & 1], uint32_t(r >> 1) & 1u);
+                    for (int i = 0; i < p.parts; ++i) {
+                        const float4 o = sh.inbox[r & 1][i];
+                        x = i ? join(x, Sums{o.x, o.y, 0.0f}, p.c) : Sums{o.x, o.y, 0.0f};
+                    }
+                }
+                const RowResult f = finish_row<REST>(p, m, x, Sums{t.top, t.s, 0.0f}, t.q_sum, t.a, part == 0 && lane == 0);
+                if (lane == 0) {
+                    sh.result = f;
+                    sh.sums = x;
+                }
+            }
+            workers_sync();
+            const RowResult f = sh.result;
+            x = sh.sums;
+            T* const to = gz + m * p.ldg;
+            const float base = x.m == -INFINITY ? 0.0f : x.m;
+            auto gradient = [&](const Vec<T>& e, float (&y)[N]) {
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) {
+                    float a, b;
+                    un2(mul2(add2(e.pair(i), mk2(-base, -base)), mk2(p.c, p.c)), a, b);
+                    un2(mul2(mk2(ex2(a), ex2(b)), mk2(f.factor, f.factor)), y[2 * i], y[2 * i + 1]);
+                }
+            };
+            stage = begin;
+            for (int i = 0; i < chunks && ok; ++i) {
+                Vec<T> e[kEach];
+                load(e, i, stage);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.empty[stage]));
+                T* const at = to + int64_t(v0 + i * kChunk + int(threadIdx.x)) * N;
+                const int left = n_v - i * kChunk;
+                uint4 out[kEach] = {};
+                if (!f.zero) {
+#pragma unroll
+                    for (int u = 0; u < kEach; ++u) {
+                        float y[N];
+                        gradient(e[u], y);
+                        out[u] = to_raw<T>(y);
+                    }
+                }
+                if (left >= kChunk) {
+#pragma unroll
+                    for (int u = 0; u < kEach; ++u) store16(at + u * kWorkers * N, out[u]);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kEach; ++u)
+                        if (left > u * kWorkers + int(threadIdx.x)) store16(at + u * kWorkers * N, out[u]);
+                }
+                advance(stage, begin_phase);
+            }
+            begin = stage;
+            if (rest && threadIdx.x == 0) {
+                float y[N] = {};
+                if (!f.zero) gradient(last[0], y);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (whole * N + i < p.V) to[whole * N + i] = rounded<T>(y[i]);
+            }
+            workers_sync();                                        // listed columns come last
+            if (!f.zero && int(threadIdx.x) < p.K) {
+                const int id = t.id[threadIdx.x], b = id - v0 * N;
+                if (id >= 0 && b >= 0 && b < (n_v + rest) * N) to[id] = rounded<T>(f.g * (f.q_total * expf((t.x[threadIdx.x] - f.base) / p.temperature - f.ln) - t.q_all[threadIdx.x]));
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.entries_empty[r & 1]));
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+        }
+    }
+    __syncthreads();
+    if (p.parts > 1) cluster_sync_all();     // nobody sends to a CTA that has left
 }
 
 template <class T, bool REST>
@@ -932,13 +1309,56 @@ int check_distill(const void* Z, int64_t ldz, int dtype, int64_t M, int64_t V, c
     if (!ids || !t) return PATCH_ERR_NULL;
     return misaligned(ids, 4) || misaligned(t, 4) ? PATCH_ERR_ALIGN : PATCH_OK;
 }
+// Rows that all CTAs of the kernel below have in flight, and their gradients, stay within what L2 keeps of them: 24 MB of logits.
+// Otherwise a row stays in shared memory.
+template <class T, bool REST>
+int launch_resident(const T* z, T* g, Distill p, cudaStream_t s) {
+    namespace R = resident;
+    auto kern = distill_resident_kernel<T, REST>;
+    static std::atomic<uint64_t> configured{0};
+    if (int rc = allow_dynamic_smem(kern, uint32_t(R::kBytes), configured)) return rc;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    cfg.blockDim = dim3(R::kBlock, 1, 1);
+    cfg.dynamicSmemBytes = R::kBytes;
+    cfg.stream = s;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {unsigned(p.parts), 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = p.parts > 1 ? 1 : 0;
+    // clusters that run at once: a grid of more would leave the last ones to themselves
+    static std::atomic<int> most[kMaxDevices][kMaxParts + 1];
+    const int d = current_device();
+    if (d < 0) return PATCH_ERR_CUDA;
+    int clusters = most[d][p.parts].load(std::memory_order_relaxed);
+    if (!clusters) {
+        cfg.gridDim = dim3(unsigned(sm_count() * R::kPerSm / p.parts * p.parts), 1, 1);
+        if (p.parts == 1) clusters = sm_count() * R::kPerSm;
+        else if (cudaOccupancyMaxActiveClusters(&clusters, kern, &cfg) != cudaSuccess || clusters < 1) { cudaGetLastError(); return PATCH_ERR_CUDA; }
+        most[d][p.parts].store(clusters, std::memory_order_relaxed);
+    }
+    cfg.gridDim = dim3(unsigned((p.M < clusters ? p.M : clusters) * p.parts), 1, 1);
+    if (cudaLaunchKernelEx(&cfg, kern, z, g, p) == cudaSuccess) return PATCH_OK;
+    cudaGetLastError();
+    return PATCH_ERR_CUDA;
+}
 template <class T, bool REST, bool GRAD>
 int launch_distill(const T* z, T* g, const Distill& p, cudaStream_t s) {
-    const size_t smem = REST ? size_t(p.V + 31) / 32 * 4 : 0;
+    if (GRAD) {
+        const int64_t vectors = p.V / Vec<T>::N, in_flight = p.M < kPerSm * sm_count() ? p.M : kPerSm * sm_count();
+        int parts = 1;
+        while (parts <= kMaxParts && vectors > int64_t(parts) * resident::kSegment) parts *= 2;
+        if (parts <= kMaxParts && in_flight * vectors * 16 > kL2Share) {
+            Distill q = p;
+            q.parts = parts;
+            return launch_resident<T, REST>(z, g, q, s);
+        }
+    }
+    const size_t smem = REST ? size_t(bit_words<T>(p.V, p.parts)) * 4 : 0;
     auto kern = distill_kernel<T, REST, GRAD>;
     static std::atomic<uint64_t> configured{0};
     if (REST) {
-        if (int rc = allow_dynamic_smem(kern, uint32_t(kMaxV / 8), configured)) return rc;
+        if (int rc = allow_dynamic_smem(kern, uint32_t(bit_words<float>(int(kMaxV), kMaxParts) * 4), configured)) return rc;
     }
     return launch_rows(kern, p.M, p.parts, smem, s, z, g, p);
 }

@@ -233,7 +233,7 @@ def distill_reference(z, ids, t, T, rest):
     return loss, gz, torch.where(inside, p + listed, w * (ln_r.exp() + q_r))
 
 
-def check_distill(B, z, ids, t, T, rest, gloss):
+def check_distill(B, z, ids, t, T, rest, gloss, resident=False):
     M, V = z.shape
     loss = torch.empty(M, device="cuda")
     want_loss, want, size = distill_reference(z, ids, t, T, rest)
@@ -246,7 +246,10 @@ def check_distill(B, z, ids, t, T, rest, gloss):
     B.patch_distill_loss(z, ids, t, temperature=T, rest=rest, loss=loss, stats=stats, gloss=gloss, gZ=buffers[0][:, :V])
     check(loss, want_loss, tol)
     alone = B.patch_distill_loss(z, ids, t, temperature=T, rest=rest)
-    assert torch.equal(alone.nan_to_num(7.0), loss.nan_to_num(7.0))
+    if resident:                                                  # another kernel than the loss alone
+        check(alone, want_loss, tol)
+    else:
+        assert torch.equal(alone.nan_to_num(7.0), loss.nan_to_num(7.0))
     B.patch_distill_loss_backward(z, ids, t, stats, gloss=gloss, temperature=T, rest=rest, gZ=buffers[1][:, :V])
     for b in buffers:
         check(b[:, :V], want * g, rel * size * (g.abs() if gloss is not None else g) + rounding(want * g, z.dtype))
@@ -285,6 +288,30 @@ def test_distill_lists_with_gaps_repetitions_and_masked_students(B, dtype, rest,
     z[7, ids[7].long()] = 200.0                                   # all probability is listed
     z[8, ids[8].long()] = -200.0                                  # none is
     check_distill(B, z, ids, t, 1.0, rest, torch.linspace(-1, 2, M, device="cuda"))
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype,M,V,K", [(F32, 200, 32000, 9), (F32, 210, 32001, 1), (BF, 150, 98303, 64), (BF, 150, 98311, 40), (BF, 149, 128256, 256), (F32, 60, 128257, 33),
+                                         (F32, 40, 200003, 12), (BF, 2000, 8000, 5)])
+def test_distill_of_rows_that_stay_in_shared_memory(B, dtype, rest, M, V, K):
+    """Batches whose rows in flight are more than L2 keeps: 1, 2, 4 and 8 CTAs to a row (and a batch just below, of short rows)."""
+    z = logits(M, V, dtype, 3, 8)
+    ids, t = teacher(z, K, 0.9, 4, M, V)
+    ids[1], ids[2, K // 2 :] = -1, ids[2, :1]
+    z[3, V // 3 :], z[4], z[5, ids[5].long()] = -math.inf, -math.inf, 150.0
+    ids[6, 0], z[6, V - 1] = V - 1, 3.0                           # the last column, in the row's short vector where it has one
+    z[7, V - 1] = 50.0
+    gloss = torch.randn(M, device="cuda")
+    gloss[M // 2] = 0.0
+    check_distill(B, z, ids, t, 0.9, rest, gloss, resident=True)
+    bad = z.clone() if V % 8 == 0 else z
+    bad[9, V // 2], bad[M - 1, 0] = math.nan, math.inf
+    gz = torch.zeros(M, (V + 7) // 8 * 8, dtype=dtype, device="cuda")[:, :V]
+    loss = B.patch_distill_loss(bad, ids, t, temperature=0.9, rest=rest, gZ=gz)
+    nan = torch.zeros(M, dtype=torch.bool, device="cuda")
+    nan[[9, M - 1]] = True
+    assert bool(loss[nan].isnan().all()) and bool(gz[nan].isnan().any(-1).all())
+    assert not bool(loss[~nan].isnan().any()) and not bool(gz[~nan].isnan().any())
 
 
 def test_everything_listed(B):
