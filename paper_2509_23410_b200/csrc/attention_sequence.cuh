@@ -115,6 +115,40 @@ struct Loader {
     }
 };
 
+// 32 rows (a warp's, lane = row) of COLS fp32 columns of TMEM, times `f` of the lane's row, as bf16 into rows [row, end).  Four neighbouring lanes
+// exchange their 64 bytes, so that a store writes 64 consecutive bytes of eight rows (a lane that writes its own row alone touches 32 lines with every
+// 16 bytes: 4 000 cycles of the load-store unit for an item of 256 x 128, against 1 000).
+template <int COLS>
+__device__ __forceinline__ void store_rows(uint32_t t, __nv_bfloat16* to, int64_t ld, int row, int end, float f) {
+    const int lane = threadIdx.x & 31, sub = lane & 3;
+#pragma unroll 1
+    for (int q = 0; q < COLS / 32; ++q) {
+        uint32_t v[32], w[4][4];                                   // w: 16-byte chunks of the lane's row, then chunk `sub` of four rows
+        attn::blk::tmem_ld32(t + 32u * q, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int c = 0; c < 16; ++c) w[c >> 2][c & 3] = attn::pack2(__uint_as_float(v[2 * c]) * f, __uint_as_float(v[2 * c + 1]) * f);
+#pragma unroll
+        for (int bit = 1; bit <= 2; bit <<= 1) {
+            const bool high = sub & bit;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (c & bit) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, high ? w[c][i] : w[c | bit][i], bit);
+                    if (high) w[c][i] = got; else w[c | bit][i] = got;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = row + (lane & ~3) + j;
+            if (r < end) *reinterpret_cast<uint4*>(to + int64_t(r) * ld + 32 * q + 8 * sub) = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+        }
+    }
+}
+
 int launch_forward(const Problem& p, int D, __nv_bfloat16* o, int64_t ldo, float* lse, cudaStream_t s);
 // stats: [Hq][M] of scratch
 int launch_backward(const Problem& p, int D, const float* lse, float2* stats, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,

@@ -8,7 +8,7 @@
 // a thread 64 columns of a row.
 //
 //   gq:      S = Q K^T (two buffers), GP = GO V^T,   GS = P (GP - delta) (over S),   GQ += GS K
-//            order of the MMAs: GQ(j), GP(j + 1), S(j + 2): the exponentials of j + 1 run beside the first two
+//            order of the MMAs: GP(j + 1), GQ(j), S(j + 2): the exponentials of j + 1 run beside the first, its GS needs no more than that
 //   gk, gv:  S^T = K Q^T,  GP^T = V GO^T (lane = key, column = query),  P^T (over S^T),  GS^T (over GP^T),  GV += P^T GO,  GK += GS^T Q
 //            order of the MMAs: GV(t), S(t + 1), GK(t), GP(t + 1): the exponentials of t + 1 run beside the last two
 // TMEM: 512 columns in both (two of scores or one, one of GP, the accumulators).
@@ -89,27 +89,6 @@ __device__ __forceinline__ void accumulate(uint32_t d_tmem, uint32_t a_tmem, uin
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) mma_ta(d_tmem, a_tmem + 8u * ks, db + uint64_t((ks * 2048) >> 4), instr_desc(D, false) | (1u << 16), !(first && ks == 0));
 }
-// a row of COLS fp32 columns of TMEM, times f, as bf16
-template <int COLS>
-__device__ __forceinline__ void store_row(uint32_t t, __nv_bfloat16* to, bool valid, float f) {
-#pragma unroll 1
-    for (int q = 0; q < COLS / 32; ++q) {
-        uint32_t v[32];
-        tmem_ld32(t + 32u * q, v);
-        tmem_ld_wait();
-        if (!valid) continue;
-#pragma unroll
-        for (int c = 0; c < 32; c += 8) {
-            uint4 w;
-            w.x = pack2(__uint_as_float(v[c]) * f, __uint_as_float(v[c + 1]) * f);
-            w.y = pack2(__uint_as_float(v[c + 2]) * f, __uint_as_float(v[c + 3]) * f);
-            w.z = pack2(__uint_as_float(v[c + 4]) * f, __uint_as_float(v[c + 5]) * f);
-            w.w = pack2(__uint_as_float(v[c + 6]) * f, __uint_as_float(v[c + 7]) * f);
-            *reinterpret_cast<uint4*>(to + 32 * q + c) = w;
-        }
-    }
-}
-
 }  // namespace bwd
 
 // (lse log2 e, delta) of every row and head, [Hq][M]
@@ -263,17 +242,18 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                         }
                         began = true;
                     }
-#pragma unroll 1
-                    for (int half = 0; half < 2 && ok; ++half) {
-                        wait(sh.gs[half], phase_gs);
-                        if (ok) accumulate<D>(t_gq, tmem + 128u * (j & 1) + 64u * half, k_tile, half, j == 0 && half == 0);
-                    }
+                    wait(sh.gs[0], phase_gs);
+                    wait(sh.gs[1], phase_gs);
                     phase_gs ^= 1u;
+                    if (ok && j + 1 < n) gps(j + 1);               // (GP(j) has been read)
+                    if (j + 2 == n) mma_commit(smem_u32(&sh.own_empty));       // the last product with the item's own tiles
+                    if (ok) {
+                        accumulate<D>(t_gq, tmem + 128u * (j & 1), k_tile, 0, j == 0);
+                        accumulate<D>(t_gq, tmem + 128u * (j & 1) + 64u, k_tile, 1, false);
+                    }
                     release(at + 2 * j);
                     if (j + 1 == n) mma_commit(smem_u32(&sh.done));
-                    if (ok && j + 1 < n) gps(j + 1);
                     if (ok && j + 2 < n) scores(j + 2);
-                    if (j + 2 == n) mma_commit(smem_u32(&sh.own_empty));       // the last products with the item's own tiles
                 }
                 at += 2 * n;
             }
@@ -336,11 +316,14 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                         float a, b;
                         un2(mul2(mk2(__uint_as_float(e[i][c]), __uint_as_float(e[i][c + 1])),
                                  add2(mk2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), delta2)), a, b);
-                        if (partly) {                              // values behind the sequence's end may be anything
-                            if (32 * i + c >= left) a = 0.0f;
-                            if (32 * i + c + 1 >= left) b = 0.0f;
-                        }
                         gs[16 * i + (c >> 1)] = pack2(a, b);
+                    }
+                }
+                if (partly) {                                      // keys after the query, and behind the sequence's end: 0 whatever the values hold there
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2) {
+                        if (c >= left) gs[c >> 1] = 0u;
+                        else if (c + 1 >= left) gs[c >> 1] &= 0xFFFFu;
                     }
                 }
                 tmem_st32(t_s, gs);
@@ -353,7 +336,7 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
             wait(sh.done, phase_done);
             if (failed) break;
             phase_done ^= 1u;
-            store_row<D / 2>(t_gq + lanes + half * (D / 2), gq + int64_t(it.begin + r) * ldgq + int64_t(it.head) * D + half * (D / 2), valid, p.scale);
+            store_rows<D / 2>(t_gq + lanes + half * (D / 2), gq + int64_t(it.head) * D + half * (D / 2), ldgq, it.begin + it.first + quad * 32, it.end, p.scale);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.read));
@@ -583,13 +566,16 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                     un2(fma2(mk2(__uint_as_float(e[c >> 5][(c & 31) + 2]), __uint_as_float(e[c >> 5][(c & 31) + 3])), scale2, mk2(l.z, l.w)), a[2], a[3]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float x = ex2(a[i]);
-                        if (partly && 64 * half + c + i < row) x = 0.0f;       // queries before the key
-                        e[c >> 5][(c & 31) + i] = __float_as_uint(x);
+                        e[c >> 5][(c & 31) + i] = __float_as_uint(ex2(a[i]));
                     }
-                    out[c >> 1] = pack2(__uint_as_float(e[c >> 5][c & 31]), __uint_as_float(e[c >> 5][(c & 31) + 1]));
-                    out[(c >> 1) + 1] = pack2(__uint_as_float(e[c >> 5][(c & 31) + 2]), __uint_as_float(e[c >> 5][(c & 31) + 3]));
                 }
+                if (partly) {                                      // queries before the key
+#pragma unroll
+                    for (int c = 0; c < 64; ++c)
+                        if (64 * half + c < row) e[c >> 5][c & 31] = 0u;
+                }
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) out[c >> 1] = pack2(__uint_as_float(e[c >> 5][c & 31]), __uint_as_float(e[c >> 5][(c & 31) + 1]));
                 tmem_st32(t_s, out);
                 tmem_st_wait();
                 tc_fence_before();
@@ -627,10 +613,9 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             wait(sh.done, phase_done);
             if (failed) break;
             phase_done ^= 1u;
-            const int r = it.first + row;
-            const bool valid = r < it.end - it.begin;
-            if (half == 0) store_row<D>(t_gv + lanes, gv + int64_t(it.begin + r) * ldgv + int64_t(it.head) * D, valid, 1.0f);
-            else store_row<D>(t_gk + lanes, gk + int64_t(it.begin + r) * ldgk + int64_t(it.head) * D, valid, p.scale);
+            const int row0 = it.begin + it.first + quad * 32;
+            if (half == 0) store_rows<D>(t_gv + lanes, gv + int64_t(it.head) * D, ldgv, row0, it.end, 1.0f);
+            else store_rows<D>(t_gk + lanes, gk + int64_t(it.head) * D, ldgk, row0, it.end, p.scale);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.read));

@@ -265,7 +265,7 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 phase_s ^= 1u;
                 const bool partly = j == n - 1;                    // the tile on the diagonal
                 const int left = partly ? row + 1 : kKeys;         // columns the row sees
-                if (j == 0) m = row_top(t_s, kKeys / 32, left);
+                if (j == 0) m = row_top(t_s, 1, left);             // every row sees the first of them
                 // The products of the first half of the keys start while the second half is worked on.
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
@@ -314,29 +314,10 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             const int r = it.first + 128 * x + row;
             const bool valid = r < it.end - it.begin;
             const float f = 1.0f / l;
-            __nv_bfloat16* to = o + int64_t(it.begin + r) * ldo + int64_t(it.head) * D;
-#pragma unroll 1
-            for (int q = 0; q < D / 32; ++q) {
-                uint32_t v[32];
-                tmem_ld32(t_o + 32u * q, v);
-                tmem_ld_wait();
-                if (q == D / 32 - 1) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&sh.o_empty[x]));
-                }
-                if (valid) {
-#pragma unroll
-                    for (int c = 0; c < 32; c += 8) {
-                        uint4 w;
-                        w.x = pack2(__uint_as_float(v[c]) * f, __uint_as_float(v[c + 1]) * f);
-                        w.y = pack2(__uint_as_float(v[c + 2]) * f, __uint_as_float(v[c + 3]) * f);
-                        w.z = pack2(__uint_as_float(v[c + 4]) * f, __uint_as_float(v[c + 5]) * f);
-                        w.w = pack2(__uint_as_float(v[c + 6]) * f, __uint_as_float(v[c + 7]) * f);
-                        *reinterpret_cast<uint4*>(to + 32 * q + c) = w;
-                    }
-                }
-            }
+            store_rows<D>(t_o, o + int64_t(it.head) * D, ldo, it.begin + it.first + 128 * x + quad * 32, it.end, f);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.o_empty[x]));
             if (valid && lse) lse[int64_t(it.begin + r) * p.Hq + it.head] = m * p.scale + logf(l);
         }
     }
