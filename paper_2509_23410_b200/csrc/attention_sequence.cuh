@@ -19,12 +19,18 @@ struct Problem {
 struct Tile { int begin, end, first; };      // rows of the sequence; the tile's first row, counted from `begin` (-1: no tile)
 __host__ __device__ __forceinline__ int64_t most_tiles(int64_t M, int64_t B, int rows) { return M / rows + B; }
 __device__ __forceinline__ int clamped(const Problem& p, int b) { return min(max(p.starts[b], 0), p.M); }
+// By one warp, all lanes: a search in 32 parts, so that up to 31 sequences take one look and thousands three.
 template <int ROWS>
 __device__ __forceinline__ Tile tile_of(const Problem& p, int slot) {
-    int lo = -1, hi = p.B;                   // the last sequence whose first tile is at or before `slot`
+    const int lane = threadIdx.x & 31;
+    int lo = -1, hi = p.B;                   // the last sequence whose first tile is at or before `slot` is lo or lies between the two
     while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (clamped(p, mid) / ROWS + mid <= slot) lo = mid; else hi = mid;
+        const int each = (hi - lo + 31) / 32, b = lo + 1 + lane * each;
+        const bool before = b < hi && clamped(p, b) / ROWS + b <= slot;
+        const int n = __popc(__ballot_sync(0xFFFFFFFFu, before));  // lanes 0 .. n - 1, where the starts ascend
+        const int last = n ? lo + 1 + (n - 1) * each : lo, next = lo + 1 + n * each;
+        hi = n < 32 && next < hi ? next : hi;
+        lo = last;
     }
     Tile t = {0, 0, -1};
     if (lo < 0) return t;

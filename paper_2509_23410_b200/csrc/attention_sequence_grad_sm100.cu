@@ -4,13 +4,14 @@
 // Two kernels, so that every sum has one owner and an order of its own: gq by blocks of 128 queries over their keys (three products a tile), gk and
 // gv by blocks of 128 keys of a key head over the queries that see them, head by head of the group (four products a tile).  The scores are computed in
 // both, seven products instead of five; the price of sums in fp32 atomics would be an order that changes from call to call, and their traffic.
-// A CTA owns an SM; roles, rings and the taking of items are the forward kernel's.  Eight warps do the elementwise part of a tile of 128 x 128,
-// a thread 64 columns of a row.
+// A CTA owns an SM; roles, rings and the taking of items are the forward kernel's.  Warps 4..11 do the elementwise part of a tile of 128 x 128,
+// a thread 64 columns of a row; warps 12..15 write an item's results while the next one is worked on.
 //
 //   gq:      S = Q K^T (two buffers), GP = GO V^T,   GS = P (GP - delta) (over S),   GQ += GS K
 //            order of the MMAs: GP(j + 1), GQ(j), S(j + 2): the exponentials of j + 1 run beside the first, its GS needs no more than that
-//   gk, gv:  S^T = K Q^T,  GP^T = V GO^T (lane = key, column = query),  P^T (over S^T),  GS^T (over GP^T),  GV += P^T GO,  GK += GS^T Q
-//            order of the MMAs: GV(t), S(t + 1), GK(t), GP(t + 1): the exponentials of t + 1 run beside the last two
+//   gk, gv:  S^T = K Q^T,  GP^T = V GO^T (lane = key, column = query),  P^T (shared memory),  GS^T (over GP^T),  GV += P^T GO,  GK += GS^T Q
+//            order of the MMAs: S(t + 1) as soon as S(t) is in registers, GV(t), GK(t), GP(t + 1).  (With P^T over S^T, S(t + 1) behind GV(t): the
+//            elementwise warps waited 870 of 3140 cycles a tile for it)
 // TMEM: 512 columns in both (two of scores or one, one of GP, the accumulators).
 #include "attention_sequence.cuh"
 
@@ -23,7 +24,7 @@ using namespace attn::blk;
 namespace bwd {
 
 constexpr int kRows = 128;                   // of an item and of a tile
-constexpr int kThreads = 384;
+constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512;
 
 struct Item { int head, begin, end, first; };         // head < 0: no more
@@ -34,6 +35,9 @@ template <int D> struct Cfg {
     static constexpr uint32_t kTile = kTileBytes<D>;
     static constexpr uint32_t kOwn = kRing * kTile;    // the item's own two tiles
     static constexpr uint32_t kMisc = kOwn + 2 * kTile;
+    static constexpr int kKeyRing = D == 128 ? 4 : 6;  // gk, gv: a tile's room is P^T's
+    static constexpr uint32_t kP = kKeyRing * kTile;   // two atoms of 64 queries
+    static_assert(kP + 32768 <= kOwn, "the ring's place");
     static constexpr uint32_t kStats = kMisc + 384;    // of two tiles of queries: [lse log2 e: 128 | delta: 128]
     static constexpr uint32_t kBytes = kStats + 2 * 1024;                      // the array itself is aligned: 227 KB leave nothing to round
     static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
@@ -41,7 +45,7 @@ template <int D> struct Cfg {
 
 struct Misc {
     uint64_t full[8], empty[8];
-    uint64_t own_full, own_empty, s[2], gp, p[2], gs[2], done, read;          // p, gs: by half of the columns; s: by buffer
+    uint64_t own_full, own_empty, s[2], s_read, gp, p[2], p_read, gs[2], done, read;  // p, gs: by half of the columns; s: by buffer
     uint64_t item_full[2], item_empty[2], stats_full[2], stats_empty[2], taken, tail;
     alignas(16) uint4 answer;
     Item item[2];
@@ -64,8 +68,10 @@ __device__ __forceinline__ void init(Misc& sh, int ring, int readers) {
     mbar_init(smem_u32(&sh.own_full), 1);
     mbar_init(smem_u32(&sh.own_empty), 1);
     mbar_init(smem_u32(&sh.gp), 1);
+    mbar_init(smem_u32(&sh.s_read), 8);
+    mbar_init(smem_u32(&sh.p_read), 1);
     mbar_init(smem_u32(&sh.done), 1);
-    mbar_init(smem_u32(&sh.read), 8);
+    mbar_init(smem_u32(&sh.read), 4);
     mbar_init(smem_u32(&sh.taken), 1);
     mbar_init(smem_u32(&sh.tail), 1);
     sh.abort = 0;
@@ -89,6 +95,24 @@ __device__ __forceinline__ void accumulate(uint32_t d_tmem, uint32_t a_tmem, uin
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) mma_ta(d_tmem, a_tmem + 8u * ks, db + uint64_t((ks * 2048) >> 4), instr_desc(D, false) | (1u << 16), !(first && ks == 0));
 }
+// the same with A in shared memory: one atom of 64 columns, K-major
+template <int D>
+__device__ __forceinline__ void accumulate_from_shared(uint32_t d_tmem, uint32_t a, uint32_t b, int half, bool first) {
+    const uint64_t da = desc_kmajor_sw128(a), db = desc_mnmajor_sw128(b + half * 64 * 128, Cfg<D>::kAtom);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) mma_dense(d_tmem, da + uint64_t((ks * 32) >> 4), db + uint64_t((ks * 2048) >> 4), instr_desc(D, false) | (1u << 16), !(first && ks == 0));
+}
+// The elementwise warps (4 .. 11) take registers of the others: 256 x 168 + 256 x 88 = 512 x 128, the launch's.  Each by all warps of two (one)
+// groups of four.
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 168;"); }
+__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+// 2^x of a pair
+__device__ __forceinline__ f2 powers(f2 x) {
+    float a, b;
+    un2(x, a, b);
+    return mk2(ex2(a), ex2(b));
+}
+
 }  // namespace bwd
 
 // (lse log2 e, delta) of every row and head, [Hq][M]
@@ -127,7 +151,7 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 32) {
-        init(sh, C::kRing, 9);                                     // an item's readers: the MMA thread, eight warps
+        init(sh, C::kRing, 13);                                    // an item's readers: the MMA thread, twelve warps
         tma_prefetch_map(&map_q);
         tma_prefetch_map(&map_go);
         tma_prefetch_map(&map_k);
@@ -139,6 +163,85 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
     tc_fence_after();
     const uint32_t tmem = sh.tmem, t_gp = tmem + 256, t_gq = tmem + 384;      // scores: tmem + 128 (j & 1)
 
+    if (warp >= 4 && warp < 12) {
+        take_registers();
+        // ---------------- elementwise: thread = row, half of the columns ----------------
+        const int half = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t lanes = uint32_t(quad * 32) << 16;
+        uint32_t phase_s = 0, phase_gp = 0;                        // phase_s: bit of the buffer
+        bool failed = false;
+        auto wait = [&](uint64_t& bar, uint32_t parity) {
+            failed = __any_sync(0xFFFFFFFFu, !mbar_wait(smem_u32(&bar), parity, abort_flag, p.status)) || failed;
+            tc_fence_after();
+        };
+        const f2 scale2 = mk2(p.scale_log2, p.scale_log2);
+        for (int item = 0;; ++item) {
+            wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
+            if (failed) break;
+            const Item it = sh.item[item & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+            if (it.head < 0) break;
+            const int n = it.first / kRows + 1, r = it.first + row;
+            const bool valid = r < it.end - it.begin;
+            const float2 st = valid ? stats[int64_t(it.head) * p.M + it.begin + r] : make_float2(0.0f, 0.0f);
+            const f2 lse2 = mk2(-st.x, -st.x), delta2 = mk2(-st.y, -st.y);
+            for (int j = 0; j < n; ++j) {
+                const uint32_t t_s = tmem + lanes + 128u * (j & 1) + 64u * half;
+                wait(sh.s[j & 1], (phase_s >> (j & 1)) & 1u);
+                if (failed) break;
+                phase_s ^= 1u << (j & 1);
+                const bool partly = j == n - 1;                    // the tile on the diagonal
+                const int left = row + 1 - 64 * half;              // columns the row sees there
+                uint32_t e[2][32];
+                tmem_ld32(t_s, e[0]);
+                tmem_ld32(t_s + 32u, e[1]);
+                tmem_ld_wait();
+                if (partly) {
+                    hide(e[0], left);
+                    hide(e[1], left - 32);
+                }
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) {
+                    float a, b;
+                    un2(powers(fma2(mk2(__uint_as_float(e[c >> 5][c & 31]), __uint_as_float(e[c >> 5][(c & 31) + 1])), scale2, lse2)), a, b);
+                    e[c >> 5][c & 31] = __float_as_uint(a);
+                    e[c >> 5][(c & 31) + 1] = __float_as_uint(b);
+                }
+                wait(sh.gp, phase_gp);
+                if (failed) break;
+                phase_gp ^= 1u;
+                uint32_t gs[32];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t v[32];
+                    tmem_ld32(tmem + lanes + 256u + 64u * half + 32u * i, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        float a, b;
+                        un2(mul2(mk2(__uint_as_float(e[i][c]), __uint_as_float(e[i][c + 1])),
+                                 add2(mk2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), delta2)), a, b);
+                        gs[16 * i + (c >> 1)] = pack2(a, b);
+                    }
+                }
+                if (partly) {                                      // keys after the query, and behind the sequence's end: 0 whatever the values hold there
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2) {
+                        if (c >= left) gs[c >> 1] = 0u;
+                        else if (c + 1 >= left) gs[c >> 1] &= 0xFFFFu;
+                    }
+                }
+                tmem_st32(t_s, gs);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.gs[half]));
+            }
+            if (failed) break;
+        }
+    } else {
+    give_registers();
     if (warp == 0) {
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
@@ -258,17 +361,14 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                 at += 2 * n;
             }
         }
-    } else if (warp >= 4) {
-        // ---------------- elementwise: thread = row, half of the columns ----------------
-        const int half = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
-        const uint32_t lanes = uint32_t(quad * 32) << 16;
-        uint32_t phase_s = 0, phase_gp = 0, phase_done = 0;        // phase_s: bit of the buffer
+    } else if (warp >= 12) {
+        // ---------------- results: thread = row ----------------
+        const int quad = warp & 3;
         bool failed = false;
         auto wait = [&](uint64_t& bar, uint32_t parity) {
-            failed = __any_sync(0xFFFFFFFFu, !mbar_wait(smem_u32(&bar), parity, abort_flag, p.status)) || failed;
+            failed = __any_sync(0xFFFFFFFFu, !mbar_wait_suspended(smem_u32(&bar), parity, abort_flag, p.status)) || failed;
             tc_fence_after();
         };
-        const f2 scale2 = mk2(p.scale_log2, p.scale_log2);
         for (int item = 0;; ++item) {
             wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
             if (failed) break;
@@ -276,71 +376,14 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
             if (it.head < 0) break;
-            const int n = it.first / kRows + 1, r = it.first + row;
-            const bool valid = r < it.end - it.begin;
-            const float2 st = valid ? stats[int64_t(it.head) * p.M + it.begin + r] : make_float2(0.0f, 0.0f);
-            const f2 lse2 = mk2(-st.x, -st.x), delta2 = mk2(-st.y, -st.y);
-            for (int j = 0; j < n; ++j) {
-                const uint32_t t_s = tmem + lanes + 128u * (j & 1) + 64u * half;
-                wait(sh.s[j & 1], (phase_s >> (j & 1)) & 1u);
-                if (failed) break;
-                phase_s ^= 1u << (j & 1);
-                const bool partly = j == n - 1;                    // the tile on the diagonal
-                const int left = row + 1 - 64 * half;              // columns the row sees there
-                uint32_t e[2][32];
-                tmem_ld32(t_s, e[0]);
-                tmem_ld32(t_s + 32u, e[1]);
-                tmem_ld_wait();
-                if (partly) {
-                    hide(e[0], left);
-                    hide(e[1], left - 32);
-                }
-#pragma unroll
-                for (int c = 0; c < 64; c += 2) {
-                    float a, b;
-                    un2(fma2(mk2(__uint_as_float(e[c >> 5][c & 31]), __uint_as_float(e[c >> 5][(c & 31) + 1])), scale2, lse2), a, b);
-                    e[c >> 5][c & 31] = __float_as_uint(ex2(a));
-                    e[c >> 5][(c & 31) + 1] = __float_as_uint(ex2(b));
-                }
-                wait(sh.gp, phase_gp);
-                if (failed) break;
-                phase_gp ^= 1u;
-                uint32_t gs[32];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t v[32];
-                    tmem_ld32(tmem + lanes + 256u + 64u * half + 32u * i, v);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) {
-                        float a, b;
-                        un2(mul2(mk2(__uint_as_float(e[i][c]), __uint_as_float(e[i][c + 1])),
-                                 add2(mk2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), delta2)), a, b);
-                        gs[16 * i + (c >> 1)] = pack2(a, b);
-                    }
-                }
-                if (partly) {                                      // keys after the query, and behind the sequence's end: 0 whatever the values hold there
-#pragma unroll
-                    for (int c = 0; c < 64; c += 2) {
-                        if (c >= left) gs[c >> 1] = 0u;
-                        else if (c + 1 >= left) gs[c >> 1] &= 0xFFFFu;
-                    }
-                }
-                tmem_st32(t_s, gs);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh.gs[half]));
-            }
+            wait(sh.done, uint32_t(item) & 1u);
             if (failed) break;
-            wait(sh.done, phase_done);
-            if (failed) break;
-            phase_done ^= 1u;
-            store_rows<D / 2>(t_gq + lanes + half * (D / 2), gq + int64_t(it.head) * D + half * (D / 2), ldgq, it.begin + it.first + quad * 32, it.end, p.scale);
+            store_rows<D>(t_gq + (uint32_t(quad * 32) << 16), gq + int64_t(it.head) * D, ldgq, it.begin + it.first + quad * 32, it.end, p.scale);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.read));
         }
+    }
     }
     tc_fence_before();
     __syncthreads();
@@ -365,7 +408,7 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 32) {
-        init(sh, C::kRing, 10);                                    // an item's readers: the MMA thread, the warp of the statistics, eight warps
+        init(sh, C::kKeyRing, 13);                                 // an item's readers: the MMA thread, twelve warps
         tma_prefetch_map(&map_q);
         tma_prefetch_map(&map_go);
         tma_prefetch_map(&map_k);
@@ -379,11 +422,124 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     // tiles of queries that see the item's keys, of one head; tile i of the item is tile first / kRows + i % tiles of head i / tiles
     auto tiles_of_item = [](const Item& it) { return (it.end - it.begin + kRows - 1) / kRows - it.first / kRows; };
 
+    if (warp >= 4 && warp < 12) {
+        take_registers();
+        // ---------------- elementwise: thread = key, half of the queries ----------------
+        const int half = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t lanes = uint32_t(quad * 32) << 16, t_s = tmem + lanes + 64u * half, t_g = t_gp + lanes + 64u * half;
+        uint32_t phase = 0;
+        int k = 0;
+        bool failed = false;
+        auto wait = [&](uint64_t& bar, uint32_t parity) {
+            failed = __any_sync(0xFFFFFFFFu, !mbar_wait(smem_u32(&bar), parity, abort_flag, p.status)) || failed;
+            tc_fence_after();
+        };
+        const f2 scale2 = mk2(p.scale_log2, p.scale_log2);
+        for (int item = 0;; ++item) {
+            wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
+            if (failed) break;
+            const Item it = sh.item[item & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+            if (it.head < 0) break;
+            const int tiles = tiles_of_item(it), n = tiles * p.G;
+            int of_head = 0;
+            for (int t = 0; t < n; ++t, ++k) {
+                const bool partly = of_head == 0;                  // the tile on the diagonal
+                if (++of_head == tiles) of_head = 0;
+                wait(sh.stats_full[k & 1], uint32_t(k >> 1) & 1u);
+                const float4* lse4 = reinterpret_cast<const float4*>(stats_sh + 256 * (k & 1) + 64 * half);
+                const float4* delta4 = lse4 + 32;
+                float4 l4[16];                                     // before the scores: the products leave little of shared memory's time
+#pragma unroll
+                for (int i = 0; i < 16; ++i) l4[i] = lse4[i];
+                if (!failed) wait(sh.s[0], phase);
+                if (failed) break;
+                uint32_t e[2][32];
+                tmem_ld32(t_s, e[0]);
+                tmem_ld32(t_s + 32u, e[1]);
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.s_read));
+                if (k >= 1) wait(sh.p_read, uint32_t(k - 1) & 1u); // the last tile's product with P^T is done
+                if (failed) break;
+                uint8_t* const p_row = smem + C::kP + half * C::kAtom;
+#pragma unroll
+                for (int c = 0; c < 64; c += 8) {
+                    uint32_t out[4];
+#pragma unroll
+                    for (int i = 0; i < 8; i += 4) {
+                        const float4 l = l4[(c + i) >> 2];
+                        uint32_t* const x = &e[c >> 5][(c & 31) + i];
+                        float a[4];
+                        un2(powers(fma2(mk2(__uint_as_float(x[0]), __uint_as_float(x[1])), scale2, mk2(l.x, l.y))), a[0], a[1]);
+                        un2(powers(fma2(mk2(__uint_as_float(x[2]), __uint_as_float(x[3])), scale2, mk2(l.z, l.w))), a[2], a[3]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(a[j]);
+                        out[i >> 1] = pack2(a[0], a[1]);
+                        out[(i >> 1) + 1] = pack2(a[2], a[3]);
+                    }
+                    *reinterpret_cast<uint4*>(p_row + atom_chunk_offset(row, c >> 3)) = make_uint4(out[0], out[1], out[2], out[3]);
+                }
+                if (partly) {                                      // queries before the key: zeros, a second time over the row
+#pragma unroll
+                    for (int c = 0; c < 64; c += 8) {
+                        uint32_t out[4];
+#pragma unroll
+                        for (int i = 0; i < 8; i += 2) {
+                            uint32_t* const x = &e[c >> 5][(c & 31) + i];
+                            if (64 * half + c + i < row) x[0] = 0u;
+                            if (64 * half + c + i + 1 < row) x[1] = 0u;
+                            out[i >> 1] = pack2(__uint_as_float(x[0]), __uint_as_float(x[1]));
+                        }
+                        *reinterpret_cast<uint4*>(p_row + atom_chunk_offset(row, c >> 3)) = make_uint4(out[0], out[1], out[2], out[3]);
+                    }
+                }
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.p[half]));
+                wait(sh.gp, phase);
+                if (failed) break;
+                uint32_t out[32];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t v[32];
+                    tmem_ld32(t_g + 32u * i, v);
+                    float4 d4[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d4[j] = delta4[8 * i + j];
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        const float4 d = d4[c >> 2];
+                        float a, b;
+                        un2(mul2(mk2(__uint_as_float(e[i][c]), __uint_as_float(e[i][c + 1])), add2(mk2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), mk2(d.x, d.y))), a, b);
+                        out[16 * i + (c >> 1)] = pack2(a, b);
+                        un2(mul2(mk2(__uint_as_float(e[i][c + 2]), __uint_as_float(e[i][c + 3])),
+                                 add2(mk2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), mk2(d.z, d.w))), a, b);
+                        out[16 * i + (c >> 1) + 1] = pack2(a, b);
+                    }
+                }
+                tmem_st32(t_g, out);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&sh.gs[half]));
+                    mbar_arrive(smem_u32(&sh.stats_empty[k & 1]));
+                }
+                phase ^= 1u;
+            }
+            if (failed) break;
+        }
+    } else {
+    give_registers();
     if (warp == 0) {
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
-        Loader<D, C::kRing> ring(smem, sh.full, sh.empty, &sh.tail, abort_flag, p.status);
-        int items = 0;
+        Loader<D, C::kKeyRing> ring(smem, sh.full, sh.empty, &sh.tail, abort_flag, p.status);
+        int items = 0, k = 0;                                      // k: tiles of queries so far
         uint32_t phase_own = 0, phase_taken = 0;
         unsigned at = blockIdx.x;
         for (;;) {
@@ -411,9 +567,22 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 }
                 __syncwarp();
                 for (int h = kvh * p.G; h < (kvh + 1) * p.G && ring.ok; ++h)
-                    for (int row = it.begin + it.first; row < it.end && ring.ok; row += kRows) {
+                    for (int row = it.begin + it.first; row < it.end && ring.ok; row += kRows, ++k) {
+                        float2 v[4];                               // statistics of the tile's queries; behind the end: probability 0
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            v[i] = row + lane + 32 * i < it.end ? stats[int64_t(h) * p.M + row + lane + 32 * i] : make_float2(INFINITY, 0.0f);
                         ring.load(&map_q, row, h * (D / 64), it.end - row, keep);
                         if (ring.ok) ring.load(&map_go, row, h * (D / 64), it.end - row, keep);
+                        if (k >= 2 && ring.ok) ring.wait(sh.stats_empty[k & 1], uint32_t((k >> 1) - 1) & 1u);
+                        if (!ring.ok) break;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            stats_sh[256 * (k & 1) + lane + 32 * i] = -v[i].x;
+                            stats_sh[256 * (k & 1) + 128 + lane + 32 * i] = -v[i].y;
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&sh.stats_full[k & 1]));
                     }
             }
             const bool before = ring.ok;
@@ -441,9 +610,9 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 ok = ok && mbar_wait(smem_u32(&bar), parity, abort_flag, p.status);
                 tc_fence_after();
             };
-            auto place = [&](int i) { return base + (i % C::kRing) * C::kTile; };
-            auto arrived = [&](int i) { wait(sh.full[i % C::kRing], uint32_t(i / C::kRing) & 1u); return place(i); };
-            auto release = [&](int i) { mma_commit(smem_u32(&sh.empty[i % C::kRing])); };
+            auto place = [&](int i) { return base + (i % C::kKeyRing) * C::kTile; };
+            auto arrived = [&](int i) { wait(sh.full[i % C::kKeyRing], uint32_t(i / C::kKeyRing) & 1u); return place(i); };
+            auto release = [&](int i) { mma_commit(smem_u32(&sh.empty[i % C::kKeyRing])); };
             const uint32_t k_tile = base + C::kOwn, v_tile = k_tile + C::kTile;
             for (int item = 0; ok; ++item) {
                 wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
@@ -475,18 +644,23 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                         }
                         began = true;
                     }
+                    if (t + 1 < n) {
+                        wait(sh.s_read, phase_p);                  // the scores are in registers
+                        if (ok) scores(t + 1);
+                    }
 #pragma unroll 1
                     for (int half = 0; half < 2 && ok; ++half) {
                         wait(sh.p[half], phase_p);
-                        if (ok) accumulate<D>(t_gv, tmem + 64u * half, place(at + 2 * t + 1), half, t == 0 && half == 0);
+                        if (ok) accumulate_from_shared<D>(t_gv, base + C::kP + half * C::kAtom, place(at + 2 * t + 1), half, t == 0 && half == 0);
                     }
+                    mma_commit(smem_u32(&sh.p_read));
                     release(at + 2 * t + 1);
-                    if (ok && t + 1 < n) scores(t + 1);
 #pragma unroll 1
                     for (int half = 0; half < 2 && ok; ++half) {
                         wait(sh.gs[half], phase_p);
                         if (ok) accumulate<D>(t_gk, t_gp + 64u * half, place(at + 2 * t), half, t == 0 && half == 0);
                     }
+                    if (t + 1 == n) wait(sh.s_read, phase_p);      // (every tile's)
                     phase_p ^= 1u;
                     release(at + 2 * t);
                     if (ok && t + 1 < n) gps(t + 1);
@@ -496,47 +670,15 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 at += 2 * n;
             }
         }
-    } else if (warp == 3) {
-        // ---------------- statistics of the tiles' queries ----------------
-        bool ok = true;
-        auto wait = [&](uint64_t& bar, uint32_t parity) { ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspended(smem_u32(&bar), parity, abort_flag, p.status)) && ok; };
-        int k = 0;                                                 // tiles so far
-        for (int item = 0; ok; ++item) {
-            wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
-            if (!ok) break;
-            const Item it = sh.item[item & 1];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
-            if (it.head < 0) break;
-            for (int h = it.head * p.G; h < (it.head + 1) * p.G && ok; ++h)
-                for (int row = it.begin + it.first; row < it.end && ok; row += kRows, ++k) {
-                    float2 v[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)                    // behind the end: probability 0
-                        v[i] = row + lane + 32 * i < it.end ? stats[int64_t(h) * p.M + row + lane + 32 * i] : make_float2(INFINITY, 0.0f);
-                    if (k >= 2) wait(sh.stats_empty[k & 1], uint32_t((k >> 1) - 1) & 1u);
-                    if (!ok) break;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        stats_sh[256 * (k & 1) + lane + 32 * i] = -v[i].x;
-                        stats_sh[256 * (k & 1) + 128 + lane + 32 * i] = -v[i].y;
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&sh.stats_full[k & 1]));
-                }
-        }
-    } else if (warp >= 4) {
-        // ---------------- elementwise: thread = key, half of the queries ----------------
-        const int half = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
-        const uint32_t lanes = uint32_t(quad * 32) << 16, t_s = tmem + lanes + 64u * half, t_g = t_gp + lanes + 64u * half;
-        uint32_t phase = 0, phase_done = 0;
-        int k = 0;
+    } else if (warp >= 12) {
+        // ---------------- results: thread = key ----------------
+        const int quad = warp & 3;
+        const uint32_t lanes = uint32_t(quad * 32) << 16;
         bool failed = false;
         auto wait = [&](uint64_t& bar, uint32_t parity) {
-            failed = __any_sync(0xFFFFFFFFu, !mbar_wait(smem_u32(&bar), parity, abort_flag, p.status)) || failed;
+            failed = __any_sync(0xFFFFFFFFu, !mbar_wait_suspended(smem_u32(&bar), parity, abort_flag, p.status)) || failed;
             tc_fence_after();
         };
-        const f2 scale2 = mk2(p.scale_log2, p.scale_log2);
         for (int item = 0;; ++item) {
             wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
             if (failed) break;
@@ -544,82 +686,16 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
             if (it.head < 0) break;
-            const int tiles = tiles_of_item(it), n = tiles * p.G;
-            int of_head = 0;
-            for (int t = 0; t < n; ++t, ++k) {
-                const bool partly = of_head == 0;                  // the tile on the diagonal
-                if (++of_head == tiles) of_head = 0;
-                wait(sh.stats_full[k & 1], uint32_t(k >> 1) & 1u);
-                if (!failed) wait(sh.s[0], phase);
-                if (failed) break;
-                const float4* lse4 = reinterpret_cast<const float4*>(stats_sh + 256 * (k & 1) + 64 * half);
-                const float4* delta4 = lse4 + 32;
-                uint32_t e[2][32], out[32];
-                tmem_ld32(t_s, e[0]);
-                tmem_ld32(t_s + 32u, e[1]);
-                tmem_ld_wait();
-#pragma unroll
-                for (int c = 0; c < 64; c += 4) {
-                    const float4 l = lse4[c >> 2];
-                    float a[4];
-                    un2(fma2(mk2(__uint_as_float(e[c >> 5][c & 31]), __uint_as_float(e[c >> 5][(c & 31) + 1])), scale2, mk2(l.x, l.y)), a[0], a[1]);
-                    un2(fma2(mk2(__uint_as_float(e[c >> 5][(c & 31) + 2]), __uint_as_float(e[c >> 5][(c & 31) + 3])), scale2, mk2(l.z, l.w)), a[2], a[3]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        e[c >> 5][(c & 31) + i] = __float_as_uint(ex2(a[i]));
-                    }
-                }
-                if (partly) {                                      // queries before the key
-#pragma unroll
-                    for (int c = 0; c < 64; ++c)
-                        if (64 * half + c < row) e[c >> 5][c & 31] = 0u;
-                }
-#pragma unroll
-                for (int c = 0; c < 64; c += 2) out[c >> 1] = pack2(__uint_as_float(e[c >> 5][c & 31]), __uint_as_float(e[c >> 5][(c & 31) + 1]));
-                tmem_st32(t_s, out);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh.p[half]));
-                wait(sh.gp, phase);
-                if (failed) break;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t v[32];
-                    tmem_ld32(t_g + 32u * i, v);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        const float4 d = delta4[8 * i + (c >> 2)];
-                        float a, b;
-                        un2(mul2(mk2(__uint_as_float(e[i][c]), __uint_as_float(e[i][c + 1])), add2(mk2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), mk2(d.x, d.y))), a, b);
-                        out[16 * i + (c >> 1)] = pack2(a, b);
-                        un2(mul2(mk2(__uint_as_float(e[i][c + 2]), __uint_as_float(e[i][c + 3])),
-                                 add2(mk2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), mk2(d.z, d.w))), a, b);
-                        out[16 * i + (c >> 1) + 1] = pack2(a, b);
-                    }
-                }
-                tmem_st32(t_g, out);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(smem_u32(&sh.gs[half]));
-                    mbar_arrive(smem_u32(&sh.stats_empty[k & 1]));
-                }
-                phase ^= 1u;
-            }
+            wait(sh.done, uint32_t(item) & 1u);
             if (failed) break;
-            wait(sh.done, phase_done);
-            if (failed) break;
-            phase_done ^= 1u;
             const int row0 = it.begin + it.first + quad * 32;
-            if (half == 0) store_rows<D>(t_gv + lanes, gv + int64_t(it.head) * D, ldgv, row0, it.end, 1.0f);
-            else store_rows<D>(t_gk + lanes, gk + int64_t(it.head) * D, ldgk, row0, it.end, p.scale);
+            store_rows<D>(t_gv + lanes, gv + int64_t(it.head) * D, ldgv, row0, it.end, 1.0f);
+            store_rows<D>(t_gk + lanes, gk + int64_t(it.head) * D, ldgk, row0, it.end, p.scale);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.read));
         }
+    }
     }
     tc_fence_before();
     __syncthreads();
