@@ -6,8 +6,7 @@
 // the sums of gk and gv also over the query heads that share the key head.  Products take bf16 operands and fp32 accumulators; p and gs are
 // rounded to bf16 for theirs (the sum l takes p unrounded).
 //
-// A CTA owns 64 rows of a sequence: queries of one head (result, gq) or keys of one key head (gk, gv; it walks over the group's query
-// heads, so that shared heads need no atomics and equal calls give equal bits).
+// The kernels are in attention_sequence_sm100.cu and attention_sequence_grad_sm100.cu; here are the checks of arguments.
 #include <math.h>
 #include "attention_sequence.cuh"
 
@@ -25,6 +24,7 @@ static int check_rows(const void* x, int64_t ld, int64_t H, int64_t D) {
     if (ld < H * D || ld % 8 || ld > (int64_t(1) << 28)) return PATCH_ERR_SHAPE;
     return aligned16(x) ? PATCH_OK : PATCH_ERR_ALIGN;
 }
+static size_t stats_bytes(int64_t M, int Hq) { return (size_t(M) * Hq * sizeof(float2) + 255) / 256 * 256; }
 static int check_scale(float scale) { return scale > 0.0f && scale <= 2e38f ? PATCH_OK : PATCH_ERR_SHAPE; }
 
 }  // namespace seq
@@ -54,7 +54,8 @@ extern "C" int patch_sequence_attention_backward_workspace_size(int64_t M, int64
     if (!bytes_out) return PATCH_ERR_NULL;
     const int rc = seq::check_shape(M, Hq, Hkv, D, B);
     if (rc) return rc;
-    *bytes_out = size_t(M) * Hq * sizeof(float2);
+    const int splits = seq::key_splits(M, B, Hkv, Hq / Hkv);
+    *bytes_out = seq::stats_bytes(M, Hq) + (splits > 1 ? size_t(splits) * 2 * M * Hkv * D * sizeof(float) : 0);
     return PATCH_OK;
 }
 
@@ -79,5 +80,6 @@ extern "C" int patch_sequence_attention_backward(const void* gO, int64_t ldgo, c
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     B16 *gq = static_cast<B16*>(gQ), *gk = static_cast<B16*>(gK), *gv = static_cast<B16*>(gV);
     float2* stats = static_cast<float2*>(workspace);
-    return seq::launch_backward(p, D, lse, stats, gq, ldgq, gk, ldgk, gv, ldgv, s);
+    float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + seq::stats_bytes(M, Hq));
+    return seq::launch_backward(p, D, lse, stats, parts, seq::key_splits(M, B, Hkv, Hq / Hkv), gq, ldgq, gk, ldgk, gv, ldgv, s);
 }

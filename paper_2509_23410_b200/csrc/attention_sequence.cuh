@@ -72,11 +72,11 @@ template <int D> constexpr uint32_t kTileBytes = kTileRows * D * 2;
 template <int D, int RING>
 struct Loader {
     uint8_t* smem;                           // the ring
-    uint64_t *full, *empty, *tail;           // tail: a barrier of its own for tiles that need work behind the copy
+    uint64_t *full, *empty, *tail;           // tail: of tiles that need work behind the copy, by stage
     volatile int* abort_flag;
     int* status;
     int stage = 0, issued = 0;
-    uint32_t phase = 0, phase_tail = 0;
+    uint32_t phase = 0;
     bool ok = true;
 
     __device__ __forceinline__ Loader(uint8_t* smem_, uint64_t* full_, uint64_t* empty_, uint64_t* tail_, volatile int* abort_, int* status_)
@@ -84,32 +84,17 @@ struct Loader {
     __device__ __forceinline__ void wait(uint64_t& bar, uint32_t parity) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bar), parity, abort_flag, status)) && ok;
     }
-    // 128 rows from `row` on of one head into the next stage; `left` < 128: rows from there on become zeros
+    // 128 rows from `row` on of one head into the next stage; `left` < 128: rows from there on become zeros (by Mender, which hands the tile on)
     __device__ __forceinline__ void load(const CUtensorMap* map, int row, int chunk, int left, uint64_t policy) {
         if (issued >= RING) wait(empty[stage], phase ^ 1u);
         if (!ok) return;
-        const int lane = threadIdx.x & 31;
-        uint8_t* const tile = smem + stage * kTileBytes<D>;
-        const bool partly = left < kTileRows;
-        if (lane == 0) {
-            const uint32_t bar = smem_u32(partly ? tail : &full[stage]);
+        if ((threadIdx.x & 31) == 0) {
+            const uint32_t bar = smem_u32(left < kTileRows ? &tail[stage] : &full[stage]);
             mbar_expect_tx(bar, kTileBytes<D>);
-            tma_tile_load_3d(smem_u32(tile), map, 0, row, chunk, bar, policy);
+            tma_tile_load_3d(smem_u32(smem) + stage * kTileBytes<D>, map, 0, row, chunk, bar, policy);
         }
         __syncwarp();
         ++issued;
-        if (partly) {
-            wait(*tail, phase_tail);
-            if (!ok) return;
-            phase_tail ^= 1u;
-            for (int i = left * (D / 8) + lane; i < kTileRows * (D / 8); i += 32) {
-                const int r = i / (D / 8), c = i - r * (D / 8);
-                *reinterpret_cast<uint4*>(tile + (c >> 3) * (kTileRows * 128) + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            attn::blk::fence_async_shared();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
-        }
         if (++stage == RING) { stage = 0; phase ^= 1u; }
     }
     // after a failure: copies on their way end before the CTA does
@@ -120,20 +105,56 @@ struct Loader {
         while (global_timer_ns() - t0 < kDrainLimitNs) {}                    // those with barriers of their own
     }
 };
+// Two warps that follow the loads, one the even and one the odd numbers, and put zeros behind a sequence's end: a probability of 0 times whatever
+// lies there is not always 0.  (The producer itself, waiting for each such copy, held up short sequences by 3 us.)
+template <int D, int RING>
+struct Mender {
+    uint8_t* smem;
+    uint64_t *full, *tail;
+    volatile int* abort_flag;
+    int* status;
+    int which;                               // 0 or 1
+    int number = 0;                          // of loads so far
+    uint32_t phases = 0;                     // of the tail barriers, by stage
+    bool ok = true;
+    // the next load of the producer, with its `left`
+    __device__ __forceinline__ void next(int left) {
+        const int i = number++, stage = i % RING;
+        if (left >= kTileRows || !ok) return;
+        phases ^= 1u << stage;               // (the other warp's tiles count too)
+        if ((i & 1) != which) return;
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspended(smem_u32(&tail[stage]), ~(phases >> stage) & 1u, abort_flag, status));
+        if (!ok) return;
+        uint8_t* const tile = smem + stage * kTileBytes<D>;
+        const int lane = threadIdx.x & 31;
+        for (int j = left * (D / 8) + lane; j < kTileRows * (D / 8); j += 32) {
+            const int r = j / (D / 8), c = j - r * (D / 8);
+            *reinterpret_cast<uint4*>(tile + (c >> 3) * (kTileRows * 128) + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        attn::blk::fence_async_shared();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&full[stage]));
+    }
+};
 
-// 32 rows (a warp's, lane = row) of COLS fp32 columns of TMEM, times `f` of the lane's row, as bf16 into rows [row, end).  Four neighbouring lanes
-// exchange their 64 bytes, so that a store writes 64 consecutive bytes of eight rows (a lane that writes its own row alone touches 32 lines with every
-// 16 bytes: 4 000 cycles of the load-store unit for an item of 256 x 128, against 1 000).
-template <int COLS>
-__device__ __forceinline__ void store_rows(uint32_t t, __nv_bfloat16* to, int64_t ld, int row, int end, float f) {
+// 32 rows (a warp's, lane = row) of COLS fp32 columns of TMEM, times `f` of the lane's row, as bf16 (or as they are, F32) into rows [row, end).  Four
+// neighbouring lanes exchange their 64 bytes, so that a store writes 64 consecutive bytes of eight rows (a lane that writes its own row alone touches 32 lines
+// with every 16 bytes: 4 000 cycles of the load-store unit for an item of 256 x 128, against 1 000).
+template <int COLS, bool F32 = false>
+__device__ __forceinline__ void store_rows(uint32_t t, void* to, int64_t ld, int row, int end, float f) {
+    constexpr int kStep = F32 ? 16 : 32, kBytes = F32 ? 4 : 2;     // columns of 64 bytes
     const int lane = threadIdx.x & 31, sub = lane & 3;
-#pragma unroll 1
-    for (int q = 0; q < COLS / 32; ++q) {
-        uint32_t v[32], w[4][4];                                   // w: 16-byte chunks of the lane's row, then chunk `sub` of four rows
-        attn::blk::tmem_ld32(t + 32u * q, v);
+    if (row >= end) return;                  // none of them
+#pragma unroll 2
+    for (int q = 0; q < COLS / kStep; ++q) {
+        uint32_t v[kStep], w[4][4];                                // w: 16-byte chunks of the lane's row, then chunk `sub` of four rows
+        attn::blk::load_quarter(t + uint32_t(kStep) * q, v);
         tmem_ld_wait();
 #pragma unroll
-        for (int c = 0; c < 16; ++c) w[c >> 2][c & 3] = attn::pack2(__uint_as_float(v[2 * c]) * f, __uint_as_float(v[2 * c + 1]) * f);
+        for (int c = 0; c < 16; ++c) {
+            if constexpr (F32) w[c >> 2][c & 3] = __float_as_uint(__uint_as_float(v[c]) * f);
+            else w[c >> 2][c & 3] = attn::pack2(__uint_as_float(v[2 * c]) * f, __uint_as_float(v[2 * c + 1]) * f);
+        }
 #pragma unroll
         for (int bit = 1; bit <= 2; bit <<= 1) {
             const bool high = sub & bit;
@@ -150,14 +171,17 @@ __device__ __forceinline__ void store_rows(uint32_t t, __nv_bfloat16* to, int64_
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int r = row + (lane & ~3) + j;
-            if (r < end) *reinterpret_cast<uint4*>(to + int64_t(r) * ld + 32 * q + 8 * sub) = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+            if (r < end) *reinterpret_cast<uint4*>(static_cast<char*>(to) + int64_t(r) * ld * kBytes + 64 * q + 16 * sub) = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
         }
     }
 }
 
 int launch_forward(const Problem& p, int D, __nv_bfloat16* o, int64_t ldo, float* lse, cudaStream_t s);
-// stats: [Hq][M] of scratch
-int launch_backward(const Problem& p, int D, const float* lse, float2* stats, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
+// Into how many parts the query heads of a key head are cut for gk and gv: 1, or a divisor of the group where the items were fewer than the SMs.  By
+// the sizes alone (sequences may leave fewer tiles than M and B allow for).
+int key_splits(int64_t M, int64_t B, int Hkv, int G);
+// stats: [Hq][M] of scratch; parts: [split][2][M][Hkv][D] where there are several
+int launch_backward(const Problem& p, int D, const float* lse, float2* stats, float* parts, int splits, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
                     int64_t ldgv, cudaStream_t s);
 
 }  // namespace seq

@@ -38,7 +38,7 @@ template <int D> struct Cfg {
     static constexpr int kKeyRing = D == 128 ? 4 : 6;  // gk, gv: a tile's room is P^T's
     static constexpr uint32_t kP = kKeyRing * kTile;   // two atoms of 64 queries
     static_assert(kP + 32768 <= kOwn, "the ring's place");
-    static constexpr uint32_t kStats = kMisc + 384;    // of two tiles of queries: [lse log2 e: 128 | delta: 128]
+    static constexpr uint32_t kStats = kMisc + 512;    // of two tiles of queries: [lse log2 e: 128 | delta: 128]
     static constexpr uint32_t kBytes = kStats + 2 * 1024;                      // the array itself is aligned: 227 KB leave nothing to round
     static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
 };
@@ -46,16 +46,16 @@ template <int D> struct Cfg {
 struct Misc {
     uint64_t full[8], empty[8];
     uint64_t own_full, own_empty, s[2], s_read, gp, p[2], p_read, gs[2], done, read;  // p, gs: by half of the columns; s: by buffer
-    uint64_t item_full[2], item_empty[2], stats_full[2], stats_empty[2], taken, tail;
+    uint64_t item_full[2], item_empty[2], stats_full[2], stats_empty[2], taken, tail[8];
     alignas(16) uint4 answer;
     Item item[2];
     uint32_t tmem;
     int abort;
 };
-static_assert(sizeof(Misc) <= 384, "fits behind the tiles");
+static_assert(sizeof(Misc) <= 512, "fits behind the tiles");
 
 __device__ __forceinline__ void init(Misc& sh, int ring, int readers) {
-    for (int i = 0; i < ring; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); }
+    for (int i = 0; i < ring; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); mbar_init(smem_u32(&sh.tail[i]), 1); }
     for (int x = 0; x < 2; ++x) {
         mbar_init(smem_u32(&sh.s[x]), 1);
         mbar_init(smem_u32(&sh.p[x]), 4);
@@ -73,7 +73,6 @@ __device__ __forceinline__ void init(Misc& sh, int ring, int readers) {
     mbar_init(smem_u32(&sh.done), 1);
     mbar_init(smem_u32(&sh.read), 4);
     mbar_init(smem_u32(&sh.taken), 1);
-    mbar_init(smem_u32(&sh.tail), 1);
     sh.abort = 0;
     mbar_init_fence();
 }
@@ -115,25 +114,38 @@ __device__ __forceinline__ f2 powers(f2 x) {
 
 }  // namespace bwd
 
-// (lse log2 e, delta) of every row and head, [Hq][M]
+// (lse log2 e, delta) of every row and head, [Hq][M].  D / 8 lanes to a head of a row; a thread has four of them on their way.
 template <int D>
 __global__ void __launch_bounds__(256) delta_kernel(const Problem p, const float* lse, float2* stats) {
-    const int64_t group = (int64_t(blockIdx.x) * 256 + threadIdx.x) / (D / 8);
-    const int c = threadIdx.x & (D / 8 - 1);
-    if (group >= int64_t(p.M) * p.Hq) return;
-    const int64_t row = group / p.Hq;
-    const int h = int(group - row * p.Hq);
-    const uint4 a = *reinterpret_cast<const uint4*>(p.o + row * p.ldo + h * D + 8 * c), b = *reinterpret_cast<const uint4*>(p.go + row * p.ldgo + h * D + 8 * c);
-    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
-    float sum = 0.0f;
+    constexpr int kLanes = D / 8, kAtOnce = 4, kGroups = 256 / kLanes;
+    grid_launch_dependents();                // they wait for what is written here
+    const int c = threadIdx.x & (kLanes - 1);
+    const int64_t first = int64_t(blockIdx.x) * kGroups * kAtOnce + threadIdx.x / kLanes, all = int64_t(p.M) * p.Hq;
+    uint4 a[kAtOnce], b[kAtOnce];
+    float l[kAtOnce];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        sum = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum);
-        sum = fmaf(__uint_as_float(x[i] & 0xFFFF0000u), __uint_as_float(y[i] & 0xFFFF0000u), sum);
+    for (int i = 0; i < kAtOnce; ++i) {
+        const int64_t group = first + i * kGroups, row = group / p.Hq;
+        if (group >= all) continue;
+        const int h = int(group - row * p.Hq);
+        a[i] = *reinterpret_cast<const uint4*>(p.o + row * p.ldo + h * D + 8 * c);
+        b[i] = *reinterpret_cast<const uint4*>(p.go + row * p.ldgo + h * D + 8 * c);
+        if (c == 0) l[i] = lse[group];
     }
 #pragma unroll
-    for (int d = D / 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-    if (c == 0) stats[int64_t(h) * p.M + row] = make_float2(lse[group] * 1.44269504f, sum);
+    for (int i = 0; i < kAtOnce; ++i) {
+        const int64_t group = first + i * kGroups, row = group / p.Hq;
+        const uint32_t x[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, y[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            sum = fmaf(__uint_as_float(x[j] << 16), __uint_as_float(y[j] << 16), sum);
+            sum = fmaf(__uint_as_float(x[j] & 0xFFFF0000u), __uint_as_float(y[j] & 0xFFFF0000u), sum);
+        }
+#pragma unroll
+        for (int d = kLanes / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+        if (c == 0 && group < all) stats[(group - row * p.Hq) * p.M + row] = make_float2(l[i] * 1.44269504f, sum);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -151,7 +163,7 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 32) {
-        init(sh, C::kRing, 13);                                    // an item's readers: the MMA thread, twelve warps
+        init(sh, C::kRing, 15);                                    // an item's readers: the MMA thread, two menders, twelve warps
         tma_prefetch_map(&map_q);
         tma_prefetch_map(&map_go);
         tma_prefetch_map(&map_k);
@@ -174,6 +186,8 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
             failed = __any_sync(0xFFFFFFFFu, !mbar_wait(smem_u32(&bar), parity, abort_flag, p.status)) || failed;
             tc_fence_after();
         };
+        grid_dependency_wait();              // the statistics
+        grid_launch_dependents();            // which the kernel of gk and gv, the next one, then finds as well
         const f2 scale2 = mk2(p.scale_log2, p.scale_log2);
         for (int item = 0;; ++item) {
             wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
@@ -246,13 +260,17 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
         const int slots = int(most_tiles(p.M, p.B, kRows));
-        Loader<D, C::kRing> ring(smem, sh.full, sh.empty, &sh.tail, abort_flag, p.status);
+        Loader<D, C::kRing> ring(smem, sh.full, sh.empty, sh.tail, abort_flag, p.status);
         int items = 0;
         uint32_t phase_own = 0, phase_taken = 0;
         unsigned at = blockIdx.x;
-        for (;;) {
+        // (The first question waits for the kernel before: a CTA that started beside it would take work from SMs that are about to be free.)
+        auto ask = [&] {
             if (lane == 0) ask_for_next(&sh.answer, &sh.taken);
             __syncwarp();
+        };
+        for (bool first = true;; first = false) {
+            if (!first) ask();
             if (at == 0) check_starts(p, lane, 32);
             const int slot = slots - 1 - int(at / unsigned(p.Hq)), head = int(at % unsigned(p.Hq));
             const Tile t = tile_of<kRows>(p, slot);
@@ -281,6 +299,10 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                     ring.load(&map_k, row, chunk, it.end - row, keep);
                     if (ring.ok) ring.load(&map_v, row, chunk, kRows, keep);
                 }
+            }
+            if (first) {
+                grid_dependency_wait();
+                ask();
             }
             const bool before = ring.ok;
             ring.ok = true;
@@ -361,7 +383,21 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                 at += 2 * n;
             }
         }
-    } else if (warp >= 12) {
+    } else if (warp < 4) {
+        // ---------------- keys behind a sequence's end ----------------
+        Mender<D, C::kRing> mender{smem, sh.full, sh.tail, abort_flag, p.status, warp - 2};
+        for (int item = 0; mender.ok; ++item) {
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspended(smem_u32(&sh.item_full[item & 1]), uint32_t(item >> 1) & 1u, abort_flag, p.status))) break;
+            const Item it = sh.item[item & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+            if (it.head < 0) break;
+            for (int j = 0; j <= it.first / kRows; ++j) {
+                mender.next(it.end - it.begin - j * kRows);
+                mender.next(kRows);
+            }
+        }
+    } else {
         // ---------------- results: thread = row ----------------
         const int quad = warp & 3;
         bool failed = false;
@@ -396,8 +432,8 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
 template <int D>
 __global__ void __launch_bounds__(bwd::kThreads, 1)
 sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUtensorMap map_k,
-                         const __grid_constant__ CUtensorMap map_v, const Problem p, const float2* const stats, __nv_bfloat16* const gk, const int64_t ldgk,
-                         __nv_bfloat16* const gv, const int64_t ldgv) {
+                         const __grid_constant__ CUtensorMap map_v, const Problem p, const float2* const stats, float* const parts, const int splits,
+                         __nv_bfloat16* const gk, const int64_t ldgk, __nv_bfloat16* const gv, const int64_t ldgv) {
     using namespace bwd;
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -408,7 +444,7 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 32) {
-        init(sh, C::kKeyRing, 13);                                 // an item's readers: the MMA thread, twelve warps
+        init(sh, C::kKeyRing, 15);                                 // an item's readers: the MMA thread, two menders, twelve warps
         tma_prefetch_map(&map_q);
         tma_prefetch_map(&map_go);
         tma_prefetch_map(&map_k);
@@ -419,6 +455,8 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh.tmem, t_gp = tmem + 128, t_gv = tmem + 256, t_gk = tmem + 384;
+    // an item's head is split * Hkv + key head; its query heads are those of the split
+    const int heads = p.G / splits;
     // tiles of queries that see the item's keys, of one head; tile i of the item is tile first / kRows + i % tiles of head i / tiles
     auto tiles_of_item = [](const Item& it) { return (it.end - it.begin + kRows - 1) / kRows - it.first / kRows; };
 
@@ -442,7 +480,7 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
             if (it.head < 0) break;
-            const int tiles = tiles_of_item(it), n = tiles * p.G;
+            const int tiles = tiles_of_item(it), n = tiles * heads;
             int of_head = 0;
             for (int t = 0; t < n; ++t, ++k) {
                 const bool partly = of_head == 0;                  // the tile on the diagonal
@@ -538,17 +576,22 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     if (warp == 0) {
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
-        Loader<D, C::kKeyRing> ring(smem, sh.full, sh.empty, &sh.tail, abort_flag, p.status);
+        Loader<D, C::kKeyRing> ring(smem, sh.full, sh.empty, sh.tail, abort_flag, p.status);
         int items = 0, k = 0;                                      // k: tiles of queries so far
         uint32_t phase_own = 0, phase_taken = 0;
         unsigned at = blockIdx.x;
-        for (;;) {
+        // (The first question waits for the kernel before: a CTA that started beside it would take work from SMs that are about to be free.)
+        auto ask = [&] {
             if (lane == 0) ask_for_next(&sh.answer, &sh.taken);
             __syncwarp();
-            const int slot = int(at / unsigned(p.Hkv)), kvh = int(at % unsigned(p.Hkv));       // a sequence's first keys, which most rows see, first
+        };
+        for (bool first = true;; first = false) {
+            if (!first) ask();
+            // a sequence's first keys, which most rows see, first
+            const int per = p.Hkv * splits, slot = int(at / unsigned(per)), which = int(at % unsigned(per)), split = which / p.Hkv, kvh = which - split * p.Hkv;
             const Tile t = tile_of<kRows>(p, slot);
             if (t.first >= 0) {
-                const Item it = {kvh, t.begin, t.end, t.first};
+                const Item it = {which, t.begin, t.end, t.first};
                 if (items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
                 if (ring.ok && lane == 0) {
                     sh.item[items & 1] = it;
@@ -566,7 +609,7 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                     tma_tile_load_3d(base + C::kOwn + C::kTile, &map_v, 0, it.begin + it.first, kvh * (D / 64), bar, once);
                 }
                 __syncwarp();
-                for (int h = kvh * p.G; h < (kvh + 1) * p.G && ring.ok; ++h)
+                for (int h = kvh * p.G + split * heads, h1 = h + heads; h < h1 && ring.ok; ++h)
                     for (int row = it.begin + it.first; row < it.end && ring.ok; row += kRows, ++k) {
                         float2 v[4];                               // statistics of the tile's queries; behind the end: probability 0
 #pragma unroll
@@ -584,6 +627,10 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                         __syncwarp();
                         if (lane == 0) mbar_arrive(smem_u32(&sh.stats_full[k & 1]));
                     }
+            }
+            if (first) {
+                grid_dependency_wait();
+                ask();
             }
             const bool before = ring.ok;
             ring.ok = true;
@@ -620,7 +667,7 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 const Item it = sh.item[item & 1];
                 mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
                 if (it.head < 0) break;
-                const int n = tiles_of_item(it) * p.G;
+                const int n = tiles_of_item(it) * heads;
                 wait(sh.own_full, phase_own);
                 phase_own ^= 1u;
                 auto scores = [&](int t) {
@@ -670,7 +717,22 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 at += 2 * n;
             }
         }
-    } else if (warp >= 12) {
+    } else if (warp < 4) {
+        // ---------------- queries and gradients behind a sequence's end ----------------
+        Mender<D, C::kKeyRing> mender{smem, sh.full, sh.tail, abort_flag, p.status, warp - 2};
+        for (int item = 0; mender.ok; ++item) {
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspended(smem_u32(&sh.item_full[item & 1]), uint32_t(item >> 1) & 1u, abort_flag, p.status))) break;
+            const Item it = sh.item[item & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+            if (it.head < 0) break;
+            for (int h = 0; h < heads; ++h)
+                for (int row = it.begin + it.first; row < it.end; row += kRows) {
+                    mender.next(it.end - row);
+                    mender.next(it.end - row);
+                }
+        }
+    } else {
         // ---------------- results: thread = key ----------------
         const int quad = warp & 3;
         const uint32_t lanes = uint32_t(quad * 32) << 16;
@@ -689,22 +751,57 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             wait(sh.done, uint32_t(item) & 1u);
             if (failed) break;
             const int row0 = it.begin + it.first + quad * 32;
-            store_rows<D>(t_gv + lanes, gv + int64_t(it.head) * D, ldgv, row0, it.end, 1.0f);
-            store_rows<D>(t_gk + lanes, gk + int64_t(it.head) * D, ldgk, row0, it.end, p.scale);
+            if (splits == 1) {
+                store_rows<D>(t_gv + lanes, gv + int64_t(it.head) * D, ldgv, row0, it.end, 1.0f);
+                store_rows<D>(t_gk + lanes, gk + int64_t(it.head) * D, ldgk, row0, it.end, p.scale);
+            } else {
+                const int split = it.head / p.Hkv, ld = p.Hkv * D;
+                float* const to = parts + int64_t(2 * split) * p.M * ld + (it.head - split * p.Hkv) * D;
+                store_rows<D, true>(t_gk + lanes, to, ld, row0, it.end, p.scale);
+                store_rows<D, true>(t_gv + lanes, to + int64_t(p.M) * ld, ld, row0, it.end, 1.0f);
+            }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.read));
         }
     }
     }
+    grid_dependency_wait();                  // not done before gq is
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (warp == 2) tmem_dealloc(tmem, kTmemCols);
 }
 
+// gk and gv from the splits' sums, in their order: eight columns of a row and result per thread
 template <int D>
-static int launch(const Problem& p, const float* lse, float2* stats, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
+__global__ void __launch_bounds__(256) join_kernel(const Problem p, const float* const parts, const int splits, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv, int64_t ldgv) {
+    grid_dependency_wait();
+    const int width = p.Hkv * D, chunks = width / 8;
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, row = i / (2 * chunks);
+    const int rest = int(i - row * 2 * chunks), what = rest / chunks, c = rest - what * chunks;
+    if (row < clamped(p, 0) || row >= clamped(p, p.B)) return;     // sequences lie one behind the other
+    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
+    for (int s = 0; s < splits; ++s) {
+        const float4* from = reinterpret_cast<const float4*>(parts + (int64_t(2 * s + what) * p.M + row) * width + 8 * c);
+        const float4 x = from[0], y = from[1];
+        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+        b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+    }
+    *reinterpret_cast<uint4*>((what ? gv + row * ldgv : gk + row * ldgk) + 8 * c) = make_uint4(pack2(a.x, a.y), pack2(a.z, a.w), pack2(b.x, b.y), pack2(b.z, b.w));
+}
+
+// Half as many items again as SMs: beyond that a split costs its sums' way through memory and gains nothing.
+int key_splits(int64_t M, int64_t B, int Hkv, int G) {
+    const int64_t items = ((M + 127) / 128 + (B < M ? B : M) / 2) * Hkv;
+    int n = 1;
+    for (int d = 1; d <= G; ++d)
+        if (G % d == 0 && items * d <= 222) n = d;
+    return n;
+}
+
+template <int D>
+static int launch(const Problem& p, const float* lse, float2* stats, float* parts, int splits, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
                   int64_t ldgv, cudaStream_t s) {
     using C = bwd::Cfg<D>;
     CUtensorMap mq, mgo, mk, mv;
@@ -717,16 +814,38 @@ static int launch(const Problem& p, const float* lse, float2* stats, __nv_bfloat
     if (!rc) rc = allow_dynamic_smem(sequence_key_grad_kernel<D>, C::kBytes, configured_k);
     if (rc) return rc;
     const int64_t groups = int64_t(p.M) * p.Hq, tiles = most_tiles(p.M, p.B, bwd::kRows);
-    delta_kernel<D><<<unsigned((groups * (D / 8) + 255) / 256), 256, 0, s>>>(p, lse, stats);
+    const int64_t per_block = 4 * 256 / (D / 8);
+    delta_kernel<D><<<unsigned((groups + per_block - 1) / per_block), 256, 0, s>>>(p, lse, stats);
     if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
-    sequence_query_grad_kernel<D><<<unsigned(tiles * p.Hq), bwd::kThreads, C::kBytes, s>>>(mq, mgo, mk, mv, p, stats, gq, ldgq);
-    if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
-    sequence_key_grad_kernel<D><<<unsigned(tiles * p.Hkv), bwd::kThreads, C::kBytes, s>>>(mq, mgo, mk, mv, p, stats, gk, ldgk, gv, ldgv);
-    return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
+    // The two kernels are launched dependently: the first sets up beside the statistics, the second takes SMs as the first leaves them (a small problem
+    // has both at once).  Its CTAs start when all of the first one's have found the statistics, and leave when that one is done.
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.blockDim = dim3(bwd::kThreads, 1, 1);
+    cfg.dynamicSmemBytes = C::kBytes;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const float2* const found = stats;
+    cfg.gridDim = dim3(unsigned(tiles * p.Hq), 1, 1);
+    bool ok = cudaLaunchKernelEx(&cfg, sequence_query_grad_kernel<D>, mq, mgo, mk, mv, p, found, gq, ldgq) == cudaSuccess;
+    cfg.gridDim = dim3(unsigned(tiles * p.Hkv * splits), 1, 1);
+    ok = ok && cudaLaunchKernelEx(&cfg, sequence_key_grad_kernel<D>, mq, mgo, mk, mv, p, found, parts, splits, gk, ldgk, gv, ldgv) == cudaSuccess;
+    if (splits > 1) {
+        cfg.blockDim = dim3(256, 1, 1);
+        cfg.dynamicSmemBytes = 0;
+        cfg.gridDim = dim3(unsigned((int64_t(p.M) * p.Hkv * (D / 8) * 2 + 255) / 256), 1, 1);
+        ok = ok && cudaLaunchKernelEx(&cfg, join_kernel<D>, p, static_cast<const float*>(parts), splits, gk, ldgk, gv, ldgv) == cudaSuccess;
+    }
+    if (ok) return PATCH_OK;
+    cudaGetLastError();                      // reported here, not by the next call
+    return PATCH_ERR_CUDA;
 }
-int launch_backward(const Problem& p, int D, const float* lse, float2* stats, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
+int launch_backward(const Problem& p, int D, const float* lse, float2* stats, float* parts, int splits, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,
                     int64_t ldgv, cudaStream_t s) {
-    return D == 128 ? launch<128>(p, lse, stats, gq, ldgq, gk, ldgk, gv, ldgv, s) : launch<64>(p, lse, stats, gq, ldgq, gk, ldgk, gv, ldgv, s);
+    return D == 128 ? launch<128>(p, lse, stats, parts, splits, gq, ldgq, gk, ldgk, gv, ldgv, s) : launch<64>(p, lse, stats, parts, splits, gq, ldgq, gk, ldgk, gv, ldgv, s);
 }
 
 }  // namespace seq

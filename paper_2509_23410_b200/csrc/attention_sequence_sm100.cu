@@ -40,7 +40,7 @@ template <int D> struct Cfg {
 struct Misc {
     uint64_t full[kRing], empty[kRing];
     uint64_t q_full[2], q_empty[2], s[2], p[4], half[2], o_full[2], o_empty[2];         // p: [half of the keys][stream]
-    uint64_t item_full[2], item_empty[2], taken, tail;
+    uint64_t item_full[2], item_empty[2], taken, tail[kRing];
     alignas(16) uint4 answer;                // of the launch control
     Item item[2];
     uint32_t tmem;
@@ -64,7 +64,7 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 32) {
-        for (int i = 0; i < kRing; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); }
+        for (int i = 0; i < kRing; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); mbar_init(smem_u32(&sh.tail[i]), 1); }
         for (int x = 0; x < 2; ++x) {
             mbar_init(smem_u32(&sh.q_full[x]), 1);
             mbar_init(smem_u32(&sh.q_empty[x]), 1);
@@ -75,10 +75,9 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             mbar_init(smem_u32(&sh.o_full[x]), 1);
             mbar_init(smem_u32(&sh.o_empty[x]), 4);
             mbar_init(smem_u32(&sh.item_full[x]), 1);
-            mbar_init(smem_u32(&sh.item_empty[x]), 9);             // the MMA thread and eight softmax warps
+            mbar_init(smem_u32(&sh.item_empty[x]), 11);            // the MMA thread, two menders and eight softmax warps
         }
         mbar_init(smem_u32(&sh.taken), 1);
-        mbar_init(smem_u32(&sh.tail), 1);
         sh.abort = 0;
         mbar_init_fence();
         tma_prefetch_map(&map_q);
@@ -101,7 +100,7 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
         const int slots = int(most_tiles(p.M, p.B, kRows));
-        Loader<D, kRing> ring(smem, sh.full, sh.empty, &sh.tail, abort_flag, p.status);
+        Loader<D, kRing> ring(smem, sh.full, sh.empty, sh.tail, abort_flag, p.status);
         int items = 0;
         uint32_t used_q = 0, phase_q = 0, phase_taken = 0;                   // used_q, phase_q: bit x
         unsigned at = blockIdx.x;
@@ -238,7 +237,22 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 }
             }
         }
-    } else if (warp >= 4) {
+    } else if (warp < 4) {
+        // ---------------- values behind a sequence's end ----------------
+        Mender<D, kRing> mender{smem, sh.full, sh.tail, abort_flag, p.status, warp - 2};
+        for (int item = 0; mender.ok; ++item) {
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspended(smem_u32(&sh.item_full[item & 1]), uint32_t(item >> 1) & 1u, abort_flag, p.status))) break;
+            const Item it = sh.item[item & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.item_empty[item & 1]));
+            if (it.head < 0) break;
+            const int n = max(tiles_of_stream(it, 0), tiles_of_stream(it, 1));
+            for (int j = 0; j < n; ++j) {
+                mender.next(kKeys);
+                mender.next(it.end - it.begin - j * kKeys);
+            }
+        }
+    } else {
         // ---------------- softmax: thread = row of the stream ----------------
         const int x = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = uint32_t(quad * 32) << 16;
