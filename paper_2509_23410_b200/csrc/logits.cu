@@ -30,10 +30,11 @@ constexpr int kCandidates = 2048;
 constexpr int kCells = 32;                   // see Cells, per thread
 constexpr int kFound = 2048;                 // cells that reach the border, most often k to 1.5 k
 constexpr size_t kListBytes = kCandidates * sizeof(uint64_t) + kFound * sizeof(uint32_t);
+constexpr int kMostParts = 16;               // the same for log probabilities (more than the portable size, allowed explicitly)
 constexpr int kMaxParts = 8;                 // CTAs of a cluster that share a row
 constexpr int64_t kL2Share = 24 << 20;       // see launch_resident
 constexpr int64_t kMaxV = int64_t(1) << 20;  // a bit per element fits shared memory
-static_assert(kMost <= kThreads && kMaxParts * kMost <= kCandidates, "lists of all parts of a row fit the candidates");
+static_assert(kMost <= kThreads, "an entry for a thread");
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -178,12 +179,19 @@ __device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
     return Sums{m, a.s * fa + b.s * fb, fa * (a.t + da * a.s) + fb * (b.t + db * b.s)};
 }
 
+// Order of the alternatives: larger value first, then lower index.  A value's sort key; NaN counts as -inf, -0 as 0.
+__device__ __forceinline__ uint32_t key_of(float x) {
+    if (!(x > -INFINITY)) x = -INFINITY;
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
+}
 struct Shared {
     Sums warp[kWarps];
     Sums part;                               // of this CTA, read by the cluster
     float value[kMost];                      // see the kernels
     int id[kMost];
-    int n, n2;
+    uint32_t border;                         // of the part's alternatives
+    int n, n2, count[2];
     int scan[kWarps];
 };
 
@@ -204,28 +212,36 @@ template <int N> __device__ __forceinline__ Sums sum_of_lanes(Sums x, float c) {
     }
     return Sums{m, x.s, x.t};
 }
-// Sums of a row from those of every thread; all threads get them.  `c`: log2(e) / T.
-__device__ __forceinline__ Sums sum_up(Sums x, float c, Shared& sh, int parts) {
+// Sums of a row from those of every thread; all threads get them.  `c`: log2(e) / T.  `border` (null: none): the least of the parts' is left there; `first` >= 0: a
+// part's is the key of its largest element, shifted by this.  Where
+// a row has several parts, what they exchange may be written again only behind another barrier of the cluster.
+__device__ __forceinline__ Sums sum_up(Sums x, float c, Shared& sh, int parts, uint32_t* border = nullptr, int first = -1) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     x = sum_of_lanes<32>(x, c);
     if (lane == 0) sh.warp[warp] = x;
     __syncthreads();
     x = sum_of_lanes<kWarps>(sh.warp[lane & (kWarps - 1)], c);
+    if (first >= 0) *border = key_of(x.m) >> first;
     if (parts == 1) {
         __syncthreads();                     // sh.warp may be written again
         return x;
     }
-    if (threadIdx.x == 0) sh.part = x;
-    cluster_sync_all();
-    for (int r = 0; r < parts; ++r) {
-        const uint32_t at = map_to_rank(smem_u32(&sh.part), r);
-        Sums o;
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.m) : "r"(at));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.s) : "r"(at + 4));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.t) : "r"(at + 8));
-        x = r ? join(x, o, c) : o;
+    if (threadIdx.x == 0) {
+        sh.part = x;
+        sh.border = border ? *border : 0u;
     }
-    return x;
+    cluster_sync_all();
+    uint32_t b = 0xFFFFFFFFu;
+    x = Sums{-INFINITY, 0.0f, 0.0f};
+    if (lane < parts) {                      // a part for every lane
+        const uint32_t at = map_to_rank(smem_u32(&sh.part), lane);
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x.m) : "r"(at) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x.s) : "r"(at + 4) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x.t) : "r"(at + 8) : "memory");
+        if (border) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(b) : "r"(map_to_rank(smem_u32(&sh.border), lane)) : "memory");
+    }
+    if (border) *border = __reduce_min_sync(0xFFFFFFFFu, b);
+    return sum_of_lanes<32>(x, c);
 }
 
 // One pass over a thread's elements, COUNT vectors at a time.  HIDE: elements whose bit is set in `bits` do not count.
@@ -314,12 +330,6 @@ __device__ __forceinline__ Sums scan_row(const Row<T>& row, Batch<T>& ahead, flo
     return scan.sums();
 }
 
-// Order of the alternatives: larger value first, then lower index.  A value's sort key; NaN counts as -inf, -0 as 0.
-__device__ __forceinline__ uint32_t key_of(float x) {
-    if (!(x > -INFINITY)) x = -INFINITY;
-    const uint32_t u = __float_as_uint(x + 0.0f);
-    return u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
-}
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key); }
 __device__ __forceinline__ uint64_t candidate(uint32_t key, int index) { return (uint64_t(key) << 32) | uint32_t(~index); }
 __device__ __forceinline__ int block_sum(int n, Shared& sh) {
@@ -348,131 +358,178 @@ __device__ __forceinline__ void rank(const uint64_t* list, int n, int k, uint64_
     }
 }
 
-// The first k elements, in order, of this CTA's part of a row (which has k) -> top[k].  `best`: the largest of the thread's elements; `cells`:
-// of its batches.  All threads of the CTA; ends with a barrier.
-template <class T>
-__device__ __forceinline__ void top_of_part(const Row<T>& row, float best, const Cells& cells, int k, uint64_t* list, uint64_t* top, Shared& sh) {
-    constexpr int N = Vec<T>::N;
-    constexpr int kLowest = sizeof(T) == 2 ? 16 : 0;                      // bf16 keys differ in their high halves
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t mine = row.first < row.count ? key_of(best) >> kLowest : 0u;        // an element's key is above 0
-    uint32_t border = 0;
-    for (int bit = 31 - kLowest; bit >= 0; --bit) {
-        const uint32_t next = border | (1u << bit);
-        const int n = __syncthreads_count(mine >= next);
-        if (n >= k) border = next;
-        if (n == k) break;
+// Where candidates go: the counter and the list of the row's first CTA (cluster addresses; a row of one CTA has its own).
+struct Leader {
+    uint32_t count, list;
+    bool here;                               // this CTA: addresses of its own shared memory
+    __device__ __forceinline__ int add(int n) const {
+        int old;
+        if (here) asm volatile("atom.relaxed.cta.shared::cta.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(count), "r"(n) : "memory");
+        else asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(count), "r"(n) : "memory");
+        return old;
     }
+    __device__ __forceinline__ void put(int i, uint64_t v) const {
+        if (here) asm volatile("st.shared::cta.u64 [%0], %1;" ::"r"(list + 8u * i), "l"(v) : "memory");
+        else asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(list + 8u * i), "l"(v) : "memory");
+    }
+};
+template <class T> struct Top {
+    static constexpr int N = Vec<T>::N;
+    static constexpr int kLowest = sizeof(T) == 2 ? 16 : 0;        // bf16 keys differ in their high halves
+    const Row<T>& row;
+    int k;
+    Shared& sh;
+
     // candidates of vector v whose keys are `least` or more
-    auto look = [&](int v, uint32_t least) {
+    __device__ __forceinline__ void look(int v, uint32_t least, const Leader& to) const {
         const Vec<T> x = row.load(v);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t key = key_of(element(x, i));
             if ((key >> kLowest) >= least && v * N + i < row.V) {
-                const int at = atomicAdd(&sh.n, 1);
-                if (at < kCandidates) list[at] = candidate(key, v * N + i);
+                const int at = to.add(1);
+                if (at < kCandidates) to.put(at, candidate(key, v * N + i));
             }
         }
-    };
-    // cells that reach the border, and the short last vector
-    uint32_t* const found = reinterpret_cast<uint32_t*>(list + kCandidates);
-    if (threadIdx.x == 0) sh.n = sh.n2 = 0;
-    __syncthreads();
-    if (mine >= border && mine) {
-        const int n = (row.batches() + (1 << cells.shift) - 1) >> cells.shift;
-        for (int g = 0; g < n; ++g)
-            if ((key_of(cells.at[g * kThreads + threadIdx.x]) >> kLowest) >= border) {
-                const int at = atomicAdd(&sh.n2, 1);
-                if (at < kFound) found[at] = uint32_t(g) << 16 | threadIdx.x;
-            }
-        if (row.rest()) look(row.whole, border);
     }
-    __syncthreads();
-    int n = sh.n2;
-    auto key_of_cell = [&](uint32_t f) { return key_of(cells.at[(f >> 16) * kThreads + (f & 0xFFFFu)]) >> kLowest; };
-    if (n > 2 * k && n <= kFound) {          // the threads' bests were few for a k of this size: the k-th cell is a better border
-        uint32_t better = 0;
+    // A lower bound of the part's k-th key from the threads' bests (their keys; 0 where a thread has no element: an element's is above it).
+    __device__ __forceinline__ uint32_t border_of(uint32_t mine, int k) const {
+        uint32_t border = 0;
         for (int bit = 31 - kLowest; bit >= 0; --bit) {
-            int sum = 0;
-            for (int i = threadIdx.x; i < n; i += kThreads) sum += key_of_cell(found[i]) >= (better | (1u << bit));
-            if (block_sum(sum, sh) >= k) better |= 1u << bit;
+            const uint32_t next = border | (1u << bit);
+            const int n = __syncthreads_count(mine >= next);
+            if (n >= k) border = next;
+            if (n == k) break;
         }
-        border = max(border, better);
+        return border;
     }
-    if (n <= kFound) {
-        const int each = kAhead << cells.shift;                    // vectors of a cell
-        for (int i = threadIdx.x; i < n * each; i += kThreads) {
-            const uint32_t f = found[i / each];
-            const int v = row.first - int(threadIdx.x) + int(f & 0xFFFFu) + (int(f >> 16) * each + i % each) * row.step;
-            if (v < row.whole && key_of_cell(f) >= border) look(v, border);
-        }
-    }
-    __syncthreads();
-    const bool few = n <= kFound && sh.n <= kCandidates;
-    n = sh.n;
-    __syncthreads();
-    if (few) {
-        rank(list, n, k, top);
+    // The part's candidates from `border` on, all parts' together k or more; a count above kCandidates says that there were too many.
+    __device__ __forceinline__ void candidates(uint32_t mine, uint32_t border, const Cells& cells, uint32_t* found, const Leader& to) const {
+        if (threadIdx.x == 0) sh.n2 = 0;
         __syncthreads();
-        return;
-    }
-    // Many elements at the border.  The k-th key itself: the border where fewer than k lie above it, else by bisection over the row.
-    auto count = [&](uint32_t least) {
-        int sum = 0;
-        for (int v = row.first; v < row.count; v += row.step) {
-            const Vec<T> x = row.load(v);
-#pragma unroll
-            for (int i = 0; i < N; ++i) sum += (key_of(element(x, i)) >> kLowest) >= least && v * N + i < row.V;
+        // cells that reach the border, and the short last vector
+        if (mine >= border && mine) {
+            const int n = (row.batches() + (1 << cells.shift) - 1) >> cells.shift;
+            for (int g = 0; g < n; ++g)
+                if ((key_of(cells.at[g * kThreads + threadIdx.x]) >> kLowest) >= border) {
+                    const int at = atomicAdd(&sh.n2, 1);
+                    if (at < kFound) found[at] = uint32_t(g) << 16 | threadIdx.x;
+                }
+            if (row.rest()) look(row.whole, border, to);
         }
-        return block_sum(sum, sh);
-    };
-    if (count(border + 1) >= k) {
-        border = 0;
+        __syncthreads();
+        const int n = sh.n2;
+        if (n > kFound) {
+            if (threadIdx.x == 0) to.add(kCandidates + 1);
+            return;
+        }
+        auto key_of_cell = [&](uint32_t f) { return key_of(cells.at[(f >> 16) * kThreads + (f & 0xFFFFu)]) >> kLowest; };
+        if (n > 2 * k + 64) {                // the threads' bests were few for a k of this size: the k-th cell is a better border
+            uint32_t better = 0;
+            for (int bit = 31 - kLowest; bit >= 0; --bit) {
+                int sum = 0;
+                for (int i = threadIdx.x; i < n; i += kThreads) sum += key_of_cell(found[i]) >= (better | (1u << bit));
+                if (block_sum(sum, sh) >= k) better |= 1u << bit;
+            }
+            border = max(border, better);
+        }
+        const int log2_each = 2 + cells.shift;                     // vectors of a cell
+        static_assert(kAhead == 4, "a power of two");
+        for (int i = threadIdx.x; i < n << log2_each; i += kThreads) {
+            const uint32_t f = found[i >> log2_each];
+            const int v = row.first - int(threadIdx.x) + int(f & 0xFFFFu) + (int(f >> 16 << log2_each) + (i & ((1 << log2_each) - 1))) * row.step;
+            if (v < row.whole && key_of_cell(f) >= border) look(v, border, to);
+        }
+    }
+    // Keeps of `list` [n] what lies at or above its k-th value, in any order, where comparing each with each would take longer than a bisection (some hundred).
+    __device__ __forceinline__ int fewer(uint64_t* list, int n) const {
+        constexpr int kEach = kCandidates / kThreads;
+        if (n <= 256 || n <= k + k / 8) return n;
+        uint64_t own[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) own[i] = int(threadIdx.x) + i * kThreads < n ? list[threadIdx.x + i * kThreads] : 0ull;
+        uint32_t border = 0;
+        for (int bit = 31; bit >= kLowest; --bit) {
+            const uint32_t next = border | (1u << bit);
+            int sum = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) sum += uint32_t(own[i] >> 32) >= next;
+            if (block_sum(sum, sh) >= k) border = next;
+        }
+        if (threadIdx.x == 0) sh.n = 0;
+        __syncthreads();                     // everybody has its own in registers
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (own[i] && uint32_t(own[i] >> 32) >= border) list[atomicAdd(&sh.n, 1)] = own[i];
+        __syncthreads();
+        return sh.n;
+    }
+    // The part's first k elements, in order, to `top`, where thousands lie at the border: the k-th key by bisection over the row, what is above it, and the
+    // first ones that equal it.
+    __device__ __forceinline__ void exact(uint64_t* list, uint64_t* top) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        const Leader here = {smem_u32(&sh.n), smem_u32(list), true};
+        auto count = [&](uint32_t least) {
+            int sum = 0;
+            for (int v = row.first; v < row.count; v += row.step) {
+                const Vec<T> x = row.load(v);
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum += (key_of(element(x, i)) >> kLowest) >= least && v * N + i < row.V;
+            }
+            return block_sum(sum, sh);
+        };
+        uint32_t border = 0;
         for (int bit = 31 - kLowest; bit >= 0; --bit)
             if (count(border | (1u << bit)) >= k) border |= 1u << bit;
-    }
-    if (threadIdx.x == 0) sh.n = 0;
-    __syncthreads();
-    for (int v = row.first; v < row.count; v += row.step) look(v, border + 1);                   // fewer than k
-    __syncthreads();
-    int have = sh.n;
-    for (int v0 = row.first - threadIdx.x; v0 < row.count && have < k; v0 += row.step) {         // and the first ones that equal it
-        const int v = v0 + threadIdx.x;
-        uint32_t equal = 0;
-        Vec<T> x;
-        if (v < row.count) {
-            x = row.load(v);
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if ((key_of(element(x, i)) >> kLowest) == border && v * N + i < row.V) equal |= 1u << i;
-        }
-        const int own = __popc(equal);
-        int before = own;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xFFFFFFFFu, before, d);
-            if (lane >= d) before += o;
-        }
-        if (lane == 31) sh.scan[warp] = before;
+        if (threadIdx.x == 0) sh.n = 0;
         __syncthreads();
-        int sum = 0;
-        before -= own;
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) before += sh.scan[w];
-            sum += sh.scan[w];
+        for (int v = row.first; v < row.count; v += row.step) look(v, border + 1, here);       // fewer than k
+        __syncthreads();
+        int have = sh.n;
+        for (int v0 = row.first - threadIdx.x; v0 < row.count && have < k; v0 += row.step) {   // and the first ones that equal it
+            const int v = v0 + threadIdx.x;
+            uint32_t equal = 0;
+            Vec<T> x;
+            if (v < row.count) {
+                x = row.load(v);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if ((key_of(element(x, i)) >> kLowest) == border && v * N + i < row.V) equal |= 1u << i;
+            }
+            const int own = __popc(equal);
+            int before = own;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xFFFFFFFFu, before, d);
+                if (lane >= d) before += o;
+            }
+            if (lane == 31) sh.scan[warp] = before;
+            __syncthreads();
+            int sum = 0;
+            before -= own;
+            for (int w = 0; w < kWarps; ++w) {
+                if (w < warp) before += sh.scan[w];
+                sum += sh.scan[w];
+            }
+            __syncthreads();
+            int at = have + before;
+            for (uint32_t todo = equal; todo && at < k; todo &= todo - 1, ++at) {
+                const int i = __ffs(todo) - 1;
+                list[at] = candidate(key_of(element(x, i)), v * N + i);
+            }
+            have += sum;
         }
         __syncthreads();
-        int at = have + before;
-        for (uint32_t todo = equal; todo && at < k; todo &= todo - 1, ++at) {
-            const int i = __ffs(todo) - 1;
-            list[at] = candidate(key_of(element(x, i)), v * N + i);
-        }
-        have += sum;
+        rank(list, min(have, k), k, top);
+        __syncthreads();
     }
-    __syncthreads();
-    rank(list, min(have, k), k, top);
-    __syncthreads();
+};
+
+// (not in line, and the row taken apart: its members would live in memory for the sake of a call that is hardly ever made)
+template <class T>
+__device__ __noinline__ void exact_top(const T* z, int V, int part, int parts, int k, Shared* sh, uint64_t* list, uint64_t* top) {
+    const Row<T> row(z, V, part, parts);
+    Top<T>{row, k, *sh}.exact(list, top);
 }
 
 struct LogProbs {
@@ -493,6 +550,10 @@ __global__ void __launch_bounds__(kThreads, kPerSm) logprobs_kernel(const T* z, 
     const Cells cells = {reinterpret_cast<float*>(list + kCandidates) + kFound, p.cell_shift};
     const int part = p.parts > 1 ? int(cluster_ctarank()) : 0;
     const int64_t rows = gridDim.x / p.parts;
+    if (TOP) {
+        if (threadIdx.x == 0) sh.count[0] = sh.count[1] = 0;
+        __syncthreads();                     // (others count here only behind the first row's barrier)
+    }
     Batch<T> ahead;
     if (int64_t m = blockIdx.x / p.parts; m < p.M) Row<T>(z + m * p.ldz, p.V, part, p.parts).fetch(ahead, 0);
     for (int64_t m = blockIdx.x / p.parts; m < p.M; m += rows) {
@@ -500,53 +561,73 @@ __global__ void __launch_bounds__(kThreads, kPerSm) logprobs_kernel(const T* z, 
         const Sums own = scan_row<T, ENTROPY, false, TOP>(row, ahead, p.c, nullptr, cells, [&](Batch<T>& x) {
             if (m + rows < p.M) Row<T>(z + (m + rows) * p.ldz, p.V, part, p.parts).fetch(x, 0);
         });
-        const Sums x = sum_up(own, p.c, sh, p.parts);
+        const Top<T> best = {row, p.k, sh};
+        uint32_t mine = 0, border = 0;
+        if (TOP) {
+            mine = row.first < row.count ? key_of(own.m) >> best.kLowest : 0u;
+            const int each = (p.k + p.parts - 1) / p.parts;        // together the parts have k elements from the least border on
+            if (each > 1) border = best.border_of(mine, each);
+        }
+        const Sums x = sum_up(own, p.c, sh, p.parts, TOP ? &border : nullptr, p.k <= p.parts ? best.kLowest : -1);
         const float base = x.m == -INFINITY ? 0.0f : x.m;
         const bool none = x.m == -INFINITY && !(x.s != x.s);      // every element is -inf: no distribution
-        const float ln = TOP || (part == 0 && threadIdx.x == 0) ? logf(x.s) : 0.0f;
-        if (part == 0 && threadIdx.x == 0) {
-            if (p.tokens) {
-                const int64_t t = p.tokens[m];
-                float y = 0.0f;
-                if (t >= p.V) {
-                    if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_SIZE);
-                } else if (t >= 0) {
-                    y = none ? -INFINITY : (as_float(row.z[t]) - base) / p.temperature - ln;
-                }
-                p.logp[m] = y;
-            }
-            if (p.lse) p.lse[m] = none ? -INFINITY : base / p.temperature + ln;
-            if (ENTROPY) p.entropy[m] = none ? 0.0f : ln - x.t / (x.s * p.temperature);
-        }
         if (TOP) {
-            top_of_part(row, own.m, cells, p.k, list, top, sh);
-            if (p.parts > 1) {
-                cluster_sync_all();
-                if (part == 0) {
-                    for (int i = threadIdx.x; i < p.parts * p.k; i += kThreads) {
+            const int turn = int((m / rows) & 1);
+            const Leader to = {part ? map_to_rank(smem_u32(&sh.count[turn]), 0) : smem_u32(&sh.count[turn]), part ? map_to_rank(smem_u32(list), 0) : smem_u32(list), part == 0};
+            if (threadIdx.x == 0) sh.count[turn ^ 1] = 0;          // (read by all before they came here)
+            best.candidates(mine, border, cells, reinterpret_cast<uint32_t*>(list + kCandidates), to);
+            if (p.parts > 1) cluster_sync_all(); else __syncthreads();
+            int n = sh.count[turn];
+            if (part) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(to.count) : "memory");
+            if (n > kCandidates) {
+                if (p.parts > 1) cluster_sync_all();               // the lists are written again
+                exact_top(row.z, p.V, part, p.parts, p.k, &sh, list, top);
+                if (p.parts > 1) {
+                    cluster_sync_all();
+                    for (int i = threadIdx.x; part == 0 && i < p.parts * p.k; i += kThreads) {
                         const int r = i / p.k;
                         uint64_t v;
                         asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(map_to_rank(smem_u32(top + (i - r * p.k)), r)) : "memory");
                         list[i] = v;
                     }
+                    cluster_sync_all();      // the others' lists have been read
+                    if (part == 0) rank(list, p.parts * p.k, p.k, top);
+                    __syncthreads();
                 }
-                cluster_sync_all();          // the others' lists have been read
-                if (part == 0) rank(list, p.parts * p.k, p.k, top);
+            } else if (part == 0) {
+                n = best.fewer(list, n);
+                rank(list, n, p.k, top);
                 __syncthreads();
             }
-            if (part == 0) {
+        }
+        if (part == 0) {
+            const float ln = TOP || threadIdx.x == 0 ? logf(x.s) : 0.0f;
+            if (TOP) {
                 for (int i = threadIdx.x; i < p.k; i += kThreads) {
                     const uint64_t v = top[i];
-                    const int id = int(~uint32_t(v));
-                    p.top_ids[m * p.k + i] = id;
+                    p.top_ids[m * p.k + i] = int(~uint32_t(v));
                     p.top_logp[m * p.k + i] = none ? -INFINITY : (value_of(uint32_t(v >> 32)) - base) / p.temperature - ln;
                 }
             }
-            __syncthreads();
-        } else if (p.parts > 1) {
-            cluster_sync_all();              // the sums have been read
+            if (threadIdx.x == 0) {
+                if (p.tokens) {
+                    const int64_t t = p.tokens[m];
+                    float y = 0.0f;
+                    if (t >= p.V) {
+                        if (p.status) atomicCAS(p.status, PATCH_OK, PATCH_ERR_SIZE);
+                    } else if (t >= 0) {
+                        y = none ? -INFINITY : (as_float(row.z[t]) - base) / p.temperature - ln;
+                    }
+                    p.logp[m] = y;
+                }
+                if (p.lse) p.lse[m] = none ? -INFINITY : base / p.temperature + ln;
+                if (ENTROPY) p.entropy[m] = none ? 0.0f : ln - x.t / (x.s * p.temperature);
+            }
         }
+        if (p.parts == 1) { if (TOP) __syncthreads(); }
+        else if (!TOP) cluster_sync_all();   // the sums have been read
     }
+    if (TOP && p.parts > 1) cluster_sync_all();                    // nobody reads from a CTA that has left
 }
 
 struct LogProbsGrad {
@@ -1007,8 +1088,7 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.entries_full[r & 1]));
-            if (!REST) continue;
-            for (int i = 0; i < chunks && ok; ++i) {
+            for (int i = 0; REST && i < chunks && ok; ++i) {
                 wait(sh.full[stage], phase);
                 T* const chunk = reinterpret_cast<T*>(smem) + stage * kChunk * N;
                 const int from = (v0 + i * kChunk) * N, count = min(kChunk, n_v - i * kChunk) * N;
@@ -1180,10 +1260,10 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(const T* z, T* g
 
 // CTAs that share a row.  Four CTAs fit an SM; a row is shared (and read by a cluster, which joins its sums in distributed shared memory) where
 // rows alone would leave SMs empty, as long as every thread keeps a few vectors.
-static int parts_of(int64_t M, int64_t vectors) {
+static int parts_of(int64_t M, int64_t vectors, int most) {
     const int64_t room = kPerSm * int64_t(sm_count());
     int parts = 1;
-    while (parts < kMaxParts && M * parts * 2 <= room && vectors >= int64_t(parts) * 2 * kThreads) parts *= 2;
+    while (parts < most && M * parts * 2 <= room && vectors >= int64_t(parts) * 2 * kThreads) parts *= 2;
     return parts;
 }
 // Parts of a row where nothing has to be joined.
@@ -1213,6 +1293,15 @@ template <class T, bool ENTROPY, bool TOP>
 static int launch_logprobs(const T* z, LogProbs p, cudaStream_t s) {
     auto kern = logprobs_kernel<T, ENTROPY, TOP>;
     size_t smem = 0;
+    if (p.parts > kMaxParts) {
+        static std::atomic<uint64_t> allowed{0};
+        const int d = current_device();
+        if (d < 0) return PATCH_ERR_CUDA;
+        if (!((allowed.load(std::memory_order_acquire) >> d) & 1u)) {
+            if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return PATCH_ERR_CUDA;
+            allowed.fetch_or(uint64_t(1) << d, std::memory_order_release);
+        }
+    }
     if (TOP) {
         const int vectors = p.V / Vec<T>::N, batches = (vectors + p.parts * kThreads * kAhead - 1) / (p.parts * kThreads * kAhead);
         p.cell_shift = Cells::shift_of(batches);
@@ -1263,7 +1352,7 @@ extern "C" int patch_token_logprobs(const void* Z, int64_t ldz, int dtype, int64
         return PATCH_ERR_ALIGN;
     if ((rc = check_device())) return rc;
     if (sm_count() <= 0) return PATCH_ERR_CUDA;
-    const int parts = parts_of(M, V / (dtype == PATCH_LOGITS_BF16 ? 8 : 4));
+    const int parts = parts_of(M, V / (dtype == PATCH_LOGITS_BF16 ? 8 : 4), k * kMostParts > kCandidates ? kMaxParts : kMostParts);       // the parts' lists fit one
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     LogProbs p = {ldz, M, int(V), k, parts, 0, 1.44269504f / temperature, temperature, tokens, logp, entropy, lse, top_logp, top_ids, status_dev};
     return dtype == PATCH_LOGITS_BF16 ? launch_logprobs<__nv_bfloat16>(Z, p, s) : launch_logprobs<float>(Z, p, s);
@@ -1391,7 +1480,7 @@ extern "C" int patch_distill_loss(const void* Z, int64_t ldz, int dtype, int64_t
     if (misaligned(loss, 4) || misaligned(stats, 4) || misaligned(gloss, 4)) return PATCH_ERR_ALIGN;
     if ((rc = check_device())) return rc;
     if (sm_count() <= 0) return PATCH_ERR_CUDA;
-    const int parts = parts_of(M, V / (dtype == PATCH_LOGITS_BF16 ? 8 : 4));
+    const int parts = parts_of(M, V / (dtype == PATCH_LOGITS_BF16 ? 8 : 4), kMaxParts);
     const Distill p = {ldz, ldg, M, int(V), K, parts, 1.44269504f / temperature, temperature, ids, t, loss, stats, gloss, status_dev};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool rest = flags & PATCH_DISTILL_REST;
