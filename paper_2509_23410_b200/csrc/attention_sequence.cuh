@@ -1,5 +1,6 @@
 // Shared by the kernels of the attention within packed sequences: the problem, and which rows a CTA owns.
 #pragma once
+#include <algorithm>
 #include "attention_tmem.cuh"
 
 namespace patch {
@@ -14,6 +15,14 @@ struct Problem {
     int* status;
 };
 
+// Key heads whose items (`items` of a head) are taken together, the largest over all sequences first: what their items read again and again (`bytes` of a head)
+// stays in L2, whose halves hold copies of what both read, and the last group has items enough, four an SM, to end together.  (gq of four
+// sequences of 2048, all 32 heads at once, 134 MB of keys and values: 226 us, three groups 200.  Groups too small for the latter: gk and
+// gv of nine sequences, 4001 tokens, 32/8 heads, 122 us, all at once 98.)
+inline int heads_at_once(int heads, int64_t bytes, int64_t items) {
+    const int64_t most = std::max((int64_t(48) << 20) / bytes, (592 + items - 1) / items), groups = most >= heads ? 1 : (heads + most - 1) / most;
+    return int((heads + groups - 1) / groups);
+}
 // Tiles of all sequences in one line: sequence b's first tile is number starts[b] / rows + b, and it has at most as many as lie before
 // the next one's first.
 struct Tile { int begin, end, first; };      // rows of the sequence; the tile's first row, counted from `begin` (-1: no tile)
@@ -40,6 +49,61 @@ __device__ __forceinline__ Tile tile_of(const Problem& p, int slot) {
     if (first >= 0 && first < t.end - t.begin) t.first = first;
     return t;
 }
+// The items in the order in which CTAs take them, those with most work first, so that no CTA begins a long one when the others are about to end.  An item's
+// work grows with the tiles up to its own (OF_KEYS: from its own to the sequence's end): with up to 128 sequences (lengths in registers, four to
+// a lane) a head's items come by their size over all sequences.  With more of them each sequence is a small part of the whole, and they come one behind
+// the other, the largest items of each first.  `heads` of them come in groups of `group` (heads_at_once).  By one warp, all lanes.
+template <int ROWS, bool OF_KEYS>
+struct Order {
+    static constexpr int kMost = 128;
+    const Problem& p;
+    const int heads, group;
+    int n[kMost / 32], most = 0;             // tiles of sequence lane + 32 i; the longest sequence's
+    __device__ __forceinline__ Order(const Problem& p_, int heads_, int group_) : p(p_), heads(heads_), group(group_) {
+#pragma unroll
+        for (int i = 0; i < kMost / 32; ++i) {
+            const int b = (threadIdx.x & 31) + 32 * i;
+            n[i] = p.B <= kMost && b < p.B ? (max(clamped(p, b + 1) - clamped(p, b), 0) + ROWS - 1) / ROWS : 0;
+            most = max(most, n[i]);
+        }
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+    }
+    // items of x or more tiles
+    __device__ __forceinline__ int items(int x) const {
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < kMost / 32; ++i) c += max(n[i] - x + 1, 0);
+        return __reduce_add_sync(0xFFFFFFFFu, c);
+    }
+    __device__ __forceinline__ Tile take(unsigned at, int& head) const {
+        const unsigned tiles = unsigned(most_tiles(p.M, p.B, ROWS)), first = at / (tiles * group) * group, here = min(unsigned(group), unsigned(heads) - first);
+        const int number = int((at - tiles * first) / here);
+        head = int(first + (at - tiles * first) % here);
+        if (p.B > kMost) return tile_of<ROWS>(p, OF_KEYS ? number : int(tiles) - 1 - number);
+        Tile t = {0, 0, -1};
+        if (number >= items(1)) return t;
+        int lo = 1, hi = most + 1, before = 0;       // items(lo) > number >= items(hi) = before
+        while (hi - lo > 1) {
+            const int x = (lo + hi) / 2, c = items(x);
+            if (c > number) lo = x;
+            else hi = x, before = c;
+        }
+        int k = number - before;                     // the k-th sequence of `lo` tiles or more
+#pragma unroll
+        for (int i = 0; i < kMost / 32; ++i) {
+            const unsigned has = __ballot_sync(0xFFFFFFFFu, n[i] >= lo);
+            if (k >= 0 && k < __popc(has)) {
+                const unsigned lane = threadIdx.x & 31, own = __ballot_sync(0xFFFFFFFFu, ((has >> lane) & 1u) && __popc(has & ((1u << lane) - 1u)) == k);
+                const int b = 32 * i + __ffs(own) - 1;
+                t.begin = clamped(p, b);
+                t.end = max(clamped(p, b + 1), t.begin);
+                t.first = (OF_KEYS ? (t.end - t.begin + ROWS - 1) / ROWS - lo : lo - 1) * ROWS;
+            }
+            k -= __popc(has);
+        }
+        return t;
+    }
+};
 // starts out of order or out of range are reported (every tile stays within the rows all the same)
 __device__ __forceinline__ void check_starts(const Problem& p, int thread, int threads) {
     if (!p.status) return;
@@ -177,8 +241,8 @@ __device__ __forceinline__ void store_rows(uint32_t t, void* to, int64_t ld, int
 }
 
 int launch_forward(const Problem& p, int D, __nv_bfloat16* o, int64_t ldo, float* lse, cudaStream_t s);
-// Into how many parts the query heads of a key head are cut for gk and gv: 1, or a divisor of the group where the items were fewer than the SMs.  By
-// the sizes alone (sequences may leave fewer tiles than M and B allow for).
+// Into how many parts the query heads of a key head are cut for gk and gv: 1, or a divisor of the group where the items were few.  By the sizes
+// alone (sequences may leave fewer tiles than M and B allow for).
 int key_splits(int64_t M, int64_t B, int Hkv, int G);
 // stats: [Hq][M] of scratch; parts: [split][2][M][Hkv][D] where there are several
 int launch_backward(const Problem& p, int D, const float* lse, float2* stats, float* parts, int splits, __nv_bfloat16* gq, int64_t ldgq, __nv_bfloat16* gk, int64_t ldgk, __nv_bfloat16* gv,

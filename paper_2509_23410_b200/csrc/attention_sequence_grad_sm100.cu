@@ -153,7 +153,8 @@ __global__ void __launch_bounds__(256) delta_kernel(const Problem p, const float
 template <int D>
 __global__ void __launch_bounds__(bwd::kThreads, 1)
 sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUtensorMap map_k,
-                           const __grid_constant__ CUtensorMap map_v, const Problem p, const float2* const stats, __nv_bfloat16* const gq, const int64_t ldgq) {
+                           const __grid_constant__ CUtensorMap map_v, const Problem p, const float2* const stats, const int group, __nv_bfloat16* const gq,
+                           const int64_t ldgq) {
     using namespace bwd;
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -259,7 +260,7 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
     if (warp == 0) {
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
-        const int slots = int(most_tiles(p.M, p.B, kRows));
+        const Order<kRows, false> order(p, p.Hq, group);
         Loader<D, C::kRing> ring(smem, sh.full, sh.empty, sh.tail, abort_flag, p.status);
         int items = 0;
         uint32_t phase_own = 0, phase_taken = 0;
@@ -272,8 +273,8 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
         for (bool first = true;; first = false) {
             if (!first) ask();
             if (at == 0) check_starts(p, lane, 32);
-            const int slot = slots - 1 - int(at / unsigned(p.Hq)), head = int(at % unsigned(p.Hq));
-            const Tile t = tile_of<kRows>(p, slot);
+            int head;
+            const Tile t = order.take(at, head);
             if (t.first >= 0) {
                 const Item it = {head, t.begin, t.end, t.first};
                 if (items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
@@ -433,7 +434,7 @@ template <int D>
 __global__ void __launch_bounds__(bwd::kThreads, 1)
 sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUtensorMap map_k,
                          const __grid_constant__ CUtensorMap map_v, const Problem p, const float2* const stats, float* const parts, const int splits,
-                         __nv_bfloat16* const gk, const int64_t ldgk, __nv_bfloat16* const gv, const int64_t ldgv) {
+                         const int group, __nv_bfloat16* const gk, const int64_t ldgk, __nv_bfloat16* const gv, const int64_t ldgv) {
     using namespace bwd;
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -577,6 +578,7 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
         Loader<D, C::kKeyRing> ring(smem, sh.full, sh.empty, sh.tail, abort_flag, p.status);
+        const Order<kRows, true> order(p, p.Hkv * splits, group);
         int items = 0, k = 0;                                      // k: tiles of queries so far
         uint32_t phase_own = 0, phase_taken = 0;
         unsigned at = blockIdx.x;
@@ -587,9 +589,9 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         };
         for (bool first = true;; first = false) {
             if (!first) ask();
-            // a sequence's first keys, which most rows see, first
-            const int per = p.Hkv * splits, slot = int(at / unsigned(per)), which = int(at % unsigned(per)), split = which / p.Hkv, kvh = which - split * p.Hkv;
-            const Tile t = tile_of<kRows>(p, slot);
+            int part;                                  // parts of a key head side by side
+            const Tile t = order.take(at, part);
+            const int kvh = part / splits, split = part - kvh * splits, which = split * p.Hkv + kvh;
             if (t.first >= 0) {
                 const Item it = {which, t.begin, t.end, t.first};
                 if (items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
@@ -791,12 +793,18 @@ __global__ void __launch_bounds__(256) join_kernel(const Problem p, const float*
     *reinterpret_cast<uint4*>((what ? gv + row * ldgv : gk + row * ldgk) + 8 * c) = make_uint4(pack2(a.x, a.y), pack2(a.z, a.w), pack2(b.x, b.y), pack2(b.z, b.w));
 }
 
-// Half as many items again as SMs: beyond that a split costs its sums' way through memory and gains nothing.
+// Enough items for every SM (up to half as many again: 300 tokens, 32/8 heads, four parts: 30 -> 26 us), and enough that the largest, which stand for a whole
+// sequence's queries, are no longer than an SM's share of the whole: with sequences of one length that is 2.2 items an SM.  Items of 8 tiles
+// need no cutting for that.  (One sequence of 8192, 40/4 heads: 2.70 -> 2.28 ms; four of 16/2 heads, 8000 tokens, D = 64: 393 -> 234 us; 4001 tokens of
+// nine with 32/8 heads, where 2.2 are reached, would lose 2 us to its sums' way through memory.)
 int key_splits(int64_t M, int64_t B, int Hkv, int G) {
-    const int64_t items = ((M + 127) / 128 + (B < M ? B : M) / 2) * Hkv;
+    if (M == 0 || B == 0) return 1;
+    const int64_t seqs = B < M ? B : M, items = ((M + 127) / 128 + seqs / 2) * Hkv, tiles = (M / seqs + 127) / 128;
     int n = 1;
-    for (int d = 1; d <= G; ++d)
-        if (G % d == 0 && items * d <= 222) n = d;
+    for (int d = 1; d <= G; ++d) {
+        if (G % d) continue;
+        if (items * d <= 222 || (items * n < 280 && tiles * G > 8 * n)) n = d;
+    }
     return n;
 }
 
@@ -829,10 +837,12 @@ static int launch(const Problem& p, const float* lse, float2* stats, float* part
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     const float2* const found = stats;
+    int at_once = heads_at_once(p.Hkv, int64_t(p.M) * D * 4, tiles * p.G);      // keys and values
     cfg.gridDim = dim3(unsigned(tiles * p.Hq), 1, 1);
-    bool ok = cudaLaunchKernelEx(&cfg, sequence_query_grad_kernel<D>, mq, mgo, mk, mv, p, found, gq, ldgq) == cudaSuccess;
+    bool ok = cudaLaunchKernelEx(&cfg, sequence_query_grad_kernel<D>, mq, mgo, mk, mv, p, found, at_once * p.G, gq, ldgq) == cudaSuccess;
+    at_once = heads_at_once(p.Hkv, int64_t(p.M) * D * 4 * p.G, tiles * splits);    // queries and their gradients
     cfg.gridDim = dim3(unsigned(tiles * p.Hkv * splits), 1, 1);
-    ok = ok && cudaLaunchKernelEx(&cfg, sequence_key_grad_kernel<D>, mq, mgo, mk, mv, p, found, parts, splits, gk, ldgk, gv, ldgv) == cudaSuccess;
+    ok = ok && cudaLaunchKernelEx(&cfg, sequence_key_grad_kernel<D>, mq, mgo, mk, mv, p, found, parts, splits, at_once * splits, gk, ldgk, gv, ldgv) == cudaSuccess;
     if (splits > 1) {
         cfg.blockDim = dim3(256, 1, 1);
         cfg.dynamicSmemBytes = 0;

@@ -53,7 +53,7 @@ static_assert(sizeof(Misc) <= 512, "fits behind the tiles");
 template <int D>
 __global__ void __launch_bounds__(fwd::kThreads, 1)
 sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Problem p,
-                        __nv_bfloat16* const o, const int64_t ldo, float* const lse) {
+                        const int group, __nv_bfloat16* const o, const int64_t ldo, float* const lse) {
     using namespace fwd;
     using C = Cfg<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -99,7 +99,7 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     if (warp == 0) {
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
-        const int slots = int(most_tiles(p.M, p.B, kRows));
+        const Order<kRows, false> order(p, p.Hq, group);
         Loader<D, kRing> ring(smem, sh.full, sh.empty, sh.tail, abort_flag, p.status);
         int items = 0;
         uint32_t used_q = 0, phase_q = 0, phase_taken = 0;                   // used_q, phase_q: bit x
@@ -108,9 +108,8 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             if (lane == 0) ask_for_next(&sh.answer, &sh.taken);
             __syncwarp();
             if (at == 0) check_starts(p, lane, 32);
-            // a sequence's last rows, which see most keys, first; heads that share keys side by side
-            const int slot = slots - 1 - int(at / unsigned(p.Hq)), head = int(at % unsigned(p.Hq));
-            const Tile t = tile_of<kRows>(p, slot);
+            int head;
+            const Tile t = order.take(at, head);
             if (t.first >= 0) {
                 const Item it = {head, t.begin, t.end, t.first};
                 if (items >= 2) ring.wait(sh.item_empty[items & 1], uint32_t((items >> 1) - 1) & 1u);
@@ -352,7 +351,7 @@ static int launch(const Problem& p, __nv_bfloat16* o, int64_t ldo, float* lse, c
     auto kern = sequence_forward_kernel<D>;
     static std::atomic<uint64_t> configured{0};
     if ((rc = allow_dynamic_smem(kern, C::kBytes, configured))) return rc;
-    kern<<<unsigned(most_tiles(p.M, p.B, fwd::kRows) * p.Hq), fwd::kThreads, C::kBytes, s>>>(mq, mk, mv, p, o, ldo, lse);
+    kern<<<unsigned(most_tiles(p.M, p.B, fwd::kRows) * p.Hq), fwd::kThreads, C::kBytes, s>>>(mq, mk, mv, p, heads_at_once(p.Hkv, int64_t(p.M) * D * 4, most_tiles(p.M, p.B, fwd::kRows) * p.G) * p.G, o, ldo, lse);
     return cudaGetLastError() == cudaSuccess ? PATCH_OK : PATCH_ERR_CUDA;
 }
 int launch_forward(const Problem& p, int D, __nv_bfloat16* o, int64_t ldo, float* lse, cudaStream_t s) {
