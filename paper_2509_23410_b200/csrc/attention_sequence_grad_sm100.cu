@@ -114,27 +114,26 @@ __device__ __forceinline__ f2 powers(f2 x) {
 
 }  // namespace bwd
 
-// (lse log2 e, delta) of every row and head, [Hq][M].  D / 8 lanes to a head of a row; a thread has four of them on their way.
+// (lse log2 e, delta) of every row and head, [Hq][M].  D / 8 lanes to a head of four rows, whose loads are on their way together and whose results fill a
+// sector of 32 bytes: bound by the reads of O and GO.
 template <int D>
 __global__ void __launch_bounds__(256) delta_kernel(const Problem p, const float* lse, float2* stats) {
-    constexpr int kLanes = D / 8, kAtOnce = 4, kGroups = 256 / kLanes;
+    constexpr int kLanes = D / 8, kRows = 4, kGroups = 256 / kLanes;
     grid_launch_dependents();                // they wait for what is written here
     const int c = threadIdx.x & (kLanes - 1);
-    const int64_t first = int64_t(blockIdx.x) * kGroups * kAtOnce + threadIdx.x / kLanes, all = int64_t(p.M) * p.Hq;
-    uint4 a[kAtOnce], b[kAtOnce];
-    float l[kAtOnce];
+    const int64_t group = int64_t(blockIdx.x) * kGroups + threadIdx.x / kLanes, row = group / p.Hq * kRows;
+    const int h = int(group % p.Hq), rows = int(min(int64_t(kRows), p.M - row));      // none or fewer behind the last row
+    uint4 a[kRows], b[kRows];
+    float l[kRows];
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-        const int64_t group = first + i * kGroups, row = group / p.Hq;
-        if (group >= all) continue;
-        const int h = int(group - row * p.Hq);
-        a[i] = *reinterpret_cast<const uint4*>(p.o + row * p.ldo + h * D + 8 * c);
-        b[i] = *reinterpret_cast<const uint4*>(p.go + row * p.ldgo + h * D + 8 * c);
-        if (c == 0) l[i] = lse[group];
+    for (int i = 0; i < kRows; ++i) {
+        if (i >= rows) continue;
+        a[i] = *reinterpret_cast<const uint4*>(p.o + (row + i) * p.ldo + h * D + 8 * c);
+        b[i] = *reinterpret_cast<const uint4*>(p.go + (row + i) * p.ldgo + h * D + 8 * c);
+        if (c == 0) l[i] = lse[(row + i) * p.Hq + h];
     }
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-        const int64_t group = first + i * kGroups, row = group / p.Hq;
+    for (int i = 0; i < kRows; ++i) {
         const uint32_t x[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, y[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
         float sum = 0.0f;
 #pragma unroll
@@ -144,7 +143,7 @@ __global__ void __launch_bounds__(256) delta_kernel(const Problem p, const float
         }
 #pragma unroll
         for (int d = kLanes / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        if (c == 0 && group < all) stats[(group - row * p.Hq) * p.M + row] = make_float2(l[i] * 1.44269504f, sum);
+        if (c == 0 && i < rows) stats[int64_t(h) * p.M + row + i] = make_float2(l[i] * 1.44269504f, sum);
     }
 }
 
@@ -821,8 +820,8 @@ static int launch(const Problem& p, const float* lse, float2* stats, float* part
     if (!rc) rc = allow_dynamic_smem(sequence_query_grad_kernel<D>, C::kBytes, configured_q);
     if (!rc) rc = allow_dynamic_smem(sequence_key_grad_kernel<D>, C::kBytes, configured_k);
     if (rc) return rc;
-    const int64_t groups = int64_t(p.M) * p.Hq, tiles = most_tiles(p.M, p.B, bwd::kRows);
-    const int64_t per_block = 4 * 256 / (D / 8);
+    const int64_t groups = (int64_t(p.M) + 3) / 4 * p.Hq, tiles = most_tiles(p.M, p.B, bwd::kRows);
+    const int64_t per_block = 256 / (D / 8);
     delta_kernel<D><<<unsigned((groups + per_block - 1) / per_block), 256, 0, s>>>(p, lse, stats);
     if (cudaGetLastError() != cudaSuccess) return PATCH_ERR_CUDA;
     // The two kernels are launched dependently: the first sets up beside the statistics, the second takes SMs as the first leaves them (a small problem

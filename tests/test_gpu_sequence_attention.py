@@ -147,6 +147,19 @@ def test_long(B, D):
     run(B, Packed([2500, 700], 4, 1, D, seed=6, scale=1.3))
 
 
+@pytest.mark.parametrize("n", [127, 128, 129, 200, 1000])
+def test_many_sequences(B, n):
+    """Items are taken by size up to a number of sequences, one sequence behind the other beyond it."""
+    lens = [(0, 1, 7, 128, 129, 260, 33)[(5 * i + i // 7) % 7] for i in range(n)]
+    run(B, Packed(lens, 2, 1, 64, seed=n, lead=3, tail=5))
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,n", [(64, 128, 128, 128), (128, 96, 48, 60), (64, 140, 70, 400)])
+def test_groups_of_heads(B, D, Hq, Hkv, n):
+    """More heads than are taken together; the last group may be smaller."""
+    run(B, Packed([(9 * i) % 53 + 200 * (i % 15 == 2) for i in range(n)], Hq, Hkv, D, seed=n))
+
+
 def test_nan_stays_in_its_sequence(B):
     x = Packed([130, 70, 200], 4, 2, 128, seed=5)
     x.q[140], x.k[150], x.v[160], x.go[170] = math.nan, math.inf, math.nan, math.nan
