@@ -697,9 +697,10 @@ enum { PATCH_DISTILL_REST = 1 };
  *   loss_dev     fp32 [M]
  *   stats_dev    NULL or fp32 [M x 2], what the gradient's own call reads
  *   gZ_dev       NULL, or the gradient of sum_m gloss[m] loss[m] in the same launch (the logits are read from HBM once): same type as
- *                Z, pitch ldg; may be Z_dev itself with the same pitch.  Rows with gloss = 0 become 0, whatever their logits
+ *                Z, pitch ldg; may be Z_dev itself with the same pitch.  Rows with gloss = 0 become 0, whatever their logits.  (The loss
+ *                beside a gradient may differ in its last bits from the loss by itself: its sums have another order.)
  *   gloss_dev    fp32 [M], NULL: all 1
- *   status_dev   PATCH_ERR_SIZE if an id is V or more (no entry then)
+ *   status_dev   PATCH_ERR_SIZE if an id is V or more (no entry then); PATCH_ERR_TIMEOUT as for the other kernels with bounded waits
  * One kernel, no workspace.
  */
 int patch_distill_loss(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int64_t V, const int32_t* ids_dev, const float* t_dev,

@@ -13,6 +13,11 @@
 //            order of the MMAs: S(t + 1) as soon as S(t) is in registers, GV(t), GK(t), GP(t + 1).  (With P^T over S^T, S(t + 1) behind GV(t): the
 //            elementwise warps waited 870 of 3140 cycles a tile for it)
 // TMEM: 512 columns in both (two of scores or one, one of GP, the accumulators).
+//
+// What bounds it: in both the chain of a tile through the elementwise warps, beside the tensor cores' part of it.  D = 128: gq 2130 cycles a tile where the products
+// take 1536, gk and gv 2800 where they take 2048; D = 64 has half the products and nearly the same times.  Four sequences of 2048, 32 heads, D = 128:
+// statistics 29 us, gq 200, gk and gv 278, 505 to 580 together as the power limit allows; 4001 tokens of nine sequences, 32/8 heads, D = 64: 8, 44, 64, 118
+// together, the largest items' length and the tiles' hidden parts.
 #include "attention_sequence.cuh"
 
 namespace patch {

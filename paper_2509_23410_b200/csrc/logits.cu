@@ -13,6 +13,11 @@
 // L2) and keeps those that reach it, k to 2 k of them in most rows.  A candidate's rank is the number of candidates before it.  Rows with thousands of
 // elements at the border (all equal, all masked) take the exact way round: the k-th key by bisection over the row, what lies above it, and
 // the first elements that equal it.
+//
+// What bounds it, with the rates measured: reads of HBM, 5.2 to 5.6 TB/s with fp32 logits and 4.7 with bf16 ones, whose element costs as many instructions for
+// half the bytes.  4095 x 128256 fp32 with the top 64 387 us; log probabilities of 8192 x 32000 bf16 110; 61 x 151936 bf16 with entropies and the top 8 13.4, one row
+// of 128256 with the top 20 11, which are latencies of the steps behind the pass.  Gradient of 4096 x 50257 bf16 158 us (5.2 TB/s read and written).  Distillation
+// with its gradient: 509 x 32000 fp32 27 us, 8192 x 128256 bf16 908 (4.6 TB/s read and written).
 #include <math.h>
 #include "patch_internal.cuh"
 #include "sm100_ptx.cuh"
@@ -1257,7 +1262,7 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(const T* z, T* g
                    g * (q_all * expf(e.x / p.temperature - lse) - e.q_all), p.parts, part, [](Batch<T>&) {});
 }
 
-// CTAs that share a row.  Four CTAs fit an SM; a row is shared (and read by a cluster, which joins its sums in distributed shared memory) where
+// CTAs that share a row.  A row is shared (and read by a cluster, which joins its sums in distributed shared memory) where
 // rows alone would leave SMs empty, as long as every thread keeps a few vectors.
 static int parts_of(int64_t M, int64_t vectors) {
     const int64_t room = kPerSm * int64_t(sm_count());
