@@ -615,7 +615,7 @@ int patch_prefix_attention(const patch_kv_cache_t* cache, const void* Q_dev, int
  * are neither read into a result nor written.  Values of a sequence are assumed finite; whatever the rows of other sequences and
  * around them hold shows in no result of it.
  *   Q_dev, O_dev  [M x Hq heads of D], pitches ldq, ldo;  K_dev, V_dev [M x Hkv heads of D], pitches ldk, ldv;  D = 64 or 128, Hq a multiple of Hkv, at
- *                 most 4096;  pitches at most 2^28
+ *                 most 4096;  pitches at most 2^28;  O overlaps no input
  *   starts_dev    int32 [B + 1], 0 <= starts[0] <= .. <= starts[B] <= M, in device memory: a captured launch follows it.  B <= 2^20
  *   lse_dev       NULL or fp32 [M x Hq], what the gradient reads
  *   status_dev    PATCH_ERR_SIZE: starts out of order or out of range (nothing out of range is read or written; results are undefined);
@@ -629,7 +629,8 @@ int patch_sequence_attention(const void* Q_dev, int64_t ldq, const void* K_dev, 
 /*
  * Gradient of patch_sequence_attention, from its inputs and results.  With p_ij = exp(scale s_ij - lse_i), delta_i = gO_i . O_i:
  *     gs_ij = scale p_ij (gO_i . v_j - delta_i),   gQ_i = sum_j gs_ij k_j,   gK_j = sum_i gs_ij q_i,   gV_j = sum_i p_ij gO_i,
- * gK and gV summed over the query heads of a key head too.  Products take p and gs rounded to bf16.
+ * gK and gV summed over the query heads of a key head too.  Products take p and gs rounded to bf16; lse is an fp32 number, so that p is off by
+ * |lse| 2^-24 of itself.
  *   gQ_dev [M x Hq heads], gK_dev, gV_dev [M x Hkv heads]: results, column ranges of one stacked gradient if wanted; they overlap no input.
  *                 Rows outside the sequences stay as they are.
  *   workspace_dev at least patch_sequence_attention_backward_workspace_size bytes, 256-byte aligned, no initialisation needed
@@ -672,7 +673,8 @@ int patch_token_logprobs(const void* Z_dev, int64_t ldz, int dtype, int64_t M, i
  *     gz_v = (1 / T) [ glogp (1[v = token] - p_v) - gentropy p_v (ln p_v + entropy) ]
  *   glogp_dev    fp32 [M] or NULL; with it tokens_dev as in the forward call (rows that do not count have no gradient from it)
  *   gentropy_dev fp32 [M] or NULL; with it entropy_dev, the forward call's
- *   lse_dev      the forward call's
+ *   lse_dev      the forward call's.  It is an fp32 number: p is off by |lse| 2^-24 of itself (a row of nothing but the type's lowest value
+ *                has an lse that says no more)
  *   gZ_dev       same type as Z; may be Z_dev itself with the same pitch.  Rows whose two factors are 0 become 0, whatever their logits.
  */
 int patch_token_logprobs_backward(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int64_t V, const int64_t* tokens_dev,
@@ -707,8 +709,8 @@ int patch_distill_loss(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int
                        int K, float temperature, int flags, float* loss_dev, float* stats_dev, const float* gloss_dev,
                        void* gZ_dev, int64_t ldg, int* status_dev, void* stream);
 
-/* The gradient by itself, for a gloss that is known only later: from the stats of the forward call.  gZ_dev is not Z_dev
- * (PATCH_ERR_SHAPE). */
+/* The gradient by itself, for a gloss that is known only later: from the stats of the forward call, with p as exact as
+ * its lse as above.  gZ_dev is not Z_dev (PATCH_ERR_SHAPE). */
 int patch_distill_loss_backward(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int64_t V, const int32_t* ids_dev,
                                 const float* t_dev, int K, float temperature, int flags, const float* stats_dev,
                                 const float* gloss_dev, void* gZ_dev, int64_t ldg, int* status_dev, void* stream);
