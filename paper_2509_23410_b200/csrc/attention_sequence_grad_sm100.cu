@@ -16,7 +16,7 @@
 //
 // What bounds it: in both the chain of a tile through the elementwise warps, beside the tensor cores' part of it.  D = 128: gq 2130 cycles a tile where the products
 // take 1536, gk and gv 2800 where they take 2048; D = 64 has half the products and nearly the same times.  Four sequences of 2048, 32 heads, D = 128:
-// statistics 29 us, gq 200, gk and gv 278, 505 to 580 together as the power limit allows; 4001 tokens of nine sequences, 32/8 heads, D = 64: 8, 44, 64, 118
+// statistics 29 us, gq 200, gk and gv 278, 505 to 580 together as the power limit allows; 4001 tokens of nine sequences, 32/8 heads, D = 64: 8, 44, 64, 115
 // together, the largest items' length and the tiles' hidden parts.
 #include "attention_sequence.cuh"
 
@@ -723,6 +723,7 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 at += 2 * n;
             }
         }
+        __syncwarp();                                              // the other lanes, in the wait for gq's kernel below, would hold this one up: one token 20 -> 16 us
     } else if (warp < 4) {
         // ---------------- queries and gradients behind a sequence's end ----------------
         Mender<D, C::kKeyRing> mender{smem, sh.full, sh.tail, abort_flag, p.status, warp - 2};
@@ -797,17 +798,18 @@ __global__ void __launch_bounds__(256) join_kernel(const Problem p, const float*
     *reinterpret_cast<uint4*>((what ? gv + row * ldgv : gk + row * ldgk) + 8 * c) = make_uint4(pack2(a.x, a.y), pack2(a.z, a.w), pack2(b.x, b.y), pack2(b.z, b.w));
 }
 
-// Enough items for every SM (up to half as many again: 300 tokens, 32/8 heads, four parts: 30 -> 26 us), and enough that the largest, which stand for a whole
-// sequence's queries, are no longer than an SM's share of the whole: with sequences of one length that is 2.2 items an SM.  Items of 8 tiles
-// need no cutting for that.  (One sequence of 8192, 40/4 heads: 2.70 -> 2.28 ms; four of 16/2 heads, 8000 tokens, D = 64: 393 -> 234 us; 4001 tokens of
-// nine with 32/8 heads, where 2.2 are reached, would lose 2 us to its sums' way through memory.)
+// Where both kernels find SMs at once, as many parts as leave it so (300 tokens of three sequences, 32/8 heads: two parts 20 us, four 23).  Otherwise enough items for
+// every SM (up to half as many again), and enough that the largest, which stand for a whole sequence's queries, are no longer than an SM's share of the
+// whole: with sequences of one length that is about two items an SM; items of 8 tiles need no cutting for that.  (One sequence of 8192, 40/4 heads: 2.70 -> 2.28
+// ms; four of 16/2 heads, 8000 tokens, D = 64: 393 -> 234 us; 4001 tokens of nine with 32/8 heads, which have two, would lose 2 us to
+// their sums' way through memory.)
 int key_splits(int64_t M, int64_t B, int Hkv, int G) {
     if (M == 0 || B == 0) return 1;
-    const int64_t seqs = B < M ? B : M, items = ((M + 127) / 128 + seqs / 2) * Hkv, tiles = (M / seqs + 127) / 128;
+    const int64_t seqs = B < M ? B : M, tiles = (M / seqs + 127) / 128, items = seqs * tiles * Hkv;
     int n = 1;
     for (int d = 1; d <= G; ++d) {
         if (G % d) continue;
-        if (items * d <= 222 || (items * n < 280 && tiles * G > 8 * n)) n = d;
+        if (items * (G + 1) <= 148 ? items * (G + d) <= 148 : items * d <= 222 || (items * n < 280 && tiles * G > 8 * n)) n = d;
     }
     return n;
 }
