@@ -1442,7 +1442,7 @@ int launch_distill(const T* z, T* g, const Distill& p, cudaStream_t s) {
     auto kern = distill_kernel<T, REST, GRAD>;
     static std::atomic<uint64_t> configured{0};
     if (REST) {
-        if (int rc = allow_dynamic_smem(kern, uint32_t(bit_words<float>(int(kMaxV), kMaxParts) * 4), configured)) return rc;
+        if (int rc = allow_dynamic_smem(kern, uint32_t(bit_words<T>(int(kMaxV), kMaxParts) * 4), configured)) return rc;
     }
     return launch_rows(kern, p.M, p.parts, smem, s, z, g, p);
 }
