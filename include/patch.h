@@ -630,7 +630,7 @@ int patch_sequence_attention(const void* Q_dev, int64_t ldq, const void* K_dev, 
  * Gradient of patch_sequence_attention, from its inputs and results.  With p_ij = exp(scale s_ij - lse_i), delta_i = gO_i . O_i:
  *     gs_ij = scale p_ij (gO_i . v_j - delta_i),   gQ_i = sum_j gs_ij k_j,   gK_j = sum_i gs_ij q_i,   gV_j = sum_i p_ij gO_i,
  * gK and gV summed over the query heads of a key head too.  Products take p and gs rounded to bf16; lse is an fp32 number, so that p is off by
- * |lse| 2^-24 of itself.
+ * |lse| 2^-23 of itself.
  *   gQ_dev [M x Hq heads], gK_dev, gV_dev [M x Hkv heads]: results, column ranges of one stacked gradient if wanted; they overlap no input.
  *                 Rows outside the sequences stay as they are.
  *   workspace_dev at least patch_sequence_attention_backward_workspace_size bytes, 256-byte aligned, no initialisation needed
@@ -673,7 +673,7 @@ int patch_token_logprobs(const void* Z_dev, int64_t ldz, int dtype, int64_t M, i
  *     gz_v = (1 / T) [ glogp (1[v = token] - p_v) - gentropy p_v (ln p_v + entropy) ]
  *   glogp_dev    fp32 [M] or NULL; with it tokens_dev as in the forward call (rows that do not count have no gradient from it)
  *   gentropy_dev fp32 [M] or NULL; with it entropy_dev, the forward call's
- *   lse_dev      the forward call's.  It is an fp32 number: p is off by |lse| 2^-24 of itself (a row of nothing but the type's lowest value
+ *   lse_dev      the forward call's.  It is an fp32 number: p is off by |lse| 2^-23 of itself (a row of nothing but the type's lowest value
  *                has an lse that says no more)
  *   gZ_dev       same type as Z; may be Z_dev itself with the same pitch.  Rows whose two factors are 0 become 0, whatever their logits.
  */
