@@ -10,9 +10,10 @@
 // Top k.  A thread's running maximum is also the best of the thread's elements, so the pass over the row pays nothing for them:
 // the k-th largest of the threads' bests is a lower bound of the k-th largest element, found by a bisection over the sort key with one vote
 // of the block per bit; only threads whose best reaches it can hold one of the k, and a warp reads each such thread's elements again (from
-// L2) and keeps those that reach it, k to 2 k of them in most rows.  A candidate's rank is the number of candidates before it.  Rows with thousands of
-// elements at the border (all equal, all masked) take the exact way round: the k-th key by bisection over the row, what lies above it, and
-// the first elements that equal it.
+// L2) and keeps those that reach it, k to 2 k of them in most rows.  For more than half as many alternatives as threads the border comes from the bests of
+// fourths of a thread's elements.  A candidate's rank is the number of candidates before it.  Rows with thousands of
+// elements at the border take the exact way round: a border that the list has room for by bisection over the row, or (all equal, all masked) the k-th key, what lies
+// above it, and the first elements that equal it.
 //
 // What bounds it, with the rates measured: reads of HBM, 5.2 to 5.6 TB/s with fp32 logits and 4.7 with bf16 ones, whose element costs as many instructions for
 // half the bytes.  4095 x 128256 fp32 with the top 64 387 us; log probabilities of 8192 x 32000 bf16 110; 61 x 151936 bf16 with entropies and the top 8 13.4, one row
@@ -32,6 +33,7 @@ constexpr int kPerSm = 3;                    // CTAs that fit an SM: 80 register
 constexpr int kAhead = 4;                    // vectors of 16 bytes that a thread has on their way together
 constexpr int kMost = 256;                   // alternatives or teacher's entries of a row, at most; kMost <= kThreads
 constexpr int kCandidates = 2048;
+constexpr int kManyOfThreads = 128;          // alternatives of a part, see border_of_cells
 constexpr int kCells = 32;                   // see Cells, per thread
 constexpr int kFound = 2048;                 // cells that reach the border, most often k to 1.5 k
 constexpr size_t kListBytes = kCandidates * sizeof(uint64_t) + kFound * sizeof(uint32_t);
@@ -407,19 +409,56 @@ template <class T> struct Top {
         }
         return border;
     }
+    // The same from the largest of every fourth of a thread's cells, four values a thread: for a k that the threads' bests are too few for (with 256 of them
+    // the border is the least, and thousands of cells reach it: 2000 x 128256 bf16, top 256, 3790 us, this way 223; top 100 146 either way, and shorter rows
+    // lose, 59 -> 66 us with 4100 columns).
+    __device__ __forceinline__ uint32_t border_of_cells(const Cells& cells, int k) const {
+        uint32_t best[4] = {0u, 0u, 0u, 0u};
+        const int n = (row.batches() + (1 << cells.shift) - 1) >> cells.shift;
+        for (int g = 0; g < n; g += 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (g + i < n) best[i] = max(best[i], key_of(cells.at[(g + i) * kThreads + threadIdx.x]) >> kLowest);
+        }
+        uint32_t border = 0;
+        for (int bit = 31 - kLowest; bit >= 0; --bit) {
+            const uint32_t next = border | (1u << bit);
+            int sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += best[i] >= next;
+            sum = block_sum(sum, sh);
+            if (sum >= k) border = next;
+            if (sum >= k && sum <= k + k / 8) break;
+        }
+        return border;
+    }
     // The part's candidates from `border` on, all parts' together k or more; a count above kCandidates says that there were too many.
     __device__ __forceinline__ void candidates(uint32_t mine, uint32_t border, const Cells& cells, uint32_t* found, const Leader& to) const {
         if (threadIdx.x == 0) sh.n2 = 0;
         __syncthreads();
         // cells that reach the border, and the short last vector
+        uint32_t reach = 0;                  // a bit per cell of the thread
         if (mine >= border && mine) {
             const int n = (row.batches() + (1 << cells.shift) - 1) >> cells.shift;
-            for (int g = 0; g < n; ++g)
-                if ((key_of(cells.at[g * kThreads + threadIdx.x]) >> kLowest) >= border) {
-                    const int at = atomicAdd(&sh.n2, 1);
-                    if (at < kFound) found[at] = uint32_t(g) << 16 | threadIdx.x;
-                }
+            static_assert(kCells <= 32, "bits");
+#pragma unroll 4
+            for (int g = 0; g < n; ++g) reach |= uint32_t((key_of(cells.at[g * kThreads + threadIdx.x]) >> kLowest) >= border) << g;
             if (row.rest()) look(row.whole, border, to);
+        }
+        __syncwarp();
+        if (__any_sync(0xFFFFFFFFu, reach != 0)) {                 // one counting for the warp: each takes as long as a look at several cells
+            const int lane = threadIdx.x & 31, own = __popc(reach);
+            int before = own;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xFFFFFFFFu, before, d);
+                if (lane >= d) before += o;
+            }
+            int at = 0;
+            if (lane == 31) at = atomicAdd(&sh.n2, before);
+            at = __shfl_sync(0xFFFFFFFFu, at, 31) + before - own;
+            for (; reach; reach &= reach - 1, ++at)
+                if (at < kFound) found[at] = uint32_t(__ffs(reach) - 1) << 16 | threadIdx.x;
         }
         __syncthreads();
         const int n = sh.n2;
@@ -468,9 +507,9 @@ template <class T> struct Top {
         __syncthreads();
         return sh.n;
     }
-    // The part's first k elements, in order, to `top`, where thousands lie at the border: the k-th key by bisection over the row, what is above it, and the
-    // first ones that equal it.
-    __device__ __forceinline__ void exact(uint64_t* list, uint64_t* top) const {
+    // The part's first k elements, in order, to `top`, where thousands reach the border: by bisection over the row a border that the list has room for, or (thousands
+    // of equal ones) the k-th key, what is above it, and the first ones that equal it.  The k-th key is known to lie between `least` and `most`.
+    __device__ __forceinline__ void exact(uint64_t* list, uint64_t* top, uint32_t least, uint32_t most) const {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const Leader here = {smem_u32(&sh.n), smem_u32(list), true};
         auto count = [&](uint32_t least) {
@@ -482,13 +521,25 @@ template <class T> struct Top {
             }
             return block_sum(sum, sh);
         };
-        uint32_t border = 0;
-        for (int bit = 31 - kLowest; bit >= 0; --bit)
-            if (count(border | (1u << bit)) >= k) border |= 1u << bit;
+        int bit = 31 - __clz(least ^ most);                        // below the first in which they differ everything is open
+        uint32_t border = bit < 0 ? least : ((least >> bit) << bit) & ~(1u << bit);
+        bool fits = false;
+        for (; bit >= 0 && !fits; --bit) {
+            const int n = count(border | (1u << bit));
+            if (n >= k) {
+                border |= 1u << bit;
+                fits = n <= kCandidates;
+            }
+        }
         if (threadIdx.x == 0) sh.n = 0;
         __syncthreads();
-        for (int v = row.first; v < row.count; v += row.step) look(v, border + 1, here);       // fewer than k
+        for (int v = row.first; v < row.count; v += row.step) look(v, fits ? border : border + 1, here);       // the latter: fewer than k
         __syncthreads();
+        if (fits) {
+            rank(list, fewer(list, sh.n), k, top);
+            __syncthreads();
+            return;
+        }
         int have = sh.n;
         for (int v0 = row.first - threadIdx.x; v0 < row.count && have < k; v0 += row.step) {   // and the first ones that equal it
             const int v = v0 + threadIdx.x;
@@ -531,9 +582,9 @@ template <class T> struct Top {
 
 // (not in line, and the row taken apart: its members would live in memory for the sake of a call that is hardly ever made)
 template <class T>
-__device__ __noinline__ void exact_top(const T* z, int V, int part, int parts, int k, Shared* sh, uint64_t* list, uint64_t* top) {
+__device__ __noinline__ void exact_top(const T* z, int V, int part, int parts, int k, Shared* sh, uint64_t* list, uint64_t* top, uint32_t least, uint32_t most) {
     const Row<T> row(z, V, part, parts);
-    Top<T>{row, k, *sh}.exact(list, top);
+    Top<T>{row, k, *sh}.exact(list, top, least, most);
 }
 
 struct LogProbs {
@@ -570,7 +621,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) logprobs_kernel(const T* z, 
         if (TOP) {
             mine = row.first < row.count ? key_of(own.m) >> best.kLowest : 0u;
             const int each = (p.k + p.parts - 1) / p.parts;        // together the parts have k elements from the least border on
-            if (each > 1) border = best.border_of(mine, each);
+            if (each > kManyOfThreads) border = best.border_of_cells(cells, each);
+            else if (each > 1) border = best.border_of(mine, each);
         }
         const Sums x = sum_up(own, p.c, sh, p.parts, TOP ? &border : nullptr, p.k <= p.parts ? best.kLowest : -1);
         const float base = x.m == -INFINITY ? 0.0f : x.m;
@@ -585,7 +637,9 @@ __global__ void __launch_bounds__(kThreads, kPerSm) logprobs_kernel(const T* z, 
             if (part) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(to.count) : "memory");
             if (n > kCandidates) {
                 if (p.parts > 1) cluster_sync_all();               // the lists are written again
-                exact_top(row.z, p.V, part, p.parts, p.k, &sh, list, top);
+                // (a part's own k-th key may lie below the row's border)
+                const uint32_t highest = ~0u >> best.kLowest;
+                exact_top(row.z, p.V, part, p.parts, p.k, &sh, list, top, p.parts == 1 ? border : 0u, p.parts == 1 ? key_of(x.m) >> best.kLowest : highest);
                 if (p.parts > 1) {
                     cluster_sync_all();
                     for (int i = threadIdx.x; part == 0 && i < p.parts * p.k; i += kThreads) {

@@ -7,7 +7,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 
-from test_gpu_logits import B, check_distill, check_forward, logits, reference, teacher  # noqa: E402, F401
+from test_gpu_logits import B, check_distill, check_forward, logits, reference, special_rows, teacher  # noqa: E402, F401
 from test_gpu_sequence_attention import Packed, run  # noqa: E402
 
 MOST = 1 << 20
@@ -21,6 +21,19 @@ def test_longest_rows(B, dtype, M):  # noqa: F811
     check_forward(B, z, 0.5, 1)
     z[0] = 2.0                                                    # a border of 2^20 equal values
     check_forward(B, z, 1.0, 200)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("k", [100, 128, 129, 200, 256])
+def test_most_alternatives_of_rows_of_one_cta(B, dtype, k):  # noqa: F811
+    """As many rows as CTAs run, or more: each is one's alone, and its threads' bests are few for so many alternatives."""
+    check_forward(B, logits(450, 70001, dtype, k), 1.0, k)
+    check_forward(B, logits(900, 4099, dtype, k, 8), 1.0, k)
+    z = torch.zeros(12 * 38, 20000, dtype=dtype, device="cuda")
+    z.view(38, 12, 20000)[:] = special_rows(20000, dtype)
+    check_forward(B, z, 1.0, k)
+    z[:, 5000:] = 1.0                                             # thousands of equal ones, the border among them or above them
+    check_forward(B, z, 1.0, k)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
