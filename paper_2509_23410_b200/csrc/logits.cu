@@ -12,8 +12,8 @@
 // of the block per bit; only threads whose best reaches it can hold one of the k, and a warp reads each such thread's elements again (from
 // L2) and keeps those that reach it, k to 2 k of them in most rows.  For more than half as many alternatives as threads the border comes from the bests of
 // fourths of a thread's elements.  A candidate's rank is the number of candidates before it.  Rows with thousands of
-// elements at the border take the exact way round: a border that the list has room for by bisection over the row, or (all equal, all masked) the k-th key, what lies
-// above it, and the first elements that equal it.
+// elements at the border take another way round: what lies above that border and the first elements that equal it (a mask that leaves 5 columns of 128256, top
+// 20: 23 us, by bisection 154), or a border that the list has room for by bisection over the row.
 //
 // What bounds it, with the rates measured: reads of HBM, 5.2 to 5.6 TB/s with fp32 logits and 4.7 with bf16 ones, whose element costs as many instructions for
 // half the bytes.  4095 x 128256 fp32 with the top 64 387 us; log probabilities of 8192 x 32000 bf16 110; 61 x 151936 bf16 with entropies and the top 8 13.4, one row
@@ -218,10 +218,9 @@ template <int N> __device__ __forceinline__ Sums sum_of_lanes(Sums x, float c) {
     }
     return Sums{m, x.s, x.t};
 }
-// Sums of a row from those of every thread; all threads get them.  `c`: log2(e) / T.  `border` (null: none): the least of the parts' is left there; `first` >= 0: a
-// part's is the key of its largest element, shifted by this.  Where
-// a row has several parts, what they exchange may be written again only behind another barrier of the cluster.
-__device__ __forceinline__ Sums sum_up(Sums x, float c, Shared& sh, int parts, uint32_t* border = nullptr, int first = -1) {
+// Sums of a row from those of every thread; all threads get them.  `c`: log2(e) / T.  `border` (null: none): the least of the parts' is left there.  `first` >= 0: the
+// part's is the key of its largest element, shifted by this, and the k-th largest of the parts' is left (k at most the parts).  Where a row has several parts, what they exchange may be written again only behind another barrier of the cluster.
+__device__ __forceinline__ Sums sum_up(Sums x, float c, Shared& sh, int parts, uint32_t* border = nullptr, int first = -1, int k = 0) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     x = sum_of_lanes<32>(x, c);
     if (lane == 0) sh.warp[warp] = x;
@@ -246,7 +245,12 @@ __device__ __forceinline__ Sums sum_up(Sums x, float c, Shared& sh, int parts, u
         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x.t) : "r"(at + 8) : "memory");
         if (border) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(b) : "r"(map_to_rank(smem_u32(&sh.border), lane)) : "memory");
     }
-    if (border) *border = __reduce_min_sync(0xFFFFFFFFu, b);
+    if (border && first < 0) *border = __reduce_min_sync(0xFFFFFFFFu, b);
+    if (border && first >= 0) {
+        int as_large = 0;                    // lanes behind the parts have nothing
+        for (int i = 0; i < parts; ++i) as_large += __shfl_sync(0xFFFFFFFFu, b, i) >= b;
+        *border = __reduce_max_sync(0xFFFFFFFFu, lane < parts && as_large >= k ? b : 0u);
+    }
     return sum_of_lanes<32>(x, c);
 }
 
@@ -469,10 +473,16 @@ template <class T> struct Top {
         auto key_of_cell = [&](uint32_t f) { return key_of(cells.at[(f >> 16) * kThreads + (f & 0xFFFFu)]) >> kLowest; };
         if (n > 2 * k + 64) {                // the threads' bests were few for a k of this size: the k-th cell is a better border
             uint32_t better = 0;
+            int reach_it = n;
             for (int bit = 31 - kLowest; bit >= 0; --bit) {
                 int sum = 0;
                 for (int i = threadIdx.x; i < n; i += kThreads) sum += key_of_cell(found[i]) >= (better | (1u << bit));
-                if (block_sum(sum, sh) >= k) better |= 1u << bit;
+                sum = block_sum(sum, sh);
+                if (sum >= k) better |= 1u << bit, reach_it = sum;
+            }
+            if (reach_it > 2 * k + 64) {     // that many at one value, as in a masked row
+                if (threadIdx.x == 0) to.add(kCandidates + 1);
+                return;
             }
             border = max(border, better);
         }
@@ -507,11 +517,20 @@ template <class T> struct Top {
         __syncthreads();
         return sh.n;
     }
-    // The part's first k elements, in order, to `top`, where thousands reach the border: by bisection over the row a border that the list has room for, or (thousands
-    // of equal ones) the k-th key, what is above it, and the first ones that equal it.  The k-th key is known to lie between `least` and `most`.
+    // The part's first k elements of those whose keys are `least` or more, in order, to `top` (0 behind them), where thousands are: what lies above `least`, if
+    // that is most of them (a masked row), else above a border that the list has room for, or above the k-th key (thousands of equal ones there too), found
+    // by bisection over the row up to `most`; and the first ones that equal it.
     __device__ __forceinline__ void exact(uint64_t* list, uint64_t* top, uint32_t least, uint32_t most) const {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const Leader here = {smem_u32(&sh.n), smem_u32(list), true};
+        auto gather = [&](uint32_t from) {
+            __syncthreads();
+            if (threadIdx.x == 0) sh.n = 0;
+            __syncthreads();
+            for (int v = row.first; v < row.count; v += row.step) look(v, from, here);
+            __syncthreads();
+            return sh.n;
+        };
         auto count = [&](uint32_t least) {
             int sum = 0;
             for (int v = row.first; v < row.count; v += row.step) {
@@ -521,26 +540,26 @@ template <class T> struct Top {
             }
             return block_sum(sum, sh);
         };
-        int bit = 31 - __clz(least ^ most);                        // below the first in which they differ everything is open
-        uint32_t border = bit < 0 ? least : ((least >> bit) << bit) & ~(1u << bit);
-        bool fits = false;
-        for (; bit >= 0 && !fits; --bit) {
-            const int n = count(border | (1u << bit));
-            if (n >= k) {
-                border |= 1u << bit;
-                fits = n <= kCandidates;
+        uint32_t border = least;
+        int have = gather(least + 1);
+        bool fits = have >= k && have <= kCandidates;
+        if (have > kCandidates) {
+            int bit = 31 - __clz(least ^ most);                    // below the first in which they differ everything is open
+            border = bit < 0 ? least : ((least >> bit) << bit) & ~(1u << bit);
+            for (; bit >= 0 && !fits; --bit) {
+                const int n = count(border | (1u << bit));
+                if (n >= k) {
+                    border |= 1u << bit;
+                    fits = n <= kCandidates;
+                }
             }
+            have = gather(fits ? border : border + 1);             // the latter: fewer than k
         }
-        if (threadIdx.x == 0) sh.n = 0;
-        __syncthreads();
-        for (int v = row.first; v < row.count; v += row.step) look(v, fits ? border : border + 1, here);       // the latter: fewer than k
-        __syncthreads();
         if (fits) {
-            rank(list, fewer(list, sh.n), k, top);
+            rank(list, fewer(list, have), k, top);
             __syncthreads();
             return;
         }
-        int have = sh.n;
         for (int v0 = row.first - threadIdx.x; v0 < row.count && have < k; v0 += row.step) {   // and the first ones that equal it
             const int v = v0 + threadIdx.x;
             uint32_t equal = 0;
@@ -575,7 +594,9 @@ template <class T> struct Top {
             have += sum;
         }
         __syncthreads();
-        rank(list, min(have, k), k, top);
+        have = min(have, k);
+        rank(list, have, k, top);
+        for (int i = have + threadIdx.x; i < k; i += kThreads) top[i] = 0ull;
         __syncthreads();
     }
 };
@@ -624,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) logprobs_kernel(const T* z, 
             if (each > kManyOfThreads) border = best.border_of_cells(cells, each);
             else if (each > 1) border = best.border_of(mine, each);
         }
-        const Sums x = sum_up(own, p.c, sh, p.parts, TOP ? &border : nullptr, p.k <= p.parts ? best.kLowest : -1);
+        const Sums x = sum_up(own, p.c, sh, p.parts, TOP ? &border : nullptr, p.k <= p.parts ? best.kLowest : -1, p.k);
         const float base = x.m == -INFINITY ? 0.0f : x.m;
         const bool none = x.m == -INFINITY && !(x.s != x.s);      // every element is -inf: no distribution
         if (TOP) {
@@ -637,9 +658,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) logprobs_kernel(const T* z, 
             if (part) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(to.count) : "memory");
             if (n > kCandidates) {
                 if (p.parts > 1) cluster_sync_all();               // the lists are written again
-                // (a part's own k-th key may lie below the row's border)
-                const uint32_t highest = ~0u >> best.kLowest;
-                exact_top(row.z, p.V, part, p.parts, p.k, &sh, list, top, p.parts == 1 ? border : 0u, p.parts == 1 ? key_of(x.m) >> best.kLowest : highest);
+                exact_top(row.z, p.V, part, p.parts, p.k, &sh, list, top, border, key_of(x.m) >> best.kLowest);
                 if (p.parts > 1) {
                     cluster_sync_all();
                     for (int i = threadIdx.x; part == 0 && i < p.parts * p.k; i += kThreads) {

@@ -37,6 +37,22 @@ def test_most_alternatives_of_rows_of_one_cta(B, dtype, k):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("mask", ["-inf", "lowest"])
+@pytest.mark.parametrize("M", [1, 13, 460])
+def test_masked_rows_with_fewer_left_than_alternatives(B, dtype, mask, M):  # noqa: F811
+    """A few columns are left of long rows, in one part of the row or in several; the others follow from the first column on."""
+    V = 40011
+    value = -math.inf if mask == "-inf" else torch.finfo(dtype).min
+    full = logits(M, V, dtype, 9)
+    for left in (1, 5, 30, 300):
+        for where in (torch.randperm(V, device="cuda")[:left], torch.arange(V - left, V, device="cuda"), torch.arange(left, device="cuda") * 8 + 4096):
+            z = torch.full((M, (V + 7) // 8 * 8), value, dtype=dtype, device="cuda")[:, :V]
+            z[:, where] = full[:, where]
+            for k in (1, 2, 20, 64, 256):
+                check_forward(B, z, 1.0, k)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("rest", [False, True])
 def test_distill_of_longest_rows(B, dtype, rest):  # noqa: F811
     for M, K in ((1, 256), (40, 3)):
