@@ -634,7 +634,7 @@ int patch_sequence_attention(const void* Q_dev, int64_t ldq, const void* K_dev, 
  *   gQ_dev [M x Hq heads], gK_dev, gV_dev [M x Hkv heads]: results, column ranges of one stacked gradient if wanted; they overlap no input.
  *                 Rows outside the sequences stay as they are.
  *   workspace_dev at least patch_sequence_attention_backward_workspace_size bytes, 256-byte aligned, no initialisation needed
- * Everything else as above.  Equal calls give equal bits (no atomics).
+ * Everything else as above (a wait that expires leaves the gradients undefined).  Equal calls give equal bits (no atomics).  Three or four launches.
  */
 int patch_sequence_attention_backward_workspace_size(int64_t M, int64_t B, int Hq, int Hkv, int D, size_t* bytes_out);
 int patch_sequence_attention_backward(const void* gO_dev, int64_t ldgo, const void* Q_dev, int64_t ldq, const void* K_dev, int64_t ldk,
