@@ -1030,21 +1030,26 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
             int stage = 0, issued = 0;
             uint32_t phase = 0;
             bool ok = true;
+#ifdef PATCH_FAULT_INJECTION
+            // test build: a status word holding kInjectMagic makes CTA 0 announce sixteen bytes more than its first stage will ever receive
+            uint32_t inject = 0u;
+            if (blockIdx.x == 0 && p.status && *p.status == kInjectMagic) {
+                inject = 16u;
+                *p.status = PATCH_OK;
+            }
+#else
+            constexpr uint32_t inject = 0u;
+#endif
             for (int64_t m = m0; m < p.M && ok; m += rows)
                 for (int i = 0; i < chunks && ok; ++i) {
                     if (issued >= kRing) ok = mbar_wait_relaxed(smem_u32(&sh.empty[stage]), phase ^ 1u, abort_flag, p.status);
                     if (!ok) break;
                     const uint32_t bytes = uint32_t(min(kChunk, n_v - i * kChunk)) * 16u, bar = smem_u32(&sh.full[stage]);
-                    mbar_expect_tx(bar, bytes);
+                    mbar_expect_tx(bar, bytes + (issued == 0 ? inject : 0u));
                     tma_bulk_load(smem_u32(smem) + uint32_t(stage) * kChunk * 16u, z + m * p.ldz + int64_t(v0 + i * kChunk) * N, bytes, bar, policy);
                     ++issued;
                     if (++stage == kRing) { stage = 0; phase ^= 1u; }
                 }
-            if (*abort_flag) {
-                const uint64_t t0 = global_timer_ns();
-                for (int j = issued > kRing ? issued - kRing : 0; j < issued; ++j)
-                    while (!mbar_try_wait(smem_u32(&sh.full[j % kRing]), uint32_t(j / kRing) & 1u) && global_timer_ns() - t0 < kDrainLimitNs) {}
-            }
         }
     } else if (warp == kWorkers / 32 + 1) {
         // ---------------- entries: lane + 32 j ----------------
@@ -1167,6 +1172,7 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
             if (lane == 0) mbar_arrive(smem_u32(&sh.entries_full[r & 1]));
             for (int i = 0; REST && i < chunks && ok; ++i) {
                 wait(sh.full[stage], phase);
+                if (!ok) break;
                 T* const chunk = reinterpret_cast<T*>(smem) + stage * kChunk * N;
                 const int from = (v0 + i * kChunk) * N, count = min(kChunk, n_v - i * kChunk) * N;
 #pragma unroll
@@ -1181,8 +1187,11 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
         }
     } else {
         // ---------------- the two passes ----------------
+        // A wait that is given up is one warp's alone (a barrier that has completed is passed whatever the others found, and warp 0 waits for the other
+        // parts by itself), so that all eight leave together: the row's barriers carry their votes, and no wait lies behind the second one.
         bool ok = true;
         auto wait = [&](uint64_t& bar, uint32_t parity) { ok = ok && mbar_wait(smem_u32(&bar), parity, abort_flag, p.status); };
+        auto given_up = [&] { return barrier_any(__any_sync(0xFFFFFFFFu, !ok), 1, kWorkers); };
         int r = 0, begin = 0;                                      // stage of the row's first chunk
         uint32_t begin_phase = 0;
         for (int64_t m = m0; m < p.M; m += rows, ++r) {
@@ -1228,7 +1237,7 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
             }
             Sums x = sum_of_lanes<32>(scan.sums(), p.c);
             if (lane == 0) sh.warp[warp] = x;
-            workers_sync();
+            if (given_up()) break;
             if (warp == 0) {                                       // one warp finishes the sums for all
                 x = sum_of_lanes<kWorkers / 32>(sh.warp[lane & (kWorkers / 32 - 1)], p.c);
                 if (p.parts > 1) {
@@ -1245,13 +1254,13 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
                         x = i ? join(x, Sums{o.x, o.y, 0.0f}, p.c) : Sums{o.x, o.y, 0.0f};
                     }
                 }
-                const RowResult f = finish_row<REST>(p, m, x, Sums{t.top, t.s, 0.0f}, t.q_sum, t.a, part == 0 && lane == 0);
+                const RowResult f = finish_row<REST>(p, m, x, Sums{t.top, t.s, 0.0f}, t.q_sum, t.a, part == 0 && lane == 0 && ok);
                 if (lane == 0) {
                     sh.result = f;
                     sh.sums = x;
                 }
             }
-            workers_sync();
+            if (given_up()) break;
             const RowResult f = sh.result;
             x = sh.sums;
             T* const to = gz + m * p.ldg;
@@ -1265,7 +1274,7 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
                 }
             };
             stage = begin;
-            for (int i = 0; i < chunks && ok; ++i) {
+            for (int i = 0; i < chunks; ++i) {
                 Vec<T> e[kEach];
                 load(e, i, stage);
                 __syncwarp();
@@ -1306,11 +1315,14 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.entries_empty[r & 1]));
-            if (!__all_sync(0xFFFFFFFFu, ok)) break;
         }
     }
     __syncthreads();
     if (p.parts > 1) cluster_sync_all();     // nobody sends to a CTA that has left
+    if (*abort_flag) {                       // what is on its way here (copies, other parts' sums) lands before this CTA has left
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < kDrainLimitNs) {}
+    }
 }
 
 template <class T, bool REST>

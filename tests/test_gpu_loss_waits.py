@@ -1,0 +1,54 @@
+"""Bounded waits of the kernels from packed sequences to a loss, made to run out in the test build (waits of 300 us; a status word tells CTA 0 to announce sixteen
+bytes more than its first stage will ever receive).  Every role of the CTA has to find its end, and so have the CTAs that wait for it: the launch is reported and ends, and the
+next one is as if nothing had been.  Nothing faults, traps or spins for ever."""
+import ctypes
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+from test_gpu_logits import B, logits, teacher  # noqa: E402, F401
+
+INJECT_MAGIC = 0x7E57
+
+
+@pytest.fixture(scope="module")
+def fi(B):  # noqa: F811
+    from paper_2509_23410_b200 import build
+    return B.load(build.build(fault_injection=True))
+
+
+def ptr(t):
+    return ctypes.c_void_p(t.data_ptr() if t is not None else 0)
+
+
+def here():
+    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype,M,V", [(F32, 1000, 16000), (F32, 1000, 32003), (BF, 450, 128256), (F32, 200, 128256), (F32, 50, 128256)])
+def test_distillation_of_rows_in_shared_memory(B, fi, dtype, M, V, rest):  # noqa: F811
+    """Rows of 1, 2, 4 and 8 CTAs, with several rows to a cluster and with one: the parts of a row wait for one another's sums."""
+    K = 40
+    z = logits(M, V, dtype, 3)
+    ids, t = teacher(z, K, 1.0, 4, M, V)
+
+    def call(lib, status):
+        loss, gz = torch.zeros(M, device="cuda"), torch.zeros(M, (V + 7) // 8 * 8, dtype=dtype, device="cuda")
+        rc = lib.patch_distill_loss(ptr(z), z.stride(0), B.LOGITS_F32 if dtype is F32 else B.LOGITS_BF16, M, V, ptr(ids), ptr(t), K, 1.0,
+                                    B.DISTILL_REST if rest else 0, ptr(loss), None, None, ptr(gz), gz.stride(0), ptr(status), here())
+        assert rc == B.OK
+        torch.cuda.synchronize()
+        return loss, gz, int(status)
+    word = lambda v: torch.full((1,), v, dtype=torch.int32, device="cuda")  # noqa: E731
+    want = call(B.lib(), word(0))
+    assert want[2] == B.OK
+    for _ in range(2):
+        got = call(fi, word(0))
+        assert got[2] == B.OK and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert call(fi, word(INJECT_MAGIC))[2] == B.ERR_TIMEOUT
+    got = call(B.lib(), word(0))
+    assert got[2] == B.OK and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
