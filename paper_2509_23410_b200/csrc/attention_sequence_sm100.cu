@@ -295,12 +295,14 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     uint32_t pr[32];
                     for (bool raised = false;; raised = true) {
                         const float sum = probabilities(t_h, left - 64 * half, partly, p.scale_log2, base_of(m), pr);
-                        if (!__any_sync(0xFFFFFFFFu, raise_maximum(sum, m, raised))) {
+                        const bool raise = raise_maximum(sum, m, raised);
+                        if (!__any_sync(0xFFFFFFFFu, raise)) {
                             l += sum;
                             break;
                         }
-                        // a higher maximum, and the scores (still in TMEM) once more: then the sum is at most the number of keys
-                        const float up = row_top(t_h, 2, left - 64 * half, m), a = up == -INFINITY ? 1.0f : ex2(exponent(m, up, p.scale_log2));
+                        // a higher maximum, and the scores (still in TMEM) once more: then the sum is at most the number of keys.  Rows that need none keep
+                        // theirs, factor 1: a row's bits are its own, whatever the warp's other rows hold, which may lie behind the sequence's end
+                        const float top = row_top(t_h, 2, left - 64 * half, m), up = raise ? top : m, a = raise ? ex2(exponent(m, up, p.scale_log2)) : 1.0f;
                         m = up;
                         l *= a;
                         if (j == 0 && half == 0) continue;
