@@ -1180,6 +1180,8 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
                     if (32 * j >= p.K) break;
                     if (id[j] >= from && id[j] < from + count) chunk[id[j] - from] = rounded<T>(-INFINITY);
                 }
+                // ordinary stores, before the bulk copy that brings the next row's chunk to the same place (through the workers' arrivals on `empty`)
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&sh.ready[stage]));
                 if (++stage == kRing) { stage = 0; phase ^= 1u; }

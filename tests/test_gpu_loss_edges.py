@@ -6,7 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
-BF = torch.bfloat16
+BF, F32 = torch.bfloat16, torch.float32
 
 from test_gpu_logits import B  # noqa: E402, F401
 
@@ -33,3 +33,24 @@ def test_rows_beside_a_sequence_leave_its_bits_alone(B, D, n):  # noqa: F811
         # (the gradients of keys are summed in as many parts as the number of sequences suggests: equal numbers of them are compared)
         assert all(torch.equal(a, b) for a, b in zip(got[0][:3], other[:3]))
     assert all(torch.equal(a, b) for first in (0, 1) for i in range(first, len(got), 2) for a, b in zip(got[first], got[i]))
+
+
+@pytest.mark.parametrize("dtype,M,V", [(F32, 1400, 16384), (BF, 1400, 32768), (BF, 300, 131072)])
+def test_listed_columns_do_not_show_in_the_rows_that_follow(B, dtype, M, V):  # noqa: F811
+    """Rows in shared memory follow one another in the same places, where the listed columns of each are overwritten: other ones in every row, in whole blocks and
+    spread.  All logits are equal, so that a -inf of another row would change a row's loss and gradient."""
+    K = 256
+    z = torch.ones(M, V, dtype=dtype, device="cuda")
+    first = (torch.arange(M, device="cuda") * 7919) % (V - 16 * K)
+    step = torch.where(torch.arange(M, device="cuda") % 2 == 0, 1, 16)
+    ids = (first[:, None] + step[:, None] * torch.arange(K, device="cuda")).int()
+    t = torch.full((M, K), math.log(0.5 / K), device="cuda")
+    for _ in range(3):
+        gz = torch.empty_like(z)
+        loss = B.patch_distill_loss(z, ids, t, rest=True, gZ=gz)
+        want = 0.5 * math.log(V) + 0.5 * math.log(V / (V - K))
+        assert float((loss - want).abs().max()) < 1e-4
+        assert len(loss.unique()) == 1                            # the same sums, whatever the list's columns
+        out = 1.0 / V - 0.5 / (V - K)                             # p (1 - q_r / p_r) and p - q
+        inside = torch.zeros(M, V, dtype=torch.bool, device="cuda").scatter_(1, ids.long(), True)
+        assert float((gz.float()[~inside] / out - 1).abs().max()) < 2.0 ** -7 and float((gz.float()[inside] / (1.0 / V - 0.5 / K) - 1).abs().max()) < 2.0 ** -7
