@@ -1190,10 +1190,10 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
     } else {
         // ---------------- the two passes ----------------
         // A wait that is given up is one warp's alone (a barrier that has completed is passed whatever the others found, and warp 0 waits for the other
-        // parts by itself), so that all eight leave together: the row's barriers carry their votes, and no wait lies behind the second one.
+        // parts by itself), so that all eight leave together: the row's second barrier carries their votes, and no wait lies behind it until
+        // the next row's.  (A vote in the first one too: 8192 x 128256 bf16 936 us instead of 924.)
         bool ok = true;
         auto wait = [&](uint64_t& bar, uint32_t parity) { ok = ok && mbar_wait(smem_u32(&bar), parity, abort_flag, p.status); };
-        auto given_up = [&] { return barrier_any(__any_sync(0xFFFFFFFFu, !ok), 1, kWorkers); };
         int r = 0, begin = 0;                                      // stage of the row's first chunk
         uint32_t begin_phase = 0;
         for (int64_t m = m0; m < p.M; m += rows, ++r) {
@@ -1239,7 +1239,7 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
             }
             Sums x = sum_of_lanes<32>(scan.sums(), p.c);
             if (lane == 0) sh.warp[warp] = x;
-            if (given_up()) break;
+            workers_sync();
             if (warp == 0) {                                       // one warp finishes the sums for all
                 x = sum_of_lanes<kWorkers / 32>(sh.warp[lane & (kWorkers / 32 - 1)], p.c);
                 if (p.parts > 1) {
@@ -1262,7 +1262,7 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
                     sh.sums = x;
                 }
             }
-            if (given_up()) break;
+            if (barrier_any(__any_sync(0xFFFFFFFFu, !ok), 1, kWorkers)) break;
             const RowResult f = sh.result;
             x = sh.sums;
             T* const to = gz + m * p.ldg;
