@@ -40,6 +40,7 @@ constexpr size_t kListBytes = kCandidates * sizeof(uint64_t) + kFound * sizeof(u
 constexpr int kMaxParts = 8;                 // CTAs of a cluster that share a row (sixteen: 16 rows of 128256 7.2 us instead of 5.6, top 20 15.3 instead of 11.4)
 constexpr int64_t kL2Share = 24 << 20;       // see launch_resident
 constexpr int64_t kMaxV = int64_t(1) << 20;  // a bit per element fits shared memory
+constexpr float kFar = -256.0f;              // an exponent from here on down is as good as -inf, 2^x is 0; factors and sums times it stay numbers
 static_assert(kMost <= kThreads && kMaxParts * kMost <= kCandidates, "an entry for a thread; lists of all parts of a row fit the candidates");
 
 __device__ __forceinline__ float ex2(float x) {
@@ -745,7 +746,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_grad_kernel(const T* z, T* 
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const float q = ex2(e[j]);
-                y[2 * i + j] = ENTROPY ? q * (a + b * fmaf(fmaxf(e[j], -1e30f), kLn2, h)) : q * a;
+                y[2 * i + j] = ENTROPY ? q * (a + b * fmaf(fmaxf(e[j], kFar), kLn2, h)) : q * a;
             }
         }
         if (v == tv) {

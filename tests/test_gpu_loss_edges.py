@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 
-from test_gpu_logits import B  # noqa: E402, F401
+from test_gpu_logits import U, B, check, ln_tol, logits, reference, rounding  # noqa: E402, F401
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -54,3 +54,19 @@ def test_listed_columns_do_not_show_in_the_rows_that_follow(B, dtype, M, V):  # 
         out = 1.0 / V - 0.5 / (V - K)                             # p (1 - q_r / p_r) and p - q
         inside = torch.zeros(M, V, dtype=torch.bool, device="cuda").scatter_(1, ids.long(), True)
         assert float((gz.float()[~inside] / out - 1).abs().max()) < 2.0 ** -7 and float((gz.float()[inside] / (1.0 / V - 0.5 / K) - 1).abs().max()) < 2.0 ** -7
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("size", [1.0, 1e6, 1e12])
+def test_entropy_gradient_of_masked_columns_is_zero_whatever_its_factor(B, dtype, size):  # noqa: F811
+    M, V, T = 5, 3001, 0.5
+    z = logits(M, V, dtype, 8)
+    z[:, 100:200], z[:, 200:300], z[2, 7:] = -math.inf, torch.finfo(dtype).min, -math.inf
+    _, ent, lse, _, _ = B.patch_token_logprobs(z, temperature=T, entropy=True, lse=True)
+    gent = torch.full((M,), size, device="cuda")
+    gz = B.patch_token_logprobs_backward(z, None, lse, entropy=ent, gentropy=gent, temperature=T)
+    assert bool((gz[:, 100:300] == 0).all()) and bool((gz[2, 7:] == 0).all())
+    lnp, p, _, h = reference(z, T)
+    want = torch.where(p > 0, -size / T * p * (torch.where(p > 0, lnp, 0.0) + h[:, None]), 0.0)
+    rel = 4 * (ln_tol(z, V, T)[:, None] + 8 * U)
+    check(gz, want, rel * size / T * p * (torch.where(p > 0, lnp, 0.0).abs() + math.log(V) + 1) + rounding(want, dtype, 1e-30 * size))
