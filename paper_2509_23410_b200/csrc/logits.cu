@@ -3,7 +3,7 @@
 // ..._backward).
 //
 // Mathematics.  With m the row's maximum and c = log2(e) / T, one pass gives S = sum 2^((x - m) c) and, for the entropy, sum 2^((x - m) c)
-// (x - m): every thread keeps a running maximum and rescales its sums when it grows (difference first, scale second, so that the largest
+// (x - m) c: every thread keeps a running maximum and rescales its sums when it grows (difference first, scale second, so that the largest
 // element's exponent is exactly 0), threads are joined by the same rule.  Sums are fp32 over some hundred elements of a thread, then over
 // a tree in a fixed order: equal calls give equal bits.
 //
@@ -40,6 +40,7 @@ constexpr size_t kListBytes = kCandidates * sizeof(uint64_t) + kFound * sizeof(u
 constexpr int kMaxParts = 8;                 // CTAs of a cluster that share a row (sixteen: 16 rows of 128256 7.2 us instead of 5.6, top 20 15.3 instead of 11.4)
 constexpr int64_t kL2Share = 24 << 20;       // see launch_resident
 constexpr int64_t kMaxV = int64_t(1) << 20;  // a bit per element fits shared memory
+constexpr float kLn2 = 0.693147180559945f;
 constexpr float kFar = -256.0f;              // an exponent from here on down is as good as -inf, 2^x is 0; factors and sums times it stay numbers
 static_assert(kMost <= kThreads && kMaxParts * kMost <= kCandidates, "an entry for a thread; lists of all parts of a row fit the candidates");
 
@@ -177,12 +178,13 @@ template <class T> struct Row {
     }
 };
 
-// maximum, sum of 2^((x - m) c), sum of that times (x - m)
+// maximum, sum of 2^((x - m) c), sum of that times (x - m) c.  (In units of the exponent: a limit below which 2^x vanishes is then one number, whatever the
+// scale of logits and temperature.)
 struct Sums { float m, s, t; };
 __device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
     if (b.m == -INFINITY) return Sums{a.m, a.s + b.s, a.t + b.t};        // nothing in b, or NaN
     if (a.m == -INFINITY) return Sums{b.m, a.s + b.s, a.t + b.t};
-    const float m = fmaxf(a.m, b.m), da = fmaxf(a.m - m, -1e30f), db = fmaxf(b.m - m, -1e30f), fa = ex2(da * c), fb = ex2(db * c);
+    const float m = fmaxf(a.m, b.m), da = fmaxf((a.m - m) * c, kFar), db = fmaxf((b.m - m) * c, kFar), fa = ex2(da), fb = ex2(db);
     return Sums{m, a.s * fa + b.s * fb, fa * (a.t + da * a.s) + fb * (b.t + db * b.s)};
 }
 
@@ -208,7 +210,7 @@ template <int N> __device__ __forceinline__ Sums sum_of_lanes(Sums x, float c) {
 #pragma unroll
     for (int d = N / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
     if (x.m > -INFINITY) {                   // else nothing, or NaN
-        const float d = fmaxf(x.m - m, -1e30f), f = ex2(d * c);
+        const float d = fmaxf((x.m - m) * c, kFar), f = ex2(d);
         x.t = f * (x.t + d * x.s);
         x.s *= f;
     }
@@ -268,7 +270,7 @@ struct Scan {
         for (int u = 1; u < COUNT; ++u) top = fmaxf(top, e[u].top());
         if (top > m) {
             if (m > -INFINITY) {
-                const float d = fmaxf(m - top, -1e30f), f = ex2(d * c);
+                const float d = fmaxf((m - top) * c, kFar), f = ex2(d);
                 if (ENTROPY) t2 = mul2(mk2(f, f), fma2(mk2(d, d), s2, t2));
                 s2 = mul2(mk2(f, f), s2);
             }
@@ -280,15 +282,11 @@ struct Scan {
         for (int u = 0; u < COUNT; ++u)
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
-                const f2 d = add2(e[u].pair(i), b2);
                 float a, b;
-                un2(mul2(d, c2), a, b);
+                un2(mul2(add2(e[u].pair(i), b2), c2), a, b);
                 const f2 p = mk2(ex2(a), ex2(b));
                 s2 = add2(s2, p);
-                if (ENTROPY) {
-                    un2(d, a, b);            // a masked element: 0 times a number, not times -inf
-                    t2 = fma2(p, mk2(fmaxf(a, -1e30f), fmaxf(b, -1e30f)), t2);
-                }
+                if (ENTROPY) t2 = fma2(p, mk2(fmaxf(a, kFar), fmaxf(b, kFar)), t2);      // a masked element: 0 times a number, not times -inf
             }
         return top;
     }
@@ -699,7 +697,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) logprobs_kernel(const T* z, 
                     p.logp[m] = y;
                 }
                 if (p.lse) p.lse[m] = none ? -INFINITY : base / p.temperature + ln;
-                if (ENTROPY) p.entropy[m] = none ? 0.0f : ln - x.t / (x.s * p.temperature);
+                if (ENTROPY) p.entropy[m] = none ? 0.0f : ln - x.t / x.s * kLn2;
             }
         }
         if (p.parts == 1) { if (TOP) __syncthreads(); }
@@ -736,7 +734,6 @@ __global__ void __launch_bounds__(kThreads) logprobs_grad_kernel(const T* z, T* 
     }
     const float base = lse * p.temperature, h = ENTROPY ? p.entropy[m] : 0.0f, a = -up;
     const int tv = token >= 0 ? int(token) / N : -1;
-    constexpr float kLn2 = 0.693147180559945f;
     auto one = [&](int v, const Vec<T>& x) {
         float y[N];
 #pragma unroll

@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 
-from test_gpu_logits import U, B, check, ln_tol, logits, reference, rounding  # noqa: E402, F401
+from test_gpu_logits import U, B, check, check_distill, check_forward, ln_tol, logits, reference, rounding, teacher  # noqa: E402, F401
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -70,3 +70,18 @@ def test_entropy_gradient_of_masked_columns_is_zero_whatever_its_factor(B, dtype
     want = torch.where(p > 0, -size / T * p * (torch.where(p > 0, lnp, 0.0) + h[:, None]), 0.0)
     rel = 4 * (ln_tol(z, V, T)[:, None] + 8 * U)
     check(gz, want, rel * size / T * p * (torch.where(p > 0, lnp, 0.0).abs() + math.log(V) + 1) + rounding(want, dtype, 1e-30 * size))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [1e-6, 1e24, 1e30, 1e33])
+@pytest.mark.parametrize("M,V", [(1, 40000), (700, 600)])
+def test_logits_and_temperatures_of_any_size(B, dtype, T, M, V):  # noqa: F811
+    """The distribution depends on z / T alone: rows of ordinary ratios at any scale, with columns masked by -inf and the type's lowest value."""
+    z = logits(M, V, dtype, 9, scale=3.0 * T)
+    z[0, 100:200] = -math.inf
+    if T < 1e28:                                                  # else the lowest value is no mask
+        z[0, 300:400] = torch.finfo(dtype).min
+    check_forward(B, z, T, 7)
+    ids, t = teacher(z, 12, T, 4, M, V)
+    for rest in (False, True):
+        check_distill(B, z, ids, t, T, rest, torch.full((M,), T, device="cuda"))        # the factor makes the gradients' size p again
