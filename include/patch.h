@@ -649,7 +649,8 @@ int patch_sequence_attention_backward(const void* gO_dev, int64_t ldgo, const vo
  * read nor written.  1 <= V <= 2^20, M < 2^31.  Arithmetic, sums and results other than gradients (which have the logits' type and are rounded
  * once) are fp32; sums are taken in an order that depends on the arguments only: equal calls give equal bits.  The distribution of a row z is
  * p = softmax(z / temperature), 0 < temperature < inf (and its reciprocal an fp32 number).  Logits of -inf are masked: probability 0,
- * gradient 0.  A row of nothing but -inf has no distribution: lse and log probabilities -inf, entropy 0, gradients 0.  NaN or +inf in a
+ * gradient 0, unless the column is the row's token, or listed with a probability: then the loss is infinite and the gradient what the formulas give
+ * with p = 0 (1 / T of glogp, - gloss q_i / T).  A row of nothing but -inf has no distribution: lse and log probabilities -inf, entropy 0, gradients 0.  NaN or +inf in a
  * row makes that row's results NaN and no other's.  The launches are ordinary ones in the sense of the section above.
  * ========================================================================================= */
 enum { PATCH_LOGITS_BF16 = 0, PATCH_LOGITS_F32 = 1 };

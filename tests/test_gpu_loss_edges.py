@@ -6,7 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
-BF, F32 = torch.bfloat16, torch.float32
+BF, F32, F64 = torch.bfloat16, torch.float32, torch.float64
 
 from test_gpu_logits import U, B, check, check_distill, check_forward, ln_tol, logits, reference, rounding, teacher  # noqa: E402, F401
 
@@ -85,3 +85,30 @@ def test_logits_and_temperatures_of_any_size(B, dtype, T, M, V):  # noqa: F811
     ids, t = teacher(z, 12, T, 4, M, V)
     for rest in (False, True):
         check_distill(B, z, ids, t, T, rest, torch.full((M,), T, device="cuda"))        # the factor makes the gradients' size p again
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [50, 40000])
+def test_masked_columns_that_are_asked_for(B, dtype, V):  # noqa: F811
+    """A masked column has no gradient unless it is the token or listed: then the loss is infinite, and the gradient is the formula's."""
+    M = 3
+    z = logits(M, V, dtype, 5)
+    z[:, 10:20] = -math.inf
+    tokens = torch.tensor([12, 3, 19], device="cuda")
+    logp, _, lse, _, _ = B.patch_token_logprobs(z, tokens, lse=True)
+    assert logp[[0, 2]].tolist() == [-math.inf] * 2 and math.isfinite(float(logp[1]))
+    glogp = torch.tensor([2.0, 2.0, 0.0], device="cuda")
+    gz = B.patch_token_logprobs_backward(z, tokens, lse, glogp)
+    assert float(gz[0, 12]) == 2.0 and bool((gz[0, [10, 11, 13, 19]] == 0).all()) and bool((gz[1, 10:20] == 0).all()) and bool((gz[2] == 0).all())
+    ids = torch.tensor([[12, 3, -1], [3, 4, 5], [15, 15, 1]], dtype=torch.int32, device="cuda")
+    t = torch.tensor([[-1.0, -2.0, 0.0], [-1.0, -2.0, -3.0], [-2.0, -1.0, -math.inf]], device="cuda")
+    for rest in (False, True):
+        q = t.double().exp() if rest else torch.softmax(t.double().masked_fill(ids < 0, -math.inf), -1)
+        stats, fused = torch.empty(M, 2, device="cuda"), torch.empty(M, (V + 7) // 8 * 8, dtype=dtype, device="cuda")[:, :V]
+        loss = B.patch_distill_loss(z, ids, t, rest=rest, stats=stats, gZ=fused)
+        assert loss[[0, 2]].tolist() == [math.inf] * 2 and math.isfinite(float(loss[1]))
+        for gz in (fused, B.patch_distill_loss_backward(z, ids, t, stats, rest=rest)):
+            assert not bool(gz.isnan().any())
+            want = torch.zeros(M, 10, dtype=F64, device="cuda")
+            want[0, 2], want[2, 5] = -q[0, 0], -q[2, :2].sum()
+            check(gz[:, 10:20], want, rounding(want, dtype) + 8 * U)
