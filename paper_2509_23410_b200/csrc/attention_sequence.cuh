@@ -129,6 +129,13 @@ __device__ __forceinline__ bool answered(const uint4* answer, unsigned& next) {
     return there != 0;
 }
 
+// Behind the CTA's last barrier, before its tensor memory goes: where a wait was given up, by whichever role, copies, answers and products may still be on their way.
+__device__ __forceinline__ void let_land(volatile int* abort_flag) {
+    if (!*abort_flag) return;
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < kDrainLimitNs) {}
+}
+
 constexpr int kTileRows = 128;               // of a tile in shared memory: [64-element half][row][128 bytes, swizzled]
 template <int D> constexpr uint32_t kTileBytes = kTileRows * D * 2;
 
@@ -160,13 +167,6 @@ struct Loader {
         __syncwarp();
         ++issued;
         if (++stage == RING) { stage = 0; phase ^= 1u; }
-    }
-    // after a failure: copies on their way end before the CTA does
-    __device__ __forceinline__ void drain() {
-        const uint64_t t0 = global_timer_ns();
-        for (int j = issued > RING ? issued - RING : 0; j < issued; ++j)
-            while (!mbar_try_wait(smem_u32(&full[j % RING]), uint32_t(j / RING) & 1u) && global_timer_ns() - t0 < kDrainLimitNs) {}
-        while (global_timer_ns() - t0 < kDrainLimitNs) {}                    // those with barriers of their own
     }
 };
 // Two warps that follow the loads, one the even and one the odd numbers, and put zeros behind a sequence's end: a probability of 0 times whatever

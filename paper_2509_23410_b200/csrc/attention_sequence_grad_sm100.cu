@@ -323,7 +323,6 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
             sh.item[items & 1].head = -1;
             mbar_arrive(smem_u32(&sh.item_full[items & 1]));
         }
-        if (*abort_flag) ring.drain();
     } else if (warp == 1) {
         // ---------------- MMAs: one thread ----------------
         if (elect_one()) {
@@ -376,7 +375,7 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                     wait(sh.gs[1], phase_gs);
                     phase_gs ^= 1u;
                     if (ok && j + 1 < n) gps(j + 1);               // (GP(j) has been read)
-                    if (j + 2 == n) mma_commit(smem_u32(&sh.own_empty));       // the last product with the item's own tiles
+                    if (j + 2 == n) mma_commit(smem_u32(&sh.own_empty));      // the last product with the item's own tiles
                     if (ok) {
                         accumulate<D>(t_gq, tmem + 128u * (j & 1), k_tile, 0, j == 0);
                         accumulate<D>(t_gq, tmem + 128u * (j & 1) + 64u, k_tile, 1, false);
@@ -429,7 +428,10 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 2) tmem_dealloc(tmem, kTmemCols);
+    if (warp == 2) {
+        let_land(abort_flag);
+        tmem_dealloc(tmem, kTmemCols);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -652,7 +654,6 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
             sh.item[items & 1].head = -1;
             mbar_arrive(smem_u32(&sh.item_full[items & 1]));
         }
-        if (*abort_flag) ring.drain();
     } else if (warp == 1) {
         // ---------------- MMAs: one thread ----------------
         if (elect_one()) {
@@ -777,7 +778,10 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 2) tmem_dealloc(tmem, kTmemCols);
+    if (warp == 2) {
+        let_land(abort_flag);
+        tmem_dealloc(tmem, kTmemCols);
+    }
 }
 
 // gk and gv from the splits' sums, in their order: eight columns of a row and result per thread

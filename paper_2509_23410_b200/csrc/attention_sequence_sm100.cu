@@ -161,7 +161,6 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             sh.item[items & 1].head = -1;
             mbar_arrive(smem_u32(&sh.item_full[items & 1]));
         }
-        if (*abort_flag) ring.drain();
     } else if (warp == 1) {
         // ---------------- MMAs: one thread ----------------
         constexpr uint32_t idesc_s = instr_desc(kKeys, false), idesc_o = instr_desc(D, false) | (1u << 16);      // V is MN-major
@@ -348,7 +347,10 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 2) tmem_dealloc(tmem, kTmemCols);
+    if (warp == 2) {
+        let_land(abort_flag);
+        tmem_dealloc(tmem, kTmemCols);
+    }
 }
 
 template <int D>
