@@ -152,6 +152,18 @@ struct Loader {
 
     __device__ __forceinline__ Loader(uint8_t* smem_, uint64_t* full_, uint64_t* empty_, uint64_t* tail_, volatile int* abort_, int* status_)
         : smem(smem_), full(full_), empty(empty_), tail(tail_), abort_flag(abort_), status(status_) {}
+#ifdef PATCH_FAULT_INJECTION
+    uint32_t inject = 0u;                    // test build: a status word holding kInjectMagic + kernel makes CTA 0 announce sixteen bytes more than its first
+    __device__ __forceinline__ void heed(int kernel) {             // stage will ever receive
+        if (blockIdx.x != 0 || !status || *status != kInjectMagic + kernel) return;
+        inject = 16u;
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) *status = PATCH_OK;
+    }
+#else
+    static constexpr uint32_t inject = 0u;
+    __device__ __forceinline__ void heed(int) {}
+#endif
     __device__ __forceinline__ void wait(uint64_t& bar, uint32_t parity) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bar), parity, abort_flag, status)) && ok;
     }
@@ -161,7 +173,7 @@ struct Loader {
         if (!ok) return;
         if ((threadIdx.x & 31) == 0) {
             const uint32_t bar = smem_u32(left < kTileRows ? &tail[stage] : &full[stage]);
-            mbar_expect_tx(bar, kTileBytes<D>);
+            mbar_expect_tx(bar, kTileBytes<D> + (issued == 0 ? inject : 0u));
             tma_tile_load_3d(smem_u32(smem) + stage * kTileBytes<D>, map, 0, row, chunk, bar, policy);
         }
         __syncwarp();

@@ -266,6 +266,7 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
         const Order<kRows, false> order(p, p.Hq, group);
         Loader<D, C::kRing> ring(smem, sh.full, sh.empty, sh.tail, abort_flag, p.status);
+        ring.heed(0);
         int items = 0;
         uint32_t phase_own = 0, phase_taken = 0;
         unsigned at = blockIdx.x;
@@ -334,8 +335,10 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                 ok = ok && mbar_wait(smem_u32(&bar), parity, abort_flag, p.status);
                 tc_fence_after();
             };
+            // (nothing after a wait given up: the producer would announce a copy to a barrier whose last one has not landed)
+            auto commit = [&](uint64_t& bar) { if (ok) mma_commit(smem_u32(&bar)); };
             auto arrived = [&](int i) { wait(sh.full[i % C::kRing], uint32_t(i / C::kRing) & 1u); return base + (i % C::kRing) * C::kTile; };
-            auto release = [&](int i) { mma_commit(smem_u32(&sh.empty[i % C::kRing])); };
+            auto release = [&](int i) { commit(sh.empty[i % C::kRing]); };
             const uint32_t q_tile = base + C::kOwn, go_tile = q_tile + C::kTile;
             for (int item = 0; ok; ++item) {
                 wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
@@ -349,18 +352,18 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                 auto scores = [&](int j) {
                     const uint32_t k_tile = arrived(at + 2 * j);
                     if (ok) product<D>(tmem + 128u * (j & 1), q_tile, k_tile);
-                    mma_commit(smem_u32(&sh.s[j & 1]));
+                    commit(sh.s[j & 1]);
                 };
                 auto gps = [&](int j) {
                     const uint32_t v_tile = arrived(at + 2 * j + 1);
                     if (ok) product<D>(t_gp, go_tile, v_tile);
-                    mma_commit(smem_u32(&sh.gp));
+                    commit(sh.gp);
                     release(at + 2 * j + 1);
                 };
                 if (ok) scores(0);
                 if (ok) gps(0);
                 if (ok && n > 1) scores(1);
-                if (n == 1) mma_commit(smem_u32(&sh.own_empty));
+                if (n == 1) commit(sh.own_empty);
 #pragma unroll 1
                 for (int j = 0; j < n && ok; ++j) {
                     const uint32_t k_tile = base + ((at + 2 * j) % C::kRing) * C::kTile;
@@ -375,13 +378,13 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                     wait(sh.gs[1], phase_gs);
                     phase_gs ^= 1u;
                     if (ok && j + 1 < n) gps(j + 1);               // (GP(j) has been read)
-                    if (j + 2 == n) mma_commit(smem_u32(&sh.own_empty));      // the last product with the item's own tiles
+                    if (j + 2 == n) commit(sh.own_empty);      // the last product with the item's own tiles
                     if (ok) {
                         accumulate<D>(t_gq, tmem + 128u * (j & 1), k_tile, 0, j == 0);
                         accumulate<D>(t_gq, tmem + 128u * (j & 1) + 64u, k_tile, 1, false);
                     }
                     release(at + 2 * j);
-                    if (j + 1 == n) mma_commit(smem_u32(&sh.done));
+                    if (j + 1 == n) commit(sh.done);
                     if (ok && j + 2 < n) scores(j + 2);
                 }
                 at += 2 * n;
@@ -584,6 +587,7 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         // ---------------- producer ----------------
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
         Loader<D, C::kKeyRing> ring(smem, sh.full, sh.empty, sh.tail, abort_flag, p.status);
+        ring.heed(1);
         const Order<kRows, true> order(p, p.Hkv * splits, group);
         int items = 0, k = 0;                                      // k: tiles of queries so far
         uint32_t phase_own = 0, phase_taken = 0;
@@ -664,9 +668,11 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 ok = ok && mbar_wait(smem_u32(&bar), parity, abort_flag, p.status);
                 tc_fence_after();
             };
+            // (nothing after a wait given up: the producer would announce a copy to a barrier whose last one has not landed)
+            auto commit = [&](uint64_t& bar) { if (ok) mma_commit(smem_u32(&bar)); };
             auto place = [&](int i) { return base + (i % C::kKeyRing) * C::kTile; };
             auto arrived = [&](int i) { wait(sh.full[i % C::kKeyRing], uint32_t(i / C::kKeyRing) & 1u); return place(i); };
-            auto release = [&](int i) { mma_commit(smem_u32(&sh.empty[i % C::kKeyRing])); };
+            auto release = [&](int i) { commit(sh.empty[i % C::kKeyRing]); };
             const uint32_t k_tile = base + C::kOwn, v_tile = k_tile + C::kTile;
             for (int item = 0; ok; ++item) {
                 wait(sh.item_full[item & 1], uint32_t(item >> 1) & 1u);
@@ -680,12 +686,12 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 auto scores = [&](int t) {
                     const uint32_t q_tile = arrived(at + 2 * t);
                     if (ok) product<D>(tmem, k_tile, q_tile);
-                    mma_commit(smem_u32(&sh.s[0]));
+                    commit(sh.s[0]);
                 };
                 auto gps = [&](int t) {
                     const uint32_t go_tile = arrived(at + 2 * t + 1);
                     if (ok) product<D>(t_gp, v_tile, go_tile);
-                    mma_commit(smem_u32(&sh.gp));
+                    commit(sh.gp);
                 };
                 if (ok) scores(0);
                 if (ok) gps(0);
@@ -707,7 +713,7 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                         wait(sh.p[half], phase_p);
                         if (ok) accumulate_from_shared<D>(t_gv, base + C::kP + half * C::kAtom, place(at + 2 * t + 1), half, t == 0 && half == 0);
                     }
-                    mma_commit(smem_u32(&sh.p_read));
+                    commit(sh.p_read);
                     release(at + 2 * t + 1);
 #pragma unroll 1
                     for (int half = 0; half < 2 && ok; ++half) {
@@ -719,8 +725,8 @@ sequence_key_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                     release(at + 2 * t);
                     if (ok && t + 1 < n) gps(t + 1);
                 }
-                mma_commit(smem_u32(&sh.own_empty));
-                mma_commit(smem_u32(&sh.done));
+                commit(sh.own_empty);
+                commit(sh.done);
                 at += 2 * n;
             }
         }

@@ -110,6 +110,7 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         const uint64_t keep = l2_policy_evict_last(), once = l2_policy_evict_first();
         const Order<kRows, false> order(p, p.Hq, group);
         Loader<D, kRing> ring(smem, sh.full, sh.empty, sh.tail, abort_flag, p.status);
+        ring.heed(0);
         int items = 0;
         uint32_t used_q = 0, phase_q = 0, phase_taken = 0;                   // used_q, phase_q: bit x
         unsigned at = blockIdx.x;
@@ -172,6 +173,8 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 ok = ok && mbar_wait(smem_u32(&bar), parity, abort_flag, p.status);
                 tc_fence_after();
             };
+            // (nothing after a wait given up: the producer would announce a copy to a barrier whose last one has not landed)
+            auto commit = [&](uint64_t& bar) { if (ok) mma_commit(smem_u32(&bar)); };
             auto advance = [&](int& s, uint32_t& ph) { if (++s == kRing) { s = 0; ph ^= 1u; } };
             auto scores = [&](int x, int k_stage) {
                 const uint64_t dq = desc_kmajor_sw128(base + C::kQ + x * C::kTile), dk = desc_kmajor_sw128(base + k_stage * C::kTile);
@@ -180,7 +183,7 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     const uint64_t off = uint64_t(((ks >> 2) * C::kAtom + (ks & 3) * 32) >> 4);
                     mma_dense(tmem + 128u * x, dq + off, dk + off, idesc_s, ks != 0);
                 }
-                mma_commit(smem_u32(&sh.s[x]));
+                commit(sh.s[x]);
             };
             auto outputs = [&](int x, int v_stage, bool first, int half) {         // of 64 keys
                 const uint64_t dv = desc_mnmajor_sw128(base + v_stage * C::kTile + half * 64 * 128, C::kAtom);
@@ -201,9 +204,9 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     wait(sh.q_full[x], (phase_q >> x) & 1u);
                     phase_q ^= 1u << x;
                     if (ok) scores(x, stage);
-                    if (n[x] == 1) mma_commit(smem_u32(&sh.q_empty[x]));
+                    if (n[x] == 1) commit(sh.q_empty[x]);
                 }
-                mma_commit(smem_u32(&sh.empty[stage]));
+                commit(sh.empty[stage]);
                 advance(stage, phase);
 #pragma unroll 1
                 for (int j = 0; j < most && ok; ++j) {
@@ -225,20 +228,20 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                         for (int half = 0; half < 2 && ok; ++half) {
                             wait(sh.p[2 * half + x], (phase_p >> x) & 1u);
                             if (ok) outputs(x, v_stage, j == 0 && half == 0, half);
-                            if (half == 0) mma_commit(smem_u32(&sh.half[x]));
+                            if (half == 0) commit(sh.half[x]);
                         }
                         phase_p ^= 1u << x;
                         if (j + 1 == n[x]) {
-                            mma_commit(smem_u32(&sh.o_full[x]));
+                            commit(sh.o_full[x]);
                         } else {
                             wait(sh.full[stage], phase);           // the same tile for both streams
                             if (ok) scores(x, stage);
-                            if (j + 2 == n[x]) mma_commit(smem_u32(&sh.q_empty[x]));
+                            if (j + 2 == n[x]) commit(sh.q_empty[x]);
                         }
                     }
-                    mma_commit(smem_u32(&sh.empty[v_stage]));
+                    commit(sh.empty[v_stage]);
                     if (more) {
-                        mma_commit(smem_u32(&sh.empty[stage]));
+                        commit(sh.empty[stage]);
                         advance(stage, phase);
                     }
                 }

@@ -10,6 +10,7 @@ pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 
 from test_gpu_logits import B, logits, teacher  # noqa: E402, F401
+from test_gpu_sequence_attention import Packed  # noqa: E402
 
 INJECT_MAGIC = 0x7E57
 
@@ -52,3 +53,41 @@ def test_distillation_of_rows_in_shared_memory(B, fi, dtype, M, V, rest):  # noq
         assert call(fi, word(INJECT_MAGIC))[2] == B.ERR_TIMEOUT
     got = call(B.lib(), word(0))
     assert got[2] == B.OK and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens,Hq,Hkv", [([1], 1, 1), ([90, 40], 2, 1), ([700, 300, 65], 4, 2), ([513, 128, 128, 300], 32, 32), ([300, 200], 48, 3)])
+def test_attention_within_sequences(B, fi, D, lens, Hq, Hkv):  # noqa: F811
+    """The forward kernel and both of the gradient; the first tile is a whole one, or one that is mended behind the sequence's end."""
+    x = Packed(lens, Hq, Hkv, D, seed=1)
+    M, n = x.M, len(lens)
+    need = B.patch_sequence_attention_backward_workspace_size(M, n, Hq, Hkv, D)
+    ld, ldo = x.q.stride(0), Hq * D
+    word = lambda v: torch.full((1,), v, dtype=torch.int32, device="cuda")  # noqa: E731
+
+    def forward(lib, status):
+        o, lse = torch.zeros(M, Hq, D, dtype=BF, device="cuda"), torch.zeros(M, Hq, device="cuda")
+        rc = lib.patch_sequence_attention(ptr(x.q), ld, ptr(x.k), ld, ptr(x.v), ld, M, Hq, Hkv, D, ptr(x.starts), n, D ** -0.5, ptr(o), ldo, ptr(lse), ptr(status),
+                                          here())
+        assert rc == B.OK
+        torch.cuda.synchronize()
+        return int(status), o, lse
+
+    def backward(lib, status, o, lse):
+        g = [torch.zeros(M, h, D, dtype=BF, device="cuda") for h in (Hq, Hkv, Hkv)]
+        ws = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+        rc = lib.patch_sequence_attention_backward(ptr(x.go), x.go.stride(0), ptr(x.q), ld, ptr(x.k), ld, ptr(x.v), ld, ptr(o), ldo, ptr(lse), M, Hq, Hkv, D, ptr(x.starts), n,
+                                                   D ** -0.5, ptr(g[0]), ldo, ptr(g[1]), Hkv * D, ptr(g[2]), Hkv * D, ptr(ws), ws.numel(), ptr(status), here())
+        assert rc == B.OK
+        torch.cuda.synchronize()
+        return int(status), *g
+    want = forward(B.lib(), word(0))
+    grads = backward(B.lib(), word(0), *want[1:])
+    same = lambda a, b: a[0] == b[0] == B.OK and all(torch.equal(u, v) for u, v in zip(a[1:], b[1:]))  # noqa: E731
+    for _ in range(2):
+        assert same(forward(fi, word(0)), want)
+        assert forward(fi, word(INJECT_MAGIC))[0] == B.ERR_TIMEOUT
+        assert same(backward(fi, word(0), *want[1:]), grads)
+        for kernel in (0, 1):                                     # of the queries, of the keys
+            assert backward(fi, word(INJECT_MAGIC + kernel), *want[1:])[0] == B.ERR_TIMEOUT
+    assert same(forward(B.lib(), word(0)), want) and same(backward(B.lib(), word(0), *want[1:]), grads)
