@@ -253,15 +253,17 @@ attn_block_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                             for (int half = 0; half < 2 && ok; ++half) {
                                 wait(bar_p + 16 * half + 8 * x, (phase_p >> x) & 1u);
                                 if (ok) outputs(x, base + v_stage * C::kTile, i < 2 && half == 0, half);
-                                if (half == 0) mma_commit(bar_h + 8 * x);
+                                if (ok && half == 0) mma_commit(bar_h + 8 * x);
                             }
                             phase_p ^= 1u << x;
-                            mma_commit(bar_empty + 8 * v_stage);
+                            if (ok) mma_commit(bar_empty + 8 * v_stage);     // (a tile that was not waited for is not the producer's to load again)
                         }
                         if (i + 2 < n) {                       // the scores of the tile that takes this one's place
                             wait(bar_full + 8 * stage, phase);
-                            if (ok) scores(x, q_tile, base + stage * C::kTile);
-                            mma_commit(bar_empty + 8 * stage);
+                            if (ok) {
+                                scores(x, q_tile, base + stage * C::kTile);
+                                mma_commit(bar_empty + 8 * stage);
+                            }
                             advance();
                         }
                     }

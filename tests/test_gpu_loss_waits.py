@@ -1,4 +1,4 @@
-"""Bounded waits of the kernels from packed sequences to a loss, made to run out in the test build (waits of 300 us; a status word tells CTA 0 to announce sixteen
+"""Bounded waits of the kernels from packed sequences to a loss (and of the block kernel behind a prefix), made to run out in the test build (waits of 300 us; a status word tells CTA 0 to announce sixteen
 bytes more than its first stage will ever receive).  Every role of the CTA has to find its end, and so have the CTAs that wait for it: the launch is reported and ends, and the
 next one is as if nothing had been.  Nothing faults, traps or spins for ever."""
 import ctypes
@@ -91,3 +91,10 @@ def test_attention_within_sequences(B, fi, D, lens, Hq, Hkv):  # noqa: F811
         for kernel in (0, 1):                                     # of the queries, of the keys
             assert backward(fi, word(INJECT_MAGIC + kernel), *want[1:])[0] == B.ERR_TIMEOUT
     assert same(forward(B.lib(), word(0)), want) and same(backward(B.lib(), word(0), *want[1:]), grads)
+
+
+@pytest.mark.parametrize("P", [120000, 262000])
+def test_attention_behind_a_long_prefix(B, P):  # noqa: F811
+    """The kernel that shares the way of a tile with them, with more tiles to a CTA than its ring holds."""
+    import test_gpu_attention_limits as limits
+    limits.test_a_wait_that_runs_out_is_reported_and_survivable(B, (40, 4, 1, P), 10000)
