@@ -181,15 +181,16 @@ struct Loader {
         if (++stage == RING) { stage = 0; phase ^= 1u; }
     }
 };
-// Two warps that follow the loads, one the even and one the odd numbers, and put zeros behind a sequence's end: a probability of 0 times whatever
-// lies there is not always 0.  (The producer itself, waiting for each such copy, held up short sequences by 3 us.)
+// A warp that follows the loads and puts zeros behind a sequence's end: a probability of 0 times whatever lies there is not always 0.  (The producer itself,
+// waiting for each such copy, held up short sequences by 3 us.)  It mends the even or the odd numbers, of the two operands of a tile: the forward kernel has one
+// for its values, the kernel of gq one for its keys, and that of gk and gv one each for queries and gradients.
 template <int D, int RING>
 struct Mender {
     uint8_t* smem;
     uint64_t *full, *tail;
     volatile int* abort_flag;
     int* status;
-    int which;                               // 0 or 1
+    const int which;                         // 0 or 1
     int number = 0;                          // of loads so far
     uint32_t phases = 0;                     // of the tail barriers, by stage
     bool ok = true;
@@ -197,7 +198,7 @@ struct Mender {
     __device__ __forceinline__ void next(int left) {
         const int i = number++, stage = i % RING;
         if (left >= kTileRows || !ok) return;
-        phases ^= 1u << stage;               // (the other warp's tiles count too)
+        phases ^= 1u << stage;               // (those of the other numbers count too: an odd ring gives a stage both)
         if ((i & 1) != which) return;
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspended(smem_u32(&tail[stage]), ~(phases >> stage) & 1u, abort_flag, status));
         if (!ok) return;

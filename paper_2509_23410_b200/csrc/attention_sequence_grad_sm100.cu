@@ -168,7 +168,7 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 32) {
-        init(sh, C::kRing, 15);                                    // an item's readers: the MMA thread, two menders, twelve warps
+        init(sh, C::kRing, 14);                                    // an item's readers: the MMA thread, the mender, twelve warps
         tma_prefetch_map(&map_q);
         tma_prefetch_map(&map_go);
         tma_prefetch_map(&map_k);
@@ -390,9 +390,9 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                 at += 2 * n;
             }
         }
-    } else if (warp < 4) {
+    } else if (warp == 2) {
         // ---------------- keys behind a sequence's end ----------------
-        Mender<D, C::kRing> mender{smem, sh.full, sh.tail, abort_flag, p.status, warp - 2};
+        Mender<D, C::kRing> mender{smem, sh.full, sh.tail, abort_flag, p.status, 0};
         for (int item = 0; mender.ok; ++item) {
             if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspended(smem_u32(&sh.item_full[item & 1]), uint32_t(item >> 1) & 1u, abort_flag, p.status))) break;
             const Item it = sh.item[item & 1];
@@ -404,7 +404,7 @@ sequence_query_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __gr
                 mender.next(kRows);
             }
         }
-    } else {
+    } else if (warp >= 4) {
         // ---------------- results: thread = row ----------------
         const int quad = warp & 3;
         bool failed = false;

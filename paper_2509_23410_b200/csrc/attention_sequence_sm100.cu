@@ -6,7 +6,7 @@
 // passes a limit.
 //   warp 0       producer: takes items, their queries and tiles of keys and values by TMA into a ring
 //   warp 1       issues the MMAs
-//   warps 2, 3   zeros over the values behind a sequence's end
+//   warp 2       zeros over the values behind a sequence's end
 //   warps 4..7   softmax and results of stream 0, one thread per row; warps 8..11 stream 1
 // Items are the CTAs of the launch: one that has started takes the place of others that have not (clusterlaunchcontrol), so that the lengths, which
 // lie in device memory, balance by themselves and the next item's queries and keys are on their way while the last one's results are written.
@@ -84,7 +84,7 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             mbar_init(smem_u32(&sh.o_full[x]), 1);
             mbar_init(smem_u32(&sh.o_empty[x]), 4);
             mbar_init(smem_u32(&sh.item_full[x]), 1);
-            mbar_init(smem_u32(&sh.item_empty[x]), 11);            // the MMA thread, two menders and eight softmax warps
+            mbar_init(smem_u32(&sh.item_empty[x]), 10);            // the MMA thread, the mender and eight softmax warps
         }
         mbar_init(smem_u32(&sh.taken), 1);
         sh.abort = 0;
@@ -247,9 +247,9 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 }
             }
         }
-    } else if (warp < 4) {
+    } else if (warp == 2) {
         // ---------------- values behind a sequence's end ----------------
-        Mender<D, kRing> mender{smem, sh.full, sh.tail, abort_flag, p.status, warp - 2};
+        Mender<D, kRing> mender{smem, sh.full, sh.tail, abort_flag, p.status, 1};
         for (int item = 0; mender.ok; ++item) {
             if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspended(smem_u32(&sh.item_full[item & 1]), uint32_t(item >> 1) & 1u, abort_flag, p.status))) break;
             const Item it = sh.item[item & 1];
@@ -262,7 +262,7 @@ sequence_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 mender.next(it.end - it.begin - j * kKeys);
             }
         }
-    } else {
+    } else if (warp >= 4) {
         // ---------------- softmax: thread = row of the stream ----------------
         const int x = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = uint32_t(quad * 32) << 16;
