@@ -15,12 +15,16 @@ struct Problem {
     int* status;
 };
 
+// SMs of the GPU that this is built for, a CTA each.  A constant, as the order of the gradient's sums goes by it (key_splits), which depends on the arguments alone, and as
+// the workspace's size is asked for without a device.
+constexpr int kSms = 148;
+
 // Key heads whose items (`items` of a head) are taken together, the largest over all sequences first: what their items read again and again (`bytes` of a head)
 // stays in L2, whose halves hold copies of what both read, and the last group has items enough, four an SM, to end together.  (gq of four
 // sequences of 2048, all 32 heads at once, 134 MB of keys and values: 226 us, three groups 200.  Groups too small for the latter: gk and
 // gv of nine sequences, 4001 tokens, 32/8 heads, 122 us, all at once 98.)
 inline int heads_at_once(int heads, int64_t bytes, int64_t items) {
-    const int64_t most = std::max((int64_t(48) << 20) / bytes, (592 + items - 1) / items), groups = most >= heads ? 1 : (heads + most - 1) / most;
+    const int64_t most = std::max((int64_t(48) << 20) / bytes, (4 * kSms + items - 1) / items), groups = most >= heads ? 1 : (heads + most - 1) / most;
     return int((heads + groups - 1) / groups);
 }
 // Tiles of all sequences in one line: sequence b's first tile is number starts[b] / rows + b, and it has at most as many as lie before

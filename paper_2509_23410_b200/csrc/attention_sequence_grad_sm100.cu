@@ -819,7 +819,7 @@ int key_splits(int64_t M, int64_t B, int Hkv, int G) {
     int n = 1;
     for (int d = 1; d <= G; ++d) {
         if (G % d) continue;
-        if (items * (G + 1) <= 148 ? items * (G + d) <= 148 : items * d <= 222 || (items * n < 280 && tiles * G > 8 * n)) n = d;
+        if (items * (G + 1) <= kSms ? items * (G + d) <= kSms : 2 * items * d <= 3 * kSms || (items * n < 2 * kSms - 16 && tiles * G > 8 * n)) n = d;
     }
     return n;
 }
