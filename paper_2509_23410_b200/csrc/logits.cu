@@ -1277,8 +1277,6 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
             for (int i = 0; i < chunks; ++i) {
                 Vec<T> e[kEach];
                 load(e, i, stage);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh.empty[stage]));
                 T* const at = to + int64_t(v0 + i * kChunk + int(threadIdx.x)) * N;
                 const int left = n_v - i * kChunk;
                 uint4 out[kEach] = {};
@@ -1298,6 +1296,11 @@ __global__ void __launch_bounds__(resident::kBlock, resident::kPerSm) distill_re
                     for (int u = 0; u < kEach; ++u)
                         if (left > u * kWorkers + int(threadIdx.x)) store16(at + u * kWorkers * N, out[u]);
                 }
+                // Behind the stores, which have the loaded values: an arrival right behind the loads overtook them where stores filled the memory unit's queue, and
+                // the next row's copy, which is not in that queue, wrote over what they had still to read (rows of 131072 columns and pitch, lines of
+                // 128 bytes in two calls of five).  917 -> 921 us of 8192 x 128256 bf16; a proxy fence instead 927
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.empty[stage]));
                 advance(stage, begin_phase);
             }
             begin = stage;

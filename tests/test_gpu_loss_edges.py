@@ -112,3 +112,21 @@ def test_masked_columns_that_are_asked_for(B, dtype, V):  # noqa: F811
             want = torch.zeros(M, 10, dtype=F64, device="cuda")
             want[0, 2], want[2, 5] = -q[0, 0], -q[2, :2].sum()
             check(gz[:, 10:20], want, rounding(want, dtype) + 8 * U)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype,M", [(F32, 273), (BF, 452)])
+def test_gradients_of_rows_whose_stores_are_slow(B, dtype, M, rest):  # noqa: F811
+    """Rows in shared memory that fill their places there, and whose pitch is a large power of two: stores wait, and the copies of the rows that follow are not to
+    overtake the last reading of a row."""
+    V = 131072
+    z = logits(M, V, dtype, 35)
+    ids, t = teacher(z, 96, 0.7, 4, M, V)
+    gloss = torch.randn(M, device="cuda")
+    check_distill(B, z, ids, t, 0.7, rest, gloss, resident=True)
+    got = []
+    for _ in range(25):
+        gz = torch.empty_like(z)
+        B.patch_distill_loss(z, ids, t, temperature=0.7, rest=rest, gloss=gloss, gZ=gz)
+        got = got[:1] + [gz]
+        assert torch.equal(got[0], got[-1])
