@@ -710,8 +710,8 @@ int patch_distill_loss(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int
                        int K, float temperature, int flags, float* loss_dev, float* stats_dev, const float* gloss_dev,
                        void* gZ_dev, int64_t ldg, int* status_dev, void* stream);
 
-/* The gradient by itself, for a gloss that is known only later: from the stats of the forward call, with p as exact as
- * its lse as above.  gZ_dev is not Z_dev (PATCH_ERR_SHAPE). */
+/* The gradient by itself, for a gloss that is known only later: from the stats of the forward call (same lists, flags and temperature), as exact as beside
+ * the loss.  gZ_dev is not Z_dev (PATCH_ERR_SHAPE). */
 int patch_distill_loss_backward(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int64_t V, const int32_t* ids_dev,
                                 const float* t_dev, int K, float temperature, int flags, const float* stats_dev,
                                 const float* gloss_dev, void* gZ_dev, int64_t ldg, int* status_dev, void* stream);

@@ -770,7 +770,7 @@ struct Distill {
     const int32_t* ids;
     const float* t;
     float* loss;
-    float* stats;                            // [M][2]: ln sum exp of the row, ln p_rest
+    float* stats;                            // [M][2]: maximum and sum of the elements that are not listed (all, where the teacher is renormalised)
     const float* gloss;
     int* status;
 };
@@ -875,7 +875,7 @@ __device__ __forceinline__ RowResult finish_row(const Distill& p, int64_t m, con
         const float ref = listed.m == -INFINITY ? 0.0f : listed.m;
         const float ce = none ? (q_sum == 0.0f ? 0.0f : q_sum * INFINITY) : q_sum * f.ln - (a + q_sum * (ref - f.base)) / p.temperature;
         p.loss[m] = ce + (q_rest > 0.0f ? -q_rest * (none ? -INFINITY : ln_rest) : 0.0f);
-        if (p.stats) { p.stats[2 * m] = none ? -INFINITY : f.base / p.temperature + f.ln; p.stats[2 * m + 1] = ln_rest; }
+        if (p.stats) { p.stats[2 * m] = x.m; p.stats[2 * m + 1] = x.s; }
     }
     f.g = p.gloss ? p.gloss[m] / p.temperature : 1.0f / p.temperature;
     f.zero = f.g == 0.0f || none;
@@ -1337,17 +1337,23 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(const T* z, T* g
     T* const to = gz + m * p.ldg;
     float q_sum;
     const Entry e = entry_of<T, REST>(p, m, row.z, q_sum, sh);
-    const float g = p.gloss ? p.gloss[m] / p.temperature : 1.0f / p.temperature, lse = p.stats[2 * m], ln_rest = REST ? p.stats[2 * m + 1] : 0.0f;
-    if (g == 0.0f || lse == -INFINITY) {
+    // the forward call's sums, of which the listed ones are made again: from lse and p_rest as numbers of 32 bits the probabilities would be off by their size,
+    // and not be numbers where the columns that are not listed are masked by the type's lowest value
+    const Sums x = {p.stats[2 * m], p.stats[2 * m + 1], 0.0f};
+    Sums listed = {-INFINITY, 0.0f, 0.0f};
+    if (REST) {
+        if (e.first) listed = Sums{fmaxf(e.x, -INFINITY), e.x == -INFINITY ? 0.0f : 1.0f + (e.x - e.x), 0.0f};           // NaN and +inf: NaN
+        listed = sum_up(listed, p.c, sh, 1);
+    }
+    const RowResult f = finish_row<REST>(p, m, x, listed, q_sum, 0.0f, false);
+    if (f.zero) {
         write_zeros(row, to);
         return;
     }
-    const float q_rest = REST ? fmaxf(1.0f - q_sum, 0.0f) : 0.0f, q_all = q_sum + q_rest;
-    const bool none = ln_rest == -INFINITY;                        // everything is listed, or masked
     Batch<T> ahead;
     row.fetch(ahead, 0);
-    write_gradient(row, ahead, to, none ? 0.0f : (lse + ln_rest) * p.temperature, p.c, none ? 0.0f : g * (q_all * expf(ln_rest) - q_rest), e,
-                   g * (q_all * expf(e.x / p.temperature - lse) - e.q_all), p.parts, part, [](Batch<T>&) {});
+    write_gradient(row, ahead, to, x.m == -INFINITY ? 0.0f : x.m, p.c, f.factor, e, f.g * (f.q_total * expf((e.x - f.base) / p.temperature - f.ln) - e.q_all), p.parts, part,
+                   [](Batch<T>&) {});
 }
 
 // CTAs that share a row.  A row is shared (and read by a cluster, which joins its sums in distributed shared memory) where

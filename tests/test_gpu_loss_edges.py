@@ -130,3 +130,59 @@ def test_gradients_of_rows_whose_stores_are_slow(B, dtype, M, rest):  # noqa: F8
         B.patch_distill_loss(z, ids, t, temperature=0.7, rest=rest, gloss=gloss, gZ=gz)
         got = got[:1] + [gz]
         assert torch.equal(got[0], got[-1])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("T", [1.0, 50.0])
+@pytest.mark.parametrize("M,V", [(12, 300), (12, 40000), (460, 20000)])
+def test_students_masked_by_the_lowest_value(B, dtype, rest, T, M, V):  # noqa: F811
+    """Columns masked by the type's lowest value: all but the listed ones, all but some of them, all of a row.  The gradient in a launch of its own is as exact as the one beside
+    the loss."""
+    K = 20
+    z, low = logits(M, V, dtype, 6, scale=3.0 * T), torch.finfo(dtype).min
+    ids, t = teacher(z, K, T, 4, M, V)
+    own = torch.gather(z, 1, ids.long())
+    z[1::5] = low
+    z[1::5] = z[1::5].scatter(1, ids[1::5].long(), own[1::5])     # the listed ones are left
+    z[2::5] = low
+    z[2::5] = z[2::5].scatter(1, ids[2::5, : K // 2].long(), own[2::5, : K // 2])
+    z[3::5] = low                                                 # nothing is: an even distribution
+    z[4::5, : V // 2] = low
+    gloss = torch.randn(M, device="cuda")
+    # differences first: beside values of 3e38 even 64 bits leave nothing of a logarithm
+    x, inside = z.to(F64), torch.zeros(M, V, dtype=torch.bool, device="cuda").scatter_(1, ids.long(), True)
+    p = torch.softmax((x - x.amax(-1, keepdim=True)) / T, -1)
+    q = t.to(F64).exp() if rest else torch.softmax(t.to(F64), -1)
+    want, size = p - torch.zeros_like(p).scatter_(1, ids.long(), q), p + torch.zeros_like(p).scatter_(1, ids.long(), q)
+    if rest:
+        q_r = 1 - q.sum(-1, keepdim=True)
+        out = x.masked_fill(inside, -math.inf)
+        w = torch.softmax((out - out.amax(-1, keepdim=True)) / T, -1)
+        p_r = p.masked_fill(inside, 0.0).sum(-1, keepdim=True)
+        want, size = torch.where(inside, want, w * (p_r - q_r)), torch.where(inside, size, w * (p_r + q_r))
+    g = gloss.to(F64)[:, None] / T
+    stats, fused = torch.empty(M, 2, device="cuda"), torch.empty(M, (V + 7) // 8 * 8, dtype=dtype, device="cuda")[:, :V]
+    loss = B.patch_distill_loss(z, ids, t, temperature=T, rest=rest, stats=stats, gloss=gloss, gZ=fused)
+    assert not bool(loss.isnan().any())
+    rel = 4 * (V / 512 + 64 + 3 * 60) * U + 300 * U               # as in check_distill, ordinary logits over T at most 15 in size
+    left = (4 + K) * U * torch.where(inside, p, w) if rest else 0.0
+    for gz in (fused, B.patch_distill_loss_backward(z, ids, t, stats, gloss=gloss, temperature=T, rest=rest)):
+        check(gz, want * g, (rel * size + left) * g.abs() + rounding(want * g, dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rest", [False, True])
+def test_gradient_in_a_launch_of_its_own_of_cold_rows(B, dtype, rest):  # noqa: F811
+    """Logits of tens of thousands over the temperature: probabilities are as exact as beside the loss."""
+    M, V, K, T = 7, 3001, 16, 1e-4
+    z = logits(M, V, dtype, 5, scale=1e-4) + 8.0
+    pad = torch.zeros(M, 3008, dtype=dtype, device="cuda")[:, :V]
+    pad.copy_(z)
+    if dtype is F32:
+        pad += 1e-4 * torch.randn(M, V, device="cuda")
+    ids, t = teacher(pad, K, T, 4, M, V)
+    stats, fused = torch.empty(M, 2, device="cuda"), torch.empty(M, 3008, dtype=dtype, device="cuda")[:, :V]
+    B.patch_distill_loss(pad, ids, t, temperature=T, rest=rest, stats=stats, gZ=fused)
+    alone = B.patch_distill_loss_backward(pad, ids, t, stats, temperature=T, rest=rest)
+    assert float((alone.double() - fused.double()).abs().max() * T) <= 2.0 ** -18 + (2.0 ** -8 if dtype is BF else 0.0)
