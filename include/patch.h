@@ -674,8 +674,8 @@ int patch_token_logprobs(const void* Z_dev, int64_t ldz, int dtype, int64_t M, i
  *     gz_v = (1 / T) [ glogp (1[v = token] - p_v) - gentropy p_v (ln p_v + entropy) ]
  *   glogp_dev    fp32 [M] or NULL; with it tokens_dev as in the forward call (rows that do not count have no gradient from it)
  *   gentropy_dev fp32 [M] or NULL; with it entropy_dev, the forward call's
- *   lse_dev      the forward call's.  It is an fp32 number: p is off by |lse| 2^-23 of itself (a row of nothing but the type's lowest value
- *                has an lse that says no more)
+ *   lse_dev      the forward call's.  It is an fp32 number: p is off by |lse| 2^-23 of itself.  Rows where it is beyond +-2^15 (cold ones, and those of
+ *                nothing but the type's lowest value) are read once more for their sums instead, each by one CTA
  *   gZ_dev       same type as Z; may be Z_dev itself with the same pitch.  Rows whose two factors are 0 become 0, whatever their logits.
  */
 int patch_token_logprobs_backward(const void* Z_dev, int64_t ldz, int dtype, int64_t M, int64_t V, const int64_t* tokens_dev,

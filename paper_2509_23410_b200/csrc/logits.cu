@@ -715,9 +715,35 @@ struct LogProbsGrad {
     int* status;
 };
 // gz = p (a + b (ln p + H)) + (v is the token) glogp / T,  a = -glogp / T,  b = -gentropy / T
+// A row whose lse says too little of its probabilities (beside a maximum over T of kCoarse its last bit is 2^-8, half a step of bf16; beside the type's lowest value nothing of a sum
+// is left), by one CTA: its maximum and sum once more, then the gradient.  (Not in line: for the registers of the others.)
+constexpr float kCoarse = 32768.0f;
 template <class T, bool ENTROPY>
-__global__ void __launch_bounds__(kThreads) logprobs_grad_kernel(const T* z, T* gz, const LogProbsGrad p) {
+__device__ __noinline__ void coarse_row(const T* z, T* g, int V, float c, float up, float b, float h, int64_t token, Shared* sh) {
     constexpr int N = Vec<T>::N;
+    const Row<T> row(z, V, 0, 1);
+    Batch<T> ahead;
+    row.fetch(ahead, 0);
+    const Sums x = sum_up(scan_row<T, false, false, false>(row, ahead, c, nullptr, Cells{}, [](Batch<T>&) {}), c, *sh, 1);
+    const bool none = x.m == -INFINITY && !(x.s != x.s);
+    const float base = x.m == -INFINITY ? 0.0f : x.m, ln = logf(x.s);
+    for (int v = row.first; v < row.count; v += row.step) {
+        const Vec<T> own = row.load(v);
+        float y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float e = (element(own, i) - base) * c, q = ex2(e) / x.s;
+            y[i] = none ? 0.0f : ENTROPY ? q * (b * (fmaf(fmaxf(e, kFar), kLn2, h) - ln) - up) : q * -up;
+            if (!none && int64_t(v) * N + i == token) y[i] += up;
+        }
+        row.store(g, v, y);
+    }
+}
+// (Four CTAs an SM: 4096 x 50257 bf16 with entropies 161 -> 145 us, fp32 as before.)
+template <class T, bool ENTROPY>
+__global__ void __launch_bounds__(kThreads, 4) logprobs_grad_kernel(const T* z, T* gz, const LogProbsGrad p) {
+    constexpr int N = Vec<T>::N;
+    __shared__ Shared sh;
     const int64_t m = blockIdx.x / p.parts;
     const Row<T> row(z + m * p.ldz, p.V, int(blockIdx.x - m * p.parts), p.parts);
     T* const g = gz + m * p.ldg;
@@ -727,12 +753,16 @@ __global__ void __launch_bounds__(kThreads) logprobs_grad_kernel(const T* z, T* 
         token = -1;
     }
     const float lse = p.lse[m], up = token >= 0 ? p.glogp[m] / p.temperature : 0.0f, b = ENTROPY ? -p.gentropy[m] / p.temperature : 0.0f;
-    if (lse == -INFINITY || (up == 0.0f && b == 0.0f)) {           // nothing is asked of the row, or it has no distribution: zeros whatever it holds
+    if (up == 0.0f && b == 0.0f) {                                 // nothing is asked of the row: zeros whatever it holds
         const float zero[N] = {};
         for (int v = row.first; v < row.count; v += row.step) row.store(g, v, zero);
         return;
     }
     const float base = lse * p.temperature, h = ENTROPY ? p.entropy[m] : 0.0f, a = -up;
+    if (fabsf(lse) > kCoarse) {                                    // a row without a distribution among them
+        if (blockIdx.x == m * p.parts) coarse_row<T, ENTROPY>(row.z, g, p.V, p.c, up, b, h, token, &sh);      // (the others' parts too: gZ may be Z)
+        return;
+    }
     const int tv = token >= 0 ? int(token) / N : -1;
     auto one = [&](int v, const Vec<T>& x) {
         float y[N];

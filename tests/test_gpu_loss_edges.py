@@ -186,3 +186,43 @@ def test_gradient_in_a_launch_of_its_own_of_cold_rows(B, dtype, rest):  # noqa: 
     B.patch_distill_loss(pad, ids, t, temperature=T, rest=rest, stats=stats, gZ=fused)
     alone = B.patch_distill_loss_backward(pad, ids, t, stats, temperature=T, rest=rest)
     assert float((alone.double() - fused.double()).abs().max() * T) <= 2.0 ** -18 + (2.0 ** -8 if dtype is BF else 0.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [1.0, 0.7, 50.0, 1e-4])
+@pytest.mark.parametrize("V", [9, 3000, 50257])
+def test_gradient_of_rows_whose_lse_says_too_little(B, dtype, T, V):  # noqa: F811
+    """Rows of nothing but the type's lowest value (an even distribution), cold ones, and ordinary ones and rows without a distribution among them; in place too."""
+    M = 9
+    z = logits(M, V, dtype, 6, extra=8)
+    z[1::4], z[2::4, V // 2 :], z[3, :] = torch.finfo(dtype).min, torch.finfo(dtype).min, -math.inf
+    z[6] = torch.finfo(dtype).max                                 # and of nothing but the highest
+    g = torch.Generator(device="cuda").manual_seed(3)
+    tokens = torch.randint(0, V // 2, (M,), generator=g, device="cuda")
+    glogp, gent = (torch.randn(M, generator=g, device="cuda") for _ in range(2))
+    glogp[4], gent[4], tokens[0] = 0.0, 0.0, -1
+    _, ent, lse, _, _ = B.patch_token_logprobs(z, tokens, temperature=T, entropy=True, lse=True)
+    x = z.to(F64)
+    none = (x == -math.inf).all(-1, keepdim=True)
+    x = (x - x.amax(-1, keepdim=True).clamp(min=-4e38)) / T       # differences first: beside 3e38 even 64 bits leave nothing of a logarithm
+    lnp = torch.log_softmax(torch.where(none, 0.0, x), -1)
+    p = torch.where(none, 0.0, lnp.exp())
+    lnp = torch.where(p > 0, lnp, 0.0)
+    hot = torch.zeros(M, V, dtype=F64, device="cuda").scatter_(1, tokens.clamp(min=0)[:, None], (tokens >= 0).to(F64)[:, None])
+    hot = torch.where(none, 0.0, hot)
+    a, h = torch.where(tokens >= 0, glogp, 0.0).to(F64)[:, None], -(p * lnp).sum(-1, keepdim=True)
+    seen = lse.to(F64).abs().clamp(max=32768.0)[:, None] * 2.0 ** -23 + (V / 512 + 64) * U                 # beyond it nothing comes from lse
+    for use in ("logp", "entropy", "both"):
+        ga, ge = (a if use != "entropy" else 0 * a), (gent.to(F64)[:, None] if use != "logp" else 0 * a)
+        want = (ga * (hot - p) - ge * p * (lnp + h)) / T
+        size = (ga.abs() * p + ge.abs() * p * (lnp.abs() + h + 1)) / T
+        kw = dict(temperature=T, **(dict(entropy=ent, gentropy=gent) if use != "logp" else {}))
+        gl = glogp if use != "entropy" else None
+        # logits of size 5 over T: the exponent's product is off by 2^-23 of itself, which is at most 110 where p is not 0
+        tol = 2 * (seen + 110 * 2.0 ** -23) * size + (ga.abs() * hot / T) * 4 * U + rounding(want, dtype)
+        gz = B.patch_token_logprobs_backward(z, tokens, lse, gl, **kw)
+        check(gz, want, tol)
+        same = torch.empty(M, (V + 7) // 8 * 8, dtype=dtype, device="cuda")[:, :V]
+        same.copy_(z)
+        B.patch_token_logprobs_backward(same, tokens, lse, gl, gZ=same, **kw)
+        assert torch.equal(same, gz)
