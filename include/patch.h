@@ -692,6 +692,8 @@ enum { PATCH_DISTILL_REST = 1 };
  *     without PATCH_DISTILL_REST   q_i = exp(t_i) / sum_j exp(t_j),   loss = - sum_i q_i ln p_{id_i}
  *     with PATCH_DISTILL_REST      q_i = exp(t_i),  q_r = max(0, 1 - sum_i q_i),  p_r = sum of p_v over the columns not listed,
  *                                  loss = - sum_i q_i ln p_{id_i} - q_r ln p_r
+ *                                  q_r is an fp32 difference, off by up to (4 + K) 2^-24.  Where the columns that are not listed are masked (all
+ *                                  -inf, or ln p_r < -10^6), a q_r below 2^-15 counts as 0; a larger one makes the loss infinite (as large)
  * patch_token_logprobs of the teacher's logits at the same temperature writes such lists (its log probabilities serve both forms).  One entry of
  * log probability 0 per row is the ordinary cross entropy.
  *   ids_dev      int32 [M x K], 1 <= K <= 256; negative: no entry.  Entries with one id add up.  A row without entries (or with

@@ -40,6 +40,7 @@ constexpr size_t kListBytes = kCandidates * sizeof(uint64_t) + kFound * sizeof(u
 constexpr int kMaxParts = 8;                 // CTAs of a cluster that share a row (sixteen: 16 rows of 128256 7.2 us instead of 5.6, top 20 15.3 instead of 11.4)
 constexpr int64_t kL2Share = 24 << 20;       // see launch_resident
 constexpr int64_t kMaxV = int64_t(1) << 20;  // a bit per element fits shared memory
+constexpr float kNoRest = 3.05e-5f;          // 2^-15: up to 256 exponentials of fp32 log probabilities, each off by 2^-22, and their sum's 2^-16
 constexpr float kLn2 = 0.693147180559945f;
 constexpr float kFar = -256.0f;              // an exponent from here on down is as good as -inf, 2^x is 0; factors and sums times it stay numbers
 static_assert(kMost <= kThreads && kMaxParts * kMost <= kCandidates, "an entry for a thread; lists of all parts of a row fit the candidates");
@@ -899,7 +900,10 @@ __device__ __forceinline__ RowResult finish_row(const Distill& p, int64_t m, con
     const bool none = all.m == -INFINITY && !(all.s != all.s);              // every element is -inf: no distribution
     f.ln = logf(all.s);
     f.base = all.m == -INFINITY ? 0.0f : all.m;
-    const float q_rest = REST ? fmaxf(1.0f - q_sum, 0.0f) : 0.0f;
+    float q_rest = REST ? fmaxf(1.0f - q_sum, 0.0f) : 0.0f;
+    // Nothing but masked columns (-inf, the type's lowest value, -10^9) is left to the student: then what rounding has left of a list that sums to 1 is nothing, and not an
+    // infinite loss.
+    if (REST && ln_rest < -1e6f && q_rest < kNoRest) q_rest = 0.0f;
     f.q_total = q_sum + q_rest;
     if (write) {
         const float ref = listed.m == -INFINITY ? 0.0f : listed.m;

@@ -226,3 +226,29 @@ def test_gradient_of_rows_whose_lse_says_too_little(B, dtype, T, V):  # noqa: F8
         same.copy_(z)
         B.patch_token_logprobs_backward(same, tokens, lse, gl, gZ=same, **kw)
         assert torch.equal(same, gz)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("mask", [-math.inf, "lowest", -1e9])
+@pytest.mark.parametrize("M,V,K", [(20, 300, 12), (20, 40000, 256), (460, 20000, 40)])
+def test_lists_that_cover_all_that_a_mask_leaves(B, dtype, mask, M, V, K):  # noqa: F811
+    """Teacher and student have the same few columns left, all of them listed: the rest is nothing, whatever rounding makes of the list's sum.  A rest that is
+    more than rounding has no place: the loss is infinite."""
+    z, full = logits(M, V, dtype, 6), logits(M, V, F32, 7)
+    left = torch.rand(M, V, device="cuda").topk(K - 3, -1).indices
+    keep = torch.zeros(M, V, dtype=torch.bool, device="cuda").scatter_(1, left, True)
+    z[~keep], full[~keep] = torch.finfo(dtype).min if mask == "lowest" else mask, -math.inf
+    *_, ids, t = B.patch_token_logprobs(full, k=K)                # the last three entries: probability 0
+    gz = torch.empty(M, (V + 7) // 8 * 8, dtype=dtype, device="cuda")[:, :V]
+    stats = torch.empty(M, 2, device="cuda")
+    loss = B.patch_distill_loss(z, ids, t, rest=True, stats=stats, gZ=gz)
+    q, lnp = t.to(F64).exp(), torch.log_softmax(z.to(F64), -1)
+    want = -torch.where(q > 0, q * lnp.gather(1, ids.long()), 0.0).sum(-1)
+    check(loss, want, 2 * ln_tol(z, V, 1.0) + 300 * U * want)
+    p = lnp.exp()
+    hot = torch.zeros_like(p).scatter_(1, ids.long(), q)
+    for g in (gz, B.patch_distill_loss_backward(z, ids, t, stats, rest=True)):
+        check(g, p - hot, 4 * (ln_tol(z, V, 1.0)[:, None] + 300 * U) * (p + hot) + rounding(p - hot, dtype))
+    t[:, 0] -= 0.1
+    loss = B.patch_distill_loss(z, ids, t, rest=True, gZ=gz)
+    assert bool((loss > 1e4).all()) and not bool(gz.isnan().any()) and (mask != -math.inf or bool((loss == math.inf).all()))
