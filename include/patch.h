@@ -613,7 +613,8 @@ int patch_prefix_attention(const patch_kv_cache_t* cache, const void* Q_dev, int
  *     s_ij = q_i . k_j (j <= i),   O_i = sum_j softmax_j(scale s_ij) v_j,   lse_i = ln sum_j exp(scale s_ij).
  * Query head h reads key head h / (Hq / Hkv).  Sequences may be of any length, 0 and 1 included; rows before the first and behind the last one
  * are neither read into a result nor written.  Values of a sequence are assumed finite; whatever the rows of other sequences and
- * around them hold shows in no result of it.
+ * around them hold shows in no bit of its results.  Scores, sums and lse are fp32; probabilities are rounded to bf16 for their product with V (the sum that
+ * divides takes them unrounded), results once: |O| is off by up to 2^-8 of sum p |v| and of itself.
  *   Q_dev, O_dev  [M x Hq heads of D], pitches ldq, ldo;  K_dev, V_dev [M x Hkv heads of D], pitches ldk, ldv;  D = 64 or 128, Hq a multiple of Hkv, at
  *                 most 4096;  pitches at most 2^28;  O overlaps no input
  *   starts_dev    int32 [B + 1], 0 <= starts[0] <= .. <= starts[B] <= M, in device memory: a captured launch follows it.  B <= 2^20
@@ -630,7 +631,7 @@ int patch_sequence_attention(const void* Q_dev, int64_t ldq, const void* K_dev, 
  * Gradient of patch_sequence_attention, from its inputs and results.  With p_ij = exp(scale s_ij - lse_i), delta_i = gO_i . O_i:
  *     gs_ij = scale p_ij (gO_i . v_j - delta_i),   gQ_i = sum_j gs_ij k_j,   gK_j = sum_i gs_ij q_i,   gV_j = sum_i p_ij gO_i,
  * gK and gV summed over the query heads of a key head too.  Products take p and gs rounded to bf16; lse is an fp32 number, so that p is off by
- * |lse| 2^-23 of itself.
+ * |lse| 2^-23 of itself (scores beyond some 2^20 have no gradient worth the name).
  *   gQ_dev [M x Hq heads], gK_dev, gV_dev [M x Hkv heads]: results, column ranges of one stacked gradient if wanted; they overlap no input.
  *                 Rows outside the sequences stay as they are.
  *   workspace_dev at least patch_sequence_attention_backward_workspace_size bytes, 256-byte aligned, no initialisation needed
@@ -648,9 +649,10 @@ int patch_sequence_attention_backward(const void* gO_dev, int64_t ldgo, const vo
  * Logits are rows of V values, bf16 or fp32, with a pitch (ld) that is a multiple of 8 elements; columns from V on are neither
  * read nor written.  1 <= V <= 2^20, M < 2^31.  Arithmetic, sums and results other than gradients (which have the logits' type and are rounded
  * once) are fp32; sums are taken in an order that depends on the arguments only: equal calls give equal bits.  The distribution of a row z is
- * p = softmax(z / temperature), 0 < temperature < inf (and its reciprocal an fp32 number).  Logits of -inf are masked: probability 0,
- * gradient 0, unless the column is the row's token, or listed with a probability: then the loss is infinite and the gradient what the formulas give
- * with p = 0 (1 / T of glogp, - gloss q_i / T).  A row of nothing but -inf has no distribution: lse and log probabilities -inf, entropy 0, gradients 0.  NaN or +inf in a
+ * p = softmax(z / temperature), 0 < temperature < inf (and its reciprocal an fp32 number; results beyond fp32, as the lse of a cold row may be, are
+ * infinite).  Logits of -inf are masked: probability 0, gradient 0, unless the column is the row's token, or listed with a probability: then
+ * the loss is infinite and the gradient what the formulas give with p = 0 (1 / T of glogp, - gloss q_i / T).  A row of nothing but -inf has no
+ * distribution: lse and log probabilities -inf, entropy 0, gradients 0.  NaN or +inf in a
  * row makes that row's results NaN and no other's.  The launches are ordinary ones in the sense of the section above.
  * ========================================================================================= */
 enum { PATCH_LOGITS_BF16 = 0, PATCH_LOGITS_F32 = 1 };
@@ -701,8 +703,9 @@ enum { PATCH_DISTILL_REST = 1 };
  *   t_dev        fp32 [M x K]
  *   loss_dev     fp32 [M]
  *   stats_dev    NULL or fp32 [M x 2], what the gradient's own call reads
- *   gZ_dev       NULL, or the gradient of sum_m gloss[m] loss[m] in the same launch (the logits are read from HBM once): same type as
- *                Z, pitch ldg; may be Z_dev itself with the same pitch.  Rows with gloss = 0 become 0, whatever their logits.  (The loss
+ *   gZ_dev       NULL, or the gradient of sum_m gloss[m] loss[m] in the same launch (the logits are read from HBM once, but for batches that L2 does not
+ *                hold of rows beyond 131072 fp32 or 262144 bf16 columns, which are read twice): same
+ *                type as Z, pitch ldg; may be Z_dev itself with the same pitch.  Rows with gloss = 0 become 0, whatever their logits.  (The loss
  *                beside a gradient may differ in its last bits from the loss by itself: its sums have another order.)
  *   gloss_dev    fp32 [M], NULL: all 1
  *   status_dev   PATCH_ERR_SIZE if an id is V or more (no entry then); PATCH_ERR_TIMEOUT as for the other kernels with bounded waits

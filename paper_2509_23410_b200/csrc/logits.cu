@@ -17,8 +17,8 @@
 //
 // What bounds it, with the rates measured: reads of HBM, 7.1 TB/s with fp32 logits, or 4.8 with bf16 ones, whose element costs as many instructions for
 // half the bytes.  4095 x 128256 fp32 296 us, with the top 64 395; log probabilities of 8192 x 32000 bf16 110; 61 x 151936 bf16 with entropies and the top 8 13.4, one row
-// of 128256 with the top 20 11, which are latencies of the steps behind the pass.  Gradient of 4096 x 50257 bf16 158 us (5.2 TB/s read and written).  Distillation
-// with its gradient: 509 x 32000 fp32 27 us, 8192 x 128256 bf16 908 (4.6 TB/s read and written).
+// of 128256 with the top 20 11, which are latencies of the steps behind the pass.  Gradient of 4096 x 50257 bf16 150 us (5.4 TB/s read and written).  Distillation
+// with its gradient: 509 x 32000 fp32 27 us, 8192 x 128256 bf16 918 (4.6 TB/s read and written).
 #include <math.h>
 #include "patch_internal.cuh"
 #include "sm100_ptx.cuh"
